@@ -386,11 +386,172 @@ un_status un_profile_enable(un_ctx* ctx, int32_t enable);
  * of one kernel class. Waits for the stream. */
 un_status un_profile_read(un_ctx* ctx, int32_t kernel_class, double* total_ms, int64_t* launches);
 
+/* ---------------------------------------------------------------------------
+ * Operators on device tensors. A context's step runs the same kernels for its
+ * UN_RMS_NORM and UN_GATED_RECURRENCE layers and its 8-bit AdamW models; these
+ * calls are for a program's own tensors.
+ *   - Pointers are device memory of one device; the call is enqueued on
+ *     `stream` (a hipStream_t of that device, NULL: the current device's default
+ *     stream) and returns without waiting. It runs on the stream's device, also
+ *     when another one is current, and leaves the current device as it is.
+ *   - Nothing is allocated and nothing is kept between calls but what the
+ *     caller passes: calls on different streams do not disturb one another as
+ *     long as their outputs and workspaces differ. All may be captured into a
+ *     HIP graph, except un_adamw_step.
+ *   - Strides are in elements; the innermost stride is 1. Tensors need their
+ *     element's alignment, no more.
+ *   - Errors are read with un_last_error(NULL) on the calling thread. A refused
+ *     call enqueues nothing.
+ * ------------------------------------------------------------------------- */
+typedef enum { UN_TYPE_F32 = 0, UN_TYPE_BF16 = 1 } un_type;
+
+/* RMS norm of `rows` rows of `width` values (1 <= width <= 16384), with the
+ * addition of a residual before it:
+ *   s = x + residual, rounded to the type (s = x without a residual),
+ *   q = 1 / sqrt(mean(s^2) + eps),  y = s * q * weight.
+ * 8 bits (scale not NULL): y holds e4m3 codes (OCP, largest value 448) with one
+ * scale per row, scale = max(max|s q weight|, 1e-30) / 448, code = nearest e4m3
+ * to s q weight / scale. sum may be x or residual itself (same stride). */
+typedef struct {
+  int32_t type;              /* un_type of x, residual, sum, y */
+  int32_t width;
+  int64_t rows;
+  float eps;                 /* >= 0 */
+  const void* x;
+  int64_t ldx;
+  const void* residual;      /* NULL: none */
+  int64_t ldr;
+  const float* weight;       /* [width] */
+  void* sum;                 /* NULL: not stored */
+  int64_t lds;
+  void* y;                   /* 8 bits: one byte per value */
+  int64_t ldy;
+  float* rstd;               /* [rows], NULL: not stored; un_rms_norm_backward reads it */
+  float* scale;              /* [rows], NULL: y in the type; else y in 8 bits */
+} un_rms_norm_args;
+un_status un_rms_norm(const un_rms_norm_args* a, void* stream);
+
+/* Its gradients, from dy at y, the stored sum s and rstd:
+ *   dx = ds + q (dy w - s q mean(dy w s q)) at x and at the residual alike
+ *   (ds: the gradient that reaches s on other ways; NULL: none), and
+ *   dweight = sum over the rows of dy s q (in a fixed order).
+ * dx may be ds or dy itself (same stride). workspace: as many bytes as
+ * un_rms_norm_workspace says. */
+typedef struct {
+  int32_t type;              /* of dy, s, ds, dx */
+  int32_t width;
+  int64_t rows;
+  const void* dy;
+  int64_t lddy;
+  const void* s;
+  int64_t lds;
+  const float* weight;
+  const float* rstd;
+  const void* ds;
+  int64_t ldds;
+  void* dx;                  /* NULL: not wanted */
+  int64_t lddx;
+  float* dweight;            /* [width], overwritten */
+  void* workspace;
+  size_t workspace_bytes;
+} un_rms_norm_grad_args;
+un_status un_rms_norm_backward(const un_rms_norm_grad_args* a, void* stream);
+un_status un_rms_norm_workspace(int32_t type, int64_t rows, int32_t width, size_t* bytes);
+
+/* Gated linear recurrence, per sequence and channel:
+ *   a_t = sigmoid(gate_t),  h_t = a_t h_{t-1} + (1 - a_t) value_t,  t = 1 .. tokens.
+ * gate and value are [batch][tokens][width] with the same strides (the two halves
+ * of one projection, say); the state is fp32. lens (device int32 [batch], NULL:
+ * all of `tokens`): steps at and behind a sequence's length (clamped to [0,
+ * tokens]) are skipped: their rows of gate and value are not used, their rows of
+ * h are written as zeros, and the last state is the one before them. A single
+ * token is a call with tokens = 1; last may be start itself.
+ * states: for the backward pass, un_gated_scan_states floats. */
+typedef struct {
+  int32_t type;              /* un_type of gate, value, h */
+  int32_t batch, tokens, width;
+  const void *gate, *value;
+  int64_t ld_in, seq_in;     /* strides of a token and of a sequence */
+  const int32_t* lens;
+  const float* start;        /* [batch][width], NULL: zeros */
+  void* h;
+  int64_t ld_h, seq_h;
+  float* last;               /* [batch][width], NULL: not wanted */
+  float* states;             /* NULL: no backward pass will follow */
+  void* workspace;
+  size_t workspace_bytes;
+} un_gated_scan_args;
+un_status un_gated_scan(const un_gated_scan_args* a, void* stream);
+
+/* Its gradients, from dh at h (rows behind a sequence's length are not used) and
+ * dlast at the last state (NULL: zeros), with `states` of the forward call and the
+ * same gate, value and lens: dgate and dvalue (zeros behind a sequence's length;
+ * same strides) and dstart, the gradient at the start state (NULL: not wanted).
+ * dgate / dvalue must not overlap the inputs. */
+typedef struct {
+  int32_t type;
+  int32_t batch, tokens, width;
+  const void *gate, *value;
+  int64_t ld_in, seq_in;
+  const int32_t* lens;
+  const float* states;
+  const void* dh;
+  int64_t ld_dh, seq_dh;
+  const float* dlast;
+  void *dgate, *dvalue;
+  int64_t ld_out, seq_out;
+  float* dstart;
+  void* workspace;
+  size_t workspace_bytes;
+} un_gated_scan_grad_args;
+un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream);
+/* Floats of `states`, and bytes of the workspace of either call (may be 0). */
+un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size_t* states, size_t* workspace_bytes);
+
+/* AdamW (decoupled weight decay) over many tensors in one launch. Per element,
+ * fp32, at step t = 1, 2, ...:
+ *   m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
+ *   w <- (1 - lr decay) w - (lr / (1 - beta1^t)) m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
+ * Weights are fp32, gradients fp32 or bf16 (one type for all tensors); copy, where
+ * not NULL, receives the new weights in bf16.
+ * 32 bits: m and v are fp32. 8 bits: m and u = sqrt(v) are e4m3 codes, with a
+ * power-of-two scale (e8m0: the byte b stands for 2^(b - 127)) per 256
+ * consecutive elements of a tensor, the least with which the block's largest
+ * magnitude is at most 448. Each new value is rounded up or down to a neighbouring
+ * code with the probability of its distance to the other (a moving average whose
+ * steps are smaller than the codes' distance would not move otherwise), from
+ * random numbers made of `key` and the element's number, so that a step with
+ * another key rounds independently; a u that is not 0 never becomes 0. A fresh
+ * state is zeros everywhere (codes, scales). */
+typedef struct {
+  float* weight;
+  const void* grad;
+  uint16_t* copy;
+  void *m, *v;               /* fp32, or one byte per element */
+  uint8_t *m_scale, *v_scale;/* 8 bits: ceil(elements / 256) bytes; else NULL */
+  int64_t elements;
+} un_adamw_tensor;
+typedef struct un_adamw un_adamw;
+/* A plan of the step over these tensors (n >= 1; elements may be 0), on the
+ * current device. It holds their addresses, not their data: they stay the caller's. */
+un_status un_adamw_create(const un_adamw_tensor* tensors, int32_t n, int32_t grad_type, int32_t state_bits, un_adamw** out);
+/* One step. lr and decay are finite and >= 0, lr * decay < 1, beta1 and beta2 in
+ * [0, 1), eps > 0, t >= 1. The rates and the count travel with the call, so a
+ * captured one would repeat its step: refused under capture (UN_ERR_UNSUPPORTED). */
+typedef struct {
+  double lr, beta1, beta2, eps, decay;
+  int64_t t;
+  uint32_t key;              /* 8 bits: of the rounding's random numbers; another one each step */
+} un_adamw_hyper;
+un_status un_adamw_step(un_adamw* plan, const un_adamw_hyper* h, void* stream);
+/* Waits for the device's work, then frees the plan. NULL is accepted. */
+void un_adamw_destroy(un_adamw* plan);
+
 /* Free the context and its arena. NULL is accepted. */
 void un_destroy(un_ctx* ctx);
 
-/* Message of the last failed call on ctx (or of the last failed un_create when
- * ctx is NULL). Never NULL; owned by the library. */
+/* Message of the last failed call on ctx (or of the last failed un_create or
+ * operator call when ctx is NULL). Never NULL; owned by the library. */
 const char* un_last_error(const un_ctx* ctx);
 
 #ifdef __cplusplus

@@ -1,0 +1,126 @@
+// Descriptors and launch plans of the operators on device tensors (RMS norm,
+// gated linear recurrence, multi-tensor AdamW), shared by their kernels
+// (operators.hip), their C entries (op_api.cpp) and the step's planner
+// (un_api.cpp), which runs the same kernels over tables of problems.
+#pragma once
+#include <stdint.h>
+
+#include <hip/hip_runtime.h>
+
+#include "../../include/unifiednn.h"
+
+namespace un {
+
+// Records the message of a failed call without a context (un_last_error(NULL)).
+un_status fail_call(un_status s, const char* msg);
+
+// ---------------------------------------------------------------------------
+// RMS norm of rows of d values:  s = x + r (rounded to the type),
+// q = 1 / sqrt(mean(s^2) + eps),  y = s q w.
+// Backward: dx = ds + q (dy w - s q mean(dy w s q)), dw = sum over rows of dy s q.
+// A row belongs to `tpr` threads, each holding up to NORM_REGS of its values in
+// registers, so every operand is read once.
+// ---------------------------------------------------------------------------
+struct NormProb {
+  const void* x;       // forward: input; backward: the stored sum s
+  const void* r;       // forward: residual (null: none); backward: the gradient ds at s from elsewhere (null: none)
+  const void* dy;      // backward
+  const float* w;
+  void* s;             // forward: the sum (null: not stored)
+  void* y;             // forward: output; backward: dx (null: not wanted)
+  float* rstd;         // forward: q per row (null: not stored); backward: read
+  float* scale;        // forward, e4m3: scale per row
+  float* part;         // backward: partial weight gradients [blocks][d]
+  int64_t ldx, ldr, lddy, lds, ldy;
+  int64_t rows;
+  int32_t d;
+  int32_t mask;        // backward: dx = 0 where s <= 0 (s is a ReLU's output)
+  int32_t blocks;      // backward: workgroups of this problem
+  float eps;
+};
+constexpr int NORM_REGS = 32;            // most values of a row per thread (16 with 1024 threads a row)
+constexpr int NORM_MAX_D = 1024 * NORM_REGS / 2;
+struct NormPlan {
+  int tpr, nv;         // threads per row; 16-byte vectors per thread
+  int group;           // rows of a workgroup at a time
+};
+NormPlan norm_plan(bool bf16, int64_t rows, int d);
+// workgroups of a backward pass over `rows` rows
+int norm_blocks(const NormPlan& p, int64_t rows);
+// One problem (by value), or a table: one (problem, block) pair per workgroup.
+hipError_t launch_norm(bool bf16, bool e4m3, const NormPlan& plan, const NormProb& p, hipStream_t s);
+hipError_t launch_norm_bwd(bool bf16, const NormPlan& plan, const NormProb& p, hipStream_t s);
+hipError_t launch_norm_table(bool bf16, bool bwd, const NormPlan& plan, const NormProb* probs, const int32_t* map, int nblocks,
+                             int64_t wsoff, hipStream_t s);
+// dw[j] = sum over the partials, in order
+hipError_t launch_norm_dw(const float* part, int nparts, int d, float* dw, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// Gated linear recurrence, per channel:  a_t = sigmoid(g_t),
+//   h_t = a_t h_{t-1} + (1 - a_t) v_t.
+// Backward, with e_t the gradient at h_t from all later places:
+//   e_t = dh_t + a_{t+1} e_{t+1},  dv_t = (1 - a_t) e_t,
+//   dg_t = a_t (1 - a_t) e_t (h_{t-1} - v_t),  dh_0 = a_1 e_1.
+// Steps at and behind a sequence's length are the identity (a = 1, input 0);
+// their rows of h, dg and dv are written as zeros.
+// ---------------------------------------------------------------------------
+struct ScanProb {
+  const void *gate, *value;   // [B][T][d], channel stride 1
+  int64_t ldi, bsi;           // strides of a step and of a sequence, in elements (gate and value)
+  const void* dh;             // backward
+  int64_t lddh, bsdh;
+  void *o1, *o2;              // forward: h, -; backward: dg, dv
+  int64_t ldo, bso;
+  const int32_t* lens;        // null: every sequence has T steps
+  const float* start;         // forward: h_0 [B][d]; backward: the gradient at the last state; null: 0
+  float* end;                 // forward: last state [B][d]; backward: dh_0; null: not wanted
+  float* states;              // h at the start of every SCAN_CHUNK steps [B][chunks][d] (forward: written if not null)
+  float* agg;                 // split passes: per segment and channel (A, H), [nseg][B][d][2], then a copy of start [B][d]
+  int32_t B, T, d;
+  int32_t tiles;              // channel tiles
+  int32_t seg, nseg;          // chunks per segment; segments
+};
+constexpr int SCAN_W = 8, SCAN_L = 16;             // waves of a workgroup; steps per wave and chunk
+constexpr int SCAN_CHUNK = SCAN_W * SCAN_L;
+inline int scan_chunks(int T) { return (T + SCAN_CHUNK - 1) / SCAN_CHUNK; }
+struct ScanPlan {
+  int vb;                     // channels per lane
+  int kind;                   // 0: one step, 1: up to SCAN_L steps (one wave), 2: chunks
+  int tiles, seg, nseg;
+};
+inline size_t scan_ws_bytes(const ScanPlan& p, int64_t B, int d) { return p.nseg > 1 ? (size_t)(2 * p.nseg + 1) * B * d * 4 : 0; }
+// pairs: every row of the operands allows loads of two channels at once
+ScanPlan scan_plan(int64_t B, int T, int d, bool pairs);
+hipError_t launch_scan(bool bf16, bool bwd, const ScanPlan& plan, const ScanProb& p, hipStream_t s);
+// table: one (problem, tile * B + sequence) pair per workgroup; every problem nseg == 1
+hipError_t launch_scan_table(bool bf16, bool bwd, int vb, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// AdamW over many tensors. States fp32, or e4m3 codes with a power of two per
+// AW_BLOCK values (8 bits: m and sqrt(v) are stored).
+// ---------------------------------------------------------------------------
+struct AdamwTensor {
+  float* p;
+  const void* g;              // fp32 or bf16
+  uint16_t* copy;             // bf16 copy of p (null: none)
+  void *m, *v;                // fp32, or e4m3 codes
+  uint8_t *ms, *vs;           // e8m0 scales, one per AW_BLOCK values (8 bits)
+  int64_t n;
+  uint32_t base;              // number of the tensor's first value, for the rounding's random numbers
+  int32_t hp;                 // index of the tensor's hyper-parameters
+};
+struct AdamwHp {
+  float decay, lr, b1, b2, c1, c2, isb2, eps;   // as OptHp's Adam, and w <- decay * w first
+};
+constexpr int AW_BLOCK = 256;                   // values per scale
+constexpr int AW_CHUNK = 16 * AW_BLOCK;         // values per workgroup
+// map: (tensor, chunk) per workgroup. hps: device array, or null: `hp` for every tensor.
+hipError_t launch_adamw(bool g16, bool eight, const AdamwTensor* ts, const int32_t* map, int nblocks, const AdamwHp& hp,
+                        const AdamwHp* hps, uint32_t key, hipStream_t s);
+
+// e4m3 (largest finite value 448) on the host, for reading and setting states
+float e4m3_value(uint8_t code);
+uint8_t e4m3_code(float x);                     // nearest, ties to even; |x| > 448 and NaN give NaN
+int scale_exponent(float amax);                 // least e with amax <= 448 * 2^e, in [-127, 127]
+
+}  // namespace un

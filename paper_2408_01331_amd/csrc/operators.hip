@@ -1,0 +1,1191 @@
+// gfx950 (CDNA4) kernels of the operators on device tensors: RMS norm, gated
+// linear recurrence, multi-tensor AdamW. All of them are bound by HBM: each
+// reads its operands once, in 16-byte (norm, AdamW) or whole-line (recurrence)
+// accesses, and keeps everything in between in registers.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "operators.h"
+
+namespace un {
+
+typedef uint16_t bf16_t;
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+// vectors at an element's alignment (rows of any stride): gfx950 takes such
+// global accesses as they are
+typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
+typedef u32x2 u32x2_a1 __attribute__((aligned(1)));
+typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
+typedef uint32_t u32_a1 __attribute__((aligned(1)));
+typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
+
+namespace {
+
+__device__ __forceinline__ float bf2f(uint32_t h) { return __uint_as_float(h << 16); }
+__device__ __forceinline__ uint32_t f2bf(float f) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)f); }
+__device__ __forceinline__ uint32_t f2bf2(float lo, float hi) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
+}
+
+// A 16-byte vector of T as floats and back.
+template <typename T> struct V16;
+template <> struct V16<float> {
+  static constexpr int N = 4;
+  __device__ static void unpack(u32x4 v, float* f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(v[e]);
+  }
+  __device__ static u32x4 pack(const float* f) {
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(f[e]);
+    return v;
+  }
+  __device__ static float round(float f) { return f; }
+  __device__ static float load1(const float* p) { return *p; }
+  __device__ static void store1(float* p, float f) { *p = f; }
+};
+template <> struct V16<bf16_t> {
+  static constexpr int N = 8;
+  __device__ static void unpack(u32x4 v, float* f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f[2 * e] = __uint_as_float(v[e] << 16);
+      f[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+    }
+  }
+  __device__ static u32x4 pack(const float* f) {
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = f2bf2(f[2 * e], f[2 * e + 1]);
+    return v;
+  }
+  __device__ static float round(float f) { return bf2f(f2bf(f)); }
+  __device__ static float load1(const bf16_t* p) { return bf2f(*p); }
+  __device__ static void store1(bf16_t* p, float f) { *p = (bf16_t)f2bf(f); }
+};
+
+// n (0 .. N) values at p; the rest are zeros
+template <typename T> __device__ __forceinline__ void load_vec(const T* p, int n, float* f) {
+  constexpr int N = V16<T>::N;
+  if (n == N) {
+    V16<T>::unpack(*(const u32x4_a2*)p, f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = e < n ? V16<T>::load1(p + e) : 0.f;
+  }
+}
+template <typename T> __device__ __forceinline__ void store_vec(T* p, int n, const float* f) {
+  constexpr int N = V16<T>::N;
+  if (n == N) {
+    *(u32x4_a2*)p = V16<T>::pack(f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < n) V16<T>::store1(p + e, f[e]);
+  }
+}
+template <int N> __device__ __forceinline__ void load_f32(const float* p, int n, float* f) {
+  if (n == N) {
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) {
+      const f32x4 v = ((const f32x4_a4*)p)[q];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[4 * q + e] = v[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = e < n ? p[e] : 0.f;
+  }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+  return v;
+}
+
+// Sum / maximum over the TPR threads of a row (TPR 64: a wave; else the whole
+// workgroup, through `sm`, one float per wave, in wave order). `sm` is free
+// again after the next barrier.
+template <int TPR> __device__ __forceinline__ float row_sum(float v, float* sm) {
+  v = wave_sum(v);
+  if constexpr (TPR > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; ++w) v += sm[w];
+  }
+  return v;
+}
+template <int TPR> __device__ __forceinline__ float row_max(float v, float* sm) {
+  v = wave_max(v);
+  if constexpr (TPR > 64) {
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = sm[0];
+#pragma unroll
+    for (int w = 1; w < TPR / 64; ++w) v = fmaxf(v, sm[w]);
+  }
+  return v;
+}
+
+// ---------------------------------------------------------------------------
+// RMS norm, forward
+// ---------------------------------------------------------------------------
+template <typename T, int TPR, int NV, bool E4M3>
+__device__ __forceinline__ void norm_fwd_row(const NormProb& p, int64_t row, float* sm) {
+  constexpr int N = V16<T>::N;
+  const int t = threadIdx.x & (TPR - 1), d = p.d;
+  const bool live = row < p.rows;  // a wave or workgroup as a whole; it keeps up with the barriers
+  const int64_t at = live ? row : 0;
+  const T* x = (const T*)p.x + at * p.ldx;
+  const T* r = p.r ? (const T*)p.r + at * p.ldr : nullptr;
+  float f[NV][N];
+  int cnt[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * TPR + t) * N;
+    cnt[j] = live ? min(max(d - c, 0), N) : 0;
+    load_vec<T>(x + c, cnt[j], f[j]);
+  }
+  if (r) {
+    float g[NV][N];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) load_vec<T>(r + (j * TPR + t) * N, cnt[j], g[j]);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[j][e] = V16<T>::round(f[j][e] + g[j][e]);  // the norm is that of the stored sum
+  }
+  if (p.s) {
+    T* s = (T*)p.s + at * p.lds;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) store_vec<T>(s + (j * TPR + t) * N, cnt[j], f[j]);
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int e = 0; e < N; ++e) ss = fmaf(f[j][e], f[j][e], ss);
+  ss = row_sum<TPR>(ss, sm);
+  const float q = 1.f / sqrtf(ss / (float)d + p.eps);
+  if (live && p.rstd && t == 0) p.rstd[row] = q;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    float w[N];
+    load_f32<N>(p.w + (j * TPR + t) * N, cnt[j], w);
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[j][e] = f[j][e] * q * w[e];
+  }
+  if constexpr (!E4M3) {
+    T* y = (T*)p.y + at * p.ldy;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) store_vec<T>(y + (j * TPR + t) * N, cnt[j], f[j]);
+  } else {
+    float m = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(f[j][e]));
+    m = row_max<TPR>(m, sm);
+    // the row's largest value becomes 448, e4m3's largest; a row of zeros keeps a scale that is not zero
+    const float scale = fmaxf(m, 1e-30f) / 448.f, inv = 448.f / fmaxf(m, 1e-30f);
+    if (live && t == 0) p.scale[row] = scale;
+    uint8_t* y = (uint8_t*)p.y + at * p.ldy;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      uint32_t code[N / 4];
+#pragma unroll
+      for (int e = 0; e < N; e += 4) {
+        // the product may pass 448 by its rounding (a NaN stays one)
+        float v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          v[k] = f[j][e + k] * inv;
+          v[k] = fabsf(v[k]) > 448.f ? copysignf(448.f, v[k]) : v[k];
+        }
+        int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
+        code[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
+      }
+      uint8_t* o = y + (j * TPR + t) * N;
+      if (cnt[j] == N) {
+        if constexpr (N == 8) *(u32x2_a1*)o = u32x2{code[0], code[1]};
+        else *(u32_a1*)o = code[0];
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (e < cnt[j]) o[e] = (uint8_t)(code[e / 4] >> (8 * (e % 4)));
+      }
+    }
+  }
+}
+
+constexpr int norm_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
+
+template <typename T, int TPR, int NV, bool E4M3>
+__global__ __launch_bounds__(norm_threads(TPR)) void norm_fwd_kernel(NormProb p) {
+  __shared__ float sm[16];
+  constexpr int G = norm_threads(TPR) / TPR;
+  norm_fwd_row<T, TPR, NV, E4M3>(p, (int64_t)blockIdx.x * G + threadIdx.x / TPR, sm);
+}
+template <typename T, int TPR, int NV>
+__global__ __launch_bounds__(norm_threads(TPR)) void norm_fwd_table_kernel(const NormProb* __restrict__ probs,
+                                                                           const int32_t* __restrict__ map) {
+  __shared__ float sm[16];
+  constexpr int G = norm_threads(TPR) / TPR;
+  const NormProb p = probs[map[2 * blockIdx.x]];
+  norm_fwd_row<T, TPR, NV, false>(p, (int64_t)map[2 * blockIdx.x + 1] * G + threadIdx.x / TPR, sm);
+}
+
+// ---------------------------------------------------------------------------
+// RMS norm, backward. A workgroup takes every `blocks`-th group of rows and
+// keeps its columns' share of dw in registers; the shares are added in order by
+// a second launch (no atomics: the result does not depend on timing).
+// ---------------------------------------------------------------------------
+template <typename T, int TPR, int NV>
+__device__ __forceinline__ void norm_bwd_rows(const NormProb& p, int blk, int64_t wsoff, float* sm, float* acc) {
+  constexpr int N = V16<T>::N, NT = norm_threads(TPR), G = NT / TPR;
+  const int t = threadIdx.x & (TPR - 1), g = threadIdx.x / TPR, d = p.d;
+  float w[NV][N], dw[NV][N];
+  int cnt[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * TPR + t) * N;
+    cnt[j] = min(max(d - c, 0), N);
+    load_f32<N>(p.w + c, cnt[j], w[j]);
+#pragma unroll
+    for (int e = 0; e < N; ++e) dw[j][e] = 0.f;
+  }
+  const float invd = 1.f / (float)d;
+  for (int64_t r0 = (int64_t)blk * G; r0 < p.rows; r0 += (int64_t)p.blocks * G) {
+    const int64_t row = r0 + g;
+    const bool live = row < p.rows;
+    const int64_t at = live ? row : 0;
+    const T* s = (const T*)p.x + at * p.ldx;
+    const T* dy = (const T*)p.dy + at * p.lddy;
+    const float q = live ? p.rstd[at] : 0.f;
+    float a[NV][N], b[NV][N];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) load_vec<T>(s + (j * TPR + t) * N, live ? cnt[j] : 0, a[j]);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) load_vec<T>(dy + (j * TPR + t) * N, live ? cnt[j] : 0, b[j]);
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float xh = a[j][e] * q;
+        dw[j][e] = fmaf(b[j][e], xh, dw[j][e]);
+        b[j][e] *= w[j][e];
+        sum = fmaf(b[j][e], xh, sum);
+      }
+    sum = row_sum<TPR>(sum, sm) * invd;
+    if (p.y) {
+      T* dx = (T*)p.y + at * p.ldy;
+      const T* ds = p.r ? (const T*)p.r + at * p.ldr : nullptr;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int n = live ? cnt[j] : 0;
+        float o[N];
+        if (ds) load_vec<T>(ds + (j * TPR + t) * N, n, o);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float v = q * (b[j][e] - a[j][e] * q * sum) + (ds ? o[e] : 0.f);
+          o[e] = p.mask && !(a[j][e] > 0.f) ? 0.f : v;
+        }
+        store_vec<T>(dx + (j * TPR + t) * N, n, o);
+      }
+    }
+  }
+  float* part = (float*)((char*)p.part + wsoff) + (int64_t)blk * d;
+  if constexpr (G == 1) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < cnt[j]) part[(j * TPR + t) * N + e] = dw[j][e];
+  } else {
+    // the groups' shares one after the other, in group order
+    for (int k = 0; k < G; ++k) {
+      if (g == k)
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const int c = (j * TPR + t) * N + e;
+            acc[c] = k ? acc[c] + dw[j][e] : dw[j][e];
+          }
+      __syncthreads();
+    }
+    for (int c = threadIdx.x; c < d; c += NT) part[c] = acc[c];
+  }
+}
+
+template <int TPR> constexpr int norm_acc() { return TPR < 256 ? TPR * NORM_REGS : 1; }
+
+template <typename T, int TPR, int NV>
+__global__ __launch_bounds__(norm_threads(TPR)) void norm_bwd_kernel(NormProb p) {
+  __shared__ float sm[16];
+  __shared__ float acc[norm_acc<TPR>()];
+  norm_bwd_rows<T, TPR, NV>(p, blockIdx.x, 0, sm, acc);
+}
+template <typename T, int TPR, int NV>
+__global__ __launch_bounds__(norm_threads(TPR)) void norm_bwd_table_kernel(const NormProb* __restrict__ probs,
+                                                                           const int32_t* __restrict__ map, int64_t wsoff) {
+  __shared__ float sm[16];
+  __shared__ float acc[norm_acc<TPR>()];
+  const NormProb p = probs[map[2 * blockIdx.x]];
+  norm_bwd_rows<T, TPR, NV>(p, map[2 * blockIdx.x + 1], wsoff, sm, acc);
+}
+
+// dw: 16 groups of 64 columns' threads, each adding a run of the partials, then
+// the groups in order
+__global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__ part, int nparts, int d,
+                                                       float* __restrict__ dw) {
+  __shared__ float sm[16][64];
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
+  const int per = (nparts + 15) / 16, k0 = g * per, k1 = min(nparts, k0 + per);
+  float a = 0.f;
+  if (c < d)
+    for (int k = k0; k < k1; k += 8) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = k + u < k1 ? part[(int64_t)(k + u) * d + c] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) a += v[u];
+    }
+  sm[g][threadIdx.x & 63] = a;
+  __syncthreads();
+  if (g == 0 && c < d) {
+    a = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) a += sm[k][threadIdx.x];
+    dw[c] = a;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Gated linear recurrence. A wave's lanes are channels (VB neighbouring ones
+// each), so a step's row is one coalesced access and a step needs no exchange
+// between lanes. A chunk is W x L steps: wave w holds steps [w L, (w + 1) L) in
+// registers and composes them into one map h -> A h + H; the maps of the waves
+// meet in LDS, each wave folds those before its own, and walks its steps again
+// from registers. So g and v are read once and the recurrence's serial part is
+// L steps long per chunk, and W folds.
+// ---------------------------------------------------------------------------
+template <typename T, int VB> struct Raw;
+template <> struct Raw<bf16_t, 1> {
+  uint16_t v;
+  __device__ float get(int) const { return bf2f(v); }
+};
+template <> struct Raw<bf16_t, 2> {
+  uint32_t v;
+  __device__ float get(int e) const { return __uint_as_float(e ? v & 0xffff0000u : v << 16); }
+};
+template <> struct Raw<float, 1> {
+  float v;
+  __device__ float get(int) const { return v; }
+};
+template <> struct Raw<float, 2> {
+  float v[2];
+  __device__ float get(int e) const { return v[e]; }
+};
+template <typename T, int VB> __device__ __forceinline__ void raw_store(T* p, const float* f) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < VB; ++e) p[e] = f[e];
+  } else if constexpr (VB == 2) {
+    *(uint32_t*)p = f2bf2(f[0], f[1]);
+  } else {
+    *p = (bf16_t)f2bf(f[0]);
+  }
+}
+
+// a = sigmoid(g) and k = 1 - a = sigmoid(-g), each to its own relative accuracy.
+// fp32: the product g log2(e) with its rounding error, so that exp is as exact for large |g|.
+template <typename T> __device__ __forceinline__ void gate_of(float g, float& a, float& k) {
+  const float x = -fabsf(g), L2E = 1.44269504f;
+  float t = x * L2E, em;
+  if constexpr (sizeof(T) == 4) {
+    const float r = fmaf(x, 1.925963033e-8f, fmaf(x, L2E, -t)) * 0.693147181f;
+    em = __builtin_amdgcn_exp2f(t);
+    em = x > -128.f ? fmaf(em, r, em) : em;  // (an infinite g has no rounding error)
+  } else {
+    em = __builtin_amdgcn_exp2f(t);
+  }
+  const float big = __builtin_amdgcn_rcpf(1.f + em), small = em * big;
+  a = g >= 0.f ? big : small;
+  k = g >= 0.f ? small : big;
+  if (g != g) a = k = g;
+}
+
+// LDS is exchanged between waves once per chunk; global loads stay in flight
+// across the barrier.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+struct Tile {
+  int c;          // first channel of this lane
+  bool on;        // within the width
+  int b, w;       // sequence; wave
+  int len;        // its steps
+  int64_t bc;     // b * d + c
+};
+template <int VB> __device__ __forceinline__ Tile tile_of(const ScanProb& p, int tile, int b) {
+  Tile t;
+  const int c = (tile * 64 + (threadIdx.x & 63)) * VB;
+  t.on = c < p.d;
+  t.c = t.on ? c : 0;
+  t.b = b;
+  t.w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  t.len = p.lens ? min(max(p.lens[b], 0), p.T) : p.T;
+  t.bc = (int64_t)b * p.d + t.c;
+  return t;
+}
+
+// Rows [t0, t0 + L) of one operand; rows at and behind `len` (> 0) repeat its last one.
+template <typename T, int VB, int L>
+__device__ __forceinline__ void load_rows(const void* base, int64_t ld, int64_t bs, const Tile& t, int t0, Raw<T, VB>* r) {
+  const T* p = (const T*)base + t.b * bs + t.c;
+#pragma unroll
+  for (int i = 0; i < L; ++i) r[i] = *(const Raw<T, VB>*)(p + (int64_t)min(t0 + i, t.len - 1) * ld);
+}
+template <typename T, int VB>
+__device__ __forceinline__ void zero_rows(void* base, int64_t ld, int64_t bs, const Tile& t, int t0, int t1, int step) {
+  const float z[VB] = {};
+  T* p = (T*)base + t.b * bs + t.c;
+  if (t.on)
+    for (int i = t0; i < t1; i += step) raw_store<T, VB>(p + (int64_t)i * ld, z);
+}
+
+// The maps of the segments before (forward) or behind (backward) `s`, folded
+// over `h` in order: each wave folds a run of them, and every wave the runs.
+template <int VB, int W>
+__device__ __forceinline__ void fold_segments(const ScanProb& p, const Tile& t, int s, bool bwd, float* h, float* sm) {
+  const int n = bwd ? p.nseg - 1 - s : s;
+  if (n == 0) return;  // the same for the whole workgroup
+  const int per = (n + W - 1) / W, j0 = min(n, t.w * per), j1 = min(n, j0 + per);
+  const int64_t stride = (int64_t)p.B * p.d * 2;
+  const float* agg = p.agg + t.bc * 2;
+  float A[VB], H[VB];
+#pragma unroll
+  for (int e = 0; e < VB; ++e) A[e] = 1.f, H[e] = 0.f;
+  for (int j = j0; j < j1; j += 8) {
+    float a[8][VB], b[8][VB];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int k = min(j + u, j1 - 1), seg = bwd ? p.nseg - 1 - k : k;
+#pragma unroll
+      for (int e = 0; e < VB; ++e) {
+        a[u][e] = agg[seg * stride + 2 * e];
+        b[u][e] = agg[seg * stride + 2 * e + 1];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (j + u < j1)
+#pragma unroll
+        for (int e = 0; e < VB; ++e) {
+          H[e] = fmaf(a[u][e], H[e], b[u][e]);
+          A[e] *= a[u][e];
+        }
+  }
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int e = 0; e < VB; ++e) {
+    sm[((t.w * VB + e) * 2 + 0) * 64 + lane] = A[e];
+    sm[((t.w * VB + e) * 2 + 1) * 64 + lane] = H[e];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < W; ++w)
+#pragma unroll
+    for (int e = 0; e < VB; ++e) h[e] = fmaf(sm[((w * VB + e) * 2) * 64 + lane], h[e], sm[((w * VB + e) * 2 + 1) * 64 + lane]);
+  __syncthreads();
+}
+
+template <typename T, int VB, int W, int L>
+__device__ __forceinline__ void scan_fwd(const ScanProb& p, int tile, int b, int s, float* sm) {
+  constexpr int C = W * L;
+  const Tile t = tile_of<VB>(p, tile, b);
+  const int lane = threadIdx.x & 63;
+  const int tb = s * p.seg * C, te = min(p.T, tb + p.seg * C);
+  const int nc = max(0, min(t.len, te) - tb + C - 1) / C;  // chunks with a live step
+  float h[VB];
+#pragma unroll
+  for (int e = 0; e < VB; ++e) {
+    h[e] = p.start ? p.start[t.bc + e] : 0.f;
+    asm volatile("" : "+v"(h[e]));  // here before the first barrier: `end` may be the same memory
+  }
+  if (W > 1) fold_segments<VB, W>(p, t, s, false, h, sm);
+  Raw<T, VB> rg[L], rv[L];
+  if (nc > 0) {
+    load_rows<T, VB, L>(p.gate, p.ldi, p.bsi, t, tb + t.w * L, rg);
+    load_rows<T, VB, L>(p.value, p.ldi, p.bsi, t, tb + t.w * L, rv);
+  }
+  T* out = (T*)p.o1 + b * p.bso + t.c;
+  for (int k = 0; k < nc; ++k) {
+    const int t0 = tb + k * C + t.w * L;
+    float a[L][VB], x[L][VB];
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int e = 0; e < VB; ++e) {
+        float keep;
+        gate_of<T>(rg[i].get(e), a[i][e], keep);
+        x[i][e] = keep * rv[i].get(e);
+      }
+    if (k + 1 < nc) {
+      load_rows<T, VB, L>(p.gate, p.ldi, p.bsi, t, t0 + C, rg);
+      load_rows<T, VB, L>(p.value, p.ldi, p.bsi, t, t0 + C, rv);
+    }
+    const bool whole = t0 + L <= t.len;
+    if (!whole)
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (t0 + i >= t.len)
+#pragma unroll
+          for (int e = 0; e < VB; ++e) a[i][e] = 1.f, x[i][e] = 0.f;
+    if (p.states && t.w == 0 && t.on) {
+      float* st = p.states + ((int64_t)b * ((p.T + C - 1) / C) + s * p.seg + k) * p.d + t.c;
+#pragma unroll
+      for (int e = 0; e < VB; ++e) st[e] = h[e];
+    }
+    float now[VB];
+#pragma unroll
+    for (int e = 0; e < VB; ++e) now[e] = h[e];
+    if constexpr (W > 1) {
+      float* buf = sm + (k & 1) * W * VB * 2 * 64;
+#pragma unroll
+      for (int e = 0; e < VB; ++e) {
+        float A = 1.f, H = 0.f;
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+          H = fmaf(a[i][e], H, x[i][e]);
+          A *= a[i][e];
+        }
+        buf[((t.w * VB + e) * 2 + 0) * 64 + lane] = A;
+        buf[((t.w * VB + e) * 2 + 1) * 64 + lane] = H;
+      }
+      // one barrier a chunk: the other half of the buffer serves the next one
+      lds_barrier();
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        if (w == t.w)
+#pragma unroll
+          for (int e = 0; e < VB; ++e) now[e] = h[e];
+#pragma unroll
+        for (int e = 0; e < VB; ++e) h[e] = fmaf(buf[((w * VB + e) * 2) * 64 + lane], h[e], buf[((w * VB + e) * 2 + 1) * 64 + lane]);
+      }
+    }
+    if (t.on) {
+#pragma unroll
+      for (int i = 0; i < L; ++i) {
+#pragma unroll
+        for (int e = 0; e < VB; ++e) now[e] = fmaf(a[i][e], now[e], x[i][e]);
+        if (whole || t0 + i < t.len) raw_store<T, VB>(out + (int64_t)(t0 + i) * p.ldo, now);
+      }
+    }
+    if constexpr (W == 1) {
+#pragma unroll
+      for (int e = 0; e < VB; ++e) h[e] = now[e];
+    }
+  }
+  zero_rows<T, VB>(p.o1, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
+  if (p.end && s == p.nseg - 1 && t.w == 0 && t.on)
+#pragma unroll
+    for (int e = 0; e < VB; ++e) p.end[t.bc + e] = h[e];
+}
+
+template <typename T, int VB, int W, int L>
+__device__ __forceinline__ void scan_bwd(const ScanProb& p, int tile, int b, int s, float* sm) {
+  constexpr int C = W * L;
+  const Tile t = tile_of<VB>(p, tile, b);
+  const int lane = threadIdx.x & 63;
+  const int tb = s * p.seg * C, te = min(p.T, tb + p.seg * C);
+  const int nc = max(0, min(t.len, te) - tb + C - 1) / C;
+  float c[VB];  // a_{t+1} e_{t+1}: the gradient that arrives from the later steps
+#pragma unroll
+  for (int e = 0; e < VB; ++e) {
+    c[e] = p.start ? p.start[t.bc + e] : 0.f;
+    asm volatile("" : "+v"(c[e]));
+  }
+  if (W > 1) fold_segments<VB, W>(p, t, s, true, c, sm);
+  const int64_t st0 = ((int64_t)b * ((p.T + C - 1) / C) + s * p.seg) * p.d + t.c;
+  Raw<T, VB> rg[L], rv[L], rd[L];
+  float rh[VB];
+  auto load = [&](int k) {
+    const int t0 = tb + k * C + t.w * L;
+    load_rows<T, VB, L>(p.gate, p.ldi, p.bsi, t, t0, rg);
+    load_rows<T, VB, L>(p.value, p.ldi, p.bsi, t, t0, rv);
+    load_rows<T, VB, L>(p.dh, p.lddh, p.bsdh, t, t0, rd);
+#pragma unroll
+    for (int e = 0; e < VB; ++e) rh[e] = p.states[st0 + (int64_t)k * p.d + e];
+  };
+  if (nc > 0) load(nc - 1);
+  T* og = (T*)p.o1 + b * p.bso + t.c;
+  T* ov = (T*)p.o2 + b * p.bso + t.c;
+  for (int k = nc - 1; k >= 0; --k) {
+    const int t0 = tb + k * C + t.w * L;
+    float a[L][VB], x[L][VB], v[L][VB], dh[L][VB], kp[L][VB], h[VB];
+#pragma unroll
+    for (int e = 0; e < VB; ++e) h[e] = rh[e];
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int e = 0; e < VB; ++e) {
+        gate_of<T>(rg[i].get(e), a[i][e], kp[i][e]);
+        v[i][e] = rv[i].get(e);
+        x[i][e] = kp[i][e] * v[i][e];
+        dh[i][e] = rd[i].get(e);
+      }
+    if (k > 0) load(k - 1);
+    const bool whole = t0 + L <= t.len;
+    if (!whole)
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (t0 + i >= t.len)
+#pragma unroll
+          for (int e = 0; e < VB; ++e) a[i][e] = 1.f, x[i][e] = 0.f, dh[i][e] = 0.f;
+    float cn[VB];
+#pragma unroll
+    for (int e = 0; e < VB; ++e) cn[e] = c[e];
+    if constexpr (W > 1) {
+      float* buf = sm + (k & 1) * W * VB * 3 * 64;
+#pragma unroll
+      for (int e = 0; e < VB; ++e) {
+        float A = 1.f, H = 0.f, Q = 0.f;
+#pragma unroll
+        for (int i = 0; i < L; ++i) {
+          H = fmaf(a[i][e], H, x[i][e]);
+          A *= a[i][e];
+        }
+#pragma unroll
+        for (int i = L - 1; i >= 0; --i) Q = a[i][e] * (dh[i][e] + Q);
+        buf[((t.w * VB + e) * 3 + 0) * 64 + lane] = A;
+        buf[((t.w * VB + e) * 3 + 1) * 64 + lane] = H;
+        buf[((t.w * VB + e) * 3 + 2) * 64 + lane] = Q;
+      }
+      lds_barrier();
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+        if (w < t.w)
+#pragma unroll
+          for (int e = 0; e < VB; ++e) h[e] = fmaf(buf[((w * VB + e) * 3) * 64 + lane], h[e], buf[((w * VB + e) * 3 + 1) * 64 + lane]);
+#pragma unroll
+      for (int w = W - 1; w >= 0; --w) {
+        if (w == t.w)
+#pragma unroll
+          for (int e = 0; e < VB; ++e) cn[e] = c[e];
+#pragma unroll
+        for (int e = 0; e < VB; ++e) c[e] = fmaf(buf[((w * VB + e) * 3) * 64 + lane], c[e], buf[((w * VB + e) * 3 + 2) * 64 + lane]);
+      }
+    }
+    // x becomes h_{t-1} - v_t, walking forward; then the gradients, walking back
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int e = 0; e < VB; ++e) {
+        const float next = fmaf(a[i][e], h[e], x[i][e]);
+        x[i][e] = h[e] - v[i][e];
+        h[e] = next;
+      }
+#pragma unroll
+    for (int i = L - 1; i >= 0; --i) {
+      float dg[VB], dv[VB];
+#pragma unroll
+      for (int e = 0; e < VB; ++e) {
+        const float g = dh[i][e] + cn[e];
+        dv[e] = kp[i][e] * g;
+        cn[e] = a[i][e] * g;
+        dg[e] = kp[i][e] * cn[e] * x[i][e];
+      }
+      if (t.on && (whole || t0 + i < t.len)) {
+        raw_store<T, VB>(og + (int64_t)(t0 + i) * p.ldo, dg);
+        raw_store<T, VB>(ov + (int64_t)(t0 + i) * p.ldo, dv);
+      }
+    }
+    if constexpr (W == 1) {
+#pragma unroll
+      for (int e = 0; e < VB; ++e) c[e] = cn[e];
+    }
+  }
+  zero_rows<T, VB>(p.o1, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
+  zero_rows<T, VB>(p.o2, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
+  if (p.end && s == 0 && t.w == 0 && t.on)
+#pragma unroll
+    for (int e = 0; e < VB; ++e) p.end[t.bc + e] = c[e];
+}
+
+// The map of one segment: forward h -> A h + H, backward c -> A c + Q.
+// Each wave composes a run of the segment's steps of its own, L at a time.
+template <typename T, int VB, int W, int L, bool BWD>
+__device__ __forceinline__ void scan_agg(const ScanProb& p, int tile, int b, int s, float* sm) {
+  const Tile t = tile_of<VB>(p, tile, b);
+  const int lane = threadIdx.x & 63;
+  const int n = p.seg * L;                         // steps per wave
+  const int tb = s * p.seg * W * L + t.w * n, te = min(t.len, tb + n);
+  float A[VB], H[VB];
+#pragma unroll
+  for (int e = 0; e < VB; ++e) A[e] = 1.f, H[e] = 0.f;
+  const int m = max(0, te - tb + L - 1) / L;
+  Raw<T, VB> rg[L], rv[L];
+  auto load = [&](int k) {
+    const int t0 = tb + (BWD ? m - 1 - k : k) * L;
+    load_rows<T, VB, L>(p.gate, p.ldi, p.bsi, t, t0, rg);
+    if (BWD) load_rows<T, VB, L>(p.dh, p.lddh, p.bsdh, t, t0, rv);
+    else load_rows<T, VB, L>(p.value, p.ldi, p.bsi, t, t0, rv);
+  };
+  if (m > 0) load(0);
+  for (int k = 0; k < m; ++k) {
+    const int t0 = tb + (BWD ? m - 1 - k : k) * L;
+    float a[L][VB], x[L][VB];
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int e = 0; e < VB; ++e) {
+        float keep;
+        gate_of<T>(rg[i].get(e), a[i][e], keep);
+        x[i][e] = (BWD ? 1.f : keep) * rv[i].get(e);
+        if (t0 + i >= te) a[i][e] = 1.f, x[i][e] = 0.f;
+      }
+    if (k + 1 < m) load(k + 1);
+#pragma unroll
+    for (int e = 0; e < VB; ++e)
+#pragma unroll
+      for (int j = 0; j < L; ++j) {
+        const int i = BWD ? L - 1 - j : j;
+        H[e] = BWD ? a[i][e] * (x[i][e] + H[e]) : fmaf(a[i][e], H[e], x[i][e]);
+        A[e] *= a[i][e];
+      }
+  }
+#pragma unroll
+  for (int e = 0; e < VB; ++e) {
+    sm[((t.w * VB + e) * 2 + 0) * 64 + lane] = A[e];
+    sm[((t.w * VB + e) * 2 + 1) * 64 + lane] = H[e];
+  }
+  __syncthreads();
+  if (t.w == 0 && t.on) {
+    float* agg = p.agg + ((int64_t)s * p.B * p.d + t.bc) * 2;
+    if (s == 0 && p.start)  // for the second launch, whose last segment may write `end` over it
+#pragma unroll
+      for (int e = 0; e < VB; ++e) p.agg[(int64_t)p.nseg * p.B * p.d * 2 + t.bc + e] = p.start[t.bc + e];
+#pragma unroll
+    for (int e = 0; e < VB; ++e) {
+      float a = 1.f, h = 0.f;
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const int w = BWD ? W - 1 - j : j;
+        const float wa = sm[((w * VB + e) * 2) * 64 + lane], wh = sm[((w * VB + e) * 2 + 1) * 64 + lane];
+        h = fmaf(wa, h, wh);
+        a *= wa;
+      }
+      agg[2 * e] = a;
+      agg[2 * e + 1] = h;
+    }
+  }
+}
+
+template <typename T, int VB, int W, int L, bool BWD>
+__global__ __launch_bounds__(64 * W) void scan_kernel(ScanProb p) {
+  __shared__ float sm[W > 1 ? 2 * W * VB * (BWD ? 3 : 2) * 64 : 1];
+  int i = blockIdx.x;
+  const int tile = i % p.tiles;
+  i /= p.tiles;
+  const int b = i % p.B, s = i / p.B;
+  if constexpr (BWD) scan_bwd<T, VB, W, L>(p, tile, b, s, sm);
+  else scan_fwd<T, VB, W, L>(p, tile, b, s, sm);
+}
+template <typename T, int VB, int W, int L, bool BWD>
+__global__ __launch_bounds__(64 * W) void scan_agg_kernel(ScanProb p) {
+  __shared__ float sm[W * VB * 2 * 64];
+  int i = blockIdx.x;
+  const int tile = i % p.tiles;
+  i /= p.tiles;
+  scan_agg<T, VB, W, L, BWD>(p, tile, i % p.B, i / p.B, sm);
+}
+template <typename T, int VB, int W, int L, bool BWD>
+__global__ __launch_bounds__(64 * W) void scan_table_kernel(const ScanProb* __restrict__ probs, const int32_t* __restrict__ map) {
+  __shared__ float sm[2 * W * VB * (BWD ? 3 : 2) * 64];
+  const ScanProb p = probs[map[2 * blockIdx.x]];
+  const int i = map[2 * blockIdx.x + 1], tile = i % p.tiles, b = i / p.tiles;
+  if constexpr (BWD) scan_bwd<T, VB, W, L>(p, tile, b, 0, sm);
+  else scan_fwd<T, VB, W, L>(p, tile, b, 0, sm);
+}
+
+// ---------------------------------------------------------------------------
+// AdamW. A wave takes AW_BLOCK values at a time, four per lane, so the block of
+// an 8-bit scale is one wave's and its maximum one reduction over the lanes.
+// ---------------------------------------------------------------------------
+// 32 bits from a value's number and the step's key: multiplications by odd
+// constants (fractions of the golden ratio, sqrt 2 and sqrt 3) between shifts
+__device__ __forceinline__ uint32_t random_bits(uint32_t i, uint32_t key) {
+  uint32_t x = i * 0x9E3779B9u + key;
+  x ^= x >> 16;
+  x *= 0x6A09E667u;
+  x ^= x >> 15;
+  x *= 0xBB67AE85u;
+  return x ^ (x >> 16);
+}
+
+// 2^(b - 127) and 2^(127 - b) of an e8m0 scale b
+__device__ __forceinline__ float scale_value(uint32_t b) { return __uint_as_float(b ? b << 23 : 0x400000u); }
+__device__ __forceinline__ float scale_inverse(uint32_t b) { return __uint_as_float(b < 254 ? (254 - b) << 23 : 0x400000u); }
+// the e8m0 scale of a block whose largest magnitude is amax (finite): the least with amax / scale <= 448
+__device__ __forceinline__ uint32_t scale_of(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  const int e = (int)(u >> 23) - 8 + ((u & 0x7fffff) > 0x600000);
+  return (uint32_t)max(e, 0);
+}
+// |x| <= 448 up or down to an e4m3 code, by the 16-bit number r (in 1/2^16 of
+// the way to the next code). A moving average whose steps are smaller than half
+// the distance of two codes would never move under rounding to nearest; rounded
+// like this it moves by the right amount on average.
+__device__ __forceinline__ uint32_t round_code(float x, uint32_t r) {
+  const uint32_t u = __float_as_uint(x), mag = u & 0x7fffffffu;
+  const float ax = __uint_as_float(mag);
+  uint32_t code;
+  if (ax < 0.015625f) code = ((uint32_t)(ax * 33554432.f) + r) >> 16;  // below 2^-6: multiples of 2^-9
+  else code = ((mag + (r << 4)) >> 20) - 960;
+  if (!(ax <= 448.f)) code = 0x7f;  // an infinity or a NaN
+  return code | (u >> 31 << 7);
+}
+
+template <bool G16, bool EIGHT>
+__device__ __forceinline__ void adamw_load(const AdamwTensor& t, int64_t i, int n, f32x4& p, float* g, f32x4& m, f32x4& v,
+                                           uint32_t& mc, uint32_t& vc) {
+  if (n == 4) {
+    p = *(const f32x4_a4*)(t.p + i);
+    if constexpr (G16) {
+      const u32x2 q = *(const u32x2_a2*)((const bf16_t*)t.g + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) g[e] = __uint_as_float(e & 1 ? q[e >> 1] & 0xffff0000u : q[e >> 1] << 16);
+    } else {
+      const f32x4 q = *(const f32x4_a4*)((const float*)t.g + i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) g[e] = q[e];
+    }
+    if constexpr (EIGHT) {
+      mc = *(const u32_a1*)((const uint8_t*)t.m + i);
+      vc = *(const u32_a1*)((const uint8_t*)t.v + i);
+    } else {
+      m = *(const f32x4_a4*)((const float*)t.m + i);
+      v = *(const f32x4_a4*)((const float*)t.v + i);
+    }
+  } else {
+    mc = vc = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool on = e < n;
+      p[e] = on ? t.p[i + e] : 0.f;
+      if constexpr (G16) g[e] = on ? bf2f(((const bf16_t*)t.g)[i + e]) : 0.f;
+      else g[e] = on ? ((const float*)t.g)[i + e] : 0.f;
+      if constexpr (EIGHT) {
+        if (on) mc |= (uint32_t)((const uint8_t*)t.m)[i + e] << (8 * e), vc |= (uint32_t)((const uint8_t*)t.v)[i + e] << (8 * e);
+      } else {
+        m[e] = on ? ((const float*)t.m)[i + e] : 0.f;
+        v[e] = on ? ((const float*)t.v)[i + e] : 0.f;
+      }
+    }
+  }
+}
+
+template <bool G16, bool EIGHT>
+__global__ __launch_bounds__(256) void adamw_kernel(const AdamwTensor* __restrict__ ts, const int32_t* __restrict__ map,
+                                                    AdamwHp hp, const AdamwHp* __restrict__ hps, uint32_t key) {
+  const AdamwTensor t = ts[map[2 * blockIdx.x]];
+  if (hps) hp = hps[t.hp];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t base = (int64_t)map[2 * blockIdx.x + 1] * AW_CHUNK;
+  constexpr int U = AW_CHUNK / AW_BLOCK / 4;  // blocks per wave, all loaded ahead
+  f32x4 p[U], m[U], v[U];
+  float g[U][4];
+  uint32_t mc[U], vc[U], ms[U], vs[U];
+  int cnt[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t b0 = base + (u * 4 + wave) * AW_BLOCK, i = b0 + lane * 4;
+    cnt[u] = (int)min((int64_t)4, max((int64_t)0, t.n - i));
+    adamw_load<G16, EIGHT>(t, i, cnt[u], p[u], g[u], m[u], v[u], mc[u], vc[u]);
+    if constexpr (EIGHT) {
+      ms[u] = b0 < t.n ? t.ms[b0 / AW_BLOCK] : 0;
+      vs[u] = b0 < t.n ? t.vs[b0 / AW_BLOCK] : 0;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t b0 = base + (u * 4 + wave) * AW_BLOCK, i = b0 + lane * 4;
+    if (b0 >= t.n) break;  // a wave as a whole
+    float nm[4], nv[4], rt[4], w[4];
+    if constexpr (EIGHT) {
+      const float sm = scale_value(ms[u]), sv = scale_value(vs[u]);
+      nm[0] = __builtin_amdgcn_cvt_f32_fp8(mc[u], 0) * sm, nm[1] = __builtin_amdgcn_cvt_f32_fp8(mc[u], 1) * sm;
+      nm[2] = __builtin_amdgcn_cvt_f32_fp8(mc[u], 2) * sm, nm[3] = __builtin_amdgcn_cvt_f32_fp8(mc[u], 3) * sm;
+      nv[0] = __builtin_amdgcn_cvt_f32_fp8(vc[u], 0) * sv, nv[1] = __builtin_amdgcn_cvt_f32_fp8(vc[u], 1) * sv;
+      nv[2] = __builtin_amdgcn_cvt_f32_fp8(vc[u], 2) * sv, nv[3] = __builtin_amdgcn_cvt_f32_fp8(vc[u], 3) * sv;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) nv[e] *= nv[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) nm[e] = m[u][e], nv[e] = v[u][e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = g[u][e];
+      nm[e] = fmaf(hp.b1, nm[e], hp.c1 * x);
+      nv[e] = fmaf(hp.b2, nv[e], hp.c2 * x * x);
+      rt[e] = sqrtf(nv[e]);
+      w[e] = p[u][e] * hp.decay - hp.lr * (nm[e] / (rt[e] * hp.isb2 + hp.eps));
+    }
+    uint32_t cm = 0, cv = 0;
+    if constexpr (EIGHT) {
+      float am = 0.f, av = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = fabsf(nm[e]), y = rt[e];
+        am = fmaxf(am, x < __builtin_inff() ? x : 0.f);
+        av = fmaxf(av, y < __builtin_inff() ? y : 0.f);
+      }
+      am = wave_max(am);
+      av = wave_max(av);
+      const uint32_t sm = scale_of(am), sv = scale_of(av);
+      const float im = scale_inverse(sm), iv = scale_inverse(sv);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t r = random_bits(t.base + (uint32_t)(i + e), key);
+        cm |= round_code(nm[e] * im, r & 0xffff) << (8 * e);
+        // a second moment that is not zero never becomes zero: the next step divides by its root
+        uint32_t c = round_code(rt[e] * iv, r >> 16);
+        if (c == 0 && rt[e] > 0.f) c = 1;
+        cv |= c << (8 * e);
+      }
+      if (lane == 0) {
+        t.ms[b0 / AW_BLOCK] = (uint8_t)sm;
+        t.vs[b0 / AW_BLOCK] = (uint8_t)sv;
+      }
+    }
+    if (cnt[u] == 4) {
+      *(f32x4_a4*)(t.p + i) = f32x4{w[0], w[1], w[2], w[3]};
+      if (t.copy) *(u32x2_a2*)(t.copy + i) = u32x2{f2bf2(w[0], w[1]), f2bf2(w[2], w[3])};
+      if constexpr (EIGHT) {
+        *(u32_a1*)((uint8_t*)t.m + i) = cm;
+        *(u32_a1*)((uint8_t*)t.v + i) = cv;
+      } else {
+        *(f32x4_a4*)((float*)t.m + i) = f32x4{nm[0], nm[1], nm[2], nm[3]};
+        *(f32x4_a4*)((float*)t.v + i) = f32x4{nv[0], nv[1], nv[2], nv[3]};
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < cnt[u]) {
+          t.p[i + e] = w[e];
+          if (t.copy) t.copy[i + e] = (bf16_t)f2bf(w[e]);
+          if constexpr (EIGHT) {
+            ((uint8_t*)t.m)[i + e] = (uint8_t)(cm >> (8 * e));
+            ((uint8_t*)t.v)[i + e] = (uint8_t)(cv >> (8 * e));
+          } else {
+            ((float*)t.m)[i + e] = nm[e];
+            ((float*)t.v)[i + e] = nv[e];
+          }
+        }
+    }
+  }
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------
+// Plans and launches
+// ---------------------------------------------------------------------------
+NormPlan norm_plan(bool bf16, int64_t rows, int d) {
+  const int n = bf16 ? 8 : 4;
+  int tpr = 64;
+  while (tpr < 1024 && tpr * NORM_REGS < d) tpr *= 4;
+  int nv = 1;
+  while (nv < (tpr == 1024 ? NORM_REGS / 2 : NORM_REGS) / n && tpr * n * nv < d) nv *= 2;
+  return NormPlan{tpr, nv, norm_threads(tpr) / tpr};
+}
+int norm_blocks(const NormPlan& p, int64_t rows) {
+  const int64_t groups = (rows + p.group - 1) / p.group;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(groups, p.tpr == 1024 ? 256 : 512));
+}
+
+namespace {
+// calls f with (element type, threads per row, vectors per thread) as constants
+template <int N> using Int = std::integral_constant<int, N>;
+template <typename F> hipError_t norm_pick(bool bf16, const NormPlan& p, F&& f) {
+  auto nv = [&](auto type, auto tpr) {
+    constexpr int most = (tpr() == 1024 ? NORM_REGS / 2 : NORM_REGS) * (int)sizeof(type) / 16;
+    if (p.nv == 1) f(type, tpr, Int<1>{});
+    else if (p.nv == 2) f(type, tpr, Int<2>{});
+    else if constexpr (most == 4) f(type, tpr, Int<4>{});
+    else if constexpr (most == 8) p.nv == 4 ? f(type, tpr, Int<4>{}) : f(type, tpr, Int<8>{});
+  };
+  auto tpr = [&](auto type) {
+    if (p.tpr == 64) nv(type, Int<64>{});
+    else if (p.tpr == 256) nv(type, Int<256>{});
+    else nv(type, Int<1024>{});
+  };
+  if (bf16) tpr(bf16_t{});
+  else tpr(float{});
+  return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_norm(bool bf16, bool e4m3, const NormPlan& plan, const NormProb& p, hipStream_t s) {
+  const int64_t grid = (p.rows + plan.group - 1) / plan.group;
+  if (grid <= 0) return hipSuccess;
+  return norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
+    using T = decltype(t);
+    const dim3 blk(norm_threads(tpr()));
+    if (e4m3) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), true>), dim3((unsigned)grid), blk, 0, s, p);
+    else hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), false>), dim3((unsigned)grid), blk, 0, s, p);
+  });
+}
+hipError_t launch_norm_bwd(bool bf16, const NormPlan& plan, const NormProb& p, hipStream_t s) {
+  return norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
+    using T = decltype(t);
+    hipLaunchKernelGGL((norm_bwd_kernel<T, tpr(), nv()>), dim3(p.blocks), dim3(norm_threads(tpr())), 0, s, p);
+  });
+}
+hipError_t launch_norm_table(bool bf16, bool bwd, const NormPlan& plan, const NormProb* probs, const int32_t* map, int nblocks,
+                             int64_t wsoff, hipStream_t s) {
+  if (nblocks <= 0) return hipSuccess;
+  return norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
+    using T = decltype(t);
+    const dim3 blk(norm_threads(tpr()));
+    if (bwd) hipLaunchKernelGGL((norm_bwd_table_kernel<T, tpr(), nv()>), dim3(nblocks), blk, 0, s, probs, map, wsoff);
+    else hipLaunchKernelGGL((norm_fwd_table_kernel<T, tpr(), nv()>), dim3(nblocks), blk, 0, s, probs, map);
+  });
+}
+hipError_t launch_norm_dw(const float* part, int nparts, int d, float* dw, hipStream_t s) {
+  hipLaunchKernelGGL(norm_dw_kernel, dim3((d + 63) / 64), dim3(1024), 0, s, part, nparts, d, dw);
+  return hipGetLastError();
+}
+
+ScanPlan scan_plan(int64_t B, int T, int d, bool pairs) {
+  ScanPlan p{};
+  p.kind = T <= 1 ? 0 : T <= SCAN_L ? 1 : 2;
+  const int64_t wide = B * ((d + 127) / 128);
+  p.vb = pairs && wide >= 512 ? 2 : 1;
+  p.tiles = (d + 64 * p.vb - 1) / (64 * p.vb);
+  const int chunks = scan_chunks(T);
+  p.seg = std::max(1, chunks);
+  p.nseg = 1;
+  const int64_t groups = B * p.tiles;
+  if (p.kind == 2 && groups < 256 && chunks > 2) {
+    const int want = (int)std::min<int64_t>(chunks, (512 + groups - 1) / groups);
+    p.seg = (chunks + want - 1) / want;
+    p.nseg = (chunks + p.seg - 1) / p.seg;
+  }
+  return p;
+}
+
+namespace {
+template <typename T, int VB, bool BWD> void scan_go(const ScanPlan& plan, const ScanProb& p, unsigned grid, hipStream_t s) {
+  if (plan.kind == 0) {
+    hipLaunchKernelGGL((scan_kernel<T, VB, 1, 1, BWD>), dim3(grid), dim3(64), 0, s, p);
+  } else if (plan.kind == 1) {
+    hipLaunchKernelGGL((scan_kernel<T, VB, 1, SCAN_L, BWD>), dim3(grid), dim3(64), 0, s, p);
+  } else {
+    ScanProb q = p;
+    if (plan.nseg > 1) {
+      hipLaunchKernelGGL((scan_agg_kernel<T, VB, SCAN_W, SCAN_L, BWD>), dim3(grid), dim3(64 * SCAN_W), 0, s, p);
+      if (p.start) q.start = p.agg + (int64_t)p.nseg * p.B * p.d * 2;
+    }
+    hipLaunchKernelGGL((scan_kernel<T, VB, SCAN_W, SCAN_L, BWD>), dim3(grid), dim3(64 * SCAN_W), 0, s, q);
+  }
+}
+}  // namespace
+
+hipError_t launch_scan(bool bf16, bool bwd, const ScanPlan& plan, const ScanProb& q, hipStream_t s) {
+  ScanProb p = q;
+  p.tiles = plan.tiles;
+  p.seg = plan.seg;
+  p.nseg = plan.nseg;
+  const unsigned grid = (unsigned)((int64_t)p.tiles * p.B * p.nseg);
+  if (grid == 0) return hipSuccess;
+  auto go = [&](auto type, auto vb) {
+    using T = decltype(type);
+    if (bwd) scan_go<T, vb(), true>(plan, p, grid, s);
+    else scan_go<T, vb(), false>(plan, p, grid, s);
+  };
+  if (bf16 && plan.vb == 2) go(bf16_t{}, Int<2>{});
+  else if (bf16) go(bf16_t{}, Int<1>{});
+  else if (plan.vb == 2) go(float{}, Int<2>{});
+  else go(float{}, Int<1>{});
+  return hipGetLastError();
+}
+
+hipError_t launch_scan_table(bool bf16, bool bwd, int vb, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s) {
+  if (nblocks <= 0) return hipSuccess;
+  auto go = [&](auto type, auto v) {
+    using T = decltype(type);
+    const dim3 blk(64 * SCAN_W);
+    if (bwd) hipLaunchKernelGGL((scan_table_kernel<T, v(), SCAN_W, SCAN_L, true>), dim3(nblocks), blk, 0, s, probs, map);
+    else hipLaunchKernelGGL((scan_table_kernel<T, v(), SCAN_W, SCAN_L, false>), dim3(nblocks), blk, 0, s, probs, map);
+  };
+  if (bf16 && vb == 2) go(bf16_t{}, Int<2>{});
+  else if (bf16) go(bf16_t{}, Int<1>{});
+  else if (vb == 2) go(float{}, Int<2>{});
+  else go(float{}, Int<1>{});
+  return hipGetLastError();
+}
+
+hipError_t launch_adamw(bool g16, bool eight, const AdamwTensor* ts, const int32_t* map, int nblocks, const AdamwHp& hp,
+                        const AdamwHp* hps, uint32_t key, hipStream_t s) {
+  if (nblocks <= 0) return hipSuccess;
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(nblocks), dim3(256), 0, s, ts, map, hp, hps, key); };
+  if (g16 && eight) go(adamw_kernel<true, true>);
+  else if (g16) go(adamw_kernel<true, false>);
+  else if (eight) go(adamw_kernel<false, true>);
+  else go(adamw_kernel<false, false>);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// e4m3 on the host
+// ---------------------------------------------------------------------------
+float e4m3_value(uint8_t c) {
+  const int e = (c >> 3) & 15, f = c & 7;
+  if (e == 15 && f == 7) return std::nanf("");
+  const float v = e ? std::ldexp(1.f + f / 8.f, e - 7) : std::ldexp((float)f, -9);
+  return c & 0x80 ? -v : v;
+}
+uint8_t e4m3_code(float x) {
+  const uint8_t sign = std::signbit(x) ? 0x80 : 0;
+  const float a = std::fabs(x);
+  if (!(a <= 448.f)) return sign | 0x7f;
+  int e;
+  std::frexp(a, &e);
+  e = std::max(e - 1, -6) - 3;  // the last place is 2^e
+  const int n = (int)std::nearbyint(std::ldexp(a, -e));  // 0 .. 16
+  // consecutive codes are consecutive multiples of the last place, across exponents too
+  return sign | (uint8_t)(n < 8 ? n : ((e + 9) << 3) + n);
+}
+int scale_exponent(float amax) {
+  if (!(amax > 0.f)) return -127;
+  int e;
+  const float f = std::frexp(amax, &e);
+  return std::min(127, std::max(-127, e - 9 + (f > 0.875f ? 1 : 0)));
+}
+
+}  // namespace un

@@ -29,6 +29,7 @@
 #include <vector>
 
 #include "internal.h"
+#include "operators.h"
 
 // Multi-tile halo forward workgroups: at most UN_HALO_MT m-tiles each, as
 // many as leave about UN_HALO_WPS workgroups per slot (two per CU).
@@ -325,6 +326,16 @@ un_status fail(un_ctx* c, un_status s, const std::string& msg) {
   else g_create_error = msg;
   return s;
 }
+
+}  // namespace
+
+// The same for a call without a context (op_api.cpp).
+un_status un::fail_call(un_status s, const char* msg) {
+  g_create_error = msg;
+  return s;
+}
+
+namespace {
 
 #define HIPCHK(ctx, expr)                                                                   \
   do {                                                                                      \

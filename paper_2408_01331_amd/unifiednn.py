@@ -33,7 +33,9 @@ EXPORTS = ["un_create", "un_create_grouped", "un_plan_bytes", "un_plan_bytes_gro
            "un_set_active", "un_set_optimizer", "un_get_opt_state", "un_set_opt_state", "un_get_params",
            "un_set_params", "un_get_grads", "un_keep_grads", "un_param_count", "un_arena_bytes", "un_sync", "un_get_stream",
            "un_set_stream", "un_graph_capture", "un_graph_step", "un_step_scratch",
-           "un_profile_enable", "un_profile_read", "un_destroy", "un_last_error"]
+           "un_profile_enable", "un_profile_read", "un_destroy", "un_last_error",
+           "un_rms_norm", "un_rms_norm_backward", "un_rms_norm_workspace", "un_gated_scan", "un_gated_scan_backward",
+           "un_gated_scan_sizes", "un_adamw_create", "un_adamw_step", "un_adamw_destroy"]
 
 
 class un_layer(ctypes.Structure):
@@ -53,6 +55,31 @@ class un_input_spec(ctypes.Structure):
 class un_optimizer(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("momentum", ctypes.c_float), ("beta1", ctypes.c_float),
                 ("beta2", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+def _struct(name, **fields):
+    """A ctypes structure: i = int32, l = int64, z = size_t, f = float, d = double, u = uint32, p = pointer."""
+    types = dict(i=ctypes.c_int32, l=ctypes.c_int64, z=ctypes.c_size_t, f=ctypes.c_float, d=ctypes.c_double,
+                 u=ctypes.c_uint32, p=ctypes.c_void_p)
+    return type(name, (ctypes.Structure,), {"_fields_": [(k, types[t]) for k, t in fields.items()]})
+
+
+# arguments of the operators on device tensors (operators.py)
+un_rms_norm_args = _struct("un_rms_norm_args", type="i", width="i", rows="l", eps="f", x="p", ldx="l", residual="p", ldr="l",
+                           weight="p", sum="p", lds="l", y="p", ldy="l", rstd="p", scale="p")
+un_rms_norm_grad_args = _struct("un_rms_norm_grad_args", type="i", width="i", rows="l", dy="p", lddy="l", s="p", lds="l",
+                                weight="p", rstd="p", ds="p", ldds="l", dx="p", lddx="l", dweight="p", workspace="p",
+                                workspace_bytes="z")
+un_gated_scan_args = _struct("un_gated_scan_args", type="i", batch="i", tokens="i", width="i", gate="p", value="p", ld_in="l",
+                             seq_in="l", lens="p", start="p", h="p", ld_h="l", seq_h="l", last="p", states="p",
+                             workspace="p", workspace_bytes="z")
+un_gated_scan_grad_args = _struct("un_gated_scan_grad_args", type="i", batch="i", tokens="i", width="i", gate="p", value="p",
+                                  ld_in="l", seq_in="l", lens="p", states="p", dh="p", ld_dh="l", seq_dh="l", dlast="p",
+                                  dgate="p", dvalue="p", ld_out="l", seq_out="l", dstart="p", workspace="p",
+                                  workspace_bytes="z")
+un_adamw_tensor = _struct("un_adamw_tensor", weight="p", grad="p", copy="p", m="p", v="p", m_scale="p", v_scale="p",
+                          elements="l")
+un_adamw_hyper = _struct("un_adamw_hyper", lr="d", beta1="d", beta2="d", eps="d", decay="d", t="l", key="u")
 
 
 class UnError(RuntimeError):
@@ -112,6 +139,16 @@ def lib():
                                                ctypes.POINTER(ctypes.c_int64)]),
             "un_destroy": (None, [P]),
             "un_last_error": (ctypes.c_char_p, [P]),
+            "un_rms_norm": (ctypes.c_int, [ctypes.POINTER(un_rms_norm_args), P]),
+            "un_rms_norm_backward": (ctypes.c_int, [ctypes.POINTER(un_rms_norm_grad_args), P]),
+            "un_rms_norm_workspace": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, c_size_p]),
+            "un_gated_scan": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_args), P]),
+            "un_gated_scan_backward": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_grad_args), P]),
+            "un_gated_scan_sizes": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, c_size_p, c_size_p]),
+            "un_adamw_create": (ctypes.c_int, [ctypes.POINTER(un_adamw_tensor), ctypes.c_int32, ctypes.c_int32,
+                                               ctypes.c_int32, ctypes.POINTER(P)]),
+            "un_adamw_step": (ctypes.c_int, [P, ctypes.POINTER(un_adamw_hyper), P]),
+            "un_adamw_destroy": (None, [P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
