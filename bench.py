@@ -31,7 +31,8 @@ if ROOT not in sys.path:
 from paper_2408_01331_amd import workloads as W  # noqa: E402
 
 PEAK = {"bf16_mfma_tflops": 2500.0, "f32_mfma_tflops": 157.3, "hbm_gbs": 8000.0}
-KCLASS = ["gemm_fwd", "gemm_bwd", "conv_fwd", "conv_dgrad", "conv_wgrad", "ce", "sgd", "other", "attn"]
+KCLASS = ["gemm_fwd", "gemm_bwd", "conv_fwd", "conv_dgrad", "conv_wgrad", "ce", "sgd", "other", "attn", "recurrence", "norm",
+          "adamw"]
 
 
 # ---------------------------------------------------------------------------
@@ -64,12 +65,12 @@ def algorithmic_work(wl):
             op = layer[0]
             ends = li + 1 < len(layers) and layers[li + 1][0] == "res_end"
             begins = li > 0 and layers[li - 1][0] == "res_begin"
-            if op in ("linear", "attention"):
+            if op in ("linear", "attention", "recurrence"):
                 # a sequence (T, d): token-wise products over B * T rows
                 R, K = (B * shape[0], shape[1]) if len(shape) == 2 else (B, int(np.prod(shape)))
                 last = li == len(layers) - 1
                 # (N, rows stored fp32?) per projection: Linear, or in- and out-projection
-                projs = [(layer[1], last)] if op == "linear" else [(3 * K, False), (K, False)]
+                projs = [(layer[1], last)] if op == "linear" else [((3 if op == "attention" else 2) * K, False), (K, False)]
                 for pj, (N, fp32_out) in enumerate(projs):
                     f = 2.0 * R * K * N
                     flops["gemm_fwd"] += f
@@ -86,6 +87,10 @@ def algorithmic_work(wl):
                     flops["attn"] += 4.0 * B * T * T * d + 8.0 * B * T * T * d
                     nbytes["attn"] += B * T * 3 * d * es + B * T * d * es + B * T * T * 4          # forward, P fp32
                     nbytes["attn"] += B * T * 3 * d * es * 2 + B * T * d * es + B * T * T * 4      # backward
+                elif op == "recurrence":
+                    el = R * K                                           # core: gate and value -> h, and back
+                    flops["recurrence"] += 28.0 * el
+                    nbytes["recurrence"] += 3 * el * es + 5 * el * es
                 else:
                     N = layer[1]
                     if last:                                             # softmax-CE: logits in, dZ out
@@ -118,6 +123,13 @@ def algorithmic_work(wl):
                 nbytes["conv_dgrad"] += in_b if begins else 0            # skip gradient
                 n_params += O * C * k * k + O
                 shape = (O, OH, OW)
+                first = False
+            elif op == "rms_norm":
+                R, K = (B * shape[0], shape[1]) if len(shape) == 2 else (B, shape[0])
+                flops["norm"] += 14.0 * R * K
+                nbytes["norm"] += R * K * es * (2 + (2 if first else 3 + begins)) + K * (4 + 4)
+                nbytes["other"] += K * 8                                 # update (split reduction kernel)
+                n_params += K
                 first = False
             elif op == "pool":
                 C, H, Wd = shape
@@ -359,7 +371,7 @@ def measure(wl, steps, warmup, repeats=0):
     # with the update in the epilogue), timed and bounded apart.
     sym = {"gemm_fwd": ["gemm_fwd"], "gemm_bwd": ["gemm_bwd"], "conv_fwd": ["conv_fwd"],
            "conv_dgrad": ["conv_dgrad"], "conv_wgrad": ["conv_wgrad"], "ce": ["ce"], "sgd": ["sgd"],
-           "other": ["other"], "attn": ["attn"]}
+           "other": ["other"], "attn": ["attn"], "recurrence": ["recurrence"], "norm": ["norm"], "adamw": ["adamw"]}
     per_sym = {}
     for name, classes in sym.items():
         ms = sum(kern[c]["ms_per_step"] for c in classes if c in kern)

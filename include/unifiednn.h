@@ -94,8 +94,23 @@ typedef enum {
    * [d, d], out_proj.bias [d]. A ReLU may follow, and residual markers may
    * enclose it (x + attn(x)). T <= 64 and the per-sample working set
    * (4 T (d + 4) + 2 T (T + 1) floats) must fit 160 KiB of LDS. */
-  UN_SELF_ATTENTION = 8
+  UN_SELF_ATTENTION = 8,
+  /* Root-mean-square norm over the features, of each token on a sequence
+   * (PyTorch's RMSNorm(d, eps=UN_RMS_NORM_EPS)): y = x / sqrt(mean(x^2) + eps) *
+   * weight; parameter weight [d], at most 16384 features. On a sequence, a Linear,
+   * attention or recurrence block's output or the flat network input, not
+   * directly after a Conv2d block; a residual block may start with one (x +
+   * f(norm(x))) but not end with one, and no ReLU follows it. */
+  UN_RMS_NORM = 9,
+  /* Gated linear recurrence over the tokens of a sequence [T, d]:
+   * [G V] = x W_in^T + b_in, h_t = a_t h_{t-1} + (1 - a_t) V_t with a =
+   * sigmoid(G) and h_0 = 0, y = h W_out^T + b_out. Parameters in order:
+   * in_proj_weight [2d, d], in_proj_bias [2d], out_proj.weight [d, d],
+   * out_proj.bias [d]. Any number of tokens. A ReLU may follow, and residual
+   * markers may enclose it. */
+  UN_GATED_RECURRENCE = 10
 } un_op;
+#define UN_RMS_NORM_EPS 1e-6f
 
 typedef struct {
   int32_t op;      /* un_op */
@@ -272,27 +287,37 @@ un_status un_get_grads(un_ctx* ctx, int32_t i, float* dst, size_t cap_elems, siz
  *   UN_OPT_ADAM      m <- fma(beta1, m, (1-beta1) g);  v <- fma(beta2, v, (1-beta2) g^2);
  *                    w <- w - (lr / (1 - beta1^t)) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  *                    (t = the model's update count, from 1; m, v start at 0)
- * These are torch.optim.SGD (momentum, no dampening, not Nesterov) and
- * torch.optim.Adam (no weight decay, no amsgrad) without weight decay. */
-typedef enum { UN_OPT_SGD = 0, UN_OPT_MOMENTUM = 1, UN_OPT_ADAM = 2 } un_opt_kind;
+ *   UN_OPT_ADAMW     w <- w - (lr * weight_decay) w, then as UN_OPT_ADAM
+ *   UN_OPT_ADAMW8    as UN_OPT_ADAMW, with m and sqrt(v) kept in 8 bits (e4m3 codes
+ *                    with a power-of-two scale per 256 values, rounded up or down
+ *                    at random by distance, as un_adamw_step's 8-bit states; the
+ *                    random numbers depend on the model's update count alone)
+ * These are torch.optim.SGD (momentum, no dampening, not Nesterov),
+ * torch.optim.Adam (no weight decay, no amsgrad) and torch.optim.AdamW (no
+ * amsgrad). A step under the last two needs 0 <= lr and lr * weight_decay < 1
+ * (UN_ERR_INVALID, nothing runs). */
+typedef enum { UN_OPT_SGD = 0, UN_OPT_MOMENTUM = 1, UN_OPT_ADAM = 2, UN_OPT_ADAMW = 3, UN_OPT_ADAMW8 = 4 } un_opt_kind;
 typedef struct {
   int32_t kind;      /* un_opt_kind */
   float momentum;    /* UN_OPT_MOMENTUM: in [0, 1) */
-  float beta1, beta2;/* UN_OPT_ADAM: in [0, 1) */
-  float eps;         /* UN_OPT_ADAM: > 0 */
+  float beta1, beta2;/* UN_OPT_ADAM, _ADAMW, _ADAMW8: in [0, 1) */
+  float eps;         /* UN_OPT_ADAM, _ADAMW, _ADAMW8: > 0 */
+  float weight_decay;/* UN_OPT_ADAMW, _ADAMW8: >= 0 (read for these kinds only) */
 } un_optimizer;
 
 /* Give model i a fresh optimizer: its state is zeroed and its update count
- * reset (as a new torch optimizer would). The first non-SGD optimizer of a
- * context allocates the state of all models (two fp32 values per parameter,
- * outside the arena) and rebuilds the step's tables. Waits for the stream.
+ * reset (as a new torch optimizer would). The first optimizer of a context
+ * with fp32 state allocates the state of all models (two fp32 values per
+ * parameter, outside the arena) and rebuilds the step's tables; UN_OPT_ADAMW8
+ * allocates the model's own state alone (2 bytes and 2 / 256 per parameter as
+ * stored), given back when the model gets another optimizer. Waits for the stream.
  * Errors: UN_ERR_RANGE (i), UN_ERR_INVALID (kind or hyper-parameters),
  * UN_ERR_OOM. */
 un_status un_set_optimizer(un_ctx* ctx, int32_t i, const un_optimizer* opt);
 
 /* Model i's optimizer state for a checkpoint: k * n_params floats, k = 0
- * (SGD), 1 (momentum buffer) or 2 (Adam: first moments, then second
- * moments), each block in un_get_params layout and order; *step receives the
+ * (SGD), 1 (momentum buffer) or 2 (Adam, AdamW: first moments, then second
+ * moments; 8-bit states as the values they stand for), each block in un_get_params layout and order; *step receives the
  * number of updates the model has taken under this optimizer. With dst ==
  * NULL only *n_elems and *step are set. Waits for the stream.
  * Errors: UN_ERR_RANGE, UN_ERR_BUFSIZE. */
@@ -300,8 +325,10 @@ un_status un_get_opt_state(un_ctx* ctx, int32_t i, float* dst, size_t cap_elems,
 
 /* Restore model i's optimizer state and update count (layout as
  * un_get_opt_state for the model's current optimizer; n_elems exact), e.g.
- * to resume from a checkpoint. Errors: UN_ERR_RANGE, UN_ERR_BUFSIZE,
- * UN_ERR_INVALID (negative step, NULL src). */
+ * to resume from a checkpoint. 8-bit states take the nearest codes: what
+ * un_get_opt_state returned comes back exactly. Errors: UN_ERR_RANGE,
+ * UN_ERR_BUFSIZE, UN_ERR_INVALID (negative step, NULL src; 8 bits: a moment that
+ * is not finite, or a negative second one). */
 un_status un_set_opt_state(un_ctx* ctx, int32_t i, const float* src, size_t n_elems, int64_t step);
 
 /* For callers that cannot allocate device memory (code under HIP graph
@@ -353,8 +380,8 @@ un_status un_set_stream(un_ctx* ctx, void* hip_stream);
  * un_set_stream, or a change of un_keep_grads or of the label mode
  * (un_load_labels / un_load_batch) make it stale. The batch, parameters and
  * labels it reads are the context's buffers: load new batches and set
- * parameters as usual between replays. Not available while a model has a
- * momentum or Adam optimizer (their per-step hyper-parameters would be frozen).
+ * parameters as usual between replays. Not available while a model has an
+ * optimizer other than SGD (their per-step hyper-parameters would be frozen).
  * Errors: UN_ERR_STATE (no batch), UN_ERR_INVALID (lr), UN_ERR_UNSUPPORTED,
  * UN_ERR_DEVICE. */
 un_status un_graph_capture(un_ctx* ctx, float lr);
@@ -374,7 +401,10 @@ typedef enum {
   UN_K_SGD = 6,         /* weight copy refresh (SGD kernel without gradient) */
   UN_K_OTHER = 7,       /* split-K reduction with the fused update (conv, long-contraction Linear) */
   UN_K_ATTN = 8,        /* self-attention core, forward and backward */
-  UN_K_COUNT = 9
+  UN_K_RECURRENCE = 9,  /* gated recurrence core, forward and backward */
+  UN_K_NORM = 10,       /* RMS norm, forward and backward */
+  UN_K_ADAMW = 11,      /* AdamW with 8-bit states */
+  UN_K_COUNT = 12
 } un_kernel_class;
 
 /* Enable (1) or disable (0) per-kernel timing: while enabled, every launch is

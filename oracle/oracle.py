@@ -35,6 +35,11 @@ paper's PyTorch prototype, whose defaults these are):
   x W_in^T + b_in (in-projection [3d, d]), A = softmax(Q K^T / sqrt(d)) V,
   y = A W_out^T + b_out; its parameters are in_proj_weight, in_proj_bias,
   out_proj.weight, out_proj.bias;
+* ``rms_norm`` divides the features (of each token) by the root of their mean
+  square plus 1e-6 and multiplies them by its weight (PyTorch's RMSNorm);
+  ``recurrence`` is, per sample and channel over the tokens, h_t = a_t h_{t-1} +
+  (1 - a_t) V_t with a = sigmoid(G), h_0 = 0 and [G V] = x W_in^T + b_in
+  (in-projection [2d, d]), y = h W_out^T + b_out;
 * a residual block (``res_begin`` ... ``res_end``) is a module returning
   inner(x) + x, the standard skip connection: the sum is formed before any
   ReLU that follows the block, and in backward the gradient at the sum flows
@@ -54,7 +59,9 @@ Precision modes:
   attention layer the two projections are Linear layers; the core reads Q, K,
   V and the gradient dA at its output as bf16 operands, keeps the scores S and
   the probabilities P in fp32 (both modes), and stores A and dQKV (read as
-  operands by the projections).
+  operands by the projections). A norm reads its input as an operand and keeps
+  its weight and the row's root in fp32; a recurrence reads G, V and the gradient
+  dh at its output as operands, keeps the state in fp32 and stores h and dG dV.
 
 Accumulation (``acc``): ``"f64"`` (the default, the reference) sums every dot
 product exactly enough to be rounded once; ``"f32"`` evaluates the same
@@ -198,6 +205,46 @@ def attention_core_bwd(da, q, k, v, p):
     return dq, dk, dv
 
 
+NORM_EPS = 1e-6
+
+
+def rms_norm_fwd(x, w):
+    """y = x / sqrt(mean(x^2) + eps) * w over the last axis. Returns (y, 1 / the root)."""
+    q = 1.0 / np.sqrt((x * x).mean(axis=-1, keepdims=True) + NORM_EPS)
+    return x * q * w, q
+
+
+def rms_norm_bwd(dy, x, w, q):
+    """(dx, dw): with xh = x q, dx = q (dy w - xh mean(dy w xh)), dw = sum over rows of dy xh."""
+    xh, g = x * q, dy * w
+    dx = q * (g - xh * (g * xh).mean(axis=-1, keepdims=True))
+    return dx, (dy * xh).reshape(-1, x.shape[-1]).sum(axis=0)
+
+
+def recurrence_fwd(g, v):
+    """h_t = a_t h_{t-1} + (1 - a_t) v_t along axis 1, a = sigmoid(g), h_0 = 0. Returns (h, a)."""
+    a = 1.0 / (1.0 + np.exp(-g))
+    h = np.zeros_like(v)
+    now = np.zeros_like(v[:, 0])
+    for t in range(v.shape[1]):
+        now = a[:, t] * now + (1.0 - a[:, t]) * v[:, t]
+        h[:, t] = now
+    return h, a
+
+
+def recurrence_bwd(dh, g, v, h, a):
+    """(dg, dv): e_t = dh_t + a_{t+1} e_{t+1}, dv_t = (1 - a_t) e_t, dg_t = a_t (1 - a_t) e_t (h_{t-1} - v_t)."""
+    dg, dv = np.zeros_like(v), np.zeros_like(v)
+    carry = np.zeros_like(v[:, 0])
+    for t in reversed(range(v.shape[1])):
+        e = dh[:, t] + carry
+        prev = h[:, t - 1] if t else np.zeros_like(carry)
+        dv[:, t] = (1.0 - a[:, t]) * e
+        dg[:, t] = a[:, t] * dv[:, t] * (prev - v[:, t])
+        carry = a[:, t] * e
+    return dg, dv
+
+
 def conv2d_fwd(h, W, b, pad):
     """z[n,o,p,q] = b[o] + sum_{c,u,v} W[o,c,u,v] * h[n,c,p+u-pad,q+v-pad]; outside reads are 0.
 
@@ -322,6 +369,11 @@ def count_params(spec, in_shape):
         elif op == "attention":
             d = shape[-1]
             total += 4 * d * d + 4 * d
+        elif op == "recurrence":
+            d = shape[-1]
+            total += 3 * d * d + 3 * d
+        elif op == "rms_norm":
+            total += shape[-1]
         elif op not in ("relu", "res_begin", "res_end"):
             raise ValueError(f"unknown op {op!r}")
     return total
@@ -376,8 +428,8 @@ def forward(spec, params, x, mode="f32", flags=None, acc="f64"):
             skip = h
             cache.append(("res_begin",))
         elif op == "res_end":
-            if skip is None or layers[li - 1][0] not in ("linear", "conv", "attention"):
-                raise ValueError("residual end must directly follow the block's last linear, conv or attention")
+            if skip is None or layers[li - 1][0] not in ("linear", "conv", "attention", "recurrence"):
+                raise ValueError("residual end must directly follow the block's last linear, conv, attention or recurrence")
             skip = None
             cache.append(("res_end",))
         elif op == "conv":
@@ -451,6 +503,35 @@ def forward(spec, params, x, mode="f32", flags=None, acc="f64"):
                     mag = mag + np.abs(R.operand(skip))
             cache.append(("attention", pi, hin, Wiq, q, k, v, p, aq, Woq))
             pi += 4
+        elif op == "rms_norm":
+            hin, w = R.operand(h), np.asarray(params[pi], dtype=F64)
+            y, q = R.run(rms_norm_fwd, hin, w)
+            h = R.store(y)
+            cache.append(("rms_norm", pi, hin, w, q))
+            pi += 1
+        elif op == "recurrence":
+            if h.ndim != 3:
+                raise ValueError("a recurrence needs a sequence (add an unflatten)")
+            Wi, bi, Wo, bo = params[pi:pi + 4]
+            hin, Wiq, Woq = R.operand(h), R.operand(Wi), R.operand(Wo)
+            d = hin.shape[2]
+            gv = R.operand(R.store(R.run(linear_fwd, hin, Wiq, np.asarray(bi, dtype=F64))))
+            gate, val = gv[..., :d], gv[..., d:]
+            s, a = R.run(recurrence_fwd, gate, val)
+            sq = R.operand(R.store(s))
+            z = R.run(linear_fwd, sq, Woq, np.asarray(bo, dtype=F64))
+            ends_block = li + 1 < len(layers) and layers[li + 1][0] == "res_end"
+            if ends_block:
+                if skip is None or skip.shape != z.shape:
+                    raise ValueError("residual block: missing begin or shape mismatch")
+                z = z + R.operand(skip)
+            h = R.store(z)
+            if flags is not None:
+                mag, last_pi = linear_fwd(np.abs(sq), np.abs(Woq), np.abs(np.asarray(bo, dtype=F64))), pi + 2
+                if ends_block:
+                    mag = mag + np.abs(R.operand(skip))
+            cache.append(("recurrence", pi, hin, Wiq, gate, val, s, a, sq, Woq))
+            pi += 4
         else:
             raise ValueError(f"unknown op {op!r}")
     return h, cache
@@ -461,7 +542,7 @@ def backward(spec, params, cache, dlogits, mode="f32", acc="f64"):
     R = _Mode(mode, acc)
     grads = [None] * len(params)
     g = np.asarray(dlogits, dtype=F64)
-    first_param_layer = min(e[1] for e in cache if e[0] in ("linear", "conv", "attention"))
+    first_param_layer = min(e[1] for e in cache if e[0] in ("linear", "conv", "attention", "rms_norm", "recurrence"))
     gskip = None  # gradient at the sum of the open residual block
     for entry in reversed(cache):
         kind = entry[0]
@@ -491,6 +572,22 @@ def backward(spec, params, cache, dlogits, mode="f32", acc="f64"):
             grads[pi + 2], grads[pi + 3] = R.store(dWo), R.store(dbo)
             dq, dk, dv = R.run(attention_core_bwd, R.operand(R.store(da)), q, k, v, p)
             gqi = R.operand(R.store(np.concatenate([dq, dk, dv], axis=-1)))
+            need_dh = pi != first_param_layer
+            dWi, dbi, dh = R.run(linear_bwd, gqi, hin, Wiq, need_dh)
+            grads[pi], grads[pi + 1] = R.store(dWi), R.store(dbi)
+            g = R.store(dh) if need_dh else None
+        elif kind == "rms_norm":
+            pi, hin, w, q = entry[1:]
+            dx, dw = R.run(rms_norm_bwd, R.operand(g), hin, w, q)
+            grads[pi] = R.store(dw)
+            g = R.store(dx) if pi != first_param_layer else None
+        elif kind == "recurrence":
+            pi, hin, Wiq, gate, val, s, a, sq, Woq = entry[1:]
+            gq = R.operand(g)
+            dWo, dbo, ds = R.run(linear_bwd, gq, sq, Woq, True)
+            grads[pi + 2], grads[pi + 3] = R.store(dWo), R.store(dbo)
+            dg, dv = R.run(recurrence_bwd, R.operand(R.store(ds)), gate, val, s, a)
+            gqi = R.operand(R.store(np.concatenate([dg, dv], axis=-1)))
             need_dh = pi != first_param_layer
             dWi, dbi, dh = R.run(linear_bwd, gqi, hin, Wiq, need_dh)
             grads[pi], grads[pi + 1] = R.store(dWi), R.store(dbi)
@@ -556,10 +653,19 @@ def adam_update(params, grads, m, v, t, lr, beta1, beta2, eps, mode="f32"):
     return out_p, out_m, out_v
 
 
+def adamw_update(params, grads, m, v, t, lr, beta1, beta2, eps, decay, mode="f32"):
+    """AdamW (torch.optim.AdamW's definition without amsgrad): theta <- theta -
+    lr decay theta, then adam_update's step. Rounding as there: theta once."""
+    out_p, out_m, out_v = adam_update(params, grads, m, v, t, lr, beta1, beta2, eps, "f64")
+    cast = (lambda a: a) if mode == "f64" else to_f32
+    return ([cast(p - lr * decay * np.asarray(q, dtype=F64)) for p, q in zip(out_p, params)],
+            [cast(a) for a in out_m], [cast(a) for a in out_v])
+
+
 def step_opt(spec, params, x, y, lr, opt, state, mode="f32", flags=None, acc="f64"):
     """One training step of one model under its optimizer.
 
-    opt: {"kind": "sgd" | "momentum" | "adam", "momentum", "betas", "eps"};
+    opt: {"kind": "sgd" | "momentum" | "adam" | "adamw", "momentum", "betas", "eps", "weight_decay"};
     state: {"t": updates taken, "s1": [...], "s2": [...]} (zeros / absent at
     the start). Returns (loss, new params, grads, new state)."""
     logits, cache = forward(spec, params, x, mode, flags, acc)
@@ -575,6 +681,10 @@ def step_opt(spec, params, x, y, lr, opt, state, mode="f32", flags=None, acc="f6
         newp, b = momentum_update(params, grads, state.get("s1", zeros), lr, opt["momentum"], mode)
         return loss, newp, grads, {"t": t, "s1": b}
     b1, b2 = opt["betas"]
+    if kind == "adamw":
+        newp, m, v = adamw_update(params, grads, state.get("s1", zeros), state.get("s2", zeros), t, lr, b1, b2,
+                                  opt["eps"], opt["weight_decay"], mode)
+        return loss, newp, grads, {"t": t, "s1": m, "s2": v}
     newp, m, v = adam_update(params, grads, state.get("s1", zeros), state.get("s2", zeros), t, lr, b1, b2,
                              opt["eps"], mode)
     return loss, newp, grads, {"t": t, "s1": m, "s2": v}

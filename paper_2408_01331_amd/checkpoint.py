@@ -13,7 +13,9 @@ child of that Sequential, a module with an ``inner`` Sequential of the
 enclosed layers whose forward returns ``inner(x) + x``: its layers are named
 ``"<block index>.inner.<layer index in the block>.weight"``. The optimizer state is
 stored as ``"momentum_buffer.<name>"`` (SGD with momentum) or
-``"exp_avg.<name>"`` / ``"exp_avg_sq.<name>"`` (Adam). The metadata holds the
+``"exp_avg.<name>"`` / ``"exp_avg_sq.<name>"`` (Adam, AdamW; 8-bit states as
+the values they stand for). A norm's parameter is its ``weight``; a recurrence's
+are ``in_proj_weight``, ``in_proj_bias``, ``out_proj.weight``, ``out_proj.bias``. The metadata holds the
 spec, the input shape, the precision, the optimizer and the update count.
 """
 from __future__ import annotations
@@ -27,7 +29,8 @@ from safetensors import safe_open
 from . import workloads as W
 from .unifiednn import split_params
 
-STATE_NAMES = {"sgd": [], "momentum": ["momentum_buffer"], "adam": ["exp_avg", "exp_avg_sq"]}
+STATE_NAMES = {"sgd": [], "momentum": ["momentum_buffer"], "adam": ["exp_avg", "exp_avg_sq"],
+               "adamw": ["exp_avg", "exp_avg_sq"], "adamw8": ["exp_avg", "exp_avg_sq"]}
 
 
 def param_names(spec):
@@ -48,6 +51,10 @@ def param_names(spec):
         prefix = f"{k}.inner.{j}" if inside else f"{k}"
         if op in ("linear", "conv"):
             names += [f"{prefix}.weight", f"{prefix}.bias"]
+        elif op == "rms_norm":
+            names.append(f"{prefix}.weight")
+        elif op == "recurrence":
+            names += [f"{prefix}.{n}" for n in ("in_proj_weight", "in_proj_bias", "out_proj.weight", "out_proj.bias")]
         if inside:
             j += 1
         else:
@@ -108,7 +115,8 @@ def load(hybrid, i, path):
     if tuple(hybrid.in_shape_of(i)) != meta["in_shape"]:
         raise ValueError(f"checkpoint {path} was trained on input shape {meta['in_shape']}")
     opt = meta["optimizer"]
-    hybrid.set_optimizer(i, opt["kind"], opt["momentum"], tuple(opt["betas"]), opt["eps"])
+    decay = {"weight_decay": opt["weight_decay"]} if "weight_decay" in opt else {}
+    hybrid.set_optimizer(i, opt["kind"], opt["momentum"], tuple(opt["betas"]), opt["eps"], **decay)
     names = param_names(spec)
     hybrid.set_params(i, np.concatenate([tensors[n].ravel() for n in names]))
     state = [tensors[f"{s}.{n}"].ravel() for s in STATE_NAMES[opt["kind"]] for n in names]

@@ -213,6 +213,7 @@ inline size_t attn_lds_bytes(int T, int d, bool bwd, int es) {
 //   kind 1  SGD momentum:  b <- fma(b1, b, g);  w <- fma(-lr, b, w)   (b1 = momentum)
 //   kind 2  Adam:          m <- fma(b1, m, c1*g);  v <- fma(b2, v, c2*g*g);
 //                          w <- w - lr * (m / (sqrt(v) * isb2 + eps))
+//   kind < 0  AdamW:       as Adam, with w <- fma(kind, w, w) first (kind = -rate * decay)
 // with, for Adam at its step t: lr = rate / (1 - beta1^t), c1 = 1 - beta1,
 // c2 = 1 - beta2, isb2 = 1 / sqrt(1 - beta2^t).
 // ---------------------------------------------------------------------------

@@ -1159,6 +1159,7 @@ __device__ __forceinline__ float opt_update1(const OptHp& h, float g, float w, f
   const float v = fmaf(h.b2, *s2, h.c2 * g * g);
   *s1 = m;
   *s2 = v;
+  if (h.kind < 0.f) w = fmaf(h.kind, w, w);
   return w - h.lr * (m / (sqrtf(v) * h.isb2 + h.eps));
 }
 
@@ -1200,6 +1201,7 @@ __device__ __forceinline__ void opt_update4(const OptHp& h, const f32x4& g, f32x
   for (int e = 0; e < 4; ++e) {
     a[e] = fmaf(h.b1, a[e], h.c1 * g[e]);
     v[e] = fmaf(h.b2, v[e], h.c2 * g[e] * g[e]);
+    if (h.kind < 0.f) w[e] = fmaf(h.kind, w[e], w[e]);
     w[e] = w[e] - h.lr * (a[e] / (sqrtf(v[e]) * h.isb2 + h.eps));
   }
   once_store<NT>(a, (gptr<f32x4>)s1);
@@ -1606,7 +1608,7 @@ void gemm_kernel(const GemmProb* __restrict__ probs,
           const float kind = s_hp[r].kind;
           const int64_t base = (int64_t)m * p.ldc + n;
           if (kind != 0.f) a1[q] = once_load<ONCE, f32x4>((gptr<const f32x4>)(p.s1 + base));
-          if (kind == 2.f) a2[q] = once_load<ONCE, f32x4>((gptr<const f32x4>)(p.s2 + base));
+          if (kind == 2.f || kind < 0.f) a2[q] = once_load<ONCE, f32x4>((gptr<const f32x4>)(p.s2 + base));
         }
       }
     }
@@ -1676,7 +1678,7 @@ void gemm_kernel(const GemmProb* __restrict__ probs,
           const float kind = s_hp[r].kind;
           f32x4 b1 = {0.f, 0.f, 0.f, 0.f}, b2 = b1;
           if (kind != 0.f) b1 = once_load<ONCE, f32x4>((gptr<const f32x4>)(p.s1 + base));
-          if (kind == 2.f) b2 = once_load<ONCE, f32x4>((gptr<const f32x4>)(p.s2 + base));
+          if (kind == 2.f || kind < 0.f) b2 = once_load<ONCE, f32x4>((gptr<const f32x4>)(p.s2 + base));
           opt_update4<ONCE>(s_hp[r], g, w, b1, b2, p.s1 + base, p.s2 + base);
         }
       } else {

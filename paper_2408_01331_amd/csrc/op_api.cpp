@@ -77,7 +77,7 @@ un_status un_rms_norm(const un_rms_norm_args* a, void* stream) {
   const int64_t d = a->width;
   if (a->rows > 1 && (a->ldx < d || a->ldy < d || (a->residual && a->ldr < d) || (a->sum && a->lds < d)))
     return bad(F, "a row stride is smaller than the width");
-  const NormPlan plan = norm_plan(a->type == UN_TYPE_BF16, a->rows, a->width);
+  const NormPlan plan = norm_plan(a->type == UN_TYPE_BF16, a->width);
   if (too_many((a->rows + plan.group - 1) / plan.group, 256 > plan.tpr ? 256 : plan.tpr)) return bad(F, "too many rows", UN_ERR_UNSUPPORTED);
   NormProb p{};
   p.x = a->x;
@@ -103,7 +103,7 @@ un_status un_rms_norm_workspace(int32_t type, int64_t rows, int32_t width, size_
   if (!type_ok(type)) return bad(F, "unknown type");
   if (rows < 0 || width < 1) return bad(F, "rows >= 0 and width >= 1 expected");
   if (width > NORM_MAX_D) return bad(F, "width above 16384 is not supported", UN_ERR_UNSUPPORTED);
-  *bytes = (size_t)norm_blocks(norm_plan(type == UN_TYPE_BF16, rows, width), rows) * width * 4;
+  *bytes = (size_t)norm_blocks(norm_plan(type == UN_TYPE_BF16, width), rows) * width * 4;
   return UN_OK;
 }
 
@@ -119,7 +119,7 @@ un_status un_rms_norm_backward(const un_rms_norm_grad_args* a, void* stream) {
   if (a->rows > 1 && (a->lddy < d || a->lds < d || (a->ds && a->ldds < d) || (a->dx && a->lddx < d)))
     return bad(F, "a row stride is smaller than the width");
   if (a->workspace_bytes < need || !a->workspace) return bad(F, "workspace too small (un_rms_norm_workspace)", UN_ERR_BUFSIZE);
-  const NormPlan plan = norm_plan(a->type == UN_TYPE_BF16, a->rows, a->width);
+  const NormPlan plan = norm_plan(a->type == UN_TYPE_BF16, a->width);
   NormProb p{};
   p.x = a->s;
   p.ldx = a->lds;
@@ -339,7 +339,8 @@ un_status un_adamw_step(un_adamw* a, const un_adamw_hyper* h, void* stream) {
   if (dev != a->device) return bad(F, "the stream is on another device than the plan");
   const double t = (double)h->t;
   AdamwHp hp;
-  hp.decay = (float)(1.0 - h->lr * h->decay);
+  hp.decay = (float)(h->lr * h->decay);
+  hp.key = h->key;
   hp.lr = (float)(h->lr / (1.0 - std::pow(h->beta1, t)));
   hp.b1 = (float)h->beta1;
   hp.b2 = (float)h->beta2;
@@ -348,7 +349,7 @@ un_status un_adamw_step(un_adamw* a, const un_adamw_hyper* h, void* stream) {
   hp.isb2 = (float)(1.0 / std::sqrt(1.0 - std::pow(h->beta2, t)));
   hp.eps = (float)h->eps;
   e = launch_adamw(a->g16, a->eight, (const AdamwTensor*)a->table, (const int32_t*)(a->table + a->map_at), a->nblocks, hp, nullptr,
-                   h->key, (hipStream_t)stream);
+                   (hipStream_t)stream);
   return e == hipSuccess ? UN_OK : device_error(F, e);
 }
 

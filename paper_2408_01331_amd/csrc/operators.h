@@ -44,7 +44,7 @@ struct NormPlan {
   int tpr, nv;         // threads per row; 16-byte vectors per thread
   int group;           // rows of a workgroup at a time
 };
-NormPlan norm_plan(bool bf16, int64_t rows, int d);
+NormPlan norm_plan(bool bf16, int d);
 // workgroups of a backward pass over `rows` rows
 int norm_blocks(const NormPlan& p, int64_t rows);
 // One problem (by value), or a table: one (problem, block) pair per workgroup.
@@ -92,8 +92,9 @@ inline size_t scan_ws_bytes(const ScanPlan& p, int64_t B, int d) { return p.nseg
 // pairs: every row of the operands allows loads of two channels at once
 ScanPlan scan_plan(int64_t B, int T, int d, bool pairs);
 hipError_t launch_scan(bool bf16, bool bwd, const ScanPlan& plan, const ScanProb& p, hipStream_t s);
-// table: one (problem, tile * B + sequence) pair per workgroup; every problem nseg == 1
-hipError_t launch_scan_table(bool bf16, bool bwd, int vb, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s);
+// table: one (problem, sequence * tiles + tile) pair per workgroup; every problem nseg == 1. kind, vb: as ScanPlan's
+// (kind 1 or 2, the same for every problem)
+hipError_t launch_scan_table(bool bf16, bool bwd, int kind, int vb, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // AdamW over many tensors. States fp32, or e4m3 codes with a power of two per
@@ -110,13 +111,14 @@ struct AdamwTensor {
   int32_t hp;                 // index of the tensor's hyper-parameters
 };
 struct AdamwHp {
-  float decay, lr, b1, b2, c1, c2, isb2, eps;   // as OptHp's Adam, and w <- decay * w first
+  float decay, lr, b1, b2, c1, c2, isb2, eps;   // as OptHp's Adam, and w <- fma(-decay, w, w) first
+  uint32_t key;                                 // of the rounding's random numbers
 };
 constexpr int AW_BLOCK = 256;                   // values per scale
 constexpr int AW_CHUNK = 16 * AW_BLOCK;         // values per workgroup
 // map: (tensor, chunk) per workgroup. hps: device array, or null: `hp` for every tensor.
 hipError_t launch_adamw(bool g16, bool eight, const AdamwTensor* ts, const int32_t* map, int nblocks, const AdamwHp& hp,
-                        const AdamwHp* hps, uint32_t key, hipStream_t s);
+                        const AdamwHp* hps, hipStream_t s);
 
 // e4m3 (largest finite value 448) on the host, for reading and setting states
 float e4m3_value(uint8_t code);

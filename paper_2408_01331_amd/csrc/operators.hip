@@ -824,7 +824,7 @@ __global__ __launch_bounds__(64 * W) void scan_agg_kernel(ScanProb p) {
 }
 template <typename T, int VB, int W, int L, bool BWD>
 __global__ __launch_bounds__(64 * W) void scan_table_kernel(const ScanProb* __restrict__ probs, const int32_t* __restrict__ map) {
-  __shared__ float sm[2 * W * VB * (BWD ? 3 : 2) * 64];
+  __shared__ float sm[W > 1 ? 2 * W * VB * (BWD ? 3 : 2) * 64 : 1];
   const ScanProb p = probs[map[2 * blockIdx.x]];
   const int i = map[2 * blockIdx.x + 1], tile = i % p.tiles, b = i / p.tiles;
   if constexpr (BWD) scan_bwd<T, VB, W, L>(p, tile, b, 0, sm);
@@ -910,7 +910,7 @@ __device__ __forceinline__ void adamw_load(const AdamwTensor& t, int64_t i, int 
 
 template <bool G16, bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(const AdamwTensor* __restrict__ ts, const int32_t* __restrict__ map,
-                                                    AdamwHp hp, const AdamwHp* __restrict__ hps, uint32_t key) {
+                                                    AdamwHp hp, const AdamwHp* __restrict__ hps) {
   const AdamwTensor t = ts[map[2 * blockIdx.x]];
   if (hps) hp = hps[t.hp];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -953,7 +953,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwTensor* __restric
       nm[e] = fmaf(hp.b1, nm[e], hp.c1 * x);
       nv[e] = fmaf(hp.b2, nv[e], hp.c2 * x * x);
       rt[e] = sqrtf(nv[e]);
-      w[e] = p[u][e] * hp.decay - hp.lr * (nm[e] / (rt[e] * hp.isb2 + hp.eps));
+      w[e] = fmaf(-hp.decay, p[u][e], p[u][e]) - hp.lr * (nm[e] / (rt[e] * hp.isb2 + hp.eps));
     }
     uint32_t cm = 0, cv = 0;
     if constexpr (EIGHT) {
@@ -970,7 +970,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwTensor* __restric
       const float im = scale_inverse(sm), iv = scale_inverse(sv);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t r = random_bits(t.base + (uint32_t)(i + e), key);
+        const uint32_t r = random_bits(t.base + (uint32_t)(i + e), hp.key);
         cm |= round_code(nm[e] * im, r & 0xffff) << (8 * e);
         // a second moment that is not zero never becomes zero: the next step divides by its root
         uint32_t c = round_code(rt[e] * iv, r >> 16);
@@ -1015,7 +1015,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwTensor* __restric
 // ---------------------------------------------------------------------------
 // Plans and launches
 // ---------------------------------------------------------------------------
-NormPlan norm_plan(bool bf16, int64_t rows, int d) {
+NormPlan norm_plan(bool bf16, int d) {
   const int n = bf16 ? 8 : 4;
   int tpr = 64;
   while (tpr < 1024 && tpr * NORM_REGS < d) tpr *= 4;
@@ -1135,14 +1135,15 @@ hipError_t launch_scan(bool bf16, bool bwd, const ScanPlan& plan, const ScanProb
   return hipGetLastError();
 }
 
-hipError_t launch_scan_table(bool bf16, bool bwd, int vb, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s) {
+hipError_t launch_scan_table(bool bf16, bool bwd, int kind, int vb, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s) {
   if (nblocks <= 0) return hipSuccess;
-  auto go = [&](auto type, auto v) {
+  auto waves = [&](auto type, auto v, auto w) {
     using T = decltype(type);
-    const dim3 blk(64 * SCAN_W);
-    if (bwd) hipLaunchKernelGGL((scan_table_kernel<T, v(), SCAN_W, SCAN_L, true>), dim3(nblocks), blk, 0, s, probs, map);
-    else hipLaunchKernelGGL((scan_table_kernel<T, v(), SCAN_W, SCAN_L, false>), dim3(nblocks), blk, 0, s, probs, map);
+    const dim3 blk(64 * w());
+    if (bwd) hipLaunchKernelGGL((scan_table_kernel<T, v(), w(), SCAN_L, true>), dim3(nblocks), blk, 0, s, probs, map);
+    else hipLaunchKernelGGL((scan_table_kernel<T, v(), w(), SCAN_L, false>), dim3(nblocks), blk, 0, s, probs, map);
   };
+  auto go = [&](auto type, auto v) { kind == 1 ? waves(type, v, Int<1>{}) : waves(type, v, Int<SCAN_W>{}); };
   if (bf16 && vb == 2) go(bf16_t{}, Int<2>{});
   else if (bf16) go(bf16_t{}, Int<1>{});
   else if (vb == 2) go(float{}, Int<2>{});
@@ -1151,9 +1152,9 @@ hipError_t launch_scan_table(bool bf16, bool bwd, int vb, const ScanProb* probs,
 }
 
 hipError_t launch_adamw(bool g16, bool eight, const AdamwTensor* ts, const int32_t* map, int nblocks, const AdamwHp& hp,
-                        const AdamwHp* hps, uint32_t key, hipStream_t s) {
+                        const AdamwHp* hps, hipStream_t s) {
   if (nblocks <= 0) return hipSuccess;
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(nblocks), dim3(256), 0, s, ts, map, hp, hps, key); };
+  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(nblocks), dim3(256), 0, s, ts, map, hp, hps); };
   if (g16 && eight) go(adamw_kernel<true, true>);
   else if (g16) go(adamw_kernel<true, false>);
   else if (eight) go(adamw_kernel<false, true>);

@@ -95,7 +95,7 @@ inline int64_t rup(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 struct Block {
-  int kind = 0;  // 0 linear, 1 conv, 2 self-attention core (between its two projections)
+  int kind = 0;  // 0 linear, 1 conv, 2 self-attention core, 3 recurrence core (each between its two projections), 4 RMS norm
   int tokens = 1;  // a Linear on a sequence acts on every token: its GEMM rows are batch * tokens
   int level = 0, model = 0;
   bool relu = false, pool = false, last = false, prev_relu = false, concat = false;
@@ -137,6 +137,10 @@ struct Block {
   size_t fws = NONE, fws_size = 0, fws_limit_size = 0;
   int64_t fldws = 0;
   int fsplits = 0, fkchunk = 0;
+  // recurrence core: the state at the start of every chunk; norm: 1 / rms of every row (fp32)
+  size_t states = NONE, rstd = NONE;
+  int nblocks = 0;         // norm: workgroups of its backward pass (its partial weight gradients, ws)
+  bool has_params() const { return kind != 2 && kind != 3; }
   // output geometry
   int out_elems_per_sample() const { return kind == 0 ? N : (pool ? PH * PW * O : OH * OW * O); }
 };
@@ -172,13 +176,15 @@ struct Group {
 };
 
 struct Launch {
-  int kind;   // 0 gemm, 1 conv fwd, 2 conv dgrad, 3 conv wgrad, 4 reduce, 5 ce, 6 sgd, 7/8 halo conv fwd/dgrad
+  int kind;   // 0 gemm, 1 conv fwd, 2 conv dgrad, 3 conv wgrad, 4 reduce, 5 ce, 6 sgd, 7/8 halo conv fwd/dgrad,
+              // 9/10 attention core fwd/bwd, 11/12 recurrence core fwd/bwd, 13/14 norm fwd/bwd
   int kclass;
   size_t probs, map;  // arena offsets
   int count;
   int mode = 0;       // GEMM: tile variant; conv weight gradient: code variant (launch_conv_wgrad); CE: problems needing the row pass
   size_t lds = 0;     // halo conv: dynamic LDS bytes
-  int bm = 0;         // conv weight gradient: output channels per tile
+  int bm = 0;         // conv weight gradient: output channels per tile; recurrence: channels per lane
+  NormPlan norm{};    // norm launches
 };
 
 struct EventRec {
@@ -284,8 +290,9 @@ struct un_ctx {
   // the number of updates each model has taken under it
   struct Opt {
     int kind = UN_OPT_SGD;
-    double momentum = 0, beta1 = 0.9, beta2 = 0.999, eps = 1e-8;
+    double momentum = 0, beta1 = 0.9, beta2 = 0.999, eps = 1e-8, decay = 0;
     int64_t t = 0;
+    char* state8 = nullptr;  // UN_OPT_ADAMW8: the model's codes and scales (Tensor8)
   };
   std::vector<Opt> opts;
   bool any_opt = false;          // some model is not plain SGD: the step uploads OptHp per model
@@ -293,6 +300,15 @@ struct un_ctx {
   size_t sbytes = 0;
   size_t opt_dev = NONE;         // OptHp per model
   const OptHp* optp = nullptr;   // opt_dev while a step with optimizers is being launched
+  // models with 8-bit AdamW: the step stores their gradients (as it does kept
+  // ones) and one launch behind the backward pass updates all of their tensors
+  struct Adamw8 {
+    char* mem = nullptr;         // AdamwHp per model, the tensors, (tensor, chunk) per workgroup
+    size_t tensors = 0, map = 0; // offsets in mem
+    int nblocks = 0;             // of the active models
+    bool any = false;            // some model, active or not
+    size_t cap = 0;              // bytes of mem
+  } aw;
   // schedule
   std::vector<Launch> fwd, bwd;
   Launch ce{}, refresh{};
@@ -450,7 +466,7 @@ un_status parse_model(const un_model_spec& s, const un_input_spec& in, int mi, M
       // the skip reads the first enclosed block's input: a block's output, or
       // the network's input when that is flat or a sequence (an image input
       // is staged channel-padded for the convolutions)
-      if ((m.blocks.empty() && !(seq || (h == 1 && w == 1))) || s.layers[i - 1].op == UN_FLATTEN) {
+      if ((m.blocks.empty() && !(seq || (h == 1 && w == 1))) || (i > 0 && s.layers[i - 1].op == UN_FLATTEN)) {
         why = where(i) + "a residual block must start at the output of a Linear, Conv2d or attention block, "
                          "or at a flat or sequence input";
         return UN_ERR_UNSUPPORTED;
@@ -471,8 +487,9 @@ un_status parse_model(const un_model_spec& s, const un_input_spec& in, int mi, M
         why = where(i) + "empty residual block";
         return UN_ERR_INVALID;
       }
-      if (s.layers[i - 1].op != UN_LINEAR && s.layers[i - 1].op != UN_CONV2D && s.layers[i - 1].op != UN_SELF_ATTENTION) {
-        why = where(i) + "a residual block must end with a Linear, Conv2d or attention (a ReLU goes after the end marker)";
+      if (s.layers[i - 1].op != UN_LINEAR && s.layers[i - 1].op != UN_CONV2D && s.layers[i - 1].op != UN_SELF_ATTENTION &&
+          s.layers[i - 1].op != UN_GATED_RECURRENCE) {
+        why = where(i) + "a residual block must end with a Linear, Conv2d, attention or recurrence (a ReLU goes after the end marker)";
         return UN_ERR_UNSUPPORTED;
       }
       Block& e = m.blocks.back();
@@ -494,8 +511,9 @@ un_status parse_model(const un_model_spec& s, const un_input_spec& in, int mi, M
       }
       continue;
     }
-    if (res_open >= 0 && L.op != UN_LINEAR && L.op != UN_CONV2D && L.op != UN_RELU && L.op != UN_SELF_ATTENTION) {
-      why = where(i) + "a residual block may enclose only Linear, Conv2d, attention and ReLU layers";
+    if (res_open >= 0 && L.op != UN_LINEAR && L.op != UN_CONV2D && L.op != UN_RELU && L.op != UN_SELF_ATTENTION &&
+        L.op != UN_GATED_RECURRENCE && L.op != UN_RMS_NORM) {
+      why = where(i) + "a residual block may enclose only Linear, Conv2d, attention, recurrence, norm and ReLU layers";
       return UN_ERR_UNSUPPORTED;
     }
     if (res_open >= 0 && L.op == UN_CONV2D && i + 1 < s.n_layers &&
@@ -576,14 +594,37 @@ un_status parse_model(const un_model_spec& s, const un_input_spec& in, int mi, M
         return UN_ERR_UNSUPPORTED;
       }
       ++i;
-    } else if (L.op == UN_SELF_ATTENTION) {
+    } else if (L.op == UN_RMS_NORM) {
+      if (!seq && !(m.blocks.empty() ? h == 1 && w == 1 : m.blocks.back().kind != 1)) {
+        why = where(i) + "a norm reads a sequence, a Linear layer's flat output or the flat input";
+        return UN_ERR_UNSUPPORTED;
+      }
+      if (!m.blocks.empty() && m.blocks.back().kind == 1) {
+        why = where(i) + "a norm may not directly follow a Conv2d block";
+        return UN_ERR_UNSUPPORTED;
+      }
+      Block b;
+      b.kind = 4;
+      b.tokens = std::max(seq, 1);
+      b.K = b.N = seq ? c : c * h * w;
+      if (b.N > NORM_MAX_D) {
+        why = where(i) + "a norm of more than 16384 features is not supported";
+        return UN_ERR_UNSUPPORTED;
+      }
+      b.n_w = (size_t)b.N;
+      b.pt_w = b.pt_b = pt;
+      pt += b.n_w;
+      ++i;
+      m.blocks.push_back(b);
+    } else if (L.op == UN_SELF_ATTENTION || L.op == UN_GATED_RECURRENCE) {
+      const bool attn = L.op == UN_SELF_ATTENTION;
       if (!seq) {
-        why = where(i) + "attention needs a sequence (add an unflatten)";
+        why = where(i) + (attn ? "attention" : "a recurrence") + " needs a sequence (add an unflatten)";
         return UN_ERR_INVALID;
       }
-      const int d = c;
-      const size_t lds = attn_lds_bytes(seq, d, true, 4);  // the fp32 layout, for both precisions
-      if (seq > 64 || lds > (size_t)160 * 1024) {
+      const int d = c, parts = attn ? 3 : 2;  // Q | K | V, or gate | value
+      const size_t lds = attn ? attn_lds_bytes(seq, d, true, 4) : 0;  // the fp32 layout, for both precisions
+      if (attn && (seq > 64 || lds > (size_t)160 * 1024)) {
         why = where(i) + "attention supports up to 64 tokens whose working set fits 160 KiB of LDS";
         return UN_ERR_UNSUPPORTED;
       }
@@ -593,15 +634,15 @@ un_status parse_model(const un_model_spec& s, const un_input_spec& in, int mi, M
       bi.tokens = seq;
       bi.in_c = d;
       bi.K = d;
-      bi.N = 3 * d;
-      bi.n_w = (size_t)3 * d * d;
-      bi.n_b = (size_t)3 * d;
+      bi.N = parts * d;
+      bi.n_w = (size_t)parts * d * d;
+      bi.n_b = (size_t)parts * d;
       bi.pt_w = pt;
       bi.pt_b = pt + bi.n_w;
       pt += bi.n_w + bi.n_b;
       m.blocks.push_back(bi);
       Block bc;
-      bc.kind = 2;
+      bc.kind = attn ? 2 : 3;
       bc.tokens = seq;
       bc.K = d;
       bc.N = d;
@@ -1196,13 +1237,95 @@ static void build_tables(un_ctx* c, Tables& T) {
     out.push_back(Launch{kind, UN_K_ATTN, po, mo, (int)(map.size() / 2)});
     out.back().lds = lds;
   };
+  // recurrence core: one workgroup per (problem, channel tile, sequence). Pairs
+  // of channels per lane where that still leaves two workgroups per CU
+  auto emit_scan = [&](std::vector<ScanProb>& ps, std::vector<Launch>& out, int kind) {
+    if (ps.empty()) return;
+    int64_t wide = 0;
+    int longest = 0;
+    for (auto& p : ps) {
+      wide += (int64_t)p.B * cdiv(p.d, 128);
+      longest = std::max(longest, p.T);
+    }
+    const int vb = wide >= 512 ? 2 : 1;
+    std::vector<int32_t> map;
+    for (size_t k = 0; k < ps.size(); ++k) {
+      ScanProb& p = ps[k];
+      p.tiles = cdiv(p.d, 64 * vb);
+      p.seg = scan_chunks(p.T);
+      p.nseg = 1;
+      for (int t = 0; t < p.tiles * p.B; ++t) {
+        map.push_back((int32_t)k);
+        map.push_back(t);
+      }
+    }
+    size_t po = put(ps.data(), ps.size() * sizeof(ScanProb));
+    for (size_t k = 0; k < ps.size(); ++k) {
+      size_t b0 = po + k * sizeof(ScanProb);
+      for (size_t f : {offsetof(ScanProb, gate), offsetof(ScanProb, value), offsetof(ScanProb, dh), offsetof(ScanProb, o1),
+                       offsetof(ScanProb, o2), offsetof(ScanProb, states)})
+        fix.push_back(b0 + f);
+    }
+    size_t mo = put(map.data(), map.size() * 4);
+    out.push_back(Launch{kind, UN_K_RECURRENCE, po, mo, (int)(map.size() / 2), longest <= SCAN_L ? 1 : 2});
+    out.back().bm = vb;
+  };
+  // norm: one workgroup per (problem, group of rows), backward per (problem,
+  // block); one launch per number of threads a row (the order of a row's sum
+  // follows its own width alone, whatever shares the step)
+  auto emit_norm_one = [&](std::vector<NormProb>& ps, std::vector<Launch>& out, int kind) {
+    int widest = 0;
+    for (auto& p : ps) widest = std::max(widest, p.d);
+    const NormPlan plan = norm_plan(bf, widest);
+    std::vector<int32_t> map;
+    for (size_t k = 0; k < ps.size(); ++k) {
+      const int nb = kind == 13 ? cdiv(ps[k].rows, plan.group) : ps[k].blocks;
+      for (int t = 0; t < nb; ++t) {
+        map.push_back((int32_t)k);
+        map.push_back(t);
+      }
+    }
+    size_t po = put(ps.data(), ps.size() * sizeof(NormProb));
+    for (size_t k = 0; k < ps.size(); ++k) {
+      size_t b0 = po + k * sizeof(NormProb);
+      for (size_t f : {offsetof(NormProb, x), offsetof(NormProb, r), offsetof(NormProb, dy), offsetof(NormProb, w),
+                       offsetof(NormProb, y), offsetof(NormProb, rstd), offsetof(NormProb, part)})
+        fix.push_back(b0 + f);
+    }
+    size_t mo = put(map.data(), map.size() * 4);
+    out.push_back(Launch{kind, UN_K_NORM, po, mo, (int)(map.size() / 2)});
+    out.back().norm = plan;
+  };
+  auto emit_norm = [&](std::vector<NormProb>& ps, std::vector<Launch>& out, int kind) {
+    for (int tpr : {64, 256, 1024}) {
+      std::vector<NormProb> same;
+      for (auto& p : ps)
+        if (norm_plan(bf, p.d).tpr == tpr) same.push_back(p);
+      if (!same.empty()) emit_norm_one(same, out, kind);
+    }
+  };
   auto conv_base = [&](const Block& b) { return conv_geometry(b, c->groups[c->models[b.model].group].B); };
 
+  // inputs, sizes and kept states of a recurrence core, for both directions
+  auto scan_geometry = [&](const Block& b, const Block& bi, int B) {
+    ScanProb p{};
+    p.gate = ptr(bi.Y);
+    p.value = ptr(sub(bi.Y, (int64_t)b.N * (int64_t)es));
+    p.ldi = bi.ldy;
+    p.bsi = bi.ldy * b.tokens;
+    p.states = (float*)ptr(b.states);
+    p.B = B;
+    p.T = b.tokens;
+    p.d = b.N;
+    return p;
+  };
   // forward levels
   for (int lv = 0; lv < levels; ++lv) {
     std::vector<GemmProb> gp;
     std::vector<ConvProb> cp;
     std::vector<AttnProb> ap;
+    std::vector<ScanProb> sp_;
+    std::vector<NormProb> np;
     std::vector<char> cat_done(c->groups.size(), 0);
     for (auto& m : c->models) {
       if (lv >= (int)m.blocks.size() || !c->active[m.blocks[0].model]) continue;
@@ -1281,6 +1404,25 @@ static void build_tables(un_ctx* c, Tables& T) {
         p.B = B;
         p.scale = (float)(1.0 / std::sqrt((double)b.N));
         ap.push_back(p);
+      } else if (b.kind == 3) {
+        const Block& bi = m.blocks[lv - 1];  // the in-projection: gate | value per token row
+        ScanProb p = scan_geometry(b, bi, B);
+        p.o1 = ptr(b.Y);
+        p.ldo = b.ldy;
+        p.bso = b.ldy * b.tokens;
+        sp_.push_back(p);
+      } else if (b.kind == 4) {
+        NormProb p{};
+        p.x = ptr(b.X);
+        p.ldx = b.ldx;
+        p.w = (const float*)ptr(b.W32);
+        p.y = ptr(b.Y);
+        p.ldy = b.ldy;
+        p.rstd = (float*)ptr(b.rstd);
+        p.rows = (int64_t)B * b.tokens;
+        p.d = b.N;
+        p.eps = UN_RMS_NORM_EPS;
+        np.push_back(p);
       } else {
         ConvProb p = conv_base(b);
         p.M = b.pool ? B * b.PH * b.PW * 4 : B * b.OH * b.OW;
@@ -1300,6 +1442,8 @@ static void build_tables(un_ctx* c, Tables& T) {
     emit_gemm(gp, fwd, UN_K_GEMM_FWD);
     emit_conv(cp, fwd, 1, UN_K_CONV_FWD);
     emit_attn(ap, fwd, 9);
+    emit_scan(sp_, fwd, 11);
+    emit_norm(np, fwd, 13);
   }
 
   // softmax-CE: the row pass for the models whose CE is not fused (listed
@@ -1466,6 +1610,8 @@ static void build_tables(un_ctx* c, Tables& T) {
     std::vector<GemmProb> gp;
     std::vector<ConvProb> dp;
     std::vector<AttnProb> ap;
+    std::vector<ScanProb> sp_;
+    std::vector<NormProb> np;
     std::vector<char> cat_done(c->groups.size(), 0);
     for (auto& m : c->models) {
       if (!c->active[m.blocks[0].model]) continue;
@@ -1517,6 +1663,65 @@ static void build_tables(un_ctx* c, Tables& T) {
         p.B = B;
         p.scale = (float)(1.0 / std::sqrt((double)b.N));
         ap.push_back(p);
+      } else if (b.kind == 3) {
+        // recurrence core backward: the gradient at its output -> that at the
+        // in-projection's output, gate | value
+        const Block& bi = m.blocks[lv - 1];
+        ScanProb p = scan_geometry(b, bi, B);
+        p.dh = ptr(b.G);
+        p.lddh = b.ldg;
+        p.bsdh = b.ldg * b.tokens;
+        p.o1 = ptr(bi.G);
+        p.o2 = ptr(sub(bi.G, (int64_t)b.N * (int64_t)es));
+        p.ldo = bi.ldg;
+        p.bso = bi.ldg * b.tokens;
+        sp_.push_back(p);
+      } else if (b.kind == 4) {
+        // norm backward: the gradient at its input (with the previous block's
+        // ReLU', and the skip's gradient where a residual block starts here), and
+        // partial weight gradients for the reduction, which applies the update
+        NormProb p{};
+        p.x = ptr(b.X);
+        p.ldx = b.ldx;
+        p.dy = ptr(b.G);
+        p.lddy = b.ldg;
+        p.w = (const float*)ptr(b.W32);
+        p.rstd = (float*)ptr(b.rstd);
+        p.part = (float*)ptr(b.ws);
+        p.rows = (int64_t)B * b.tokens;
+        p.d = b.N;
+        p.blocks = b.nblocks;
+        if (lv > 0) {
+          Block& pb = m.blocks[lv - 1];
+          p.y = ptr(pb.G);
+          p.ldy = pb.ldg * pb.tokens / b.tokens;
+          p.mask = pb.relu;
+          if (b.res_to >= 0) {
+            const Block& eb = m.blocks[b.res_to];
+            p.r = ptr(eb.G);
+            p.ldr = eb.ldg;
+          }
+        }
+        np.push_back(p);
+        // the reduction's tensor of one row: its last column takes the bias's place
+        ReduceProb r{};
+        r.ws = (const float*)ptr(b.ws);
+        r.ldws = b.N;
+        r.splits = b.nblocks;
+        r.O = 1;
+        r.J = b.N - 1;
+        r.C = 1;
+        r.gW = (float*)ptr(b.gW);
+        r.ldgw = b.N;
+        r.gb = (float*)ptr(sub(b.gW, (int64_t)r.J * 4));
+        r.W = (float*)ptr(b.W32);
+        r.bmaster = (float*)ptr(sub(b.W32, (int64_t)r.J * 4));
+        r.model = b.model;
+        r.s1 = sp(b.S1, 0);
+        r.s2 = sp(b.S2, 0);
+        r.sb1 = sp(b.S1, (int64_t)r.J * 4);
+        r.sb2 = sp(b.S2, (int64_t)r.J * 4);
+        rp.push_back(r);
       } else {
         const int J = b.KH * b.KH * b.C;
         if (lv > 0) {
@@ -1572,6 +1777,8 @@ static void build_tables(un_ctx* c, Tables& T) {
     }
     emit_gemm(gp, bwd, UN_K_GEMM_BWD);
     emit_attn(ap, bwd, 10);
+    emit_scan(sp_, bwd, 12);
+    emit_norm(np, bwd, 14);
     emit_conv(dp, bwd, 2, UN_K_CONV_DGRAD);
   }
   emit_conv(wp, bwd, 3, UN_K_CONV_WGRAD);
@@ -1718,7 +1925,7 @@ static un_status plan_and_alloc(un_ctx* c, bool dry = false) {
     bool any_linear0 = false, any_conv0 = false;
     for (auto& m : c->models) {
       if (m.group != (int)gi) continue;
-      if (m.blocks[0].kind == 0) any_linear0 = true;
+      if (m.blocks[0].kind != 1) any_linear0 = true;
       else any_conv0 = true;
     }
     // A first conv whose input channels are not a whole number of 16-byte
@@ -1793,6 +2000,26 @@ static un_status plan_and_alloc(un_ctx* c, bool dry = false) {
         b.ldg = b.N;
         b.G = A.take((size_t)R * b.ldg * es);
         b.P = A.take((size_t)B * b.tokens * b.tokens * 4);
+      } else if (b.kind == 3) {
+        // recurrence core: its output [R][d] and its gradient, the states its backward starts from; no weights
+        b.ldy = b.N;
+        b.Y = A.take((size_t)R * b.ldy * es);
+        b.ldg = b.N;
+        b.G = A.take((size_t)R * b.ldg * es);
+        b.states = A.take((size_t)B * scan_chunks(b.tokens) * b.N * 4);
+      } else if (b.kind == 4) {
+        b.rows = 1;
+        b.ldw = b.N;
+        b.W32 = A.take((size_t)b.N * 4);
+        b.gW = A.take((size_t)b.N * 4);
+        b.ldy = rup(b.N, 8);
+        b.Y = A.take((size_t)R * b.ldy * es);
+        b.ldg = rup(b.N, 8);
+        b.G = A.take((size_t)R * b.ldg * es);
+        b.rstd = A.take((size_t)R * 4);
+        // a thread of the reduction adds a column's partials one after the other: at most 64
+        b.nblocks = std::min(64, norm_blocks(norm_plan(bf, b.N), R));
+        b.ws_size = b.ws_limit_size = (size_t)b.nblocks * b.N * 4;  // placed in the workspace range below
       } else if (b.kind == 0) {
         b.rows = b.N;
         b.ldw = rup(b.K, 8);
@@ -2031,7 +2258,10 @@ static inline int64_t lin_col(const Block& b, int64_t col) {
 }
 
 static void to_internal(const Block& b, const float* pt, std::vector<float>& w, std::vector<float>& bias) {
-  if (b.kind == 0) {
+  if (b.kind == 4) {
+    w.assign(pt + b.pt_w, pt + b.pt_w + b.n_w);
+    bias.clear();
+  } else if (b.kind == 0) {
     w.assign((size_t)b.N * b.ldw, 0.f);
     for (int o = 0; o < b.N; ++o)
       for (int k = 0; k < b.Kr; ++k) w[(size_t)o * b.ldw + lin_col(b, k)] = pt[b.pt_w + (size_t)o * b.Kr + k];
@@ -2050,7 +2280,9 @@ static void to_internal(const Block& b, const float* pt, std::vector<float>& w, 
 }
 
 static void from_internal(const Block& b, const std::vector<float>& w, const std::vector<float>& bias, float* pt) {
-  if (b.kind == 0) {
+  if (b.kind == 4) {
+    std::copy(w.begin(), w.end(), pt + b.pt_w);
+  } else if (b.kind == 0) {
     for (int o = 0; o < b.N; ++o)
       for (int k = 0; k < b.Kr; ++k) pt[b.pt_w + (size_t)o * b.Kr + k] = w[(size_t)o * b.ldw + lin_col(b, k)];
     std::copy(bias.begin(), bias.end(), pt + b.pt_b);
@@ -2080,11 +2312,11 @@ static un_status write_blocks(un_ctx* c, int i, char* base, size_t Block::*wf, s
   Model& m = c->models[i];
   std::vector<float> w, bias;
   for (auto& b : m.blocks) {
-    if (b.kind == 2) continue;  // the attention core has no parameters
+    if (!b.has_params()) continue;
     to_internal(b, src, w, bias);
     // on the context's stream, completed before the host buffers go away
     HIPCHK(c, hipMemcpyAsync(base + b.*wf, w.data(), w.size() * 4, hipMemcpyHostToDevice, c->stream));
-    HIPCHK(c, hipMemcpyAsync(base + b.*bf, bias.data(), bias.size() * 4, hipMemcpyHostToDevice, c->stream));
+    if (!bias.empty()) HIPCHK(c, hipMemcpyAsync(base + b.*bf, bias.data(), bias.size() * 4, hipMemcpyHostToDevice, c->stream));
     HIPCHK(c, hipStreamSynchronize(c->stream));
   }
   return UN_OK;
@@ -2095,11 +2327,11 @@ static un_status read_blocks(un_ctx* c, int i, const char* base, size_t Block::*
   HIPCHK(c, hipStreamSynchronize(c->stream));
   std::vector<float> w, bias;
   for (auto& b : m.blocks) {
-    if (b.kind == 2) continue;
+    if (!b.has_params()) continue;
     w.resize((size_t)b.rows * b.ldw);
-    bias.resize(b.rows);
+    bias.resize(b.n_b ? b.rows : 0);
     HIPCHK(c, hipMemcpyAsync(w.data(), base + b.*wf, w.size() * 4, hipMemcpyDeviceToHost, c->stream));
-    HIPCHK(c, hipMemcpyAsync(bias.data(), base + b.*bf, bias.size() * 4, hipMemcpyDeviceToHost, c->stream));
+    if (!bias.empty()) HIPCHK(c, hipMemcpyAsync(bias.data(), base + b.*bf, bias.size() * 4, hipMemcpyDeviceToHost, c->stream));
     HIPCHK(c, hipStreamSynchronize(c->stream));
     from_internal(b, w, bias, dst);
   }
@@ -2121,7 +2353,11 @@ static void init_host(const Model& m, std::vector<float>& pt) {
   pt.assign(m.n_params, 0.f);
   int t = 0;
   for (auto& b : m.blocks) {
-    if (b.kind == 2) continue;
+    if (!b.has_params()) continue;
+    if (b.kind == 4) {  // ones
+      std::fill(pt.begin() + b.pt_w, pt.begin() + b.pt_w + b.n_w, 1.f);
+      continue;
+    }
     const double fan_in = b.kind == 0 ? (double)b.Kr : (double)b.Cr * b.KH * b.KH;
     const double wb = std::sqrt(6.0 / fan_in), bb = 1.0 / std::sqrt(fan_in);
     for (int part = 0; part < 2; ++part, ++t) {
@@ -2161,7 +2397,7 @@ static hipError_t run_launch(un_ctx* c, const Launch& l, float lr) {
   switch (l.kind) {
     case 0:
       e = launch_gemm(c->bf16, l.kclass == UN_K_GEMM_BWD, l.mode, c->at<GemmProb>(l.probs), c->at<int32_t>(l.map), l.count, lr,
-                      c->lrv, c->optp, c->keep_grads, c->at<int32_t>(c->ydev), c->labels_per_model, c->wsoff,
+                      c->lrv, c->optp, c->keep_grads || c->aw.any, c->at<int32_t>(c->ydev), c->labels_per_model, c->wsoff,
                       CeFinish{c->at<CeProb>(c->ce.probs), ce_part, c->losses_host, cdiv(c->maxB, CE_ROWS), c->ce.count},
                       c->stream);
       break;
@@ -2182,7 +2418,7 @@ static hipError_t run_launch(un_ctx* c, const Launch& l, float lr) {
       break;
     case 4:
       e = launch_reduce(c->bf16, c->at<ReduceProb>(l.probs), c->at<int32_t>(l.map), l.count, lr, c->lrv, c->optp,
-                        c->keep_grads, c->wsoff, c->stream);
+                        c->keep_grads || c->aw.any, c->wsoff, c->stream);
       break;
     case 5:
       e = launch_ce(c->bf16, c->at<CeProb>(l.probs), l.mode, c->at<int32_t>(c->ydev), c->labels_per_model, c->maxB,
@@ -2195,6 +2431,20 @@ static hipError_t run_launch(un_ctx* c, const Launch& l, float lr) {
     case 10:
       e = launch_attn(c->bf16, l.kind == 10, c->at<AttnProb>(l.probs), c->at<int32_t>(l.map), l.count, l.lds,
                       c->stream);
+      break;
+    case 11:
+    case 12:
+      e = launch_scan_table(c->bf16, l.kind == 12, l.mode, l.bm, c->at<ScanProb>(l.probs), c->at<int32_t>(l.map), l.count,
+                            c->stream);
+      break;
+    case 13:
+    case 14:
+      e = launch_norm_table(c->bf16, l.kind == 14, l.norm, c->at<NormProb>(l.probs), c->at<int32_t>(l.map), l.count, c->wsoff,
+                            c->stream);
+      break;
+    case 15:
+      e = launch_adamw(false, true, (const AdamwTensor*)(c->aw.mem + c->aw.tensors), (const int32_t*)(c->aw.mem + c->aw.map),
+                       l.count, AdamwHp{}, (const AdamwHp*)c->aw.mem, c->stream);
       break;
   }
   if (c->profiling && a && b) {
@@ -2416,6 +2666,14 @@ static hipError_t enqueue_step(un_ctx* c, float lr) {
     if (e != hipSuccess) return e;
     e = run_launch(c, l, lr);
   }
+  if (c->aw.nblocks > 0) {
+    if (e == hipSuccess) e = run_launch(c, Launch{15, UN_K_ADAMW, 0, 0, c->aw.nblocks}, lr);
+    // the transposed copies of conv weights (the update writes the plain ones)
+    for (size_t i = 0; i < c->models.size() && e == hipSuccess; ++i)
+      if (c->active[i] && c->opts[i].kind == UN_OPT_ADAMW8 && c->models[i].blocks[0].kind == 1)
+        e = launch_sgd(c->bf16, c->at<SgdTensor>(c->refresh.probs), c->at<int32_t>(c->refresh.map), c->refresh_rng[i].first,
+                       c->refresh_rng[i].second, 0.f, false, c->stream);
+  }
   return e;
 }
 
@@ -2445,6 +2703,13 @@ static un_status step_common(un_ctx* c, float lr, const float* lrs, float* losse
   const size_t n = c->models.size();
   if (c->any_opt) {
     std::vector<OptHp> hp(n);
+    std::vector<AdamwHp> hp8(c->aw.any ? n : 0);
+    for (size_t i = 0; i < n; ++i) {
+      const auto& o = c->opts[i];
+      const double rate = lrs ? (double)lrs[i] : (double)lr;
+      if (c->active[i] && (o.kind == UN_OPT_ADAMW || o.kind == UN_OPT_ADAMW8) && !(rate >= 0.0 && rate * o.decay < 1.0))
+        return fail(c, UN_ERR_INVALID, "model " + std::to_string(i) + ": AdamW needs 0 <= lr and lr * weight_decay < 1");
+    }
     for (size_t i = 0; i < n; ++i) {
       const auto& o = c->opts[i];
       const double rate = lrs ? (double)lrs[i] : (double)lr;
@@ -2454,7 +2719,7 @@ static un_status step_common(un_ctx* c, float lr, const float* lrs, float* losse
       h.eps = (float)o.eps;
       if (o.kind == UN_OPT_MOMENTUM) {
         h.b1 = (float)o.momentum;
-      } else if (o.kind == UN_OPT_ADAM) {
+      } else if (o.kind == UN_OPT_ADAM || o.kind == UN_OPT_ADAMW || o.kind == UN_OPT_ADAMW8) {
         const double t = (double)(o.t + 1);  // this step's count
         h.b1 = (float)o.beta1;
         h.b2 = (float)o.beta2;
@@ -2462,8 +2727,16 @@ static un_status step_common(un_ctx* c, float lr, const float* lrs, float* losse
         h.c2 = (float)(1.0 - o.beta2);
         h.lr = (float)(rate / (1.0 - std::pow(o.beta1, t)));
         h.isb2 = (float)(1.0 / std::sqrt(1.0 - std::pow(o.beta2, t)));
+        const float decay = (float)(rate * o.decay);
+        h.kind = o.kind != UN_OPT_ADAM && decay > 0.f ? -decay : (float)UN_OPT_ADAM;
+        if (o.kind == UN_OPT_ADAMW8) {
+          hp8[i] = AdamwHp{decay, h.lr, h.b1, h.b2, h.c1, h.c2, h.isb2, h.eps, (uint32_t)(o.t + 1) * 0x01000193u + 0x5EEDu};
+          h = OptHp{};  // the backward pass leaves its weights (SGD at rate 0)
+        }
       }
     }
+    if (c->aw.any)
+      HIPCHK(c, launch_set_values((float*)c->aw.mem, (const float*)hp8.data(), (int)(n * sizeof(AdamwHp) / 4), c->stream));
     HIPCHK(c, launch_set_values(c->at<float>(c->opt_dev), (const float*)hp.data(), (int)(n * OPT_FLOATS), c->stream));
     c->optp = c->at<OptHp>(c->opt_dev);
   } else if (lrs) {
@@ -2515,7 +2788,7 @@ static size_t state_layout(un_ctx* c) {
   }
   for (size_t mi = 0; mi < c->models.size(); ++mi)
     for (auto& b : c->models[mi].blocks) {
-      if (b.kind == 2) continue;
+      if (!b.has_params()) continue;
       if (b.concat) {
         const Group& g = c->groups[c->models[mi].group];
         const size_t roff = (size_t)c->cat_off[mi];
@@ -2525,9 +2798,9 @@ static size_t state_layout(un_ctx* c) {
         b.S2b = g.catS2b + roff * 4;
       } else {
         b.S1 = S.take((size_t)b.rows * b.ldw * 4);
-        b.S1b = S.take((size_t)b.rows * 4);
+        if (b.n_b) b.S1b = S.take((size_t)b.rows * 4);
         b.S2 = S.take((size_t)b.rows * b.ldw * 4);
-        b.S2b = S.take((size_t)b.rows * 4);
+        if (b.n_b) b.S2b = S.take((size_t)b.rows * 4);
       }
     }
   return S.top;
@@ -2551,9 +2824,10 @@ static un_status alloc_state(un_ctx* c) {
 static un_status clear_state(un_ctx* c, int i) {
   if (!c->sbase) return UN_OK;
   for (auto& b : c->models[i].blocks) {
-    if (b.kind == 2) continue;
+    if (!b.has_params()) continue;
     HIPCHK(c, hipMemsetAsync(c->sbase + b.S1, 0, (size_t)b.rows * b.ldw * 4, c->stream));
     HIPCHK(c, hipMemsetAsync(c->sbase + b.S2, 0, (size_t)b.rows * b.ldw * 4, c->stream));
+    if (!b.n_b) continue;
     HIPCHK(c, hipMemsetAsync(c->sbase + b.S1b, 0, (size_t)b.rows * 4, c->stream));
     HIPCHK(c, hipMemsetAsync(c->sbase + b.S2b, 0, (size_t)b.rows * 4, c->stream));
   }
@@ -2561,24 +2835,215 @@ static un_status clear_state(un_ctx* c, int i) {
   return UN_OK;
 }
 
-static int state_tensors(int kind) { return kind == UN_OPT_ADAM ? 2 : kind == UN_OPT_MOMENTUM ? 1 : 0; }
+static int state_tensors(int kind) {
+  return kind == UN_OPT_ADAM || kind == UN_OPT_ADAMW || kind == UN_OPT_ADAMW8 ? 2 : kind == UN_OPT_MOMENTUM ? 1 : 0;
+}
+
+// ---- AdamW with 8-bit states ------------------------------------------------
+// One tensor of a model as its state sees it: the weights or the bias of a
+// block, n consecutive floats as they lie in the arena (padding columns
+// included: weight, gradient and state are 0 there and stay 0). Offsets of its
+// codes and scales in the model's state allocation; number of its first value.
+struct Tensor8 {
+  const Block* b;
+  bool bias;
+  int64_t n;
+  size_t m, v, ms, vs;
+  uint32_t base;
+};
+static size_t layout8(const Model& mod, std::vector<Tensor8>& out) {
+  Arena S;
+  uint32_t base = 0;
+  for (auto& b : mod.blocks)
+    for (int part = 0; part < 2 && b.has_params(); ++part) {
+      if (part == 1 && !b.n_b) continue;
+      Tensor8 t{&b, part == 1, part == 1 ? (int64_t)b.rows : (int64_t)b.rows * b.ldw, 0, 0, 0, 0, base};
+      const size_t blocks = (size_t)(t.n + AW_BLOCK - 1) / AW_BLOCK;
+      t.m = S.take((size_t)t.n);
+      t.v = S.take((size_t)t.n);
+      t.ms = S.take(blocks);
+      t.vs = S.take(blocks);
+      base += (uint32_t)(blocks * AW_BLOCK);
+      out.push_back(t);
+    }
+  return S.top;
+}
+
+// The table of every active 8-bit model's tensors, into `mem` (of `cap` bytes;
+// NULL: only *need, the size with all of them active). The stream is idle.
+static un_status table8(un_ctx* c, char* mem, size_t cap, size_t* need, un_ctx::Adamw8* out) {
+  std::vector<AdamwTensor> ts;
+  std::vector<int32_t> map;
+  for (size_t i = 0; i < c->models.size(); ++i) {
+    const char* q = c->opts[i].state8;
+    if (!q || (mem && !c->active[i])) continue;
+    std::vector<Tensor8> t8;
+    layout8(c->models[i], t8);
+    for (auto& t : t8) {
+      const Block& b = *t.b;
+      AdamwTensor a{};
+      a.p = c->at<float>(t.bias ? b.b32 : b.W32);
+      a.g = c->at<float>(t.bias ? b.gb : b.gW);
+      a.copy = t.bias ? nullptr : c->at<uint16_t>(b.Wb);
+      a.m = (void*)(q + t.m);
+      a.v = (void*)(q + t.v);
+      a.ms = (uint8_t*)q + t.ms;
+      a.vs = (uint8_t*)q + t.vs;
+      a.n = t.n;
+      a.base = t.base;
+      a.hp = (int32_t)i;
+      for (int64_t k = 0; k < (t.n + AW_CHUNK - 1) / AW_CHUNK; ++k) {
+        map.push_back((int32_t)ts.size());
+        map.push_back((int32_t)k);
+      }
+      ts.push_back(a);
+    }
+  }
+  un_ctx::Adamw8 r;
+  r.tensors = (size_t)rup((int64_t)(c->models.size() * sizeof(AdamwHp)), 256);
+  r.map = (size_t)rup((int64_t)(r.tensors + ts.size() * sizeof(AdamwTensor)), 256);
+  const size_t total = r.map + map.size() * 4;
+  if (need) *need = total + 256;
+  if (!mem) return UN_OK;
+  if (total > cap) return fail(c, UN_ERR_UNSUPPORTED, "8-bit optimizer table exceeds its allocation");
+  r.mem = mem;
+  r.nblocks = (int)(map.size() / 2);
+  r.any = out->any;
+  if (!ts.empty()) {
+    HIPCHK(c, hipMemcpyAsync(mem + r.tensors, ts.data(), ts.size() * sizeof(AdamwTensor), hipMemcpyHostToDevice, c->stream));
+    HIPCHK(c, hipMemcpyAsync(mem + r.map, map.data(), map.size() * 4, hipMemcpyHostToDevice, c->stream));
+    HIPCHK(c, hipStreamSynchronize(c->stream));
+  }
+  r.cap = cap;
+  *out = r;
+  return UN_OK;
+}
+
+// Gives model i (the stream idle) a fresh 8-bit state, or takes it away, with a
+// table of what there is then. On failure nothing has changed.
+static un_status set_state8(un_ctx* c, int i, bool on) {
+  char*& q = c->opts[i].state8;
+  if (!on && !q) return UN_OK;
+  std::vector<Tensor8> t8;
+  const size_t bytes = layout8(c->models[i], t8);
+  char* const had = q;
+  char* fresh = nullptr;
+  if (on) {
+    if (!had && hipMalloc((void**)&fresh, bytes) != hipSuccess) {
+      (void)hipGetLastError();
+      return fail(c, UN_ERR_OOM, "8-bit optimizer state: hipMalloc of " + std::to_string(bytes) + " bytes failed");
+    }
+    q = had ? had : fresh;
+  } else {
+    q = nullptr;
+  }
+  bool any = false;
+  for (auto& o : c->opts) any = any || o.state8;
+  un_ctx::Adamw8 next;
+  next.any = any;
+  un_status st = UN_OK;
+  if (any) {
+    size_t need = 0;
+    char* mem = nullptr;
+    table8(c, nullptr, 0, &need, nullptr);
+    if (hipMalloc((void**)&mem, need) != hipSuccess) {
+      (void)hipGetLastError();
+      st = fail(c, UN_ERR_OOM, "8-bit optimizer table: hipMalloc of " + std::to_string(need) + " bytes failed");
+    } else {
+      st = table8(c, mem, need, nullptr, &next);
+      if (st != UN_OK) hipFree(mem);
+    }
+  }
+  if (st != UN_OK) {
+    q = had;
+    if (fresh) hipFree(fresh);
+    return st;
+  }
+  if (c->aw.mem) hipFree(c->aw.mem);
+  c->aw = next;
+  if (!on) hipFree(had);
+  else {
+    HIPCHK(c, hipMemsetAsync(q, 0, bytes, c->stream));
+    HIPCHK(c, hipStreamSynchronize(c->stream));
+  }
+  return UN_OK;
+}
+
+// The moments of model i's 8-bit state as floats in the PyTorch layout (which:
+// 0 the first, 1 the second), and back (nearest codes; u = sqrt(v) that is not
+// zero never becomes zero).
+static un_status read_state8(un_ctx* c, int i, float* dst) {
+  std::vector<Tensor8> t8;
+  const size_t bytes = layout8(c->models[i], t8), np = c->models[i].n_params;
+  std::vector<uint8_t> q(bytes);
+  HIPCHK(c, hipMemcpyAsync(q.data(), c->opts[i].state8, bytes, hipMemcpyDeviceToHost, c->stream));
+  HIPCHK(c, hipStreamSynchronize(c->stream));
+  std::vector<float> w, bias;
+  for (int which = 0; which < 2; ++which)
+    for (size_t k = 0; k < t8.size(); ++k) {
+      const Tensor8& t = t8[k];
+      std::vector<float>& x = t.bias ? bias : w;
+      x.resize((size_t)t.n);
+      for (int64_t e = 0; e < t.n; ++e) {
+        const float f = std::ldexp(e4m3_value(q[(which ? t.v : t.m) + e]), (int)q[(which ? t.vs : t.ms) + e / AW_BLOCK] - 127);
+        x[(size_t)e] = which ? f * f : f;
+      }
+      if (!t.b->n_b) bias.clear();
+      if (t.bias || !t.b->n_b) from_internal(*t.b, w, bias, dst + which * np);
+    }
+  return UN_OK;
+}
+static un_status write_state8(un_ctx* c, int i, const float* src) {
+  std::vector<Tensor8> t8;
+  const size_t bytes = layout8(c->models[i], t8), np = c->models[i].n_params;
+  for (size_t e = 0; e < 2 * np; ++e)
+    if (!std::isfinite(src[e]) || (e >= np && src[e] < 0.f))
+      return fail(c, UN_ERR_INVALID, "8-bit states hold finite moments, the second not negative");
+  std::vector<uint8_t> q(bytes, 0);
+  std::vector<float> w, bias;
+  for (int which = 0; which < 2; ++which)
+    for (auto& t : t8) {
+      if (!t.bias) to_internal(*t.b, src + which * np, w, bias);
+      const std::vector<float>& x = t.bias ? bias : w;
+      for (int64_t b0 = 0; b0 < t.n; b0 += AW_BLOCK) {
+        const int64_t b1 = std::min(t.n, b0 + AW_BLOCK);
+        float top = 0.f;
+        auto at = [&](int64_t e) { return which ? std::sqrt(x[(size_t)e]) : x[(size_t)e]; };
+        for (int64_t e = b0; e < b1; ++e) top = std::max(top, std::fabs(at(e)));
+        const int ex = scale_exponent(top);
+        q[(which ? t.vs : t.ms) + b0 / AW_BLOCK] = (uint8_t)(ex + 127);
+        for (int64_t e = b0; e < b1; ++e) {
+          uint8_t code = e4m3_code(std::ldexp(at(e), -ex));
+          if (which && code == 0 && x[(size_t)e] > 0.f) code = 1;
+          q[(which ? t.v : t.m) + e] = code;
+        }
+      }
+    }
+  HIPCHK(c, hipMemcpyAsync(c->opts[i].state8, q.data(), bytes, hipMemcpyHostToDevice, c->stream));
+  HIPCHK(c, hipStreamSynchronize(c->stream));
+  return UN_OK;
+}
 
 un_status un_set_optimizer(un_ctx* c, int32_t i, const un_optimizer* o) {
   CHECK_CTX(c);
   if (i < 0 || i >= (int)c->models.size()) return fail(c, UN_ERR_RANGE, "model index out of range");
   if (!o) return fail(c, UN_ERR_INVALID, "optimizer is NULL");
   auto unit = [](float x) { return std::isfinite(x) && x >= 0.f && x < 1.f; };
-  if (o->kind != UN_OPT_SGD && o->kind != UN_OPT_MOMENTUM && o->kind != UN_OPT_ADAM)
+  const bool wd = o->kind == UN_OPT_ADAMW || o->kind == UN_OPT_ADAMW8;
+  if (o->kind != UN_OPT_SGD && o->kind != UN_OPT_MOMENTUM && o->kind != UN_OPT_ADAM && !wd)
     return fail(c, UN_ERR_INVALID, "unknown optimizer kind");
   if (o->kind == UN_OPT_MOMENTUM && !unit(o->momentum)) return fail(c, UN_ERR_INVALID, "momentum must be in [0, 1)");
-  if (o->kind == UN_OPT_ADAM && (!unit(o->beta1) || !unit(o->beta2) || !std::isfinite(o->eps) || !(o->eps > 0.f)))
+  if ((o->kind == UN_OPT_ADAM || wd) && (!unit(o->beta1) || !unit(o->beta2) || !std::isfinite(o->eps) || !(o->eps > 0.f)))
     return fail(c, UN_ERR_INVALID, "Adam needs beta1, beta2 in [0, 1) and eps > 0");
+  if (wd && (!std::isfinite(o->weight_decay) || o->weight_decay < 0.f))
+    return fail(c, UN_ERR_INVALID, "AdamW needs weight_decay finite and >= 0");
   HIPCHK(c, hipStreamSynchronize(c->stream));
-  if (o->kind != UN_OPT_SGD && !c->sbase) {
+  if (o->kind != UN_OPT_SGD && o->kind != UN_OPT_ADAMW8 && !c->sbase) {
     un_status st = alloc_state(c);
     if (st != UN_OK) return st;
   }
   un_status st = clear_state(c, i);
+  if (st == UN_OK) st = set_state8(c, i, o->kind == UN_OPT_ADAMW8);
   if (st != UN_OK) return st;
   un_ctx::Opt& d = c->opts[i];
   d.kind = o->kind;
@@ -2586,6 +3051,7 @@ un_status un_set_optimizer(un_ctx* c, int32_t i, const un_optimizer* o) {
   d.beta1 = o->beta1;
   d.beta2 = o->beta2;
   d.eps = o->eps;
+  d.decay = wd ? o->weight_decay : 0.0;
   d.t = 0;
   c->any_opt = false;
   for (auto& x : c->opts) c->any_opt = c->any_opt || x.kind != UN_OPT_SGD;
@@ -2601,6 +3067,7 @@ un_status un_get_opt_state(un_ctx* c, int32_t i, float* dst, size_t cap, size_t*
   if (step) *step = c->opts[i].t;
   if (!dst || k == 0) return UN_OK;
   if (cap < k * np) return fail(c, UN_ERR_BUFSIZE, "buffer holds " + std::to_string(cap) + " < " + std::to_string(k * np));
+  if (c->opts[i].kind == UN_OPT_ADAMW8) return read_state8(c, i, dst);
   un_status st = read_blocks(c, i, c->sbase, &Block::S1, &Block::S1b, dst);
   if (st == UN_OK && k == 2) st = read_blocks(c, i, c->sbase, &Block::S2, &Block::S2b, dst + np);
   return st;
@@ -2615,7 +3082,10 @@ un_status un_set_opt_state(un_ctx* c, int32_t i, const float* src, size_t n, int
   if (step < 0) return fail(c, UN_ERR_INVALID, "negative step count");
   if (k > 0 && !src) return fail(c, UN_ERR_INVALID, "src is NULL");
   HIPCHK(c, hipStreamSynchronize(c->stream));
-  if (k > 0) {
+  if (c->opts[i].kind == UN_OPT_ADAMW8) {
+    un_status st = write_state8(c, i, src);
+    if (st != UN_OK) return st;
+  } else if (k > 0) {
     un_status st = write_blocks(c, i, c->sbase, &Block::S1, &Block::S1b, src);
     if (st == UN_OK && k == 2) st = write_blocks(c, i, c->sbase, &Block::S2, &Block::S2b, src + np);
     if (st != UN_OK) return st;
@@ -2668,6 +3138,10 @@ un_status un_set_active(un_ctx* c, const uint8_t* mask) {
   if (st != UN_OK) {
     c->active = before;
     return st;
+  }
+  if (c->aw.any) {
+    st = table8(c, c->aw.mem, c->aw.cap, nullptr, &c->aw);
+    if (st != UN_OK) return st;
   }
   // Models that sat out some steps kept their transposed weight copy in the
   // buffer of that time; rewrite every model's current copies from the master.
@@ -2732,7 +3206,7 @@ un_status un_graph_capture(un_ctx* c, float lr) {
   if (!c->all_loaded()) return fail(c, UN_ERR_STATE, "un_graph_capture before a batch of every input group is loaded");
   if (!std::isfinite(lr)) return fail(c, UN_ERR_INVALID, "lr is not finite");
   if (c->any_opt)
-    return fail(c, UN_ERR_UNSUPPORTED, "a model has a momentum / Adam optimizer (its hyper-parameters change every step)");
+    return fail(c, UN_ERR_UNSUPPORTED, "a model has an optimizer with state (its hyper-parameters change every step)");
   HIPCHK(c, hipStreamSynchronize(c->stream));
   if (c->gexec) hipGraphExecDestroy(c->gexec);
   if (c->graph) hipGraphDestroy(c->graph);
@@ -2876,6 +3350,9 @@ void un_destroy(un_ctx* c) {
   if (c->graph) hipGraphDestroy(c->graph);
   if (c->base) hipFree(c->base);
   if (c->sbase) hipFree(c->sbase);
+  if (c->aw.mem) hipFree(c->aw.mem);
+  for (auto& o : c->opts)
+    if (o.state8) hipFree(o.state8);
   if (c->losses_host) g_losses.give(c->losses_host, c->models.size() * 4);
   if (c->own_stream) hipStreamDestroy(c->own_stream);
   delete c;

@@ -21,11 +21,13 @@ UN_OK, UN_ERR_INVALID, UN_ERR_STATE, UN_ERR_OOM, UN_ERR_DEVICE, UN_ERR_RANGE, UN
 STATUS_NAMES = ["UN_OK", "UN_ERR_INVALID", "UN_ERR_STATE", "UN_ERR_OOM", "UN_ERR_DEVICE", "UN_ERR_RANGE",
                 "UN_ERR_BUFSIZE", "UN_ERR_UNSUPPORTED"]
 UN_F32, UN_BF16_F32MASTER = 0, 1
-UN_OPT_SGD, UN_OPT_MOMENTUM, UN_OPT_ADAM = 0, 1, 2
-OPT_KINDS = {"sgd": UN_OPT_SGD, "momentum": UN_OPT_MOMENTUM, "adam": UN_OPT_ADAM}
+UN_OPT_SGD, UN_OPT_MOMENTUM, UN_OPT_ADAM, UN_OPT_ADAMW, UN_OPT_ADAMW8 = range(5)
+OPT_KINDS = {"sgd": UN_OPT_SGD, "momentum": UN_OPT_MOMENTUM, "adam": UN_OPT_ADAM, "adamw": UN_OPT_ADAMW,
+             "adamw8": UN_OPT_ADAMW8}
 OPS = {"linear": 0, "conv": 1, "relu": 2, "pool": 3, "flatten": 4, "res_begin": 5, "res_end": 6, "unflatten": 7,
-       "attention": 8}
-KERNEL_CLASSES = ["gemm_fwd", "gemm_bwd", "conv_fwd", "conv_dgrad", "conv_wgrad", "ce", "sgd", "other", "attn"]
+       "attention": 8, "rms_norm": 9, "recurrence": 10}
+KERNEL_CLASSES = ["gemm_fwd", "gemm_bwd", "conv_fwd", "conv_dgrad", "conv_wgrad", "ce", "sgd", "other", "attn",
+                  "recurrence", "norm", "adamw"]
 
 # Every symbol the header declares.
 EXPORTS = ["un_create", "un_create_grouped", "un_plan_bytes", "un_plan_bytes_grouped", "un_load_group_batch",
@@ -54,7 +56,7 @@ class un_input_spec(ctypes.Structure):
 
 class un_optimizer(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("momentum", ctypes.c_float), ("beta1", ctypes.c_float),
-                ("beta2", ctypes.c_float), ("eps", ctypes.c_float)]
+                ("beta2", ctypes.c_float), ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float)]
 
 
 def _struct(name, **fields):
@@ -310,10 +312,11 @@ def un_get_grads(ctx, i):
     return out
 
 
-def un_set_optimizer(ctx, i, kind="sgd", momentum=0.0, betas=(0.9, 0.999), eps=1e-8):
+def un_set_optimizer(ctx, i, kind="sgd", momentum=0.0, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01):
     if kind not in OPT_KINDS:
         raise ValueError(f"optimizer kind must be one of {sorted(OPT_KINDS)}")
-    o = un_optimizer(OPT_KINDS[kind], float(momentum), float(betas[0]), float(betas[1]), float(eps))
+    o = un_optimizer(OPT_KINDS[kind], float(momentum), float(betas[0]), float(betas[1]), float(eps),
+                     float(weight_decay))
     _check(lib().un_set_optimizer(ctx, i, ctypes.byref(o)), ctx)
 
 
@@ -492,11 +495,14 @@ class Hybrid:
     def get_grads(self, i):
         return un_get_grads(self.ctx, i)
 
-    def set_optimizer(self, i, kind="sgd", momentum=0.0, betas=(0.9, 0.999), eps=1e-8):
-        """Fresh optimizer for model i ("sgd", "momentum" or "adam")."""
-        un_set_optimizer(self.ctx, i, kind, momentum, betas, eps)
+    def set_optimizer(self, i, kind="sgd", momentum=0.0, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01):
+        """Fresh optimizer for model i ("sgd", "momentum", "adam", "adamw" or,
+        with its state in 8 bits, "adamw8"; weight_decay is the last two's)."""
+        un_set_optimizer(self.ctx, i, kind, momentum, betas, eps, weight_decay)
         self.optimizers[i] = dict(kind=kind, momentum=float(momentum), betas=[float(b) for b in betas],
                                   eps=float(eps))
+        if kind.startswith("adamw"):
+            self.optimizers[i]["weight_decay"] = float(weight_decay)
 
     def get_opt_state(self, i):
         return un_get_opt_state(self.ctx, i)

@@ -31,6 +31,8 @@ Design overview):
 * ``("unflatten", T)``             flat features as T tokens (a sequence); a
   following ``linear`` acts on every token
 * ``("attention",)``               single-head self-attention on a sequence
+* ``("rms_norm",)``                root-mean-square norm over the features, with a weight
+* ``("recurrence",)``              gated linear recurrence over a sequence's tokens
 """
 from __future__ import annotations
 
@@ -41,7 +43,7 @@ from dataclasses import dataclass, field
 import numpy as np
 
 OP_CODES = {"linear": 0, "conv": 1, "relu": 2, "pool": 3, "flatten": 4, "res_begin": 5, "res_end": 6,
-            "unflatten": 7, "attention": 8}
+            "unflatten": 7, "attention": 8, "rms_norm": 9, "recurrence": 10}
 
 
 @dataclass
@@ -106,18 +108,27 @@ def param_shapes(spec, in_shape):
         elif op == "attention":
             d = shape[-1]
             out += [((3 * d, d), d), ((3 * d,), d), ((d, d), d), ((d,), d)]
+        elif op == "recurrence":
+            d = shape[-1]
+            out += [((2 * d, d), d), ((2 * d,), d), ((d, d), d), ((d,), d)]
+        elif op == "rms_norm":
+            out.append(((shape[-1],), 0))  # fan-in 0: a norm's weight, which starts at one
     return out
 
 
 def init_params(spec, in_shape, seed, model_index, rule="kaiming"):
     """Initial parameters, fp32: biases U(+-1/sqrt(fan_in)); weights
     U(+-sqrt(6/fan_in)) (Kaiming/He uniform, rule "kaiming") or U(+-1/sqrt(fan_in))
-    (rule "torch", the bound of PyTorch's own Linear / Conv2d initialisation)."""
+    (rule "torch", the bound of PyTorch's own Linear / Conv2d initialisation);
+    a norm's weights are ones."""
     if rule not in ("kaiming", "torch"):
         raise ValueError(f"unknown init rule {rule!r}")
     rng = np.random.default_rng([seed, 1, model_index])
     params = []
     for shape, fan_in in param_shapes(spec, in_shape):
+        if fan_in == 0:
+            params.append(np.ones(shape, dtype=np.float32))
+            continue
         wbound = math.sqrt(6.0 / fan_in) if rule == "kaiming" else 1.0 / math.sqrt(fan_in)
         bound = wbound if len(shape) > 1 else 1.0 / math.sqrt(fan_in)
         params.append(rng.uniform(-bound, bound, size=shape).astype(np.float32))
@@ -273,6 +284,32 @@ def attn8(seed=0):
 
 
 WORKLOADS["attn8"] = attn8
+
+
+def recur8(seed=0):
+    """N=8 gated-recurrence classifiers on synthetic token sequences: the input
+    [64, 8192] is 128 tokens of 64 features; each model embeds the tokens
+    (token-wise Linear to a width from {64, 128}), then 1-2 blocks of
+    [x + recurrence(norm(x)), x + MLP(norm(x)) of twice the width], a last norm, a
+    token-wise Linear to 8, flatten and Linear-10. bf16 with fp32 master weights."""
+    rng = np.random.default_rng([seed, 6])
+    T, d0 = 128, 64
+    RB, RE, R, NRM = ("res_begin",), ("res_end",), ("relu",), ("rms_norm",)
+    specs = []
+    for _ in range(8):
+        width = int(rng.choice([64, 128]))
+        blocks = int(rng.integers(1, 3))
+        layers = [("unflatten", T), ("linear", width)]
+        for _ in range(blocks):
+            layers += [RB, NRM, ("recurrence",), RE, RB, NRM, ("linear", 2 * width), R, ("linear", width), RE]
+        layers += [NRM, ("linear", 8), ("flatten",), ("linear", 10)]
+        specs.append({"layers": layers, "num_classes": 10})
+    return Workload("recur8_b64_bf16", 8, 64, (T * d0,), "bf16", specs, 0.01, 5, seed,
+                    "8 gated-recurrence classifiers (128 tokens x 64 features, 1-2 pre-norm recurrence + MLP blocks, "
+                    "widths {64,128}) on [64,8192], bf16 with fp32 master", init="torch")
+
+
+WORKLOADS["recur8"] = recur8
 
 
 def get(name, seed=0) -> Workload:
