@@ -18,8 +18,8 @@ un_status fail_call(un_status s, const char* msg);
 // RMS norm of rows of d values:  s = x + r (rounded to the type),
 // q = 1 / sqrt(mean(s^2) + eps),  y = s q w.
 // Backward: dx = ds + q (dy w - s q mean(dy w s q)), dw = sum over rows of dy s q.
-// A row belongs to `tpr` threads, each holding up to NORM_REGS of its values in
-// registers, so every operand is read once.
+// A row belongs to `tpr` threads that hold its values in registers, so every
+// operand is read once.
 // ---------------------------------------------------------------------------
 struct NormProb {
   const void* x;       // forward: input; backward: the stored sum s
@@ -38,11 +38,12 @@ struct NormProb {
   int32_t blocks;      // backward: workgroups of this problem
   float eps;
 };
-constexpr int NORM_REGS = 32;            // most values of a row per thread (16 with 1024 threads a row)
-constexpr int NORM_MAX_D = 1024 * NORM_REGS / 2;
+constexpr int NORM_MAX_D = 1024 * 16;
+constexpr int NORM_R = 4;                // 16-byte vectors per thread and operand at a time: rows x vectors of a row
 struct NormPlan {
   int tpr, nv;         // threads per row; 16-byte vectors per thread
-  int group;           // rows of a workgroup at a time
+  int group;           // rows side by side in a workgroup
+  int rows;            // rows of a workgroup at a time
 };
 NormPlan norm_plan(bool bf16, int d);
 // workgroups of a backward pass over `rows` rows

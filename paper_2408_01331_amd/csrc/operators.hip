@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "operators.h"
 
@@ -105,164 +106,228 @@ template <int N> __device__ __forceinline__ void load_f32(const float* p, int n,
   }
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+// Reductions over the 16 lanes of a DPP row (quad swaps, then the halves of a
+// row mirrored), whose result every lane of the row has, and over a wave (the
+// four rows' values read to scalars, in order). No LDS traffic.
+template <typename F> __device__ __forceinline__ float row16(float v, F&& op) {
+  auto dpp = [](float x, auto ctrl) {
+    const int i = __float_as_int(x);
+    return __int_as_float(__builtin_amdgcn_update_dpp(i, i, decltype(ctrl)::value, 0xf, 0xf, false));
+  };
+  v = op(v, dpp(v, std::integral_constant<int, 0xB1>{}));   // quad_perm [1, 0, 3, 2]
+  v = op(v, dpp(v, std::integral_constant<int, 0x4E>{}));   // quad_perm [2, 3, 0, 1]
+  v = op(v, dpp(v, std::integral_constant<int, 0x141>{}));  // row_half_mirror
+  v = op(v, dpp(v, std::integral_constant<int, 0x140>{}));  // row_mirror
   return v;
 }
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-  return v;
+template <typename F> __device__ __forceinline__ float wave64(float v, F&& op) {
+  v = row16(v, op);
+  auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+  return op(op(lane(0), lane(16)), op(lane(32), lane(48)));
 }
+struct Add {
+  __device__ float operator()(float a, float b) const { return a + b; }
+};
+struct Max {
+  __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+__device__ __forceinline__ float wave_max(float v) { return wave64(v, Max{}); }
 
-// Sum / maximum over the TPR threads of a row (TPR 64: a wave; else the whole
-// workgroup, through `sm`, one float per wave, in wave order). `sm` is free
-// again after the next barrier.
-template <int TPR> __device__ __forceinline__ float row_sum(float v, float* sm) {
-  v = wave_sum(v);
-  if constexpr (TPR > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
+// v[r] <- the reduction over the TPR threads of a row (16: a DPP row, 64: a
+// wave, else the whole workgroup through `sm`, R floats per wave, in wave
+// order), for R rows at once. `flip` alternates between calls: the halves of sm
+// take turns, so a call needs one barrier.
+template <int TPR, int R, typename F> __device__ __forceinline__ void row_reduce(float (&v)[R], F op, float* sm, int& flip) {
+  if constexpr (TPR == 16) {
 #pragma unroll
-    for (int w = 0; w < TPR / 64; ++w) v += sm[w];
-  }
-  return v;
-}
-template <int TPR> __device__ __forceinline__ float row_max(float v, float* sm) {
-  v = wave_max(v);
-  if constexpr (TPR > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = sm[0];
+    for (int r = 0; r < R; ++r) v[r] = row16(v[r], op);
+  } else {
 #pragma unroll
-    for (int w = 1; w < TPR / 64; ++w) v = fmaxf(v, sm[w]);
+    for (int r = 0; r < R; ++r) v[r] = wave64(v[r], op);
   }
-  return v;
+  if constexpr (TPR > 64) {
+    float* buf = sm + flip * (TPR / 64) * R;
+    flip ^= 1;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int r = 0; r < R; ++r) buf[(threadIdx.x >> 6) * R + r] = v[r];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = buf[r];
+#pragma unroll
+    for (int w = 1; w < TPR / 64; ++w)
+#pragma unroll
+      for (int r = 0; r < R; ++r) v[r] = op(v[r], buf[w * R + r]);
+  }
 }
 
 // ---------------------------------------------------------------------------
-// RMS norm, forward
+// RMS norm. A row belongs to TPR threads of NV 16-byte vectors each; a
+// workgroup holds G = NT / TPR rows side by side and R in each thread, so R
+// rows' loads are in flight together and share one reduction's latency and one
+// load of the weights.
 // ---------------------------------------------------------------------------
-template <typename T, int TPR, int NV, bool E4M3>
-__device__ __forceinline__ void norm_fwd_row(const NormProb& p, int64_t row, float* sm) {
-  constexpr int N = V16<T>::N;
+constexpr int norm_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
+template <int TPR, int R> constexpr int norm_sm() { return TPR > 64 ? 2 * TPR / 64 * R : 1; }
+
+template <typename T, int NV> struct RowVec {
+  static constexpr int N = V16<T>::N;
+  u32x4 raw[NV];
+  __device__ void load(const T* p, const int (&cnt)[NV], int step, int t) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const T* q = p + (j * step + t) * N;
+      if (cnt[j] == N) raw[j] = *(const u32x4_a2*)q;
+      else {
+        float f[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = e < cnt[j] ? V16<T>::load1(q + e) : 0.f;
+        raw[j] = V16<T>::pack(f);
+      }
+    }
+  }
+  __device__ void get(int j, float* f) const { V16<T>::unpack(raw[j], f); }
+  // From here on the values come from the packed ones again: keeping both over
+  // a reduction costs more registers than the unpacking costs time.
+  __device__ void forget() {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(raw[j]));
+  }
+};
+// rows per thread at a time: as many as leave registers for two workgroups more
+template <int TPR, int NV> constexpr int norm_rows() { return std::max(1, (TPR == 1024 ? NORM_R / 2 : NORM_R) / NV); }
+
+template <typename T, int TPR, int NV, int R, bool E4M3>
+__device__ __forceinline__ void norm_fwd_rows(const NormProb& p, int64_t row0, float* sm) {
+  constexpr int N = V16<T>::N, G = norm_threads(TPR) / TPR;
   const int t = threadIdx.x & (TPR - 1), d = p.d;
-  const bool live = row < p.rows;  // a wave or workgroup as a whole; it keeps up with the barriers
-  const int64_t at = live ? row : 0;
-  const T* x = (const T*)p.x + at * p.ldx;
-  const T* r = p.r ? (const T*)p.r + at * p.ldr : nullptr;
-  float f[NV][N];
-  int cnt[NV];
+  int cnt[NV], flip = 0;
+  float w[NV][N];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = (j * TPR + t) * N;
-    cnt[j] = live ? min(max(d - c, 0), N) : 0;
-    load_vec<T>(x + c, cnt[j], f[j]);
+    cnt[j] = min(max(d - c, 0), N);
+    load_f32<N>(p.w + c, cnt[j], w[j]);
   }
-  if (r) {
-    float g[NV][N];
+  row0 += threadIdx.x / TPR;
+  RowVec<T, NV> x[R], r[R];
+  int live[R][NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) load_vec<T>(r + (j * TPR + t) * N, cnt[j], g[j]);
+  for (int k = 0; k < R; ++k) {
+    const int64_t row = row0 + (int64_t)k * G, at = row < p.rows ? row : 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int e = 0; e < N; ++e) f[j][e] = V16<T>::round(f[j][e] + g[j][e]);  // the norm is that of the stored sum
+    for (int j = 0; j < NV; ++j) live[k][j] = row < p.rows ? cnt[j] : 0;
+    x[k].load((const T*)p.x + at * p.ldx, live[k], TPR, t);
+    if (p.r) r[k].load((const T*)p.r + at * p.ldr, live[k], TPR, t);
   }
-  if (p.s) {
-    T* s = (T*)p.s + at * p.lds;
+  float sum[R];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) store_vec<T>(s + (j * TPR + t) * N, cnt[j], f[j]);
-  }
-  float ss = 0.f;
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int e = 0; e < N; ++e) ss = fmaf(f[j][e], f[j][e], ss);
-  ss = row_sum<TPR>(ss, sm);
-  const float q = 1.f / sqrtf(ss / (float)d + p.eps);
-  if (live && p.rstd && t == 0) p.rstd[row] = q;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    float w[N];
-    load_f32<N>(p.w + (j * TPR + t) * N, cnt[j], w);
-#pragma unroll
-    for (int e = 0; e < N; ++e) f[j][e] = f[j][e] * q * w[e];
-  }
-  if constexpr (!E4M3) {
-    T* y = (T*)p.y + at * p.ldy;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) store_vec<T>(y + (j * TPR + t) * N, cnt[j], f[j]);
-  } else {
-    float m = 0.f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(f[j][e]));
-    m = row_max<TPR>(m, sm);
-    // the row's largest value becomes 448, e4m3's largest; a row of zeros keeps a scale that is not zero
-    const float scale = fmaxf(m, 1e-30f) / 448.f, inv = 448.f / fmaxf(m, 1e-30f);
-    if (live && t == 0) p.scale[row] = scale;
-    uint8_t* y = (uint8_t*)p.y + at * p.ldy;
+  for (int k = 0; k < R; ++k) {
+    const int64_t row = row0 + (int64_t)k * G;
+    sum[k] = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      uint32_t code[N / 4];
+      float f[N];
+      x[k].get(j, f);
+      if (p.r) {
+        float g[N];
+        r[k].get(j, g);
 #pragma unroll
-      for (int e = 0; e < N; e += 4) {
-        // the product may pass 448 by its rounding (a NaN stays one)
-        float v[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          v[k] = f[j][e + k] * inv;
-          v[k] = fabsf(v[k]) > 448.f ? copysignf(448.f, v[k]) : v[k];
-        }
-        int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
-        code[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
+        for (int e = 0; e < N; ++e) f[e] += g[e];
+        x[k].raw[j] = V16<T>::pack(f);
+        x[k].get(j, f);  // the norm is that of the stored sum
       }
-      uint8_t* o = y + (j * TPR + t) * N;
-      if (cnt[j] == N) {
-        if constexpr (N == 8) *(u32x2_a1*)o = u32x2{code[0], code[1]};
-        else *(u32_a1*)o = code[0];
-      } else {
+      if (p.s) store_vec<T>((T*)p.s + row * p.lds + (j * TPR + t) * N, live[k][j], f);
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (e < cnt[j]) o[e] = (uint8_t)(code[e / 4] >> (8 * (e % 4)));
+      for (int e = 0; e < N; ++e) sum[k] = fmaf(f[e], f[e], sum[k]);
+    }
+  }
+  row_reduce<TPR, R>(sum, Add{}, sm, flip);
+#pragma unroll
+  for (int k = 0; k < R; ++k) x[k].forget();
+  float q[R], top[R];
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const int64_t row = row0 + (int64_t)k * G;
+    q[k] = 1.f / sqrtf(sum[k] / (float)d + p.eps);
+    if (p.rstd && t == 0 && row < p.rows) p.rstd[row] = q[k];
+    top[k] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float f[N];
+      x[k].get(j, f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        f[e] = f[e] * q[k] * w[j][e];
+        top[k] = fmaxf(top[k], fabsf(f[e]));
+      }
+      if constexpr (!E4M3) store_vec<T>((T*)p.y + row * p.ldy + (j * TPR + t) * N, live[k][j], f);
+    }
+  }
+  if constexpr (E4M3) {
+    row_reduce<TPR, R>(top, Max{}, sm, flip);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      x[k].forget();
+      const int64_t row = row0 + (int64_t)k * G;
+      // the row's largest value becomes 448, e4m3's largest; a row of zeros keeps a scale that is not zero
+      const float m = fmaxf(top[k], 1e-30f), inv = 448.f / m;
+      if (t == 0 && row < p.rows) p.scale[row] = m / 448.f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        float f[N];
+        x[k].get(j, f);
+        uint32_t code[N / 4];
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+          // the product may pass 448 by its rounding (a NaN stays one)
+          float v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            v[i] = f[e + i] * q[k] * w[j][e + i] * inv;
+            v[i] = fabsf(v[i]) > 448.f ? copysignf(448.f, v[i]) : v[i];
+          }
+          const int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
+          code[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
+        }
+        uint8_t* o = (uint8_t*)p.y + row * p.ldy + (j * TPR + t) * N;
+        if (live[k][j] == N) {
+          if constexpr (N == 8) *(u32x2_a1*)o = u32x2{code[0], code[1]};
+          else *(u32_a1*)o = code[0];
+        } else {
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (e < live[k][j]) o[e] = (uint8_t)(code[e / 4] >> (8 * (e % 4)));
+        }
       }
     }
   }
 }
 
-constexpr int norm_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
-
-template <typename T, int TPR, int NV, bool E4M3>
+template <typename T, int TPR, int NV, int R, bool E4M3>
 __global__ __launch_bounds__(norm_threads(TPR)) void norm_fwd_kernel(NormProb p) {
-  __shared__ float sm[16];
+  __shared__ float sm[norm_sm<TPR, R>()];
   constexpr int G = norm_threads(TPR) / TPR;
-  norm_fwd_row<T, TPR, NV, E4M3>(p, (int64_t)blockIdx.x * G + threadIdx.x / TPR, sm);
+  norm_fwd_rows<T, TPR, NV, R, E4M3>(p, (int64_t)blockIdx.x * (G * R), sm);
 }
-template <typename T, int TPR, int NV>
+template <typename T, int TPR, int NV, int R>
 __global__ __launch_bounds__(norm_threads(TPR)) void norm_fwd_table_kernel(const NormProb* __restrict__ probs,
                                                                            const int32_t* __restrict__ map) {
-  __shared__ float sm[16];
+  __shared__ float sm[norm_sm<TPR, R>()];
   constexpr int G = norm_threads(TPR) / TPR;
   const NormProb p = probs[map[2 * blockIdx.x]];
-  norm_fwd_row<T, TPR, NV, false>(p, (int64_t)map[2 * blockIdx.x + 1] * G + threadIdx.x / TPR, sm);
+  norm_fwd_rows<T, TPR, NV, R, false>(p, (int64_t)map[2 * blockIdx.x + 1] * (G * R), sm);
 }
 
-// ---------------------------------------------------------------------------
-// RMS norm, backward. A workgroup takes every `blocks`-th group of rows and
-// keeps its columns' share of dw in registers; the shares are added in order by
-// a second launch (no atomics: the result does not depend on timing).
-// ---------------------------------------------------------------------------
-template <typename T, int TPR, int NV>
+// Backward. A workgroup takes every `blocks`-th run of G R rows and keeps its
+// columns' share of dw in registers; the shares are added in order by a second
+// launch (no atomics: the result does not depend on timing).
+template <typename T, int TPR, int NV, int R>
 __device__ __forceinline__ void norm_bwd_rows(const NormProb& p, int blk, int64_t wsoff, float* sm, float* acc) {
   constexpr int N = V16<T>::N, NT = norm_threads(TPR), G = NT / TPR;
   const int t = threadIdx.x & (TPR - 1), g = threadIdx.x / TPR, d = p.d;
   float w[NV][N], dw[NV][N];
-  int cnt[NV];
+  int cnt[NV], flip = 0;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = (j * TPR + t) * N;
@@ -272,43 +337,57 @@ __device__ __forceinline__ void norm_bwd_rows(const NormProb& p, int blk, int64_
     for (int e = 0; e < N; ++e) dw[j][e] = 0.f;
   }
   const float invd = 1.f / (float)d;
-  for (int64_t r0 = (int64_t)blk * G; r0 < p.rows; r0 += (int64_t)p.blocks * G) {
-    const int64_t row = r0 + g;
-    const bool live = row < p.rows;
-    const int64_t at = live ? row : 0;
-    const T* s = (const T*)p.x + at * p.ldx;
-    const T* dy = (const T*)p.dy + at * p.lddy;
-    const float q = live ? p.rstd[at] : 0.f;
-    float a[NV][N], b[NV][N];
+  for (int64_t r0 = (int64_t)blk * (G * R); r0 < p.rows; r0 += (int64_t)p.blocks * (G * R)) {
+    RowVec<T, NV> s[R], dy[R], ds[R];
+    float q[R], sum[R];
+    int live[R][NV];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) load_vec<T>(s + (j * TPR + t) * N, live ? cnt[j] : 0, a[j]);
+    for (int k = 0; k < R; ++k) {
+      const int64_t row = r0 + k * G + g, at = row < p.rows ? row : 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) load_vec<T>(dy + (j * TPR + t) * N, live ? cnt[j] : 0, b[j]);
-    float sum = 0.f;
+      for (int j = 0; j < NV; ++j) live[k][j] = row < p.rows ? cnt[j] : 0;
+      s[k].load((const T*)p.x + at * p.ldx, live[k], TPR, t);
+      dy[k].load((const T*)p.dy + at * p.lddy, live[k], TPR, t);
+      if (p.r) ds[k].load((const T*)p.r + at * p.ldr, live[k], TPR, t);
+      q[k] = row < p.rows ? p.rstd[at] : 0.f;
+    }
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float xh = a[j][e] * q;
-        dw[j][e] = fmaf(b[j][e], xh, dw[j][e]);
-        b[j][e] *= w[j][e];
-        sum = fmaf(b[j][e], xh, sum);
-      }
-    sum = row_sum<TPR>(sum, sm) * invd;
-    if (p.y) {
-      T* dx = (T*)p.y + at * p.ldy;
-      const T* ds = p.r ? (const T*)p.r + at * p.ldr : nullptr;
+    for (int k = 0; k < R; ++k) {
+      sum[k] = 0.f;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int n = live ? cnt[j] : 0;
-        float o[N];
-        if (ds) load_vec<T>(ds + (j * TPR + t) * N, n, o);
+        float a[N], b[N];
+        s[k].get(j, a);
+        dy[k].get(j, b);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          const float v = q * (b[j][e] - a[j][e] * q * sum) + (ds ? o[e] : 0.f);
-          o[e] = p.mask && !(a[j][e] > 0.f) ? 0.f : v;
+          const float gx = b[e] * (a[e] * q[k]);
+          dw[j][e] += gx;
+          sum[k] = fmaf(gx, w[j][e], sum[k]);
         }
-        store_vec<T>(dx + (j * TPR + t) * N, n, o);
+      }
+    }
+    row_reduce<TPR, R>(sum, Add{}, sm, flip);
+    if (p.y) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        s[k].forget();
+        dy[k].forget();
+        const int64_t row = r0 + k * G + g;
+        const float c = sum[k] * invd * q[k];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          float a[N], b[N], o[N];
+          s[k].get(j, a);
+          dy[k].get(j, b);
+          if (p.r) ds[k].get(j, o);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float v = q[k] * (b[e] * w[j][e] - a[e] * c) + (p.r ? o[e] : 0.f);
+            o[e] = p.mask && !(a[e] > 0.f) ? 0.f : v;
+          }
+          store_vec<T>((T*)p.y + row * p.ldy + (j * TPR + t) * N, live[k][j], o);
+        }
       }
     }
   }
@@ -320,46 +399,46 @@ __device__ __forceinline__ void norm_bwd_rows(const NormProb& p, int blk, int64_
       for (int e = 0; e < N; ++e)
         if (e < cnt[j]) part[(j * TPR + t) * N + e] = dw[j][e];
   } else {
-    // the groups' shares one after the other, in group order
-    for (int k = 0; k < G; ++k) {
-      if (g == k)
+    // the groups' shares side by side in LDS, added in group order
+    constexpr int ROW = TPR * NV * N;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
-            const int c = (j * TPR + t) * N + e;
-            acc[c] = k ? acc[c] + dw[j][e] : dw[j][e];
-          }
-      __syncthreads();
+      for (int e = 0; e < N; ++e) acc[g * ROW + (j * TPR + t) * N + e] = dw[j][e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < d; c += NT) {
+      float a = acc[c];
+#pragma unroll
+      for (int k = 1; k < G; ++k) a += acc[k * ROW + c];
+      part[c] = a;
     }
-    for (int c = threadIdx.x; c < d; c += NT) part[c] = acc[c];
   }
 }
 
-template <int TPR> constexpr int norm_acc() { return TPR < 256 ? TPR * NORM_REGS : 1; }
+template <typename T, int TPR, int NV> constexpr int norm_acc() { return TPR < 256 ? 256 * NV * V16<T>::N : 1; }
 
-template <typename T, int TPR, int NV>
+template <typename T, int TPR, int NV, int R>
 __global__ __launch_bounds__(norm_threads(TPR)) void norm_bwd_kernel(NormProb p) {
-  __shared__ float sm[16];
-  __shared__ float acc[norm_acc<TPR>()];
-  norm_bwd_rows<T, TPR, NV>(p, blockIdx.x, 0, sm, acc);
+  __shared__ float sm[norm_sm<TPR, R>()];
+  __shared__ float acc[norm_acc<T, TPR, NV>()];
+  norm_bwd_rows<T, TPR, NV, R>(p, blockIdx.x, 0, sm, acc);
 }
-template <typename T, int TPR, int NV>
+template <typename T, int TPR, int NV, int R>
 __global__ __launch_bounds__(norm_threads(TPR)) void norm_bwd_table_kernel(const NormProb* __restrict__ probs,
                                                                            const int32_t* __restrict__ map, int64_t wsoff) {
-  __shared__ float sm[16];
-  __shared__ float acc[norm_acc<TPR>()];
+  __shared__ float sm[norm_sm<TPR, R>()];
+  __shared__ float acc[norm_acc<T, TPR, NV>()];
   const NormProb p = probs[map[2 * blockIdx.x]];
-  norm_bwd_rows<T, TPR, NV>(p, map[2 * blockIdx.x + 1], wsoff, sm, acc);
+  norm_bwd_rows<T, TPR, NV, R>(p, map[2 * blockIdx.x + 1], wsoff, sm, acc);
 }
 
-// dw: 16 groups of 64 columns' threads, each adding a run of the partials, then
+// dw: 32 groups of 32 columns' threads, each adding a run of the partials, then
 // the groups in order
 __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__ part, int nparts, int d,
                                                        float* __restrict__ dw) {
-  __shared__ float sm[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
-  const int per = (nparts + 15) / 16, k0 = g * per, k1 = min(nparts, k0 + per);
+  __shared__ float sm[32][33];
+  const int l = threadIdx.x & 31, c = blockIdx.x * 32 + l, g = threadIdx.x >> 5;
+  const int per = (nparts + 31) / 32, k0 = g * per, k1 = min(nparts, k0 + per);
   float a = 0.f;
   if (c < d)
     for (int k = k0; k < k1; k += 8) {
@@ -369,12 +448,12 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__
 #pragma unroll
       for (int u = 0; u < 8; ++u) a += v[u];
     }
-  sm[g][threadIdx.x & 63] = a;
+  sm[g][l] = a;
   __syncthreads();
   if (g == 0 && c < d) {
     a = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) a += sm[k][threadIdx.x];
+    for (int k = 0; k < 32; ++k) a += sm[k][l];
     dw[c] = a;
   }
 }
@@ -1017,15 +1096,15 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwTensor* __restric
 // ---------------------------------------------------------------------------
 NormPlan norm_plan(bool bf16, int d) {
   const int n = bf16 ? 8 : 4;
-  int tpr = 64;
-  while (tpr < 1024 && tpr * NORM_REGS < d) tpr *= 4;
+  int tpr = 16;
+  while (tpr < 1024 && tpr * n * 2 < d) tpr *= 4;
   int nv = 1;
-  while (nv < (tpr == 1024 ? NORM_REGS / 2 : NORM_REGS) / n && tpr * n * nv < d) nv *= 2;
-  return NormPlan{tpr, nv, norm_threads(tpr) / tpr};
+  while (tpr * n * nv < d) nv *= 2;
+  return NormPlan{tpr, nv, norm_threads(tpr) / tpr, norm_threads(tpr) / tpr * std::max(1, (tpr == 1024 ? NORM_R / 2 : NORM_R) / nv)};
 }
 int norm_blocks(const NormPlan& p, int64_t rows) {
-  const int64_t groups = (rows + p.group - 1) / p.group;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(groups, p.tpr == 1024 ? 256 : 512));
+  const int64_t groups = (rows + p.rows - 1) / p.rows;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(groups, p.tpr == 1024 ? 512 : 1024));
 }
 
 namespace {
@@ -1033,14 +1112,13 @@ namespace {
 template <int N> using Int = std::integral_constant<int, N>;
 template <typename F> hipError_t norm_pick(bool bf16, const NormPlan& p, F&& f) {
   auto nv = [&](auto type, auto tpr) {
-    constexpr int most = (tpr() == 1024 ? NORM_REGS / 2 : NORM_REGS) * (int)sizeof(type) / 16;
     if (p.nv == 1) f(type, tpr, Int<1>{});
     else if (p.nv == 2) f(type, tpr, Int<2>{});
-    else if constexpr (most == 4) f(type, tpr, Int<4>{});
-    else if constexpr (most == 8) p.nv == 4 ? f(type, tpr, Int<4>{}) : f(type, tpr, Int<8>{});
+    else if constexpr (tpr() == 1024 && sizeof(type) == 4) f(type, tpr, Int<4>{});
   };
   auto tpr = [&](auto type) {
-    if (p.tpr == 64) nv(type, Int<64>{});
+    if (p.tpr == 16) nv(type, Int<16>{});
+    else if (p.tpr == 64) nv(type, Int<64>{});
     else if (p.tpr == 256) nv(type, Int<256>{});
     else nv(type, Int<1024>{});
   };
@@ -1051,19 +1129,23 @@ template <typename F> hipError_t norm_pick(bool bf16, const NormPlan& p, F&& f) 
 }  // namespace
 
 hipError_t launch_norm(bool bf16, bool e4m3, const NormPlan& plan, const NormProb& p, hipStream_t s) {
-  const int64_t grid = (p.rows + plan.group - 1) / plan.group;
-  if (grid <= 0) return hipSuccess;
+  if (p.rows <= 0) return hipSuccess;
+  // one row per thread where several would leave CUs without work
+  const bool few = p.rows < (int64_t)plan.rows * 512;
+  const int64_t per = few ? plan.group : plan.rows, grid = (p.rows + per - 1) / per;
   return norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
     using T = decltype(t);
-    const dim3 blk(norm_threads(tpr()));
-    if (e4m3) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), true>), dim3((unsigned)grid), blk, 0, s, p);
-    else hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), false>), dim3((unsigned)grid), blk, 0, s, p);
+    const dim3 g((unsigned)grid), blk(norm_threads(tpr()));
+    if (e4m3 && few) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), 1, true>), g, blk, 0, s, p);
+    else if (e4m3) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), norm_rows<tpr(), nv()>(), true>), g, blk, 0, s, p);
+    else if (few) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), 1, false>), g, blk, 0, s, p);
+    else hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), norm_rows<tpr(), nv()>(), false>), g, blk, 0, s, p);
   });
 }
 hipError_t launch_norm_bwd(bool bf16, const NormPlan& plan, const NormProb& p, hipStream_t s) {
   return norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
     using T = decltype(t);
-    hipLaunchKernelGGL((norm_bwd_kernel<T, tpr(), nv()>), dim3(p.blocks), dim3(norm_threads(tpr())), 0, s, p);
+    hipLaunchKernelGGL((norm_bwd_kernel<T, tpr(), nv(), norm_rows<tpr(), nv()>()>), dim3(p.blocks), dim3(norm_threads(tpr())), 0, s, p);
   });
 }
 hipError_t launch_norm_table(bool bf16, bool bwd, const NormPlan& plan, const NormProb* probs, const int32_t* map, int nblocks,
@@ -1072,12 +1154,12 @@ hipError_t launch_norm_table(bool bf16, bool bwd, const NormPlan& plan, const No
   return norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
     using T = decltype(t);
     const dim3 blk(norm_threads(tpr()));
-    if (bwd) hipLaunchKernelGGL((norm_bwd_table_kernel<T, tpr(), nv()>), dim3(nblocks), blk, 0, s, probs, map, wsoff);
-    else hipLaunchKernelGGL((norm_fwd_table_kernel<T, tpr(), nv()>), dim3(nblocks), blk, 0, s, probs, map);
+    if (bwd) hipLaunchKernelGGL((norm_bwd_table_kernel<T, tpr(), nv(), norm_rows<tpr(), nv()>()>), dim3(nblocks), blk, 0, s, probs, map, wsoff);
+    else hipLaunchKernelGGL((norm_fwd_table_kernel<T, tpr(), nv(), norm_rows<tpr(), nv()>()>), dim3(nblocks), blk, 0, s, probs, map);
   });
 }
 hipError_t launch_norm_dw(const float* part, int nparts, int d, float* dw, hipStream_t s) {
-  hipLaunchKernelGGL(norm_dw_kernel, dim3((d + 63) / 64), dim3(1024), 0, s, part, nparts, d, dw);
+  hipLaunchKernelGGL(norm_dw_kernel, dim3((d + 31) / 32), dim3(1024), 0, s, part, nparts, d, dw);
   return hipGetLastError();
 }
 

@@ -1271,15 +1271,12 @@ static void build_tables(un_ctx* c, Tables& T) {
     out.back().bm = vb;
   };
   // norm: one workgroup per (problem, group of rows), backward per (problem,
-  // block); one launch per number of threads a row (the order of a row's sum
-  // follows its own width alone, whatever shares the step)
-  auto emit_norm_one = [&](std::vector<NormProb>& ps, std::vector<Launch>& out, int kind) {
-    int widest = 0;
-    for (auto& p : ps) widest = std::max(widest, p.d);
-    const NormPlan plan = norm_plan(bf, widest);
+  // block). Problems of one launch have the same plan, which decides the order
+  // of their sums: a model's own width decides, whatever shares the step.
+  auto emit_norm_one = [&](std::vector<NormProb>& ps, const NormPlan& plan, std::vector<Launch>& out, int kind) {
     std::vector<int32_t> map;
     for (size_t k = 0; k < ps.size(); ++k) {
-      const int nb = kind == 13 ? cdiv(ps[k].rows, plan.group) : ps[k].blocks;
+      const int nb = kind == 13 ? cdiv(ps[k].rows, plan.rows) : ps[k].blocks;
       for (int t = 0; t < nb; ++t) {
         map.push_back((int32_t)k);
         map.push_back(t);
@@ -1297,11 +1294,15 @@ static void build_tables(un_ctx* c, Tables& T) {
     out.back().norm = plan;
   };
   auto emit_norm = [&](std::vector<NormProb>& ps, std::vector<Launch>& out, int kind) {
-    for (int tpr : {64, 256, 1024}) {
-      std::vector<NormProb> same;
-      for (auto& p : ps)
-        if (norm_plan(bf, p.d).tpr == tpr) same.push_back(p);
-      if (!same.empty()) emit_norm_one(same, out, kind);
+    while (!ps.empty()) {
+      const NormPlan plan = norm_plan(bf, ps[0].d);
+      std::vector<NormProb> same, other;
+      for (auto& p : ps) {
+        const NormPlan q = norm_plan(bf, p.d);
+        (q.tpr == plan.tpr && q.nv == plan.nv ? same : other).push_back(p);
+      }
+      emit_norm_one(same, plan, out, kind);
+      ps = other;
     }
   };
   auto conv_base = [&](const Block& b) { return conv_geometry(b, c->groups[c->models[b.model].group].B); };

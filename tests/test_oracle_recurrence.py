@@ -280,7 +280,7 @@ def test_parameters_and_8_bit_states_on_the_host(precision, tmp_path):
 
 
 def test_launches_of_a_step(tmp_path):
-    """One launch per level and operator for all models; short sequences on one wave, norms by their threads per row."""
+    """One launch per level and operator for all models; short sequences on one wave, norms by their rows' plans."""
     res = H.run("""
 U_, N, G = (lambda t: ("unflatten", t)), ("rms_norm",), ("recurrence",)
 a = {"layers": [U_(8), N, G, ("flatten",), ("linear", 3)], "num_classes": 3}
@@ -297,4 +297,4 @@ result = [names([a]), names([a, b]), names([{"layers": [("linear", w), ("relu",)
     short, mixed, wide = res
     assert len(short) == 5 and sum("scan" in x and x.endswith(" 64") for x in short) == 2 and "adamw" in short[-1]
     assert len(mixed) == 5 and sum("scan" in x and x.endswith(" 512") for x in mixed) == 2
-    assert sum("norm_fwd" in x for x in wide) == 2  # 64 and 128 features: a wave per row; 4096: a workgroup
+    assert sum("norm_fwd" in x for x in wide) == 2  # 64 and 128 features in one, 4096 in another
