@@ -12,11 +12,14 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch._C import _cuda_getCurrentRawStream as _current_stream  # torch.cuda.current_stream(i).cuda_stream without its 1 us
 
 from . import unifiednn as _un
 from .unifiednn import UnError  # noqa: F401  (raised by every call here)
 
-_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
+_TYPES = {_F32: 0, _BF16: 1}
+_byref, _empty, _empty_like = ctypes.byref, torch.empty, torch.empty_like
 
 
 def _require(ok, what):
@@ -25,33 +28,55 @@ def _require(ok, what):
 
 
 def _check_type(x, name):
+    """The type's number and the device's index of an operator's first tensor."""
     _require(isinstance(x, torch.Tensor), f"{name} must be a tensor")
-    _require(x.dtype in _TYPES, f"{name} must be float32 or bfloat16, not {x.dtype}")
-    return _TYPES[x.dtype]
+    t = _TYPES.get(x.dtype)
+    _require(t is not None, f"{name} must be float32 or bfloat16, not {x.dtype}")
+    dev = x.get_device()
+    _require(dev >= 0, f"{name} must be on a GPU, not {x.device}")
+    return t, dev
 
 
-def _like(x, name, shape, dtype, device):
-    """x is a tensor of this shape and type on this device, its last axis dense."""
-    _require(isinstance(x, torch.Tensor), f"{name} must be a tensor")
-    _require(x.device == device and device.type == "cuda", f"{name} must be on {device if device.type == 'cuda' else 'a GPU'}, not {x.device}")
-    _require(x.dtype == dtype, f"{name} must be {dtype}, not {x.dtype}")
-    _require(tuple(x.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}, not {tuple(x.shape)}")
-    _require(x.shape[-1] <= 1 or x.stride(-1) == 1, f"{name}'s last axis must be dense")
-    return x
+def _like(x, name, shape, dtype, dev):
+    """x is a tensor of this shape and type on GPU `dev`, its last axis dense. (One test for what fits; a call's latency counts.)"""
+    if not (isinstance(x, torch.Tensor) and x.dtype is dtype and x.get_device() == dev and x.shape == shape
+            and (x.stride(-1) == 1 or x.shape[-1] <= 1)):
+        _require(isinstance(x, torch.Tensor), f"{name} must be a tensor")
+        _require(x.get_device() == dev, f"{name} must be on cuda:{dev}, not {x.device}")
+        _require(x.dtype is dtype, f"{name} must be {dtype}, not {x.dtype}")
+        _require(x.shape == shape, f"{name} must have shape {tuple(shape)}, not {tuple(x.shape)}")
+        _require(False, f"{name}'s last axis must be dense")
 
 
-def _flat(x, name, shape, dtype, device):
-    _like(x, name, shape, dtype, device)
-    _require(x.is_contiguous(), f"{name} must be contiguous")
-    return x
+def _flat(x, name, shape, dtype, dev):
+    if not (isinstance(x, torch.Tensor) and x.dtype is dtype and x.get_device() == dev and x.shape == shape and x.is_contiguous()):
+        _like(x, name, torch.Size(shape), dtype, dev) if len(shape) else None
+        _require(False, f"{name} must be contiguous")
 
 
 def _ptr(x):
     return None if x is None else x.data_ptr()
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+def _fresh(x, dtype):
+    """A new dense tensor of x's shape."""
+    return _empty_like(x, dtype=dtype) if x.is_contiguous() else _empty(x.shape, dtype=dtype, device=x.device)
+
+
+def _call(fn, args, dev):
+    status = fn(_byref(args), _current_stream(dev))
+    if status:
+        _un._check(status)
+
+
+_fns = None
+
+
+def _lib():
+    global _fns
+    if _fns is None:
+        _fns = _un.lib()
+    return _fns
 
 
 # ---------------------------------------------------------------------------
@@ -59,33 +84,37 @@ def _stream(device):
 # ---------------------------------------------------------------------------
 def _rows(x):
     """x as rows: (rows, row stride, x to pass on). A tensor whose leading axes do not have one stride is copied."""
-    width = x.shape[-1]
-    if x.dim() == 2:
-        return x.shape[0], x.stride(0) if x.shape[0] > 1 else width, x
+    shape = x.shape
+    width = shape[-1]
+    if len(shape) == 2:
+        rows = shape[0]
+        return rows, x.stride(0) if rows > 1 else width, x
     try:
-        v = x.view(-1, width) if x.dim() > 1 else x.unsqueeze(0)
+        v = x.view(-1, width) if len(shape) > 1 else x.unsqueeze(0)
     except RuntimeError:
         v = x.reshape(-1, width)
     return v.shape[0], v.stride(0) if v.shape[0] > 1 else width, v
 
 
 def _norm(x, weight, residual, eps, keep, e4m3):
-    t = _check_type(x, "x")
-    _require(x.dim() >= 1 and x.shape[-1] >= 1, "x needs a last axis of at least one value")
-    dev, shape = x.device, x.shape
-    _like(x, "x", shape, x.dtype, dev)
-    _flat(weight, "weight", (shape[-1],), torch.float32, dev)
-    if residual is not None:
-        _like(residual, "residual", shape, x.dtype, dev)
+    t, dev = _check_type(x, "x")
+    shape, dtype = x.shape, x.dtype
+    _require(len(shape) >= 1 and shape[-1] >= 1, "x needs a last axis of at least one value")
+    width = shape[-1]
+    _like(x, "x", shape, dtype, dev)
+    _flat(weight, "weight", (width,), _F32, dev)
     rows, ldx, xv = _rows(x)
-    _, ldr, rv = _rows(residual) if residual is not None else (0, 0, None)
-    y = torch.empty(shape, dtype=torch.float8_e4m3fn if e4m3 else x.dtype, device=dev)
-    s = torch.empty(shape, dtype=x.dtype, device=dev) if residual is not None else x
-    rstd = torch.empty(shape[:-1], dtype=torch.float32, device=dev) if keep else None
-    scale = torch.empty(shape[:-1], dtype=torch.float32, device=dev) if e4m3 else None
-    a = _un.un_rms_norm_args(t, shape[-1], rows, float(eps), _ptr(xv), ldx, _ptr(rv), ldr, _ptr(weight),
-                             _ptr(s) if residual is not None else None, shape[-1], _ptr(y), shape[-1], _ptr(rstd), _ptr(scale))
-    _un._check(_un.lib().un_rms_norm(ctypes.byref(a), _stream(dev)))
+    y = _fresh(x, torch.float8_e4m3fn if e4m3 else dtype)
+    ldr, rp, sp, s = 0, None, None, x
+    if residual is not None:
+        _like(residual, "residual", shape, dtype, dev)
+        _, ldr, rv = _rows(residual)
+        s = _fresh(x, dtype)
+        rp, sp = rv.data_ptr(), s.data_ptr()
+    rstd = _empty(shape[:-1], dtype=_F32, device=x.device) if keep else None
+    scale = _empty(shape[:-1], dtype=_F32, device=x.device) if e4m3 else None
+    _call(_lib().un_rms_norm, _un.un_rms_norm_args(t, width, rows, float(eps), xv.data_ptr(), ldx, rp, ldr, weight.data_ptr(), sp, width,
+                                                   y.data_ptr(), width, _ptr(rstd), _ptr(scale)), dev)
     return y, s, rstd, scale
 
 
@@ -107,53 +136,65 @@ def rms_norm_e4m3(x, weight, residual=None, eps=1e-6):
 def rms_norm_backward(dy, s, weight, rstd, ds=None):
     """(dx, dweight) of rms_norm from the gradient dy at y, and ds at s (None: s
     is used by nothing else). dx is the gradient at x and at the residual."""
-    t = _check_type(s, "s")
-    dev, shape = s.device, s.shape
+    t, dev = _check_type(s, "s")
+    shape, dtype = s.shape, s.dtype
+    _require(len(shape) >= 1 and shape[-1] >= 1, "s needs a last axis of at least one value")
     width = shape[-1]
-    _like(s, "s", shape, s.dtype, dev)
-    _like(dy, "dy", shape, s.dtype, dev)
-    if ds is not None:
-        _like(ds, "ds", shape, s.dtype, dev)
-    _flat(weight, "weight", (width,), torch.float32, dev)
-    _flat(rstd, "rstd", shape[:-1], torch.float32, dev) if s.dim() > 1 else _require(rstd.numel() == 1, "rstd must have one value")
+    _like(s, "s", shape, dtype, dev)
+    _like(dy, "dy", shape, dtype, dev)
+    _flat(weight, "weight", (width,), _F32, dev)
+    _flat(rstd, "rstd", shape[:-1], _F32, dev)
     rows, lds, sv = _rows(s)
     _, lddy, dyv = _rows(dy)
-    _, ldds, dsv = _rows(ds) if ds is not None else (0, 0, None)
-    dx = torch.empty(shape, dtype=s.dtype, device=dev)
-    dw = torch.empty(width, dtype=torch.float32, device=dev)
+    ldds, dsp = 0, None
+    if ds is not None:
+        _like(ds, "ds", shape, dtype, dev)
+        _, ldds, dsv = _rows(ds)
+        dsp = dsv.data_ptr()
+    dx = _fresh(s, dtype)
     need = ctypes.c_size_t()
-    _un._check(_un.lib().un_rms_norm_workspace(t, rows, width, ctypes.byref(need)))
-    ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
-    a = _un.un_rms_norm_grad_args(t, width, rows, _ptr(dyv), lddy, _ptr(sv), lds, _ptr(weight), _ptr(rstd), _ptr(dsv), ldds,
-                                  _ptr(dx), width, _ptr(dw), _ptr(ws), need.value)
-    _un._check(_un.lib().un_rms_norm_backward(ctypes.byref(a), _stream(dev)))
-    return dx, dw
+    fns = _lib()
+    status = fns.un_rms_norm_workspace(t, rows, width, _byref(need))
+    if status:
+        _un._check(status)
+    # one allocation: the weight gradient, then (256-byte aligned) the workspace
+    at = -(-width // 64) * 64
+    buf = _empty(at + need.value // 4, dtype=_F32, device=s.device)
+    p = buf.data_ptr()
+    _call(fns.un_rms_norm_backward, _un.un_rms_norm_grad_args(t, width, rows, dyv.data_ptr(), lddy, sv.data_ptr(), lds,
+                                                              weight.data_ptr(), rstd.data_ptr(), dsp, ldds, dx.data_ptr(), width, p,
+                                                              p + 4 * at, need.value), dev)
+    return dx, buf[:width]
 
 
 # ---------------------------------------------------------------------------
 # Gated linear recurrence
 # ---------------------------------------------------------------------------
-def _strides(x):
+def _strides(x, shape):
     """(token, sequence) strides of [batch, tokens, width]."""
-    return x.stride(1) if x.shape[1] > 1 else x.shape[2], x.stride(0)
+    st = x.stride()
+    return st[1] if shape[1] > 1 else shape[2], st[0]
 
 
 def _scan_sizes(batch, tokens, width):
     n, ws = ctypes.c_size_t(), ctypes.c_size_t()
-    _un._check(_un.lib().un_gated_scan_sizes(batch, tokens, width, ctypes.byref(n), ctypes.byref(ws)))
+    status = _lib().un_gated_scan_sizes(batch, tokens, width, _byref(n), _byref(ws))
+    if status:
+        _un._check(status)
     return n.value, ws.value
 
 
 def _scan_inputs(gate, value, lens):
-    t = _check_type(gate, "gate")
-    _require(gate.dim() == 3, "gate must be [batch, tokens, width]")
-    dev, shape = gate.device, gate.shape
+    _require(isinstance(gate, torch.Tensor) and gate.dim() == 3, "gate must be a tensor [batch, tokens, width]")
+    t, dev = _check_type(gate, "gate")
+    shape = gate.shape
     _like(gate, "gate", shape, gate.dtype, dev)
     _like(value, "value", shape, gate.dtype, dev)
-    _require(gate.numel() == 0 or _strides(gate) == _strides(value), "gate and value must have the same strides")
+    st = _strides(gate, shape)
+    _require(st == _strides(value, shape) or gate.numel() == 0, "gate and value must have the same strides")
     if lens is not None:
-        _flat(lens, "lens", shape[:1], torch.int32, dev)
-    return t, dev, shape
+        _flat(lens, "lens", shape[:1], _I32, dev)
+    return t, dev, shape, st
 
 
 def gated_scan(gate, value, h0=None, lens=None, keep=False, last=None):
@@ -165,21 +206,24 @@ def gated_scan(gate, value, h0=None, lens=None, keep=False, last=None):
     last (the state after the last step, float32) may be given, h0 itself among
     others, to be written in place. states (None unless `keep`) is what
     gated_scan_backward needs."""
-    t, dev, (b, n, d) = _scan_inputs(gate, value, lens)
+    t, dev, shape, (ld, seq) = _scan_inputs(gate, value, lens)
+    b, n, d = shape
     if h0 is not None:
-        _flat(h0, "h0", (b, d), torch.float32, dev)
+        _flat(h0, "h0", (b, d), _F32, dev)
+    device = gate.device
     if last is None:
-        last = torch.empty((b, d), dtype=torch.float32, device=dev)
+        last = _empty((b, d), dtype=_F32, device=device)
     else:
-        _flat(last, "last", (b, d), torch.float32, dev)
-    h = torch.empty((b, n, d), dtype=gate.dtype, device=dev)
-    n_states, n_ws = _scan_sizes(b, n, d)
-    states = torch.empty(n_states, dtype=torch.float32, device=dev) if keep else None
-    ws = torch.empty(n_ws, dtype=torch.uint8, device=dev) if n_ws else None
-    ld, seq = _strides(gate)
-    a = _un.un_gated_scan_args(t, b, n, d, _ptr(gate), _ptr(value), ld, seq, _ptr(lens), _ptr(h0), _ptr(h), d, n * d, _ptr(last),
-                               _ptr(states), _ptr(ws), n_ws)
-    _un._check(_un.lib().un_gated_scan(ctypes.byref(a), _stream(dev)))
+        _flat(last, "last", (b, d), _F32, dev)
+    h = _empty(shape, dtype=gate.dtype, device=device)
+    states = ws = None
+    n_ws = 0
+    if n > 16 or keep:  # (a short call keeps no states and needs no workspace)
+        n_states, n_ws = _scan_sizes(b, n, d)
+        states = _empty(n_states, dtype=_F32, device=device) if keep else None
+        ws = _empty(n_ws, dtype=torch.uint8, device=device) if n_ws else None
+    _call(_lib().un_gated_scan, _un.un_gated_scan_args(t, b, n, d, gate.data_ptr(), value.data_ptr(), ld, seq, _ptr(lens), _ptr(h0),
+                                                       h.data_ptr(), d, n * d, last.data_ptr(), _ptr(states), _ptr(ws), n_ws), dev)
     return h, last, states
 
 
@@ -188,23 +232,26 @@ def gated_scan_backward(gate, value, states, dh, dlast=None, lens=None, out=None
     (two tensors of gate's shape and equal strides, the halves of one buffer, say);
     without `out`, (dgate, dvalue, dh0). gate, value, lens: as given to gated_scan;
     states: what it returned; dh: the gradient at h; dlast: at the last state."""
-    t, dev, (b, n, d) = _scan_inputs(gate, value, lens)
+    t, dev, shape, (ld, seq) = _scan_inputs(gate, value, lens)
+    b, n, d = shape
+    dtype, device = gate.dtype, gate.device
     n_states, n_ws = _scan_sizes(b, n, d)
-    _flat(states, "states", (n_states,), torch.float32, dev)
-    _like(dh, "dh", (b, n, d), gate.dtype, dev)
+    _flat(states, "states", (n_states,), _F32, dev)
+    _like(dh, "dh", shape, dtype, dev)
     if dlast is not None:
-        _flat(dlast, "dlast", (b, d), torch.float32, dev)
+        _flat(dlast, "dlast", (b, d), _F32, dev)
     given = out is not None
-    dg, dv = out if given else torch.empty((2, b, n, d), dtype=gate.dtype, device=dev).unbind(0)
-    _like(dg, "dgate", (b, n, d), gate.dtype, dev)
-    _like(dv, "dvalue", (b, n, d), gate.dtype, dev)
-    _require(dg.numel() == 0 or _strides(dg) == _strides(dv), "dgate and dvalue must have the same strides")
-    dh0 = torch.empty((b, d), dtype=torch.float32, device=dev)
-    ws = torch.empty(n_ws, dtype=torch.uint8, device=dev) if n_ws else None
-    (ld, seq), (ldd, seqd), (ldo, seqo) = _strides(gate), _strides(dh), _strides(dg)
-    a = _un.un_gated_scan_grad_args(t, b, n, d, _ptr(gate), _ptr(value), ld, seq, _ptr(lens), _ptr(states), _ptr(dh), ldd, seqd,
-                                    _ptr(dlast), _ptr(dg), _ptr(dv), ldo, seqo, _ptr(dh0), _ptr(ws), n_ws)
-    _un._check(_un.lib().un_gated_scan_backward(ctypes.byref(a), _stream(dev)))
+    dg, dv = out if given else _empty((2, b, n, d), dtype=dtype, device=device).unbind(0)
+    _like(dg, "dgate", shape, dtype, dev)
+    _like(dv, "dvalue", shape, dtype, dev)
+    (ldo, seqo), (ldd, seqd) = _strides(dg, shape), _strides(dh, shape)
+    _require((ldo, seqo) == _strides(dv, shape) or dg.numel() == 0, "dgate and dvalue must have the same strides")
+    dh0 = _empty((b, d), dtype=_F32, device=device)
+    ws = _empty(n_ws, dtype=torch.uint8, device=device) if n_ws else None
+    _call(_lib().un_gated_scan_backward, _un.un_gated_scan_grad_args(t, b, n, d, gate.data_ptr(), value.data_ptr(), ld, seq, _ptr(lens),
+                                                                     states.data_ptr(), dh.data_ptr(), ldd, seqd, _ptr(dlast),
+                                                                     dg.data_ptr(), dv.data_ptr(), ldo, seqo, dh0.data_ptr(), _ptr(ws),
+                                                                     n_ws), dev)
     return dh0 if given else (dg, dv, dh0)
 
 
@@ -239,30 +286,32 @@ class AdamW:
             lists.update(m_scales=m_scales, v_scales=v_scales)
         for k, x in lists.items():
             _require(len(x) == n, f"{k} must hold {n} tensors, not {len(x)}")
-        dev = params[0].device
+        _, dev = _check_type(params[0], "params[0]")
+        device = params[0].device
         gt = grads[0].dtype
         _require(gt in _TYPES, f"gradients must be float32 or bfloat16, not {gt}")
         st = torch.float8_e4m3fn if eight else torch.float32
         arr = (_un.un_adamw_tensor * n)()
         for i, p in enumerate(params):
-            shape, k = p.shape, p.numel()
-            _flat(p.view(-1) if p.dim() == 0 else p, f"params[{i}]", shape or (1,), torch.float32, dev)
+            _require(isinstance(p, torch.Tensor) and p.get_device() == dev and p.dtype is _F32 and p.is_contiguous(),
+                     f"params[{i}] must be a contiguous {_F32} tensor on {device}")
+            k = p.numel()
             for name, x, dt in (("grads", grads, gt), ("m", m, st), ("v", v, st), ("copies", copies, torch.bfloat16)):
                 if x is not None:
                     y = x[i]
-                    _require(isinstance(y, torch.Tensor) and y.device == dev and y.dtype == dt and y.numel() == k and y.is_contiguous(),
-                             f"{name}[{i}] must be a contiguous {dt} tensor of {k} elements on {dev}")
+                    _require(isinstance(y, torch.Tensor) and y.get_device() == dev and y.dtype is dt and y.numel() == k and y.is_contiguous(),
+                             f"{name}[{i}] must be a contiguous {dt} tensor of {k} elements on {device}")
             if eight:
                 for name, x in (("m_scales", m_scales), ("v_scales", v_scales)):
-                    _require(x[i].device == dev and x[i].dtype == torch.float8_e8m0fnu and x[i].numel() == -(-k // QBLOCK) and x[i].is_contiguous(),
-                             f"{name}[{i}] must be a contiguous float8_e8m0fnu tensor of {-(-k // QBLOCK)} elements on {dev}")
+                    _require(x[i].get_device() == dev and x[i].dtype == torch.float8_e8m0fnu and x[i].numel() == -(-k // QBLOCK) and x[i].is_contiguous(),
+                             f"{name}[{i}] must be a contiguous float8_e8m0fnu tensor of {-(-k // QBLOCK)} elements on {device}")
             arr[i] = _un.un_adamw_tensor(_ptr(p), _ptr(grads[i]), _ptr(copies[i]) if copies is not None else None, _ptr(m[i]), _ptr(v[i]),
                                          _ptr(m_scales[i]) if eight else None, _ptr(v_scales[i]) if eight else None, k)
         self._held = [params, lists]
-        self.device = dev
+        self.device, self._index = device, dev
         plan = ctypes.c_void_p()
-        with torch.cuda.device(dev):
-            _un._check(_un.lib().un_adamw_create(arr, n, _TYPES[gt], 8 if eight else 32, ctypes.byref(plan)))
+        with torch.cuda.device(device):
+            _un._check(_lib().un_adamw_create(arr, n, _TYPES[gt], 8 if eight else 32, ctypes.byref(plan)))
         self._plan = plan
 
     @staticmethod
@@ -275,7 +324,9 @@ class AdamW:
     def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, key=0):
         """Step number `step` (from 1). key: with 8-bit states, another whole number each step."""
         h = _un.un_adamw_hyper(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step), int(key) & 0xFFFFFFFF)
-        _un._check(_un.lib().un_adamw_step(self._plan, ctypes.byref(h), _stream(self.device)))
+        status = _lib().un_adamw_step(self._plan, _byref(h), _current_stream(self._index))
+        if status:
+            _un._check(status)
 
     def close(self):
         if self._plan:
