@@ -257,7 +257,12 @@ def _run_scan(st):
         if not train:
             return dict(h=h, last=last)
         dz = torch.empty((case["batch"], n, 2 * d), dtype=gate.dtype, device=gate.device)
-        dh0 = ops.gated_scan_backward(gate, value, states, st["dh"], dlast=st["dlast"], lens=lens,
+        dlast = st["dlast"]
+        if lens is None and gate.dtype == torch.float32:
+            # the program adds the last state's gradient to that of the last step, in its own buffer, as the pass below does
+            st["dh"][:, -1] += dlast
+            dlast = None
+        dh0 = ops.gated_scan_backward(gate, value, states, st["dh"], dlast=dlast, lens=lens,
                                       out=(dz[..., :d], dz[..., d:]))
         return dict(h=h, last=last, dz=dz, dh0=dh0)
     t = gate.dtype
