@@ -491,7 +491,8 @@ un_status un_rms_norm_workspace(int32_t type, int64_t rows, int32_t width, size_
 /* Gated linear recurrence, per sequence and channel:
  *   a_t = sigmoid(gate_t),  h_t = a_t h_{t-1} + (1 - a_t) value_t,  t = 1 .. tokens.
  * gate and value are [batch][tokens][width] with the same strides (the two halves
- * of one projection, say); the state is fp32. lens (device int32 [batch], NULL:
+ * of one projection, say), width and token strides up to 2^24; the state is fp32.
+ * lens (device int32 [batch], NULL:
  * all of `tokens`): steps at and behind a sequence's length (clamped to [0,
  * tokens]) are skipped: their rows of gate and value are not used, their rows of
  * h are written as zeros, and the last state is the one before them. A single

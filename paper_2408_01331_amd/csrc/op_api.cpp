@@ -148,8 +148,7 @@ un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size
   const char* F = "un_gated_scan_sizes";
   if (batch < 0 || tokens < 0 || width < 0) return bad(F, "negative size");
   if (states) *states = (size_t)batch * scan_chunks(tokens) * width;
-  // (only one channel per lane ever comes with segments)
-  const ScanPlan p = scan_plan(batch, tokens, width, false);
+  const ScanPlan p = scan_plan(batch, tokens, width);
   if (workspace_bytes) *workspace_bytes = scan_ws_bytes(p, batch, width);
   return UN_OK;
 }
@@ -157,23 +156,21 @@ un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size
 namespace {
 // what both directions check: sizes, strides and the workspace
 un_status scan_common(const char* F, int32_t type, int32_t B, int32_t T, int32_t d, int64_t ld, int64_t ld2, int64_t ld3,
-                      int64_t seq_out, const void* workspace, size_t bytes, bool pairs, ScanPlan* plan) {
+                      int64_t seq_out, const void* workspace, size_t bytes, ScanPlan* plan) {
   if (!type_ok(type)) return bad(F, "unknown type");
   if (B < 0 || T < 0 || d < 0) return bad(F, "negative size");
   if (T > (1 << 30)) return bad(F, "more than 2^30 tokens are not supported", UN_ERR_UNSUPPORTED);
+  if (d > SCAN_MAX_LD || (T > 1 && (ld > SCAN_MAX_LD || ld2 > SCAN_MAX_LD || ld3 > SCAN_MAX_LD)))
+    return bad(F, "a width or token stride above 2^24 is not supported", UN_ERR_UNSUPPORTED);
   if (T > 1 && (ld < d || ld2 < d || ld3 < d)) return bad(F, "a token stride is smaller than the width");
   if (B > 1 && seq_out < d) return bad(F, "the output's sequence stride is smaller than the width");
   size_t need = 0;
   un_gated_scan_sizes(B, T, d, nullptr, &need);
   if (need && (!workspace || bytes < need)) return bad(F, "workspace too small (un_gated_scan_sizes)", UN_ERR_BUFSIZE);
-  *plan = scan_plan(B, T, d, pairs);
-  if (too_many((int64_t)plan->tiles * B * plan->nseg, plan->kind == 2 ? 64 * SCAN_W : 64))
+  *plan = scan_plan(B, T, d);
+  if (too_many((int64_t)plan->tiles * B * plan->nseg, plan->kind >= SCAN_CHUNKS ? 64 * SCAN_W : 64))
     return bad(F, "too many sequences and channels", UN_ERR_UNSUPPORTED);
   return UN_OK;
-}
-// two neighbouring channels in one access, for every row of the operand
-bool pairs_ok(int32_t type, const void* p, int64_t ld, int64_t seq) {
-  return (uintptr_t)p % (type == UN_TYPE_BF16 ? 4 : 8) == 0 && ld % 2 == 0 && seq % 2 == 0;
 }
 }  // namespace
 
@@ -181,10 +178,8 @@ un_status un_gated_scan(const un_gated_scan_args* a, void* stream) {
   const char* F = "un_gated_scan";
   if (!a) return bad(F, "args is NULL");
   ScanPlan plan;
-  const bool pairs = a->width % 2 == 0 && pairs_ok(a->type, a->gate, a->ld_in, a->seq_in) &&
-                     pairs_ok(a->type, a->value, a->ld_in, a->seq_in) && pairs_ok(a->type, a->h, a->ld_h, a->seq_h);
   const un_status st = scan_common(F, a->type, a->batch, a->tokens, a->width, a->ld_in, a->ld_h, a->ld_h, a->seq_h,
-                                   a->workspace, a->workspace_bytes, pairs, &plan);
+                                   a->workspace, a->workspace_bytes, &plan);
   if (st != UN_OK) return st;
   if (a->batch == 0 || a->width == 0) return UN_OK;
   if (a->tokens > 0 && (!a->gate || !a->value || !a->h)) return bad(F, "gate, value or h is NULL");
@@ -211,11 +206,8 @@ un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream)
   const char* F = "un_gated_scan_backward";
   if (!a) return bad(F, "args is NULL");
   ScanPlan plan;
-  const bool pairs = a->width % 2 == 0 && pairs_ok(a->type, a->gate, a->ld_in, a->seq_in) &&
-                     pairs_ok(a->type, a->value, a->ld_in, a->seq_in) && pairs_ok(a->type, a->dh, a->ld_dh, a->seq_dh) &&
-                     pairs_ok(a->type, a->dgate, a->ld_out, a->seq_out) && pairs_ok(a->type, a->dvalue, a->ld_out, a->seq_out);
   const un_status st = scan_common(F, a->type, a->batch, a->tokens, a->width, a->ld_in, a->ld_dh, a->ld_out, a->seq_out,
-                                   a->workspace, a->workspace_bytes, pairs, &plan);
+                                   a->workspace, a->workspace_bytes, &plan);
   if (st != UN_OK) return st;
   if (a->batch == 0 || a->width == 0) return UN_OK;
   if (a->tokens > 0 && (!a->gate || !a->value || !a->dh || !a->states || !a->dgate || !a->dvalue))

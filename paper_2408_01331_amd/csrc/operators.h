@@ -75,27 +75,30 @@ struct ScanProb {
   const int32_t* lens;        // null: every sequence has T steps
   const float* start;         // forward: h_0 [B][d]; backward: the gradient at the last state; null: 0
   float* end;                 // forward: last state [B][d]; backward: dh_0; null: not wanted
-  float* states;              // h at the start of every SCAN_CHUNK steps [B][chunks][d] (forward: written if not null)
+  float* states;              // h at the start of every SCAN_STATE steps [B][scan_chunks][d] (forward: written if not null)
   float* agg;                 // split passes: per segment and channel (A, H), [nseg][B][d][2], then a copy of start [B][d]
   int32_t B, T, d;
-  int32_t tiles;              // channel tiles
-  int32_t seg, nseg;          // chunks per segment; segments
+  int32_t tiles;              // tiles of 64 channels
+  int32_t seg, nseg;          // steps per segment, in SCAN_STATE; segments
 };
-constexpr int SCAN_W = 8, SCAN_L = 16;             // waves of a workgroup; steps per wave and chunk
-constexpr int SCAN_CHUNK = SCAN_W * SCAN_L;
-inline int scan_chunks(int T) { return (T + SCAN_CHUNK - 1) / SCAN_CHUNK; }
+constexpr int SCAN_STATE = 64;                     // steps between two kept states
+constexpr int SCAN_SHORT = 16;                     // steps that one wave takes at once
+constexpr int SCAN_W = 8;                          // waves of a workgroup over longer sequences
+// 16 rows of a stride up to this and their width fit 31 bits in bytes
+constexpr int64_t SCAN_MAX_LD = 1 << 24;
+__host__ __device__ inline int scan_chunks(int T) { return (T + SCAN_STATE - 1) / SCAN_STATE; }
+// One step; up to SCAN_SHORT (a wave each); chunks of SCAN_W waves x 8 steps; x 16.
+enum ScanKind { SCAN_ONE, SCAN_WAVE, SCAN_CHUNKS, SCAN_LONG_CHUNKS };
 struct ScanPlan {
-  int vb;                     // channels per lane
-  int kind;                   // 0: one step, 1: up to SCAN_L steps (one wave), 2: chunks
+  ScanKind kind;
   int tiles, seg, nseg;
 };
 inline size_t scan_ws_bytes(const ScanPlan& p, int64_t B, int d) { return p.nseg > 1 ? (size_t)(2 * p.nseg + 1) * B * d * 4 : 0; }
-// pairs: every row of the operands allows loads of two channels at once
-ScanPlan scan_plan(int64_t B, int T, int d, bool pairs);
+ScanPlan scan_plan(int64_t B, int T, int d);
 hipError_t launch_scan(bool bf16, bool bwd, const ScanPlan& plan, const ScanProb& p, hipStream_t s);
-// table: one (problem, sequence * tiles + tile) pair per workgroup; every problem nseg == 1. kind, vb: as ScanPlan's
-// (kind 1 or 2, the same for every problem)
-hipError_t launch_scan_table(bool bf16, bool bwd, int kind, int vb, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s);
+// table: one (problem, sequence * tiles + tile) pair per workgroup; every problem has nseg == 1 and, where `shorts`, at
+// most SCAN_SHORT steps
+hipError_t launch_scan_table(bool bf16, bool bwd, bool shorts, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // AdamW over many tensors. States fp32, or e4m3 codes with a power of two per

@@ -459,61 +459,44 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__
 }
 
 // ---------------------------------------------------------------------------
-// Gated linear recurrence. A wave's lanes are channels (VB neighbouring ones
-// each), so a step's row is one coalesced access and a step needs no exchange
-// between lanes. A chunk is W x L steps: wave w holds steps [w L, (w + 1) L) in
-// registers and composes them into one map h -> A h + H; the maps of the waves
-// meet in LDS, each wave folds those before its own, and walks its steps again
-// from registers. So g and v are read once and the recurrence's serial part is
-// L steps long per chunk, and W folds.
+// Gated linear recurrence. A wave's lanes are 64 neighbouring channels, so a
+// step's row is one coalesced access (a whole 128-byte line in bf16) and a step
+// needs no exchange between lanes. A chunk is W x L steps: wave w holds steps
+// [w L, (w + 1) L) in registers and composes them into one map h -> A h + H; the
+// maps of the waves meet in LDS, each wave folds those before its own, and walks
+// its steps again from registers. So every operand is read once and the
+// recurrence's serial part is W folds and L steps per chunk.
 // ---------------------------------------------------------------------------
-template <typename T, int VB> struct Raw;
-template <> struct Raw<bf16_t, 1> {
-  uint16_t v;
-  __device__ float get(int) const { return bf2f(v); }
-};
-template <> struct Raw<bf16_t, 2> {
-  uint32_t v;
-  __device__ float get(int e) const { return __uint_as_float(e ? v & 0xffff0000u : v << 16); }
-};
-template <> struct Raw<float, 1> {
-  float v;
-  __device__ float get(int) const { return v; }
-};
-template <> struct Raw<float, 2> {
-  float v[2];
-  __device__ float get(int e) const { return v[e]; }
-};
-template <typename T, int VB> __device__ __forceinline__ void raw_store(T* p, const float* f) {
+typedef __amdgpu_buffer_rsrc_t Rsrc;
+// A value of a row at byte offset vo of the lane plus so, the row's (past the
+// descriptor's end: zero, or nothing stored).
+template <typename T> __device__ __forceinline__ T raw_load(Rsrc r, uint32_t vo, uint32_t so) {
+  if constexpr (sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(r, vo, so, 0);
+  else return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, vo, so, 0));
+}
+template <typename T> __device__ __forceinline__ void raw_store(Rsrc r, uint32_t vo, uint32_t so, float f) {
+  if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16((bf16_t)f2bf(f), r, vo, so, 0);
+  else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(f), r, vo, so, 0);
+}
+__device__ __forceinline__ float value_of(bf16_t v) { return bf2f(v); }
+__device__ __forceinline__ float value_of(float v) { return v; }
+
+// a = sigmoid(g) and k = 1 - a, each to its own relative accuracy: with e =
+// exp(-g), a = 1 / (1 + e), and k = e a where e < 1, else 1 - a (an infinite e
+// gives 0 and 1, a NaN stays one). fp32: e with the rounding error of its
+// argument, so that it is as exact for large |g|.
+template <typename T> __device__ __forceinline__ void gate_of(T raw, float& a, float& k) {
+  const float g = value_of(raw), L2E = -1.44269504f, t = g * L2E;
+  float e = __builtin_amdgcn_exp2f(t);
   if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int e = 0; e < VB; ++e) p[e] = f[e];
-  } else if constexpr (VB == 2) {
-    *(uint32_t*)p = f2bf2(f[0], f[1]);
-  } else {
-    *p = (bf16_t)f2bf(f[0]);
+    const float r = fmaf(g, -1.925963033e-8f, fmaf(g, L2E, -t)) * 0.693147181f;
+    e = fabsf(g) < 128.f ? fmaf(e, r, e) : e;  // (an infinite g has no rounding error)
   }
+  a = __builtin_amdgcn_rcpf(1.f + e);
+  k = e < 1.f ? e * a : 1.f - a;
 }
 
-// a = sigmoid(g) and k = 1 - a = sigmoid(-g), each to its own relative accuracy.
-// fp32: the product g log2(e) with its rounding error, so that exp is as exact for large |g|.
-template <typename T> __device__ __forceinline__ void gate_of(float g, float& a, float& k) {
-  const float x = -fabsf(g), L2E = 1.44269504f;
-  float t = x * L2E, em;
-  if constexpr (sizeof(T) == 4) {
-    const float r = fmaf(x, 1.925963033e-8f, fmaf(x, L2E, -t)) * 0.693147181f;
-    em = __builtin_amdgcn_exp2f(t);
-    em = x > -128.f ? fmaf(em, r, em) : em;  // (an infinite g has no rounding error)
-  } else {
-    em = __builtin_amdgcn_exp2f(t);
-  }
-  const float big = __builtin_amdgcn_rcpf(1.f + em), small = em * big;
-  a = g >= 0.f ? big : small;
-  k = g >= 0.f ? small : big;
-  if (g != g) a = k = g;
-}
-
-// LDS is exchanged between waves once per chunk; global loads stay in flight
+// LDS is exchanged between waves once per chunk; global accesses stay in flight
 // across the barrier.
 __device__ __forceinline__ void lds_barrier() {
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -522,15 +505,16 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 struct Tile {
-  int c;          // first channel of this lane
+  int c;          // channel of this lane (0 for a lane past the width)
   bool on;        // within the width
   int b, w;       // sequence; wave
   int len;        // its steps
   int64_t bc;     // b * d + c
+  template <typename T> __device__ uint32_t at() const { return on ? (uint32_t)c * (uint32_t)sizeof(T) : 0x80000000u; }
 };
-template <int VB> __device__ __forceinline__ Tile tile_of(const ScanProb& p, int tile, int b) {
+__device__ __forceinline__ Tile tile_of(const ScanProb& p, int tile, int b) {
   Tile t;
-  const int c = (tile * 64 + (threadIdx.x & 63)) * VB;
+  const int c = tile * 64 + (threadIdx.x & 63);
   t.on = c < p.d;
   t.c = t.on ? c : 0;
   t.b = b;
@@ -540,374 +524,349 @@ template <int VB> __device__ __forceinline__ Tile tile_of(const ScanProb& p, int
   return t;
 }
 
-// Rows [t0, t0 + L) of one operand; rows at and behind `len` (> 0) repeat its last one.
-template <typename T, int VB, int L>
-__device__ __forceinline__ void load_rows(const void* base, int64_t ld, int64_t bs, const Tile& t, int t0, Raw<T, VB>* r) {
-  const T* p = (const T*)base + t.b * bs + t.c;
-#pragma unroll
-  for (int i = 0; i < L; ++i) r[i] = *(const Raw<T, VB>*)(p + (int64_t)min(t0 + i, t.len - 1) * ld);
+// Rows of an operand from step i on: a descriptor of 2^31 - 1 bytes, within which
+// the L rows of a lane lie (SCAN_MAX_LD); a lane past the width has an offset of
+// 2^31, so that it reads zeros and stores nothing. Further rows by a scalar offset:
+// a row costs no vector arithmetic (with 64-bit lane addresses the forward pass of
+// 16 x 2048 x 1024 in bf16 took 52 us, so 48).
+template <typename T> __device__ __forceinline__ Rsrc rows_at(const void* base, int64_t ld, int64_t bs, const Tile& t, int i) {
+  return __builtin_amdgcn_make_buffer_rsrc((char*)base + (t.b * bs + (int64_t)i * ld) * (int64_t)sizeof(T), (short)0,
+                                           0x7fffffff, 0x00020000);
 }
-template <typename T, int VB>
+
+// Rows [t0, t0 + L) of one operand; rows at and behind `len` (> 0) repeat its last one.
+template <typename T, int L>
+__device__ __forceinline__ void load_rows(const void* base, int64_t ld, int64_t bs, const Tile& t, int t0, T* r) {
+  const int first = min(t0, t.len - 1), most = t.len - 1 - first;
+  const uint32_t step = (uint32_t)(ld * (int64_t)sizeof(T));
+  const Rsrc rows = rows_at<T>(base, ld, bs, t, first);
+#pragma unroll
+  for (int i = 0; i < L; ++i) r[i] = raw_load<T>(rows, t.at<T>(), min(i, most) * step);
+}
+template <typename T>
 __device__ __forceinline__ void zero_rows(void* base, int64_t ld, int64_t bs, const Tile& t, int t0, int t1, int step) {
-  const float z[VB] = {};
-  T* p = (T*)base + t.b * bs + t.c;
-  if (t.on)
-    for (int i = t0; i < t1; i += step) raw_store<T, VB>(p + (int64_t)i * ld, z);
+  for (int i = t0; i < t1; i += step) raw_store<T>(rows_at<T>(base, ld, bs, t, i), t.at<T>(), 0, 0.f);
 }
 
 // The maps of the segments before (forward) or behind (backward) `s`, folded
 // over `h` in order: each wave folds a run of them, and every wave the runs.
-template <int VB, int W>
-__device__ __forceinline__ void fold_segments(const ScanProb& p, const Tile& t, int s, bool bwd, float* h, float* sm) {
+template <int W>
+__device__ __forceinline__ void fold_segments(const ScanProb& p, const Tile& t, int s, bool bwd, float& h, float* sm) {
   const int n = bwd ? p.nseg - 1 - s : s;
   if (n == 0) return;  // the same for the whole workgroup
   const int per = (n + W - 1) / W, j0 = min(n, t.w * per), j1 = min(n, j0 + per);
-  const int64_t stride = (int64_t)p.B * p.d * 2;
-  const float* agg = p.agg + t.bc * 2;
-  float A[VB], H[VB];
-#pragma unroll
-  for (int e = 0; e < VB; ++e) A[e] = 1.f, H[e] = 0.f;
+  const int64_t stride = (int64_t)p.B * p.d;
+  const float2* agg = (const float2*)p.agg + t.bc;
+  float A = 1.f, H = 0.f;
   for (int j = j0; j < j1; j += 8) {
-    float a[8][VB], b[8][VB];
+    float2 m[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int k = min(j + u, j1 - 1), seg = bwd ? p.nseg - 1 - k : k;
-#pragma unroll
-      for (int e = 0; e < VB; ++e) {
-        a[u][e] = agg[seg * stride + 2 * e];
-        b[u][e] = agg[seg * stride + 2 * e + 1];
-      }
+      const int k = min(j + u, j1 - 1);
+      m[u] = agg[(bwd ? p.nseg - 1 - k : k) * stride];
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u)
-      if (j + u < j1)
-#pragma unroll
-        for (int e = 0; e < VB; ++e) {
-          H[e] = fmaf(a[u][e], H[e], b[u][e]);
-          A[e] *= a[u][e];
-        }
+      if (j + u < j1) {
+        H = fmaf(m[u].x, H, m[u].y);
+        A *= m[u].x;
+      }
   }
+  float2* maps = (float2*)sm;
   const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int e = 0; e < VB; ++e) {
-    sm[((t.w * VB + e) * 2 + 0) * 64 + lane] = A[e];
-    sm[((t.w * VB + e) * 2 + 1) * 64 + lane] = H[e];
-  }
+  maps[t.w * 64 + lane] = float2{A, H};
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < W; ++w)
-#pragma unroll
-    for (int e = 0; e < VB; ++e) h[e] = fmaf(sm[((w * VB + e) * 2) * 64 + lane], h[e], sm[((w * VB + e) * 2 + 1) * 64 + lane]);
+  for (int w = 0; w < W; ++w) h = fmaf(maps[w * 64 + lane].x, h, maps[w * 64 + lane].y);
   __syncthreads();
 }
 
-template <typename T, int VB, int W, int L>
+// Runs prepare(k, slot) and finish(k, slot) over nc chunks, k = first, first +
+// dir, ..., with the barrier between them. PIPE: a chunk is prepared while the one
+// before it is finished, so the two streams of instructions fill one another's
+// stalls; without, slot 0 alone is used (fewer registers, more workgroups per CU).
+template <int W, bool PIPE, typename P, typename F>
+__device__ __forceinline__ void chunks(int nc, int first, int dir, P&& prepare, F&& finish) {
+  auto sync = [] {
+    if (W > 1) lds_barrier();
+  };
+  using Slot0 = std::integral_constant<int, 0>;
+  using Slot1 = std::integral_constant<int, 1>;
+  if constexpr (!PIPE) {
+    // LDS by the chunk's parity: one barrier a chunk
+    for (int n = 0; n < nc; ++n) {
+      prepare(first + n * dir, Slot0{}, n & 1);
+      sync();
+      finish(first + n * dir, Slot0{}, n & 1);
+    }
+  } else {
+    if (nc > 0) {
+      prepare(first, Slot0{}, 0);
+      sync();
+    }
+    for (int n = 0; n < nc; n += 2) {
+      if (n + 1 < nc) prepare(first + (n + 1) * dir, Slot1{}, 1);
+      finish(first + n * dir, Slot0{}, 0);
+      sync();
+      if (n + 1 == nc) break;
+      if (n + 2 < nc) prepare(first + (n + 2) * dir, Slot0{}, 0);
+      finish(first + (n + 1) * dir, Slot1{}, 1);
+      sync();
+    }
+  }
+}
+
+template <typename T, int W, int L, bool PIPE>
 __device__ __forceinline__ void scan_fwd(const ScanProb& p, int tile, int b, int s, float* sm) {
   constexpr int C = W * L;
-  const Tile t = tile_of<VB>(p, tile, b);
-  const int lane = threadIdx.x & 63;
-  const int tb = s * p.seg * C, te = min(p.T, tb + p.seg * C);
+  const Tile t = tile_of(p, tile, b);
+  const int lane = threadIdx.x & 63, span = p.seg * SCAN_STATE;  // steps of a segment
+  const int tb = s * span, te = min(p.T, tb + span);
   const int nc = max(0, min(t.len, te) - tb + C - 1) / C;  // chunks with a live step
-  float h[VB];
-#pragma unroll
-  for (int e = 0; e < VB; ++e) {
-    h[e] = p.start ? p.start[t.bc + e] : 0.f;
-    asm volatile("" : "+v"(h[e]));  // here before the first barrier: `end` may be the same memory
-  }
-  if (W > 1) fold_segments<VB, W>(p, t, s, false, h, sm);
-  Raw<T, VB> rg[L], rv[L];
-  if (nc > 0) {
-    load_rows<T, VB, L>(p.gate, p.ldi, p.bsi, t, tb + t.w * L, rg);
-    load_rows<T, VB, L>(p.value, p.ldi, p.bsi, t, tb + t.w * L, rv);
-  }
-  T* out = (T*)p.o1 + b * p.bso + t.c;
-  for (int k = 0; k < nc; ++k) {
+  float h = p.start ? p.start[t.bc] : 0.f;
+  asm volatile("" : "+v"(h));  // here before the first barrier: `end` may be the same memory
+  T rg[L], rv[L];
+  struct Steps {
+    float a[L], x[L];
+  } steps[PIPE ? 2 : 1];
+  auto load = [&](int k) {
+    load_rows<T, L>(p.gate, p.ldi, p.bsi, t, tb + k * C + t.w * L, rg);
+    load_rows<T, L>(p.value, p.ldi, p.bsi, t, tb + k * C + t.w * L, rv);
+  };
+  if (nc > 0) load(0);
+  if (W > 1) fold_segments<W>(p, t, s, false, h, sm);
+  auto prepare = [&](int k, auto slot, int half) {
+    Steps& q = steps[slot()];
     const int t0 = tb + k * C + t.w * L;
-    float a[L][VB], x[L][VB];
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int e = 0; e < VB; ++e) {
-        float keep;
-        gate_of<T>(rg[i].get(e), a[i][e], keep);
-        x[i][e] = keep * rv[i].get(e);
-      }
-    if (k + 1 < nc) {
-      load_rows<T, VB, L>(p.gate, p.ldi, p.bsi, t, t0 + C, rg);
-      load_rows<T, VB, L>(p.value, p.ldi, p.bsi, t, t0 + C, rv);
+    for (int i = 0; i < L; ++i) {
+      float keep;
+      gate_of<T>(rg[i], q.a[i], keep);
+      q.x[i] = keep * value_of(rv[i]);
     }
-    const bool whole = t0 + L <= t.len;
-    if (!whole)
+    if (k + 1 < nc) load(k + 1);
+    if (t0 + L > t.len)
 #pragma unroll
       for (int i = 0; i < L; ++i)
-        if (t0 + i >= t.len)
-#pragma unroll
-          for (int e = 0; e < VB; ++e) a[i][e] = 1.f, x[i][e] = 0.f;
-    if (p.states && t.w == 0 && t.on) {
-      float* st = p.states + ((int64_t)b * ((p.T + C - 1) / C) + s * p.seg + k) * p.d + t.c;
-#pragma unroll
-      for (int e = 0; e < VB; ++e) st[e] = h[e];
-    }
-    float now[VB];
-#pragma unroll
-    for (int e = 0; e < VB; ++e) now[e] = h[e];
+        if (t0 + i >= t.len) q.a[i] = 1.f, q.x[i] = 0.f;
     if constexpr (W > 1) {
-      float* buf = sm + (k & 1) * W * VB * 2 * 64;
-#pragma unroll
-      for (int e = 0; e < VB; ++e) {
-        float A = 1.f, H = 0.f;
-#pragma unroll
-        for (int i = 0; i < L; ++i) {
-          H = fmaf(a[i][e], H, x[i][e]);
-          A *= a[i][e];
-        }
-        buf[((t.w * VB + e) * 2 + 0) * 64 + lane] = A;
-        buf[((t.w * VB + e) * 2 + 1) * 64 + lane] = H;
-      }
-      // one barrier a chunk: the other half of the buffer serves the next one
-      lds_barrier();
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        if (w == t.w)
-#pragma unroll
-          for (int e = 0; e < VB; ++e) now[e] = h[e];
-#pragma unroll
-        for (int e = 0; e < VB; ++e) h[e] = fmaf(buf[((w * VB + e) * 2) * 64 + lane], h[e], buf[((w * VB + e) * 2 + 1) * 64 + lane]);
-      }
-    }
-    if (t.on) {
+      float A = 1.f, H = 0.f;
 #pragma unroll
       for (int i = 0; i < L; ++i) {
+        H = fmaf(q.a[i], H, q.x[i]);
+        A *= q.a[i];
+      }
+      ((float2*)sm)[(half * W + t.w) * 64 + lane] = float2{A, H};
+    }
+  };
+  auto finish = [&](int k, auto slot, int half) {
+    const Steps& q = steps[slot()];
+    const int t0 = tb + k * C + t.w * L;
+    float now = h;
+    if constexpr (W > 1) {
+      float2 m[W];
 #pragma unroll
-        for (int e = 0; e < VB; ++e) now[e] = fmaf(a[i][e], now[e], x[i][e]);
-        if (whole || t0 + i < t.len) raw_store<T, VB>(out + (int64_t)(t0 + i) * p.ldo, now);
+      for (int w = 0; w < W; ++w) m[w] = ((const float2*)sm)[(half * W + w) * 64 + lane];
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        now = w == t.w ? h : now;
+        h = fmaf(m[w].x, h, m[w].y);
       }
     }
-    if constexpr (W == 1) {
+    if (p.states && t0 % SCAN_STATE == 0 && t0 < p.T && t.on) p.states[((int64_t)b * scan_chunks(p.T) + t0 / SCAN_STATE) * p.d + t.c] = now;
+    const Rsrc rows = rows_at<T>(p.o1, p.ldo, p.bso, t, t0);
+    const uint32_t step = (uint32_t)(p.ldo * (int64_t)sizeof(T));
+    auto walk = [&](auto all) {
 #pragma unroll
-      for (int e = 0; e < VB; ++e) h[e] = now[e];
-    }
-  }
-  zero_rows<T, VB>(p.o1, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
-  if (p.end && s == p.nseg - 1 && t.w == 0 && t.on)
-#pragma unroll
-    for (int e = 0; e < VB; ++e) p.end[t.bc + e] = h[e];
+      for (int i = 0; i < L; ++i) {
+        now = fmaf(q.a[i], now, q.x[i]);
+        if (decltype(all)::value || t0 + i < t.len) raw_store<T>(rows, t.at<T>(), i * step, now);
+      }
+    };
+    t0 + L <= t.len ? walk(std::true_type{}) : walk(std::false_type{});
+    if (W == 1) h = now;
+  };
+  chunks<W, PIPE>(nc, 0, 1, prepare, finish);
+  zero_rows<T>(p.o1, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
+  if (p.end && s == p.nseg - 1 && t.w == 0 && t.on) p.end[t.bc] = h;
 }
 
-template <typename T, int VB, int W, int L>
+template <typename T, int W, int L, bool PIPE>
 __device__ __forceinline__ void scan_bwd(const ScanProb& p, int tile, int b, int s, float* sm) {
   constexpr int C = W * L;
-  const Tile t = tile_of<VB>(p, tile, b);
-  const int lane = threadIdx.x & 63;
-  const int tb = s * p.seg * C, te = min(p.T, tb + p.seg * C);
+  const Tile t = tile_of(p, tile, b);
+  const int lane = threadIdx.x & 63, span = p.seg * SCAN_STATE;
+  const int tb = s * span, te = min(p.T, tb + span);
   const int nc = max(0, min(t.len, te) - tb + C - 1) / C;
-  float c[VB];  // a_{t+1} e_{t+1}: the gradient that arrives from the later steps
-#pragma unroll
-  for (int e = 0; e < VB; ++e) {
-    c[e] = p.start ? p.start[t.bc + e] : 0.f;
-    asm volatile("" : "+v"(c[e]));
-  }
-  if (W > 1) fold_segments<VB, W>(p, t, s, true, c, sm);
-  const int64_t st0 = ((int64_t)b * ((p.T + C - 1) / C) + s * p.seg) * p.d + t.c;
-  Raw<T, VB> rg[L], rv[L], rd[L];
-  float rh[VB];
+  float c = p.start ? p.start[t.bc] : 0.f;  // a_{t+1} e_{t+1}: the gradient that arrives from the later steps
+  asm volatile("" : "+v"(c));
+  const float* states = p.states + ((int64_t)b * scan_chunks(p.T) + tb / SCAN_STATE) * p.d + t.c;
+  T rg[L], rv[L], rd[L];
+  float rh = 0.f;
+  struct Steps {
+    float a[L], kp[L], v[L], dh[L], h;
+  } steps[PIPE ? 2 : 1];
   auto load = [&](int k) {
     const int t0 = tb + k * C + t.w * L;
-    load_rows<T, VB, L>(p.gate, p.ldi, p.bsi, t, t0, rg);
-    load_rows<T, VB, L>(p.value, p.ldi, p.bsi, t, t0, rv);
-    load_rows<T, VB, L>(p.dh, p.lddh, p.bsdh, t, t0, rd);
-#pragma unroll
-    for (int e = 0; e < VB; ++e) rh[e] = p.states[st0 + (int64_t)k * p.d + e];
+    load_rows<T, L>(p.gate, p.ldi, p.bsi, t, t0, rg);
+    load_rows<T, L>(p.value, p.ldi, p.bsi, t, t0, rv);
+    load_rows<T, L>(p.dh, p.lddh, p.bsdh, t, t0, rd);
+    rh = states[(int64_t)k * (C / SCAN_STATE ? C / SCAN_STATE : 1) * p.d];
   };
   if (nc > 0) load(nc - 1);
-  T* og = (T*)p.o1 + b * p.bso + t.c;
-  T* ov = (T*)p.o2 + b * p.bso + t.c;
-  for (int k = nc - 1; k >= 0; --k) {
+  if (W > 1) fold_segments<W>(p, t, s, true, c, sm);
+  auto prepare = [&](int k, auto slot, int half) {
+    Steps& q = steps[slot()];
     const int t0 = tb + k * C + t.w * L;
-    float a[L][VB], x[L][VB], v[L][VB], dh[L][VB], kp[L][VB], h[VB];
+    q.h = rh;
 #pragma unroll
-    for (int e = 0; e < VB; ++e) h[e] = rh[e];
-#pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int e = 0; e < VB; ++e) {
-        gate_of<T>(rg[i].get(e), a[i][e], kp[i][e]);
-        v[i][e] = rv[i].get(e);
-        x[i][e] = kp[i][e] * v[i][e];
-        dh[i][e] = rd[i].get(e);
-      }
+    for (int i = 0; i < L; ++i) {
+      gate_of<T>(rg[i], q.a[i], q.kp[i]);
+      q.v[i] = value_of(rv[i]);
+      q.dh[i] = value_of(rd[i]);
+    }
     if (k > 0) load(k - 1);
-    const bool whole = t0 + L <= t.len;
-    if (!whole)
+    if (t0 + L > t.len)
 #pragma unroll
       for (int i = 0; i < L; ++i)
-        if (t0 + i >= t.len)
-#pragma unroll
-          for (int e = 0; e < VB; ++e) a[i][e] = 1.f, x[i][e] = 0.f, dh[i][e] = 0.f;
-    float cn[VB];
-#pragma unroll
-    for (int e = 0; e < VB; ++e) cn[e] = c[e];
+        if (t0 + i >= t.len) q.a[i] = 1.f, q.kp[i] = q.v[i] = q.dh[i] = 0.f;
     if constexpr (W > 1) {
-      float* buf = sm + (k & 1) * W * VB * 3 * 64;
+      float A = 1.f, H = 0.f, Q = 0.f;
 #pragma unroll
-      for (int e = 0; e < VB; ++e) {
-        float A = 1.f, H = 0.f, Q = 0.f;
-#pragma unroll
-        for (int i = 0; i < L; ++i) {
-          H = fmaf(a[i][e], H, x[i][e]);
-          A *= a[i][e];
-        }
-#pragma unroll
-        for (int i = L - 1; i >= 0; --i) Q = a[i][e] * (dh[i][e] + Q);
-        buf[((t.w * VB + e) * 3 + 0) * 64 + lane] = A;
-        buf[((t.w * VB + e) * 3 + 1) * 64 + lane] = H;
-        buf[((t.w * VB + e) * 3 + 2) * 64 + lane] = Q;
+      for (int i = 0; i < L; ++i) {
+        H = fmaf(q.a[i], H, q.kp[i] * q.v[i]);
+        A *= q.a[i];
       }
-      lds_barrier();
 #pragma unroll
-      for (int w = 0; w < W; ++w)
-        if (w < t.w)
+      for (int i = L - 1; i >= 0; --i) Q = q.a[i] * (q.dh[i] + Q);
+      ((f32x4*)sm)[(half * W + t.w) * 64 + lane] = f32x4{A, H, Q, 0.f};
+    }
+  };
+  auto finish = [&](int k, auto slot, int half) {
+    Steps& q = steps[slot()];
+    const int t0 = tb + k * C + t.w * L;
+    float cn = c, h = q.h;
+    if constexpr (W > 1) {
+      f32x4 m[W];
 #pragma unroll
-          for (int e = 0; e < VB; ++e) h[e] = fmaf(buf[((w * VB + e) * 3) * 64 + lane], h[e], buf[((w * VB + e) * 3 + 1) * 64 + lane]);
+      for (int w = 0; w < W; ++w) m[w] = ((const f32x4*)sm)[(half * W + w) * 64 + lane];
+#pragma unroll
+      for (int w = 0; w < W - 1; ++w) h = w < t.w ? fmaf(m[w][0], h, m[w][1]) : h;
 #pragma unroll
       for (int w = W - 1; w >= 0; --w) {
-        if (w == t.w)
-#pragma unroll
-          for (int e = 0; e < VB; ++e) cn[e] = c[e];
-#pragma unroll
-        for (int e = 0; e < VB; ++e) c[e] = fmaf(buf[((w * VB + e) * 3) * 64 + lane], c[e], buf[((w * VB + e) * 3 + 2) * 64 + lane]);
+        cn = w == t.w ? c : cn;
+        c = fmaf(m[w][0], c, m[w][2]);
       }
     }
-    // x becomes h_{t-1} - v_t, walking forward; then the gradients, walking back
+    // v becomes h_{t-1} - v_t, walking forward; then the gradients, walking back
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int e = 0; e < VB; ++e) {
-        const float next = fmaf(a[i][e], h[e], x[i][e]);
-        x[i][e] = h[e] - v[i][e];
-        h[e] = next;
-      }
-#pragma unroll
-    for (int i = L - 1; i >= 0; --i) {
-      float dg[VB], dv[VB];
-#pragma unroll
-      for (int e = 0; e < VB; ++e) {
-        const float g = dh[i][e] + cn[e];
-        dv[e] = kp[i][e] * g;
-        cn[e] = a[i][e] * g;
-        dg[e] = kp[i][e] * cn[e] * x[i][e];
-      }
-      if (t.on && (whole || t0 + i < t.len)) {
-        raw_store<T, VB>(og + (int64_t)(t0 + i) * p.ldo, dg);
-        raw_store<T, VB>(ov + (int64_t)(t0 + i) * p.ldo, dv);
-      }
+    for (int i = 0; i < L; ++i) {
+      const float next = fmaf(q.a[i], h, q.kp[i] * q.v[i]);
+      q.v[i] = h - q.v[i];
+      h = next;
     }
-    if constexpr (W == 1) {
+    const Rsrc og = rows_at<T>(p.o1, p.ldo, p.bso, t, t0), ov = rows_at<T>(p.o2, p.ldo, p.bso, t, t0);
+    const uint32_t step = (uint32_t)(p.ldo * (int64_t)sizeof(T));
+    auto walk = [&](auto all) {
 #pragma unroll
-      for (int e = 0; e < VB; ++e) c[e] = cn[e];
-    }
-  }
-  zero_rows<T, VB>(p.o1, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
-  zero_rows<T, VB>(p.o2, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
-  if (p.end && s == 0 && t.w == 0 && t.on)
-#pragma unroll
-    for (int e = 0; e < VB; ++e) p.end[t.bc + e] = c[e];
+      for (int i = L - 1; i >= 0; --i) {
+        const float g = q.dh[i] + cn;
+        cn = q.a[i] * g;
+        if (decltype(all)::value || t0 + i < t.len) {
+          raw_store<T>(og, t.at<T>(), i * step, q.kp[i] * cn * q.v[i]);
+          raw_store<T>(ov, t.at<T>(), i * step, q.kp[i] * g);
+        }
+      }
+    };
+    t0 + L <= t.len ? walk(std::true_type{}) : walk(std::false_type{});
+    if (W == 1) c = cn;
+  };
+  chunks<W, PIPE>(nc, nc - 1, -1, prepare, finish);
+  zero_rows<T>(p.o1, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
+  zero_rows<T>(p.o2, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
+  if (p.end && s == 0 && t.w == 0 && t.on) p.end[t.bc] = c;
 }
 
 // The map of one segment: forward h -> A h + H, backward c -> A c + Q.
 // Each wave composes a run of the segment's steps of its own, L at a time.
-template <typename T, int VB, int W, int L, bool BWD>
+template <typename T, int W, int L, bool BWD>
 __device__ __forceinline__ void scan_agg(const ScanProb& p, int tile, int b, int s, float* sm) {
-  const Tile t = tile_of<VB>(p, tile, b);
+  const Tile t = tile_of(p, tile, b);
   const int lane = threadIdx.x & 63;
-  const int n = p.seg * L;                         // steps per wave
-  const int tb = s * p.seg * W * L + t.w * n, te = min(t.len, tb + n);
-  float A[VB], H[VB];
-#pragma unroll
-  for (int e = 0; e < VB; ++e) A[e] = 1.f, H[e] = 0.f;
+  const int n = p.seg * SCAN_STATE / W;            // steps per wave
+  const int tb = s * p.seg * SCAN_STATE + t.w * n, te = min(t.len, tb + n);
+  float A = 1.f, H = 0.f;
   const int m = max(0, te - tb + L - 1) / L;
-  Raw<T, VB> rg[L], rv[L];
+  T rg[L], rv[L];
   auto load = [&](int k) {
     const int t0 = tb + (BWD ? m - 1 - k : k) * L;
-    load_rows<T, VB, L>(p.gate, p.ldi, p.bsi, t, t0, rg);
-    if (BWD) load_rows<T, VB, L>(p.dh, p.lddh, p.bsdh, t, t0, rv);
-    else load_rows<T, VB, L>(p.value, p.ldi, p.bsi, t, t0, rv);
+    load_rows<T, L>(p.gate, p.ldi, p.bsi, t, t0, rg);
+    if (BWD) load_rows<T, L>(p.dh, p.lddh, p.bsdh, t, t0, rv);
+    else load_rows<T, L>(p.value, p.ldi, p.bsi, t, t0, rv);
   };
   if (m > 0) load(0);
   for (int k = 0; k < m; ++k) {
     const int t0 = tb + (BWD ? m - 1 - k : k) * L;
-    float a[L][VB], x[L][VB];
+    float a[L], x[L];
 #pragma unroll
-    for (int i = 0; i < L; ++i)
-#pragma unroll
-      for (int e = 0; e < VB; ++e) {
-        float keep;
-        gate_of<T>(rg[i].get(e), a[i][e], keep);
-        x[i][e] = (BWD ? 1.f : keep) * rv[i].get(e);
-        if (t0 + i >= te) a[i][e] = 1.f, x[i][e] = 0.f;
-      }
+    for (int i = 0; i < L; ++i) {
+      float keep;
+      gate_of<T>(rg[i], a[i], keep);
+      x[i] = (BWD ? 1.f : keep) * value_of(rv[i]);
+      if (t0 + i >= te) a[i] = 1.f, x[i] = 0.f;
+    }
     if (k + 1 < m) load(k + 1);
 #pragma unroll
-    for (int e = 0; e < VB; ++e)
-#pragma unroll
-      for (int j = 0; j < L; ++j) {
-        const int i = BWD ? L - 1 - j : j;
-        H[e] = BWD ? a[i][e] * (x[i][e] + H[e]) : fmaf(a[i][e], H[e], x[i][e]);
-        A[e] *= a[i][e];
-      }
+    for (int j = 0; j < L; ++j) {
+      const int i = BWD ? L - 1 - j : j;
+      H = BWD ? a[i] * (x[i] + H) : fmaf(a[i], H, x[i]);
+      A *= a[i];
+    }
   }
-#pragma unroll
-  for (int e = 0; e < VB; ++e) {
-    sm[((t.w * VB + e) * 2 + 0) * 64 + lane] = A[e];
-    sm[((t.w * VB + e) * 2 + 1) * 64 + lane] = H[e];
-  }
+  float2* maps = (float2*)sm;
+  maps[t.w * 64 + lane] = float2{A, H};
   __syncthreads();
   if (t.w == 0 && t.on) {
-    float* agg = p.agg + ((int64_t)s * p.B * p.d + t.bc) * 2;
-    if (s == 0 && p.start)  // for the second launch, whose last segment may write `end` over it
+    float a = 1.f, h = 0.f;
 #pragma unroll
-      for (int e = 0; e < VB; ++e) p.agg[(int64_t)p.nseg * p.B * p.d * 2 + t.bc + e] = p.start[t.bc + e];
-#pragma unroll
-    for (int e = 0; e < VB; ++e) {
-      float a = 1.f, h = 0.f;
-#pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const int w = BWD ? W - 1 - j : j;
-        const float wa = sm[((w * VB + e) * 2) * 64 + lane], wh = sm[((w * VB + e) * 2 + 1) * 64 + lane];
-        h = fmaf(wa, h, wh);
-        a *= wa;
-      }
-      agg[2 * e] = a;
-      agg[2 * e + 1] = h;
+    for (int j = 0; j < W; ++j) {
+      const float2 g = maps[(BWD ? W - 1 - j : j) * 64 + lane];
+      h = fmaf(g.x, h, g.y);
+      a *= g.x;
     }
+    ((float2*)p.agg)[(int64_t)s * p.B * p.d + t.bc] = float2{a, h};
+    if (s == (BWD ? 1 : 0) && p.start)  // for the second launch, whose last segment may write `end` over it
+      p.agg[(int64_t)p.nseg * p.B * p.d * 2 + t.bc] = p.start[t.bc];
   }
 }
 
-template <typename T, int VB, int W, int L, bool BWD>
+template <int W, bool BWD> constexpr int scan_sm() { return W > 1 ? 2 * W * (BWD ? 4 : 2) * 64 : 1; }
+template <typename T, int W, int L, bool PIPE, bool BWD>
 __global__ __launch_bounds__(64 * W) void scan_kernel(ScanProb p) {
-  __shared__ float sm[W > 1 ? 2 * W * VB * (BWD ? 3 : 2) * 64 : 1];
+  __shared__ __attribute__((aligned(16))) float sm[scan_sm<W, BWD>()];
   int i = blockIdx.x;
   const int tile = i % p.tiles;
   i /= p.tiles;
   const int b = i % p.B, s = i / p.B;
-  if constexpr (BWD) scan_bwd<T, VB, W, L>(p, tile, b, s, sm);
-  else scan_fwd<T, VB, W, L>(p, tile, b, s, sm);
+  if constexpr (BWD) scan_bwd<T, W, L, PIPE>(p, tile, b, s, sm);
+  else scan_fwd<T, W, L, PIPE>(p, tile, b, s, sm);
 }
-template <typename T, int VB, int W, int L, bool BWD>
+// Every segment but the one that no other needs (forward the last, backward the first).
+template <typename T, int W, int L, bool BWD>
 __global__ __launch_bounds__(64 * W) void scan_agg_kernel(ScanProb p) {
-  __shared__ float sm[W * VB * 2 * 64];
+  __shared__ __attribute__((aligned(16))) float sm[W * 2 * 64];
   int i = blockIdx.x;
   const int tile = i % p.tiles;
   i /= p.tiles;
-  scan_agg<T, VB, W, L, BWD>(p, tile, i % p.B, i / p.B, sm);
+  scan_agg<T, W, L, BWD>(p, tile, i % p.B, i / p.B + (BWD ? 1 : 0), sm);
 }
-template <typename T, int VB, int W, int L, bool BWD>
+template <typename T, int W, int L, bool BWD>
 __global__ __launch_bounds__(64 * W) void scan_table_kernel(const ScanProb* __restrict__ probs, const int32_t* __restrict__ map) {
-  __shared__ float sm[W > 1 ? 2 * W * VB * (BWD ? 3 : 2) * 64 : 1];
+  __shared__ __attribute__((aligned(16))) float sm[scan_sm<W, BWD>()];
   const ScanProb p = probs[map[2 * blockIdx.x]];
   const int i = map[2 * blockIdx.x + 1], tile = i % p.tiles, b = i / p.tiles;
-  if constexpr (BWD) scan_bwd<T, VB, W, L>(p, tile, b, 0, sm);
-  else scan_fwd<T, VB, W, L>(p, tile, b, 0, sm);
+  if constexpr (BWD) scan_bwd<T, W, L, false>(p, tile, b, 0, sm);
+  else scan_fwd<T, W, L, true>(p, tile, b, 0, sm);
 }
 
 // ---------------------------------------------------------------------------
@@ -1163,37 +1122,53 @@ hipError_t launch_norm_dw(const float* part, int nparts, int d, float* dw, hipSt
   return hipGetLastError();
 }
 
-ScanPlan scan_plan(int64_t B, int T, int d, bool pairs) {
+// Sequences and channel tiles of fewer than 256 workgroups leave CUs without
+// work: the time axis is split, into as many segments as give two workgroups per
+// CU. A first launch composes the segments' maps (it reads two of the operands once
+// more), the second folds those before its own segment. Forward and backward of one
+// 65536 x 512 sequence, bf16, with 512 / 768 / 1024 / 2048 workgroups: 156 / 161 /
+// 160 / 168 us; 4 x 4096 x 1024 73 / 83 / 77 / 81.
+// Between 256 and 512 workgroups a CU has one: chunks of 8 x 16 steps, one prepared
+// while another is finished, take the place of the second (16 x 2048 x 1024 with
+// chunks of 8 x 8 / 8 x 16: forward 42 / 38 us, backward 83 / 76). Above, and in
+// segments, two or more workgroups per CU fill one another's stalls, and chunks of
+// 8 x 8 leave room for them (64 x 1024 x 1024: forward 90 / 89, backward 146 / 148;
+// 4 x 4096 x 1024 32 / 38 and 43 / 49); the backward's are not prepared ahead
+// (163 us with, 146 without).
+constexpr int SCAN_GROUPS = 512;
+ScanPlan scan_plan(int64_t B, int T, int d) {
   ScanPlan p{};
-  p.kind = T <= 1 ? 0 : T <= SCAN_L ? 1 : 2;
-  const int64_t wide = B * ((d + 127) / 128);
-  p.vb = pairs && wide >= 512 ? 2 : 1;
-  p.tiles = (d + 64 * p.vb - 1) / (64 * p.vb);
-  const int chunks = scan_chunks(T);
-  p.seg = std::max(1, chunks);
+  p.kind = T <= 1 ? SCAN_ONE : T <= SCAN_SHORT ? SCAN_WAVE : SCAN_CHUNKS;
+  p.tiles = (d + 63) / 64;
+  const int states = scan_chunks(T);
+  p.seg = std::max(1, states);
   p.nseg = 1;
   const int64_t groups = B * p.tiles;
-  if (p.kind == 2 && groups < 256 && chunks > 2) {
-    const int want = (int)std::min<int64_t>(chunks, (512 + groups - 1) / groups);
-    p.seg = (chunks + want - 1) / want;
-    p.nseg = (chunks + p.seg - 1) / p.seg;
+  if (p.kind == SCAN_CHUNKS && groups < 256 && states > 4) {
+    const int want = (int)std::min<int64_t>(states, (SCAN_GROUPS + groups - 1) / groups);
+    p.seg = (states + want - 1) / want;
+    p.nseg = (states + p.seg - 1) / p.seg;
   }
+  if (p.kind == SCAN_CHUNKS && p.nseg == 1 && groups < SCAN_GROUPS) p.kind = SCAN_LONG_CHUNKS;
   return p;
 }
 
 namespace {
-template <typename T, int VB, bool BWD> void scan_go(const ScanPlan& plan, const ScanProb& p, unsigned grid, hipStream_t s) {
-  if (plan.kind == 0) {
-    hipLaunchKernelGGL((scan_kernel<T, VB, 1, 1, BWD>), dim3(grid), dim3(64), 0, s, p);
-  } else if (plan.kind == 1) {
-    hipLaunchKernelGGL((scan_kernel<T, VB, 1, SCAN_L, BWD>), dim3(grid), dim3(64), 0, s, p);
+template <typename T, bool BWD> void scan_go(const ScanPlan& plan, const ScanProb& p, unsigned grid, hipStream_t s) {
+  constexpr int W = SCAN_W;
+  if (plan.kind == SCAN_ONE) {
+    hipLaunchKernelGGL((scan_kernel<T, 1, 1, false, BWD>), dim3(grid), dim3(64), 0, s, p);
+  } else if (plan.kind == SCAN_WAVE) {
+    hipLaunchKernelGGL((scan_kernel<T, 1, SCAN_SHORT, false, BWD>), dim3(grid), dim3(64), 0, s, p);
+  } else if (plan.kind == SCAN_LONG_CHUNKS) {
+    hipLaunchKernelGGL((scan_kernel<T, W, 16, true, BWD>), dim3(grid), dim3(64 * W), 0, s, p);
   } else {
     ScanProb q = p;
     if (plan.nseg > 1) {
-      hipLaunchKernelGGL((scan_agg_kernel<T, VB, SCAN_W, SCAN_L, BWD>), dim3(grid), dim3(64 * SCAN_W), 0, s, p);
+      hipLaunchKernelGGL((scan_agg_kernel<T, W, 8, BWD>), dim3(grid - grid / plan.nseg), dim3(64 * W), 0, s, p);
       if (p.start) q.start = p.agg + (int64_t)p.nseg * p.B * p.d * 2;
     }
-    hipLaunchKernelGGL((scan_kernel<T, VB, SCAN_W, SCAN_L, BWD>), dim3(grid), dim3(64 * SCAN_W), 0, s, q);
+    hipLaunchKernelGGL((scan_kernel<T, W, 8, !BWD, BWD>), dim3(grid), dim3(64 * W), 0, s, q);
   }
 }
 }  // namespace
@@ -1205,31 +1180,25 @@ hipError_t launch_scan(bool bf16, bool bwd, const ScanPlan& plan, const ScanProb
   p.nseg = plan.nseg;
   const unsigned grid = (unsigned)((int64_t)p.tiles * p.B * p.nseg);
   if (grid == 0) return hipSuccess;
-  auto go = [&](auto type, auto vb) {
-    using T = decltype(type);
-    if (bwd) scan_go<T, vb(), true>(plan, p, grid, s);
-    else scan_go<T, vb(), false>(plan, p, grid, s);
-  };
-  if (bf16 && plan.vb == 2) go(bf16_t{}, Int<2>{});
-  else if (bf16) go(bf16_t{}, Int<1>{});
-  else if (plan.vb == 2) go(float{}, Int<2>{});
-  else go(float{}, Int<1>{});
+  if (bf16 && bwd) scan_go<bf16_t, true>(plan, p, grid, s);
+  else if (bf16) scan_go<bf16_t, false>(plan, p, grid, s);
+  else if (bwd) scan_go<float, true>(plan, p, grid, s);
+  else scan_go<float, false>(plan, p, grid, s);
   return hipGetLastError();
 }
 
-hipError_t launch_scan_table(bool bf16, bool bwd, int kind, int vb, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s) {
+hipError_t launch_scan_table(bool bf16, bool bwd, bool shorts, const ScanProb* probs, const int32_t* map, int nblocks, hipStream_t s) {
   if (nblocks <= 0) return hipSuccess;
-  auto waves = [&](auto type, auto v, auto w) {
+  auto go = [&](auto type, auto w, auto l) {
     using T = decltype(type);
     const dim3 blk(64 * w());
-    if (bwd) hipLaunchKernelGGL((scan_table_kernel<T, v(), w(), SCAN_L, true>), dim3(nblocks), blk, 0, s, probs, map);
-    else hipLaunchKernelGGL((scan_table_kernel<T, v(), w(), SCAN_L, false>), dim3(nblocks), blk, 0, s, probs, map);
+    if (bwd) hipLaunchKernelGGL((scan_table_kernel<T, w(), l(), true>), dim3(nblocks), blk, 0, s, probs, map);
+    else hipLaunchKernelGGL((scan_table_kernel<T, w(), l(), false>), dim3(nblocks), blk, 0, s, probs, map);
   };
-  auto go = [&](auto type, auto v) { kind == 1 ? waves(type, v, Int<1>{}) : waves(type, v, Int<SCAN_W>{}); };
-  if (bf16 && vb == 2) go(bf16_t{}, Int<2>{});
-  else if (bf16) go(bf16_t{}, Int<1>{});
-  else if (vb == 2) go(float{}, Int<2>{});
-  else go(float{}, Int<1>{});
+  if (bf16 && shorts) go(bf16_t{}, Int<1>{}, Int<SCAN_SHORT>{});
+  else if (bf16) go(bf16_t{}, Int<SCAN_W>{}, Int<8>{});
+  else if (shorts) go(float{}, Int<1>{}, Int<SCAN_SHORT>{});
+  else go(float{}, Int<SCAN_W>{}, Int<8>{});
   return hipGetLastError();
 }
 

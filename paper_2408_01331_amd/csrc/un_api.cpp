@@ -183,7 +183,7 @@ struct Launch {
   int count;
   int mode = 0;       // GEMM: tile variant; conv weight gradient: code variant (launch_conv_wgrad); CE: problems needing the row pass
   size_t lds = 0;     // halo conv: dynamic LDS bytes
-  int bm = 0;         // conv weight gradient: output channels per tile; recurrence: channels per lane
+  int bm = 0;         // conv weight gradient: output channels per tile
   NormPlan norm{};    // norm launches
 };
 
@@ -1237,21 +1237,16 @@ static void build_tables(un_ctx* c, Tables& T) {
     out.push_back(Launch{kind, UN_K_ATTN, po, mo, (int)(map.size() / 2)});
     out.back().lds = lds;
   };
-  // recurrence core: one workgroup per (problem, channel tile, sequence). Pairs
-  // of channels per lane where that still leaves two workgroups per CU
+  // recurrence core: one workgroup per (problem, channel tile, sequence), of one
+  // wave where every sequence is short (which gives the same bits)
   auto emit_scan = [&](std::vector<ScanProb>& ps, std::vector<Launch>& out, int kind) {
     if (ps.empty()) return;
-    int64_t wide = 0;
     int longest = 0;
-    for (auto& p : ps) {
-      wide += (int64_t)p.B * cdiv(p.d, 128);
-      longest = std::max(longest, p.T);
-    }
-    const int vb = wide >= 512 ? 2 : 1;
+    for (auto& p : ps) longest = std::max(longest, p.T);
     std::vector<int32_t> map;
     for (size_t k = 0; k < ps.size(); ++k) {
       ScanProb& p = ps[k];
-      p.tiles = cdiv(p.d, 64 * vb);
+      p.tiles = cdiv(p.d, 64);
       p.seg = scan_chunks(p.T);
       p.nseg = 1;
       for (int t = 0; t < p.tiles * p.B; ++t) {
@@ -1267,8 +1262,7 @@ static void build_tables(un_ctx* c, Tables& T) {
         fix.push_back(b0 + f);
     }
     size_t mo = put(map.data(), map.size() * 4);
-    out.push_back(Launch{kind, UN_K_RECURRENCE, po, mo, (int)(map.size() / 2), longest <= SCAN_L ? 1 : 2});
-    out.back().bm = vb;
+    out.push_back(Launch{kind, UN_K_RECURRENCE, po, mo, (int)(map.size() / 2), longest <= SCAN_SHORT});
   };
   // norm: one workgroup per (problem, group of rows), backward per (problem,
   // block). Problems of one launch have the same plan, which decides the order
@@ -2435,7 +2429,7 @@ static hipError_t run_launch(un_ctx* c, const Launch& l, float lr) {
       break;
     case 11:
     case 12:
-      e = launch_scan_table(c->bf16, l.kind == 12, l.mode, l.bm, c->at<ScanProb>(l.probs), c->at<int32_t>(l.map), l.count,
+      e = launch_scan_table(c->bf16, l.kind == 12, l.mode != 0, c->at<ScanProb>(l.probs), c->at<int32_t>(l.map), l.count,
                             c->stream);
       break;
     case 13:
