@@ -3,6 +3,7 @@
 // before every check has passed.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -244,6 +245,7 @@ struct un_adamw {
   char* table = nullptr;   // the tensors, then the workgroups' (tensor, chunk)
   size_t map_at = 0;
   int nblocks = 0;
+  int64_t bytes = 0;       // of the tensors, gradients and states
 };
 
 un_status un_adamw_create(const un_adamw_tensor* t, int32_t n, int32_t grad_type, int32_t bits, un_adamw** out) {
@@ -283,6 +285,7 @@ un_status un_adamw_create(const un_adamw_tensor* t, int32_t n, int32_t grad_type
         map.push_back((int32_t)b);
       }
       base += (uint32_t)((q.elements + AW_BLOCK - 1) / AW_BLOCK * AW_BLOCK);
+      a->bytes += q.elements * (4 + (a->g16 ? 2 : 4) + (q.copy ? 2 : 0) + (a->eight ? 2 : 8));
     }
     a->map_at = (ts.size() * sizeof(AdamwTensor) + 255) / 256 * 256;
     std::vector<char> host(a->map_at + map.size() * 4);
@@ -340,7 +343,8 @@ un_status un_adamw_step(un_adamw* a, const un_adamw_hyper* h, void* stream) {
   hp.c2 = (float)(1.0 - h->beta2);
   hp.isb2 = (float)(1.0 / std::sqrt(1.0 - std::pow(h->beta2, t)));
   hp.eps = (float)h->eps;
-  e = launch_adamw(a->g16, a->eight, (const AdamwTensor*)a->table, (const int32_t*)(a->table + a->map_at), a->nblocks, hp, nullptr,
+  if (a->eight) hp.eps = std::fmax(hp.eps, FLT_MIN);  // its reciprocal takes a subnormal one for 0
+  e = launch_adamw(a->g16, a->eight, (const AdamwTensor*)a->table, (const int32_t*)(a->table + a->map_at), a->nblocks, a->bytes, hp, nullptr,
                    (hipStream_t)stream);
   return e == hipSuccess ? UN_OK : device_error(F, e);
 }

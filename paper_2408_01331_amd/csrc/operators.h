@@ -119,9 +119,10 @@ struct AdamwHp {
   uint32_t key;                                 // of the rounding's random numbers
 };
 constexpr int AW_BLOCK = 256;                   // values per scale
-constexpr int AW_CHUNK = 16 * AW_BLOCK;         // values per workgroup
-// map: (tensor, chunk) per workgroup. hps: device array, or null: `hp` for every tensor.
-hipError_t launch_adamw(bool g16, bool eight, const AdamwTensor* ts, const int32_t* map, int nblocks, const AdamwHp& hp,
+constexpr int AW_CHUNK = 4 * AW_BLOCK;         // values per workgroup
+// map: (tensor, chunk) per workgroup. bytes: of all the tensors with their gradients and states. hps: device array, or
+// null: `hp` for every tensor.
+hipError_t launch_adamw(bool g16, bool eight, const AdamwTensor* ts, const int32_t* map, int nblocks, int64_t bytes, const AdamwHp& hp,
                         const AdamwHp* hps, hipStream_t s);
 
 // e4m3 (largest finite value 448) on the host, for reading and setting states

@@ -870,8 +870,11 @@ __global__ __launch_bounds__(64 * W) void scan_table_kernel(const ScanProb* __re
 }
 
 // ---------------------------------------------------------------------------
-// AdamW. A wave takes AW_BLOCK values at a time, four per lane, so the block of
-// an 8-bit scale is one wave's and its maximum one reduction over the lanes.
+// AdamW. A wave takes AW_BLOCK values, four per lane, so the block of an 8-bit
+// scale is one wave's and its maximum one reduction over the lanes. One block per
+// wave: with four, all loaded ahead, the registers left half of the waves' room
+// (200 M parameters, 8-bit states 589 us, so 538; 6 M 27.5, so 20.9; 32 bits 1058,
+// so 1051).
 // ---------------------------------------------------------------------------
 // 32 bits from a value's number and the step's key: multiplications by odd
 // constants (fractions of the golden ratio, sqrt 2 and sqrt 3) between shifts
@@ -907,26 +910,42 @@ __device__ __forceinline__ uint32_t round_code(float x, uint32_t r) {
   return code | (u >> 31 << 7);
 }
 
-template <bool G16, bool EIGHT>
+// Four values at an element's alignment. ONCE: past the caches (launch_adamw says
+// when); the bf16 copy is read soon after, and stays.
+#define UN_FOUR(NAME, V, A)                                                        \
+  template <bool ONCE> __device__ __forceinline__ V load_##NAME(const void* p) {   \
+    if constexpr (ONCE) return __builtin_nontemporal_load((const A*)p);            \
+    else return *(const A*)p;                                                      \
+  }                                                                                \
+  template <bool ONCE> __device__ __forceinline__ void store_##NAME(void* p, V v) { \
+    if constexpr (ONCE) __builtin_nontemporal_store(v, (A*)p);                     \
+    else *(A*)p = v;                                                               \
+  }
+UN_FOUR(floats, f32x4, f32x4_a4)
+UN_FOUR(halves, u32x2, u32x2_a2)
+UN_FOUR(bytes, uint32_t, u32_a1)
+#undef UN_FOUR
+
+template <bool G16, bool EIGHT, bool ONCE>
 __device__ __forceinline__ void adamw_load(const AdamwTensor& t, int64_t i, int n, f32x4& p, float* g, f32x4& m, f32x4& v,
                                            uint32_t& mc, uint32_t& vc) {
   if (n == 4) {
-    p = *(const f32x4_a4*)(t.p + i);
+    p = load_floats<ONCE>(t.p + i);
     if constexpr (G16) {
-      const u32x2 q = *(const u32x2_a2*)((const bf16_t*)t.g + i);
+      const u32x2 q = load_halves<ONCE>((const bf16_t*)t.g + i);
 #pragma unroll
       for (int e = 0; e < 4; ++e) g[e] = __uint_as_float(e & 1 ? q[e >> 1] & 0xffff0000u : q[e >> 1] << 16);
     } else {
-      const f32x4 q = *(const f32x4_a4*)((const float*)t.g + i);
+      const f32x4 q = load_floats<ONCE>((const float*)t.g + i);
 #pragma unroll
       for (int e = 0; e < 4; ++e) g[e] = q[e];
     }
     if constexpr (EIGHT) {
-      mc = *(const u32_a1*)((const uint8_t*)t.m + i);
-      vc = *(const u32_a1*)((const uint8_t*)t.v + i);
+      mc = load_bytes<ONCE>((const uint8_t*)t.m + i);
+      vc = load_bytes<ONCE>((const uint8_t*)t.v + i);
     } else {
-      m = *(const f32x4_a4*)((const float*)t.m + i);
-      v = *(const f32x4_a4*)((const float*)t.v + i);
+      m = load_floats<ONCE>((const float*)t.m + i);
+      v = load_floats<ONCE>((const float*)t.v + i);
     }
   } else {
     mc = vc = 0;
@@ -946,105 +965,101 @@ __device__ __forceinline__ void adamw_load(const AdamwTensor& t, int64_t i, int 
   }
 }
 
-template <bool G16, bool EIGHT>
+template <bool G16, bool EIGHT, bool ONCE>
 __global__ __launch_bounds__(256) void adamw_kernel(const AdamwTensor* __restrict__ ts, const int32_t* __restrict__ map,
                                                     AdamwHp hp, const AdamwHp* __restrict__ hps) {
   const AdamwTensor t = ts[map[2 * blockIdx.x]];
   if (hps) hp = hps[t.hp];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t base = (int64_t)map[2 * blockIdx.x + 1] * AW_CHUNK;
-  constexpr int U = AW_CHUNK / AW_BLOCK / 4;  // blocks per wave, all loaded ahead
-  f32x4 p[U], m[U], v[U];
-  float g[U][4];
-  uint32_t mc[U], vc[U], ms[U], vs[U];
-  int cnt[U];
+  const int64_t b0 = (int64_t)map[2 * blockIdx.x + 1] * AW_CHUNK + wave * AW_BLOCK, i = b0 + lane * 4;
+  if (b0 >= t.n) return;  // a wave as a whole
+  const int cnt = (int)min((int64_t)4, max((int64_t)0, t.n - i));
+  f32x4 p, m, v;
+  float g[4];
+  uint32_t mc, vc, ms = 0, vs = 0;
+  adamw_load<G16, EIGHT, ONCE>(t, i, cnt, p, g, m, v, mc, vc);
+  if constexpr (EIGHT) {
+    ms = t.ms[b0 / AW_BLOCK];
+    vs = t.vs[b0 / AW_BLOCK];
+  }
+  float nm[4], nv[4], rt[4], w[4];
+  if constexpr (EIGHT) {
+    const float sm = scale_value(ms), sv = scale_value(vs);
+    nm[0] = __builtin_amdgcn_cvt_f32_fp8(mc, 0) * sm, nm[1] = __builtin_amdgcn_cvt_f32_fp8(mc, 1) * sm;
+    nm[2] = __builtin_amdgcn_cvt_f32_fp8(mc, 2) * sm, nm[3] = __builtin_amdgcn_cvt_f32_fp8(mc, 3) * sm;
+    nv[0] = __builtin_amdgcn_cvt_f32_fp8(vc, 0) * sv, nv[1] = __builtin_amdgcn_cvt_f32_fp8(vc, 1) * sv;
+    nv[2] = __builtin_amdgcn_cvt_f32_fp8(vc, 2) * sv, nv[3] = __builtin_amdgcn_cvt_f32_fp8(vc, 3) * sv;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t b0 = base + (u * 4 + wave) * AW_BLOCK, i = b0 + lane * 4;
-    cnt[u] = (int)min((int64_t)4, max((int64_t)0, t.n - i));
-    adamw_load<G16, EIGHT>(t, i, cnt[u], p[u], g[u], m[u], v[u], mc[u], vc[u]);
-    if constexpr (EIGHT) {
-      ms[u] = b0 < t.n ? t.ms[b0 / AW_BLOCK] : 0;
-      vs[u] = b0 < t.n ? t.vs[b0 / AW_BLOCK] : 0;
-    }
+    for (int e = 0; e < 4; ++e) nv[e] *= nv[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) nm[e] = m[e], nv[e] = v[e];
   }
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t b0 = base + (u * 4 + wave) * AW_BLOCK, i = b0 + lane * 4;
-    if (b0 >= t.n) break;  // a wave as a whole
-    float nm[4], nv[4], rt[4], w[4];
+  for (int e = 0; e < 4; ++e) {
+    const float x = g[e];
+    nm[e] = fmaf(hp.b1, nm[e], hp.c1 * x);
+    nv[e] = fmaf(hp.b2, nv[e], hp.c2 * x * x);
+    const float kept = fmaf(-hp.decay, p[e], p[e]);
     if constexpr (EIGHT) {
-      const float sm = scale_value(ms[u]), sv = scale_value(vs[u]);
-      nm[0] = __builtin_amdgcn_cvt_f32_fp8(mc[u], 0) * sm, nm[1] = __builtin_amdgcn_cvt_f32_fp8(mc[u], 1) * sm;
-      nm[2] = __builtin_amdgcn_cvt_f32_fp8(mc[u], 2) * sm, nm[3] = __builtin_amdgcn_cvt_f32_fp8(mc[u], 3) * sm;
-      nv[0] = __builtin_amdgcn_cvt_f32_fp8(vc[u], 0) * sv, nv[1] = __builtin_amdgcn_cvt_f32_fp8(vc[u], 1) * sv;
-      nv[2] = __builtin_amdgcn_cvt_f32_fp8(vc[u], 2) * sv, nv[3] = __builtin_amdgcn_cvt_f32_fp8(vc[u], 3) * sv;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) nv[e] *= nv[e];
+      // to 1 ulp: the step is bound by its arithmetic, and neither the update nor a code shows the difference
+      rt[e] = __builtin_amdgcn_sqrtf(nv[e]);
+      w[e] = fmaf(-hp.lr * nm[e], __builtin_amdgcn_rcpf(fmaf(rt[e], hp.isb2, hp.eps)), kept);
     } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) nm[e] = m[u][e], nv[e] = v[u][e];
+      w[e] = kept - hp.lr * (nm[e] / (sqrtf(nv[e]) * hp.isb2 + hp.eps));
     }
+  }
+  uint32_t cm = 0, cv = 0;
+  if constexpr (EIGHT) {
+    float am = 0.f, av = 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float x = g[u][e];
-      nm[e] = fmaf(hp.b1, nm[e], hp.c1 * x);
-      nv[e] = fmaf(hp.b2, nv[e], hp.c2 * x * x);
-      rt[e] = sqrtf(nv[e]);
-      w[e] = fmaf(-hp.decay, p[u][e], p[u][e]) - hp.lr * (nm[e] / (rt[e] * hp.isb2 + hp.eps));
+      const float x = fabsf(nm[e]), y = rt[e];
+      am = fmaxf(am, x < __builtin_inff() ? x : 0.f);
+      av = fmaxf(av, y < __builtin_inff() ? y : 0.f);
     }
-    uint32_t cm = 0, cv = 0;
+    am = wave_max(am);
+    av = wave_max(av);
+    const uint32_t sm = scale_of(am), sv = scale_of(av);
+    const float im = scale_inverse(sm), iv = scale_inverse(sv);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t r = random_bits(t.base + (uint32_t)(i + e), hp.key);
+      cm |= round_code(nm[e] * im, r & 0xffff) << (8 * e);
+      // a second moment that is not zero never becomes zero: the next step divides by its root
+      uint32_t c = round_code(rt[e] * iv, r >> 16);
+      if (c == 0 && rt[e] > 0.f) c = 1;
+      cv |= c << (8 * e);
+    }
+    if (lane == 0) {
+      t.ms[b0 / AW_BLOCK] = (uint8_t)sm;
+      t.vs[b0 / AW_BLOCK] = (uint8_t)sv;
+    }
+  }
+  if (cnt == 4) {
+    store_floats<ONCE>(t.p + i, f32x4{w[0], w[1], w[2], w[3]});
+    if (t.copy) store_halves<false>(t.copy + i, u32x2{f2bf2(w[0], w[1]), f2bf2(w[2], w[3])});
     if constexpr (EIGHT) {
-      float am = 0.f, av = 0.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = fabsf(nm[e]), y = rt[e];
-        am = fmaxf(am, x < __builtin_inff() ? x : 0.f);
-        av = fmaxf(av, y < __builtin_inff() ? y : 0.f);
-      }
-      am = wave_max(am);
-      av = wave_max(av);
-      const uint32_t sm = scale_of(am), sv = scale_of(av);
-      const float im = scale_inverse(sm), iv = scale_inverse(sv);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t r = random_bits(t.base + (uint32_t)(i + e), hp.key);
-        cm |= round_code(nm[e] * im, r & 0xffff) << (8 * e);
-        // a second moment that is not zero never becomes zero: the next step divides by its root
-        uint32_t c = round_code(rt[e] * iv, r >> 16);
-        if (c == 0 && rt[e] > 0.f) c = 1;
-        cv |= c << (8 * e);
-      }
-      if (lane == 0) {
-        t.ms[b0 / AW_BLOCK] = (uint8_t)sm;
-        t.vs[b0 / AW_BLOCK] = (uint8_t)sv;
-      }
-    }
-    if (cnt[u] == 4) {
-      *(f32x4_a4*)(t.p + i) = f32x4{w[0], w[1], w[2], w[3]};
-      if (t.copy) *(u32x2_a2*)(t.copy + i) = u32x2{f2bf2(w[0], w[1]), f2bf2(w[2], w[3])};
-      if constexpr (EIGHT) {
-        *(u32_a1*)((uint8_t*)t.m + i) = cm;
-        *(u32_a1*)((uint8_t*)t.v + i) = cv;
-      } else {
-        *(f32x4_a4*)((float*)t.m + i) = f32x4{nm[0], nm[1], nm[2], nm[3]};
-        *(f32x4_a4*)((float*)t.v + i) = f32x4{nv[0], nv[1], nv[2], nv[3]};
-      }
+      store_bytes<ONCE>((uint8_t*)t.m + i, cm);
+      store_bytes<ONCE>((uint8_t*)t.v + i, cv);
     } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < cnt[u]) {
-          t.p[i + e] = w[e];
-          if (t.copy) t.copy[i + e] = (bf16_t)f2bf(w[e]);
-          if constexpr (EIGHT) {
-            ((uint8_t*)t.m)[i + e] = (uint8_t)(cm >> (8 * e));
-            ((uint8_t*)t.v)[i + e] = (uint8_t)(cv >> (8 * e));
-          } else {
-            ((float*)t.m)[i + e] = nm[e];
-            ((float*)t.v)[i + e] = nv[e];
-          }
-        }
+      store_floats<ONCE>((float*)t.m + i, f32x4{nm[0], nm[1], nm[2], nm[3]});
+      store_floats<ONCE>((float*)t.v + i, f32x4{nv[0], nv[1], nv[2], nv[3]});
     }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < cnt) {
+        t.p[i + e] = w[e];
+        if (t.copy) t.copy[i + e] = (bf16_t)f2bf(w[e]);
+        if constexpr (EIGHT) {
+          ((uint8_t*)t.m)[i + e] = (uint8_t)(cm >> (8 * e));
+          ((uint8_t*)t.v)[i + e] = (uint8_t)(cv >> (8 * e));
+        } else {
+          ((float*)t.m)[i + e] = nm[e];
+          ((float*)t.v)[i + e] = nv[e];
+        }
+      }
   }
 }
 
@@ -1202,14 +1217,23 @@ hipError_t launch_scan_table(bool bf16, bool bwd, bool shorts, const ScanProb* p
   return hipGetLastError();
 }
 
-hipError_t launch_adamw(bool g16, bool eight, const AdamwTensor* ts, const int32_t* map, int nblocks, const AdamwHp& hp,
+// Above half of the last-level cache (256 MiB) a step's tensors would only push
+// one another and the rest of the program out of it. Steps with ordinary accesses /
+// past the caches, three sets of tensors in turn, us: states in 32 bits, 4 M
+// parameters (72 MB) 18.9 / 21.8, 8 M (144 MB) 44.7 / 39.5, 200 M 1039 / 992; in 8
+// bits, 8 M (80 MB) 24.3 / 26.4, 16 M (160 MB) 50.7 / 46.5, 200 M 537 / 514.
+hipError_t launch_adamw(bool g16, bool eight, const AdamwTensor* ts, const int32_t* map, int nblocks, int64_t bytes, const AdamwHp& hp,
                         const AdamwHp* hps, hipStream_t s) {
   if (nblocks <= 0) return hipSuccess;
-  auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(nblocks), dim3(256), 0, s, ts, map, hp, hps); };
-  if (g16 && eight) go(adamw_kernel<true, true>);
-  else if (g16) go(adamw_kernel<true, false>);
-  else if (eight) go(adamw_kernel<false, true>);
-  else go(adamw_kernel<false, false>);
+  auto go = [&](auto g, auto e) {
+    const dim3 grid(nblocks), blk(256);
+    if (bytes > (int64_t)128 << 20) hipLaunchKernelGGL((adamw_kernel<g(), e(), true>), grid, blk, 0, s, ts, map, hp, hps);
+    else hipLaunchKernelGGL((adamw_kernel<g(), e(), false>), grid, blk, 0, s, ts, map, hp, hps);
+  };
+  using F = std::false_type;
+  using T = std::true_type;
+  if (g16) eight ? go(T{}, T{}) : go(T{}, F{});
+  else eight ? go(F{}, T{}) : go(F{}, F{});
   return hipGetLastError();
 }
 

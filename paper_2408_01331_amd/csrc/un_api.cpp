@@ -19,6 +19,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -306,6 +307,7 @@ struct un_ctx {
     char* mem = nullptr;         // AdamwHp per model, the tensors, (tensor, chunk) per workgroup
     size_t tensors = 0, map = 0; // offsets in mem
     int nblocks = 0;             // of the active models
+    int64_t bytes = 0;           // their weights, gradients and states
     bool any = false;            // some model, active or not
     size_t cap = 0;              // bytes of mem
   } aw;
@@ -2439,7 +2441,7 @@ static hipError_t run_launch(un_ctx* c, const Launch& l, float lr) {
       break;
     case 15:
       e = launch_adamw(false, true, (const AdamwTensor*)(c->aw.mem + c->aw.tensors), (const int32_t*)(c->aw.mem + c->aw.map),
-                       l.count, AdamwHp{}, (const AdamwHp*)c->aw.mem, c->stream);
+                       l.count, c->aw.bytes, AdamwHp{}, (const AdamwHp*)c->aw.mem, c->stream);
       break;
   }
   if (c->profiling && a && b) {
@@ -2725,7 +2727,7 @@ static un_status step_common(un_ctx* c, float lr, const float* lrs, float* losse
         const float decay = (float)(rate * o.decay);
         h.kind = o.kind != UN_OPT_ADAM && decay > 0.f ? -decay : (float)UN_OPT_ADAM;
         if (o.kind == UN_OPT_ADAMW8) {
-          hp8[i] = AdamwHp{decay, h.lr, h.b1, h.b2, h.c1, h.c2, h.isb2, h.eps, (uint32_t)(o.t + 1) * 0x01000193u + 0x5EEDu};
+          hp8[i] = AdamwHp{decay, h.lr, h.b1, h.b2, h.c1, h.c2, h.isb2, std::fmax(h.eps, FLT_MIN), (uint32_t)(o.t + 1) * 0x01000193u + 0x5EEDu};
           h = OptHp{};  // the backward pass leaves its weights (SGD at rate 0)
         }
       }
@@ -2869,6 +2871,7 @@ static size_t layout8(const Model& mod, std::vector<Tensor8>& out) {
 static un_status table8(un_ctx* c, char* mem, size_t cap, size_t* need, un_ctx::Adamw8* out) {
   std::vector<AdamwTensor> ts;
   std::vector<int32_t> map;
+  int64_t bytes = 0;
   for (size_t i = 0; i < c->models.size(); ++i) {
     const char* q = c->opts[i].state8;
     if (!q || (mem && !c->active[i])) continue;
@@ -2887,6 +2890,7 @@ static un_status table8(un_ctx* c, char* mem, size_t cap, size_t* need, un_ctx::
       a.n = t.n;
       a.base = t.base;
       a.hp = (int32_t)i;
+      bytes += t.n * (a.copy ? 12 : 10);
       for (int64_t k = 0; k < (t.n + AW_CHUNK - 1) / AW_CHUNK; ++k) {
         map.push_back((int32_t)ts.size());
         map.push_back((int32_t)k);
@@ -2903,6 +2907,7 @@ static un_status table8(un_ctx* c, char* mem, size_t cap, size_t* need, un_ctx::
   if (total > cap) return fail(c, UN_ERR_UNSUPPORTED, "8-bit optimizer table exceeds its allocation");
   r.mem = mem;
   r.nblocks = (int)(map.size() / 2);
+  r.bytes = bytes;
   r.any = out->any;
   if (!ts.empty()) {
     HIPCHK(c, hipMemcpyAsync(mem + r.tensors, ts.data(), ts.size() * sizeof(AdamwTensor), hipMemcpyHostToDevice, c->stream));
