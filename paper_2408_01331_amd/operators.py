@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch._C import _cuda_getDevice as _current_device
 from torch._C import _cuda_getCurrentRawStream as _current_stream  # torch.cuda.current_stream(i).cuda_stream without its 1 us
 
 from . import unifiednn as _un
@@ -63,10 +64,19 @@ def _fresh(x, dtype):
     return _empty_like(x, dtype=dtype) if x.is_contiguous() else _empty(x.shape, dtype=dtype, device=x.device)
 
 
-def _call(fn, args, dev):
-    status = fn(_byref(args), _current_stream(dev))
+def _launch(fn, dev, *args):
+    """fn on torch's current stream of GPU `dev`. (The default stream has no device of its own: it is the current one's.)"""
+    if _current_device() == dev:
+        status = fn(*args, _current_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, _current_stream(dev))
     if status:
         _un._check(status)
+
+
+def _call(fn, args, dev):
+    _launch(fn, dev, _byref(args))
 
 
 _fns = None
@@ -173,7 +183,7 @@ def rms_norm_backward(dy, s, weight, rstd, ds=None):
 def _strides(x, shape):
     """(token, sequence) strides of [batch, tokens, width]."""
     st = x.stride()
-    return st[1] if shape[1] > 1 else shape[2], st[0]
+    return st[1] if shape[1] > 1 else shape[2], st[0] if shape[0] > 1 else 0
 
 
 def _scan_sizes(batch, tokens, width):
@@ -269,9 +279,10 @@ class AdamW:
     bfloat16 tensors that receive the new values. States: float32 m and v, or in
     8 bits float8_e4m3fn m and v (v holds sqrt(v)) with m_scales and v_scales,
     float8_e8m0fnu, one per QBLOCK consecutive elements of a tensor
-    (`AdamW.state8` makes fresh ones). Every tensor is contiguous; the plan holds
-    references to all of them. Gradients are read where they were when the plan
-    was made: write the next step's into the same tensors."""
+    (`AdamW.state8` makes fresh ones). Every tensor is contiguous, and none that is
+    written may overlap another; the plan holds references to all of them.
+    Gradients are read where they were when the plan was made: write the next
+    step's into the same tensors."""
 
     def __init__(self, params, grads, m, v, copies=None, m_scales=None, v_scales=None):
         self._plan = None
@@ -307,6 +318,9 @@ class AdamW:
                              f"{name}[{i}] must be a contiguous float8_e8m0fnu tensor of {-(-k // QBLOCK)} elements on {device}")
             arr[i] = _un.un_adamw_tensor(_ptr(p), _ptr(grads[i]), _ptr(copies[i]) if copies is not None else None, _ptr(m[i]), _ptr(v[i]),
                                          _ptr(m_scales[i]) if eight else None, _ptr(v_scales[i]) if eight else None, k)
+        written = sorted((y.data_ptr(), y.data_ptr() + y.numel() * y.element_size())
+                         for x in (params, m, v, copies, m_scales, v_scales) for y in x or () if y.numel())
+        _require(all(a[1] <= b[0] for a, b in zip(written, written[1:])), "tensors that are written overlap")
         self._held = [params, lists]
         self.device, self._index = device, dev
         plan = ctypes.c_void_p()
@@ -324,9 +338,7 @@ class AdamW:
     def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, key=0):
         """Step number `step` (from 1). key: with 8-bit states, another whole number each step."""
         h = _un.un_adamw_hyper(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step), int(key) & 0xFFFFFFFF)
-        status = _lib().un_adamw_step(self._plan, _byref(h), _current_stream(self._index))
-        if status:
-            _un._check(status)
+        _launch(_lib().un_adamw_step, self._index, self._plan, _byref(h))
 
     def close(self):
         if self._plan:
