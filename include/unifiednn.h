@@ -491,7 +491,7 @@ un_status un_rms_norm_workspace(int32_t type, int64_t rows, int32_t width, size_
 /* Gated linear recurrence, per sequence and channel:
  *   a_t = sigmoid(gate_t),  h_t = a_t h_{t-1} + (1 - a_t) value_t,  t = 1 .. tokens.
  * gate and value are [batch][tokens][width] with the same strides (the two halves
- * of one projection, say), width and token strides up to 2^24; the state is fp32.
+ * of one projection, say), width and token strides below 2^24; the state is fp32.
  * lens (device int32 [batch], NULL:
  * all of `tokens`): steps at and behind a sequence's length (clamped to [0,
  * tokens]) are skipped: their rows of gate and value are not used, their rows of
@@ -536,7 +536,8 @@ typedef struct {
   size_t workspace_bytes;
 } un_gated_scan_grad_args;
 un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream);
-/* Floats of `states`, and bytes of the workspace of either call (may be 0). */
+/* Floats of `states`, and bytes of the workspace of either call (may be 0; 8-byte
+ * aligned). */
 un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size_t* states, size_t* workspace_bytes);
 
 /* AdamW (decoupled weight decay) over many tensors in one launch. Per element,
@@ -564,7 +565,8 @@ typedef struct {
 } un_adamw_tensor;
 typedef struct un_adamw un_adamw;
 /* A plan of the step over these tensors (n >= 1; elements may be 0), on the
- * current device. It holds their addresses, not their data: they stay the caller's. */
+ * current device. It holds their addresses, not their data: they stay the caller's,
+ * and none that is written may overlap another. */
 un_status un_adamw_create(const un_adamw_tensor* tensors, int32_t n, int32_t grad_type, int32_t state_bits, un_adamw** out);
 /* One step. lr and decay are finite and >= 0, lr * decay < 1, beta1 and beta2 in
  * [0, 1), eps > 0, t >= 1. The rates and the count travel with the call, so a

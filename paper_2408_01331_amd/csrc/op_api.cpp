@@ -149,26 +149,28 @@ un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size
   const char* F = "un_gated_scan_sizes";
   if (batch < 0 || tokens < 0 || width < 0) return bad(F, "negative size");
   if (states) *states = (size_t)batch * scan_chunks(tokens) * width;
-  const ScanPlan p = scan_plan(batch, tokens, width);
-  if (workspace_bytes) *workspace_bytes = scan_ws_bytes(p, batch, width);
+  if (workspace_bytes)
+    *workspace_bytes = 8 * (size_t)std::max(scan_ws_words(scan_plan(batch, tokens, width, false), batch, width),
+                                            scan_ws_words(scan_plan(batch, tokens, width, true), batch, width));
   return UN_OK;
 }
 
 namespace {
 // what both directions check: sizes, strides and the workspace
 un_status scan_common(const char* F, int32_t type, int32_t B, int32_t T, int32_t d, int64_t ld, int64_t ld2, int64_t ld3,
-                      int64_t seq_out, const void* workspace, size_t bytes, ScanPlan* plan) {
+                      int64_t seq_out, const void* workspace, size_t bytes, bool bwd, ScanPlan* plan) {
   if (!type_ok(type)) return bad(F, "unknown type");
   if (B < 0 || T < 0 || d < 0) return bad(F, "negative size");
   if (T > (1 << 30)) return bad(F, "more than 2^30 tokens are not supported", UN_ERR_UNSUPPORTED);
   if (d > SCAN_MAX_LD || (T > 1 && (ld > SCAN_MAX_LD || ld2 > SCAN_MAX_LD || ld3 > SCAN_MAX_LD)))
-    return bad(F, "a width or token stride above 2^24 is not supported", UN_ERR_UNSUPPORTED);
+    return bad(F, "a width or token stride of 2^24 or more is not supported", UN_ERR_UNSUPPORTED);
   if (T > 1 && (ld < d || ld2 < d || ld3 < d)) return bad(F, "a token stride is smaller than the width");
-  if (B > 1 && seq_out < d) return bad(F, "the output's sequence stride is smaller than the width");
+  if (B > 1 && T > 0 && seq_out < d) return bad(F, "the output's sequence stride is smaller than the width");
   size_t need = 0;
   un_gated_scan_sizes(B, T, d, nullptr, &need);
   if (need && (!workspace || bytes < need)) return bad(F, "workspace too small (un_gated_scan_sizes)", UN_ERR_BUFSIZE);
-  *plan = scan_plan(B, T, d);
+  if (need && (uintptr_t)workspace % 8) return bad(F, "workspace is not 8-byte aligned");
+  *plan = scan_plan(B, T, d, bwd);
   if (too_many((int64_t)plan->tiles * B * plan->nseg, plan->kind >= SCAN_CHUNKS ? 64 * SCAN_W : 64))
     return bad(F, "too many sequences and channels", UN_ERR_UNSUPPORTED);
   return UN_OK;
@@ -180,7 +182,7 @@ un_status un_gated_scan(const un_gated_scan_args* a, void* stream) {
   if (!a) return bad(F, "args is NULL");
   ScanPlan plan;
   const un_status st = scan_common(F, a->type, a->batch, a->tokens, a->width, a->ld_in, a->ld_h, a->ld_h, a->seq_h,
-                                   a->workspace, a->workspace_bytes, &plan);
+                                   a->workspace, a->workspace_bytes, false, &plan);
   if (st != UN_OK) return st;
   if (a->batch == 0 || a->width == 0) return UN_OK;
   if (a->tokens > 0 && (!a->gate || !a->value || !a->h)) return bad(F, "gate, value or h is NULL");
@@ -196,7 +198,7 @@ un_status un_gated_scan(const un_gated_scan_args* a, void* stream) {
   p.start = a->start;
   p.end = a->last;
   p.states = a->states;
-  p.agg = (float*)a->workspace;
+  p.joint = (uint64_t*)a->workspace;
   p.B = a->batch;
   p.T = a->tokens;
   p.d = a->width;
@@ -208,7 +210,7 @@ un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream)
   if (!a) return bad(F, "args is NULL");
   ScanPlan plan;
   const un_status st = scan_common(F, a->type, a->batch, a->tokens, a->width, a->ld_in, a->ld_dh, a->ld_out, a->seq_out,
-                                   a->workspace, a->workspace_bytes, &plan);
+                                   a->workspace, a->workspace_bytes, true, &plan);
   if (st != UN_OK) return st;
   if (a->batch == 0 || a->width == 0) return UN_OK;
   if (a->tokens > 0 && (!a->gate || !a->value || !a->dh || !a->states || !a->dgate || !a->dvalue))
@@ -229,7 +231,7 @@ un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream)
   p.start = a->dlast;
   p.end = a->dstart;
   p.states = const_cast<float*>(a->states);
-  p.agg = (float*)a->workspace;
+  p.joint = (uint64_t*)a->workspace;
   p.B = a->batch;
   p.T = a->tokens;
   p.d = a->width;

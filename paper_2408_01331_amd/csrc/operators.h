@@ -76,25 +76,32 @@ struct ScanProb {
   const float* start;         // forward: h_0 [B][d]; backward: the gradient at the last state; null: 0
   float* end;                 // forward: last state [B][d]; backward: dh_0; null: not wanted
   float* states;              // h at the start of every SCAN_STATE steps [B][scan_chunks][d] (forward: written if not null)
-  float* agg;                 // split passes: per segment and channel (A, H), [nseg][B][d][2], then a copy of start [B][d]
+  uint64_t* joint;            // split passes: scan_ws_words, 8-byte aligned: the next place [B][tiles], the maps [nseg][B][d],
+                              // the values between runs of segments
   int32_t B, T, d;
   int32_t tiles;              // tiles of 64 channels
-  int32_t seg, nseg;          // steps per segment, in SCAN_STATE; segments
+  int32_t nseg;               // segments, a workgroup each
 };
 constexpr int SCAN_STATE = 64;                     // steps between two kept states
 constexpr int SCAN_SHORT = 16;                     // steps that one wave takes at once
 constexpr int SCAN_W = 8;                          // waves of a workgroup over longer sequences
-// 16 rows of a stride up to this and their width fit 31 bits in bytes
-constexpr int64_t SCAN_MAX_LD = 1 << 24;
+// 32 rows of a stride up to this and their width fit 31 bits in bytes
+constexpr int64_t SCAN_MAX_LD = (1 << 24) - 1;
 __host__ __device__ inline int scan_chunks(int T) { return (T + SCAN_STATE - 1) / SCAN_STATE; }
 // One step; up to SCAN_SHORT (a wave each); chunks of SCAN_W waves x 8 steps; x 16.
-enum ScanKind { SCAN_ONE, SCAN_WAVE, SCAN_CHUNKS, SCAN_LONG_CHUNKS };
+enum ScanKind { SCAN_ONE, SCAN_WAVE, SCAN_CHUNKS, SCAN_LONG_CHUNKS, SCAN_SPLIT, SCAN_LONG_SPLIT };
 struct ScanPlan {
   ScanKind kind;
-  int tiles, seg, nseg;
+  int tiles, nseg;
 };
-inline size_t scan_ws_bytes(const ScanPlan& p, int64_t B, int d) { return p.nseg > 1 ? (size_t)(2 * p.nseg + 1) * B * d * 4 : 0; }
-ScanPlan scan_plan(int64_t B, int T, int d);
+// Segments that join by their maps; many segments in longer runs, whose maps are
+// more to read, where the values between the runs would be a long chain.
+constexpr int SCAN_RUN = 32, SCAN_LONG_RUN = 128;
+__host__ __device__ inline int scan_run(int nseg) { return nseg <= 512 ? SCAN_RUN : SCAN_LONG_RUN; }
+inline int64_t scan_ws_words(const ScanPlan& p, int64_t B, int64_t d) {
+  return p.nseg > 1 ? B * p.tiles + (p.nseg + (p.nseg - 1) / scan_run(p.nseg)) * B * d : 0;
+}
+ScanPlan scan_plan(int64_t B, int T, int d, bool bwd);
 hipError_t launch_scan(bool bf16, bool bwd, const ScanPlan& plan, const ScanProb& p, hipStream_t s);
 // table: one (problem, sequence * tiles + tile) pair per workgroup; every problem has nseg == 1 and, where `shorts`, at
 // most SCAN_SHORT steps

@@ -548,38 +548,90 @@ __device__ __forceinline__ void zero_rows(void* base, int64_t ld, int64_t bs, co
   for (int i = t0; i < t1; i += step) raw_store<T>(rows_at<T>(base, ld, bs, t, i), t.at<T>(), 0, 0.f);
 }
 
-// The maps of the segments before (forward) or behind (backward) `s`, folded
-// over `h` in order: each wave folds a run of them, and every wave the runs.
-template <int W>
-__device__ __forceinline__ void fold_segments(const ScanProb& p, const Tile& t, int s, bool bwd, float& h, float* sm) {
-  const int n = bwd ? p.nseg - 1 - s : s;
-  if (n == 0) return;  // the same for the whole workgroup
-  const int per = (n + W - 1) / W, j0 = min(n, t.w * per), j1 = min(n, j0 + per);
-  const int64_t stride = (int64_t)p.B * p.d;
-  const float2* agg = (const float2*)p.agg + t.bc;
-  float A = 1.f, H = 0.f;
-  for (int j = j0; j < j1; j += 8) {
-    float2 m[8];
+// What a workgroup of a split pass hands on: a 64-bit word per channel in the
+// cleared workspace, written and read as one access of the whole card, so the word
+// that is not EMPTY any more is the whole message and nothing else has to be ordered.
+constexpr uint64_t EMPTY = ~0ull;
+__device__ __forceinline__ void hand_on(uint64_t* p, float lo, float hi) {
+  const uint32_t a = __float_as_uint(lo);
+  const uint64_t v = (uint64_t)__float_as_uint(hi) << 32 | (a == 0xffffffffu ? 0x7fc00000u : a);  // (one NaN for another)
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t look(const uint64_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 take_over(const uint64_t* p, uint64_t v) {  // v: a first look
+  while (v == EMPTY) {
+    __builtin_amdgcn_s_sleep(1);
+    v = look(p);
+  }
+  return float2{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+
+// Segment `o` in the order of the recurrence (backward: from the last): hands its
+// map on, and returns the value that arrives at it. Within a run of segments
+// (scan_run) every one takes the maps of those before it, each wave a part of them;
+// the last of a run hands on the value behind it, from which the next run starts. `maps`: those
+// of the workgroup's own waves (A and the part at SECOND of STRIDE floats per lane).
+template <int W, bool BWD, int RUN>
+__device__ __forceinline__ float join_run(const ScanProb& p, const Tile& t, int o, float h, const float* maps, float2* sm) {
+  constexpr int STRIDE = BWD ? 4 : 2, SECOND = BWD ? 2 : 1, PER = RUN / W;
+  const int lane = threadIdx.x & 63, run = o / RUN, k = o % RUN;
+  const bool last = o == p.nseg - 1, closes = k == RUN - 1;
+  const int64_t row = (int64_t)p.B * p.d;
+  uint64_t* mine = p.joint + (int64_t)p.B * p.tiles + o * row + t.bc;
+  uint64_t* ends = p.joint + (int64_t)p.B * p.tiles + p.nseg * row + t.bc;
+  auto own = [&](float& A, float& H) {  // the waves' maps over (A, H)
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int k = min(j + u, j1 - 1);
-      m[u] = agg[(bwd ? p.nseg - 1 - k : k) * stride];
+    for (int j = 0; j < W; ++j) {
+      const float* m = maps + ((BWD ? W - 1 - j : j) * 64 + lane) * STRIDE;
+      H = fmaf(m[0], H, m[SECOND]);
+      A *= m[0];
     }
+  };
+  if (t.w == W - 1 && !last && !closes && t.on) {  // (the wave with the fewest maps to take)
+    float A = 1.f, H = 0.f;
+    own(A, H);
+    hand_on(mine, A, H);
+  }
+  float A = 1.f, H = 0.f;
+  if (t.on) {
+    const uint64_t* from = mine + (t.w * PER - k) * row;
+    uint64_t v[PER];
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (j + u < j1) {
-        H = fmaf(m[u].x, H, m[u].y);
-        A *= m[u].x;
+    for (int u = 0; u < PER; ++u)
+      if (t.w * PER + u < k) v[u] = look(from + u * row);
+    if (t.w == W - 1 && run > 0) h = take_over(ends + (run - 1) * row, look(ends + (run - 1) * row)).x;
+#pragma unroll
+    for (int u = 0; u < PER; ++u)
+      if (t.w * PER + u < k) {
+        const float2 m = take_over(from + u * row, v[u]);
+        H = fmaf(m.x, H, m.y);
+        A *= m.x;
       }
   }
-  float2* maps = (float2*)sm;
-  const int lane = threadIdx.x & 63;
-  maps[t.w * 64 + lane] = float2{A, H};
-  __syncthreads();
+  sm[t.w * 64 + lane] = float2{A, H};
+  if (t.w == W - 1) sm[W * 64 + lane].x = h;
+  lds_barrier();
+  h = sm[W * 64 + lane].x;
 #pragma unroll
-  for (int w = 0; w < W; ++w) h = fmaf(maps[w * 64 + lane].x, h, maps[w * 64 + lane].y);
-  __syncthreads();
+  for (int w = 0; w < W; ++w) h = fmaf(sm[w * 64 + lane].x, h, sm[w * 64 + lane].y);
+  if (t.w == 0 && closes && !last && t.on) {
+    float e = h, one = 1.f;
+    own(one, e);
+    hand_on(ends + run * row, e, 0.f);
+  }
+  return h;
 }
+
+template <int W, bool BWD>
+__device__ __forceinline__ float join(const ScanProb& p, const Tile& t, int o, float h, const float* maps, float2* sm) {
+  return scan_run(p.nseg) == SCAN_RUN ? join_run<W, BWD, SCAN_RUN>(p, t, o, h, maps, sm)
+                                      : join_run<W, BWD, SCAN_LONG_RUN>(p, t, o, h, maps, sm);
+}
+
+template <int N> using Int = std::integral_constant<int, N>;
+enum class ScanForm { EACH, AHEAD, SPLIT };
 
 // Runs prepare(k, slot) and finish(k, slot) over nc chunks, k = first, first +
 // dir, ..., with the barrier between them. PIPE: a chunk is prepared while the one
@@ -590,51 +642,49 @@ __device__ __forceinline__ void chunks(int nc, int first, int dir, P&& prepare, 
   auto sync = [] {
     if (W > 1) lds_barrier();
   };
-  using Slot0 = std::integral_constant<int, 0>;
-  using Slot1 = std::integral_constant<int, 1>;
   if constexpr (!PIPE) {
     // LDS by the chunk's parity: one barrier a chunk
     for (int n = 0; n < nc; ++n) {
-      prepare(first + n * dir, Slot0{}, n & 1);
+      prepare(first + n * dir, Int<0>{}, n & 1);
       sync();
-      finish(first + n * dir, Slot0{}, n & 1);
+      finish(first + n * dir, Int<0>{}, n & 1);
     }
   } else {
     if (nc > 0) {
-      prepare(first, Slot0{}, 0);
+      prepare(first, Int<0>{}, 0);
       sync();
     }
     for (int n = 0; n < nc; n += 2) {
-      if (n + 1 < nc) prepare(first + (n + 1) * dir, Slot1{}, 1);
-      finish(first + n * dir, Slot0{}, 0);
+      if (n + 1 < nc) prepare(first + (n + 1) * dir, Int<1>{}, 1);
+      finish(first + n * dir, Int<0>{}, 0);
       sync();
       if (n + 1 == nc) break;
-      if (n + 2 < nc) prepare(first + (n + 2) * dir, Slot0{}, 0);
-      finish(first + (n + 1) * dir, Slot1{}, 1);
+      if (n + 2 < nc) prepare(first + (n + 2) * dir, Int<0>{}, 0);
+      finish(first + (n + 1) * dir, Int<1>{}, 1);
       sync();
     }
   }
 }
 
-template <typename T, int W, int L, bool PIPE>
-__device__ __forceinline__ void scan_fwd(const ScanProb& p, int tile, int b, int s, float* sm) {
+template <typename T, int W, int L, ScanForm FORM>
+__device__ __forceinline__ void scan_fwd(const ScanProb& p, int tile, int b, float* sm, int s = 0) {
   constexpr int C = W * L;
   const Tile t = tile_of(p, tile, b);
-  const int lane = threadIdx.x & 63, span = p.seg * SCAN_STATE;  // steps of a segment
-  const int tb = s * span, te = min(p.T, tb + span);
+  const int lane = threadIdx.x & 63;
+  constexpr bool SPLIT = FORM == ScanForm::SPLIT;
+  const int tb = SPLIT ? s * C : 0, te = SPLIT ? min(p.T, tb + C) : p.T;
   const int nc = max(0, min(t.len, te) - tb + C - 1) / C;  // chunks with a live step
   float h = p.start ? p.start[t.bc] : 0.f;
   asm volatile("" : "+v"(h));  // here before the first barrier: `end` may be the same memory
   T rg[L], rv[L];
   struct Steps {
     float a[L], x[L];
-  } steps[PIPE ? 2 : 1];
+  } steps[FORM == ScanForm::AHEAD ? 2 : 1];
   auto load = [&](int k) {
     load_rows<T, L>(p.gate, p.ldi, p.bsi, t, tb + k * C + t.w * L, rg);
     load_rows<T, L>(p.value, p.ldi, p.bsi, t, tb + k * C + t.w * L, rv);
   };
   if (nc > 0) load(0);
-  if (W > 1) fold_segments<W>(p, t, s, false, h, sm);
   auto prepare = [&](int k, auto slot, int half) {
     Steps& q = steps[slot()];
     const int t0 = tb + k * C + t.w * L;
@@ -644,7 +694,7 @@ __device__ __forceinline__ void scan_fwd(const ScanProb& p, int tile, int b, int
       gate_of<T>(rg[i], q.a[i], keep);
       q.x[i] = keep * value_of(rv[i]);
     }
-    if (k + 1 < nc) load(k + 1);
+    if (!SPLIT && k + 1 < nc) load(k + 1);
     if (t0 + L > t.len)
 #pragma unroll
       for (int i = 0; i < L; ++i)
@@ -686,35 +736,43 @@ __device__ __forceinline__ void scan_fwd(const ScanProb& p, int tile, int b, int
     t0 + L <= t.len ? walk(std::true_type{}) : walk(std::false_type{});
     if (W == 1) h = now;
   };
-  chunks<W, PIPE>(nc, 0, 1, prepare, finish);
+  if constexpr (SPLIT) {
+    if (nc > 0) prepare(0, Int<0>{}, 0);
+    else ((float2*)sm)[t.w * 64 + lane] = float2{1.f, 0.f};
+    lds_barrier();
+    h = join<W, false>(p, t, s, h, sm, (float2*)sm + W * 64);
+    if (nc > 0) finish(0, Int<0>{}, 0);
+  } else {
+    chunks<W, FORM == ScanForm::AHEAD>(nc, 0, 1, prepare, finish);
+  }
   zero_rows<T>(p.o1, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
   if (p.end && s == p.nseg - 1 && t.w == 0 && t.on) p.end[t.bc] = h;
 }
 
-template <typename T, int W, int L, bool PIPE>
-__device__ __forceinline__ void scan_bwd(const ScanProb& p, int tile, int b, int s, float* sm) {
+template <typename T, int W, int L, ScanForm FORM>
+__device__ __forceinline__ void scan_bwd(const ScanProb& p, int tile, int b, float* sm, int s = 0) {
   constexpr int C = W * L;
   const Tile t = tile_of(p, tile, b);
-  const int lane = threadIdx.x & 63, span = p.seg * SCAN_STATE;
-  const int tb = s * span, te = min(p.T, tb + span);
+  const int lane = threadIdx.x & 63;
+  constexpr bool SPLIT = FORM == ScanForm::SPLIT;
+  const int tb = SPLIT ? s * C : 0, te = SPLIT ? min(p.T, tb + C) : p.T;
   const int nc = max(0, min(t.len, te) - tb + C - 1) / C;
   float c = p.start ? p.start[t.bc] : 0.f;  // a_{t+1} e_{t+1}: the gradient that arrives from the later steps
   asm volatile("" : "+v"(c));
-  const float* states = p.states + ((int64_t)b * scan_chunks(p.T) + tb / SCAN_STATE) * p.d + t.c;
+  const float* states = p.states + (int64_t)b * scan_chunks(p.T) * p.d + t.c;
   T rg[L], rv[L], rd[L];
   float rh = 0.f;
   struct Steps {
     float a[L], kp[L], v[L], dh[L], h;
-  } steps[PIPE ? 2 : 1];
+  } steps[FORM == ScanForm::AHEAD ? 2 : 1];
   auto load = [&](int k) {
     const int t0 = tb + k * C + t.w * L;
     load_rows<T, L>(p.gate, p.ldi, p.bsi, t, t0, rg);
     load_rows<T, L>(p.value, p.ldi, p.bsi, t, t0, rv);
     load_rows<T, L>(p.dh, p.lddh, p.bsdh, t, t0, rd);
-    rh = states[(int64_t)k * (C / SCAN_STATE ? C / SCAN_STATE : 1) * p.d];
+    rh = states[(int64_t)((tb + k * C) / SCAN_STATE) * p.d];
   };
   if (nc > 0) load(nc - 1);
-  if (W > 1) fold_segments<W>(p, t, s, true, c, sm);
   auto prepare = [&](int k, auto slot, int half) {
     Steps& q = steps[slot()];
     const int t0 = tb + k * C + t.w * L;
@@ -725,7 +783,7 @@ __device__ __forceinline__ void scan_bwd(const ScanProb& p, int tile, int b, int
       q.v[i] = value_of(rv[i]);
       q.dh[i] = value_of(rd[i]);
     }
-    if (k > 0) load(k - 1);
+    if (!SPLIT && k > 0) load(k - 1);
     if (t0 + L > t.len)
 #pragma unroll
       for (int i = 0; i < L; ++i)
@@ -781,92 +839,56 @@ __device__ __forceinline__ void scan_bwd(const ScanProb& p, int tile, int b, int
     t0 + L <= t.len ? walk(std::true_type{}) : walk(std::false_type{});
     if (W == 1) c = cn;
   };
-  chunks<W, PIPE>(nc, nc - 1, -1, prepare, finish);
+  if constexpr (SPLIT) {
+    if (nc > 0) prepare(0, Int<0>{}, 0);
+    else ((f32x4*)sm)[t.w * 64 + lane] = f32x4{1.f, 0.f, 0.f, 0.f};
+    lds_barrier();
+    c = join<W, true>(p, t, p.nseg - 1 - s, c, sm, (float2*)sm + W * 128);
+    if (nc > 0) finish(0, Int<0>{}, 0);
+  } else {
+    chunks<W, FORM == ScanForm::AHEAD>(nc, nc - 1, -1, prepare, finish);
+  }
   zero_rows<T>(p.o1, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
   zero_rows<T>(p.o2, p.ldo, p.bso, t, max(tb, t.len) + t.w, te, W);
   if (p.end && s == 0 && t.w == 0 && t.on) p.end[t.bc] = c;
 }
 
-// The map of one segment: forward h -> A h + H, backward c -> A c + Q.
-// Each wave composes a run of the segment's steps of its own, L at a time.
-template <typename T, int W, int L, bool BWD>
-__device__ __forceinline__ void scan_agg(const ScanProb& p, int tile, int b, int s, float* sm) {
-  const Tile t = tile_of(p, tile, b);
-  const int lane = threadIdx.x & 63;
-  const int n = p.seg * SCAN_STATE / W;            // steps per wave
-  const int tb = s * p.seg * SCAN_STATE + t.w * n, te = min(t.len, tb + n);
-  float A = 1.f, H = 0.f;
-  const int m = max(0, te - tb + L - 1) / L;
-  T rg[L], rv[L];
-  auto load = [&](int k) {
-    const int t0 = tb + (BWD ? m - 1 - k : k) * L;
-    load_rows<T, L>(p.gate, p.ldi, p.bsi, t, t0, rg);
-    if (BWD) load_rows<T, L>(p.dh, p.lddh, p.bsdh, t, t0, rv);
-    else load_rows<T, L>(p.value, p.ldi, p.bsi, t, t0, rv);
-  };
-  if (m > 0) load(0);
-  for (int k = 0; k < m; ++k) {
-    const int t0 = tb + (BWD ? m - 1 - k : k) * L;
-    float a[L], x[L];
-#pragma unroll
-    for (int i = 0; i < L; ++i) {
-      float keep;
-      gate_of<T>(rg[i], a[i], keep);
-      x[i] = (BWD ? 1.f : keep) * value_of(rv[i]);
-      if (t0 + i >= te) a[i] = 1.f, x[i] = 0.f;
-    }
-    if (k + 1 < m) load(k + 1);
-#pragma unroll
-    for (int j = 0; j < L; ++j) {
-      const int i = BWD ? L - 1 - j : j;
-      H = BWD ? a[i] * (x[i] + H) : fmaf(a[i], H, x[i]);
-      A *= a[i];
-    }
-  }
-  float2* maps = (float2*)sm;
-  maps[t.w * 64 + lane] = float2{A, H};
-  __syncthreads();
-  if (t.w == 0 && t.on) {
-    float a = 1.f, h = 0.f;
-#pragma unroll
-    for (int j = 0; j < W; ++j) {
-      const float2 g = maps[(BWD ? W - 1 - j : j) * 64 + lane];
-      h = fmaf(g.x, h, g.y);
-      a *= g.x;
-    }
-    ((float2*)p.agg)[(int64_t)s * p.B * p.d + t.bc] = float2{a, h};
-    if (s == (BWD ? 1 : 0) && p.start)  // for the second launch, whose last segment may write `end` over it
-      p.agg[(int64_t)p.nseg * p.B * p.d * 2 + t.bc] = p.start[t.bc];
-  }
-}
-
 template <int W, bool BWD> constexpr int scan_sm() { return W > 1 ? 2 * W * (BWD ? 4 : 2) * 64 : 1; }
-template <typename T, int W, int L, bool PIPE, bool BWD>
+template <typename T, int W, int L, ScanForm FORM, bool BWD>
 __global__ __launch_bounds__(64 * W) void scan_kernel(ScanProb p) {
   __shared__ __attribute__((aligned(16))) float sm[scan_sm<W, BWD>()];
-  int i = blockIdx.x;
-  const int tile = i % p.tiles;
-  i /= p.tiles;
-  const int b = i % p.B, s = i / p.B;
-  if constexpr (BWD) scan_bwd<T, W, L, PIPE>(p, tile, b, s, sm);
-  else scan_fwd<T, W, L, PIPE>(p, tile, b, s, sm);
+  const int tile = blockIdx.x % p.tiles, b = blockIdx.x / p.tiles;
+  if constexpr (BWD) scan_bwd<T, W, L, FORM>(p, tile, b, sm);
+  else scan_fwd<T, W, L, FORM>(p, tile, b, sm);
 }
-// Every segment but the one that no other needs (forward the last, backward the first).
+// A split pass: a workgroup takes the next place of its sequence and channels when
+// it starts, so the segments that it waits for belong to workgroups that have
+// started, and the first of these waits for none: every wait ends. (Rows loaded
+// meanwhile for the place that the workgroup's number suggests were too often the
+// wrong ones: the forward pass of 2 x 16384 x 1024 in bf16 took 51 us, so 43.)
 template <typename T, int W, int L, bool BWD>
-__global__ __launch_bounds__(64 * W) void scan_agg_kernel(ScanProb p) {
-  __shared__ __attribute__((aligned(16))) float sm[W * 2 * 64];
-  int i = blockIdx.x;
-  const int tile = i % p.tiles;
-  i /= p.tiles;
-  scan_agg<T, W, L, BWD>(p, tile, i % p.B, i / p.B + (BWD ? 1 : 0), sm);
+__global__ __launch_bounds__(64 * W) void scan_split_kernel(ScanProb p) {
+  __shared__ __attribute__((aligned(16))) float sm[W * (BWD ? 4 : 2) * 64 + (W + 1) * 2 * 64];
+  __shared__ int place;
+  const int groups = p.tiles * p.B, g = blockIdx.x % groups, tile = g % p.tiles, b = g / p.tiles;
+  if (threadIdx.x == 0)  // (the cleared word is -1)
+    place = (int)__hip_atomic_fetch_add((uint32_t*)(p.joint + g), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+  __syncthreads();
+  const int o = __builtin_amdgcn_readfirstlane(place);
+  if constexpr (BWD) scan_bwd<T, W, L, ScanForm::SPLIT>(p, tile, b, sm, p.nseg - 1 - o);
+  else scan_fwd<T, W, L, ScanForm::SPLIT>(p, tile, b, sm, o);
+}
+__global__ __launch_bounds__(256) void scan_clear_kernel(uint64_t* p, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) p[i] = EMPTY;
 }
 template <typename T, int W, int L, bool BWD>
 __global__ __launch_bounds__(64 * W) void scan_table_kernel(const ScanProb* __restrict__ probs, const int32_t* __restrict__ map) {
   __shared__ __attribute__((aligned(16))) float sm[scan_sm<W, BWD>()];
   const ScanProb p = probs[map[2 * blockIdx.x]];
   const int i = map[2 * blockIdx.x + 1], tile = i % p.tiles, b = i / p.tiles;
-  if constexpr (BWD) scan_bwd<T, W, L, false>(p, tile, b, 0, sm);
-  else scan_fwd<T, W, L, true>(p, tile, b, 0, sm);
+  if constexpr (BWD) scan_bwd<T, W, L, ScanForm::EACH>(p, tile, b, sm);
+  else scan_fwd<T, W, L, ScanForm::AHEAD>(p, tile, b, sm);
 }
 
 // ---------------------------------------------------------------------------
@@ -1083,7 +1105,6 @@ int norm_blocks(const NormPlan& p, int64_t rows) {
 
 namespace {
 // calls f with (element type, threads per row, vectors per thread) as constants
-template <int N> using Int = std::integral_constant<int, N>;
 template <typename F> hipError_t norm_pick(bool bf16, const NormPlan& p, F&& f) {
   auto nv = [&](auto type, auto tpr) {
     if (p.nv == 1) f(type, tpr, Int<1>{});
@@ -1137,53 +1158,62 @@ hipError_t launch_norm_dw(const float* part, int nparts, int d, float* dw, hipSt
   return hipGetLastError();
 }
 
-// Sequences and channel tiles of fewer than 256 workgroups leave CUs without
-// work: the time axis is split, into as many segments as give two workgroups per
-// CU. A first launch composes the segments' maps (it reads two of the operands once
-// more), the second folds those before its own segment. Forward and backward of one
-// 65536 x 512 sequence, bf16, with 512 / 768 / 1024 / 2048 workgroups: 156 / 161 /
-// 160 / 168 us; 4 x 4096 x 1024 73 / 83 / 77 / 81.
+// Sequences and channel tiles of fewer than 256 workgroups leave CUs without work:
+// the time axis is split, a segment per workgroup, which holds it in registers while
+// the value that arrives is put together (join), so that every operand is still read
+// once. A segment is as long as the registers allow (8 waves x 32 steps forward, x 16
+// backward: two workgroups per CU) where that gives two workgroups per CU, else 8 x 8.
+// Forward / backward in us, against two launches of which the first composed the
+// segments' maps: 2 x 16384 x 1024 in bf16 43 / 88, so 62 / 103; 1 x 65536 x 512 51 /
+// 101, so 60 / 96; 4 x 4096 x 1024 25 / 39, so 32 / 42; 8 x 2048 x 1024 in fp32 38 /
+// 75, so 50 / 83. Segments of 8 x 8 steps throughout: 1 x 65536 x 512 backward 128;
+// workgroups of 4 waves 81 / 154; of 16 53 / 117.
 // Between 256 and 512 workgroups a CU has one: chunks of 8 x 16 steps, one prepared
 // while another is finished, take the place of the second (16 x 2048 x 1024 with
-// chunks of 8 x 8 / 8 x 16: forward 42 / 38 us, backward 83 / 76). Above, and in
-// segments, two or more workgroups per CU fill one another's stalls, and chunks of
-// 8 x 8 leave room for them (64 x 1024 x 1024: forward 90 / 89, backward 146 / 148;
-// 4 x 4096 x 1024 32 / 38 and 43 / 49); the backward's are not prepared ahead
-// (163 us with, 146 without).
+// chunks of 8 x 8 / 8 x 16: forward 42 / 38 us, backward 83 / 76). Above, two or more
+// workgroups per CU fill one another's stalls, and chunks of 8 x 8 leave room for
+// them (64 x 1024 x 1024: forward 90 / 89, backward 146 / 148); the backward's are
+// not prepared ahead (163 us with, 146 without).
+constexpr int SCAN_HELD_FWD = 32, SCAN_HELD_BWD = 16;
 constexpr int SCAN_GROUPS = 512;
-ScanPlan scan_plan(int64_t B, int T, int d) {
+ScanPlan scan_plan(int64_t B, int T, int d, bool bwd) {
   ScanPlan p{};
   p.kind = T <= 1 ? SCAN_ONE : T <= SCAN_SHORT ? SCAN_WAVE : SCAN_CHUNKS;
   p.tiles = (d + 63) / 64;
-  const int states = scan_chunks(T);
-  p.seg = std::max(1, states);
   p.nseg = 1;
   const int64_t groups = B * p.tiles;
-  if (p.kind == SCAN_CHUNKS && groups < 256 && states > 4) {
-    const int want = (int)std::min<int64_t>(states, (SCAN_GROUPS + groups - 1) / groups);
-    p.seg = (states + want - 1) / want;
-    p.nseg = (states + p.seg - 1) / p.seg;
+  if (p.kind != SCAN_CHUNKS) return p;
+  if (groups < 256 && T > 4 * SCAN_STATE) {
+    const int most = SCAN_W * (bwd ? SCAN_HELD_BWD : SCAN_HELD_FWD);
+    const bool enough = groups * ((T + most - 1) / most) >= SCAN_GROUPS;
+    const int steps = enough ? most : SCAN_W * 8;
+    p.kind = enough ? SCAN_LONG_SPLIT : SCAN_SPLIT;
+    p.nseg = (T + steps - 1) / steps;
+  } else if (groups < SCAN_GROUPS) {
+    p.kind = SCAN_LONG_CHUNKS;
   }
-  if (p.kind == SCAN_CHUNKS && p.nseg == 1 && groups < SCAN_GROUPS) p.kind = SCAN_LONG_CHUNKS;
   return p;
 }
 
 namespace {
 template <typename T, bool BWD> void scan_go(const ScanPlan& plan, const ScanProb& p, unsigned grid, hipStream_t s) {
   constexpr int W = SCAN_W;
-  if (plan.kind == SCAN_ONE) {
-    hipLaunchKernelGGL((scan_kernel<T, 1, 1, false, BWD>), dim3(grid), dim3(64), 0, s, p);
-  } else if (plan.kind == SCAN_WAVE) {
-    hipLaunchKernelGGL((scan_kernel<T, 1, SCAN_SHORT, false, BWD>), dim3(grid), dim3(64), 0, s, p);
-  } else if (plan.kind == SCAN_LONG_CHUNKS) {
-    hipLaunchKernelGGL((scan_kernel<T, W, 16, true, BWD>), dim3(grid), dim3(64 * W), 0, s, p);
-  } else {
-    ScanProb q = p;
-    if (plan.nseg > 1) {
-      hipLaunchKernelGGL((scan_agg_kernel<T, W, 8, BWD>), dim3(grid - grid / plan.nseg), dim3(64 * W), 0, s, p);
-      if (p.start) q.start = p.agg + (int64_t)p.nseg * p.B * p.d * 2;
-    }
-    hipLaunchKernelGGL((scan_kernel<T, W, 8, !BWD, BWD>), dim3(grid), dim3(64 * W), 0, s, q);
+  const dim3 one(64), all(64 * W);
+  if (plan.nseg > 1) {
+    const int64_t n = scan_ws_words(plan, p.B, p.d);
+    hipLaunchKernelGGL(scan_clear_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, p.joint, n);
+  }
+  switch (plan.kind) {
+    case SCAN_ONE: hipLaunchKernelGGL((scan_kernel<T, 1, 1, ScanForm::EACH, BWD>), dim3(grid), one, 0, s, p); break;
+    case SCAN_WAVE: hipLaunchKernelGGL((scan_kernel<T, 1, SCAN_SHORT, ScanForm::EACH, BWD>), dim3(grid), one, 0, s, p); break;
+    case SCAN_CHUNKS:
+      hipLaunchKernelGGL((scan_kernel<T, W, 8, BWD ? ScanForm::EACH : ScanForm::AHEAD, BWD>), dim3(grid), all, 0, s, p);
+      break;
+    case SCAN_LONG_CHUNKS: hipLaunchKernelGGL((scan_kernel<T, W, 16, ScanForm::AHEAD, BWD>), dim3(grid), all, 0, s, p); break;
+    case SCAN_SPLIT: hipLaunchKernelGGL((scan_split_kernel<T, W, 8, BWD>), dim3(grid), all, 0, s, p); break;
+    case SCAN_LONG_SPLIT:
+      hipLaunchKernelGGL((scan_split_kernel<T, W, BWD ? SCAN_HELD_BWD : SCAN_HELD_FWD, BWD>), dim3(grid), all, 0, s, p);
+      break;
   }
 }
 }  // namespace
@@ -1191,7 +1221,6 @@ template <typename T, bool BWD> void scan_go(const ScanPlan& plan, const ScanPro
 hipError_t launch_scan(bool bf16, bool bwd, const ScanPlan& plan, const ScanProb& q, hipStream_t s) {
   ScanProb p = q;
   p.tiles = plan.tiles;
-  p.seg = plan.seg;
   p.nseg = plan.nseg;
   const unsigned grid = (unsigned)((int64_t)p.tiles * p.B * p.nseg);
   if (grid == 0) return hipSuccess;

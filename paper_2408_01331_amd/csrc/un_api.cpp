@@ -1249,7 +1249,6 @@ static void build_tables(un_ctx* c, Tables& T) {
     for (size_t k = 0; k < ps.size(); ++k) {
       ScanProb& p = ps[k];
       p.tiles = cdiv(p.d, 64);
-      p.seg = scan_chunks(p.T);
       p.nseg = 1;
       for (int t = 0; t < p.tiles * p.B; ++t) {
         map.push_back((int32_t)k);

@@ -33,7 +33,7 @@ def out_bound(want, bound, dtype):
 # RMS norm
 # ---------------------------------------------------------------------------
 NORM_SIZES = [(1, 1), (3, 7), (5, 8), (1, 64), (70, 100), (9, 999), (4, 2048), (3, 2056), (2, 8191), (2, 8200), (1, 16384),
-              (1100, 40), (0, 16)]
+              (1100, 40), (0, 16), (33000, 40), (66000, 33), (2100, 2048)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
@@ -120,7 +120,7 @@ def test_norm_in_place_sum(ops):
 # Gated linear recurrence
 # ---------------------------------------------------------------------------
 SCAN_SIZES = [(1, 1, 1), (3, 1, 70), (2, 2, 64), (5, 15, 33), (2, 16, 130), (2, 17, 8), (1, 127, 65), (1, 128, 64), (2, 129, 66),
-              (1, 257, 3), (3, 1000, 100), (1, 5000, 17), (300, 130, 128), (520, 140, 130)]
+              (1, 257, 3), (3, 1000, 100), (1, 5000, 17), (300, 130, 128), (520, 140, 130), (130, 300, 100), (64, 300, 200)]
 
 
 def check_scan(ops, gate, value, h0, lens, dh, dlast, dtype, cols=None):
@@ -159,6 +159,52 @@ def test_scan_long_split(ops, dtype):
     gate, value, dh = rand(1, (b, n, w), dtype, mean=4.0, std=2.0).clamp(-8, 8), rand(2, (b, n, w), dtype), rand(3, (b, n, w), dtype)
     lens = torch.tensor([6000, 2049, 129], dtype=torch.int32, device="cuda")
     check_scan(ops, gate, value, rand(4, (b, w)), lens, dh, rand(5, (b, w)), dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+def test_scan_split_many(ops, dtype):
+    """Many sequences and channels that are split all the same, with lengths of 0, 1, within, at and past a segment's end."""
+    b, n, w = 8, 2100, 500
+    gate, value, dh = rand(1, (b, n, w), dtype, mean=4.0, std=2.0).clamp(-8, 8), rand(2, (b, n, w), dtype), rand(3, (b, n, w), dtype)
+    lens = torch.tensor([2100, 0, 1, 255, 256, 257, 1024, 2099], dtype=torch.int32, device="cuda")
+    check_scan(ops, gate, value, rand(4, (b, w)), lens, dh, rand(5, (b, w)), dtype)
+
+
+@pytest.mark.parametrize("n,w", [(2400, 70), (33100, 5)])
+def test_scan_split_runs(ops, n, w):
+    """More segments than join by their maps (runs of 32, and of 128 above 512 segments); the same bits each time."""
+    gate, value, dh = rand(1, (1, n, w), BF16, mean=6.0).clamp(-8, 8), rand(2, (1, n, w), BF16), rand(3, (1, n, w), BF16)
+    h0, dlast = rand(4, (1, w)), rand(5, (1, w))
+    first = check_scan(ops, gate, value, h0, None, dh, dlast, BF16)
+    for _ in range(10):
+        h, last, states = ops.gated_scan(gate, value, h0=h0, keep=True)
+        again = (h, last, *ops.gated_scan_backward(gate, value, states, dh, dlast=dlast))
+        assert all(torch.equal(x, y) for x, y in zip(first, again))
+
+
+def test_scan_split_values_that_are_not_finite(ops):
+    """A NaN (of any bits, all ones among them) reaches every later step of its channel, and no other channel."""
+    gate, value = rand(1, (2, 3000, 70), mean=3.0), rand(2, (2, 3000, 70))
+    clean = ops.gated_scan(gate, value)[0]
+    value.view(torch.int32)[0, 500, 3] = -1
+    gate.view(torch.int32)[1, 64, 69] = -1
+    value[0, 700, 4] = float("inf")
+    h, last, _ = ops.gated_scan(gate, value)
+    assert torch.isnan(h[0, 500:, 3]).all() and torch.isnan(h[1, 64:, 69]).all() and torch.isnan(last[0, 3]) and torch.isnan(last[1, 69])
+    assert torch.isinf(h[0, 700:, 4]).all()
+    for x in (h, clean):
+        x[0, 500:, 3], x[1, 64:, 69], x[0, 700:, 4] = 0, 0, 0
+    assert torch.equal(h, clean)
+
+
+@pytest.mark.parametrize("b,n", [(2, 0), (0, 5), (0, 3000)])
+def test_scan_of_nothing(ops, b, n):
+    gate, h0, dlast = rand(1, (b, n, 70)), rand(2, (b, 70)), rand(3, (b, 70))
+    h, last, states = ops.gated_scan(gate, gate, h0=h0, keep=True)
+    assert h.shape == gate.shape and torch.equal(last, h0)
+    assert torch.equal(ops.gated_scan(gate, gate)[1], torch.zeros_like(h0))
+    dg, dv, dh0 = ops.gated_scan_backward(gate, gate, states, gate, dlast=dlast)
+    assert dg.shape == dv.shape == gate.shape and torch.equal(dh0, dlast)
 
 
 def test_scan_strides(ops):
@@ -354,6 +400,31 @@ def test_adamw8_rounds_without_bias(ops):
         assert (off[~floor] <= 2.5 / math.sqrt(draws) + 1e-4).all()
 
 
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("gtype", DTYPES, ids=["f32", "bf16"])
+def test_adamw_large_lists(ops, eight, gtype):
+    """Above 128 MiB a step's accesses pass the caches: the same bits as for the first tensor alone, with a ragged end."""
+    counts = [9_000_003, 8_000_001]
+    p, g = params_of(1, F32, counts), params_of(100, gtype, counts)
+    got = []
+    for k in (1, 2):
+        q = [x.clone() for x in p[:k]]
+        c = [torch.zeros_like(x, dtype=BF16) for x in q]
+        if eight:
+            m, v, ms, vs = ops.AdamW.state8(q)
+            opt = ops.AdamW(q, g[:k], m, v, copies=c, m_scales=ms, v_scales=vs)
+            state = [m[0].view(torch.uint8), v[0].view(torch.uint8), ms[0].view(torch.uint8), vs[0].view(torch.uint8)]
+        else:
+            m, v = [torch.zeros_like(x) for x in q], [torch.zeros_like(x) for x in q]
+            opt = ops.AdamW(q, g[:k], m, v, copies=c)
+            state = [m[0], v[0]]
+        for t in (1, 2):
+            opt.step(0.01, t, key=t, **HYPER)
+        assert all(torch.equal(a, b.to(BF16)) for a, b in zip(c, q)) and not torch.equal(q[-1], p[k - 1])
+        got.append([q[0], *state])
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_adamw8_depends_on_key_alone(ops):
     """The same step twice gives the same bits; another key rounds otherwise."""
     res = []
@@ -398,6 +469,15 @@ def test_adamw_refusals(ops):
         ops.AdamW(p, [torch.zeros(9, device="cuda")], z(), z())
     with pytest.raises(ValueError, match="m\\["):
         ops.AdamW(p, z(), [torch.zeros(10, device="cuda", dtype=BF16)], z())
+    with pytest.raises(ValueError, match="overlap"):
+        ops.AdamW(p + p, z() + z(), z() + z(), z() + z())
+    m = z()
+    with pytest.raises(ValueError, match="overlap"):
+        ops.AdamW(p, z(), m, m)
+    whole = rand(1, (20,))
+    with pytest.raises(ValueError, match="overlap"):
+        ops.AdamW([whole[:10], whole[9:19]], z() + z(), z() + z(), z() + z())
+    ops.AdamW([whole[:10], whole[10:]], z() + z(), z() + z(), z() + z(), copies=[torch.zeros(10, device="cuda", dtype=BF16) for _ in range(2)])
 
 
 # ---------------------------------------------------------------------------

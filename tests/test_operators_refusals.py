@@ -61,6 +61,9 @@ SCANG = dict(type=0, batch=2, tokens=5, width=64, gate=P, value=P, ld_in=64, seq
     ("un_gated_scan", SCAN, dict(ld_h=10), 1, "stride"),
     ("un_gated_scan", SCAN, dict(seq_h=0), 1, "stride"),
     ("un_gated_scan", SCAN, dict(batch=1, tokens=100000), 6, "workspace"),
+    ("un_gated_scan", SCAN, dict(batch=1, tokens=1000, workspace=P + 4, workspace_bytes=1 << 20), 1, "aligned"),
+    ("un_gated_scan", SCAN, dict(width=1 << 24, ld_in=1 << 24, ld_h=1 << 24, seq_h=1 << 28), 7, "2^24"),
+    ("un_gated_scan", SCAN, dict(ld_in=1 << 24), 7, "2^24"),
     ("un_gated_scan", SCAN, dict(tokens=(1 << 30) + 1), 7, "tokens"),
     ("un_gated_scan", SCAN, dict(batch=1 << 30, tokens=17, width=4096, ld_in=4096, ld_h=4096, seq_h=1 << 20), 7, "too many"),
     ("un_gated_scan_backward", SCANG, dict(states=None), 1, "NULL"),
@@ -68,6 +71,8 @@ SCANG = dict(type=0, batch=2, tokens=5, width=64, gate=P, value=P, ld_in=64, seq
     ("un_gated_scan_backward", SCANG, dict(ld_out=63), 1, "stride"),
     ("un_gated_scan_backward", SCANG, dict(seq_out=0), 1, "stride"),
     ("un_gated_scan_backward", SCANG, dict(batch=1, tokens=100000), 6, "workspace"),
+    ("un_gated_scan_backward", SCANG, dict(batch=1, tokens=1000, workspace=P + 4, workspace_bytes=1 << 20), 1, "aligned"),
+    ("un_gated_scan_backward", SCANG, dict(ld_dh=1 << 24), 7, "2^24"),
 ])
 def test_refused(fn, base, change, want, text):
     args = getattr(U, {"un_rms_norm": "un_rms_norm_args", "un_rms_norm_backward": "un_rms_norm_grad_args",
@@ -97,9 +102,9 @@ def test_sizes():
     L = U.lib()
     n, b = ctypes.c_size_t(), ctypes.c_size_t()
     assert L.un_gated_scan_sizes(3, 129, 10, ctypes.byref(n), ctypes.byref(b)) == U.UN_OK
-    assert n.value == 3 * 2 * 10 and b.value == 0
+    assert n.value == 3 * 3 * 10 and b.value == 0  # a state every 64 steps
     assert L.un_gated_scan_sizes(1, 65536, 512, ctypes.byref(n), ctypes.byref(b)) == U.UN_OK
-    assert n.value == 512 * 512 and b.value > 0 and b.value % (512 * 4) == 0
+    assert n.value == 1024 * 512 and b.value > 0 and b.value % 8 == 0
     assert L.un_gated_scan_sizes(1, -1, 4, ctypes.byref(n), ctypes.byref(b)) == U.UN_ERR_INVALID
     assert L.un_rms_norm_workspace(0, 5, 100, ctypes.byref(b)) == U.UN_OK and b.value % 400 == 0 and b.value >= 400
     assert L.un_rms_norm_workspace(0, 5, 100, None) == U.UN_ERR_INVALID
