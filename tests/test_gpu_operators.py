@@ -86,6 +86,21 @@ def test_norm_strides_and_alignment(ops, dtype):
     assert torch.equal(ops.rms_norm(x3[0, 0, 0], w)[0], y[0, 0, 0])
 
 
+def test_norm_past_the_caches(ops):
+    """Above 256 MiB a call's reads pass the caches: the same bits as for its first rows alone."""
+    rows, less, width = 40000, 30000, 1000
+    x, r, w, dy, ds = (rand(k, (rows, width), BF16) if k != 3 else rand(3, (width,), mean=1.0, std=0.3) for k in range(1, 6))
+    got = []
+    for k in (rows, less):
+        y, s, rstd = ops.rms_norm(x[:k], w, residual=r[:k], keep=True)
+        got.append((y, s, rstd, *ops.rms_norm_backward(dy[:k], s, w, rstd, ds=ds[:k])))
+    for a, b in zip(got[0][:4], got[1][:4]):
+        assert torch.equal(a[:less], b)
+    terms = dy.double() * got[0][1].double() * got[0][2].double()[:, None]
+    # dw: a rounding per term and per sum, and the two of each product
+    assert ((got[0][4].double() - terms.sum(0)).abs() <= terms.abs().sum(0) * R.U32 * (rows + 40)).all()
+
+
 def test_norm_special_values(ops):
     """Rows of zeros, a NaN or an infinity concern their own row alone."""
     w = torch.ones(40, device="cuda")
@@ -205,6 +220,20 @@ def test_scan_of_nothing(ops, b, n):
     assert torch.equal(ops.gated_scan(gate, gate)[1], torch.zeros_like(h0))
     dg, dv, dh0 = ops.gated_scan_backward(gate, gate, states, gate, dlast=dlast)
     assert dg.shape == dv.shape == gate.shape and torch.equal(dh0, dlast)
+
+
+@pytest.mark.parametrize("b,less,n,w", [(1200, 600, 300, 128), (250, 150, 1500, 128), (3, 1, 125000, 128)])
+def test_scan_past_the_caches(ops, b, less, n, w):
+    """Above 256 MiB a call's accesses pass the caches: the same bits as for its first sequences alone."""
+    z, dh = rand(1, (b, n, 2 * w), BF16, mean=1.0), rand(2, (b, n, w), BF16)
+    got = []
+    for k in (b, less):
+        gate, value = z[:k, :, :w], z[:k, :, w:]
+        h, last, states = ops.gated_scan(gate, value, keep=True)
+        got.append((h, last, *ops.gated_scan_backward(gate, value, states, dh[:k])))
+    assert 6 * b * n * w >= 1 << 28 > 6 * less * n * w
+    for x, y in zip(*got):
+        assert torch.equal(x[:less], y)
 
 
 def test_scan_strides(ops):
