@@ -303,25 +303,28 @@ class AdamW:
         _require(gt in _TYPES, f"gradients must be float32 or bfloat16, not {gt}")
         st = torch.float8_e4m3fn if eight else torch.float32
         arr = (_un.un_adamw_tensor * n)()
+        lists = dict(params=params, **lists)
+        types = dict(params=_F32, grads=gt, m=st, v=st, copies=_BF16, m_scales=torch.float8_e8m0fnu, v_scales=torch.float8_e8m0fnu)
+        order = [(lists[k], types[k], k, k.endswith("scales")) if k in lists else None
+                 for k in ("params", "grads", "copies", "m", "v", "m_scales", "v_scales")]
         for i, p in enumerate(params):
-            _require(isinstance(p, torch.Tensor) and p.get_device() == dev and p.dtype is _F32 and p.is_contiguous(),
-                     f"params[{i}] must be a contiguous {_F32} tensor on {device}")
+            _require(isinstance(p, torch.Tensor), f"params[{i}] must be a tensor")
             k = p.numel()
-            for name, x, dt in (("grads", grads, gt), ("m", m, st), ("v", v, st), ("copies", copies, torch.bfloat16)):
-                if x is not None:
-                    y = x[i]
-                    _require(isinstance(y, torch.Tensor) and y.get_device() == dev and y.dtype is dt and y.numel() == k and y.is_contiguous(),
-                             f"{name}[{i}] must be a contiguous {dt} tensor of {k} elements on {device}")
-            if eight:
-                for name, x in (("m_scales", m_scales), ("v_scales", v_scales)):
-                    _require(x[i].get_device() == dev and x[i].dtype == torch.float8_e8m0fnu and x[i].numel() == -(-k // QBLOCK) and x[i].is_contiguous(),
-                             f"{name}[{i}] must be a contiguous float8_e8m0fnu tensor of {-(-k // QBLOCK)} elements on {device}")
-            arr[i] = _un.un_adamw_tensor(_ptr(p), _ptr(grads[i]), _ptr(copies[i]) if copies is not None else None, _ptr(m[i]), _ptr(v[i]),
-                                         _ptr(m_scales[i]) if eight else None, _ptr(v_scales[i]) if eight else None, k)
+            at = []
+            for entry in order:
+                if entry is None:
+                    at.append(None)
+                    continue
+                x, dt, name, scales = entry
+                y, size = x[i], -(-k // QBLOCK) if scales else k
+                if not (isinstance(y, torch.Tensor) and y.get_device() == dev and y.dtype is dt and y.numel() == size and y.is_contiguous()):
+                    _require(False, f"{name}[{i}] must be a contiguous {dt} tensor of {size} elements on {device}")
+                at.append(y.data_ptr())
+            arr[i] = _un.un_adamw_tensor(*at, k)
         written = sorted((y.data_ptr(), y.data_ptr() + y.numel() * y.element_size())
                          for x in (params, m, v, copies, m_scales, v_scales) for y in x or () if y.numel())
         _require(all(a[1] <= b[0] for a, b in zip(written, written[1:])), "tensors that are written overlap")
-        self._held = [params, lists]
+        self._held = [list(x) for x in lists.values()]
         self.device, self._index = device, dev
         plan = ctypes.c_void_p()
         with torch.cuda.device(device):
