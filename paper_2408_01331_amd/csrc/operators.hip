@@ -162,10 +162,13 @@ template <int TPR, int R, typename F> __device__ __forceinline__ void row_reduce
 }
 
 // ---------------------------------------------------------------------------
-// RMS norm. A row belongs to TPR threads of NV 16-byte vectors each; a
-// workgroup holds G = NT / TPR rows side by side and R in each thread, so R
-// rows' loads are in flight together and share one reduction's latency and one
-// load of the weights.
+// RMS norm. A row belongs to TPR threads of NV 16-byte vectors each, and a
+// workgroup holds G = NT / TPR rows side by side; a row stays in registers from its
+// load to its result. Backward, R rows in each thread: their loads are in flight
+// together and share one reduction's latency and one load of the weights. Forward,
+// where nothing is kept between rows, more workgroups do the same for less (R = 4
+// rows a thread, so 1, in bf16, us: 262144 x 64 30.4, so 25.5; 33000 x 300 28.8, so
+// 22.6; 8192 x 2048 21.6, so 20.6; 8192 x 8192 83, so 83).
 // ---------------------------------------------------------------------------
 constexpr int norm_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
 template <int TPR, int R> constexpr int norm_sm() { return TPR > 64 ? 2 * TPR / 64 * R : 1; }
@@ -199,126 +202,104 @@ template <typename T, int NV> struct RowVec {
 // rows per thread at a time: as many as leave registers for two workgroups more
 template <int TPR, int NV> constexpr int norm_rows() { return std::max(1, (TPR == 1024 ? NORM_R / 2 : NORM_R) / NV); }
 
-template <typename T, int TPR, int NV, int R, bool E4M3, bool ONCE>
+template <typename T, int TPR, int NV, bool E4M3, bool ONCE>
 __device__ __forceinline__ void norm_fwd_rows(const NormProb& p, int64_t row0, float* sm) {
-  constexpr int N = V16<T>::N, G = norm_threads(TPR) / TPR;
+  constexpr int N = V16<T>::N;
   const int t = threadIdx.x & (TPR - 1), d = p.d;
-  int cnt[NV], flip = 0;
+  const int64_t row = row0 + threadIdx.x / TPR, at = row < p.rows ? row : 0;
+  int cnt[NV], live[NV], flip = 0;
   float w[NV][N];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = (j * TPR + t) * N;
     cnt[j] = min(max(d - c, 0), N);
+    live[j] = row < p.rows ? cnt[j] : 0;
     load_f32<N>(p.w + c, cnt[j], w[j]);
   }
-  row0 += threadIdx.x / TPR;
-  RowVec<T, NV> x[R], r[R];
-  int live[R][NV];
+  RowVec<T, NV> x, r;
+  x.template load<ONCE>((const T*)p.x + at * p.ldx, live, TPR, t);
+  if (p.r) r.template load<ONCE>((const T*)p.r + at * p.ldr, live, TPR, t);
+  float sum[1] = {0.f}, top[1] = {0.f};
 #pragma unroll
-  for (int k = 0; k < R; ++k) {
-    const int64_t row = row0 + (int64_t)k * G, at = row < p.rows ? row : 0;
+  for (int j = 0; j < NV; ++j) {
+    float f[N];
+    x.get(j, f);
+    if (p.r) {
+      float g[N];
+      r.get(j, g);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) live[k][j] = row < p.rows ? cnt[j] : 0;
-    x[k].template load<ONCE>((const T*)p.x + at * p.ldx, live[k], TPR, t);
-    if (p.r) r[k].template load<ONCE>((const T*)p.r + at * p.ldr, live[k], TPR, t);
-  }
-  float sum[R];
-#pragma unroll
-  for (int k = 0; k < R; ++k) {
-    const int64_t row = row0 + (int64_t)k * G;
-    sum[k] = 0.f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float f[N];
-      x[k].get(j, f);
-      if (p.r) {
-        float g[N];
-        r[k].get(j, g);
-#pragma unroll
-        for (int e = 0; e < N; ++e) f[e] += g[e];
-        x[k].raw[j] = V16<T>::pack(f);
-        x[k].get(j, f);  // the norm is that of the stored sum
-      }
-      if (p.s) store_vec<T>((T*)p.s + row * p.lds + (j * TPR + t) * N, live[k][j], f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) sum[k] = fmaf(f[e], f[e], sum[k]);
+      for (int e = 0; e < N; ++e) f[e] += g[e];
+      x.raw[j] = V16<T>::pack(f);
+      x.get(j, f);  // the norm is that of the stored sum
     }
+    if (p.s) store_vec<T>((T*)p.s + row * p.lds + (j * TPR + t) * N, live[j], f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[0] = fmaf(f[e], f[e], sum[0]);
   }
-  row_reduce<TPR, R>(sum, Add{}, sm, flip);
+  row_reduce<TPR, 1>(sum, Add{}, sm, flip);
+  x.forget();
+  const float q = 1.f / sqrtf(sum[0] / (float)d + p.eps);
+  if (p.rstd && t == 0 && row < p.rows) p.rstd[row] = q;
 #pragma unroll
-  for (int k = 0; k < R; ++k) x[k].forget();
-  float q[R], top[R];
+  for (int j = 0; j < NV; ++j) {
+    float f[N];
+    x.get(j, f);
 #pragma unroll
-  for (int k = 0; k < R; ++k) {
-    const int64_t row = row0 + (int64_t)k * G;
-    q[k] = 1.f / sqrtf(sum[k] / (float)d + p.eps);
-    if (p.rstd && t == 0 && row < p.rows) p.rstd[row] = q[k];
-    top[k] = 0.f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float f[N];
-      x[k].get(j, f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        f[e] = f[e] * q[k] * w[j][e];
-        top[k] = fmaxf(top[k], fabsf(f[e]));
-      }
-      if constexpr (!E4M3) store_vec<T>((T*)p.y + row * p.ldy + (j * TPR + t) * N, live[k][j], f);
+    for (int e = 0; e < N; ++e) {
+      f[e] = f[e] * q * w[j][e];
+      top[0] = fmaxf(top[0], fabsf(f[e]));
     }
+    if constexpr (!E4M3) store_vec<T>((T*)p.y + row * p.ldy + (j * TPR + t) * N, live[j], f);
   }
   if constexpr (E4M3) {
-    row_reduce<TPR, R>(top, Max{}, sm, flip);
+    row_reduce<TPR, 1>(top, Max{}, sm, flip);
+    x.forget();
+    // the row's largest value becomes 448, e4m3's largest; a row of zeros keeps a scale that is not zero
+    const float m = fmaxf(top[0], 1e-30f), inv = 448.f / m;
+    if (t == 0 && row < p.rows) p.scale[row] = m / 448.f;
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-      x[k].forget();
-      const int64_t row = row0 + (int64_t)k * G;
-      // the row's largest value becomes 448, e4m3's largest; a row of zeros keeps a scale that is not zero
-      const float m = fmaxf(top[k], 1e-30f), inv = 448.f / m;
-      if (t == 0 && row < p.rows) p.scale[row] = m / 448.f;
+    for (int j = 0; j < NV; ++j) {
+      float f[N];
+      x.get(j, f);
+      uint32_t code[N / 4];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        float f[N];
-        x[k].get(j, f);
-        uint32_t code[N / 4];
+      for (int e = 0; e < N; e += 4) {
+        // the product may pass 448 by its rounding (a NaN stays one)
+        float v[4];
 #pragma unroll
-        for (int e = 0; e < N; e += 4) {
-          // the product may pass 448 by its rounding (a NaN stays one)
-          float v[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            v[i] = f[e + i] * q[k] * w[j][e + i] * inv;
-            v[i] = fabsf(v[i]) > 448.f ? copysignf(448.f, v[i]) : v[i];
-          }
-          const int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
-          code[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
+        for (int i = 0; i < 4; ++i) {
+          v[i] = f[e + i] * q * w[j][e + i] * inv;
+          v[i] = fabsf(v[i]) > 448.f ? copysignf(448.f, v[i]) : v[i];
         }
-        uint8_t* o = (uint8_t*)p.y + row * p.ldy + (j * TPR + t) * N;
-        if (live[k][j] == N) {
-          if constexpr (N == 8) *(u32x2_a1*)o = u32x2{code[0], code[1]};
-          else *(u32_a1*)o = code[0];
-        } else {
+        const int c = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
+        code[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], c, true);
+      }
+      uint8_t* o = (uint8_t*)p.y + row * p.ldy + (j * TPR + t) * N;
+      if (live[j] == N) {
+        if constexpr (N == 8) *(u32x2_a1*)o = u32x2{code[0], code[1]};
+        else *(u32_a1*)o = code[0];
+      } else {
 #pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (e < live[k][j]) o[e] = (uint8_t)(code[e / 4] >> (8 * (e % 4)));
-        }
+        for (int e = 0; e < N; ++e)
+          if (e < live[j]) o[e] = (uint8_t)(code[e / 4] >> (8 * (e % 4)));
       }
     }
   }
 }
 
-template <typename T, int TPR, int NV, int R, bool E4M3, bool ONCE>
+template <typename T, int TPR, int NV, bool E4M3, bool ONCE>
 __global__ __launch_bounds__(norm_threads(TPR)) void norm_fwd_kernel(NormProb p) {
-  __shared__ float sm[norm_sm<TPR, R>()];
+  __shared__ float sm[norm_sm<TPR, 1>()];
   constexpr int G = norm_threads(TPR) / TPR;
-  norm_fwd_rows<T, TPR, NV, R, E4M3, ONCE>(p, (int64_t)blockIdx.x * (G * R), sm);
+  norm_fwd_rows<T, TPR, NV, E4M3, ONCE>(p, (int64_t)blockIdx.x * G, sm);
 }
-template <typename T, int TPR, int NV, int R>
+template <typename T, int TPR, int NV>
 __global__ __launch_bounds__(norm_threads(TPR)) void norm_fwd_table_kernel(const NormProb* __restrict__ probs,
                                                                            const int32_t* __restrict__ map) {
-  __shared__ float sm[norm_sm<TPR, R>()];
+  __shared__ float sm[norm_sm<TPR, 1>()];
   constexpr int G = norm_threads(TPR) / TPR;
   const NormProb p = probs[map[2 * blockIdx.x]];
-  norm_fwd_rows<T, TPR, NV, R, false, false>(p, (int64_t)map[2 * blockIdx.x + 1] * (G * R), sm);
+  norm_fwd_rows<T, TPR, NV, false, false>(p, (int64_t)map[2 * blockIdx.x + 1] * G, sm);
 }
 
 // Backward. A workgroup takes every `blocks`-th run of G R rows and keeps its
@@ -893,9 +874,15 @@ __global__ __launch_bounds__(64 * W) void scan_split_kernel(ScanProb p) {
   if constexpr (BWD) scan_bwd<T, W, L, ScanForm::SPLIT, ONCE>(p, tile, b, sm, p.nseg - 1 - o);
   else scan_fwd<T, W, L, ScanForm::SPLIT, ONCE>(p, tile, b, sm, o);
 }
+// (written through: 2 x 16384 x 1024 backward 84 us, with ordinary stores of one
+// word a thread, so 81)
+constexpr int SCAN_CLEAR = 4;
 __global__ __launch_bounds__(256) void scan_clear_kernel(uint64_t* p, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i < n) p[i] = EMPTY;
+#pragma unroll
+  for (int k = 0; k < SCAN_CLEAR; ++k) {
+    const int64_t i = ((int64_t)blockIdx.x * SCAN_CLEAR + k) * 256 + threadIdx.x;
+    if (i < n) __hip_atomic_store(p + i, EMPTY, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
 }
 template <typename T, int W, int L, bool BWD>
 __global__ __launch_bounds__(64 * W) void scan_table_kernel(const ScanProb* __restrict__ probs, const int32_t* __restrict__ map) {
@@ -1113,9 +1100,13 @@ NormPlan norm_plan(bool bf16, int d) {
   while (tpr * n * nv < d) nv *= 2;
   return NormPlan{tpr, nv, norm_threads(tpr) / tpr, norm_threads(tpr) / tpr * std::max(1, (tpr == 1024 ? NORM_R / 2 : NORM_R) / nv)};
 }
+// Workgroups of the backward pass: about as many as the registers let run at once;
+// more only write more shares of dw, and fewer leave CUs without work. Half / this /
+// twice as many, bf16, us: 262144 x 64 (768) 63 / 38 / 48; 32768 x 2048 (512) 114 / 90
+// / 98; 8192 x 8192 (256) 135 / 100 / 102; 512 x 12000 23 / 23 / 34.
 int norm_blocks(const NormPlan& p, int64_t rows) {
   const int64_t groups = (rows + p.rows - 1) / p.rows;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(groups, p.tpr == 1024 ? 512 : 1024));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(groups, p.tpr == 1024 ? 256 : p.tpr == 256 ? 512 : 768));
 }
 
 namespace {
@@ -1141,24 +1132,17 @@ template <typename F> hipError_t norm_pick(bool bf16, const NormPlan& p, F&& f) 
 
 // Reads of a call that moves more than the last-level cache holds pass it by. Forward
 // and backward with a residual in bf16, ordinary / past it, us: 32768 x 2048 (537 MB a
-// call) 210 / 190; 16384 x 2048 (268 MB) 101 /
-// 98; below, 4096 x 2048 35 / 39. (Not with e4m3 codes, where it measured nothing.)
+// call) 210 / 190; 16384 x 2048 (268 MB) 101 / 98; below, 4096 x 2048 35 / 39. (Not
+// with e4m3 codes, where it measured nothing.)
 hipError_t launch_norm(bool bf16, bool e4m3, const NormPlan& plan, const NormProb& p, hipStream_t s) {
   if (p.rows <= 0) return hipSuccess;
-  // one row per thread where several would leave CUs without work
-  const bool few = p.rows < (int64_t)plan.rows * 512;
-  const int64_t per = few ? plan.group : plan.rows, grid = (p.rows + per - 1) / per;
-  const int es = bf16 ? 2 : 4;
-  const bool once = p.rows * p.d * es * ((p.r ? 2 : 1) + (p.s ? 2 : 1)) >= LAST_LEVEL;
+  const bool once = p.rows * p.d * (bf16 ? 2 : 4) * ((p.r ? 2 : 1) + (p.s ? 2 : 1)) >= LAST_LEVEL;
   return norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
     using T = decltype(t);
-    constexpr int MANY = norm_rows<tpr(), nv()>();
-    const dim3 g((unsigned)grid), blk(norm_threads(tpr()));
-    if (e4m3 && few) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), 1, true, false>), g, blk, 0, s, p);
-    else if (e4m3) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), MANY, true, false>), g, blk, 0, s, p);
-    else if (few) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), 1, false, false>), g, blk, 0, s, p);
-    else if (once) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), MANY, false, true>), g, blk, 0, s, p);
-    else hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), MANY, false, false>), g, blk, 0, s, p);
+    const dim3 g((unsigned)((p.rows + plan.group - 1) / plan.group)), blk(norm_threads(tpr()));
+    if (e4m3) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), true, false>), g, blk, 0, s, p);
+    else if (once) hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), false, true>), g, blk, 0, s, p);
+    else hipLaunchKernelGGL((norm_fwd_kernel<T, tpr(), nv(), false, false>), g, blk, 0, s, p);
   });
 }
 hipError_t launch_norm_bwd(bool bf16, const NormPlan& plan, const NormProb& p, hipStream_t s) {
@@ -1178,7 +1162,7 @@ hipError_t launch_norm_table(bool bf16, bool bwd, const NormPlan& plan, const No
     using T = decltype(t);
     const dim3 blk(norm_threads(tpr()));
     if (bwd) hipLaunchKernelGGL((norm_bwd_table_kernel<T, tpr(), nv(), norm_rows<tpr(), nv()>()>), dim3(nblocks), blk, 0, s, probs, map, wsoff);
-    else hipLaunchKernelGGL((norm_fwd_table_kernel<T, tpr(), nv(), norm_rows<tpr(), nv()>()>), dim3(nblocks), blk, 0, s, probs, map);
+    else hipLaunchKernelGGL((norm_fwd_table_kernel<T, tpr(), nv()>), dim3(nblocks), blk, 0, s, probs, map);
   });
 }
 hipError_t launch_norm_dw(const float* part, int nparts, int d, float* dw, hipStream_t s) {
@@ -1229,7 +1213,7 @@ template <typename T, bool BWD, bool ONCE> void scan_go(const ScanPlan& plan, co
   const dim3 one(64), all(64 * W);
   if (plan.nseg > 1) {
     const int64_t n = scan_ws_words(plan, p.B, p.d);
-    hipLaunchKernelGGL(scan_clear_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, p.joint, n);
+    hipLaunchKernelGGL(scan_clear_kernel, dim3((unsigned)((n + 256 * SCAN_CLEAR - 1) / (256 * SCAN_CLEAR))), dim3(256), 0, s, p.joint, n);
   }
   switch (plan.kind) {
     case SCAN_ONE: hipLaunchKernelGGL((scan_kernel<T, 1, 1, ScanForm::EACH, BWD, false>), dim3(grid), one, 0, s, p); break;

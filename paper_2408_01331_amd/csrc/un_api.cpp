@@ -1271,7 +1271,7 @@ static void build_tables(un_ctx* c, Tables& T) {
   auto emit_norm_one = [&](std::vector<NormProb>& ps, const NormPlan& plan, std::vector<Launch>& out, int kind) {
     std::vector<int32_t> map;
     for (size_t k = 0; k < ps.size(); ++k) {
-      const int nb = kind == 13 ? cdiv(ps[k].rows, plan.rows) : ps[k].blocks;
+      const int nb = kind == 13 ? cdiv(ps[k].rows, plan.group) : ps[k].blocks;
       for (int t = 0; t < nb; ++t) {
         map.push_back((int32_t)k);
         map.push_back(t);
