@@ -68,13 +68,14 @@ typedef enum {
    * marker, x is added to their result, before any ReLU that follows the END
    * marker. In PyTorch terms the markers wrap the enclosed layers in a module
    * whose forward returns inner(x) + x. The enclosed layers are one or more
-   * [Linear, optional ReLU] or [Conv2d, optional ReLU] blocks (no ReLU
-   * directly before the END marker, no MaxPool2 inside or right after), the
-   * result has the shape of x, x is the output of a Linear or Conv2d block (a
-   * block never starts at the network input or after a Flatten), the block
-   * does not end at the logits layer and blocks do not nest; other patterns
-   * return UN_ERR_UNSUPPORTED (shape mismatches UN_ERR_INVALID). The markers
-   * have no parameters. */
+   * [Linear, optional ReLU] or [Conv2d, optional ReLU] blocks, or the blocks
+   * whose entries below say that markers may enclose them (no ReLU directly
+   * before the END marker, no MaxPool2 inside or right after), the result has
+   * the shape of x, x is the output of a Linear or Conv2d block (a block never
+   * starts at the network input or after a Flatten), the block does not end at
+   * the logits layer and blocks do not nest; other patterns return
+   * UN_ERR_UNSUPPORTED (shape mismatches UN_ERR_INVALID). The markers have no
+   * parameters. */
   UN_RESIDUAL_BEGIN = 5,
   UN_RESIDUAL_END = 6,
   /* View flat features as a sequence of `out` tokens of F / out features each
@@ -144,6 +145,8 @@ typedef struct {
  * present, then one or more [Linear, optional ReLU] blocks, the last Linear
  * having no ReLU and out == num_classes; residual markers may enclose runs of
  * the Linear blocks or of the Conv2d blocks as UN_RESIDUAL_BEGIN describes.
+ * Sequences, attention, norms and recurrences stand among the Linear blocks where
+ * their entries in un_op say.
  * Size restrictions (UN_ERR_UNSUPPORTED otherwise): when some model starts
  * with a Linear layer, in_c * in_h * in_w is a multiple of 8; a Linear layer
  * reading a flattened conv output reads a multiple of 8 features

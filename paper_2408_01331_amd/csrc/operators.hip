@@ -167,8 +167,8 @@ template <int TPR, int R, typename F> __device__ __forceinline__ void row_reduce
 // load to its result. Backward, R rows in each thread: their loads are in flight
 // together and share one reduction's latency and one load of the weights. Forward,
 // where nothing is kept between rows, more workgroups do the same for less (R = 4
-// rows a thread, so 1, in bf16, us: 262144 x 64 30.4, so 25.5; 33000 x 300 28.8, so
-// 22.6; 8192 x 2048 21.6, so 20.6; 8192 x 8192 83, so 83).
+// rows a thread, so 1, in bf16, us: 262144 x 64 30.5, so 26.5; 33000 x 300 28.8, so
+// 23.2; 8192 x 2048 21.8, so 20.7; 8192 x 8192 83, so 84).
 // ---------------------------------------------------------------------------
 constexpr int norm_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
 template <int TPR, int R> constexpr int norm_sm() { return TPR > 64 ? 2 * TPR / 64 * R : 1; }

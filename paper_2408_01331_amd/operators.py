@@ -6,10 +6,12 @@ which a context's step runs for its own layers and optimizers too).
 Argument checks and marshalling only; the work runs in the library's HIP
 kernels, on torch's current stream of the tensors' device. A call allocates its
 outputs and workspace from torch's allocator and does not wait for the device.
+Nothing is recorded for autograd: the backward passes are calls of their own.
 """
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 from torch._C import _cuda_getDevice as _current_device
@@ -106,6 +108,15 @@ def _rows(x):
     return v.shape[0], v.stride(0) if v.shape[0] > 1 else width, v
 
 
+@functools.lru_cache(maxsize=1024)
+def _norm_workspace(t, rows, width):
+    need = ctypes.c_size_t()
+    status = _lib().un_rms_norm_workspace(t, rows, width, _byref(need))
+    if status:
+        _un._check(status)
+    return need.value
+
+
 def _norm(x, weight, residual, eps, keep, e4m3):
     t, dev = _check_type(x, "x")
     shape, dtype = x.shape, x.dtype
@@ -121,8 +132,8 @@ def _norm(x, weight, residual, eps, keep, e4m3):
         _, ldr, rv = _rows(residual)
         s = _fresh(x, dtype)
         rp, sp = rv.data_ptr(), s.data_ptr()
-    rstd = _empty(shape[:-1], dtype=_F32, device=x.device) if keep else None
-    scale = _empty(shape[:-1], dtype=_F32, device=x.device) if e4m3 else None
+    rstd = x.new_empty(shape[:-1], dtype=_F32) if keep else None
+    scale = x.new_empty(shape[:-1], dtype=_F32) if e4m3 else None
     _call(_lib().un_rms_norm, _un.un_rms_norm_args(t, width, rows, float(eps), xv.data_ptr(), ldx, rp, ldr, weight.data_ptr(), sp, width,
                                                    y.data_ptr(), width, _ptr(rstd), _ptr(scale)), dev)
     return y, s, rstd, scale
@@ -162,18 +173,14 @@ def rms_norm_backward(dy, s, weight, rstd, ds=None):
         _, ldds, dsv = _rows(ds)
         dsp = dsv.data_ptr()
     dx = _fresh(s, dtype)
-    need = ctypes.c_size_t()
-    fns = _lib()
-    status = fns.un_rms_norm_workspace(t, rows, width, _byref(need))
-    if status:
-        _un._check(status)
+    need = _norm_workspace(t, rows, width)
     # one allocation: the weight gradient, then (256-byte aligned) the workspace
     at = -(-width // 64) * 64
-    buf = _empty(at + need.value // 4, dtype=_F32, device=s.device)
+    buf = s.new_empty(at + need // 4, dtype=_F32)
     p = buf.data_ptr()
-    _call(fns.un_rms_norm_backward, _un.un_rms_norm_grad_args(t, width, rows, dyv.data_ptr(), lddy, sv.data_ptr(), lds,
+    _call(_lib().un_rms_norm_backward, _un.un_rms_norm_grad_args(t, width, rows, dyv.data_ptr(), lddy, sv.data_ptr(), lds,
                                                               weight.data_ptr(), rstd.data_ptr(), dsp, ldds, dx.data_ptr(), width, p,
-                                                              p + 4 * at, need.value), dev)
+                                                              p + 4 * at, need), dev)
     return dx, buf[:width]
 
 
@@ -186,6 +193,7 @@ def _strides(x, shape):
     return st[1] if shape[1] > 1 else shape[2], st[0] if shape[0] > 1 else 0
 
 
+@functools.lru_cache(maxsize=1024)
 def _scan_sizes(batch, tokens, width):
     n, ws = ctypes.c_size_t(), ctypes.c_size_t()
     status = _lib().un_gated_scan_sizes(batch, tokens, width, _byref(n), _byref(ws))
@@ -220,18 +228,17 @@ def gated_scan(gate, value, h0=None, lens=None, keep=False, last=None):
     b, n, d = shape
     if h0 is not None:
         _flat(h0, "h0", (b, d), _F32, dev)
-    device = gate.device
     if last is None:
-        last = _empty((b, d), dtype=_F32, device=device)
+        last = gate.new_empty((b, d), dtype=_F32)
     else:
         _flat(last, "last", (b, d), _F32, dev)
-    h = _empty(shape, dtype=gate.dtype, device=device)
+    h = gate.new_empty(shape)
     states = ws = None
     n_ws = 0
     if n > 16 or keep:  # (a short call keeps no states and needs no workspace)
         n_states, n_ws = _scan_sizes(b, n, d)
-        states = _empty(n_states, dtype=_F32, device=device) if keep else None
-        ws = _empty(n_ws, dtype=torch.uint8, device=device) if n_ws else None
+        states = gate.new_empty(n_states, dtype=_F32) if keep else None
+        ws = gate.new_empty(n_ws, dtype=torch.uint8) if n_ws else None
     _call(_lib().un_gated_scan, _un.un_gated_scan_args(t, b, n, d, gate.data_ptr(), value.data_ptr(), ld, seq, _ptr(lens), _ptr(h0),
                                                        h.data_ptr(), d, n * d, last.data_ptr(), _ptr(states), _ptr(ws), n_ws), dev)
     return h, last, states
@@ -244,20 +251,20 @@ def gated_scan_backward(gate, value, states, dh, dlast=None, lens=None, out=None
     states: what it returned; dh: the gradient at h; dlast: at the last state."""
     t, dev, shape, (ld, seq) = _scan_inputs(gate, value, lens)
     b, n, d = shape
-    dtype, device = gate.dtype, gate.device
+    dtype = gate.dtype
     n_states, n_ws = _scan_sizes(b, n, d)
     _flat(states, "states", (n_states,), _F32, dev)
     _like(dh, "dh", shape, dtype, dev)
     if dlast is not None:
         _flat(dlast, "dlast", (b, d), _F32, dev)
     given = out is not None
-    dg, dv = out if given else _empty((2, b, n, d), dtype=dtype, device=device).unbind(0)
+    dg, dv = out if given else gate.new_empty((2, b, n, d)).unbind(0)
     _like(dg, "dgate", shape, dtype, dev)
     _like(dv, "dvalue", shape, dtype, dev)
     (ldo, seqo), (ldd, seqd) = _strides(dg, shape), _strides(dh, shape)
     _require((ldo, seqo) == _strides(dv, shape) or dg.numel() == 0, "dgate and dvalue must have the same strides")
-    dh0 = _empty((b, d), dtype=_F32, device=device)
-    ws = _empty(n_ws, dtype=torch.uint8, device=device) if n_ws else None
+    dh0 = gate.new_empty((b, d), dtype=_F32)
+    ws = gate.new_empty(n_ws, dtype=torch.uint8) if n_ws else None
     _call(_lib().un_gated_scan_backward, _un.un_gated_scan_grad_args(t, b, n, d, gate.data_ptr(), value.data_ptr(), ld, seq, _ptr(lens),
                                                                      states.data_ptr(), dh.data_ptr(), ldd, seqd, _ptr(dlast),
                                                                      dg.data_ptr(), dv.data_ptr(), ldo, seqo, dh0.data_ptr(), _ptr(ws),

@@ -35,9 +35,10 @@ def close(got, want, bound, what):
 # ---------------------------------------------------------------------------
 # RMS norm
 # ---------------------------------------------------------------------------
-# 1/rms: a thread adds up to 32 squares, 6 steps join a wave and up to 16 waves
-# follow; with the division, root and reciprocal halved and rounded: under 32 u
-# relative. The value itself: two products more.
+# 1/rms: a thread adds up to 16 squares, 6 steps join a wave and up to 16 waves
+# follow: 38 u of the sum, of which the root halves; with the division, the sum
+# with eps, the root and the reciprocal: under 32 u relative. The value itself:
+# two products more.
 NORM_U = 36 * U32
 
 
