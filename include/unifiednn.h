@@ -432,7 +432,7 @@ un_status un_profile_read(un_ctx* ctx, int32_t kernel_class, double* total_ms, i
  *     long as their outputs and workspaces differ. All may be captured into a
  *     HIP graph, except un_adamw_step.
  *   - Strides are in elements; the innermost stride is 1. Tensors need their
- *     element's alignment, no more.
+ *     element's alignment, no more (a workspace 8 bytes).
  *   - Errors are read with un_last_error(NULL) on the calling thread. A refused
  *     call enqueues nothing.
  * ------------------------------------------------------------------------- */
@@ -495,12 +495,12 @@ un_status un_rms_norm_workspace(int32_t type, int64_t rows, int32_t width, size_
  *   a_t = sigmoid(gate_t),  h_t = a_t h_{t-1} + (1 - a_t) value_t,  t = 1 .. tokens.
  * gate and value are [batch][tokens][width] with the same strides (the two halves
  * of one projection, say), width and token strides below 2^24; the state is fp32.
- * lens (device int32 [batch], NULL:
- * all of `tokens`): steps at and behind a sequence's length (clamped to [0,
- * tokens]) are skipped: their rows of gate and value are not used, their rows of
- * h are written as zeros, and the last state is the one before them. A single
- * token is a call with tokens = 1; last may be start itself.
- * states: for the backward pass, un_gated_scan_states floats. */
+ * lens (device int32 [batch], NULL: all of `tokens`): steps at and behind a
+ * sequence's length (clamped to [0, tokens]) are skipped: their rows of gate and
+ * value are not used, their rows of h are written as zeros, and the last state is
+ * the one before them. A single token is a call with tokens = 1; last may be start
+ * itself. h must not overlap the inputs. states (for the backward pass) and
+ * workspace: as un_gated_scan_sizes says. */
 typedef struct {
   int32_t type;              /* un_type of gate, value, h */
   int32_t batch, tokens, width;
@@ -539,8 +539,7 @@ typedef struct {
   size_t workspace_bytes;
 } un_gated_scan_grad_args;
 un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream);
-/* Floats of `states`, and bytes of the workspace of either call (may be 0; 8-byte
- * aligned). */
+/* Floats of `states`, and bytes of the workspace of either call (may be 0). */
 un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size_t* states, size_t* workspace_bytes);
 
 /* AdamW (decoupled weight decay) over many tensors in one launch. Per element,

@@ -2932,10 +2932,15 @@ static un_status set_state8(un_ctx* c, int i, bool on) {
       (void)hipGetLastError();
       return fail(c, UN_ERR_OOM, "8-bit optimizer state: hipMalloc of " + std::to_string(bytes) + " bytes failed");
     }
-    q = had ? had : fresh;
-  } else {
-    q = nullptr;
+    hipError_t e = hipMemsetAsync(had ? had : fresh, 0, bytes, c->stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(c->stream);
+    if (e != hipSuccess) {
+      if (fresh) hipFree(fresh);
+      HIPCHK(c, e);
+    }
+    if (had) return UN_OK;
   }
+  q = fresh;
   bool any = false;
   for (auto& o : c->opts) any = any || o.state8;
   un_ctx::Adamw8 next;
@@ -2960,11 +2965,7 @@ static un_status set_state8(un_ctx* c, int i, bool on) {
   }
   if (c->aw.mem) hipFree(c->aw.mem);
   c->aw = next;
-  if (!on) hipFree(had);
-  else {
-    HIPCHK(c, hipMemsetAsync(q, 0, bytes, c->stream));
-    HIPCHK(c, hipStreamSynchronize(c->stream));
-  }
+  if (had) hipFree(had);
   return UN_OK;
 }
 
@@ -3041,8 +3042,8 @@ un_status un_set_optimizer(un_ctx* c, int32_t i, const un_optimizer* o) {
     un_status st = alloc_state(c);
     if (st != UN_OK) return st;
   }
-  un_status st = clear_state(c, i);
-  if (st == UN_OK) st = set_state8(c, i, o->kind == UN_OPT_ADAMW8);
+  un_status st = set_state8(c, i, o->kind == UN_OPT_ADAMW8);  // (first: when it fails, the model keeps what it has)
+  if (st == UN_OK) st = clear_state(c, i);
   if (st != UN_OK) return st;
   un_ctx::Opt& d = c->opts[i];
   d.kind = o->kind;

@@ -246,9 +246,10 @@ def gated_scan(gate, value, h0=None, lens=None, keep=False, last=None):
 
 def gated_scan_backward(gate, value, states, dh, dlast=None, lens=None, out=None):
     """dh0, with the gradients at gate and value written to out = (dgate, dvalue)
-    (two tensors of gate's shape and equal strides, the halves of one buffer, say);
-    without `out`, (dgate, dvalue, dh0). gate, value, lens: as given to gated_scan;
-    states: what it returned; dh: the gradient at h; dlast: at the last state."""
+    (two tensors of gate's shape and equal strides that overlap no input, the
+    halves of one buffer, say); without `out`, (dgate, dvalue, dh0). gate, value,
+    lens: as given to gated_scan; states: what it returned; dh: the gradient at h;
+    dlast: at the last state."""
     t, dev, shape, (ld, seq) = _scan_inputs(gate, value, lens)
     b, n, d = shape
     dtype = gate.dtype

@@ -156,3 +156,36 @@ def test_python_checks():
         ops.AdamW([], [], [], [])
     with pytest.raises(ValueError, match="grads must hold 2"):
         ops.AdamW([w, w], [w], [w, w], [w, w])
+
+
+def test_8_bit_states_come_and_go(tmp_path):
+    """An 8-bit state and its table are given back when the optimizer changes, and when their clearing fails."""
+    import _host_hip as H
+    res = H.run("""
+spec = {"layers": [("linear", 16), ("relu",), ("linear", 3)], "num_classes": 3}
+h = U.Hybrid([spec, spec], 4, (8,), "bf16")
+h.set_optimizer(0, "adam")
+n = sum(int(np.prod(s)) for s in ((16, 8), (16,), (3, 16), (3,)))
+U.un_set_opt_state(h.ctx, 0, np.arange(2 * n, dtype=np.float32), 5)
+held = stub.stub_device()
+U.un_set_optimizer(h.ctx, 0, "adamw8")
+result = [stub.stub_device() - held]
+state, step = U.un_get_opt_state(h.ctx, 0)
+result.append([float(np.abs(state).max()), int(step)])
+U.un_set_opt_state(h.ctx, 0, np.arange(2 * n, dtype=np.float32), 5)
+U.un_set_optimizer(h.ctx, 0, "adamw8")
+result.append([float(np.abs(U.un_get_opt_state(h.ctx, 0)[0]).max()), stub.stub_device() - held])
+U.un_set_optimizer(h.ctx, 1, "adamw8")
+U.un_set_optimizer(h.ctx, 0, "sgd")
+U.un_set_optimizer(h.ctx, 1, "adam")
+result.append(stub.stub_device() - held)
+stub.stub_fail_memset(0)
+try:
+    U.un_set_optimizer(h.ctx, 0, "adamw8")
+except U.UnError as e:
+    result.append([e.status == U.UN_ERR_DEVICE, stub.stub_device() - held])
+stub.stub_fail_memset(-1)
+h.close()
+result.append(stub.stub_device())
+""", tmp_path)
+    assert res == [2, [0.0, 0], [0.0, 2], 0, [True, 0], 0]
