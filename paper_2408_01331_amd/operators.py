@@ -40,6 +40,10 @@ def _check_type(x, name):
     return t, dev
 
 
+def _dense(x, name):
+    _require(x.stride(-1) == 1 or x.shape[-1] <= 1, f"{name}'s last axis must be dense")
+
+
 def _like(x, name, shape, dtype, dev):
     """x is a tensor of this shape and type on GPU `dev`, its last axis dense. (One test for what fits; a call's latency counts.)"""
     if not (isinstance(x, torch.Tensor) and x.dtype is dtype and x.get_device() == dev and x.shape == shape
@@ -48,7 +52,7 @@ def _like(x, name, shape, dtype, dev):
         _require(x.get_device() == dev, f"{name} must be on cuda:{dev}, not {x.device}")
         _require(x.dtype is dtype, f"{name} must be {dtype}, not {x.dtype}")
         _require(x.shape == shape, f"{name} must have shape {tuple(shape)}, not {tuple(x.shape)}")
-        _require(False, f"{name}'s last axis must be dense")
+        _dense(x, name)
 
 
 def _flat(x, name, shape, dtype, dev):
@@ -122,7 +126,7 @@ def _norm(x, weight, residual, eps, keep, e4m3):
     shape, dtype = x.shape, x.dtype
     _require(len(shape) >= 1 and shape[-1] >= 1, "x needs a last axis of at least one value")
     width = shape[-1]
-    _like(x, "x", shape, dtype, dev)
+    _dense(x, "x")
     _flat(weight, "weight", (width,), _F32, dev)
     rows, ldx, xv = _rows(x)
     y = _fresh(x, torch.float8_e4m3fn if e4m3 else dtype)
@@ -161,7 +165,7 @@ def rms_norm_backward(dy, s, weight, rstd, ds=None):
     shape, dtype = s.shape, s.dtype
     _require(len(shape) >= 1 and shape[-1] >= 1, "s needs a last axis of at least one value")
     width = shape[-1]
-    _like(s, "s", shape, dtype, dev)
+    _dense(s, "s")
     _like(dy, "dy", shape, dtype, dev)
     _flat(weight, "weight", (width,), _F32, dev)
     _flat(rstd, "rstd", shape[:-1], _F32, dev)
@@ -206,7 +210,7 @@ def _scan_inputs(gate, value, lens):
     _require(isinstance(gate, torch.Tensor) and gate.dim() == 3, "gate must be a tensor [batch, tokens, width]")
     t, dev = _check_type(gate, "gate")
     shape = gate.shape
-    _like(gate, "gate", shape, gate.dtype, dev)
+    _dense(gate, "gate")
     _like(value, "value", shape, gate.dtype, dev)
     st = _strides(gate, shape)
     _require(st == _strides(value, shape) or gate.numel() == 0, "gate and value must have the same strides")
