@@ -557,8 +557,9 @@ __device__ __forceinline__ float2 take_over(const uint64_t* p, uint64_t v) {  //
 // Segment `o` in the order of the recurrence (backward: from the last): hands its
 // map on, and returns the value that arrives at it. Within a run of segments
 // (scan_run) every one takes the maps of those before it, each wave a part of them;
-// the last of a run hands on the value behind it, from which the next run starts. `maps`: those
-// of the workgroup's own waves (A and the part at SECOND of STRIDE floats per lane).
+// the last of a run hands on the value behind it, from which the next run starts.
+// `maps`: those of the workgroup's own waves (A and the part at SECOND of STRIDE
+// floats per lane). What is combined, and in which order, is fixed by `o` alone.
 template <int W, bool BWD, int RUN>
 __device__ __forceinline__ float join_run(const ScanProb& p, const Tile& t, int o, float h, const float* maps, float2* sm) {
   constexpr int STRIDE = BWD ? 4 : 2, SECOND = BWD ? 2 : 1, PER = RUN / W;
@@ -1175,11 +1176,11 @@ hipError_t launch_norm_dw(const float* part, int nparts, int d, float* dw, hipSt
 // the value that arrives is put together (join), so that every operand is still read
 // once. A segment is as long as the registers allow (8 waves x 32 steps forward, x 16
 // backward: two workgroups per CU) where that gives two workgroups per CU, else 8 x 8.
-// Forward / backward in us, against two launches of which the first composed the
-// segments' maps: 2 x 16384 x 1024 in bf16 43 / 88, so 62 / 103; 1 x 65536 x 512 51 /
-// 101, so 60 / 96; 4 x 4096 x 1024 25 / 39, so 32 / 42; 8 x 2048 x 1024 in fp32 38 /
-// 75, so 50 / 83. Segments of 8 x 8 steps throughout: 1 x 65536 x 512 backward 128;
-// workgroups of 4 waves 81 / 154; of 16 53 / 117.
+// Forward / backward in us, two launches of which the first composed the segments'
+// maps, so this one, operands not in the caches: 2 x 16384 x 1024 in bf16 75 / 112, so
+// 50 / 82; 1 x 65536 x 512 77 / 106, so 55 / 89; 4 x 4096 x 1024 37 / 60, so 28 / 47; 8
+// x 2048 x 1024 in fp32 60 / 94, so 49 / 68. Workgroups of 4 waves: 1 x 65536 x 512 70 /
+// 130; of 16 waves x 8 steps, or segments of 8 x 8 throughout, a quarter more backward.
 // Between 256 and 512 workgroups a CU has one: chunks of 8 x 16 steps, one prepared
 // while another is finished, take the place of the second (16 x 2048 x 1024 with
 // chunks of 8 x 8 / 8 x 16: forward 42 / 38 us, backward 83 / 76). Above, two or more
