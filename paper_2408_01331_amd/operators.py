@@ -22,7 +22,7 @@ from .unifiednn import UnError  # noqa: F401  (raised by every call here)
 
 _F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
 _TYPES = {_F32: 0, _BF16: 1}
-_byref, _empty, _empty_like = ctypes.byref, torch.empty, torch.empty_like
+_byref, _empty_like = ctypes.byref, torch.empty_like
 
 
 def _require(ok, what):
@@ -65,24 +65,15 @@ def _ptr(x):
     return None if x is None else x.data_ptr()
 
 
-def _fresh(x, dtype):
-    """A new dense tensor of x's shape."""
-    return _empty_like(x, dtype=dtype) if x.is_contiguous() else _empty(x.shape, dtype=dtype, device=x.device)
-
-
-def _launch(fn, dev, *args):
+def _call(fn, args, dev, plan=None):
     """fn on torch's current stream of GPU `dev`. (The default stream has no device of its own: it is the current one's.)"""
-    if _current_device() == dev:
-        status = fn(*args, _current_stream(dev))
-    else:
+    if _current_device() != dev:
         with torch.cuda.device(dev):
-            status = fn(*args, _current_stream(dev))
+            return _call(fn, args, dev, plan)
+    stream = _current_stream(dev)
+    status = fn(_byref(args), stream) if plan is None else fn(plan, _byref(args), stream)
     if status:
         _un._check(status)
-
-
-def _call(fn, args, dev):
-    _launch(fn, dev, _byref(args))
 
 
 _fns = None
@@ -98,18 +89,36 @@ def _lib():
 # ---------------------------------------------------------------------------
 # RMS norm
 # ---------------------------------------------------------------------------
-def _rows(x):
+def _rows(x, name):
     """x as rows: (rows, row stride, x to pass on). A tensor whose leading axes do not have one stride is copied."""
     shape = x.shape
+    _require(len(shape) >= 1 and shape[-1] >= 1, f"{name} needs a last axis of at least one value")
     width = shape[-1]
+    if x.is_contiguous():
+        return x.numel() // width, width, x
+    _dense(x, name)
     if len(shape) == 2:
         rows = shape[0]
         return rows, x.stride(0) if rows > 1 else width, x
     try:
-        v = x.view(-1, width) if len(shape) > 1 else x.unsqueeze(0)
+        v = x.view(-1, width)
     except RuntimeError:
         v = x.reshape(-1, width)
     return v.shape[0], v.stride(0) if v.shape[0] > 1 else width, v
+
+
+def _operand(x, name, shape, dtype, dev):
+    """(address, row stride, x to pass on) of another tensor of the same shape and type."""
+    if isinstance(x, torch.Tensor) and x.dtype is dtype and x.get_device() == dev and x.shape == shape and x.is_contiguous():
+        return x.data_ptr(), shape[-1], x
+    _like(x, name, shape, dtype, dev)
+    _, ld, v = _rows(x, name)
+    return v.data_ptr(), ld, v
+
+
+def _fresh(x, dtype):
+    """A new dense tensor of x's shape."""
+    return _empty_like(x, dtype=dtype) if x.is_contiguous() else x.new_empty(x.shape, dtype=dtype)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -123,21 +132,18 @@ def _norm_workspace(t, rows, width):
 
 def _norm(x, weight, residual, eps, keep, e4m3):
     t, dev = _check_type(x, "x")
+    rows, ldx, xv = _rows(x, "x")
     shape, dtype = x.shape, x.dtype
-    _require(len(shape) >= 1 and shape[-1] >= 1, "x needs a last axis of at least one value")
     width = shape[-1]
-    _dense(x, "x")
     _flat(weight, "weight", (width,), _F32, dev)
-    rows, ldx, xv = _rows(x)
     y = _fresh(x, torch.float8_e4m3fn if e4m3 else dtype)
-    ldr, rp, sp, s = 0, None, None, x
+    rp, ldr, rv, sp, s = None, 0, None, None, x
     if residual is not None:
-        _like(residual, "residual", shape, dtype, dev)
-        _, ldr, rv = _rows(residual)
+        rp, ldr, rv = _operand(residual, "residual", shape, dtype, dev)
         s = _fresh(x, dtype)
-        rp, sp = rv.data_ptr(), s.data_ptr()
-    rstd = x.new_empty(shape[:-1], dtype=_F32) if keep else None
-    scale = x.new_empty(shape[:-1], dtype=_F32) if e4m3 else None
+        sp = s.data_ptr()
+    rstd = weight.new_empty(shape[:-1]) if keep else None
+    scale = weight.new_empty(shape[:-1]) if e4m3 else None
     _call(_lib().un_rms_norm, _un.un_rms_norm_args(t, width, rows, float(eps), xv.data_ptr(), ldx, rp, ldr, weight.data_ptr(), sp, width,
                                                    y.data_ptr(), width, _ptr(rstd), _ptr(scale)), dev)
     return y, s, rstd, scale
@@ -162,30 +168,20 @@ def rms_norm_backward(dy, s, weight, rstd, ds=None):
     """(dx, dweight) of rms_norm from the gradient dy at y, and ds at s (None: s
     is used by nothing else). dx is the gradient at x and at the residual."""
     t, dev = _check_type(s, "s")
+    rows, lds, sv = _rows(s, "s")
     shape, dtype = s.shape, s.dtype
-    _require(len(shape) >= 1 and shape[-1] >= 1, "s needs a last axis of at least one value")
     width = shape[-1]
-    _dense(s, "s")
-    _like(dy, "dy", shape, dtype, dev)
+    dyp, lddy, dyv = _operand(dy, "dy", shape, dtype, dev)
     _flat(weight, "weight", (width,), _F32, dev)
     _flat(rstd, "rstd", shape[:-1], _F32, dev)
-    rows, lds, sv = _rows(s)
-    _, lddy, dyv = _rows(dy)
-    ldds, dsp = 0, None
-    if ds is not None:
-        _like(ds, "ds", shape, dtype, dev)
-        _, ldds, dsv = _rows(ds)
-        dsp = dsv.data_ptr()
-    dx = _fresh(s, dtype)
+    dsp, ldds, dsv = (None, 0, None) if ds is None else _operand(ds, "ds", shape, dtype, dev)
+    dx, dw = _fresh(s, dtype), _empty_like(weight)
     need = _norm_workspace(t, rows, width)
-    # one allocation: the weight gradient, then (256-byte aligned) the workspace
-    at = -(-width // 64) * 64
-    buf = s.new_empty(at + need // 4, dtype=_F32)
-    p = buf.data_ptr()
-    _call(_lib().un_rms_norm_backward, _un.un_rms_norm_grad_args(t, width, rows, dyv.data_ptr(), lddy, sv.data_ptr(), lds,
-                                                              weight.data_ptr(), rstd.data_ptr(), dsp, ldds, dx.data_ptr(), width, p,
-                                                              p + 4 * at, need), dev)
-    return dx, buf[:width]
+    ws = weight.new_empty(need // 4)
+    _call(_lib().un_rms_norm_backward, _un.un_rms_norm_grad_args(t, width, rows, dyp, lddy, sv.data_ptr(), lds, weight.data_ptr(),
+                                                                 rstd.data_ptr(), dsp, ldds, dx.data_ptr(), width, dw.data_ptr(),
+                                                                 ws.data_ptr(), need), dev)
+    return dx, dw
 
 
 # ---------------------------------------------------------------------------
@@ -209,11 +205,13 @@ def _scan_sizes(batch, tokens, width):
 def _scan_inputs(gate, value, lens):
     _require(isinstance(gate, torch.Tensor) and gate.dim() == 3, "gate must be a tensor [batch, tokens, width]")
     t, dev = _check_type(gate, "gate")
-    shape = gate.shape
-    _dense(gate, "gate")
-    _like(value, "value", shape, gate.dtype, dev)
+    shape, stride = gate.shape, gate.stride()
+    if not (isinstance(value, torch.Tensor) and value.dtype is gate.dtype and value.get_device() == dev and value.shape == shape
+            and value.stride() == stride and stride[2] == 1):
+        _dense(gate, "gate")
+        _like(value, "value", shape, gate.dtype, dev)
+        _require(_strides(gate, shape) == _strides(value, shape) or gate.numel() == 0, "gate and value must have the same strides")
     st = _strides(gate, shape)
-    _require(st == _strides(value, shape) or gate.numel() == 0, "gate and value must have the same strides")
     if lens is not None:
         _flat(lens, "lens", shape[:1], _I32, dev)
     return t, dev, shape, st
@@ -233,7 +231,7 @@ def gated_scan(gate, value, h0=None, lens=None, keep=False, last=None):
     if h0 is not None:
         _flat(h0, "h0", (b, d), _F32, dev)
     if last is None:
-        last = gate.new_empty((b, d), dtype=_F32)
+        last = gate.new_empty((b, d), dtype=_F32) if h0 is None else _empty_like(h0)
     else:
         _flat(last, "last", (b, d), _F32, dev)
     h = gate.new_empty(shape)
@@ -353,7 +351,7 @@ class AdamW:
     def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, key=0):
         """Step number `step` (from 1). key: with 8-bit states, another whole number each step."""
         h = _un.un_adamw_hyper(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step), int(key) & 0xFFFFFFFF)
-        _launch(_lib().un_adamw_step, self._index, self._plan, _byref(h))
+        _call(_lib().un_adamw_step, h, self._index, self._plan)
 
     def close(self):
         if self._plan:
