@@ -862,7 +862,9 @@ __global__ __launch_bounds__(64 * W) void scan_kernel(ScanProb p) {
 // it starts, so the segments that it waits for belong to workgroups that have
 // started, and the first of these waits for none: every wait ends. (Rows loaded
 // meanwhile for the place that the workgroup's number suggests were too often the
-// wrong ones: the forward pass of 2 x 16384 x 1024 in bf16 took 51 us, so 43.)
+// wrong ones: the forward pass of 2 x 16384 x 1024 in bf16 took 51 us, so 43. As many
+// workgroups as run at once, each with its next segment's rows in flight while it
+// joins, took 64: what it waits for returns behind those rows.)
 template <typename T, int W, int L, bool BWD, bool ONCE>
 __global__ __launch_bounds__(64 * W) void scan_split_kernel(ScanProb p) {
   __shared__ __attribute__((aligned(16))) float sm[W * (BWD ? 4 : 2) * 64 + (W + 1) * 2 * 64];
