@@ -3,7 +3,6 @@
 // before every check has passed.
 #include <hip/hip_runtime.h>
 
-#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -345,7 +344,6 @@ un_status un_adamw_step(un_adamw* a, const un_adamw_hyper* h, void* stream) {
   hp.c2 = (float)(1.0 - h->beta2);
   hp.isb2 = (float)(1.0 / std::sqrt(1.0 - std::pow(h->beta2, t)));
   hp.eps = (float)h->eps;
-  if (a->eight) hp.eps = std::fmax(hp.eps, FLT_MIN);  // its reciprocal takes a subnormal one for 0
   e = launch_adamw(a->g16, a->eight, (const AdamwTensor*)a->table, (const int32_t*)(a->table + a->map_at), a->nblocks, a->bytes, hp, nullptr,
                    (hipStream_t)stream);
   return e == hipSuccess ? UN_OK : device_error(F, e);

@@ -1028,13 +1028,11 @@ __global__ __launch_bounds__(256) void adamw_kernel(const AdamwTensor* __restric
     nm[e] = fmaf(hp.b1, nm[e], hp.c1 * x);
     nv[e] = fmaf(hp.b2, nv[e], hp.c2 * x * x);
     const float kept = fmaf(-hp.decay, p[e], p[e]);
-    if constexpr (EIGHT) {
-      // to 1 ulp: the step is bound by its arithmetic, and neither the update nor a code shows the difference
-      rt[e] = __builtin_amdgcn_sqrtf(nv[e]);
-      w[e] = fmaf(-hp.lr * nm[e], __builtin_amdgcn_rcpf(fmaf(rt[e], hp.isb2, hp.eps)), kept);
-    } else {
-      w[e] = kept - hp.lr * (nm[e] / (sqrtf(nv[e]) * hp.isb2 + hp.eps));
-    }
+    // the nearest root and quotient with 8-bit states, too: the weights are the same bits as with fp32 states, and a
+    // code next to a border is the one of the moment. (By the instructions' root and reciprocal, to 1 ulp: 6 M
+    // parameters 20.8 us, were 20.3; 200 M 544, were 509.)
+    rt[e] = sqrtf(nv[e]);
+    w[e] = kept - hp.lr * (nm[e] / (rt[e] * hp.isb2 + hp.eps));
   }
   uint32_t cm = 0, cv = 0;
   if constexpr (EIGHT) {

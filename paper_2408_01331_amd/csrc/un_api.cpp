@@ -19,7 +19,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -2726,7 +2725,7 @@ static un_status step_common(un_ctx* c, float lr, const float* lrs, float* losse
         const float decay = (float)(rate * o.decay);
         h.kind = o.kind != UN_OPT_ADAM && decay > 0.f ? -decay : (float)UN_OPT_ADAM;
         if (o.kind == UN_OPT_ADAMW8) {
-          hp8[i] = AdamwHp{decay, h.lr, h.b1, h.b2, h.c1, h.c2, h.isb2, std::fmax(h.eps, FLT_MIN), (uint32_t)(o.t + 1) * 0x01000193u + 0x5EEDu};
+          hp8[i] = AdamwHp{decay, h.lr, h.b1, h.b2, h.c1, h.c2, h.isb2, h.eps, (uint32_t)(o.t + 1) * 0x01000193u + 0x5EEDu};
           h = OptHp{};  // the backward pass leaves its weights (SGD at rate 0)
         }
       }

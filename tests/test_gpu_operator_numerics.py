@@ -1,0 +1,109 @@
+"""GPU tests of the operators at values next to a rounding border, at gates whose
+exponential overflows, and of what the torch calls tell autograd."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import _operator_refs as R  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+DTYPES = [F32, BF16]
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2408_01331_amd import operators
+    return operators
+
+
+def rand(seed, shape, dtype=F32, mean=0.0, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std + mean).to(dtype).cuda()
+
+
+# ---------------------------------------------------------------------------
+# AdamW with 8-bit states
+# ---------------------------------------------------------------------------
+BETAS = (0.9, 0.99)
+C1, C2 = np.float32(1 - BETAS[0]), np.float32(1 - BETAS[1])
+
+
+def random_bits(i, key):
+    """The numbers of the stochastic rounding: 32 bits of an element's number and the step's key."""
+    low = np.uint64(0xFFFFFFFF)
+    x = (i.astype(np.uint64) * np.uint64(0x9E3779B9) + np.uint64(key)) & low
+    x ^= x >> np.uint64(16)
+    x = (x * np.uint64(0x6A09E667)) & low
+    x ^= x >> np.uint64(15)
+    x = (x * np.uint64(0xBB67AE85)) & low
+    return (x ^ (x >> np.uint64(16))).astype(np.uint32)
+
+
+def codes_of(x, e, r):
+    """fp32 values on e4m3 codes of scale 2^e: up where the 16-bit numbers r pass the way to the code below."""
+    v = np.ldexp(x, -e).astype(np.float32)
+    mag, sign = np.abs(v), (np.signbit(v).astype(np.uint32) << 7)
+    bits = mag.view(np.uint32)
+    normal = ((bits + (r.astype(np.uint32) << 4)) >> 20) - np.uint32(960)
+    small = ((np.minimum(mag, np.float32(2.0 ** -6)) * np.float32(2.0 ** 25)).astype(np.uint32) + r) >> 16
+    return (np.where(mag < 2.0 ** -6, small, normal) | sign).astype(np.uint8)
+
+
+def borders(n, key):
+    """Gradients whose second moment's root (from zero moments) lies on the border between two codes, as the element's random
+    number draws it, or one step of fp32 below: the code shows whether the root is the nearest fp32 value."""
+    rng = np.random.default_rng(7)
+    i = np.arange(n)
+    r = random_bits(i, key) >> 16
+    # a root in [1/2, 1) whose low 20 bits carry into the code's with (r << 4), or just do not
+    low = ((1 << 20) - (r.astype(np.int64) << 4)) & 0xFFFFF
+    want = ((126 << 23) + (rng.integers(0, 8, n) << 20) + low - rng.integers(0, 2, n)).astype(np.uint32).view(np.float32)
+    x = (want.astype(np.float64) / math.sqrt(C2)).astype(np.float32)
+    for _ in range(8):  # a few steps of fp32 around: take one that hits, where there is one
+        root = np.sqrt((C2 * x) * x)
+        x = np.where(root < want, np.nextafter(x, np.float32(np.inf)), np.where(root > want, np.nextafter(x, np.float32(0)), x))
+    x[::256] = 12.0  # the block's largest: a root of 1.2, a scale of 2^-8
+    return x
+
+
+def test_adamw8_codes_at_borders(ops):
+    """Codes and scales are those of the moments in fp32 arithmetic, each operation rounded to the nearest: equal bits."""
+    n, key = 1 << 18, 99
+    x = borders(n, key)
+    root = np.sqrt((C2 * x) * x)
+    p, g = [torch.zeros(n, device="cuda")], [torch.tensor(x, device="cuda")]
+    m, v, ms, vs = ops.AdamW.state8(p)
+    ops.AdamW(p, g, m, v, m_scales=ms, v_scales=vs).step(0.01, 1, betas=BETAS, key=key)
+    r = random_bits(np.arange(n), key)
+    assert (vs[0].view(torch.uint8).cpu().numpy() == 127 - 8).all()
+    got = v[0].view(torch.uint8).cpu().numpy()
+    want = codes_of(root, -8, r >> 16)
+    assert (got != want).sum() == 0, f"{(got != want).sum()} of {n} codes of the root differ"
+    # the first moment: its largest value is 1.2, too
+    assert (ms[0].view(torch.uint8).cpu().numpy() == 127 - 8).all()
+    assert (m[0].view(torch.uint8).cpu().numpy() == codes_of(C1 * x, -8, r & 0xFFFF)).all()
+
+
+@pytest.mark.parametrize("gtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("scale,eps", [(1.0, 1e-8), (1e-12, 1e-20), (1e-19, 1e-30), (1e-20, 1e-38)])
+def test_adamw8_weights_are_those_of_32_bits(ops, gtype, scale, eps):
+    """From fresh states a step's new weights do not depend on how the states are kept: the same bits, also where the second
+    moment is subnormal (1e-20 squared and weighted: 1e-42) and where eps is."""
+    n = 100_003
+    start, g = rand(1, (n,), std=0.05), [rand(2, (n,)).mul(scale).to(gtype)]
+    new = []
+    for eight in (False, True):
+        p, c = [start.clone()], [torch.zeros(n, device="cuda", dtype=BF16)]
+        if eight:
+            m, v, ms, vs = ops.AdamW.state8(p)
+            opt = ops.AdamW(p, g, m, v, copies=c, m_scales=ms, v_scales=vs)
+        else:
+            opt = ops.AdamW(p, g, [torch.zeros(n, device="cuda")], [torch.zeros(n, device="cuda")], copies=c)
+        opt.step(0.01, 3, betas=BETAS, eps=eps, weight_decay=0.1)
+        new.append((p[0], c[0]))
+    for a, b in zip(*new):
+        assert torch.equal(a, b), f"{(a != b).sum().item()} of {n} differ"
