@@ -468,15 +468,17 @@ __device__ __forceinline__ float value_of(bf16_t v) { return bf2f(v); }
 __device__ __forceinline__ float value_of(float v) { return v; }
 
 // a = sigmoid(g) and k = 1 - a, each to its own relative accuracy: with e =
-// exp(-g), a = 1 / (1 + e), and k = e a where e < 1, else 1 - a (an infinite e
-// gives 0 and 1, a NaN stays one). fp32: e with the rounding error of its
-// argument, so that it is as exact for large |g|.
+// exp(-g), a = 1 / (1 + e), and k = e a where e < 1, else 1 - a (an infinite e, of a
+// g below -88.72, gives 0 and 1, a NaN stays one). fp32: e with the rounding error of
+// its argument, so that it is as exact for large |g|; from +-88 on, where e or 1 / e
+// is below 2^-126 and may be infinite or 0 by now, it is left as it is (infinity plus
+// infinity times an error of either sign would be NaN).
 template <typename T> __device__ __forceinline__ void gate_of(T raw, float& a, float& k) {
   const float g = value_of(raw), L2E = -1.44269504f, t = g * L2E;
   float e = __builtin_amdgcn_exp2f(t);
   if constexpr (sizeof(T) == 4) {
     const float r = fmaf(g, -1.925963033e-8f, fmaf(g, L2E, -t)) * 0.693147181f;
-    e = fabsf(g) < 128.f ? fmaf(e, r, e) : e;  // (an infinite g has no rounding error)
+    e = fabsf(g) < 88.f ? fmaf(e, r, e) : e;
   }
   a = __builtin_amdgcn_rcpf(1.f + e);
   k = e < 1.f ? e * a : 1.f - a;

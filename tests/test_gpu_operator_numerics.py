@@ -107,3 +107,71 @@ def test_adamw8_weights_are_those_of_32_bits(ops, gtype, scale, eps):
         new.append((p[0], c[0]))
     for a, b in zip(*new):
         assert torch.equal(a, b), f"{(a != b).sum().item()} of {n} differ"
+
+
+# ---------------------------------------------------------------------------
+# Gates whose exponential overflows
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 3, 40])
+def test_scan_gates_over_the_whole_range(ops, dtype, n):
+    """Gates from -140 to 140, among them those below -88.7, where exp(-gate) is infinite in fp32: a reset, forward and back."""
+    w = 8001
+    gate = torch.linspace(-140, 140, w)[None, None].repeat(1, n, 1).to(dtype).cuda()
+    value, dh, h0 = rand(1, (1, n, w), dtype), rand(2, (1, n, w), dtype), rand(3, (1, w))
+    h, last, states = ops.gated_scan(gate, value, h0=h0, keep=True)
+    grads = ops.gated_scan_backward(gate, value, states, dh)
+    for x in (h, last, *grads):
+        assert torch.isfinite(x).all(), f"{(~torch.isfinite(x)).sum().item()} of {x.numel()} are not finite"
+    # bf16 gates: the exponential's argument t = g log2(e) has the constant's rounding (0.22 u) and the product's (1 u), so e is
+    # off by 1.22 u |g|, 171 u at 140, beside the 32 u of a step that the bounds count (which hold such arguments to |g| = 8)
+    wide = 1 if dtype == F32 else 1 + 171 / 32
+    half = lambda want, bound: wide * bound + (R.half_step(dtype) * (want.abs() + wide * bound) if dtype != F32 else 0)  # noqa: E731
+    wh, bh, wl, bl = R.scan_fwd(gate, value, h0, None)
+    R.close(h, wh, half(wh, bh) + R.TINY, "h")
+    R.close(last, wl, wide * bl + R.TINY, "last")
+    (wg, bg), (wv, bv), (w0, b0) = R.scan_bwd(gate, value, h0, None, dh, None)
+    for got, want, bound, what in ((grads[0], wg, half(wg, bg), "dgate"), (grads[1], wv, half(wv, bv), "dvalue"),
+                                   (grads[2], w0, wide * b0, "dh0")):
+        R.close(got, want, bound + R.TINY, what)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("b,n,w", [(1, 3000, 70), (40, 300, 700), (300, 140, 130)], ids=["split", "long chunks", "chunks"])
+def test_scan_resets_by_large_gates(ops, dtype, b, n, w):
+    """Large negative gates amid ordinary ones, where the axis is split and where it is not, forward and back."""
+    gate, value, dh = rand(1, (b, n, w), dtype, mean=2.0).clamp(-8, 8), rand(2, (b, n, w), dtype), rand(3, (b, n, w), dtype)
+    at = torch.arange(5, n, 37)
+    gate[:, at] = -torch.linspace(88, 128, len(at), device="cuda").to(dtype)[None, :, None]
+    h, last, states = ops.gated_scan(gate, value, keep=True)
+    grads = ops.gated_scan_backward(gate, value, states, dh)
+    for x in (h, last, *grads):
+        assert torch.isfinite(x).all()
+    assert torch.equal(h[:, at], value[:, at])
+    few = [x[:2, :, :8].contiguous() for x in (gate, value, dh)]
+    half = lambda want, bound: bound + (R.half_step(dtype) * (want.abs() + bound) if dtype != F32 else 0)  # noqa: E731
+    wh, bh, _, _ = R.scan_fwd(few[0], few[1], None, None)
+    R.close(h[:2, :, :8], wh, half(wh, bh), "h")
+    (wg, bg), (wv, bv), _ = R.scan_bwd(few[0], few[1], None, None, few[2], None)
+    R.close(grads[0][:2, :, :8], wg, half(wg, bg) + R.TINY, "dgate")
+    R.close(grads[1][:2, :, :8], wv, half(wv, bv) + R.TINY, "dvalue")
+
+
+def test_step_with_large_gates():
+    """A context's fp32 recurrence whose gates are near -100 everywhere: h is the value, and the loss is the oracle's."""
+    import oracle
+    from paper_2408_01331_amd import workloads as W
+    from paper_2408_01331_amd.unifiednn import Hybrid, flatten_params
+    spec = {"layers": [("unflatten", 24), ("recurrence",), ("flatten",), ("linear", 10)], "num_classes": 10}
+    wl = W.Workload("gates", 1, 16, (192,), "f32", [spec], 0.05, 1, 3, init="torch")
+    params = W.init_params(spec, wl.in_shape, 3, 0, "torch")
+    params[1][:8] = -np.linspace(92, 125, 8)
+    x, y = W.make_batch(wl, 0)
+    with np.errstate(over="ignore"):
+        want, _ = oracle.softmax_ce(oracle.forward(spec, params, x, "f32")[0], y)
+    with Hybrid([spec], 16, (192,), "f32") as h:
+        h.set_params(0, flatten_params(params))
+        h.load_batch(x, y)
+        loss = h.step(0.05)
+        assert np.isfinite(loss).all() and np.isfinite(h.get_params(0)).all()
+        assert abs(loss[0] - want) <= 1e-4 * abs(want)
