@@ -110,6 +110,36 @@ def test_adamw8_weights_are_those_of_32_bits(ops, gtype, scale, eps):
 
 
 # ---------------------------------------------------------------------------
+# RMS norm in e4m3
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+def test_norm_e4m3_codes_at_borders(ops, dtype):
+    """Rows of ones without eps, whose output is the weight itself: the codes are the nearest to weight / scale in fp32, also
+    where that lies next to the middle between two codes."""
+    grid = torch.arange(0, 127, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    mid = (grid[1:] + grid[:-1]) / 2
+    rng = np.random.default_rng(1)
+    wrong = total = 0
+    for k in range(40):
+        top = np.float32(rng.uniform(1, 2) * 2.0 ** rng.integers(-3, 4))
+        scale = top / np.float32(448)
+        w = (mid.numpy() * scale).astype(np.float32)
+        near = [w]
+        for _ in range(3):
+            near = [np.nextafter(near[0], np.float32(0)), *near, np.nextafter(near[-1], np.float32(np.inf))]
+        w = np.concatenate([[top], *near]).astype(np.float32) * rng.choice([-1, 1], 1 + 7 * mid.numel()).astype(np.float32)
+        w = np.clip(w, -top, top)
+        want = torch.tensor(w / scale).clamp(-448, 448).to(torch.float8_e4m3fn)
+        x = torch.ones(2, w.size, dtype=dtype, device="cuda")
+        q, got, _ = ops.rms_norm_e4m3(x, torch.tensor(w, device="cuda"), eps=0.0)
+        assert (got.cpu().numpy() == scale).all()
+        for row in q.cpu():
+            wrong += (row.float() != want.float()).sum().item()
+            total += w.size
+    assert wrong == 0, f"{wrong} of {total} codes differ"
+
+
+# ---------------------------------------------------------------------------
 # Gates whose exponential overflows
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
