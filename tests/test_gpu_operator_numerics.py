@@ -109,6 +109,40 @@ def test_adamw8_weights_are_those_of_32_bits(ops, gtype, scale, eps):
         assert torch.equal(a, b), f"{(a != b).sum().item()} of {n} differ"
 
 
+def test_adamw8_without_keys_rounds_without_bias(ops):
+    """A loop that passes no key draws anew each step: over many steps the mean of a stored moment is the moment. (Bounds: a
+    draw is one of two codes a step apart; 5 standard deviations of the mean of n draws are 2.5 steps / sqrt(n).)"""
+    n, draws = 1024, 400
+    g = rand(3, (n,))
+    sums = torch.zeros(2, n, dtype=torch.float64)
+    for k in range(draws):
+        p = [torch.zeros(n, device="cuda")]
+        m, v, ms, vs = ops.AdamW.state8(p)
+        ops.AdamW(p, [g], m, v, m_scales=ms, v_scales=vs).step(0.0, k + 1, betas=BETAS)
+        sums[0] += R.widen(m[0], ms[0])
+        sums[1] += R.widen(v[0], vs[0])
+    _, wm, wv, _ = R.adamw(p[0], g, p[0], p[0], 0.0, BETAS, 1e-8, 0.01, 1)
+    for mean, x, sc in ((sums[0] / draws, wm, ms[0]), (sums[1] / draws, wv.sqrt(), vs[0])):
+        scale = torch.repeat_interleave(torch.pow(2.0, sc.cpu().view(torch.uint8).double() - 127), 256)
+        step = torch.maximum(torch.pow(2.0, torch.floor(torch.log2(x.abs().clamp_min(1e-300))) - 3), scale * 2.0 ** -9)
+        off = (mean - x).abs() / step
+        floor = x.abs() < scale * 2.0 ** -9  # (the smallest code stands for everything below it in sqrt(v))
+        assert (off[~floor] <= 2.5 / math.sqrt(draws) + 1e-4).all(), off[~floor].max()
+
+
+def test_adamw8_key_of_its_own(ops):
+    """A key that is given is the key, zero among them: the same bits at any step's number."""
+    res = []
+    for key, step in ((0, 1), (0, 2), (7, 1), (None, 1), (None, 2), (None, 1)):
+        p, g = [rand(1, (5000,))], [rand(2, (5000,))]
+        m, v, ms, vs = ops.AdamW.state8(p)
+        ops.AdamW(p, g, m, v, m_scales=ms, v_scales=vs).step(0.01, step, key=key)
+        res.append(torch.cat([x.view(torch.uint8) for x in m + v]))
+    assert torch.equal(res[0], res[1]) and torch.equal(res[3], res[5])
+    for a, b in ((0, 2), (0, 3), (3, 4)):
+        assert (res[a] != res[b]).float().mean() > 0.2
+
+
 # ---------------------------------------------------------------------------
 # RMS norm in e4m3
 # ---------------------------------------------------------------------------
