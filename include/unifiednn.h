@@ -539,7 +539,9 @@ typedef struct {
   size_t workspace_bytes;
 } un_gated_scan_grad_args;
 un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream);
-/* Floats of `states`, and bytes of the workspace of either call (may be 0). */
+/* Floats of `states`, and bytes of the workspace of either call (may be 0). Sizes that
+ * no call takes are refused: more than 2^30 tokens, widths of 2^24 or more, more
+ * workgroups than a launch holds (UN_ERR_UNSUPPORTED). */
 un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size_t* states, size_t* workspace_bytes);
 
 /* AdamW (decoupled weight decay) over many tensors in one launch. Per element,

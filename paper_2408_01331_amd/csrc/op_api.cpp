@@ -144,12 +144,27 @@ un_status un_rms_norm_backward(const un_rms_norm_grad_args* a, void* stream) {
 // ---------------------------------------------------------------------------
 // Gated linear recurrence
 // ---------------------------------------------------------------------------
+namespace {
+// sizes that a direction's launch plan and the kernels can count; that plan
+un_status scan_sizes_ok(const char* F, int32_t B, int32_t T, int32_t d, bool bwd, ScanPlan* plan) {
+  if (B < 0 || T < 0 || d < 0) return bad(F, "negative size");
+  if (T > (1 << 30)) return bad(F, "more than 2^30 tokens are not supported", UN_ERR_UNSUPPORTED);
+  if (d > SCAN_MAX_LD) return bad(F, "a width of 2^24 or more is not supported", UN_ERR_UNSUPPORTED);
+  *plan = scan_plan(B, T, d, bwd);
+  if (too_many((int64_t)plan->tiles * B * plan->nseg, plan->kind >= SCAN_CHUNKS ? 64 * SCAN_W : 64))
+    return bad(F, "too many sequences and channels", UN_ERR_UNSUPPORTED);
+  return UN_OK;
+}
+}  // namespace
+
 un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size_t* states, size_t* workspace_bytes) {
   const char* F = "un_gated_scan_sizes";
-  if (batch < 0 || tokens < 0 || width < 0) return bad(F, "negative size");
+  ScanPlan fwd;  // (the backward pass has no fewer workgroups)
+  const un_status st = scan_sizes_ok(F, batch, tokens, width, false, &fwd);
+  if (st != UN_OK) return st;
   if (states) *states = (size_t)batch * scan_chunks(tokens) * width;
   if (workspace_bytes)
-    *workspace_bytes = 8 * (size_t)std::max(scan_ws_words(scan_plan(batch, tokens, width, false), batch, width),
+    *workspace_bytes = 8 * (size_t)std::max(scan_ws_words(fwd, batch, width),
                                             scan_ws_words(scan_plan(batch, tokens, width, true), batch, width));
   return UN_OK;
 }
@@ -159,19 +174,17 @@ namespace {
 un_status scan_common(const char* F, int32_t type, int32_t B, int32_t T, int32_t d, int64_t ld, int64_t ld2, int64_t ld3,
                       int64_t seq_out, const void* workspace, size_t bytes, bool bwd, ScanPlan* plan) {
   if (!type_ok(type)) return bad(F, "unknown type");
-  if (B < 0 || T < 0 || d < 0) return bad(F, "negative size");
-  if (T > (1 << 30)) return bad(F, "more than 2^30 tokens are not supported", UN_ERR_UNSUPPORTED);
-  if (d > SCAN_MAX_LD || (T > 1 && (ld > SCAN_MAX_LD || ld2 > SCAN_MAX_LD || ld3 > SCAN_MAX_LD)))
-    return bad(F, "a width or token stride of 2^24 or more is not supported", UN_ERR_UNSUPPORTED);
+  un_status st = scan_sizes_ok(F, B, T, d, bwd, plan);
+  if (st != UN_OK) return st;
+  if (T > 1 && (ld > SCAN_MAX_LD || ld2 > SCAN_MAX_LD || ld3 > SCAN_MAX_LD))
+    return bad(F, "a token stride of 2^24 or more is not supported", UN_ERR_UNSUPPORTED);
   if (T > 1 && (ld < d || ld2 < d || ld3 < d)) return bad(F, "a token stride is smaller than the width");
   if (B > 1 && T > 0 && seq_out < d) return bad(F, "the output's sequence stride is smaller than the width");
   size_t need = 0;
-  un_gated_scan_sizes(B, T, d, nullptr, &need);
+  st = un_gated_scan_sizes(B, T, d, nullptr, &need);
+  if (st != UN_OK) return st;
   if (need && (!workspace || bytes < need)) return bad(F, "workspace too small (un_gated_scan_sizes)", UN_ERR_BUFSIZE);
   if (need && (uintptr_t)workspace % 8) return bad(F, "workspace is not 8-byte aligned");
-  *plan = scan_plan(B, T, d, bwd);
-  if (too_many((int64_t)plan->tiles * B * plan->nseg, plan->kind >= SCAN_CHUNKS ? 64 * SCAN_W : 64))
-    return bad(F, "too many sequences and channels", UN_ERR_UNSUPPORTED);
   return UN_OK;
 }
 }  // namespace

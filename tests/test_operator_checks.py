@@ -1,0 +1,41 @@
+"""CPU tests of the operators' checks of sizes, of overlapping tensors and of messages."""
+import ctypes
+import os
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2408_01331_amd import unifiednn as U  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not os.path.exists(U.LIB_PATH):
+        from paper_2408_01331_amd.build import build
+        build()
+    U.lib()
+
+
+# ---------------------------------------------------------------------------
+# Sizes of the recurrence's states and workspace
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("batch,tokens,width,text", [
+    (1, (1 << 30) + 1, 8, "tokens"), (1, (1 << 31) - 1, 8, "tokens"), (1, (1 << 31) - 60, 1, "tokens"),
+    (1, 100, 1 << 24, "width"), (1, 100, (1 << 31) - 1, "width"), (1, (1 << 31) - 1, (1 << 31) - 1, "tokens"),
+    ((1 << 31) - 1, 16, 64, "too many"), (1, 1 << 30, 100, "too many"), ((1 << 31) - 1, 1 << 30, (1 << 24) - 1, "too many"),
+])
+def test_scan_sizes_refused(batch, tokens, width, text):
+    """Sizes that no call takes have no workspace either, up to the largest that the arguments can name."""
+    n, b = ctypes.c_size_t(7), ctypes.c_size_t(7)
+    assert U.lib().un_gated_scan_sizes(batch, tokens, width, ctypes.byref(n), ctypes.byref(b)) == U.UN_ERR_UNSUPPORTED
+    assert text in U.lib().un_last_error(None).decode() and (n.value, b.value) == (7, 7)
+
+
+@pytest.mark.parametrize("batch,tokens,width", [(1, 1 << 30, 1), (1, 1 << 30, 64), (3, 5, (1 << 24) - 1), (1 << 25, 16, 64)])
+def test_scan_sizes_at_the_limits(batch, tokens, width):
+    """A state every 64 tokens; the workspace, where there is one, holds a word per segment, sequence and channel at least."""
+    n, b = ctypes.c_size_t(), ctypes.c_size_t()
+    assert U.lib().un_gated_scan_sizes(batch, tokens, width, ctypes.byref(n), ctypes.byref(b)) == U.UN_OK
+    assert n.value == batch * -(-tokens // 64) * width
+    assert (b.value >= 8 * (tokens // 256) * batch * width) if tokens > 1 << 20 else b.value == 0
