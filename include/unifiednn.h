@@ -570,7 +570,7 @@ typedef struct {
 typedef struct un_adamw un_adamw;
 /* A plan of the step over these tensors (n >= 1; elements may be 0), on the
  * current device. It holds their addresses, not their data: they stay the caller's,
- * and none that is written may overlap another. */
+ * and none that is written may overlap another, a gradient among them (not checked). */
 un_status un_adamw_create(const un_adamw_tensor* tensors, int32_t n, int32_t grad_type, int32_t state_bits, un_adamw** out);
 /* One step. lr and decay are finite and >= 0, lr * decay < 1, beta1 and beta2 in
  * [0, 1), eps > 0, t >= 1. The rates and the count travel with the call, so a

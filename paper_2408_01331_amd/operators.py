@@ -281,6 +281,20 @@ def gated_scan_backward(gate, value, states, dh, dlast=None, lens=None, out=None
 QBLOCK = 256  # elements that share a scale in the 8-bit states
 
 
+def _disjoint(written, read):
+    """No (contiguous) tensor of `written` shares memory with another one of either list."""
+    spans = sorted((y.data_ptr(), y.data_ptr() + y.numel() * y.element_size(), w) for x, w in ((written, True), (read, False))
+                   for y in x if y.numel())
+    end = end_written = 0
+    for lo, hi, w in spans:
+        if lo < (end if w else end_written):
+            return False
+        end = max(end, hi)
+        if w:
+            end_written = max(end_written, hi)
+    return True
+
+
 class AdamW:
     """AdamW over many tensors in one launch, in place on tensors that the
     caller holds.
@@ -290,7 +304,8 @@ class AdamW:
     8 bits float8_e4m3fn m and v (v holds sqrt(v)) with m_scales and v_scales,
     float8_e8m0fnu, one per QBLOCK consecutive elements of a tensor
     (`AdamW.state8` makes fresh ones). Every tensor is contiguous, and none that is
-    written may overlap another; the plan holds references to all of them.
+    written may overlap another, a gradient among them; the plan holds references
+    to all of them.
     Gradients are read where they were when the plan was made: write the next
     step's into the same tensors."""
 
@@ -331,9 +346,8 @@ class AdamW:
                     _require(False, f"{name}[{i}] must be a contiguous {dt} tensor of {size} elements on {device}")
                 at.append(y.data_ptr())
             arr[i] = _un.un_adamw_tensor(*at, k)
-        written = sorted((y.data_ptr(), y.data_ptr() + y.numel() * y.element_size())
-                         for x in (params, m, v, copies, m_scales, v_scales) for y in x or () if y.numel())
-        _require(all(a[1] <= b[0] for a, b in zip(written, written[1:])), "tensors that are written overlap")
+        flat = lambda *lists: [y for x in lists for y in x or ()]  # noqa: E731
+        _require(_disjoint(flat(params, m, v, copies, m_scales, v_scales), grads), "a tensor that is written overlaps another one")
         self._held = [list(x) for x in lists.values()]
         self.device, self._index = device, dev
         plan = ctypes.c_void_p()

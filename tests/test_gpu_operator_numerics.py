@@ -143,6 +143,24 @@ def test_adamw8_key_of_its_own(ops):
         assert (res[a] != res[b]).float().mean() > 0.2
 
 
+def test_adamw_gradients_that_overlap(ops):
+    """A gradient that shares memory with something written is refused; gradients may share among themselves."""
+    z = lambda n=10: torch.zeros(n, device="cuda")  # noqa: E731
+    p = z()
+    with pytest.raises(ValueError, match="overlap"):
+        ops.AdamW([p], [p], [z()], [z()])
+    whole = z(20)
+    with pytest.raises(ValueError, match="overlap"):
+        ops.AdamW([p], [whole[5:15]], [whole[:10]], [z()])
+    half = z().to(BF16)
+    with pytest.raises(ValueError, match="overlap"):
+        ops.AdamW([p], [half], [z()], [z()], copies=[half])
+    g = rand(1, (10,))
+    ops.AdamW([p, whole[:10]], [g, g], [z(), z()], [z(), z()]).step(0.1, 1)
+    ops.AdamW([whole[:10]], [whole[10:]], [z()], [z()]).step(0.1, 1)
+    assert torch.equal(p != 0, g != 0)
+
+
 # ---------------------------------------------------------------------------
 # RMS norm in e4m3
 # ---------------------------------------------------------------------------

@@ -39,3 +39,21 @@ def test_scan_sizes_at_the_limits(batch, tokens, width):
     assert U.lib().un_gated_scan_sizes(batch, tokens, width, ctypes.byref(n), ctypes.byref(b)) == U.UN_OK
     assert n.value == batch * -(-tokens // 64) * width
     assert (b.value >= 8 * (tokens // 256) * batch * width) if tokens > 1 << 20 else b.value == 0
+
+
+# ---------------------------------------------------------------------------
+# Tensors that overlap
+# ---------------------------------------------------------------------------
+def test_disjoint():
+    """What is written shares no memory with anything; what is only read may share it with what is only read."""
+    from paper_2408_01331_amd.operators import _disjoint
+    x = torch.zeros(100)
+    cut = lambda a, b: x[a:b]  # noqa: E731
+    assert _disjoint([], []) and _disjoint([cut(0, 10), cut(10, 20)], [cut(20, 30), cut(20, 30), cut(25, 40)])
+    assert _disjoint([cut(5, 5), cut(0, 10)], [cut(3, 3)])  # empty ones share nothing
+    assert _disjoint([cut(40, 50)], [cut(0, 40), cut(10, 20), cut(50, 100)])
+    for written, read in (([cut(0, 10), cut(9, 20)], []), ([cut(0, 10), cut(0, 10)], []), ([cut(0, 10)], [cut(0, 10)]),
+                          ([cut(0, 10)], [cut(9, 12)]), ([cut(9, 12)], [cut(0, 10)]), ([cut(5, 6)], [cut(0, 100), cut(1, 2)]),
+                          ([cut(0, 100), cut(200, 200)], [cut(99, 100)]), ([cut(0, 60), cut(80, 90)], [cut(70, 75), cut(20, 30)]),
+                          ([cut(50, 60).view(torch.uint8), cut(10, 20)], [cut(59, 61)])):
+        assert not _disjoint(written, read)
