@@ -6,7 +6,9 @@ which a context's step runs for its own layers and optimizers too).
 Argument checks and marshalling only; the work runs in the library's HIP
 kernels, on torch's current stream of the tensors' device. A call allocates its
 outputs and workspace from torch's allocator and does not wait for the device.
-Nothing is recorded for autograd: the backward passes are calls of their own.
+Nothing is recorded for autograd: the backward passes are calls of their own, and
+a call on tensors that require gradients is refused where autograd records (call
+it under torch.no_grad(), or in a torch.autograd.Function).
 """
 from __future__ import annotations
 
@@ -59,6 +61,14 @@ def _flat(x, name, shape, dtype, dev):
     if not (isinstance(x, torch.Tensor) and x.dtype is dtype and x.get_device() == dev and x.shape == shape and x.is_contiguous()):
         _like(x, name, torch.Size(shape), dtype, dev) if len(shape) else None
         _require(False, f"{name} must be contiguous")
+
+
+def _unrecorded(*tensors):
+    """No graph is cut: none of the tensors (None: not given) requires a gradient while autograd records."""
+    for x in tensors:
+        if x is not None and x.requires_grad and torch.is_grad_enabled():
+            raise ValueError("a tensor requires a gradient, and this call records nothing for autograd: call it under torch.no_grad() "
+                             "or in a torch.autograd.Function, with the backward call of its own")
 
 
 def _ptr(x):
@@ -140,6 +150,8 @@ def _norm(x, weight, residual, eps, keep, e4m3):
     rp, ldr, rv, sp, s = None, 0, None, None, x
     if residual is not None:
         rp, ldr, rv = _operand(residual, "residual", shape, dtype, dev)
+    _unrecorded(x, weight, residual)
+    if residual is not None:
         s = _fresh(x, dtype)
         sp = s.data_ptr()
     rstd = weight.new_empty(shape[:-1]) if keep else None
@@ -175,6 +187,7 @@ def rms_norm_backward(dy, s, weight, rstd, ds=None):
     _flat(weight, "weight", (width,), _F32, dev)
     _flat(rstd, "rstd", shape[:-1], _F32, dev)
     dsp, ldds, dsv = (None, 0, None) if ds is None else _operand(ds, "ds", shape, dtype, dev)
+    _unrecorded(dy, s, weight, rstd, ds)
     dx, dw = _fresh(s, dtype), _empty_like(weight)
     need = _norm_workspace(t, rows, width)
     ws = weight.new_empty(need // 4)
@@ -230,10 +243,11 @@ def gated_scan(gate, value, h0=None, lens=None, keep=False, last=None):
     b, n, d = shape
     if h0 is not None:
         _flat(h0, "h0", (b, d), _F32, dev)
+    if last is not None:
+        _flat(last, "last", (b, d), _F32, dev)
+    _unrecorded(gate, value, h0, last)
     if last is None:
         last = gate.new_empty((b, d), dtype=_F32) if h0 is None else _empty_like(h0)
-    else:
-        _flat(last, "last", (b, d), _F32, dev)
     h = gate.new_empty(shape)
     states = ws = None
     n_ws = 0
@@ -266,6 +280,7 @@ def gated_scan_backward(gate, value, states, dh, dlast=None, lens=None, out=None
     _like(dv, "dvalue", shape, dtype, dev)
     (ldo, seqo), (ldd, seqd) = _strides(dg, shape), _strides(dh, shape)
     _require((ldo, seqo) == _strides(dv, shape) or dg.numel() == 0, "dgate and dvalue must have the same strides")
+    _unrecorded(gate, value, states, dh, dlast, dg, dv)
     dh0 = gate.new_empty((b, d), dtype=_F32)
     ws = gate.new_empty(n_ws, dtype=torch.uint8) if n_ws else None
     _call(_lib().un_gated_scan_backward, _un.un_gated_scan_grad_args(t, b, n, d, gate.data_ptr(), value.data_ptr(), ld, seq, _ptr(lens),

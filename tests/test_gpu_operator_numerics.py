@@ -257,3 +257,44 @@ def test_step_with_large_gates():
         loss = h.step(0.05)
         assert np.isfinite(loss).all() and np.isfinite(h.get_params(0)).all()
         assert abs(loss[0] - want) <= 1e-4 * abs(want)
+
+
+# ---------------------------------------------------------------------------
+# Autograd
+# ---------------------------------------------------------------------------
+def test_tensors_that_require_gradients(ops):
+    """A call that would cut the graph silently is refused; under no_grad, or on detached tensors, it runs."""
+    x, w, z, dh = rand(1, (4, 16)), rand(2, (16,)), rand(3, (2, 5, 16)), rand(4, (2, 5, 16))
+    leaf = lambda t: t.clone().requires_grad_()  # noqa: E731
+    y, s, rstd = ops.rms_norm(x, w, keep=True)
+    h, last, states = ops.gated_scan(z, z, keep=True)
+    refused = [lambda: ops.rms_norm(leaf(x), w), lambda: ops.rms_norm(x, leaf(w)), lambda: ops.rms_norm(x, w, residual=leaf(x)),
+               lambda: ops.rms_norm_e4m3(leaf(x), w), lambda: ops.rms_norm_backward(leaf(x), s, w, rstd),
+               lambda: ops.rms_norm_backward(x, s, leaf(w), rstd), lambda: ops.rms_norm_backward(x, s, w, rstd, ds=leaf(x)),
+               lambda: ops.gated_scan(leaf(z), z), lambda: ops.gated_scan(z, leaf(z)), lambda: ops.gated_scan(z, z, h0=leaf(last)),
+               lambda: ops.gated_scan(z, z, last=leaf(last)), lambda: ops.gated_scan_backward(z, z, states, leaf(dh)),
+               lambda: ops.gated_scan_backward(leaf(z), z, states, dh), lambda: ops.gated_scan_backward(z, z, states, dh, dlast=leaf(last)),
+               lambda: ops.gated_scan_backward(z, z, states, dh, out=(leaf(dh), dh.clone()))]
+    for k, call in enumerate(refused):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+            pytest.fail(f"call {k} was not refused")
+    with torch.no_grad():
+        assert torch.equal(ops.rms_norm(leaf(x), leaf(w))[0], y)
+    assert torch.equal(ops.gated_scan(leaf(z).detach(), z)[0], h)
+
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w):
+            y, s, rstd = ops.rms_norm(x, w, keep=True)
+            ctx.save_for_backward(s, w, rstd)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            return ops.rms_norm_backward(dy, *ctx.saved_tensors)
+
+    a, b = leaf(x), leaf(w)
+    Norm.apply(a, b).backward(x)
+    dx, dw = ops.rms_norm_backward(x, s, w, rstd)
+    assert torch.equal(a.grad, dx) and torch.equal(b.grad, dw)

@@ -57,3 +57,20 @@ def test_disjoint():
                           ([cut(0, 100), cut(200, 200)], [cut(99, 100)]), ([cut(0, 60), cut(80, 90)], [cut(70, 75), cut(20, 30)]),
                           ([cut(50, 60).view(torch.uint8), cut(10, 20)], [cut(59, 61)])):
         assert not _disjoint(written, read)
+
+
+# ---------------------------------------------------------------------------
+# Autograd
+# ---------------------------------------------------------------------------
+def test_tensors_that_require_gradients():
+    """Refused where autograd records, taken where it does not."""
+    from paper_2408_01331_amd.operators import _unrecorded
+    x, leaf = torch.zeros(3), torch.zeros(3, requires_grad=True)
+    _unrecorded(x, None, leaf.detach())
+    for args in ((leaf,), (x, None, leaf), (x, leaf * 2)):
+        with pytest.raises(ValueError, match="requires a gradient.*no_grad"):
+            _unrecorded(*args)
+        with torch.no_grad():
+            _unrecorded(*args)
+        with torch.inference_mode():
+            _unrecorded(*args)
