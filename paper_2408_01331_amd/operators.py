@@ -8,7 +8,8 @@ kernels, on torch's current stream of the tensors' device. A call allocates its
 outputs and workspace from torch's allocator and does not wait for the device.
 Nothing is recorded for autograd: the backward passes are calls of their own, and
 a call on tensors that require gradients is refused where autograd records (call
-it under torch.no_grad(), or in a torch.autograd.Function).
+it under torch.no_grad(), or in a torch.autograd.Function). Tensors that a call
+writes in place get a new version, as by torch's own operations.
 """
 from __future__ import annotations
 
@@ -25,6 +26,7 @@ from .unifiednn import UnError  # noqa: F401  (raised by every call here)
 _F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
 _TYPES = {_F32: 0, _BF16: 1}
 _byref, _empty_like = ctypes.byref, torch.empty_like
+_written = torch.autograd.graph.increment_version
 
 
 def _require(ok, what):
@@ -248,6 +250,8 @@ def gated_scan(gate, value, h0=None, lens=None, keep=False, last=None):
     _unrecorded(gate, value, h0, last)
     if last is None:
         last = gate.new_empty((b, d), dtype=_F32) if h0 is None else _empty_like(h0)
+    else:
+        _written(last)
     h = gate.new_empty(shape)
     states = ws = None
     n_ws = 0
@@ -281,6 +285,8 @@ def gated_scan_backward(gate, value, states, dh, dlast=None, lens=None, out=None
     (ldo, seqo), (ldd, seqd) = _strides(dg, shape), _strides(dh, shape)
     _require((ldo, seqo) == _strides(dv, shape) or dg.numel() == 0, "dgate and dvalue must have the same strides")
     _unrecorded(gate, value, states, dh, dlast, dg, dv)
+    if given:
+        _written((dg, dv))
     dh0 = gate.new_empty((b, d), dtype=_F32)
     ws = gate.new_empty(n_ws, dtype=torch.uint8) if n_ws else None
     _call(_lib().un_gated_scan_backward, _un.un_gated_scan_grad_args(t, b, n, d, gate.data_ptr(), value.data_ptr(), ld, seq, _ptr(lens),
@@ -364,6 +370,9 @@ class AdamW:
         flat = lambda *lists: [y for x in lists for y in x or ()]  # noqa: E731
         _require(_disjoint(flat(params, m, v, copies, m_scales, v_scales), grads), "a tensor that is written overlaps another one")
         self._held = [list(x) for x in lists.values()]
+        # a view's version is its base's: one of each is enough (each takes 40 ns of every step's call)
+        bases = [y if y._base is None else y._base for y in flat(params, m, v, copies, m_scales, v_scales)]
+        self._written = list({id(y): y for y in bases}.values())
         self.device, self._index = device, dev
         plan = ctypes.c_void_p()
         with torch.cuda.device(device):
@@ -384,6 +393,7 @@ class AdamW:
             key = 0x5EED + int(step) * 0x01000193  # as for a context's models
         h = _un.un_adamw_hyper(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step), int(key) & 0xFFFFFFFF)
         _call(_lib().un_adamw_step, h, self._index, self._plan)
+        _written(self._written)
 
     def close(self):
         if self._plan:

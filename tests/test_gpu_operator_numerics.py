@@ -298,3 +298,38 @@ def test_tensors_that_require_gradients(ops):
     Norm.apply(a, b).backward(x)
     dx, dw = ops.rms_norm_backward(x, s, w, rstd)
     assert torch.equal(a.grad, dx) and torch.equal(b.grad, dw)
+
+
+def test_writes_in_place_are_seen_by_autograd(ops):
+    """Tensors that a call writes in place get a new version, so that a backward pass that saved their old values refuses."""
+    z, h0 = rand(1, (2, 5, 16)), rand(2, (2, 16))
+    leaf = torch.ones(2, 16, device="cuda", requires_grad=True)
+    out = leaf * h0  # saves h0
+    ops.gated_scan(z, z, h0=h0, last=h0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+    h, last, states = ops.gated_scan(z, z, keep=True)
+    buf = torch.zeros(2, 2, 5, 16, device="cuda").unbind(0)
+    before = [t._version for t in buf]
+    ops.gated_scan_backward(z, z, states, z, out=buf)
+    assert all(t._version > v for t, v in zip(buf, before))
+    for eight in (False, True):
+        p, g = [torch.nn.Parameter(rand(3, (300,)))], [rand(4, (300,))]
+        c = [torch.zeros(300, device="cuda", dtype=BF16)]
+        states = ops.AdamW.state8(p) if eight else ([torch.zeros(300, device="cuda")], [torch.zeros(300, device="cuda")])
+        opt = ops.AdamW(p, g, *states[:2], copies=c, **(dict(m_scales=states[2], v_scales=states[3]) if eight else {}))
+        written, read = [x[0] for x in (p, c, *states)], g[0]._version
+        before = [t._version for t in written]
+        loss = (p[0] * p[0]).sum()
+        opt.step(0.1, 1)
+        assert all(t._version > v for t, v in zip(written, before)) and g[0]._version == read
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    whole, z10 = torch.zeros(20, device="cuda"), lambda: [torch.zeros(10, device="cuda") for _ in range(2)]
+    parts = [whole[:10], whole[10:]]
+    ops.AdamW(parts, z10(), z10(), z10()).step(0.1, 1)
+    assert whole._version > 0 and parts[0]._version > 0 and parts[1]._version > 0
+    with torch.inference_mode():  # tensors without versions
+        s = h0.clone()
+        ops.gated_scan(z, z, h0=s, last=s)
+    assert not torch.equal(s, h0)
