@@ -61,7 +61,7 @@ def _like(x, name, shape, dtype, dev):
 
 def _flat(x, name, shape, dtype, dev):
     if not (isinstance(x, torch.Tensor) and x.dtype is dtype and x.get_device() == dev and x.shape == shape and x.is_contiguous()):
-        _like(x, name, torch.Size(shape), dtype, dev) if len(shape) else None
+        _like(x, name, torch.Size(shape), dtype, dev)
         _require(False, f"{name} must be contiguous")
 
 

@@ -333,3 +333,12 @@ def test_writes_in_place_are_seen_by_autograd(ops):
         s = h0.clone()
         ops.gated_scan(z, z, h0=s, last=s)
     assert not torch.equal(s, h0)
+
+
+def test_messages_of_scalars(ops):
+    """A row's rstd is a tensor without axes: what does not fit is named."""
+    x, w = rand(1, (16,)), rand(2, (16,))
+    y, s, rstd = ops.rms_norm(x, w, keep=True)
+    for bad, text in ((rstd[None], "shape"), (rstd.double(), "float32"), (rstd.cpu(), "cuda"), (1.0, "tensor")):
+        with pytest.raises(ValueError, match=f"rstd must .*{text}"):
+            ops.rms_norm_backward(x, s, w, bad)

@@ -74,3 +74,22 @@ def test_tensors_that_require_gradients():
             _unrecorded(*args)
         with torch.inference_mode():
             _unrecorded(*args)
+
+
+# ---------------------------------------------------------------------------
+# Messages
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("shape", [(), (1,), (4, 1), (4, 3)])
+def test_messages_of_dense_arguments(shape):
+    """What does not fit is named, of tensors without axes too; contiguity only where nothing else is wrong."""
+    from paper_2408_01331_amd.operators import _flat
+    fits = torch.zeros(shape)
+    _flat(fits, "rstd", shape, torch.float32, -1)  # (a CPU tensor's device has the number -1)
+    for bad, text in ((fits[None], "shape"), (fits.double(), "float32"), (1.0, "a tensor"), (None, "a tensor")):
+        with pytest.raises(ValueError, match=f"rstd must .*{text}"):
+            _flat(bad, "rstd", shape, torch.float32, -1)
+    with pytest.raises(ValueError, match="rstd must be on cuda:0"):
+        _flat(fits, "rstd", shape, torch.float32, 0)
+    if len(shape) == 2:
+        with pytest.raises(ValueError, match="contiguous"):
+            _flat(torch.zeros(8, shape[1])[::2], "rstd", shape, torch.float32, -1)
