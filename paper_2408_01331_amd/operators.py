@@ -389,6 +389,7 @@ class AdamW:
     def step(self, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, key=None):
         """Step number `step` (from 1). key: with 8-bit states, a whole number of which the rounding's random numbers are made,
         another one each step; None: one made of `step`."""
+        _require(self._plan is not None, "the plan is closed")
         if key is None:
             key = 0x5EED + int(step) * 0x01000193  # as for a context's models
         h = _un.un_adamw_hyper(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), int(step), int(key) & 0xFFFFFFFF)

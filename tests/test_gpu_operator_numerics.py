@@ -161,6 +161,15 @@ def test_adamw_gradients_that_overlap(ops):
     assert torch.equal(p != 0, g != 0)
 
 
+def test_adamw_after_close(ops):
+    z = lambda: [torch.zeros(10, device="cuda")]  # noqa: E731
+    opt = ops.AdamW(z(), z(), z(), z())
+    opt.close()
+    opt.close()
+    with pytest.raises(ValueError, match="closed"):
+        opt.step(0.1, 1)
+
+
 # ---------------------------------------------------------------------------
 # RMS norm in e4m3
 # ---------------------------------------------------------------------------

@@ -93,3 +93,12 @@ def test_messages_of_dense_arguments(shape):
     if len(shape) == 2:
         with pytest.raises(ValueError, match="contiguous"):
             _flat(torch.zeros(8, shape[1])[::2], "rstd", shape, torch.float32, -1)
+
+
+def test_step_of_a_closed_plan():
+    from paper_2408_01331_amd.operators import AdamW
+    opt = AdamW.__new__(AdamW)
+    opt._plan = None
+    opt.close()
+    with pytest.raises(ValueError, match="closed"):
+        opt.step(0.1, 1)
