@@ -48,7 +48,6 @@ template <> struct V16<float> {
     for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(f[e]);
     return v;
   }
-  __device__ static float round(float f) { return f; }
   __device__ static float load1(const float* p) { return *p; }
   __device__ static void store1(float* p, float f) { *p = f; }
 };
@@ -67,21 +66,11 @@ template <> struct V16<bf16_t> {
     for (int e = 0; e < 4; ++e) v[e] = f2bf2(f[2 * e], f[2 * e + 1]);
     return v;
   }
-  __device__ static float round(float f) { return bf2f(f2bf(f)); }
   __device__ static float load1(const bf16_t* p) { return bf2f(*p); }
   __device__ static void store1(bf16_t* p, float f) { *p = (bf16_t)f2bf(f); }
 };
 
-// n (0 .. N) values at p; the rest are zeros
-template <typename T> __device__ __forceinline__ void load_vec(const T* p, int n, float* f) {
-  constexpr int N = V16<T>::N;
-  if (n == N) {
-    V16<T>::unpack(*(const u32x4_a2*)p, f);
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = e < n ? V16<T>::load1(p + e) : 0.f;
-  }
-}
+// n (0 .. N) values to p
 template <typename T> __device__ __forceinline__ void store_vec(T* p, int n, const float* f) {
   constexpr int N = V16<T>::N;
   if (n == N) {
@@ -92,6 +81,7 @@ template <typename T> __device__ __forceinline__ void store_vec(T* p, int n, con
       if (e < n) V16<T>::store1(p + e, f[e]);
   }
 }
+// n (0 .. N) values at p; the rest are zeros
 template <int N> __device__ __forceinline__ void load_f32(const float* p, int n, float* f) {
   if (n == N) {
 #pragma unroll
