@@ -53,7 +53,7 @@ def listed():
         _scan("scan_train_bf16", 16, 2048, 1024, "bf16", "train"),
         # one very long sequence: few channels in all, so the long axis has to be split
         _scan("scan_train_bf16_long", 1, 65536, 512, "bf16", "train"),
-        # the tensors of a few small MLPs (this repository's eight-MLP hybrid in size): hundreds of short ones
+        # the tensors of a few small MLPs (this repository's eight-MLP hybrid in size): 35, most of them short
         _adamw("adamw32_small", "mlp", 2_000_000, 32, "f32", False),
         # a large model's tensors, states in 32 bits, bf16 gradients and working copies
         _adamw("adamw32_large", "wide", 200_000_000, 32, "bf16", True),
@@ -257,13 +257,10 @@ def _run_scan(st):
         if not train:
             return dict(h=h, last=last)
         dz = torch.empty((case["batch"], n, 2 * d), dtype=gate.dtype, device=gate.device)
-        dlast = st["dlast"]
-        if lens is None and gate.dtype == torch.float32:
-            # the program adds the last state's gradient to that of the last step, in its own buffer, as the pass below does
-            st["dh"][:, -1] += dlast
-            dlast = None
-        dh0 = ops.gated_scan_backward(gate, value, states, st["dh"], dlast=dlast, lens=lens,
+        dh0 = ops.gated_scan_backward(gate, value, states, st["dh"], dlast=st["dlast"], lens=lens,
                                       out=(dz[..., :d], dz[..., d:]))
+        if lens is None and gate.dtype == torch.float32:
+            st["dh"][:, -1] += st["dlast"]  # as the pass below leaves this buffer, so that the next pass has its inputs
         return dict(h=h, last=last, dz=dz, dh0=dh0)
     t = gate.dtype
     g, v = gate.float(), value.float()
