@@ -248,6 +248,24 @@ def test_scan_resets_by_large_gates(ops, dtype, b, n, w):
     R.close(grads[1][:2, :, :8], wv, half(wv, bv) + R.TINY, "dvalue")
 
 
+@pytest.mark.parametrize("b,n,w", [(2, 3000, 70), (40, 300, 700), (300, 140, 130), (5, 16, 8)], ids=["split", "long chunks", "chunks", "wave"])
+def test_scan_infinite_states(ops, b, n, w):
+    """A state that is infinite is never finite again, whatever the gates (infinite, or NaN where a product of gates underflows
+    or a gate resets it), and concerns its own channel alone."""
+    gate, value, dh = rand(1, (b, n, w), mean=-1.0), rand(2, (b, n, w)), rand(3, (b, n, w))
+    gate[:, n // 2] = -100.0
+    clean, _, states = ops.gated_scan(gate, value, keep=True)
+    grads = ops.gated_scan_backward(gate, value, states, dh)
+    at = n // 4
+    value[0, at, 3] = float("inf")
+    h, last, states = ops.gated_scan(gate, value, keep=True)
+    assert not torch.isfinite(h[0, at:, 3]).any() and not torch.isfinite(last[0, 3])
+    again = ops.gated_scan_backward(gate, value, states, dh)
+    for x, y in ((h, clean), (again[0], grads[0]), (again[1], grads[1])):
+        x[0, :, 3], y[0, :, 3] = 0, 0
+        assert torch.equal(x, y)
+
+
 def test_step_with_large_gates():
     """A context's fp32 recurrence whose gates are near -100 everywhere: h is the value, and the loss is the oracle's."""
     import oracle
