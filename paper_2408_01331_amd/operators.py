@@ -345,6 +345,7 @@ class AdamW:
             _require(len(x) == n, f"{k} must hold {n} tensors, not {len(x)}")
         _, dev = _check_type(params[0], "params[0]")
         device = params[0].device
+        _require(isinstance(grads[0], torch.Tensor), "grads[0] must be a tensor")
         gt = grads[0].dtype
         _require(gt in _TYPES, f"gradients must be float32 or bfloat16, not {gt}")
         st = torch.float8_e4m3fn if eight else torch.float32

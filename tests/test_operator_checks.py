@@ -102,3 +102,12 @@ def test_step_of_a_closed_plan():
     opt.close()
     with pytest.raises(ValueError, match="closed"):
         opt.step(0.1, 1)
+
+
+def test_adamw_without_gradients(monkeypatch):
+    """A parameter's grad before any backward pass is None: refused by name."""
+    from paper_2408_01331_amd import operators as ops
+    monkeypatch.setattr(ops, "_check_type", lambda x, name: (0, 0))  # (a CPU tensor would be refused first)
+    w = torch.zeros(3)
+    with pytest.raises(ValueError, match=r"grads\[0\] must be a tensor"):
+        ops.AdamW([w], [None], [w.clone()], [w.clone()])
