@@ -433,6 +433,7 @@ un_status un_profile_read(un_ctx* ctx, int32_t kernel_class, double* total_ms, i
  *     HIP graph, except un_adamw_step.
  *   - Strides are in elements; the innermost stride is 1. Tensors need their
  *     element's alignment, no more (a workspace 8 bytes).
+ *     (un_adamw_create and _destroy allocate and free: not while a capture is on.)
  *   - Errors are read with un_last_error(NULL) on the calling thread. A refused
  *     call enqueues nothing.
  * ------------------------------------------------------------------------- */
@@ -500,7 +501,11 @@ un_status un_rms_norm_workspace(int32_t type, int64_t rows, int32_t width, size_
  * value are not used, their rows of h are written as zeros, and the last state is
  * the one before them. A single token is a call with tokens = 1; last may be start
  * itself. h must not overlap the inputs. states (for the backward pass) and
- * workspace: as un_gated_scan_sizes says. */
+ * workspace: as un_gated_scan_sizes says.
+ *   The time axis is divided by the sizes of the call: the same sequence in a batch of
+ * another size may differ in its last bits (one call repeated gives the same bits). A
+ * state that has become infinite is never finite again, but may be NaN further on
+ * where step after step it would stay infinite (a product of gates that underflows). */
 typedef struct {
   int32_t type;              /* un_type of gate, value, h */
   int32_t batch, tokens, width;
@@ -558,7 +563,8 @@ un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size
  * steps are smaller than the codes' distance would not move otherwise), from
  * random numbers made of `key` and the element's number, so that a step with
  * another key rounds independently; a u that is not 0 never becomes 0. A fresh
- * state is zeros everywhere (codes, scales). */
+ * state is zeros everywhere (codes, scales). The weights get the same bits as with
+ * fp32 states of the same values. */
 typedef struct {
   float* weight;
   const void* grad;

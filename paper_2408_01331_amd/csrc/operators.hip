@@ -893,11 +893,12 @@ __global__ __launch_bounds__(64 * W) void scan_table_kernel(const ScanProb* __re
 // AdamW. A wave takes AW_BLOCK values, four per lane, so the block of an 8-bit
 // scale is one wave's and its maximum one reduction over the lanes. One block per
 // wave: with four, all loaded ahead, the registers left half of the waves' room
-// (200 M parameters, 8-bit states 589 us, so 538; 6 M 27.5, so 20.9; 32 bits 1058,
-// so 1051).
+// (200 M parameters, 8-bit states 589 us, one block 538; 6 M 27.5 and 20.9; 32 bits
+// 1058 and 1051: each with roots and reciprocals to 1 ulp and ordinary accesses).
 // ---------------------------------------------------------------------------
-// 32 bits from a value's number and the step's key: multiplications by odd
-// constants (fractions of the golden ratio, sqrt 2 and sqrt 3) between shifts
+// 32 bits from a value's number and the step's key: the published kind of integer
+// hash that takes xor-shifts and multiplications by odd constants in turn (here
+// fractions of the golden ratio, sqrt 2 and sqrt 3), each of which loses nothing
 __device__ __forceinline__ uint32_t random_bits(uint32_t i, uint32_t key) {
   uint32_t x = i * 0x9E3779B9u + key;
   x ^= x >> 16;
@@ -1265,8 +1266,8 @@ hipError_t launch_scan_table(bool bf16, bool bwd, bool shorts, const ScanProb* p
 // Above half of the last-level cache (256 MiB) a step's tensors would only push
 // one another and the rest of the program out of it. Steps with ordinary accesses /
 // past the caches, three sets of tensors in turn, us: states in 32 bits, 4 M
-// parameters (72 MB) 18.9 / 21.8, 8 M (144 MB) 44.7 / 39.5, 200 M 1039 / 992; in 8
-// bits, 8 M (80 MB) 24.3 / 26.4, 16 M (160 MB) 50.7 / 46.5, 200 M 537 / 514.
+// parameters (72 MB) 19.4 / 22.0, 8 M (144 MB) 47.4 / 41.3, 200 M 1034 / 988; in 8
+// bits, 8 M (80 MB) 25.1 / 26.8, 16 M (160 MB) 51.8 / 49.0, 200 M 575 / 559.
 hipError_t launch_adamw(bool g16, bool eight, const AdamwTensor* ts, const int32_t* map, int nblocks, int64_t bytes, const AdamwHp& hp,
                         const AdamwHp* hps, hipStream_t s) {
   if (nblocks <= 0) return hipSuccess;

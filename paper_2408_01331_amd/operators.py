@@ -237,7 +237,8 @@ def gated_scan(gate, value, h0=None, lens=None, keep=False, last=None):
     a = sigmoid(gate), per sequence and channel. gate, value: [batch, tokens,
     width] float32 or bfloat16, of any equal strides with a dense last axis (the
     halves of one projection). h0: float32 [batch, width], None for zeros. lens:
-    int32 [batch], steps used of each sequence (rows of h behind are zeros).
+    int32 [batch], steps used of each sequence (rows of h behind are zeros). The
+    last bits of a sequence may depend on the batch's size (un_gated_scan).
     last (the state after the last step, float32) may be given, h0 itself among
     others, to be written in place. states (None unless `keep`) is what
     gated_scan_backward needs."""
