@@ -430,10 +430,10 @@ un_status un_profile_read(un_ctx* ctx, int32_t kernel_class, double* total_ms, i
  *   - Nothing is allocated and nothing is kept between calls but what the
  *     caller passes: calls on different streams do not disturb one another as
  *     long as their outputs and workspaces differ. All may be captured into a
- *     HIP graph, except un_adamw_step.
+ *     HIP graph, except un_adamw_step. (un_adamw_create and _destroy
+ *     allocate and free memory: not while a capture is on.)
  *   - Strides are in elements; the innermost stride is 1. Tensors need their
  *     element's alignment, no more (a workspace 8 bytes).
- *     (un_adamw_create and _destroy allocate and free: not while a capture is on.)
  *   - Errors are read with un_last_error(NULL) on the calling thread. A refused
  *     call enqueues nothing.
  * ------------------------------------------------------------------------- */
