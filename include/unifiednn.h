@@ -492,6 +492,57 @@ typedef struct {
 un_status un_rms_norm_backward(const un_rms_norm_grad_args* a, void* stream);
 un_status un_rms_norm_workspace(int32_t type, int64_t rows, int32_t width, size_t* bytes);
 
+/* Layer norm of `rows` rows of `width` values (1 <= width <= 16384), with the
+ * addition of a residual before it:
+ *   s = x + residual, rounded to the type (s = x without a residual),
+ *   m = mean(s),  q = 1 / sqrt(mean((s - m)^2) + eps),  y = (s - m) q weight + bias.
+ * sum may be x or residual itself (same stride). */
+typedef struct {
+  int32_t type;              /* un_type of x, residual, sum, y */
+  int32_t width;
+  int64_t rows;
+  float eps;                 /* >= 0 */
+  const void* x;
+  int64_t ldx;
+  const void* residual;      /* NULL: none */
+  int64_t ldr;
+  const float *weight, *bias;/* [width]; bias NULL: none */
+  void* sum;                 /* NULL: not stored */
+  int64_t lds;
+  void* y;
+  int64_t ldy;
+  float* stats;              /* [rows][2], m and q; NULL: not stored; un_layer_norm_backward reads it */
+} un_layer_norm_args;
+un_status un_layer_norm(const un_layer_norm_args* a, void* stream);
+
+/* Its gradients, from dy at y, the stored sum s and stats, with h = (s - m) q:
+ *   dx = ds + q (dy weight - mean(dy weight) - h mean(dy weight h)) at x and at the
+ *   residual alike (ds: the gradient that reaches s on other ways; NULL: none),
+ *   dweight = sum over the rows of dy h and dbias = sum over the rows of dy (in a
+ *   fixed order).
+ * dx may be ds or dy itself (same stride). workspace: as many bytes as
+ * un_layer_norm_workspace says. */
+typedef struct {
+  int32_t type;              /* of dy, s, ds, dx */
+  int32_t width;
+  int64_t rows;
+  const void* dy;
+  int64_t lddy;
+  const void* s;
+  int64_t lds;
+  const float* weight;
+  const float* stats;
+  const void* ds;
+  int64_t ldds;
+  void* dx;                  /* NULL: not wanted */
+  int64_t lddx;
+  float *dweight, *dbias;    /* [width], overwritten; dbias NULL: not wanted */
+  void* workspace;
+  size_t workspace_bytes;
+} un_layer_norm_grad_args;
+un_status un_layer_norm_backward(const un_layer_norm_grad_args* a, void* stream);
+un_status un_layer_norm_workspace(int32_t type, int64_t rows, int32_t width, size_t* bytes);
+
 /* Gated linear recurrence, per sequence and channel:
  *   a_t = sigmoid(gate_t),  h_t = a_t h_{t-1} + (1 - a_t) value_t,  t = 1 .. tokens.
  * gate and value are [batch][tokens][width] with the same strides (the two halves

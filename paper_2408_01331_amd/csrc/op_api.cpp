@@ -142,6 +142,82 @@ un_status un_rms_norm_backward(const un_rms_norm_grad_args* a, void* stream) {
 }
 
 // ---------------------------------------------------------------------------
+// Layer norm
+// ---------------------------------------------------------------------------
+un_status un_layer_norm(const un_layer_norm_args* a, void* stream) {
+  const char* F = "un_layer_norm";
+  if (!a) return bad(F, "args is NULL");
+  if (!type_ok(a->type)) return bad(F, "unknown type");
+  if (a->rows < 0 || a->width < 1) return bad(F, "rows >= 0 and width >= 1 expected");
+  if (a->width > NORM_MAX_D) return bad(F, "width above 16384 is not supported", UN_ERR_UNSUPPORTED);
+  if (!(a->eps >= 0.f) || !std::isfinite(a->eps)) return bad(F, "eps must be finite and >= 0");
+  if (a->rows == 0) return UN_OK;
+  if (!a->x || !a->weight || !a->y) return bad(F, "x, weight or y is NULL");
+  const int64_t d = a->width;
+  if (a->rows > 1 && (a->ldx < d || a->ldy < d || (a->residual && a->ldr < d) || (a->sum && a->lds < d)))
+    return bad(F, "a row stride is smaller than the width");
+  const NormPlan plan = norm_plan(a->type == UN_TYPE_BF16, a->width);
+  if (too_many((a->rows + plan.group - 1) / plan.group, 256 > plan.tpr ? 256 : plan.tpr)) return bad(F, "too many rows", UN_ERR_UNSUPPORTED);
+  LayerProb p{};
+  p.x = a->x;
+  p.ldx = a->ldx;
+  p.r = a->residual;
+  p.ldr = a->ldr;
+  p.w = a->weight;
+  p.b = a->bias;
+  p.s = a->sum;
+  p.lds = a->lds;
+  p.y = a->y;
+  p.ldy = a->ldy;
+  p.stats = a->stats;
+  p.rows = a->rows;
+  p.d = a->width;
+  p.eps = a->eps;
+  return enqueue(F, stream, [&](hipStream_t s) { return launch_layer(a->type == UN_TYPE_BF16, plan, p, s); });
+}
+
+un_status un_layer_norm_workspace(int32_t type, int64_t rows, int32_t width, size_t* bytes) {
+  const char* F = "un_layer_norm_workspace";
+  if (!bytes) return bad(F, "bytes is NULL");
+  if (!type_ok(type)) return bad(F, "unknown type");
+  if (rows < 0 || width < 1) return bad(F, "rows >= 0 and width >= 1 expected");
+  if (width > NORM_MAX_D) return bad(F, "width above 16384 is not supported", UN_ERR_UNSUPPORTED);
+  *bytes = (size_t)norm_blocks(norm_plan(type == UN_TYPE_BF16, width), rows) * width * 8;
+  return UN_OK;
+}
+
+un_status un_layer_norm_backward(const un_layer_norm_grad_args* a, void* stream) {
+  const char* F = "un_layer_norm_backward";
+  if (!a) return bad(F, "args is NULL");
+  size_t need = 0;
+  const un_status st = un_layer_norm_workspace(a->type, a->rows, a->width, &need);
+  if (st != UN_OK) return st;
+  if (!a->dweight || !a->weight) return bad(F, "weight or dweight is NULL");
+  if (a->rows > 0 && (!a->dy || !a->s || !a->stats)) return bad(F, "dy, s or stats is NULL");
+  const int64_t d = a->width;
+  if (a->rows > 1 && (a->lddy < d || a->lds < d || (a->ds && a->ldds < d) || (a->dx && a->lddx < d)))
+    return bad(F, "a row stride is smaller than the width");
+  if (a->workspace_bytes < need || !a->workspace) return bad(F, "workspace too small (un_layer_norm_workspace)", UN_ERR_BUFSIZE);
+  const NormPlan plan = norm_plan(a->type == UN_TYPE_BF16, a->width);
+  LayerProb p{};
+  p.x = a->s;
+  p.ldx = a->lds;
+  p.r = a->ds;
+  p.ldr = a->ldds;
+  p.dy = a->dy;
+  p.lddy = a->lddy;
+  p.w = a->weight;
+  p.y = a->dx;
+  p.ldy = a->lddx;
+  p.stats = const_cast<float*>(a->stats);
+  p.part = (float*)a->workspace;
+  p.rows = a->rows;
+  p.d = a->width;
+  p.blocks = norm_blocks(plan, a->rows);
+  return enqueue(F, stream, [&](hipStream_t s) { return launch_layer_bwd(a->type == UN_TYPE_BF16, plan, p, a->dweight, a->dbias, s); });
+}
+
+// ---------------------------------------------------------------------------
 // Gated linear recurrence
 // ---------------------------------------------------------------------------
 namespace {

@@ -1,5 +1,5 @@
-// Descriptors and launch plans of the operators on device tensors (RMS norm,
-// gated linear recurrence, multi-tensor AdamW), shared by their kernels
+// Descriptors and launch plans of the operators on device tensors (RMS norm, layer
+// norm, gated linear recurrence, multi-tensor AdamW), shared by their kernels
 // (operators.hip), their C entries (op_api.cpp) and the step's planner
 // (un_api.cpp), which runs the same kernels over tables of problems.
 #pragma once
@@ -55,6 +55,31 @@ hipError_t launch_norm_table(bool bf16, bool bwd, const NormPlan& plan, const No
                              int64_t wsoff, hipStream_t s);
 // dw[j] = sum over the partials, in order
 hipError_t launch_norm_dw(const float* part, int nparts, int d, float* dw, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// Layer norm:  s = x + r (rounded to the type), m = mean(s),
+// q = 1 / sqrt(mean((s - m)^2) + eps),  h = (s - m) q,  y = h w + b.
+// Backward: dx = ds + q (dy w - mean(dy w) - h mean(dy w h)), dw = sum over rows
+// of dy h, db = sum over rows of dy.
+// ---------------------------------------------------------------------------
+struct LayerProb {
+  const void* x;       // forward: input; backward: the stored sum s
+  const void* r;       // forward: residual (null: none); backward: the gradient ds at s from elsewhere (null: none)
+  const void* dy;      // backward
+  const float *w, *b;  // b: null: none
+  void* s;             // forward: the sum (null: not stored)
+  void* y;             // forward: output; backward: dx (null: not wanted)
+  float* stats;        // m and q per row, side by side (forward, null: not stored)
+  float* part;         // backward: partial gradients [blocks][2][d], of the weight and of the bias
+  int64_t ldx, ldr, lddy, lds, ldy;
+  int64_t rows;
+  int32_t d;
+  int32_t blocks;      // backward: workgroups
+  float eps;
+};
+hipError_t launch_layer(bool bf16, const NormPlan& plan, const LayerProb& p, hipStream_t s);
+// and the gradients from the partials (db null: not wanted)
+hipError_t launch_layer_bwd(bool bf16, const NormPlan& plan, const LayerProb& p, float* dw, float* db, hipStream_t s);
 
 // ---------------------------------------------------------------------------
 // Gated linear recurrence, per channel:  a_t = sigmoid(g_t),

@@ -1,5 +1,5 @@
-// gfx950 (CDNA4) kernels of the operators on device tensors: RMS norm, gated
-// linear recurrence, multi-tensor AdamW. All of them are bound by HBM: each
+// gfx950 (CDNA4) kernels of the operators on device tensors: RMS norm, layer norm,
+// gated linear recurrence, multi-tensor AdamW. All of them are bound by HBM: each
 // reads its operands once, in 16-byte (norm, AdamW) or whole-line (recurrence)
 // accesses, and keeps everything in between in registers.
 #include <hip/hip_runtime.h>
@@ -8,120 +8,12 @@
 #include <cmath>
 #include <type_traits>
 
+#include "op_device.h"
 #include "operators.h"
 
 namespace un {
 
-typedef uint16_t bf16_t;
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-// vectors at an element's alignment (rows of any stride): gfx950 takes such
-// global accesses as they are
-typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
-typedef u32x2 u32x2_a1 __attribute__((aligned(1)));
-typedef u32x2 u32x2_a2 __attribute__((aligned(2)));
-typedef uint32_t u32_a1 __attribute__((aligned(1)));
-typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
-
 namespace {
-
-__device__ __forceinline__ float bf2f(uint32_t h) { return __uint_as_float(h << 16); }
-__device__ __forceinline__ uint32_t f2bf(float f) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)f); }
-__device__ __forceinline__ uint32_t f2bf2(float lo, float hi) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){lo, hi}, bf16x2));
-}
-
-// A 16-byte vector of T as floats and back.
-template <typename T> struct V16;
-template <> struct V16<float> {
-  static constexpr int N = 4;
-  __device__ static void unpack(u32x4 v, float* f) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(v[e]);
-  }
-  __device__ static u32x4 pack(const float* f) {
-    u32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(f[e]);
-    return v;
-  }
-  __device__ static float load1(const float* p) { return *p; }
-  __device__ static void store1(float* p, float f) { *p = f; }
-};
-template <> struct V16<bf16_t> {
-  static constexpr int N = 8;
-  __device__ static void unpack(u32x4 v, float* f) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      f[2 * e] = __uint_as_float(v[e] << 16);
-      f[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
-    }
-  }
-  __device__ static u32x4 pack(const float* f) {
-    u32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = f2bf2(f[2 * e], f[2 * e + 1]);
-    return v;
-  }
-  __device__ static float load1(const bf16_t* p) { return bf2f(*p); }
-  __device__ static void store1(bf16_t* p, float f) { *p = (bf16_t)f2bf(f); }
-};
-
-// n (0 .. N) values to p
-template <typename T> __device__ __forceinline__ void store_vec(T* p, int n, const float* f) {
-  constexpr int N = V16<T>::N;
-  if (n == N) {
-    *(u32x4_a2*)p = V16<T>::pack(f);
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (e < n) V16<T>::store1(p + e, f[e]);
-  }
-}
-// n (0 .. N) values at p; the rest are zeros
-template <int N> __device__ __forceinline__ void load_f32(const float* p, int n, float* f) {
-  if (n == N) {
-#pragma unroll
-    for (int q = 0; q < N / 4; ++q) {
-      const f32x4 v = ((const f32x4_a4*)p)[q];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[4 * q + e] = v[e];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = e < n ? p[e] : 0.f;
-  }
-}
-
-// Reductions over the 16 lanes of a DPP row (quad swaps, then the halves of a
-// row mirrored), whose result every lane of the row has, and over a wave (the
-// four rows' values read to scalars, in order). No LDS traffic.
-template <typename F> __device__ __forceinline__ float row16(float v, F&& op) {
-  auto dpp = [](float x, auto ctrl) {
-    const int i = __float_as_int(x);
-    return __int_as_float(__builtin_amdgcn_update_dpp(i, i, decltype(ctrl)::value, 0xf, 0xf, false));
-  };
-  v = op(v, dpp(v, std::integral_constant<int, 0xB1>{}));   // quad_perm [1, 0, 3, 2]
-  v = op(v, dpp(v, std::integral_constant<int, 0x4E>{}));   // quad_perm [2, 3, 0, 1]
-  v = op(v, dpp(v, std::integral_constant<int, 0x141>{}));  // row_half_mirror
-  v = op(v, dpp(v, std::integral_constant<int, 0x140>{}));  // row_mirror
-  return v;
-}
-template <typename F> __device__ __forceinline__ float wave64(float v, F&& op) {
-  v = row16(v, op);
-  auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
-  return op(op(lane(0), lane(16)), op(lane(32), lane(48)));
-}
-struct Add {
-  __device__ float operator()(float a, float b) const { return a + b; }
-};
-struct Max {
-  __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
-};
-__device__ __forceinline__ float wave_max(float v) { return wave64(v, Max{}); }
 
 // v[r] <- the reduction over the TPR threads of a row (16: a DPP row, 64: a
 // wave, else the whole workgroup through `sm`, R floats per wave, in wave
@@ -407,9 +299,9 @@ __global__ __launch_bounds__(norm_threads(TPR)) void norm_bwd_table_kernel(const
 }
 
 // dw: 32 groups of 32 columns' threads, each adding a run of the partials, then
-// the groups in order
+// the groups in order. The columns from `split` on are db's.
 __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__ part, int nparts, int d,
-                                                       float* __restrict__ dw) {
+                                                       float* __restrict__ dw, float* __restrict__ db, int split) {
   __shared__ float sm[32][33];
   const int l = threadIdx.x & 31, c = blockIdx.x * 32 + l, g = threadIdx.x >> 5;
   const int per = (nparts + 31) / 32, k0 = g * per, k1 = min(nparts, k0 + per);
@@ -428,7 +320,184 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__
     a = 0.f;
 #pragma unroll
     for (int k = 0; k < 32; ++k) a += sm[k][l];
-    dw[c] = a;
+    if (c < split) dw[c] = a;
+    else if (db) db[c - split] = a;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Layer norm, on the RMS norm's layout of rows. The mean is taken first and the
+// squares are those of the centred values, from the registers: a mean that is large
+// against the spread costs no digits.
+// ---------------------------------------------------------------------------
+// n of a vector's values less m, the others 0
+template <int N> __device__ __forceinline__ void centre(float (&f)[N], int n, float m) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) f[e] = e < n ? f[e] - m : 0.f;
+}
+
+template <typename T, int TPR, int NV, bool ONCE>
+__global__ __launch_bounds__(norm_threads(TPR)) void layer_fwd_kernel(LayerProb p) {
+  constexpr int N = V16<T>::N;
+  __shared__ float sm[norm_sm<TPR, 1>()];
+  const int t = threadIdx.x & (TPR - 1), d = p.d;
+  const int64_t row = (int64_t)blockIdx.x * (norm_threads(TPR) / TPR) + threadIdx.x / TPR, at = row < p.rows ? row : 0;
+  int live[NV], flip = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) live[j] = row < p.rows ? min(max(d - (j * TPR + t) * N, 0), N) : 0;
+  RowVec<T, NV> x, r;
+  x.template load<ONCE>((const T*)p.x + at * p.ldx, live, TPR, t);
+  if (p.r) r.template load<ONCE>((const T*)p.r + at * p.ldr, live, TPR, t);
+  float sum[1] = {0.f};
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    float f[N];
+    x.get(j, f);
+    if (p.r) {
+      float g[N];
+      r.get(j, g);
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[e] += g[e];
+      x.raw[j] = V16<T>::pack(f);
+      x.get(j, f);  // the norm is that of the stored sum
+    }
+    if (p.s) store_vec<T>((T*)p.s + row * p.lds + (j * TPR + t) * N, live[j], f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[0] += f[e];
+  }
+  row_reduce<TPR, 1>(sum, Add{}, sm, flip);
+  x.forget();
+  const float mean = sum[0] / (float)d;
+  float sq[1] = {0.f};
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    float f[N];
+    x.get(j, f);
+    centre(f, live[j], mean);
+#pragma unroll
+    for (int e = 0; e < N; ++e) sq[0] = fmaf(f[e], f[e], sq[0]);
+  }
+  row_reduce<TPR, 1>(sq, Add{}, sm, flip);
+  x.forget();
+  const float q = 1.f / sqrtf(sq[0] / (float)d + p.eps);
+  if (p.stats && t == 0 && row < p.rows) {
+    p.stats[2 * row] = mean;
+    p.stats[2 * row + 1] = q;
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * TPR + t) * N;
+    float f[N], w[N], b[N];
+    load_f32<N>(p.w + c, live[j], w);
+    if (p.b) load_f32<N>(p.b + c, live[j], b);
+    x.get(j, f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = fmaf((f[e] - mean) * q, w[e], p.b ? b[e] : 0.f);
+    store_vec<T>((T*)p.y + row * p.ldy + c, live[j], f);
+  }
+}
+
+// Backward, as the RMS norm's: shares of dw and db per workgroup, joined in order by
+// a second launch.
+template <typename T, int TPR, int NV, int R, bool ONCE>
+__global__ __launch_bounds__(norm_threads(TPR)) void layer_bwd_kernel(LayerProb p) {
+  constexpr int N = V16<T>::N, NT = norm_threads(TPR), G = NT / TPR;
+  __shared__ float sm[norm_sm<TPR, 2 * R>()];
+  __shared__ float acc[norm_acc<T, TPR, NV>()];
+  const int t = threadIdx.x & (TPR - 1), g = threadIdx.x / TPR, d = p.d;
+  float w[NV][N], dw[NV][N], db[NV][N];
+  int cnt[NV], flip = 0;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * TPR + t) * N;
+    cnt[j] = min(max(d - c, 0), N);
+    load_f32<N>(p.w + c, cnt[j], w[j]);
+#pragma unroll
+    for (int e = 0; e < N; ++e) dw[j][e] = db[j][e] = 0.f;
+  }
+  const float invd = 1.f / (float)d;
+  for (int64_t r0 = (int64_t)blockIdx.x * (G * R); r0 < p.rows; r0 += (int64_t)p.blocks * (G * R)) {
+    RowVec<T, NV> s[R], dy[R], ds[R];
+    float mean[R], q[R], sum[2 * R];  // sums of dy w, then of dy w xhat
+    int live[R][NV];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const int64_t row = r0 + k * G + g, at = row < p.rows ? row : 0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) live[k][j] = row < p.rows ? cnt[j] : 0;
+      s[k].template load<ONCE>((const T*)p.x + at * p.ldx, live[k], TPR, t);
+      dy[k].template load<ONCE>((const T*)p.dy + at * p.lddy, live[k], TPR, t);
+      if (p.r) ds[k].template load<ONCE>((const T*)p.r + at * p.ldr, live[k], TPR, t);
+      mean[k] = row < p.rows ? p.stats[2 * at] : 0.f;
+      q[k] = row < p.rows ? p.stats[2 * at + 1] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      sum[k] = sum[R + k] = 0.f;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        float a[N], b[N];
+        s[k].get(j, a);
+        dy[k].get(j, b);
+        centre(a, live[k][j], mean[k]);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float gx = b[e] * (a[e] * q[k]);
+          dw[j][e] += gx;
+          db[j][e] += b[e];
+          sum[k] = fmaf(b[e], w[j][e], sum[k]);
+          sum[R + k] = fmaf(gx, w[j][e], sum[R + k]);
+        }
+      }
+    }
+    row_reduce<TPR, 2 * R>(sum, Add{}, sm, flip);
+    if (p.y) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        s[k].forget();
+        dy[k].forget();
+        const int64_t row = r0 + k * G + g;
+        const float c0 = sum[k] * invd, c1 = sum[R + k] * invd * q[k];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          float a[N], b[N], o[N];
+          s[k].get(j, a);
+          dy[k].get(j, b);
+          if (p.r) ds[k].get(j, o);
+#pragma unroll
+          for (int e = 0; e < N; ++e) o[e] = q[k] * (fmaf(b[e], w[j][e], -c0) - (a[e] - mean[k]) * c1) + (p.r ? o[e] : 0.f);
+          store_vec<T>((T*)p.y + row * p.ldy + (j * TPR + t) * N, live[k][j], o);
+        }
+      }
+    }
+  }
+  float* part = p.part + (int64_t)blockIdx.x * 2 * d;
+  if constexpr (G == 1) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < cnt[j]) {
+          part[(j * TPR + t) * N + e] = dw[j][e];
+          part[d + (j * TPR + t) * N + e] = db[j][e];
+        }
+  } else {
+    constexpr int ROW = TPR * NV * N;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (half) __syncthreads();
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[g * ROW + (j * TPR + t) * N + e] = half ? db[j][e] : dw[j][e];
+      __syncthreads();
+      for (int c = threadIdx.x; c < d; c += NT) {
+        float a = acc[c];
+#pragma unroll
+        for (int k = 1; k < G; ++k) a += acc[k * ROW + c];
+        part[half * d + c] = a;
+      }
+    }
   }
 }
 
@@ -610,7 +679,6 @@ __device__ __forceinline__ float join(const ScanProb& p, const Tile& t, int o, f
                                       : join_run<W, BWD, SCAN_LONG_RUN>(p, t, o, h, maps, sm);
 }
 
-template <int N> using Int = std::integral_constant<int, N>;
 enum class ScanForm { EACH, AHEAD, SPLIT };
 
 // Runs prepare(k, slot) and finish(k, slot) over nc chunks, k = first, first +
@@ -1106,7 +1174,6 @@ int norm_blocks(const NormPlan& p, int64_t rows) {
 
 namespace {
 // calls f with (element type, threads per row, vectors per thread) as constants
-constexpr int64_t LAST_LEVEL = (int64_t)256 << 20;  // bytes of the cache that all XCDs share
 template <typename F> hipError_t norm_pick(bool bf16, const NormPlan& p, F&& f) {
   auto nv = [&](auto type, auto tpr) {
     if (p.nv == 1) f(type, tpr, Int<1>{});
@@ -1161,7 +1228,31 @@ hipError_t launch_norm_table(bool bf16, bool bwd, const NormPlan& plan, const No
   });
 }
 hipError_t launch_norm_dw(const float* part, int nparts, int d, float* dw, hipStream_t s) {
-  hipLaunchKernelGGL(norm_dw_kernel, dim3((d + 31) / 32), dim3(1024), 0, s, part, nparts, d, dw);
+  hipLaunchKernelGGL(norm_dw_kernel, dim3((d + 31) / 32), dim3(1024), 0, s, part, nparts, d, dw, (float*)nullptr, d);
+  return hipGetLastError();
+}
+
+hipError_t launch_layer(bool bf16, const NormPlan& plan, const LayerProb& p, hipStream_t s) {
+  if (p.rows <= 0) return hipSuccess;
+  const bool once = p.rows * p.d * (bf16 ? 2 : 4) * ((p.r ? 2 : 1) + (p.s ? 2 : 1)) >= LAST_LEVEL;  // as the RMS norm's
+  return norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
+    using T = decltype(t);
+    const dim3 g((unsigned)((p.rows + plan.group - 1) / plan.group)), blk(norm_threads(tpr()));
+    if (once) hipLaunchKernelGGL((layer_fwd_kernel<T, tpr(), nv(), true>), g, blk, 0, s, p);
+    else hipLaunchKernelGGL((layer_fwd_kernel<T, tpr(), nv(), false>), g, blk, 0, s, p);
+  });
+}
+hipError_t launch_layer_bwd(bool bf16, const NormPlan& plan, const LayerProb& p, float* dw, float* db, hipStream_t s) {
+  const bool once = p.rows * p.d * (bf16 ? 2 : 4) * (p.r ? 4 : 3) >= LAST_LEVEL;
+  const hipError_t e = norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
+    using T = decltype(t);
+    constexpr int MANY = norm_rows<tpr(), nv()>();
+    const dim3 g(p.blocks), blk(norm_threads(tpr()));
+    if (once) hipLaunchKernelGGL((layer_bwd_kernel<T, tpr(), nv(), MANY, true>), g, blk, 0, s, p);
+    else hipLaunchKernelGGL((layer_bwd_kernel<T, tpr(), nv(), MANY, false>), g, blk, 0, s, p);
+  });
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(norm_dw_kernel, dim3((2 * p.d + 31) / 32), dim3(1024), 0, s, p.part, p.blocks, 2 * p.d, dw, db, p.d);
   return hipGetLastError();
 }
 

@@ -200,6 +200,66 @@ def rms_norm_backward(dy, s, weight, rstd, ds=None):
 
 
 # ---------------------------------------------------------------------------
+# Layer norm
+# ---------------------------------------------------------------------------
+@functools.lru_cache(maxsize=1024)
+def _layer_workspace(t, rows, width):
+    need = ctypes.c_size_t()
+    status = _lib().un_layer_norm_workspace(t, rows, width, _byref(need))
+    if status:
+        _un._check(status)
+    return need.value
+
+
+def layer_norm(x, weight, bias=None, residual=None, eps=1e-5, keep=False):
+    """(y, s, stats): s = x + residual in x's type (x itself without a residual),
+    y = (s - mean(s)) / sqrt(var(s) + eps) * weight + bias over the last axis. x:
+    [..., width] float32 or bfloat16; weight, bias: float32 [width]. stats (float32
+    [..., 2]: the mean and the reciprocal root, None unless `keep`) and s are what
+    layer_norm_backward needs."""
+    t, dev = _check_type(x, "x")
+    rows, ldx, xv = _rows(x, "x")
+    shape, dtype = x.shape, x.dtype
+    width = shape[-1]
+    _flat(weight, "weight", (width,), _F32, dev)
+    if bias is not None:
+        _flat(bias, "bias", (width,), _F32, dev)
+    rp, ldr, rv, sp, s = None, 0, None, None, x
+    if residual is not None:
+        rp, ldr, rv = _operand(residual, "residual", shape, dtype, dev)
+    _unrecorded(x, weight, bias, residual)
+    y = _fresh(x, dtype)
+    if residual is not None:
+        s = _fresh(x, dtype)
+        sp = s.data_ptr()
+    stats = weight.new_empty((*shape[:-1], 2)) if keep else None
+    _call(_lib().un_layer_norm, _un.un_layer_norm_args(t, width, rows, float(eps), xv.data_ptr(), ldx, rp, ldr, weight.data_ptr(),
+                                                       _ptr(bias), sp, width, y.data_ptr(), width, _ptr(stats)), dev)
+    return y, s, stats
+
+
+def layer_norm_backward(dy, s, weight, stats, ds=None):
+    """(dx, dweight, dbias) of layer_norm from the gradient dy at y, and ds at s
+    (None: s is used by nothing else). dx is the gradient at x and at the residual."""
+    t, dev = _check_type(s, "s")
+    rows, lds, sv = _rows(s, "s")
+    shape, dtype = s.shape, s.dtype
+    width = shape[-1]
+    dyp, lddy, dyv = _operand(dy, "dy", shape, dtype, dev)
+    _flat(weight, "weight", (width,), _F32, dev)
+    _flat(stats, "stats", (*shape[:-1], 2), _F32, dev)
+    dsp, ldds, dsv = (None, 0, None) if ds is None else _operand(ds, "ds", shape, dtype, dev)
+    _unrecorded(dy, s, weight, stats, ds)
+    dx, dw, db = _fresh(s, dtype), _empty_like(weight), _empty_like(weight)
+    need = _layer_workspace(t, rows, width)
+    ws = weight.new_empty(need // 4)
+    _call(_lib().un_layer_norm_backward, _un.un_layer_norm_grad_args(t, width, rows, dyp, lddy, sv.data_ptr(), lds, weight.data_ptr(),
+                                                                     stats.data_ptr(), dsp, ldds, dx.data_ptr(), width, dw.data_ptr(),
+                                                                     db.data_ptr(), ws.data_ptr(), need), dev)
+    return dx, dw, db
+
+
+# ---------------------------------------------------------------------------
 # Gated linear recurrence
 # ---------------------------------------------------------------------------
 def _strides(x, shape):

@@ -36,7 +36,8 @@ EXPORTS = ["un_create", "un_create_grouped", "un_plan_bytes", "un_plan_bytes_gro
            "un_set_params", "un_get_grads", "un_keep_grads", "un_param_count", "un_arena_bytes", "un_sync", "un_get_stream",
            "un_set_stream", "un_graph_capture", "un_graph_step", "un_step_scratch",
            "un_profile_enable", "un_profile_read", "un_destroy", "un_last_error",
-           "un_rms_norm", "un_rms_norm_backward", "un_rms_norm_workspace", "un_gated_scan", "un_gated_scan_backward",
+           "un_rms_norm", "un_rms_norm_backward", "un_rms_norm_workspace",
+           "un_layer_norm", "un_layer_norm_backward", "un_layer_norm_workspace", "un_gated_scan", "un_gated_scan_backward",
            "un_gated_scan_sizes", "un_adamw_create", "un_adamw_step", "un_adamw_destroy"]
 
 
@@ -72,6 +73,11 @@ un_rms_norm_args = _struct("un_rms_norm_args", type="i", width="i", rows="l", ep
 un_rms_norm_grad_args = _struct("un_rms_norm_grad_args", type="i", width="i", rows="l", dy="p", lddy="l", s="p", lds="l",
                                 weight="p", rstd="p", ds="p", ldds="l", dx="p", lddx="l", dweight="p", workspace="p",
                                 workspace_bytes="z")
+un_layer_norm_args = _struct("un_layer_norm_args", type="i", width="i", rows="l", eps="f", x="p", ldx="l", residual="p", ldr="l",
+                             weight="p", bias="p", sum="p", lds="l", y="p", ldy="l", stats="p")
+un_layer_norm_grad_args = _struct("un_layer_norm_grad_args", type="i", width="i", rows="l", dy="p", lddy="l", s="p", lds="l",
+                                  weight="p", stats="p", ds="p", ldds="l", dx="p", lddx="l", dweight="p", dbias="p",
+                                  workspace="p", workspace_bytes="z")
 un_gated_scan_args = _struct("un_gated_scan_args", type="i", batch="i", tokens="i", width="i", gate="p", value="p", ld_in="l",
                              seq_in="l", lens="p", start="p", h="p", ld_h="l", seq_h="l", last="p", states="p",
                              workspace="p", workspace_bytes="z")
@@ -144,6 +150,9 @@ def lib():
             "un_rms_norm": (ctypes.c_int, [ctypes.POINTER(un_rms_norm_args), P]),
             "un_rms_norm_backward": (ctypes.c_int, [ctypes.POINTER(un_rms_norm_grad_args), P]),
             "un_rms_norm_workspace": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, c_size_p]),
+            "un_layer_norm": (ctypes.c_int, [ctypes.POINTER(un_layer_norm_args), P]),
+            "un_layer_norm_backward": (ctypes.c_int, [ctypes.POINTER(un_layer_norm_grad_args), P]),
+            "un_layer_norm_workspace": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, c_size_p]),
             "un_gated_scan": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_args), P]),
             "un_gated_scan_backward": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_grad_args), P]),
             "un_gated_scan_sizes": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, c_size_p, c_size_p]),
