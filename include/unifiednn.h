@@ -600,6 +600,47 @@ un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream)
  * workgroups than a launch holds (UN_ERR_UNSUPPORTED). */
 un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size_t* states, size_t* workspace_bytes);
 
+/* Embedding lookup: y_n = scale weight[token_n], rounded once, for `tokens` tokens and
+ * a table of vocab rows. A token outside [0, vocab) gets a row of zeros. */
+typedef struct {
+  int32_t type;              /* un_type of weight, y */
+  int32_t width, vocab;      /* >= 1; width up to 2^24 */
+  int32_t index_bits;        /* of a token: 32 or 64 (signed) */
+  int64_t tokens;            /* up to 2^30 */
+  const void* ids;           /* [tokens] */
+  const void* weight;        /* [vocab][width] */
+  int64_t ldw;
+  float scale;               /* finite */
+  void* y;                   /* [tokens][width] */
+  int64_t ldy;
+} un_embedding_args;
+un_status un_embedding(const un_embedding_args* a, void* stream);
+
+/* Its gradient: dweight[v] = scale * (the sum of dy_n over the n with token_n = v, in
+ * fp32 in a fixed order, which depends on `tokens` alone), rounded once; rows that no
+ * token names are zeros. accumulate != 0: added onto dweight instead, whose other rows
+ * stay as they are. Tokens equal to `padding` (negative: none) and tokens outside [0,
+ * vocab) have no gradient, and their rows of dy are not used. workspace: as many
+ * bytes as un_embedding_workspace says. */
+typedef struct {
+  int32_t type;              /* of dy, dweight */
+  int32_t width, vocab;
+  int32_t index_bits;
+  int64_t tokens;
+  const void* ids;
+  const void* dy;
+  int64_t lddy;
+  float scale;
+  int64_t padding;
+  void* dweight;             /* [vocab][width], overlaps nothing else */
+  int64_t lddw;
+  int32_t accumulate;
+  void* workspace;
+  size_t workspace_bytes;
+} un_embedding_grad_args;
+un_status un_embedding_backward(const un_embedding_grad_args* a, void* stream);
+un_status un_embedding_workspace(int64_t tokens, int32_t vocab, int32_t width, size_t* bytes);
+
 /* AdamW (decoupled weight decay) over many tensors in one launch. Per element,
  * fp32, at step t = 1, 2, ...:
  *   m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;

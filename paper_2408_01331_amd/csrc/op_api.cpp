@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "operators.h"
+#include "vocab.h"
 
 using namespace un;
 
@@ -324,6 +325,86 @@ un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream)
   p.T = a->tokens;
   p.d = a->width;
   return enqueue(F, stream, [&](hipStream_t s) { return launch_scan(a->type == UN_TYPE_BF16, true, plan, p, s); });
+}
+
+// ---------------------------------------------------------------------------
+// Embedding
+// ---------------------------------------------------------------------------
+namespace {
+constexpr int64_t MOST_TOKENS = (int64_t)1 << 30;
+
+un_status embed_ok(const char* F, int32_t type, int32_t width, int32_t vocab, int32_t index_bits, int64_t tokens) {
+  if (!type_ok(type)) return bad(F, "unknown type");
+  if (width < 1 || vocab < 1 || tokens < 0) return bad(F, "width >= 1, vocab >= 1 and tokens >= 0 expected");
+  if (index_bits != 32 && index_bits != 64) return bad(F, "index_bits must be 32 or 64");
+  if (vocab == INT32_MAX) return bad(F, "a vocabulary of 2^31 - 1 rows is not supported", UN_ERR_UNSUPPORTED);
+  if (width > (1 << 24)) return bad(F, "a width above 2^24 is not supported", UN_ERR_UNSUPPORTED);
+  if (tokens > MOST_TOKENS) return bad(F, "more than 2^30 tokens are not supported", UN_ERR_UNSUPPORTED);
+  // units of a wave: 256 columns (fp32) of a row each, and 16 rows of the table
+  if (too_many((tokens * ((width + 255) / 256) + vocab + 3) / 4 + 1, 256)) return bad(F, "too many tokens and columns", UN_ERR_UNSUPPORTED);
+  return UN_OK;
+}
+}  // namespace
+
+un_status un_embedding(const un_embedding_args* a, void* stream) {
+  const char* F = "un_embedding";
+  if (!a) return bad(F, "args is NULL");
+  const un_status st = embed_ok(F, a->type, a->width, a->vocab, a->index_bits, a->tokens);
+  if (st != UN_OK) return st;
+  if (!std::isfinite(a->scale)) return bad(F, "scale must be finite");
+  if (a->tokens == 0) return UN_OK;
+  if (!a->ids || !a->weight || !a->y) return bad(F, "ids, weight or y is NULL");
+  if ((a->vocab > 1 && a->ldw < a->width) || (a->tokens > 1 && a->ldy < a->width)) return bad(F, "a row stride is smaller than the width");
+  EmbedProb p{};
+  p.tokens = a->ids;
+  p.x = a->weight;
+  p.ldx = a->ldw;
+  p.y = a->y;
+  p.ldy = a->ldy;
+  p.n = a->tokens;
+  p.vocab = a->vocab;
+  p.d = a->width;
+  p.scale = a->scale;
+  p.wide = a->index_bits == 64;
+  return enqueue(F, stream, [&](hipStream_t s) { return launch_embed(a->type == UN_TYPE_BF16, p, s); });
+}
+
+un_status un_embedding_workspace(int64_t tokens, int32_t vocab, int32_t width, size_t* bytes) {
+  const char* F = "un_embedding_workspace";
+  if (!bytes) return bad(F, "bytes is NULL");
+  const un_status st = embed_ok(F, UN_TYPE_F32, width, vocab, 32, tokens);
+  if (st != UN_OK) return st;
+  *bytes = embed_plan(tokens, vocab, width).bytes;
+  return UN_OK;
+}
+
+un_status un_embedding_backward(const un_embedding_grad_args* a, void* stream) {
+  const char* F = "un_embedding_backward";
+  if (!a) return bad(F, "args is NULL");
+  const un_status st = embed_ok(F, a->type, a->width, a->vocab, a->index_bits, a->tokens);
+  if (st != UN_OK) return st;
+  if (!std::isfinite(a->scale)) return bad(F, "scale must be finite");
+  if (a->tokens == 0 && a->accumulate) return UN_OK;
+  if (!a->dweight || (a->tokens > 0 && (!a->ids || !a->dy))) return bad(F, "ids, dy or dweight is NULL");
+  if ((a->vocab > 1 && a->lddw < a->width) || (a->tokens > 1 && a->lddy < a->width)) return bad(F, "a row stride is smaller than the width");
+  const EmbedPlan plan = embed_plan(a->tokens, a->vocab, a->width);
+  if (plan.bytes && (!a->workspace || a->workspace_bytes < plan.bytes))
+    return bad(F, "workspace too small (un_embedding_workspace)", UN_ERR_BUFSIZE);
+  if (plan.bytes && (uintptr_t)a->workspace % 8) return bad(F, "workspace is not 8-byte aligned");
+  EmbedProb p{};
+  p.tokens = a->ids;
+  p.x = a->dy;
+  p.ldx = a->lddy;
+  p.y = a->dweight;
+  p.ldy = a->lddw;
+  p.n = a->tokens;
+  p.padding = a->padding;
+  p.vocab = a->vocab;
+  p.d = a->width;
+  p.scale = a->scale;
+  p.wide = a->index_bits == 64;
+  p.add = a->accumulate != 0;
+  return enqueue(F, stream, [&](hipStream_t s) { return launch_embed_bwd(a->type == UN_TYPE_BF16, plan, p, a->workspace, s); });
 }
 
 // ---------------------------------------------------------------------------

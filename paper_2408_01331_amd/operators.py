@@ -1,7 +1,9 @@
-"""Operators on device tensors: RMS norm, gated linear recurrence and AdamW
-over many tensors, forward, backward and single-token forms (the C calls
-un_rms_norm, un_gated_scan, un_adamw_step and their kin of include/unifiednn.h,
-which a context's step runs for its own layers and optimizers too).
+"""Operators on device tensors: RMS norm, layer norm, gated linear recurrence,
+embedding and AdamW over many tensors, forward, backward and single-token forms
+(the C calls un_rms_norm, un_layer_norm, un_gated_scan, un_embedding,
+un_adamw_step and their kin of include/unifiednn.h; a context's step runs the
+kernels of the RMS norm, the recurrence and AdamW for its own layers and
+optimizers too).
 
 Argument checks and marshalling only; the work runs in the library's HIP
 kernels, on torch's current stream of the tensors' device. A call allocates its
@@ -355,6 +357,83 @@ def gated_scan_backward(gate, value, states, dh, dlast=None, lens=None, out=None
                                                                      dg.data_ptr(), dv.data_ptr(), ldo, seqo, dh0.data_ptr(), _ptr(ws),
                                                                      n_ws), dev)
     return dh0 if given else (dg, dv, dh0)
+
+
+# ---------------------------------------------------------------------------
+# Embedding
+# ---------------------------------------------------------------------------
+_INDEX = {torch.int32: 32, torch.int64: 64}
+
+
+def _indices(x, name, dev, shape=None):
+    """(bits of an index, x to pass on) of a tensor of whole numbers, which is copied where it is not contiguous."""
+    if not (isinstance(x, torch.Tensor) and x.dtype in _INDEX and x.get_device() == dev and (shape is None or x.shape == shape)):
+        _require(isinstance(x, torch.Tensor), f"{name} must be a tensor")
+        _require(x.dtype in _INDEX, f"{name} must be int32 or int64, not {x.dtype}")
+        _require(x.get_device() == dev, f"{name} must be on cuda:{dev}, not {x.device}")
+        _require(False, f"{name} must have shape {tuple(shape)}, not {tuple(x.shape)}")
+    return _INDEX[x.dtype], x if x.is_contiguous() else x.contiguous()
+
+
+def _table(x, name, shape=None):
+    """(rows, width, row stride) of a tensor [rows, width] with a dense last axis."""
+    _require(x.dim() == 2 and x.shape[0] >= 1 and x.shape[1] >= 1, f"{name} must have shape [vocab, width], not {tuple(x.shape)}")
+    _dense(x, name)
+    rows, width = x.shape
+    ld = x.stride(0) if rows > 1 else width
+    _require(ld >= width, f"{name}'s rows must not overlap")
+    return rows, width, ld
+
+
+def embedding(tokens, weight, scale=1.0):
+    """scale * weight[tokens]: tokens of any shape, int32 or int64; weight: [vocab,
+    width] float32 or bfloat16. A token outside [0, vocab) gets zeros."""
+    t, dev = _check_type(weight, "weight")
+    vocab, width, ldw = _table(weight, "weight")
+    bits, ids = _indices(tokens, "tokens", dev)
+    _unrecorded(weight)
+    y = weight.new_empty((*ids.shape, width))
+    _call(_lib().un_embedding, _un.un_embedding_args(t, width, vocab, bits, ids.numel(), ids.data_ptr(), weight.data_ptr(), ldw,
+                                                     float(scale), y.data_ptr(), width), dev)
+    return y
+
+
+@functools.lru_cache(maxsize=1024)
+def _embed_workspace(tokens, vocab, width):
+    need = ctypes.c_size_t()
+    status = _lib().un_embedding_workspace(tokens, vocab, width, _byref(need))
+    if status:
+        _un._check(status)
+    return need.value
+
+
+def embedding_backward(dy, tokens, vocab, scale=1.0, padding=None, out=None):
+    """The gradient at embedding's weight, [vocab, width] in dy's type, from the
+    gradient dy at its output. Rows that no token names are zeros. out: a tensor of
+    that shape and type (its rows may be apart) onto which the gradient is added
+    instead, and which is returned. Tokens equal to `padding` have no gradient."""
+    t, dev = _check_type(dy, "dy")
+    bits, ids = _indices(tokens, "tokens", dev)
+    _require(dy.dim() == ids.dim() + 1 and dy.shape[:-1] == ids.shape, f"dy must have shape {(*ids.shape, 'width')}, not {tuple(dy.shape)}")
+    _, lddy, dyv = _rows(dy, "dy")
+    width = dy.shape[-1]
+    vocab = int(vocab)
+    _require(1 <= vocab < 1 << 31, f"vocab must be at least 1 and below 2^31, not {vocab}")
+    if out is not None:
+        _like(out, "out", torch.Size((vocab, width)), dy.dtype, dev)
+        _, _, lddw = _table(out, "out")
+    _unrecorded(dy, out)
+    need = _embed_workspace(ids.numel(), vocab, width)
+    given = out is not None
+    if given:
+        _written(out)
+    else:
+        out, lddw = dy.new_empty((vocab, width)), width
+    ws = dy.new_empty(need, dtype=torch.uint8)
+    _call(_lib().un_embedding_backward, _un.un_embedding_grad_args(t, width, vocab, bits, ids.numel(), ids.data_ptr(), dyv.data_ptr(), lddy,
+                                                                   float(scale), -1 if padding is None else int(padding),
+                                                                   out.data_ptr(), lddw, given, ws.data_ptr(), need), dev)
+    return out
 
 
 # ---------------------------------------------------------------------------

@@ -37,7 +37,8 @@ EXPORTS = ["un_create", "un_create_grouped", "un_plan_bytes", "un_plan_bytes_gro
            "un_set_stream", "un_graph_capture", "un_graph_step", "un_step_scratch",
            "un_profile_enable", "un_profile_read", "un_destroy", "un_last_error",
            "un_rms_norm", "un_rms_norm_backward", "un_rms_norm_workspace",
-           "un_layer_norm", "un_layer_norm_backward", "un_layer_norm_workspace", "un_gated_scan", "un_gated_scan_backward",
+           "un_layer_norm", "un_layer_norm_backward", "un_layer_norm_workspace",
+           "un_embedding", "un_embedding_backward", "un_embedding_workspace", "un_gated_scan", "un_gated_scan_backward",
            "un_gated_scan_sizes", "un_adamw_create", "un_adamw_step", "un_adamw_destroy"]
 
 
@@ -78,6 +79,11 @@ un_layer_norm_args = _struct("un_layer_norm_args", type="i", width="i", rows="l"
 un_layer_norm_grad_args = _struct("un_layer_norm_grad_args", type="i", width="i", rows="l", dy="p", lddy="l", s="p", lds="l",
                                   weight="p", stats="p", ds="p", ldds="l", dx="p", lddx="l", dweight="p", dbias="p",
                                   workspace="p", workspace_bytes="z")
+un_embedding_args = _struct("un_embedding_args", type="i", width="i", vocab="i", index_bits="i", tokens="l", ids="p", weight="p",
+                            ldw="l", scale="f", y="p", ldy="l")
+un_embedding_grad_args = _struct("un_embedding_grad_args", type="i", width="i", vocab="i", index_bits="i", tokens="l", ids="p",
+                                 dy="p", lddy="l", scale="f", padding="l", dweight="p", lddw="l", accumulate="i", workspace="p",
+                                 workspace_bytes="z")
 un_gated_scan_args = _struct("un_gated_scan_args", type="i", batch="i", tokens="i", width="i", gate="p", value="p", ld_in="l",
                              seq_in="l", lens="p", start="p", h="p", ld_h="l", seq_h="l", last="p", states="p",
                              workspace="p", workspace_bytes="z")
@@ -153,6 +159,9 @@ def lib():
             "un_layer_norm": (ctypes.c_int, [ctypes.POINTER(un_layer_norm_args), P]),
             "un_layer_norm_backward": (ctypes.c_int, [ctypes.POINTER(un_layer_norm_grad_args), P]),
             "un_layer_norm_workspace": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, c_size_p]),
+            "un_embedding": (ctypes.c_int, [ctypes.POINTER(un_embedding_args), P]),
+            "un_embedding_backward": (ctypes.c_int, [ctypes.POINTER(un_embedding_grad_args), P]),
+            "un_embedding_workspace": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, c_size_p]),
             "un_gated_scan": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_args), P]),
             "un_gated_scan_backward": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_grad_args), P]),
             "un_gated_scan_sizes": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, c_size_p, c_size_p]),

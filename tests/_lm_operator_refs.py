@@ -48,3 +48,30 @@ class LayerNorm:
         rows, hr, er = (t.reshape(-1, t.shape[-1]) for t in (dy, h, self.e_h))
         n = U32 * (rows.shape[0] + 40)
         return (dx, e, (rows * hr).sum(0), ((rows * hr).abs() * n + rows.abs() * er).sum(0), rows.sum(0), rows.abs().sum(0) * n)
+
+
+# ---------------------------------------------------------------------------
+# Embedding
+# ---------------------------------------------------------------------------
+def embedding(tokens, weight, scale):
+    """y, by definition: zeros for tokens outside the table."""
+    t, w = tokens.cpu().long(), d(weight)
+    there = (t >= 0) & (t < w.shape[0])
+    return torch.where(there[..., None], w[t.clamp(0, w.shape[0] - 1)] * scale, 0.0)
+
+
+def embedding_backward(dy, tokens, vocab, scale, padding, onto):
+    """(dweight, its bound): sums of up to `count` terms in fp32, the scale's product, and the addition onto what is there.
+    (The call holds the scale in fp32, which is off by up to u of it: one u more of the magnitudes.)"""
+    t, g = tokens.cpu().long().flatten(), d(dy).reshape(-1, dy.shape[-1])
+    keep = (t >= 0) & (t < vocab)
+    if padding is not None:
+        keep &= t != padding
+    t, g = t[keep], g[keep]
+    dw = torch.zeros(vocab, g.shape[1], dtype=torch.float64).index_add_(0, t, g) * scale
+    mag = torch.zeros_like(dw).index_add_(0, t, g.abs()) * abs(scale)
+    bound = mag * U32 * (torch.bincount(t, minlength=vocab).double()[:, None] + 3)
+    if onto is not None:
+        dw = dw + d(onto)
+        bound = bound + U32 * (d(onto).abs() + mag) * (mag > 0)
+    return dw, bound

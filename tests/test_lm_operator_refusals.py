@@ -74,3 +74,72 @@ def test_layer_norm_python():
         ops.layer_norm(x.half(), w)
     with pytest.raises(ValueError, match="s must be a tensor"):
         ops.layer_norm_backward(x, None, w, w)
+
+
+# ---------------------------------------------------------------------------
+# Embedding
+# ---------------------------------------------------------------------------
+EMBED = dict(type=0, width=64, vocab=10, index_bits=64, tokens=4, ids=P, weight=P, ldw=64, scale=1.0, y=P, ldy=64)
+EMBEDG = dict(type=1, width=64, vocab=10, index_bits=32, tokens=4, ids=P, dy=P, lddy=64, scale=1.0, padding=-1, dweight=P, lddw=64,
+              workspace=P, workspace_bytes=1 << 20)
+SIZES = [(dict(type=3), 1, "type"), (dict(width=0), 1, "width"), (dict(vocab=0), 1, "vocab"), (dict(tokens=-1), 1, "tokens"),
+         (dict(index_bits=16), 1, "index_bits"), (dict(vocab=(1 << 31) - 1), 7, "vocabulary"), (dict(tokens=(1 << 30) + 1), 7, "2^30"),
+         (dict(width=(1 << 24) + 1), 7, "2^24"), (dict(width=4096, tokens=1 << 30), 7, "too many"), (dict(scale=float("inf")), 1, "scale"),
+         (dict(ids=None), 1, "NULL")]
+
+
+@pytest.mark.parametrize("change,want,text", SIZES + [
+    (dict(weight=None), 1, "NULL"), (dict(y=None), 1, "NULL"), (dict(ldw=63), 1, "stride"), (dict(ldy=63), 1, "stride")])
+def test_embedding_refused(change, want, text):
+    refused("un_embedding", "un_embedding_args", EMBED, change, want, text)
+
+
+@pytest.mark.parametrize("change,want,text", SIZES + [
+    (dict(dy=None), 1, "NULL"), (dict(dweight=None), 1, "NULL"), (dict(lddw=63), 1, "stride"), (dict(lddy=63), 1, "stride"),
+    (dict(workspace=None), 6, "workspace"), (dict(workspace_bytes=10), 6, "workspace"), (dict(workspace=P + 4), 1, "aligned")])
+def test_embedding_backward_refused(change, want, text):
+    refused("un_embedding_backward", "un_embedding_grad_args", EMBEDG, change, want, text)
+
+
+def test_embedding_without_tokens():
+    L = U.lib()
+    assert L.un_embedding(ctypes.byref(U.un_embedding_args(**{**EMBED, "tokens": 0, "y": None})), None) == U.UN_OK
+    assert L.un_embedding_backward(ctypes.byref(U.un_embedding_grad_args(**{**EMBEDG, "tokens": 0, "accumulate": 1})), None) == U.UN_OK
+    for fn in ("un_embedding", "un_embedding_backward"):
+        assert getattr(L, fn)(None, None) == U.UN_ERR_INVALID
+
+
+def test_embedding_workspace():
+    b = ctypes.c_size_t(5)
+    assert U.lib().un_embedding_workspace(0, 10, 64, ctypes.byref(b)) == U.UN_OK and b.value == 0
+    assert U.lib().un_embedding_workspace(100, 10, 64, ctypes.byref(b)) == U.UN_OK and b.value >= 100 * 16
+    assert U.lib().un_embedding_workspace(100, 10, 0, ctypes.byref(b)) == U.UN_ERR_INVALID
+    assert U.lib().un_embedding_workspace(100, 10, 64, None) == U.UN_ERR_INVALID
+
+
+def test_embedding_python(monkeypatch):
+    from paper_2408_01331_amd import operators as ops
+    w, t = torch.zeros(5, 8), torch.zeros(3, dtype=torch.int64)
+    with pytest.raises(ValueError, match="GPU"):
+        ops.embedding(t, w)
+    monkeypatch.setattr(ops, "_check_type", lambda x, name: (0, -1))  # (a CPU tensor's device has the number -1)
+    with pytest.raises(ValueError, match=r"weight must have shape \[vocab, width\]"):
+        ops.embedding(t, w[0])
+    with pytest.raises(ValueError, match="rows must not overlap"):
+        ops.embedding(t, torch.zeros(8).expand(5, 8))
+    with pytest.raises(ValueError, match="last axis"):
+        ops.embedding(t, w.t())
+    with pytest.raises(ValueError, match="tokens must be int32 or int64"):
+        ops.embedding(t.float(), w)
+    with pytest.raises(ValueError, match="tokens must be a tensor"):
+        ops.embedding([1], w)
+    with pytest.raises(ValueError, match="requires a gradient"):
+        ops.embedding(t, w.clone().requires_grad_())
+    with pytest.raises(ValueError, match="dy must have shape"):
+        ops.embedding_backward(torch.zeros(4, 8), t, 5)
+    with pytest.raises(ValueError, match="vocab must be"):
+        ops.embedding_backward(torch.zeros(3, 8), t, 0)
+    with pytest.raises(ValueError, match="out must have shape"):
+        ops.embedding_backward(torch.zeros(3, 8), t, 5, out=torch.zeros(4, 8))
+    with pytest.raises(ValueError, match="out's rows must not overlap"):
+        ops.embedding_backward(torch.zeros(3, 8), t, 5, out=torch.zeros(8).expand(5, 8))
