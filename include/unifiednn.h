@@ -433,7 +433,7 @@ un_status un_profile_read(un_ctx* ctx, int32_t kernel_class, double* total_ms, i
  *     HIP graph, except un_adamw_step. (un_adamw_create and _destroy
  *     allocate and free memory: not while a capture is on.)
  *   - Strides are in elements; the innermost stride is 1. Tensors need their
- *     element's alignment, no more (a workspace 8 bytes).
+ *     element's alignment, no more (a workspace 8 bytes, of the losses over a vocabulary 16).
  *   - Errors are read with un_last_error(NULL) on the calling thread. A refused
  *     call enqueues nothing.
  * ------------------------------------------------------------------------- */
@@ -640,6 +640,123 @@ typedef struct {
 } un_embedding_grad_args;
 un_status un_embedding_backward(const un_embedding_grad_args* a, void* stream);
 un_status un_embedding_workspace(int64_t tokens, int32_t vocab, int32_t width, size_t* bytes);
+
+/* Softmax cross entropy over a vocabulary, from the last hidden states: with z = x
+ * weight^T (fp32 sums; no more of z than a tile exists at any time),
+ *   lse_n = log(sum over v of exp(z_nv)),  loss_n = lse_n - z_n[target_n]  (>= 0).
+ * A row whose target is `ignore` or outside [0, vocab) is left out: loss and lse are 0,
+ * its x is not used, and it costs next to nothing. fp32 operands are multiplied as three
+ * bf16 terms each (products to 2^-24 of the terms' size); a value that is not finite
+ * makes the sums that it enters not finite or NaN. workspace: as many bytes as
+ * un_vocab_workspace says. */
+typedef struct {
+  int32_t type;              /* un_type of x, weight */
+  int32_t width, vocab;      /* width in [1, 65536], vocab >= 1 */
+  int32_t index_bits;        /* of a target: 32 or 64 (signed) */
+  int64_t rows;              /* up to 2^24 */
+  const void* x;             /* [rows][width] */
+  int64_t ldx;
+  const void* weight;        /* [vocab][width] */
+  int64_t ldw;
+  const void* targets;       /* [rows] */
+  int64_t ignore;
+  float *loss, *lse;         /* [rows] */
+  void* workspace;
+  size_t workspace_bytes;
+} un_vocab_loss_args;
+un_status un_vocab_loss(const un_vocab_loss_args* a, void* stream);
+
+/* Its gradients, from dloss at the losses and the forward call's lse, with z computed
+ * again in pieces of the vocabulary: g_n = dloss_n (softmax(z_n) - 1 at the target),
+ *   dx = g weight (zeros in the rows that are left out),  dweight = g^T x,
+ * summed in fp32 in a fixed order and rounded once; g itself enters the products as the
+ * operands do (in bf16: rounded to it). accumulate != 0: dweight is added onto what is
+ * there. dx and dweight must not overlap anything else. */
+typedef struct {
+  int32_t type;              /* of x, weight, dx, dweight */
+  int32_t width, vocab;
+  int32_t index_bits;
+  int64_t rows;
+  const void* x;
+  int64_t ldx;
+  const void* weight;
+  int64_t ldw;
+  const void* targets;
+  int64_t ignore;
+  const float* lse;          /* [rows] */
+  const float* dloss;        /* row n's at dloss[n * dloss_stride] (stride 0: one for all) */
+  int64_t dloss_stride;
+  void* dx;                  /* [rows][width] */
+  int64_t lddx;
+  void* dweight;             /* [vocab][width] */
+  int64_t lddw;
+  int32_t accumulate;
+  void* workspace;
+  size_t workspace_bytes;
+} un_vocab_loss_grad_args;
+un_status un_vocab_loss_backward(const un_vocab_loss_grad_args* a, void* stream);
+
+/* Distillation from a teacher's top logits. A row's entries are the k with an id in [0,
+ * vocab) and a logit above -inf; p = softmax(logits / T) over them, z = x weight^T / T:
+ *   lse_n = log(sum over v of exp(z_nv)),
+ *   loss_n = T^2 sum over the entries of p_k (log p_k - z_n[id_k] + lse_n).
+ * A row without entries is left out, as a row without a target is. An id that stands
+ * twice in a row counts twice. picked receives z at the entries, for the backward pass
+ * (0 elsewhere). */
+typedef struct {
+  int32_t type;              /* un_type of x, weight */
+  int32_t width, vocab;
+  int32_t index_bits;        /* of an id */
+  int64_t rows;
+  const void* x;
+  int64_t ldx;
+  const void* weight;
+  int64_t ldw;
+  int32_t top;               /* in [1, 128] */
+  int32_t logits_type;       /* un_type */
+  const void* ids;           /* [rows][top] */
+  const void* logits;        /* [rows][top] */
+  float temperature;         /* finite, > 0 */
+  float *loss, *lse;         /* [rows] */
+  float* picked;             /* [rows][top] */
+  void* workspace;
+  size_t workspace_bytes;
+} un_distill_loss_args;
+un_status un_distill_loss(const un_distill_loss_args* a, void* stream);
+
+/* Its gradients at x and weight (the teacher's logits get none), as
+ * un_vocab_loss_backward's with g_n = dloss_n T (softmax(z_n) - p_n). */
+typedef struct {
+  int32_t type;
+  int32_t width, vocab;
+  int32_t index_bits;
+  int64_t rows;
+  const void* x;
+  int64_t ldx;
+  const void* weight;
+  int64_t ldw;
+  int32_t top;
+  int32_t logits_type;
+  const void* ids;
+  const void* logits;
+  float temperature;
+  const float *lse, *picked; /* of the forward call */
+  const float* dloss;
+  int64_t dloss_stride;
+  void* dx;
+  int64_t lddx;
+  void* dweight;
+  int64_t lddw;
+  int32_t accumulate;
+  void* workspace;
+  size_t workspace_bytes;
+} un_distill_loss_grad_args;
+un_status un_distill_loss_backward(const un_distill_loss_grad_args* a, void* stream);
+/* Bytes of the workspace of these four calls. in_place != 0: for bf16 weights at a
+ * multiple of 16 bytes whose width and row stride are multiples of 8, the stride at most
+ * 2^20, which are read where they are; others are laid out in the workspace first. */
+un_status un_vocab_workspace(int32_t type, int64_t rows, int32_t width, int32_t vocab, int32_t in_place, int32_t backward,
+                             size_t* bytes);
 
 /* AdamW (decoupled weight decay) over many tensors in one launch. Per element,
  * fp32, at step t = 1, 2, ...:

@@ -15,7 +15,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libunifiednn.so")
 BUILD_DIR = os.path.join(PKG, "_build")
 
-SOURCES = ["kernels.hip", "operators.hip", "embed.hip", "un_api.cpp", "op_api.cpp"]
+SOURCES = ["kernels.hip", "operators.hip", "embed.hip", "head.hip", "un_api.cpp", "op_api.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,512 @@
+// gfx950 (CDNA4) kernels of the losses over a vocabulary: softmax cross entropy from
+// the last hidden states, and distillation from a teacher's top logits. The products
+// (head_gemm.h) take nearly all the time; what stands here numbers the rows that
+// count, lays the operands out, and finishes the rows.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "head_gemm.h"
+
+namespace un {
+
+namespace {
+
+__device__ __forceinline__ int64_t index_at(const void* p, int wide, int64_t i) {
+  return wide ? ((const int64_t*)p)[i] : (int64_t)((const int32_t*)p)[i];
+}
+
+struct HeadRows {
+  HeadCall c;
+  int32_t *map, *inv, *target, *live;   // [live] -> row; [row] -> number or -1; [live]
+  float *lse, *coef;                    // [live] (backward)
+  uint8_t* flag;                        // [row] (distillation)
+};
+
+// ---------------------------------------------------------------------------
+// A teacher's row, a wave's: lane l holds entries l and l + 64. An entry counts if its
+// id is in the vocabulary and its logit is not -inf.
+// ---------------------------------------------------------------------------
+struct Teacher {
+  int32_t id[2];      // -1: no entry
+  float u[2];         // logit / T
+  __device__ void load(const HeadCall& c, int64_t row) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = lane + 64 * h;
+      id[h] = -1;
+      u[h] = -INFINITY;
+      if (k < c.top) {
+        const int64_t at = row * c.top + k, i = index_at(c.ids, c.wide, at);
+        const float v = c.logits16 ? bf2f(((const bf16_t*)c.logits)[at]) : ((const float*)c.logits)[at];
+        if (i >= 0 && i < c.vocab && !(v == -INFINITY)) {
+          id[h] = (int32_t)i;
+          u[h] = v / c.temperature;
+        }
+      }
+    }
+  }
+  __device__ bool any() const { return __ballot(id[0] >= 0 || id[1] >= 0) != 0; }
+  // p and log p of the entries (0 and 0 elsewhere)
+  __device__ void softmax(float (&p)[2], float (&logp)[2]) const {
+    const float m = wave_max(fmaxf(u[0], u[1]));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) p[h] = id[h] >= 0 ? expf(u[h] - m) : 0.f;
+    const float sum = wave64(p[0] + p[1], Add{}), log_sum = logf(sum);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      logp[h] = id[h] >= 0 ? u[h] - m - log_sum : 0.f;
+      p[h] /= sum;
+    }
+  }
+};
+
+__global__ __launch_bounds__(256) void head_flag_kernel(HeadRows r) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= r.c.rows) return;
+  Teacher t;
+  t.load(r.c, row);
+  const bool any = t.any();
+  if ((threadIdx.x & 63) == 0) r.flag[row] = any;
+}
+
+// Numbers the rows that count, in order (one workgroup; 8 rows a thread at a time),
+// with what the products read of each. A row that does not count gets its zeros here.
+__global__ __launch_bounds__(1024) void head_rows_kernel(HeadRows r, int backward) {
+  constexpr int PER = 8;
+  __shared__ int32_t sums[16];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const HeadCall& c = r.c;
+  int32_t base = 0;
+  for (int64_t r0 = 0; r0 < c.rows; r0 += 1024 * PER) {
+    int32_t target[PER], count = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int64_t row = r0 + threadIdx.x * PER + k;
+      target[k] = -1;
+      if (row < c.rows) {
+        if (c.targets) {
+          const int64_t t = index_at(c.targets, c.wide, row);
+          if (t >= 0 && t < c.vocab && t != c.ignore) target[k] = (int32_t)t;
+        } else if (r.flag[row]) {
+          target[k] = 0;
+        }
+      }
+      count += target[k] >= 0;
+    }
+    int32_t run = count;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int32_t v = __shfl_up(run, o);
+      if (lane >= o) run += v;
+    }
+    if (lane == 63) sums[w] = run;
+    __syncthreads();
+    int32_t at = base + run - count;
+    for (int v = 0; v < 16; ++v) {
+      if (v < w) at += sums[v];
+      base += sums[v];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int64_t row = r0 + threadIdx.x * PER + k;
+      if (row >= c.rows) break;
+      const bool on = target[k] >= 0;
+      r.inv[row] = on ? at : -1;
+      if (on) {
+        r.map[at] = (int32_t)row;
+        r.target[at] = target[k];
+        if (backward) {
+          r.lse[at] = c.lse[row];
+          r.coef[at] = c.dloss[row * c.dloss_step] * c.temperature;
+        }
+        ++at;
+      } else if (!backward) {
+        c.loss[row] = 0.f;
+        c.lse[row] = 0.f;
+      }
+    }
+  }
+  if (threadIdx.x == 0) *r.live = base;
+}
+
+// Rows of 8-value chunks, bf16 or three bf16 planes of fp32, padded with zeros to `dp`
+// columns. live not null: the rows that count, then zeros up to the next HEAD_PAD.
+template <typename T> __global__ __launch_bounds__(256) void head_layout_kernel(const T* x, int64_t ld, int d, int64_t rows, const int32_t* map,
+                                                                               const int32_t* live, uint16_t* o, int64_t dp, int64_t plane) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = dp / 8;
+  const int64_t row = i / per;
+  const int c = (int)(i - row * per) * 8;
+  if (row >= rows) return;
+  const int64_t n = live ? *live : rows;
+  if (row >= (n + HEAD_PAD - 1) / HEAD_PAD * HEAD_PAD) return;
+  const int64_t from = row < n ? (map ? map[row] : row) : 0;
+  const int have = row < n ? min(max(d - c, 0), 8) : 0;
+  if constexpr (sizeof(T) == 2) {
+    u32x4 v = {0, 0, 0, 0};
+    const T* p = x + from * ld + c;
+    if (have == 8) v = *(const u32x4_a2*)p;
+    else
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < have) v[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+    *(u32x4*)(o + row * dp + c) = v;
+  } else {
+    float f[8];
+    load_f32<8>(x + from * ld + c, have, f);
+    uint32_t h[8][3];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) three_terms(f[e], h[e]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      *(u32x4*)(o + k * plane + row * dp + c) =
+          u32x4{h[0][k] | h[1][k] << 16, h[2][k] | h[3][k] << 16, h[4][k] | h[5][k] << 16, h[6][k] | h[7][k] << 16};
+  }
+}
+
+// The tiles' statistics of 16 rows, joined by 64 groups of their threads and then in
+// order: the rows' lse, and the cross entropy's loss.
+__global__ __launch_bounds__(1024) void head_finish_kernel(HeadRows r, const float2* stat, int tiles, int64_t ldn, const float* picked) {
+  __shared__ float2 sm[64][16];
+  const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const int live = *r.live;
+  if ((int64_t)blockIdx.x * 16 >= live) return;
+  const int64_t n = (int64_t)blockIdx.x * 16 + l;
+  float2 a{-INFINITY, 0.f};
+  for (int t = g; t < tiles; t += 64 * 4) {
+    float2 b[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) b[u] = t + 64 * u < tiles ? stat[(t + 64 * u) * ldn + n] : float2{-INFINITY, 0.f};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) a = join_stat(a, b[u]);
+  }
+  sm[g][l] = a;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    __syncthreads();
+    if (g < o) sm[g][l] = join_stat(sm[g][l], sm[g + o][l]);
+  }
+  if (g == 0 && n < live) {
+    a = sm[0][l];
+    const float lse = a.x + logf(a.y);
+    const int64_t row = r.map[n];
+    r.c.lse[row] = lse;
+    if (r.c.targets) {
+      const float loss = lse - picked[n];
+      r.c.loss[row] = loss < 0.f ? 0.f : loss;  // (the two sums of the same z round differently)
+    }
+  }
+}
+
+// Distillation, forward: a wave per row that counts. z at the entries by their own dot
+// products in fp32, and the loss T^2 sum p (log p - z + lse).
+template <typename T> __global__ __launch_bounds__(256) void head_distill_kernel(HeadRows r) {
+  constexpr int N = V16<T>::N, U = 4;  // entries at a time
+  const HeadCall& c = r.c;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= c.rows) return;
+  if (r.inv[row] < 0) {
+    for (int k = lane; k < c.top; k += 64) c.picked[row * c.top + k] = 0.f;
+    return;
+  }
+  Teacher t;
+  t.load(c, row);
+  float p[2], logp[2], z[2] = {0.f, 0.f};
+  t.softmax(p, logp);
+  const T* x = (const T*)c.x + row * c.ldx;
+  const T* w = (const T*)c.w;
+  for (int k0 = 0; k0 < c.top; k0 += U) {
+    int32_t id[U];
+    float dot[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u;
+      id[u] = k < c.top ? __builtin_amdgcn_readlane(k < 64 ? t.id[0] : t.id[1], k & 63) : -1;
+      dot[u] = 0.f;
+    }
+    for (int j = lane * N; j < c.width; j += 64 * N) {
+      const int have = min(c.width - j, N);
+      float f[N];
+      u32x4 raw[U];
+      auto load = [&](const T* q) {
+        if (have == N) return *(const u32x4_a2*)q;
+        float g[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) g[e] = e < have ? V16<T>::load1(q + e) : 0.f;
+        return (u32x4_a2)V16<T>::pack(g);
+      };
+      V16<T>::unpack(load(x + j), f);
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = id[u] >= 0 ? (u32x4)load(w + id[u] * c.ldw + j) : u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float g[N];
+        V16<T>::unpack(raw[u], g);
+#pragma unroll
+        for (int e = 0; e < N; ++e) dot[u] = fmaf(f[e], g[e], dot[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float s = wave64(dot[u], Add{}) / c.temperature;
+      if (id[u] >= 0 && lane == k0 + u) z[0] = s;
+      if (id[u] >= 0 && lane + 64 == k0 + u) z[1] = s;
+    }
+  }
+  const float lse = c.lse[row];
+  float sum = 0.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (lane + 64 * h < c.top) c.picked[row * c.top + lane + 64 * h] = z[h];
+    if (t.id[h] >= 0 && !(p[h] == 0.f)) sum = fmaf(p[h], logp[h] - z[h] + lse, sum);  // (p log p is 0 at p = 0)
+  }
+  sum = wave64(sum, Add{});
+  if (lane == 0) c.loss[row] = sum * (c.temperature * c.temperature);
+}
+
+// Distillation, backward: the entries of g in this piece, each from its own z in fp32
+// before it is rounded (q - p cancels where the student has learned the teacher's p).
+// An id that stands twice gets both shares, and both entries write the same value.
+__global__ __launch_bounds__(256) void head_entries_kernel(HeadRows r, uint16_t* g, int64_t ldg, int64_t gplane, int planes, int first, int count) {
+  const HeadCall& c = r.c;
+  const int64_t n = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (n >= *r.live) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = r.map[n];
+  Teacher t;
+  t.load(c, row);
+  float p[2], logp[2], share[2] = {0.f, 0.f};
+  t.softmax(p, logp);
+  for (int k = 0; k < c.top; ++k) {
+    const int32_t id = __builtin_amdgcn_readlane(k < 64 ? t.id[0] : t.id[1], k & 63);
+    const float q = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k < 64 ? p[0] : p[1]), k & 63));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) share[h] += id == t.id[h] ? q : 0.f;
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int v = t.id[h] - first;
+    if (t.id[h] < 0 || v < 0 || v >= count) continue;
+    const float q = expf(c.picked[row * c.top + lane + 64 * h] - r.lse[n]), f = r.coef[n] * (q - share[h]);
+    uint16_t* o = g + n * ldg + v;
+    if (planes == 1) {
+      *o = (uint16_t)f2bf(f);
+    } else {
+      uint32_t b[3];
+      three_terms(f, b);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) o[k * gplane] = (uint16_t)b[k];
+    }
+  }
+}
+
+// dx of every row: the parts of its number's sum in order, or zeros
+template <typename T> __global__ __launch_bounds__(256) void head_dx_kernel(HeadRows r, const float* part, int splits, int64_t ldn, int64_t ldd) {
+  const int per = (r.c.width + 3) / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+  if (row >= r.c.rows) return;
+  const int col = (int)(i - row * per) * 4, n = r.inv[row];
+  f32x4 a = {0.f, 0.f, 0.f, 0.f};
+  if (n >= 0) {
+    const float* p = part + n * ldd + col;
+    a = *(const f32x4*)p;
+    for (int s = 1; s < splits; ++s) a += *(const f32x4*)(p + s * ldn * ldd);
+  }
+  T* o = (T*)r.c.dx + row * r.c.lddx + col;
+  if (col + 4 <= r.c.width) {
+    if constexpr (sizeof(T) == 4) *(f32x4_a4*)o = a;
+    else *(u32x2_a2*)o = u32x2{f2bf2(a[0], a[1]), f2bf2(a[2], a[3])};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < r.c.width) V16<T>::store1(o + e, a[e]);
+  }
+}
+
+typedef HeadCfg<256, 128, 2, 2, 3> Wide;
+typedef HeadCfg<256, 64, 4, 1, 4> Narrow;
+
+template <HeadKind KIND> void head_launch(bool bf16, bool narrow, HeadProb& p, int64_t n, hipStream_t s) {
+  p.tiles_n = (int)((n + (narrow ? Narrow::bn : Wide::bn) - 1) / (narrow ? Narrow::bn : Wide::bn));
+  if constexpr (KIND == HEAD_DW) {
+    if (bf16) narrow ? head_go<KIND, Narrow, bf16_t>(p, s) : head_go<KIND, Wide, bf16_t>(p, s);
+    else narrow ? head_go<KIND, Narrow, float>(p, s) : head_go<KIND, Wide, float>(p, s);
+  } else {
+    narrow ? head_go<KIND, Narrow, bf16_t>(p, s) : head_go<KIND, Wide, bf16_t>(p, s);
+  }
+}
+
+}  // namespace
+
+constexpr int64_t HEAD_G_BYTES = (int64_t)512 << 20;   // of g's piece
+constexpr int HEAD_SLOTS = 512;                        // workgroups that run at once
+
+HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool in_place, bool backward) {
+  HeadPlan p{};
+  p.planes = bf16 ? 1 : 3;
+  auto up = [](int64_t x, int64_t m) { return (x + m - 1) / m * m; };
+  p.dp = up(width, HEAD_BK);
+  p.npad = up(rows, HEAD_PAD);
+  const int64_t mv = up(vocab, HEAD_BM), md = up(width, HEAD_BM) / HEAD_BM;
+  p.piece = mv;
+  if (backward && rows > 0) p.piece = std::min(mv, std::max<int64_t>(4096, HEAD_G_BYTES / (p.npad * 2 * p.planes) / HEAD_BM * HEAD_BM));
+  auto narrow = [&](int64_t tiles_m, int64_t n) { return n <= 64 || tiles_m * ((n + 63) / 64) <= HEAD_SLOTS; };
+  p.narrow[HEAD_STATS] = narrow(mv / HEAD_BM, rows);
+  p.narrow[HEAD_GRAD] = narrow(p.piece / HEAD_BM, rows);
+  p.narrow[HEAD_DX] = rows <= 64;
+  p.narrow[HEAD_DW] = narrow(md, p.piece);
+  p.splits = 1;
+  p.ldd = md * HEAD_BM;
+  if (backward && rows > 0) {
+    // as many parts of k as fill the card best; each at least 512 deep
+    const int64_t bn = p.narrow[HEAD_DX] ? 64 : 128, tiles = md * ((rows + bn - 1) / bn), most = std::max<int64_t>(1, p.piece / 512);
+    double best = 0;
+    for (int s = 1; s <= std::min<int64_t>(64, most); ++s) {
+      const int64_t n = tiles * s, rounds = (n + HEAD_SLOTS - 1) / HEAD_SLOTS;
+      const double use = (double)n / (rounds * HEAD_SLOTS) - 0.01 * s;
+      if (use > best) best = use, p.splits = s;
+    }
+  }
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t a = at;
+    at += (size_t)up(bytes, 256);
+    return a;
+  };
+  p.at_live = take(4);
+  p.at_map = take(rows * 4);
+  p.at_inv = take(rows * 4);
+  p.at_target = take(rows * 4);
+  p.at_flag = take(rows);
+  p.at_x = take(p.npad * p.dp * 2 * p.planes);
+  p.at_w = take(in_place ? 0 : (int64_t)vocab * p.dp * 2 * p.planes);
+  if (backward) {
+    p.at_lse = take(rows * 4);
+    p.at_coef = take(rows * 4);
+    p.at_g = take(p.npad * p.piece * 2 * p.planes);
+    p.at_part = take(p.splits * p.npad * p.ldd * 4);
+  } else {
+    p.at_picked = take(rows * 4);
+    p.at_stat = take(mv / HEAD_BM * p.npad * 8);
+  }
+  p.bytes = at;
+  return p;
+}
+
+hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, void* workspace, hipStream_t s) {
+  char* ws = (char*)workspace;
+  HeadRows r{};
+  r.c = c;
+  r.live = (int32_t*)(ws + plan.at_live);
+  r.map = (int32_t*)(ws + plan.at_map);
+  r.inv = (int32_t*)(ws + plan.at_inv);
+  r.target = (int32_t*)(ws + plan.at_target);
+  r.flag = (uint8_t*)(ws + plan.at_flag);
+  r.lse = (float*)(ws + plan.at_lse);
+  r.coef = (float*)(ws + plan.at_coef);
+  const bool distill = !c.targets;
+  auto grid = [](int64_t n) { return dim3((unsigned)n); };
+  if (distill && c.rows > 0) hipLaunchKernelGGL(head_flag_kernel, grid((c.rows + 3) / 4), dim3(256), 0, s, r);
+  hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(1024), 0, s, r, backward);
+  uint16_t *xs = (uint16_t*)(ws + plan.at_x), *wl = (uint16_t*)(ws + plan.at_w);
+  auto layout = [&](const void* from, int64_t ld, int64_t rows, const int32_t* map, const int32_t* live, uint16_t* to) {
+    const int64_t n = rows * (plan.dp / 8);
+    if (n <= 0) return;
+    if (c.bf16)
+      hipLaunchKernelGGL((head_layout_kernel<bf16_t>), grid((n + 255) / 256), dim3(256), 0, s, (const bf16_t*)from, ld, c.width, rows, map, live, to,
+                         plan.dp, rows * plan.dp);
+    else
+      hipLaunchKernelGGL((head_layout_kernel<float>), grid((n + 255) / 256), dim3(256), 0, s, (const float*)from, ld, c.width, rows, map, live, to,
+                         plan.dp, rows * plan.dp);
+  };
+  layout(c.x, c.ldx, plan.npad, r.map, r.live, xs);
+  const bool in_place = head_in_place(c.bf16, c.w, c.width, c.ldw);
+  if (!in_place && c.rows > 0) layout(c.w, c.ldw, c.vocab, nullptr, nullptr, wl);
+  const HeadOperand x{xs, plan.dp, plan.npad * plan.dp, plan.npad, (int32_t)plan.dp};
+  auto weights = [&](int64_t v0, int64_t n) {
+    if (in_place) return HeadOperand{(const uint16_t*)c.w + v0 * c.ldw, c.ldw, 0, n, c.width};
+    return HeadOperand{wl + v0 * plan.dp, plan.dp, (int64_t)c.vocab * plan.dp, n, (int32_t)plan.dp};
+  };
+  HeadProb base{};
+  base.pairs = c.bf16 ? 1 : 6;
+  base.live = r.live;
+  base.inv_t = 1.f / c.temperature;
+  base.splits = 1;
+  base.ldn = plan.npad;
+  base.target = distill ? nullptr : r.target;
+  const int md = (int)(plan.ldd / HEAD_BM);
+  if (!backward) {
+    HeadProb p = base;
+    p.a = weights(0, c.vocab);
+    p.b = x;
+    p.kb = (int)(plan.dp / HEAD_BK);
+    p.tiles_m = (int)((c.vocab + HEAD_BM - 1) / HEAD_BM);
+    p.vocab = c.vocab;
+    p.stat = (float2*)(ws + plan.at_stat);
+    p.picked = (float*)(ws + plan.at_picked);
+    head_launch<HEAD_STATS>(c.bf16, plan.narrow[HEAD_STATS], p, c.rows, s);
+    hipLaunchKernelGGL(head_finish_kernel, grid((c.rows + 15) / 16), dim3(1024), 0, s, r, p.stat, p.tiles_m, p.ldn, p.picked);
+    if (distill) {
+      if (c.bf16) hipLaunchKernelGGL((head_distill_kernel<bf16_t>), grid((c.rows + 3) / 4), dim3(256), 0, s, r);
+      else hipLaunchKernelGGL((head_distill_kernel<float>), grid((c.rows + 3) / 4), dim3(256), 0, s, r);
+    }
+    return hipGetLastError();
+  }
+  uint16_t* g = (uint16_t*)(ws + plan.at_g);
+  float* part = (float*)(ws + plan.at_part);
+  const int64_t gplane = plan.npad * plan.piece;
+  for (int64_t v0 = 0; v0 < c.vocab; v0 += plan.piece) {
+    const int64_t n = std::min<int64_t>(plan.piece, c.vocab - v0), padded = (n + HEAD_BM - 1) / HEAD_BM * HEAD_BM;
+    const HeadOperand gop{g, plan.piece, gplane, plan.npad, (int32_t)padded};
+    if (c.rows > 0) {
+      HeadProb p = base;
+      p.a = weights(v0, n);
+      p.b = x;
+      p.kb = (int)(plan.dp / HEAD_BK);
+      p.tiles_m = (int)(padded / HEAD_BM);
+      p.vocab = (int32_t)n;
+      p.first = (int32_t)v0;
+      p.lse = r.lse;
+      p.coef = r.coef;
+      p.g = g;
+      p.ldg = plan.piece;
+      p.gplane = gplane;
+      head_launch<HEAD_GRAD>(c.bf16, plan.narrow[HEAD_GRAD], p, c.rows, s);
+      if (distill)
+        hipLaunchKernelGGL(head_entries_kernel, grid((c.rows + 3) / 4), dim3(256), 0, s, r, g, plan.piece, gplane, plan.planes, (int)v0, (int)n);
+      HeadProb q = base;
+      q.a = weights(v0, n);
+      q.b = gop;
+      q.kb = (int)((n + HEAD_BK - 1) / HEAD_BK);
+      q.tiles_m = md;
+      q.splits = plan.splits;
+      q.per = (q.kb + plan.splits - 1) / plan.splits;
+      q.part = part;
+      q.ldd = plan.ldd;
+      q.add = v0 > 0;
+      head_launch<HEAD_DX>(c.bf16, plan.narrow[HEAD_DX], q, c.rows, s);
+    }
+    HeadProb q = base;
+    q.a = x;
+    q.b = gop;
+    q.tiles_m = md;
+    q.vocab = (int32_t)n;
+    q.out = (char*)c.dw + v0 * c.lddw * (c.bf16 ? 2 : 4);
+    q.ldo = c.lddw;
+    q.out_cols = c.width;
+    q.add = c.add;
+    q.vec = c.width % 4 == 0 && c.lddw % 4 == 0 && (uintptr_t)c.dw % (c.bf16 ? 8 : 16) == 0;
+    head_launch<HEAD_DW>(c.bf16, plan.narrow[HEAD_DW], q, n, s);
+  }
+  if (c.rows > 0) {
+    const int64_t n = c.rows * ((c.width + 3) / 4);
+    if (c.bf16) hipLaunchKernelGGL((head_dx_kernel<bf16_t>), grid((n + 255) / 256), dim3(256), 0, s, r, part, plan.splits, plan.npad, plan.ldd);
+    else hipLaunchKernelGGL((head_dx_kernel<float>), grid((n + 255) / 256), dim3(256), 0, s, r, part, plan.splits, plan.npad, plan.ldd);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace un

@@ -408,6 +408,145 @@ un_status un_embedding_backward(const un_embedding_grad_args* a, void* stream) {
 }
 
 // ---------------------------------------------------------------------------
+// Losses over a vocabulary
+// ---------------------------------------------------------------------------
+}  // extern "C"
+
+namespace {
+un_status head_sizes_ok(const char* F, int32_t type, int64_t rows, int32_t width, int32_t vocab) {
+  if (!type_ok(type)) return bad(F, "unknown type");
+  if (rows < 0 || width < 1 || vocab < 1) return bad(F, "rows >= 0, width >= 1 and vocab >= 1 expected");
+  if (width > HEAD_MAX_WIDTH) return bad(F, "a width above 65536 is not supported", UN_ERR_UNSUPPORTED);
+  if (rows > HEAD_MAX_ROWS) return bad(F, "more than 2^24 rows are not supported", UN_ERR_UNSUPPORTED);
+  if (vocab > (1 << 30)) return bad(F, "a vocabulary above 2^30 is not supported", UN_ERR_UNSUPPORTED);
+  // tiles of 256 x 64, and 8 values per thread of the layouts
+  const int64_t v = ((int64_t)vocab + 255) / 256, n = (rows + 63) / 64 + 4, w = ((int64_t)width + 31) / 32 * 4;
+  if (too_many(v * n + 8, 256) || too_many((vocab * w + 255) / 256, 256) || too_many(((rows + 256) * w + 255) / 256, 256))
+    return bad(F, "too many rows, columns or vocabulary", UN_ERR_UNSUPPORTED);
+  return UN_OK;
+}
+
+// what all four calls check and take over (A: their arguments)
+template <typename A> un_status head_common(const char* F, const A* a, bool backward, HeadCall* c, HeadPlan* plan) {
+  const un_status st = head_sizes_ok(F, a->type, a->rows, a->width, a->vocab);
+  if (st != UN_OK) return st;
+  if (a->index_bits != 32 && a->index_bits != 64) return bad(F, "index_bits must be 32 or 64");
+  if (a->rows > 0 && (!a->x || !a->weight || !a->lse)) return bad(F, "x, weight or lse is NULL");
+  if ((a->rows > 1 && a->ldx < a->width) || (a->vocab > 1 && a->ldw < a->width)) return bad(F, "a row stride is smaller than the width");
+  c->bf16 = a->type == UN_TYPE_BF16;
+  c->rows = a->rows;
+  c->width = a->width;
+  c->vocab = a->vocab;
+  c->x = a->x;
+  c->w = a->weight;
+  c->ldx = a->ldx;
+  c->ldw = a->ldw;
+  c->wide = a->index_bits == 64;
+  c->lse = const_cast<float*>(a->lse);
+  c->temperature = 1.f;
+  *plan = head_plan(c->bf16, a->rows, a->width, a->vocab, head_in_place(c->bf16, a->weight, a->width, a->ldw), backward);
+  if (a->rows == 0 && !backward) return UN_OK;
+  if (!a->workspace || a->workspace_bytes < plan->bytes) return bad(F, "workspace too small (un_vocab_workspace)", UN_ERR_BUFSIZE);
+  if ((uintptr_t)a->workspace % 16) return bad(F, "workspace is not 16-byte aligned");
+  return UN_OK;
+}
+template <typename A> un_status head_grads(const char* F, const A* a, HeadCall* c) {
+  if (!a->dweight || (a->rows > 0 && (!a->dloss || !a->dx))) return bad(F, "dloss, dx or dweight is NULL");
+  if (a->dloss_stride < 0) return bad(F, "a negative stride of dloss");
+  if ((a->rows > 1 && a->lddx < a->width) || (a->vocab > 1 && a->lddw < a->width)) return bad(F, "a row stride is smaller than the width");
+  c->dloss = a->dloss;
+  c->dloss_step = a->dloss_stride;
+  c->dx = a->dx;
+  c->lddx = a->lddx;
+  c->dw = a->dweight;
+  c->lddw = a->lddw;
+  c->add = a->accumulate != 0;
+  return UN_OK;
+}
+template <typename A> un_status head_teacher(const char* F, const A* a, HeadCall* c) {
+  if (a->top < 1) return bad(F, "top >= 1 expected");
+  if (a->top > HEAD_MAX_TOP) return bad(F, "more than 128 entries are not supported", UN_ERR_UNSUPPORTED);
+  if (!type_ok(a->logits_type)) return bad(F, "unknown type of the logits");
+  if (!std::isfinite(a->temperature) || !(a->temperature > 0.f)) return bad(F, "temperature must be finite and > 0");
+  if (a->rows > 0 && (!a->ids || !a->logits || !a->picked)) return bad(F, "ids, logits or picked is NULL");
+  c->top = a->top;
+  c->ids = a->ids;
+  c->logits = a->logits;
+  c->logits16 = a->logits_type == UN_TYPE_BF16;
+  c->temperature = a->temperature;
+  c->picked = const_cast<float*>(a->picked);
+  return UN_OK;
+}
+}  // namespace
+
+extern "C" {
+
+un_status un_vocab_workspace(int32_t type, int64_t rows, int32_t width, int32_t vocab, int32_t in_place, int32_t backward, size_t* bytes) {
+  const char* F = "un_vocab_workspace";
+  if (!bytes) return bad(F, "bytes is NULL");
+  const un_status st = head_sizes_ok(F, type, rows, width, vocab);
+  if (st != UN_OK) return st;
+  *bytes = head_plan(type == UN_TYPE_BF16, rows, width, vocab, in_place && type == UN_TYPE_BF16, backward != 0).bytes;
+  return UN_OK;
+}
+
+un_status un_vocab_loss(const un_vocab_loss_args* a, void* stream) {
+  const char* F = "un_vocab_loss";
+  if (!a) return bad(F, "args is NULL");
+  HeadCall c{};
+  HeadPlan plan;
+  const un_status st = head_common(F, a, false, &c, &plan);
+  if (st != UN_OK) return st;
+  if (a->rows == 0) return UN_OK;
+  if (!a->targets || !a->loss) return bad(F, "targets or loss is NULL");
+  c.targets = a->targets;
+  c.ignore = a->ignore;
+  c.loss = a->loss;
+  return enqueue(F, stream, [&](hipStream_t s) { return launch_head(plan, c, false, a->workspace, s); });
+}
+
+un_status un_vocab_loss_backward(const un_vocab_loss_grad_args* a, void* stream) {
+  const char* F = "un_vocab_loss_backward";
+  if (!a) return bad(F, "args is NULL");
+  HeadCall c{};
+  HeadPlan plan;
+  un_status st = head_common(F, a, true, &c, &plan);
+  if (st == UN_OK) st = head_grads(F, a, &c);
+  if (st != UN_OK) return st;
+  if (a->rows > 0 && !a->targets) return bad(F, "targets is NULL");
+  static const int32_t none = 0;
+  c.targets = a->targets ? a->targets : &none;  // (without rows nothing reads it)
+  c.ignore = a->ignore;
+  return enqueue(F, stream, [&](hipStream_t s) { return launch_head(plan, c, true, a->workspace, s); });
+}
+
+un_status un_distill_loss(const un_distill_loss_args* a, void* stream) {
+  const char* F = "un_distill_loss";
+  if (!a) return bad(F, "args is NULL");
+  HeadCall c{};
+  HeadPlan plan;
+  un_status st = head_common(F, a, false, &c, &plan);
+  if (st == UN_OK) st = head_teacher(F, a, &c);
+  if (st != UN_OK) return st;
+  if (a->rows == 0) return UN_OK;
+  if (!a->loss) return bad(F, "loss is NULL");
+  c.loss = a->loss;
+  return enqueue(F, stream, [&](hipStream_t s) { return launch_head(plan, c, false, a->workspace, s); });
+}
+
+un_status un_distill_loss_backward(const un_distill_loss_grad_args* a, void* stream) {
+  const char* F = "un_distill_loss_backward";
+  if (!a) return bad(F, "args is NULL");
+  HeadCall c{};
+  HeadPlan plan;
+  un_status st = head_common(F, a, true, &c, &plan);
+  if (st == UN_OK) st = head_teacher(F, a, &c);
+  if (st == UN_OK) st = head_grads(F, a, &c);
+  if (st != UN_OK) return st;
+  return enqueue(F, stream, [&](hipStream_t s) { return launch_head(plan, c, true, a->workspace, s); });
+}
+
+// ---------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------
 struct un_adamw {

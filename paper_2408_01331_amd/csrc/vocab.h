@@ -1,6 +1,6 @@
 // Descriptors and launches of the operators at a vocabulary's two ends: the
-// embedding lookup and its gradient (embed.hip). Shared by their kernels and their
-// C entries (op_api.cpp).
+// embedding lookup and its gradient (embed.hip), and the losses from the last hidden
+// states (head.hip). Shared by their kernels and their C entries (op_api.cpp).
 #pragma once
 #include <stdint.h>
 
@@ -47,5 +47,101 @@ struct EmbedPlan {
 EmbedPlan embed_plan(int64_t n, int32_t vocab, int32_t d);
 hipError_t launch_embed(bool bf16, const EmbedProb& p, hipStream_t s);
 hipError_t launch_embed_bwd(bool bf16, const EmbedPlan& plan, EmbedProb p, void* workspace, hipStream_t s);
+
+// ---------------------------------------------------------------------------
+// The losses over a vocabulary (head.hip). With z = x W^T / T of the rows that count
+// ("live": numbered c = 0 .. live - 1, in the rows' order),
+//   forward:  lse_c = log(sum over v of exp(z_cv));
+//   backward, for a loss whose gradient at z_c is coef_c (softmax(z_c) - p_c) with
+//     few p_cv that are not 0:  g = that,  dx = g W,  dW = g^T x.
+// z and g exist in pieces only: z in the accumulators of a tile, g in the workspace for
+// a piece of the vocabulary. All three products run on one kernel of bf16 matrix
+// instructions; fp32 operands enter as three bf16 terms whose sum they are, and six of
+// the nine products of terms (the others are below 2^-24 of the result's terms).
+// ---------------------------------------------------------------------------
+constexpr int HEAD_BK = 32;         // k of a block
+constexpr int HEAD_BM = 256;        // vocabulary (or hidden) columns of a tile
+constexpr int HEAD_PAD = 256;       // live rows are padded to this with zeros
+struct HeadOperand {
+  const uint16_t* p;                // bf16 [planes][rows][ld]
+  int64_t ld, plane, rows;
+  int32_t cols;
+};
+// products C[m][n] = sum over k of A(m, k) B(n, k); an operand's rows are m (n), its columns k, or, k-major, the other way
+enum HeadKind {
+  HEAD_STATS,   // A = W, B = x: maxima and sums of exponentials of each tile's part of a row, and z at the target
+  HEAD_GRAD,    // A = W, B = x: g
+  HEAD_DX,      // A = W (k-major), B = g: partial dx
+  HEAD_DW       // A = x (k-major), B = g (k-major): dW
+};
+struct HeadProb {
+  HeadOperand a, b;
+  int32_t kb;                       // k-blocks (HEAD_DW: counted from `live`)
+  int32_t pairs;                    // products of planes: 1 or 6
+  int32_t tiles_m, tiles_n;
+  int32_t splits, per;              // HEAD_DX: parts of k, and k-blocks of each
+  const int32_t* live;              // rows that count
+  int32_t vocab;                    // HEAD_STATS, HEAD_GRAD: rows of A (the piece's)
+  float inv_t;
+  const int32_t* target;            // [c], counted from the piece's first row; none: negative
+  float2* stat;                     // HEAD_STATS: [tiles_m][ldn]
+  float* picked;                    // HEAD_STATS: z at the target
+  const float *lse, *coef;          // HEAD_GRAD: [c]
+  int32_t first;                    // HEAD_GRAD: the piece's first row of the table
+  uint16_t* g;                      // HEAD_GRAD
+  int64_t ldg, gplane;
+  float* part;                      // HEAD_DX: [splits][ldn][ldd]
+  int64_t ldn, ldd;
+  void* out;                        // HEAD_DW: [rows of the piece][ldo]
+  int64_t ldo;
+  int32_t out_cols;
+  int32_t add, vec;                 // HEAD_DX, HEAD_DW: onto what is there; HEAD_DW: 4 values at a time are aligned
+};
+
+
+// A loss's call. Rows count by their target (CE), or by their teacher's entries.
+struct HeadCall {
+  bool bf16;
+  int64_t rows;
+  int32_t width, vocab;
+  const void *x, *w;
+  int64_t ldx, ldw;
+  int32_t wide;                     // indices of 64 bits
+  // cross entropy
+  const void* targets;              // null: distillation
+  int64_t ignore;
+  // distillation
+  int32_t top;
+  const void* ids;                  // [rows][top]
+  const void* logits;               // [rows][top], bf16 or fp32
+  bool logits16;
+  float temperature;                // 1 for cross entropy
+  float* picked;                    // [rows][top]: z / T at the entries (forward: written)
+  float *loss, *lse;                // [rows]; backward: lse read
+  // backward
+  const float* dloss;
+  int64_t dloss_step;
+  void *dx, *dw;
+  int64_t lddx, lddw;
+  bool add;                         // dW onto what is there
+};
+constexpr int HEAD_MAX_WIDTH = 1 << 16, HEAD_MAX_TOP = 128;
+constexpr int64_t HEAD_MAX_ROWS = (int64_t)1 << 24, HEAD_MAX_LD = (int64_t)1 << 20;
+// weights that the products read where they are; others are laid out in the workspace first
+inline bool head_in_place(bool bf16, const void* w, int32_t width, int64_t ldw) {
+  return bf16 && (uintptr_t)w % 16 == 0 && width % 8 == 0 && ldw % 8 == 0 && ldw <= HEAD_MAX_LD;
+}
+struct HeadPlan {
+  int planes;
+  int64_t dp, npad;                 // columns and rows of the laid-out hidden states
+  bool narrow[4];                   // by HeadKind: tiles of 64 columns, not 128
+  int64_t piece;                    // vocabulary of a piece
+  int splits;                       // HEAD_DX
+  int64_t ldd;
+  // offsets in the workspace
+  size_t at_map, at_inv, at_target, at_lse, at_coef, at_flag, at_live, at_x, at_w, at_stat, at_picked, at_g, at_part, bytes;
+};
+HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool in_place, bool backward);
+hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, void* workspace, hipStream_t s);
 
 }  // namespace un

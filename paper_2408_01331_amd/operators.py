@@ -1,9 +1,10 @@
 """Operators on device tensors: RMS norm, layer norm, gated linear recurrence,
-embedding and AdamW over many tensors, forward, backward and single-token forms
-(the C calls un_rms_norm, un_layer_norm, un_gated_scan, un_embedding,
-un_adamw_step and their kin of include/unifiednn.h; a context's step runs the
-kernels of the RMS norm, the recurrence and AdamW for its own layers and
-optimizers too).
+embedding, the losses over a vocabulary (cross entropy, distillation) and AdamW
+over many tensors, forward, backward and single-token forms (the C calls
+un_rms_norm, un_layer_norm, un_gated_scan, un_embedding, un_vocab_loss,
+un_distill_loss, un_adamw_step and their kin of include/unifiednn.h; a context's
+step runs the kernels of the RMS norm, the recurrence and AdamW for its own layers
+and optimizers too).
 
 Argument checks and marshalling only; the work runs in the library's HIP
 kernels, on torch's current stream of the tensors' device. A call allocates its
@@ -434,6 +435,152 @@ def embedding_backward(dy, tokens, vocab, scale=1.0, padding=None, out=None):
                                                                    float(scale), -1 if padding is None else int(padding),
                                                                    out.data_ptr(), lddw, given, ws.data_ptr(), need), dev)
     return out
+
+
+# ---------------------------------------------------------------------------
+# Losses over a vocabulary
+# ---------------------------------------------------------------------------
+@functools.lru_cache(maxsize=1024)
+def _head_workspace(t, rows, width, vocab, in_place, backward):
+    need = ctypes.c_size_t()
+    status = _lib().un_vocab_workspace(t, rows, width, vocab, in_place, backward, _byref(need))
+    if status:
+        _un._check(status)
+    return need.value
+
+
+def _head(x, weight):
+    """What the losses check of x [..., width] and weight [vocab, width]: (type, device, the rows' shape, the arguments of
+    both, what keeps x's rows alive)."""
+    t, dev = _check_type(x, "x")
+    _require(isinstance(weight, torch.Tensor), "weight must be a tensor")
+    _require(weight.dim() == 2, f"weight must have shape [vocab, width], not {tuple(weight.shape)}")
+    _like(weight, "weight", torch.Size((weight.shape[0], x.shape[-1])) if x.dim() else weight.shape, x.dtype, dev)
+    rows, ldx, xv = _rows(x, "x")
+    vocab, width, ldw = _table(weight, "weight")
+    return t, dev, x.shape[:-1], (rows, xv.data_ptr(), ldx, weight.data_ptr(), ldw), (vocab, width), xv
+
+
+def _head_ws(t, rows, width, vocab, w, ldw, backward, like):
+    in_place = t == 1 and w % 16 == 0 and width % 8 == 0 and ldw % 8 == 0 and ldw <= 1 << 20
+    need = _head_workspace(t, rows, width, vocab, in_place, backward)
+    return like.new_empty(need, dtype=torch.uint8), need
+
+
+def _head_out(weight, lead, dloss, out, dev):
+    """(dloss's address, its stride, dweight's row stride, what keeps dloss alive) of a backward call."""
+    step = 1
+    if isinstance(dloss, torch.Tensor) and dloss.dim() == 0:
+        step = 0
+        _flat(dloss, "dloss", (), _F32, dev)
+    elif not (isinstance(dloss, torch.Tensor) and dloss.dtype is _F32 and dloss.get_device() == dev and dloss.shape == lead
+              and dloss.is_contiguous()):
+        if isinstance(dloss, torch.Tensor) and not dloss.is_contiguous():
+            if dloss.dim() == 1:
+                step = dloss.stride(0)  # (0: expanded from one number)
+            else:
+                dloss = dloss.contiguous()
+        _require(isinstance(dloss, torch.Tensor), "dloss must be a tensor")
+        _require(dloss.get_device() == dev, f"dloss must be on cuda:{dev}, not {dloss.device}")
+        _require(dloss.dtype is _F32, f"dloss must be {_F32}, not {dloss.dtype}")
+        _require(dloss.shape == lead, f"dloss must have shape {tuple(lead)}, not {tuple(dloss.shape)}")
+    lddw = weight.shape[1]
+    if out is not None:
+        _like(out, "out", weight.shape, weight.dtype, dev)
+        _, _, lddw = _table(out, "out")
+    return dloss.data_ptr(), step, lddw, dloss
+
+
+def vocab_loss(x, weight, targets, ignore=-100):
+    """(loss, lse): softmax cross entropy of the logits x @ weight.T, which are never
+    stored, per row. x: [..., width], weight: [vocab, width], both float32 or both
+    bfloat16; targets: int32 or int64 [...]. loss, lse (log of the sum of the
+    exponentials, for vocab_loss_backward): float32 [...]. Rows whose target is
+    `ignore` or outside [0, vocab) are left out: zeros."""
+    t, dev, lead, (rows, xp, ldx, wp, ldw), (vocab, width), xv = _head(x, weight)
+    bits, targets = _indices(targets, "targets", dev, lead)
+    _unrecorded(x, weight)
+    loss = x.new_empty(lead, dtype=_F32)
+    lse = _empty_like(loss)
+    ws, need = _head_ws(t, rows, width, vocab, wp, ldw, 0, x)
+    _call(_lib().un_vocab_loss, _un.un_vocab_loss_args(t, width, vocab, bits, rows, xp, ldx, wp, ldw, targets.data_ptr(), int(ignore),
+                                                       loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), need), dev)
+    return loss, lse
+
+
+def vocab_loss_backward(x, weight, targets, lse, dloss, ignore=-100, out=None):
+    """(dx, dweight) of vocab_loss from the gradient dloss at the losses (float32, of
+    their shape, or one number's tensor for all rows). lse: as vocab_loss returned it.
+    out: a tensor of weight's shape and type (its rows may be apart) onto which
+    dweight is added instead, and which is returned."""
+    t, dev, lead, (rows, xp, ldx, wp, ldw), (vocab, width), xv = _head(x, weight)
+    bits, targets = _indices(targets, "targets", dev, lead)
+    _flat(lse, "lse", lead, _F32, dev)
+    dlp, step, lddw, dloss = _head_out(weight, lead, dloss, out, dev)
+    _unrecorded(x, weight, lse, dloss, out)
+    given = out is not None
+    dx = x.new_empty(x.shape)
+    if given:
+        _written(out)
+    else:
+        out = weight.new_empty(weight.shape)
+    ws, need = _head_ws(t, rows, width, vocab, wp, ldw, 1, x)
+    _call(_lib().un_vocab_loss_backward, _un.un_vocab_loss_grad_args(t, width, vocab, bits, rows, xp, ldx, wp, ldw, targets.data_ptr(),
+                                                                     int(ignore), lse.data_ptr(), dlp, step, dx.data_ptr(), width,
+                                                                     out.data_ptr(), lddw, given, ws.data_ptr(), need), dev)
+    return dx, out
+
+
+def _teacher(ids, logits, lead, dev):
+    _require(isinstance(ids, torch.Tensor) and ids.dim() == len(lead) + 1 and ids.shape[:-1] == lead,
+             f"ids must be a tensor of shape {(*lead, 'top')}")
+    bits, ids = _indices(ids, "ids", dev)
+    _require(isinstance(logits, torch.Tensor) and logits.dtype in _TYPES, "logits must be a float32 or bfloat16 tensor")
+    _like(logits, "logits", ids.shape, logits.dtype, dev)
+    return bits, ids, _TYPES[logits.dtype], logits if logits.is_contiguous() else logits.contiguous()
+
+
+def distill_loss(x, weight, ids, logits, temperature=1.0):
+    """(loss, lse, picked): temperature^2 KL(p, q) per row, of a teacher's p = softmax(
+    logits / temperature) over its `top` entries and the student's q = softmax(x @
+    weight.T / temperature) over the vocabulary. x, weight: as vocab_loss's; ids: int32
+    or int64 [..., top], logits: float32 or bfloat16 [..., top], top up to 128. Entries
+    with an id outside [0, vocab) or a logit of -inf do not count; a row without
+    entries is left out: zeros. lse and picked (float32 [..., top]) are what
+    distill_loss_backward needs."""
+    t, dev, lead, (rows, xp, ldx, wp, ldw), (vocab, width), xv = _head(x, weight)
+    bits, ids, lt, logits = _teacher(ids, logits, lead, dev)
+    _unrecorded(x, weight, logits)
+    loss = x.new_empty(lead, dtype=_F32)
+    lse, picked = _empty_like(loss), x.new_empty(ids.shape, dtype=_F32)
+    ws, need = _head_ws(t, rows, width, vocab, wp, ldw, 0, x)
+    _call(_lib().un_distill_loss, _un.un_distill_loss_args(t, width, vocab, bits, rows, xp, ldx, wp, ldw, ids.shape[-1], lt, ids.data_ptr(),
+                                                           logits.data_ptr(), float(temperature), loss.data_ptr(), lse.data_ptr(),
+                                                           picked.data_ptr(), ws.data_ptr(), need), dev)
+    return loss, lse, picked
+
+
+def distill_loss_backward(x, weight, ids, logits, lse, picked, dloss, temperature=1.0, out=None):
+    """(dx, dweight) of distill_loss (the teacher gets no gradient). lse, picked: as
+    distill_loss returned them; dloss, out: as vocab_loss_backward's."""
+    t, dev, lead, (rows, xp, ldx, wp, ldw), (vocab, width), xv = _head(x, weight)
+    bits, ids, lt, logits = _teacher(ids, logits, lead, dev)
+    _flat(lse, "lse", lead, _F32, dev)
+    _flat(picked, "picked", ids.shape, _F32, dev)
+    dlp, step, lddw, dloss = _head_out(weight, lead, dloss, out, dev)
+    _unrecorded(x, weight, logits, lse, picked, dloss, out)
+    given = out is not None
+    dx = x.new_empty(x.shape)
+    if given:
+        _written(out)
+    else:
+        out = weight.new_empty(weight.shape)
+    ws, need = _head_ws(t, rows, width, vocab, wp, ldw, 1, x)
+    _call(_lib().un_distill_loss_backward, _un.un_distill_loss_grad_args(t, width, vocab, bits, rows, xp, ldx, wp, ldw, ids.shape[-1], lt,
+                                                                         ids.data_ptr(), logits.data_ptr(), float(temperature),
+                                                                         lse.data_ptr(), picked.data_ptr(), dlp, step, dx.data_ptr(),
+                                                                         width, out.data_ptr(), lddw, given, ws.data_ptr(), need), dev)
+    return dx, out
 
 
 # ---------------------------------------------------------------------------

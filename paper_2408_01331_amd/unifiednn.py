@@ -38,7 +38,8 @@ EXPORTS = ["un_create", "un_create_grouped", "un_plan_bytes", "un_plan_bytes_gro
            "un_profile_enable", "un_profile_read", "un_destroy", "un_last_error",
            "un_rms_norm", "un_rms_norm_backward", "un_rms_norm_workspace",
            "un_layer_norm", "un_layer_norm_backward", "un_layer_norm_workspace",
-           "un_embedding", "un_embedding_backward", "un_embedding_workspace", "un_gated_scan", "un_gated_scan_backward",
+           "un_embedding", "un_embedding_backward", "un_embedding_workspace",
+           "un_vocab_loss", "un_vocab_loss_backward", "un_distill_loss", "un_distill_loss_backward", "un_vocab_workspace", "un_gated_scan", "un_gated_scan_backward",
            "un_gated_scan_sizes", "un_adamw_create", "un_adamw_step", "un_adamw_destroy"]
 
 
@@ -84,6 +85,14 @@ un_embedding_args = _struct("un_embedding_args", type="i", width="i", vocab="i",
 un_embedding_grad_args = _struct("un_embedding_grad_args", type="i", width="i", vocab="i", index_bits="i", tokens="l", ids="p",
                                  dy="p", lddy="l", scale="f", padding="l", dweight="p", lddw="l", accumulate="i", workspace="p",
                                  workspace_bytes="z")
+_head = dict(type="i", width="i", vocab="i", index_bits="i", rows="l", x="p", ldx="l", weight="p", ldw="l")
+_head_grads = dict(dloss="p", dloss_stride="l", dx="p", lddx="l", dweight="p", lddw="l", accumulate="i", workspace="p", workspace_bytes="z")
+un_vocab_loss_args = _struct("un_vocab_loss_args", **_head, targets="p", ignore="l", loss="p", lse="p", workspace="p", workspace_bytes="z")
+un_vocab_loss_grad_args = _struct("un_vocab_loss_grad_args", **_head, targets="p", ignore="l", lse="p", **_head_grads)
+_teacher = dict(top="i", logits_type="i", ids="p", logits="p", temperature="f")
+un_distill_loss_args = _struct("un_distill_loss_args", **_head, **_teacher, loss="p", lse="p", picked="p", workspace="p",
+                               workspace_bytes="z")
+un_distill_loss_grad_args = _struct("un_distill_loss_grad_args", **_head, **_teacher, lse="p", picked="p", **_head_grads)
 un_gated_scan_args = _struct("un_gated_scan_args", type="i", batch="i", tokens="i", width="i", gate="p", value="p", ld_in="l",
                              seq_in="l", lens="p", start="p", h="p", ld_h="l", seq_h="l", last="p", states="p",
                              workspace="p", workspace_bytes="z")
@@ -162,6 +171,12 @@ def lib():
             "un_embedding": (ctypes.c_int, [ctypes.POINTER(un_embedding_args), P]),
             "un_embedding_backward": (ctypes.c_int, [ctypes.POINTER(un_embedding_grad_args), P]),
             "un_embedding_workspace": (ctypes.c_int, [ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, c_size_p]),
+            "un_vocab_loss": (ctypes.c_int, [ctypes.POINTER(un_vocab_loss_args), P]),
+            "un_vocab_loss_backward": (ctypes.c_int, [ctypes.POINTER(un_vocab_loss_grad_args), P]),
+            "un_distill_loss": (ctypes.c_int, [ctypes.POINTER(un_distill_loss_args), P]),
+            "un_distill_loss_backward": (ctypes.c_int, [ctypes.POINTER(un_distill_loss_grad_args), P]),
+            "un_vocab_workspace": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                                  ctypes.c_int32, c_size_p]),
             "un_gated_scan": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_args), P]),
             "un_gated_scan_backward": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_grad_args), P]),
             "un_gated_scan_sizes": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, c_size_p, c_size_p]),
