@@ -647,7 +647,7 @@ un_status un_embedding_workspace(int64_t tokens, int32_t vocab, int32_t width, s
  * A row whose target is `ignore` or outside [0, vocab) is left out: loss and lse are 0,
  * its x is not used, and it costs next to nothing. fp32 operands are multiplied as three
  * bf16 terms each (products to 2^-24 of the terms' size); a value that is not finite
- * makes the sums that it enters not finite or NaN. workspace: as many bytes as
+ * makes the sums that it enters NaN. workspace: as many bytes as
  * un_vocab_workspace says. */
 typedef struct {
   int32_t type;              /* un_type of x, weight */
@@ -752,11 +752,8 @@ typedef struct {
   size_t workspace_bytes;
 } un_distill_loss_grad_args;
 un_status un_distill_loss_backward(const un_distill_loss_grad_args* a, void* stream);
-/* Bytes of the workspace of these four calls. in_place != 0: for bf16 weights at a
- * multiple of 16 bytes whose width and row stride are multiples of 8, the stride at most
- * 2^20, which are read where they are; others are laid out in the workspace first. */
-un_status un_vocab_workspace(int32_t type, int64_t rows, int32_t width, int32_t vocab, int32_t in_place, int32_t backward,
-                             size_t* bytes);
+/* Bytes of the workspace of these four calls. */
+un_status un_vocab_workspace(int32_t type, int64_t rows, int32_t width, int32_t vocab, int32_t backward, size_t* bytes);
 
 /* AdamW (decoupled weight decay) over many tensors in one launch. Per element,
  * fp32, at step t = 1, 2, ...:

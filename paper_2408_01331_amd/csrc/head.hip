@@ -132,17 +132,17 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(HeadRows r, int backwar
   if (threadIdx.x == 0) *r.live = base;
 }
 
-// Rows of 8-value chunks, bf16 or three bf16 planes of fp32, padded with zeros to `dp`
-// columns. live not null: the rows that count, then zeros up to the next HEAD_PAD.
+// The rows that count, in chunks of 8 values, as bf16 or three bf16 terms of fp32, padded
+// with zeros to `dp` columns and to the next HEAD_PAD rows.
 template <typename T> __global__ __launch_bounds__(256) void head_layout_kernel(const T* x, int64_t ld, int d, int64_t rows, const int32_t* map,
                                                                                const int32_t* live, uint16_t* o, int64_t dp, int64_t plane) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = dp / 8;
   const int64_t row = i / per;
   const int c = (int)(i - row * per) * 8;
   if (row >= rows) return;
-  const int64_t n = live ? *live : rows;
+  const int64_t n = *live;
   if (row >= (n + HEAD_PAD - 1) / HEAD_PAD * HEAD_PAD) return;
-  const int64_t from = row < n ? (map ? map[row] : row) : 0;
+  const int64_t from = row < n ? map[row] : 0;
   const int have = row < n ? min(max(d - c, 0), 8) : 0;
   if constexpr (sizeof(T) == 2) {
     u32x4 v = {0, 0, 0, 0};
@@ -156,13 +156,11 @@ template <typename T> __global__ __launch_bounds__(256) void head_layout_kernel(
   } else {
     float f[8];
     load_f32<8>(x + from * ld + c, have, f);
-    uint32_t h[8][3];
+    uint32_t h[4][3];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) three_terms(f[e], h[e]);
+    for (int e = 0; e < 4; ++e) three_terms2(f[2 * e], f[2 * e + 1], h[e]);
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
-      *(u32x4*)(o + k * plane + row * dp + c) =
-          u32x4{h[0][k] | h[1][k] << 16, h[2][k] | h[3][k] << 16, h[4][k] | h[5][k] << 16, h[6][k] | h[7][k] << 16};
+    for (int k = 0; k < 3; ++k) *(u32x4*)(o + k * plane + row * dp + c) = u32x4{h[0][k], h[1][k], h[2][k], h[3][k]};
   }
 }
 
@@ -296,7 +294,7 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadRows r, uint16_t*
       *o = (uint16_t)f2bf(f);
     } else {
       uint32_t b[3];
-      three_terms(f, b);
+      three_terms2(f, 0.f, b);
 #pragma unroll
       for (int k = 0; k < 3; ++k) o[k * gplane] = (uint16_t)b[k];
     }
@@ -326,48 +324,59 @@ template <typename T> __global__ __launch_bounds__(256) void head_dx_kernel(Head
   }
 }
 
-typedef HeadCfg<256, 128, 2, 2, 3> Wide;
-typedef HeadCfg<256, 64, 4, 1, 4> Narrow;
-
-template <HeadKind KIND> void head_launch(bool bf16, bool narrow, HeadProb& p, int64_t n, hipStream_t s) {
-  p.tiles_n = (int)((n + (narrow ? Narrow::bn : Wide::bn) - 1) / (narrow ? Narrow::bn : Wide::bn));
-  if constexpr (KIND == HEAD_DW) {
-    if (bf16) narrow ? head_go<KIND, Narrow, bf16_t>(p, s) : head_go<KIND, Wide, bf16_t>(p, s);
-    else narrow ? head_go<KIND, Narrow, float>(p, s) : head_go<KIND, Wide, float>(p, s);
-  } else {
-    narrow ? head_go<KIND, Narrow, bf16_t>(p, s) : head_go<KIND, Wide, bf16_t>(p, s);
-  }
-}
-
-}  // namespace
+typedef HeadCfg<256, 128, 2, 2, 3, 1> Large;
+typedef HeadCfg<128, 64, 2, 2, 4, 1> Small;
+typedef HeadCfg<128, 64, 2, 2, 2, 3> Terms;   // fp32
 
 constexpr int64_t HEAD_G_BYTES = (int64_t)512 << 20;   // of g's piece
 constexpr int HEAD_SLOTS = 512;                        // workgroups that run at once
 
-HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool in_place, bool backward) {
+template <HeadKind KIND, class C, typename T, bool REG> void head_go(HeadProb& p, int64_t m, int64_t n, hipStream_t s) {
+  p.tiles_m = (int)((m + C::bm - 1) / C::bm);
+  p.tiles_n = (int)((n + C::bn - 1) / C::bn);
+  const int64_t all = (int64_t)p.tiles_m * p.tiles_n * p.splits;
+  hipLaunchKernelGGL((head_kernel<KIND, C, T, REG>), dim3((unsigned)((all + 7) / 8 * 8)), dim3(C::waves * 64), 0, s, p);
+}
+// a product of m x n; direct: the weights' rows can be loaded directly
+template <HeadKind KIND> void head_launch(const HeadPlan& plan, bool direct, HeadProb& p, int64_t m, int64_t n, hipStream_t s) {
+  constexpr bool W = KIND != HEAD_DW;  // A is the weights
+  if (plan.planes == 3) head_go<KIND, Terms, float, W>(p, m, n, s);
+  else if (plan.small[KIND]) W && !direct ? head_go<KIND, Small, bf16_t, W>(p, m, n, s) : head_go<KIND, Small, bf16_t, false>(p, m, n, s);
+  else W && !direct ? head_go<KIND, Large, bf16_t, W>(p, m, n, s) : head_go<KIND, Large, bf16_t, false>(p, m, n, s);
+}
+
+}  // namespace
+
+HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool backward) {
   HeadPlan p{};
   p.planes = bf16 ? 1 : 3;
   auto up = [](int64_t x, int64_t m) { return (x + m - 1) / m * m; };
   p.dp = up(width, HEAD_BK);
   p.npad = up(rows, HEAD_PAD);
-  const int64_t mv = up(vocab, HEAD_BM), md = up(width, HEAD_BM) / HEAD_BM;
+  p.ldn = up(rows, Large::bn);
+  p.ldd = up(width, HEAD_BM);
+  const int64_t mv = up(vocab, HEAD_BM);
   p.piece = mv;
   if (backward && rows > 0) p.piece = std::min(mv, std::max<int64_t>(4096, HEAD_G_BYTES / (p.npad * 2 * p.planes) / HEAD_BM * HEAD_BM));
-  auto narrow = [&](int64_t tiles_m, int64_t n) { return n <= 64 || tiles_m * ((n + 63) / 64) <= HEAD_SLOTS; };
-  p.narrow[HEAD_STATS] = narrow(mv / HEAD_BM, rows);
-  p.narrow[HEAD_GRAD] = narrow(p.piece / HEAD_BM, rows);
-  p.narrow[HEAD_DX] = rows <= 64;
-  p.narrow[HEAD_DW] = narrow(md, p.piece);
+  // small tiles where there are few of them, or few rows
+  auto tiles = [](int64_t m, int64_t n, bool small) {
+    return small ? (m + Small::bm - 1) / Small::bm * ((n + Small::bn - 1) / Small::bn) : (m + Large::bm - 1) / Large::bm * ((n + Large::bn - 1) / Large::bn);
+  };
+  auto small = [&](int64_t m, int64_t n) { return !bf16 || n <= Small::bn || tiles(m, n, true) <= HEAD_SLOTS; };
+  p.small[HEAD_STATS] = small(vocab, rows);
+  p.small[HEAD_GRAD] = small(p.piece, rows);
+  p.small[HEAD_DX] = !bf16 || rows <= Small::bn;
+  p.small[HEAD_DW] = small(width, p.piece);
   p.splits = 1;
-  p.ldd = md * HEAD_BM;
   if (backward && rows > 0) {
-    // as many parts of k as fill the card best; each at least 512 deep
-    const int64_t bn = p.narrow[HEAD_DX] ? 64 : 128, tiles = md * ((rows + bn - 1) / bn), most = std::max<int64_t>(1, p.piece / 512);
-    double best = 0;
-    for (int s = 1; s <= std::min<int64_t>(64, most); ++s) {
-      const int64_t n = tiles * s, rounds = (n + HEAD_SLOTS - 1) / HEAD_SLOTS;
-      const double use = (double)n / (rounds * HEAD_SLOTS) - 0.01 * s;
-      if (use > best) best = use, p.splits = s;
+    // Parts of k: the time in units of a block, of the rounds that the card takes, each with what a tile costs beside its
+    // blocks, and of writing and reading the partial sums (4 bytes twice, some 2 MB in a block's time).
+    const int64_t n = tiles(width, rows, p.small[HEAD_DX]), kb = up(p.piece, HEAD_BK) / HEAD_BK;
+    double best = 1e30;
+    for (int s = 1; s <= 128 && s * 4 <= kb + 3; ++s) {
+      const int64_t rounds = (n * s + HEAD_SLOTS - 1) / HEAD_SLOTS, per = (kb + s - 1) / s;
+      const double t = (double)rounds * (per + 12) + (double)s * rows * p.ldd * 8 / 2e6;
+      if (t < best) best = t, p.splits = s;
     }
   }
   size_t at = 0;
@@ -382,15 +391,14 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool i
   p.at_target = take(rows * 4);
   p.at_flag = take(rows);
   p.at_x = take(p.npad * p.dp * 2 * p.planes);
-  p.at_w = take(in_place ? 0 : (int64_t)vocab * p.dp * 2 * p.planes);
   if (backward) {
     p.at_lse = take(rows * 4);
     p.at_coef = take(rows * 4);
     p.at_g = take(p.npad * p.piece * 2 * p.planes);
-    p.at_part = take(p.splits * p.npad * p.ldd * 4);
+    p.at_part = take(p.splits * p.ldn * p.ldd * 4);
   } else {
     p.at_picked = take(rows * 4);
-    p.at_stat = take(mv / HEAD_BM * p.npad * 8);
+    p.at_stat = take(mv / Small::bm * p.npad * 8);
   }
   p.bytes = at;
   return p;
@@ -411,43 +419,34 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
   if (distill && c.rows > 0) hipLaunchKernelGGL(head_flag_kernel, grid((c.rows + 3) / 4), dim3(256), 0, s, r);
   hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(1024), 0, s, r, backward);
-  uint16_t *xs = (uint16_t*)(ws + plan.at_x), *wl = (uint16_t*)(ws + plan.at_w);
-  auto layout = [&](const void* from, int64_t ld, int64_t rows, const int32_t* map, const int32_t* live, uint16_t* to) {
-    const int64_t n = rows * (plan.dp / 8);
-    if (n <= 0) return;
+  uint16_t* xs = (uint16_t*)(ws + plan.at_x);
+  if (c.rows > 0) {
+    const dim3 g = grid((plan.npad * (plan.dp / 8) + 255) / 256);
     if (c.bf16)
-      hipLaunchKernelGGL((head_layout_kernel<bf16_t>), grid((n + 255) / 256), dim3(256), 0, s, (const bf16_t*)from, ld, c.width, rows, map, live, to,
-                         plan.dp, rows * plan.dp);
+      hipLaunchKernelGGL((head_layout_kernel<bf16_t>), g, dim3(256), 0, s, (const bf16_t*)c.x, c.ldx, c.width, plan.npad, r.map, r.live, xs,
+                         plan.dp, plan.npad * plan.dp);
     else
-      hipLaunchKernelGGL((head_layout_kernel<float>), grid((n + 255) / 256), dim3(256), 0, s, (const float*)from, ld, c.width, rows, map, live, to,
-                         plan.dp, rows * plan.dp);
-  };
-  layout(c.x, c.ldx, plan.npad, r.map, r.live, xs);
-  const bool in_place = head_in_place(c.bf16, c.w, c.width, c.ldw);
-  if (!in_place && c.rows > 0) layout(c.w, c.ldw, c.vocab, nullptr, nullptr, wl);
+      hipLaunchKernelGGL((head_layout_kernel<float>), g, dim3(256), 0, s, (const float*)c.x, c.ldx, c.width, plan.npad, r.map, r.live, xs,
+                         plan.dp, plan.npad * plan.dp);
+  }
+  const bool direct = head_direct(c.bf16, c.w, c.width, c.ldw);
   const HeadOperand x{xs, plan.dp, plan.npad * plan.dp, plan.npad, (int32_t)plan.dp};
-  auto weights = [&](int64_t v0, int64_t n) {
-    if (in_place) return HeadOperand{(const uint16_t*)c.w + v0 * c.ldw, c.ldw, 0, n, c.width};
-    return HeadOperand{wl + v0 * plan.dp, plan.dp, (int64_t)c.vocab * plan.dp, n, (int32_t)plan.dp};
-  };
+  auto weights = [&](int64_t v0, int64_t n) { return HeadOperand{(const char*)c.w + v0 * c.ldw * (c.bf16 ? 2 : 4), c.ldw, 0, n, c.width}; };
   HeadProb base{};
-  base.pairs = c.bf16 ? 1 : 6;
   base.live = r.live;
   base.inv_t = 1.f / c.temperature;
   base.splits = 1;
-  base.ldn = plan.npad;
   base.target = distill ? nullptr : r.target;
-  const int md = (int)(plan.ldd / HEAD_BM);
   if (!backward) {
     HeadProb p = base;
     p.a = weights(0, c.vocab);
     p.b = x;
     p.kb = (int)(plan.dp / HEAD_BK);
-    p.tiles_m = (int)((c.vocab + HEAD_BM - 1) / HEAD_BM);
     p.vocab = c.vocab;
     p.stat = (float2*)(ws + plan.at_stat);
+    p.ldn = plan.npad;
     p.picked = (float*)(ws + plan.at_picked);
-    head_launch<HEAD_STATS>(c.bf16, plan.narrow[HEAD_STATS], p, c.rows, s);
+    head_launch<HEAD_STATS>(plan, direct, p, c.vocab, c.rows, s);
     hipLaunchKernelGGL(head_finish_kernel, grid((c.rows + 15) / 16), dim3(1024), 0, s, r, p.stat, p.tiles_m, p.ldn, p.picked);
     if (distill) {
       if (c.bf16) hipLaunchKernelGGL((head_distill_kernel<bf16_t>), grid((c.rows + 3) / 4), dim3(256), 0, s, r);
@@ -466,7 +465,6 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
       p.a = weights(v0, n);
       p.b = x;
       p.kb = (int)(plan.dp / HEAD_BK);
-      p.tiles_m = (int)(padded / HEAD_BM);
       p.vocab = (int32_t)n;
       p.first = (int32_t)v0;
       p.lse = r.lse;
@@ -474,37 +472,36 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
       p.g = g;
       p.ldg = plan.piece;
       p.gplane = gplane;
-      head_launch<HEAD_GRAD>(c.bf16, plan.narrow[HEAD_GRAD], p, c.rows, s);
+      head_launch<HEAD_GRAD>(plan, direct, p, padded, c.rows, s);
       if (distill)
         hipLaunchKernelGGL(head_entries_kernel, grid((c.rows + 3) / 4), dim3(256), 0, s, r, g, plan.piece, gplane, plan.planes, (int)v0, (int)n);
       HeadProb q = base;
       q.a = weights(v0, n);
       q.b = gop;
       q.kb = (int)((n + HEAD_BK - 1) / HEAD_BK);
-      q.tiles_m = md;
       q.splits = plan.splits;
       q.per = (q.kb + plan.splits - 1) / plan.splits;
       q.part = part;
+      q.ldn = plan.ldn;
       q.ldd = plan.ldd;
       q.add = v0 > 0;
-      head_launch<HEAD_DX>(c.bf16, plan.narrow[HEAD_DX], q, c.rows, s);
+      head_launch<HEAD_DX>(plan, direct, q, c.width, c.rows, s);
     }
     HeadProb q = base;
     q.a = x;
     q.b = gop;
-    q.tiles_m = md;
     q.vocab = (int32_t)n;
     q.out = (char*)c.dw + v0 * c.lddw * (c.bf16 ? 2 : 4);
     q.ldo = c.lddw;
     q.out_cols = c.width;
     q.add = c.add;
     q.vec = c.width % 4 == 0 && c.lddw % 4 == 0 && (uintptr_t)c.dw % (c.bf16 ? 8 : 16) == 0;
-    head_launch<HEAD_DW>(c.bf16, plan.narrow[HEAD_DW], q, n, s);
+    head_launch<HEAD_DW>(plan, direct, q, c.width, n, s);
   }
   if (c.rows > 0) {
     const int64_t n = c.rows * ((c.width + 3) / 4);
-    if (c.bf16) hipLaunchKernelGGL((head_dx_kernel<bf16_t>), grid((n + 255) / 256), dim3(256), 0, s, r, part, plan.splits, plan.npad, plan.ldd);
-    else hipLaunchKernelGGL((head_dx_kernel<float>), grid((n + 255) / 256), dim3(256), 0, s, r, part, plan.splits, plan.npad, plan.ldd);
+    if (c.bf16) hipLaunchKernelGGL((head_dx_kernel<bf16_t>), grid((n + 255) / 256), dim3(256), 0, s, r, part, plan.splits, plan.ldn, plan.ldd);
+    else hipLaunchKernelGGL((head_dx_kernel<float>), grid((n + 255) / 256), dim3(256), 0, s, r, part, plan.splits, plan.ldn, plan.ldd);
   }
   return hipGetLastError();
 }

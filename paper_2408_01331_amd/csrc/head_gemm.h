@@ -7,6 +7,11 @@
 // its barrier, the next stage's first operands are on their way from LDS and the stage
 // that was freed is being filled again.
 //
+// fp32 operands are three bf16 terms each, side by side in a stage, and a block is
+// multiplied with six of the nine products of terms. Weights in fp32, and weights in
+// bf16 whose rows do not lie at 16-byte boundaries, pass through registers on their way
+// to LDS (and are split there): they are read once, as they are.
+//
 // LDS images, in 16-byte chunks. An operand with k innermost: rows of 4 chunks, chunk c
 // of row r at c ^ (r / 4 % 4), so the 16 rows that a read takes at once lie in different
 // banks. One with k outermost: rows of R / 8 chunks, read transposed; the 64-byte groups
@@ -67,7 +72,7 @@ template <bool COL, int R, int W> struct HeadTile {
     const int64_t at = plane * op.plane + (COL ? k0 * op.ld + r0 : r0 * op.ld + k0);
     const int64_t rows = COL ? min(op.rows - k0, (int64_t)HEAD_BK) : min(op.rows - r0, (int64_t)R);
     const int64_t left = op.cols - (COL ? r0 : k0);
-    const uint64_t base = (uint64_t)(op.p + at);
+    const uint64_t base = (uint64_t)((const uint16_t*)op.p + at);
     const uint32_t bytes = real && rows > 0 && left > 0 ? (uint32_t)(((rows - 1) * op.ld + left) * 2) : 0;
     const u32x4 rsrc = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base),
                         (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffff),
@@ -76,6 +81,75 @@ template <bool COL, int R, int W> struct HeadTile {
     for (int t = 0; t < LOADS; ++t) {
       const uint32_t v = COL ? voff[t] : (int64_t)k8 < left ? voff[t] : HEAD_OUT;
       lds_load(__builtin_amdgcn_readfirstlane(lds + (wave + t * W) * 1024), v, rsrc);
+    }
+  }
+};
+
+// Two floats as three pairs of bf16 terms whose sums they are, to 2^-24. (An infinity
+// gives NaN terms.)
+__device__ __forceinline__ void three_terms2(float a, float b, uint32_t (&h)[3]) {
+  h[0] = f2bf2(a, b);
+  a -= __uint_as_float(h[0] << 16);
+  b -= __uint_as_float(h[0] & 0xffff0000u);
+  h[1] = f2bf2(a, b);
+  a -= __uint_as_float(h[1] << 16);
+  b -= __uint_as_float(h[1] & 0xffff0000u);
+  h[2] = f2bf2(a, b);
+}
+
+// One operand's tile of R rows (or columns) x 32 k of T, of any row stride, through
+// registers: chunks of 8 values, zeros where the operand ends.
+template <typename T, bool COL, int R, int NT> struct HeadRegs {
+  static constexpr int CH = R * 4 / NT, V = sizeof(T) / 2;
+  u32x4 raw[CH][V];
+  __device__ static uint32_t lds_at(int t) {
+    const uint32_t i = threadIdx.x + t * NT;
+    if constexpr (!COL) return (i >> 2) * 64 + (((i & 3) ^ ((i >> 4) & 3)) << 4);
+    else return i / (R / 8) * (R * 2) + (((i % (R / 8)) ^ HeadTile<COL, R, 1>::swizzle(i / (R / 8))) << 4);
+  }
+  __device__ void load(const HeadOperand& op, int64_t r0, int kb, bool real) {
+    const int64_t k0 = (int64_t)kb * HEAD_BK;
+#pragma unroll
+    for (int t = 0; t < CH; ++t) {
+      const int i = threadIdx.x + t * NT;
+      const int64_t row = COL ? k0 + i / (R / 8) : r0 + (i >> 2), col = COL ? r0 + i % (R / 8) * 8 : k0 + (i & 3) * 8;
+      const int have = real && row < op.rows ? (int)min(max(op.cols - col, (int64_t)0), (int64_t)8) : 0;
+      const T* q = (const T*)op.p + row * op.ld + col;
+      if (have == 8) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) raw[t][v] = ((const u32x4_a2*)q)[v];
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          raw[t][v] = u32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int e = 0; e < 8 / V; ++e)
+            if (v * (8 / V) + e < have) {
+              if constexpr (V == 1) raw[t][v][e / 2] |= (uint32_t)q[e] << (16 * (e & 1));
+              else raw[t][v][e] = __float_as_uint(q[v * 4 + e]);
+            }
+        }
+      }
+    }
+  }
+  __device__ void store(uint32_t lds) const {
+#pragma unroll
+    for (int t = 0; t < CH; ++t) {
+      const uint32_t at = lds + lds_at(t);
+      if constexpr (V == 1) {
+        *(UN_LDS u32x4*)at = raw[t][0];
+      } else {
+        u32x4 h[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          uint32_t w[3];
+          three_terms2(__uint_as_float(raw[t][e / 2][e % 2 * 2]), __uint_as_float(raw[t][e / 2][e % 2 * 2 + 1]), w);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) h[p][e] = w[p];
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) *(UN_LDS u32x4*)(at + p * (R * 64)) = h[p];
+      }
     }
   }
 };
@@ -114,34 +188,33 @@ template <bool COL, int R, int F> struct HeadFrags {
   }
 };
 
-// (plane of A, plane of B) of product `pair`, the smallest first: (0, 2), (2, 0), (1, 1), (0, 1), (1, 0), (0, 0)
-__device__ __forceinline__ int plane_a(int pairs, int pair) { return pairs == 1 ? 0 : (0x010120 >> (4 * pair)) & 15; }
-__device__ __forceinline__ int plane_b(int pairs, int pair) { return pairs == 1 ? 0 : (0x001102 >> (4 * pair)) & 15; }
-
 template <HeadKind KIND> struct HeadShape {
   static constexpr bool COL_A = KIND == HEAD_DX || KIND == HEAD_DW, COL_B = KIND == HEAD_DW;
 };
 
-template <int BM, int BN, int WGM, int WGN, int ST> struct HeadCfg {
-  static constexpr int bm = BM, bn = BN, wgm = WGM, wgn = WGN, st = ST, waves = WGM * WGN;
+// P: terms of an operand
+template <int BM, int BN, int WGM, int WGN, int ST, int P> struct HeadCfg {
+  static constexpr int bm = BM, bn = BN, wgm = WGM, wgn = WGN, st = ST, planes = P, waves = WGM * WGN;
   static constexpr int fm = BM / WGM / 32, fn = BN / WGN / 32;
-  static constexpr int stage = (BM + BN) * 64;
+  static constexpr int stage = (BM + BN) * 64 * P;
 };
 
-// acc <- the tile's products over blocks [0, n) of its k range; leaves no load in flight and LDS free
-template <HeadKind KIND, class C>
+// acc <- the tile's products over k-blocks [kb0, kb1); leaves no load in flight and LDS
+// free. REG: A passes through registers, as values of T.
+template <HeadKind KIND, class C, typename T, bool REG>
 __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int64_t n0, int kb0, int kb1, char* sm, f32x16 (&acc)[C::fm][C::fn]) {
   constexpr bool CA = HeadShape<KIND>::COL_A, CB = HeadShape<KIND>::COL_B;
-  constexpr int W = C::waves, ST = C::st, FM = C::fm, FN = C::fn;
+  constexpr int W = C::waves, ST = C::st, FM = C::fm, FN = C::fn, P = C::planes;
   typedef HeadTile<CA, C::bm, W> TA;
   typedef HeadTile<CB, C::bn, W> TB;
-  constexpr int PER = TA::LOADS + TB::LOADS;
+  constexpr int PER = P * ((REG ? 0 : TA::LOADS) + TB::LOADS);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int per = max(kb1 - kb0, 0), n = per * p.pairs;
+  const int n = max(kb1 - kb0, 0);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(UN_LDS char*)sm;
   TA ta;
   TB tb;
-  ta.setup(p.a, m0, wave);
+  HeadRegs<T, CA, C::bm, W * 64> ra;
+  if constexpr (!REG) ta.setup(p.a, m0, wave);
   tb.setup(p.b, n0, wave);
   HeadFrags<CA, C::bm, FM> fa;
   HeadFrags<CB, C::bn, FN> fb;
@@ -154,51 +227,64 @@ __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int6
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
   if (n == 0) return;
-  int next = 0, kb = kb0, pair = 0;  // the block that is loaded next
+  // (behind the last block zeros are loaded: the counts of loads in flight stay the same)
+  int next = 0;  // the block whose loads are issued next, of A one before where it passes through registers
+  if constexpr (REG) ra.load(p.a, m0, kb0, true);
   auto issue = [&](uint32_t slot) {
-    // (behind the last block zeros are loaded: the counts of loads in flight stay the same)
-    const bool real = next < n;
     const uint32_t lds = lds0 + slot * C::stage;
-    ta.load(p.a, m0, plane_a(p.pairs, pair), kb, real, lds, wave);
-    tb.load(p.b, n0, plane_b(p.pairs, pair), kb, real, lds + TA::BYTES, wave);
+    if constexpr (REG) {
+      ra.store(lds);  // (the compiler waits for these loads, and so for all before them)
+      ra.load(p.a, m0, kb0 + next + 1, next + 1 < n);
+    }
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      if constexpr (!REG) ta.load(p.a, m0, k, kb0 + next, next < n, lds + k * TA::BYTES, wave);
+      tb.load(p.b, n0, k, kb0 + next, next < n, lds + P * TA::BYTES + k * TB::BYTES, wave);
+    }
     ++next;
-    if (++kb == kb1) kb = kb0, pair = min(pair + 1, p.pairs - 1);
   };
-  bf16x8 a[2][FM], b[2][FN];
+  bf16x8 a[2][P][FM], b[2][P][FN];
+  auto read = [&](uint32_t slot, int s) {
+    const uint32_t lds = lds0 + slot * C::stage;
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      fa.read(lds + k * TA::BYTES, s, a[s][k]);
+      fb.read(lds + P * TA::BYTES + k * TB::BYTES, s, b[s][k]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply = [&](int s) {
+    // products of terms, the smallest first: (0, 2), (2, 0), (1, 1), (0, 1), (1, 0), (0, 0)
+    constexpr int PA[6] = {0, 2, 1, 0, 1, 0}, PB[6] = {2, 0, 1, 1, 0, 0};
+#pragma unroll
+    for (int t = P == 1 ? 5 : 0; t < 6; ++t)
+#pragma unroll
+      for (int x = 0; x < FM; ++x)
+#pragma unroll
+        for (int y = 0; y < FN; ++y)
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s][PA[t]][x], b[s][PB[t]][y], acc[x][y], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
 #pragma unroll
   for (int s = 0; s < ST; ++s) issue(s);
-  wait_loads<(ST - 1) * PER>();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  wait_loads<REG ? 0 : (ST - 1) * PER>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  fa.read(lds0, 0, a[0]);
-  fb.read(lds0 + TA::BYTES, 0, b[0]);
+  read(0, 0);
   uint32_t slot = 0;
   for (int i = 0; i < n; ++i) {
-    const uint32_t lds = lds0 + slot * C::stage;
     const uint32_t slot1 = slot + 1 == ST ? 0 : slot + 1;
-    fa.read(lds, 1, a[1]);
-    fb.read(lds + TA::BYTES, 1, b[1]);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int x = 0; x < FM; ++x)
-#pragma unroll
-      for (int y = 0; y < FN; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0][x], b[0][y], acc[x][y], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
+    read(slot, 1);
+    multiply(0);
     // this stage is read, by every wave; the next one is there
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    wait_loads<(ST - 2) * PER>();
+    wait_loads<REG ? 0 : (ST - 2) * PER>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     issue(slot);
-    const uint32_t lds1 = lds0 + slot1 * C::stage;
-    fa.read(lds1, 0, a[0]);
-    fb.read(lds1 + TA::BYTES, 0, b[0]);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int x = 0; x < FM; ++x)
-#pragma unroll
-      for (int y = 0; y < FN; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1][x], b[1][y], acc[x][y], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
+    read(slot1, 0);
+    multiply(1);
     slot = slot1;
   }
   wait_loads<0>();
@@ -231,17 +317,8 @@ __device__ __forceinline__ float2 join_stat(float2 a, float2 b) {
   return float2{m, (a.x == -INFINITY ? a.y : a.y * ea) + (b.x == -INFINITY ? b.y : b.y * eb)};
 }
 
-// Three bf16 terms whose sum is x, to 2^-24 (an x that is not finite: itself, 0, 0).
-__device__ __forceinline__ void three_terms(float x, uint32_t (&h)[3]) {
-  h[0] = f2bf(x);
-  const float r = x - bf2f(h[0]);
-  const bool fine = fabsf(x) < INFINITY && fabsf(bf2f(h[0])) < INFINITY;
-  h[1] = fine ? f2bf(r) : 0;
-  h[2] = fine ? f2bf(r - bf2f(h[1])) : 0;
-}
-
-template <HeadKind KIND, class C, typename T>
-__global__ __launch_bounds__(C::waves * 64) void head_kernel(HeadProb p) {
+template <HeadKind KIND, class C, typename T, bool REG>
+__global__ __launch_bounds__(C::waves * 64, 2) void head_kernel(HeadProb p) {
   __shared__ __attribute__((aligned(1024))) char sm[C::stage * C::st];
   const int live = *p.live;
   const int tn = KIND == HEAD_DW ? p.tiles_n : min(p.tiles_n, (live + C::bn - 1) / C::bn);
@@ -260,7 +337,7 @@ __global__ __launch_bounds__(C::waves * 64) void head_kernel(HeadProb p) {
   if constexpr (KIND == HEAD_DX) kb0 = split * p.per, kb1 = min(p.kb, kb0 + p.per);
   if constexpr (KIND == HEAD_DW) kb1 = (live + HEAD_BK - 1) / HEAD_BK;
   f32x16 acc[C::fm][C::fn];
-  head_product<KIND, C>(p, m0, n0, kb0, kb1, sm, acc);
+  head_product<KIND, C, T, REG>(p, m0, n0, kb0, kb1, sm, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 
   if constexpr (KIND == HEAD_STATS) {
@@ -327,18 +404,19 @@ __global__ __launch_bounds__(C::waves * 64) void head_kernel(HeadProb p) {
         g[e] = n0 + n < live && m0 + m + e < p.vocab ? g[e] : 0.f;
       }
       uint16_t* o = p.g + (n0 + n) * p.ldg + m0 + m;
-      if (p.pairs == 1) {
+      if constexpr (C::planes == 1) {
         *(u32x2*)o = u32x2{f2bf2(g[0], g[1]), f2bf2(g[2], g[3])};
       } else {
-        uint32_t h[4][3];
+        uint32_t h[2][3];
+        three_terms2(g[0], g[1], h[0]);
+        three_terms2(g[2], g[3], h[1]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) three_terms(g[e], h[e]);
-#pragma unroll
-        for (int k = 0; k < 3; ++k) *(u32x2*)(o + k * p.gplane) = u32x2{h[0][k] | h[1][k] << 16, h[2][k] | h[3][k] << 16};
+        for (int k = 0; k < 3; ++k) *(u32x2*)(o + k * p.gplane) = u32x2{h[0][k], h[1][k]};
       }
     });
   } else if constexpr (KIND == HEAD_DX) {
     head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {
+      if (n0 + n >= live) return;
       f32x4* o = (f32x4*)(p.part + ((int64_t)split * p.ldn + n0 + n) * p.ldd + m0 + m);
       const f32x4 r = {v[0], v[1], v[2], v[3]};
       *o = p.add ? *o + r : r;
@@ -370,11 +448,6 @@ __global__ __launch_bounds__(C::waves * 64) void head_kernel(HeadProb p) {
       }
     });
   }
-}
-
-template <HeadKind KIND, class C, typename T> void head_go(const HeadProb& p, hipStream_t s) {
-  const int64_t n = (int64_t)p.tiles_m * p.tiles_n * p.splits;
-  hipLaunchKernelGGL((head_kernel<KIND, C, T>), dim3((unsigned)((n + 7) / 8 * 8)), dim3(C::waves * 64), 0, s, p);
 }
 
 }  // namespace

@@ -419,9 +419,9 @@ un_status head_sizes_ok(const char* F, int32_t type, int64_t rows, int32_t width
   if (width > HEAD_MAX_WIDTH) return bad(F, "a width above 65536 is not supported", UN_ERR_UNSUPPORTED);
   if (rows > HEAD_MAX_ROWS) return bad(F, "more than 2^24 rows are not supported", UN_ERR_UNSUPPORTED);
   if (vocab > (1 << 30)) return bad(F, "a vocabulary above 2^30 is not supported", UN_ERR_UNSUPPORTED);
-  // tiles of 256 x 64, and 8 values per thread of the layouts
-  const int64_t v = ((int64_t)vocab + 255) / 256, n = (rows + 63) / 64 + 4, w = ((int64_t)width + 31) / 32 * 4;
-  if (too_many(v * n + 8, 256) || too_many((vocab * w + 255) / 256, 256) || too_many(((rows + 256) * w + 255) / 256, 256))
+  // tiles of 128 x 64, up to 128 parts of a sum, and 4 values a thread of the rows' kernels
+  const int64_t v = ((int64_t)vocab + 127) / 128 + 2, n = (rows + 63) / 64 + 4, d = ((int64_t)width + 127) / 128 + 1;
+  if (too_many(v * n + 8, 256) || too_many(d * n * 128 + 8, 256) || too_many(d * 2 * v + 8, 256) || too_many((rows + 256) * d * 32 / 256 + 8, 256))
     return bad(F, "too many rows, columns or vocabulary", UN_ERR_UNSUPPORTED);
   return UN_OK;
 }
@@ -444,7 +444,7 @@ template <typename A> un_status head_common(const char* F, const A* a, bool back
   c->wide = a->index_bits == 64;
   c->lse = const_cast<float*>(a->lse);
   c->temperature = 1.f;
-  *plan = head_plan(c->bf16, a->rows, a->width, a->vocab, head_in_place(c->bf16, a->weight, a->width, a->ldw), backward);
+  *plan = head_plan(c->bf16, a->rows, a->width, a->vocab, backward);
   if (a->rows == 0 && !backward) return UN_OK;
   if (!a->workspace || a->workspace_bytes < plan->bytes) return bad(F, "workspace too small (un_vocab_workspace)", UN_ERR_BUFSIZE);
   if ((uintptr_t)a->workspace % 16) return bad(F, "workspace is not 16-byte aligned");
@@ -481,12 +481,12 @@ template <typename A> un_status head_teacher(const char* F, const A* a, HeadCall
 
 extern "C" {
 
-un_status un_vocab_workspace(int32_t type, int64_t rows, int32_t width, int32_t vocab, int32_t in_place, int32_t backward, size_t* bytes) {
+un_status un_vocab_workspace(int32_t type, int64_t rows, int32_t width, int32_t vocab, int32_t backward, size_t* bytes) {
   const char* F = "un_vocab_workspace";
   if (!bytes) return bad(F, "bytes is NULL");
   const un_status st = head_sizes_ok(F, type, rows, width, vocab);
   if (st != UN_OK) return st;
-  *bytes = head_plan(type == UN_TYPE_BF16, rows, width, vocab, in_place && type == UN_TYPE_BF16, backward != 0).bytes;
+  *bytes = head_plan(type == UN_TYPE_BF16, rows, width, vocab, backward != 0).bytes;
   return UN_OK;
 }
 

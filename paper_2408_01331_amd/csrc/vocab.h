@@ -60,10 +60,10 @@ hipError_t launch_embed_bwd(bool bf16, const EmbedPlan& plan, EmbedProb p, void*
 // the nine products of terms (the others are below 2^-24 of the result's terms).
 // ---------------------------------------------------------------------------
 constexpr int HEAD_BK = 32;         // k of a block
-constexpr int HEAD_BM = 256;        // vocabulary (or hidden) columns of a tile
+constexpr int HEAD_BM = 256;        // the vocabulary's pieces and the partial sums' columns are padded to this
 constexpr int HEAD_PAD = 256;       // live rows are padded to this with zeros
 struct HeadOperand {
-  const uint16_t* p;                // bf16 [planes][rows][ld]
+  const void* p;                    // bf16 [planes][rows][ld], or the weights as they are
   int64_t ld, plane, rows;
   int32_t cols;
 };
@@ -77,7 +77,6 @@ enum HeadKind {
 struct HeadProb {
   HeadOperand a, b;
   int32_t kb;                       // k-blocks (HEAD_DW: counted from `live`)
-  int32_t pairs;                    // products of planes: 1 or 6
   int32_t tiles_m, tiles_n;
   int32_t splits, per;              // HEAD_DX: parts of k, and k-blocks of each
   const int32_t* live;              // rows that count
@@ -127,21 +126,21 @@ struct HeadCall {
 };
 constexpr int HEAD_MAX_WIDTH = 1 << 16, HEAD_MAX_TOP = 128;
 constexpr int64_t HEAD_MAX_ROWS = (int64_t)1 << 24, HEAD_MAX_LD = (int64_t)1 << 20;
-// weights that the products read where they are; others are laid out in the workspace first
-inline bool head_in_place(bool bf16, const void* w, int32_t width, int64_t ldw) {
+// weights whose rows the direct loads take; others pass through registers
+inline bool head_direct(bool bf16, const void* w, int32_t width, int64_t ldw) {
   return bf16 && (uintptr_t)w % 16 == 0 && width % 8 == 0 && ldw % 8 == 0 && ldw <= HEAD_MAX_LD;
 }
 struct HeadPlan {
   int planes;
   int64_t dp, npad;                 // columns and rows of the laid-out hidden states
-  bool narrow[4];                   // by HeadKind: tiles of 64 columns, not 128
+  bool small[4];                    // by HeadKind: small tiles (fp32: always)
   int64_t piece;                    // vocabulary of a piece
   int splits;                       // HEAD_DX
-  int64_t ldd;
+  int64_t ldn, ldd;                 // rows and columns of its partial sums
   // offsets in the workspace
-  size_t at_map, at_inv, at_target, at_lse, at_coef, at_flag, at_live, at_x, at_w, at_stat, at_picked, at_g, at_part, bytes;
+  size_t at_map, at_inv, at_target, at_lse, at_coef, at_flag, at_live, at_x, at_stat, at_picked, at_g, at_part, bytes;
 };
-HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool in_place, bool backward);
+HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool backward);
 hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, void* workspace, hipStream_t s);
 
 }  // namespace un

@@ -441,9 +441,9 @@ def embedding_backward(dy, tokens, vocab, scale=1.0, padding=None, out=None):
 # Losses over a vocabulary
 # ---------------------------------------------------------------------------
 @functools.lru_cache(maxsize=1024)
-def _head_workspace(t, rows, width, vocab, in_place, backward):
+def _head_workspace(t, rows, width, vocab, backward):
     need = ctypes.c_size_t()
-    status = _lib().un_vocab_workspace(t, rows, width, vocab, in_place, backward, _byref(need))
+    status = _lib().un_vocab_workspace(t, rows, width, vocab, backward, _byref(need))
     if status:
         _un._check(status)
     return need.value
@@ -459,12 +459,6 @@ def _head(x, weight):
     rows, ldx, xv = _rows(x, "x")
     vocab, width, ldw = _table(weight, "weight")
     return t, dev, x.shape[:-1], (rows, xv.data_ptr(), ldx, weight.data_ptr(), ldw), (vocab, width), xv
-
-
-def _head_ws(t, rows, width, vocab, w, ldw, backward, like):
-    in_place = t == 1 and w % 16 == 0 and width % 8 == 0 and ldw % 8 == 0 and ldw <= 1 << 20
-    need = _head_workspace(t, rows, width, vocab, in_place, backward)
-    return like.new_empty(need, dtype=torch.uint8), need
 
 
 def _head_out(weight, lead, dloss, out, dev):
@@ -502,7 +496,8 @@ def vocab_loss(x, weight, targets, ignore=-100):
     _unrecorded(x, weight)
     loss = x.new_empty(lead, dtype=_F32)
     lse = _empty_like(loss)
-    ws, need = _head_ws(t, rows, width, vocab, wp, ldw, 0, x)
+    need = _head_workspace(t, rows, width, vocab, 0)
+    ws = x.new_empty(need, dtype=torch.uint8)
     _call(_lib().un_vocab_loss, _un.un_vocab_loss_args(t, width, vocab, bits, rows, xp, ldx, wp, ldw, targets.data_ptr(), int(ignore),
                                                        loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), need), dev)
     return loss, lse
@@ -524,7 +519,8 @@ def vocab_loss_backward(x, weight, targets, lse, dloss, ignore=-100, out=None):
         _written(out)
     else:
         out = weight.new_empty(weight.shape)
-    ws, need = _head_ws(t, rows, width, vocab, wp, ldw, 1, x)
+    need = _head_workspace(t, rows, width, vocab, 1)
+    ws = x.new_empty(need, dtype=torch.uint8)
     _call(_lib().un_vocab_loss_backward, _un.un_vocab_loss_grad_args(t, width, vocab, bits, rows, xp, ldx, wp, ldw, targets.data_ptr(),
                                                                      int(ignore), lse.data_ptr(), dlp, step, dx.data_ptr(), width,
                                                                      out.data_ptr(), lddw, given, ws.data_ptr(), need), dev)
@@ -553,7 +549,8 @@ def distill_loss(x, weight, ids, logits, temperature=1.0):
     _unrecorded(x, weight, logits)
     loss = x.new_empty(lead, dtype=_F32)
     lse, picked = _empty_like(loss), x.new_empty(ids.shape, dtype=_F32)
-    ws, need = _head_ws(t, rows, width, vocab, wp, ldw, 0, x)
+    need = _head_workspace(t, rows, width, vocab, 0)
+    ws = x.new_empty(need, dtype=torch.uint8)
     _call(_lib().un_distill_loss, _un.un_distill_loss_args(t, width, vocab, bits, rows, xp, ldx, wp, ldw, ids.shape[-1], lt, ids.data_ptr(),
                                                            logits.data_ptr(), float(temperature), loss.data_ptr(), lse.data_ptr(),
                                                            picked.data_ptr(), ws.data_ptr(), need), dev)
@@ -575,7 +572,8 @@ def distill_loss_backward(x, weight, ids, logits, lse, picked, dloss, temperatur
         _written(out)
     else:
         out = weight.new_empty(weight.shape)
-    ws, need = _head_ws(t, rows, width, vocab, wp, ldw, 1, x)
+    need = _head_workspace(t, rows, width, vocab, 1)
+    ws = x.new_empty(need, dtype=torch.uint8)
     _call(_lib().un_distill_loss_backward, _un.un_distill_loss_grad_args(t, width, vocab, bits, rows, xp, ldx, wp, ldw, ids.shape[-1], lt,
                                                                          ids.data_ptr(), logits.data_ptr(), float(temperature),
                                                                          lse.data_ptr(), picked.data_ptr(), dlp, step, dx.data_ptr(),

@@ -176,7 +176,7 @@ def lib():
             "un_distill_loss": (ctypes.c_int, [ctypes.POINTER(un_distill_loss_args), P]),
             "un_distill_loss_backward": (ctypes.c_int, [ctypes.POINTER(un_distill_loss_grad_args), P]),
             "un_vocab_workspace": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
-                                                  ctypes.c_int32, c_size_p]),
+                                                  c_size_p]),
             "un_gated_scan": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_args), P]),
             "un_gated_scan_backward": (ctypes.c_int, [ctypes.POINTER(un_gated_scan_grad_args), P]),
             "un_gated_scan_sizes": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, c_size_p, c_size_p]),
