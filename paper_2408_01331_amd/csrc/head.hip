@@ -164,7 +164,7 @@ template <typename T> __global__ __launch_bounds__(256) void head_layout_kernel(
   }
 }
 
-// The tiles' statistics of 16 rows, joined by 64 groups of their threads and then in
+// The statistics of 16 rows, joined by 64 groups of their threads and then in
 // order: the rows' lse, and the cross entropy's loss.
 __global__ __launch_bounds__(1024) void head_finish_kernel(HeadRows r, const float2* stat, int tiles, int64_t ldn, const float* picked) {
   __shared__ float2 sm[64][16];
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(1024) void head_finish_kernel(HeadRows r, const flo
   }
   if (g == 0 && n < live) {
     a = sm[0][l];
-    const float lse = a.x + logf(a.y);
+    const float lse = a.x == -INFINITY ? logf(a.y) : fmaf(a.x, LN2, fmaf(a.x, LN2_LOW, logf(a.y)));
     const int64_t row = r.map[n];
     r.c.lse[row] = lse;
     if (r.c.targets) {
@@ -324,12 +324,12 @@ template <typename T> __global__ __launch_bounds__(256) void head_dx_kernel(Head
   }
 }
 
-typedef HeadCfg<256, 128, 2, 2, 3, 1> Large;
-typedef HeadCfg<128, 64, 2, 2, 4, 1> Small;
-typedef HeadCfg<128, 64, 2, 2, 2, 3> Terms;   // fp32
+typedef HeadCfg<256, 256, 2, 4, 2, 64, 1> Large;
+typedef HeadCfg<128, 128, 2, 2, 2, 64, 1> Medium;
+typedef HeadCfg<128, 64, 2, 2, 3, 64, 1> Small;
+typedef HeadCfg<128, 64, 2, 2, 2, 32, 3> Terms;   // fp32
 
 constexpr int64_t HEAD_G_BYTES = (int64_t)512 << 20;   // of g's piece
-constexpr int HEAD_SLOTS = 512;                        // workgroups that run at once
 
 template <HeadKind KIND, class C, typename T, bool REG> void head_go(HeadProb& p, int64_t m, int64_t n, hipStream_t s) {
   p.tiles_m = (int)((m + C::bm - 1) / C::bm);
@@ -340,9 +340,40 @@ template <HeadKind KIND, class C, typename T, bool REG> void head_go(HeadProb& p
 // a product of m x n; direct: the weights' rows can be loaded directly
 template <HeadKind KIND> void head_launch(const HeadPlan& plan, bool direct, HeadProb& p, int64_t m, int64_t n, hipStream_t s) {
   constexpr bool W = KIND != HEAD_DW;  // A is the weights
+  auto go = [&](auto cfg) {
+    using C = decltype(cfg);
+    W && !direct ? head_go<KIND, C, bf16_t, W>(p, m, n, s) : head_go<KIND, C, bf16_t, false>(p, m, n, s);
+  };
   if (plan.planes == 3) head_go<KIND, Terms, float, W>(p, m, n, s);
-  else if (plan.small[KIND]) W && !direct ? head_go<KIND, Small, bf16_t, W>(p, m, n, s) : head_go<KIND, Small, bf16_t, false>(p, m, n, s);
-  else W && !direct ? head_go<KIND, Large, bf16_t, W>(p, m, n, s) : head_go<KIND, Large, bf16_t, false>(p, m, n, s);
+  else if (plan.tile[KIND] == 0) go(Large{});
+  else if (plan.tile[KIND] == 1) go(Medium{});
+  else go(Small{});
+}
+
+// A product's time on tiles of a kind, in us: rounds of the workgroups that run at once,
+// each with its blocks and what it takes beside them (the first loads, the epilogue).
+struct HeadTime {
+  int bm, bn, slots, kb;
+  double block, rest;
+};
+constexpr HeadTime HEAD_TIMES[4] = {{256, 256, 256, 64, 1.63, 6.0}, {128, 128, 512, 64, 0.97, 3.0}, {128, 64, 512, 64, 0.6, 2.5}, {128, 64, 512, 32, 0.8, 2.5}};
+double head_time(const HeadTime& t, int64_t m, int64_t n, int64_t k, int64_t splits = 1) {
+  const int64_t tiles = (m + t.bm - 1) / t.bm * ((n + t.bn - 1) / t.bn) * splits, kb = ((k + splits - 1) / splits + t.kb - 1) / t.kb;
+  return (double)((tiles + t.slots - 1) / t.slots) * (kb * t.block + t.rest);
+}
+// the kind of tiles, and for HEAD_DX the parts of k, that take the least; partial sums are written and read at some 4 TB/s
+int head_tiles(bool bf16, int64_t m, int64_t n, int64_t k, int* splits = nullptr) {
+  int best = 0;
+  double least = 1e300;
+  for (int t = bf16 ? 0 : 3; t < (bf16 ? 3 : 4); ++t)
+    for (int64_t s = 1; s <= (splits ? std::min<int64_t>(128, k / 128 + 1) : 1); ++s) {
+      const double us = head_time(HEAD_TIMES[t], m, n, k, s) + (splits ? (double)s * m * n * 8 / 4e6 : 0);
+      if (us >= least) continue;
+      least = us;
+      best = t;
+      if (splits) *splits = (int)s;
+    }
+  return best;
 }
 
 }  // namespace
@@ -358,27 +389,11 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool b
   const int64_t mv = up(vocab, HEAD_BM);
   p.piece = mv;
   if (backward && rows > 0) p.piece = std::min(mv, std::max<int64_t>(4096, HEAD_G_BYTES / (p.npad * 2 * p.planes) / HEAD_BM * HEAD_BM));
-  // small tiles where there are few of them, or few rows
-  auto tiles = [](int64_t m, int64_t n, bool small) {
-    return small ? (m + Small::bm - 1) / Small::bm * ((n + Small::bn - 1) / Small::bn) : (m + Large::bm - 1) / Large::bm * ((n + Large::bn - 1) / Large::bn);
-  };
-  auto small = [&](int64_t m, int64_t n) { return !bf16 || n <= Small::bn || tiles(m, n, true) <= HEAD_SLOTS; };
-  p.small[HEAD_STATS] = small(vocab, rows);
-  p.small[HEAD_GRAD] = small(p.piece, rows);
-  p.small[HEAD_DX] = !bf16 || rows <= Small::bn;
-  p.small[HEAD_DW] = small(width, p.piece);
   p.splits = 1;
-  if (backward && rows > 0) {
-    // Parts of k: the time in units of a block, of the rounds that the card takes, each with what a tile costs beside its
-    // blocks, and of writing and reading the partial sums (4 bytes twice, some 2 MB in a block's time).
-    const int64_t n = tiles(width, rows, p.small[HEAD_DX]), kb = up(p.piece, HEAD_BK) / HEAD_BK;
-    double best = 1e30;
-    for (int s = 1; s <= 128 && s * 4 <= kb + 3; ++s) {
-      const int64_t rounds = (n * s + HEAD_SLOTS - 1) / HEAD_SLOTS, per = (kb + s - 1) / s;
-      const double t = (double)rounds * (per + 12) + (double)s * rows * p.ldd * 8 / 2e6;
-      if (t < best) best = t, p.splits = s;
-    }
-  }
+  p.tile[HEAD_STATS] = head_tiles(bf16, vocab, rows, width);
+  p.tile[HEAD_GRAD] = head_tiles(bf16, p.piece, rows, width);
+  p.tile[HEAD_DX] = head_tiles(bf16, width, rows, p.piece, &p.splits);
+  p.tile[HEAD_DW] = head_tiles(bf16, width, p.piece, rows);
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t a = at;
@@ -398,7 +413,7 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool b
     p.at_part = take(p.splits * p.ldn * p.ldd * 4);
   } else {
     p.at_picked = take(rows * 4);
-    p.at_stat = take(mv / Small::bm * p.npad * 8);
+    p.at_stat = take(mv / 128 * p.npad * 8);
   }
   p.bytes = at;
   return p;
@@ -435,19 +450,20 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
   HeadProb base{};
   base.live = r.live;
   base.inv_t = 1.f / c.temperature;
+  base.scale = (float)(1.4426950408889634 / c.temperature);
   base.splits = 1;
   base.target = distill ? nullptr : r.target;
   if (!backward) {
     HeadProb p = base;
     p.a = weights(0, c.vocab);
     p.b = x;
-    p.kb = (int)(plan.dp / HEAD_BK);
+    p.k = c.width;
     p.vocab = c.vocab;
     p.stat = (float2*)(ws + plan.at_stat);
     p.ldn = plan.npad;
     p.picked = (float*)(ws + plan.at_picked);
     head_launch<HEAD_STATS>(plan, direct, p, c.vocab, c.rows, s);
-    hipLaunchKernelGGL(head_finish_kernel, grid((c.rows + 15) / 16), dim3(1024), 0, s, r, p.stat, p.tiles_m, p.ldn, p.picked);
+    hipLaunchKernelGGL(head_finish_kernel, grid((c.rows + 15) / 16), dim3(1024), 0, s, r, p.stat, (c.vocab + 127) / 128, p.ldn, p.picked);
     if (distill) {
       if (c.bf16) hipLaunchKernelGGL((head_distill_kernel<bf16_t>), grid((c.rows + 3) / 4), dim3(256), 0, s, r);
       else hipLaunchKernelGGL((head_distill_kernel<float>), grid((c.rows + 3) / 4), dim3(256), 0, s, r);
@@ -464,7 +480,7 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
       HeadProb p = base;
       p.a = weights(v0, n);
       p.b = x;
-      p.kb = (int)(plan.dp / HEAD_BK);
+      p.k = c.width;
       p.vocab = (int32_t)n;
       p.first = (int32_t)v0;
       p.lse = r.lse;
@@ -478,9 +494,9 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
       HeadProb q = base;
       q.a = weights(v0, n);
       q.b = gop;
-      q.kb = (int)((n + HEAD_BK - 1) / HEAD_BK);
+      q.k = (int)n;
       q.splits = plan.splits;
-      q.per = (q.kb + plan.splits - 1) / plan.splits;
+      q.per = (int)((n + (int64_t)plan.splits * HEAD_BK - 1) / ((int64_t)plan.splits * HEAD_BK)) * HEAD_BK;
       q.part = part;
       q.ldn = plan.ldn;
       q.ldd = plan.ldd;
@@ -495,7 +511,6 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
     q.ldo = c.lddw;
     q.out_cols = c.width;
     q.add = c.add;
-    q.vec = c.width % 4 == 0 && c.lddw % 4 == 0 && (uintptr_t)c.dw % (c.bf16 ? 8 : 16) == 0;
     head_launch<HEAD_DW>(plan, direct, q, c.width, n, s);
   }
   if (c.rows > 0) {

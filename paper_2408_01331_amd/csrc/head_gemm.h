@@ -2,21 +2,22 @@
 // A(m, k) B(n, k) on v_mfma_f32_32x32x16_bf16, with the epilogues of HeadKind.
 //
 // A workgroup owns a BM x BN tile, its WGM x WGN waves (BM / WGM) x (BN / WGN) of it
-// in 32x32 blocks. k-blocks of 32 come into LDS by direct loads (no register between),
-// ST stages deep; while a stage's second half is multiplied the workgroup has passed
-// its barrier, the next stage's first operands are on their way from LDS and the stage
-// that was freed is being filled again.
+// in 32x32 blocks. k-blocks of KB come into LDS by direct loads (no register between),
+// ST stages deep; while a stage's last 16 k are multiplied the workgroup has passed its
+// barrier, the next stage's first operands are on their way from LDS and the stage that
+// was freed is being filled again.
 //
 // fp32 operands are three bf16 terms each, side by side in a stage, and a block is
 // multiplied with six of the nine products of terms. Weights in fp32, and weights in
 // bf16 whose rows do not lie at 16-byte boundaries, pass through registers on their way
 // to LDS (and are split there): they are read once, as they are.
 //
-// LDS images, in 16-byte chunks. An operand with k innermost: rows of 4 chunks, chunk c
-// of row r at c ^ (r / 4 % 4), so the 16 rows that a read takes at once lie in different
-// banks. One with k outermost: rows of R / 8 chunks, read transposed; the 64-byte groups
-// of the four k that a read takes are moved apart the same way. The direct loads write
-// LDS in lane order, so the order of chunks is made by the lanes' addresses in memory.
+// LDS images, in 16-byte chunks. An operand with k innermost: rows of KB / 8 chunks,
+// chunk c of row r at c ^ (r / 4 % 4) (KB = 32) or c ^ (r / 2 % 8) (64), so the 16 rows
+// that a read takes at once lie in different banks. One with k outermost: rows of R / 8
+// chunks, read transposed; the 64-byte groups of the four k that a read takes are moved
+// apart the same way. The direct loads write LDS in lane order, so the order of chunks is
+// made by the lanes' addresses in memory.
 #pragma once
 #include "op_device.h"
 #include "vocab.h"
@@ -29,6 +30,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 #define UN_LDS __attribute__((address_space(3)))
+
+// log2(e) and ln(2) in fp32, and what these lack
+constexpr float LOG2E = 1.44269504f, LOG2E_LOW = 1.92596299e-8f, LN2 = 0.693147182f, LN2_LOW = -1.90465421e-9f;
 
 constexpr uint32_t HEAD_OUT = 0x80000000u;   // an offset past every descriptor's end: a direct load writes zeros
 
@@ -43,22 +47,25 @@ template <int N> __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// One operand's tile of R rows (or columns) x 32 k.
-template <bool COL, int R, int W> struct HeadTile {
-  static constexpr int LOADS = R / 16 / W;     // direct loads of a wave
-  static constexpr int BYTES = R * 64;
-  static_assert(LOADS >= 1 && R % (16 * W) == 0, "every wave loads the same");
-  uint32_t voff[LOADS], k8;                    // k8: first k of the lane's chunk (k innermost)
+// Where chunk c of row r lies in its row, k innermost.
+template <int KB> __device__ __forceinline__ uint32_t head_chunk(uint32_t r, uint32_t c) { return c ^ (KB == 32 ? (r >> 2) & 3 : (r >> 1) & 7); }
+
+// One operand's tile of R rows (or columns) x KB k.
+template <bool COL, int R, int W, int KB> struct HeadTile {
+  static constexpr int BYTES = R * KB * 2, LOADS = BYTES / 1024 / W;  // direct loads of a wave
+  static_assert(LOADS >= 1 && BYTES % (1024 * W) == 0, "every wave loads the same");
+  uint32_t voff[LOADS];
+  uint32_t k8[COL ? 1 : LOADS];                // first k of the lane's chunk (k innermost)
   __device__ static uint32_t swizzle(int k) { return R >= 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2; }
   __device__ void setup(const HeadOperand& op, int64_t r0, int wave) {
     const int lane = threadIdx.x & 63;
-    k8 = 0;
 #pragma unroll
     for (int t = 0; t < LOADS; ++t) {
       if constexpr (!COL) {
-        const uint32_t row = (wave + t * W) * 16 + (lane >> 2), chunk = (lane & 3) ^ ((lane >> 4) & 3);
+        constexpr int C = KB / 8;
+        const uint32_t row = (wave + t * W) * (64 / C) + lane / C, chunk = head_chunk<KB>(row, lane % C);
         voff[t] = row * (uint32_t)(op.ld * 2) + chunk * 16;
-        k8 = chunk * 8;
+        k8[t] = chunk * 8;
       } else {
         constexpr int C = R / 8, KPI = 64 / C;
         const uint32_t k = (wave + t * W) * KPI + lane / C, chunk = (lane % C) ^ swizzle(k);
@@ -66,22 +73,25 @@ template <bool COL, int R, int W> struct HeadTile {
       }
     }
   }
-  // k-block kb of a plane into LDS at `lds`; !real: zeros
-  __device__ void load(const HeadOperand& op, int64_t r0, int plane, int kb, bool real, uint32_t lds, int wave) const {
-    const int64_t k0 = (int64_t)kb * HEAD_BK;
+  // The descriptor of k-block kb of a plane (!real: of nothing, so that zeros are loaded), and the wave's t-th load.
+  struct Block {
+    u32x4 rsrc;
+    int64_t left;
+  };
+  __device__ static Block block(const HeadOperand& op, int64_t r0, int plane, int kb, bool real) {
+    const int64_t k0 = (int64_t)kb * KB;
     const int64_t at = plane * op.plane + (COL ? k0 * op.ld + r0 : r0 * op.ld + k0);
-    const int64_t rows = COL ? min(op.rows - k0, (int64_t)HEAD_BK) : min(op.rows - r0, (int64_t)R);
+    const int64_t rows = COL ? min(op.rows - k0, (int64_t)KB) : min(op.rows - r0, (int64_t)R);
     const int64_t left = op.cols - (COL ? r0 : k0);
     const uint64_t base = (uint64_t)((const uint16_t*)op.p + at);
     const uint32_t bytes = real && rows > 0 && left > 0 ? (uint32_t)(((rows - 1) * op.ld + left) * 2) : 0;
-    const u32x4 rsrc = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base),
-                        (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffff),
-                        (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
-#pragma unroll
-    for (int t = 0; t < LOADS; ++t) {
-      const uint32_t v = COL ? voff[t] : (int64_t)k8 < left ? voff[t] : HEAD_OUT;
-      lds_load(__builtin_amdgcn_readfirstlane(lds + (wave + t * W) * 1024), v, rsrc);
-    }
+    return Block{{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffff),
+                  (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u},
+                 left};
+  }
+  __device__ void load(const Block& b, int t, uint32_t lds, int wave) const {
+    const uint32_t v = COL ? voff[t] : (int64_t)k8[COL ? 0 : t] < b.left ? voff[t] : HEAD_OUT;
+    lds_load(__builtin_amdgcn_readfirstlane(lds + (wave + t * W) * 1024), v, b.rsrc);
   }
 };
 
@@ -97,22 +107,22 @@ __device__ __forceinline__ void three_terms2(float a, float b, uint32_t (&h)[3])
   h[2] = f2bf2(a, b);
 }
 
-// One operand's tile of R rows (or columns) x 32 k of T, of any row stride, through
+// One operand's tile of R rows (or columns) x KB k of T, of any row stride, through
 // registers: chunks of 8 values, zeros where the operand ends.
-template <typename T, bool COL, int R, int NT> struct HeadRegs {
-  static constexpr int CH = R * 4 / NT, V = sizeof(T) / 2;
+template <typename T, bool COL, int R, int NT, int KB> struct HeadRegs {
+  static constexpr int CH = R * (KB / 8) / NT, V = sizeof(T) / 2, C = COL ? R / 8 : KB / 8;  // C: chunks of a row
   u32x4 raw[CH][V];
   __device__ static uint32_t lds_at(int t) {
     const uint32_t i = threadIdx.x + t * NT;
-    if constexpr (!COL) return (i >> 2) * 64 + (((i & 3) ^ ((i >> 4) & 3)) << 4);
-    else return i / (R / 8) * (R * 2) + (((i % (R / 8)) ^ HeadTile<COL, R, 1>::swizzle(i / (R / 8))) << 4);
+    if constexpr (!COL) return i / C * (KB * 2) + (head_chunk<KB>(i / C, i % C) << 4);
+    else return i / C * (R * 2) + (((i % C) ^ HeadTile<COL, R, 1, KB>::swizzle(i / C)) << 4);
   }
   __device__ void load(const HeadOperand& op, int64_t r0, int kb, bool real) {
-    const int64_t k0 = (int64_t)kb * HEAD_BK;
+    const int64_t k0 = (int64_t)kb * KB;
 #pragma unroll
     for (int t = 0; t < CH; ++t) {
       const int i = threadIdx.x + t * NT;
-      const int64_t row = COL ? k0 + i / (R / 8) : r0 + (i >> 2), col = COL ? r0 + i % (R / 8) * 8 : k0 + (i & 3) * 8;
+      const int64_t row = (COL ? k0 : r0) + i / C, col = (COL ? r0 : k0) + i % C * 8;
       const int have = real && row < op.rows ? (int)min(max(op.cols - col, (int64_t)0), (int64_t)8) : 0;
       const T* q = (const T*)op.p + row * op.ld + col;
       if (have == 8) {
@@ -148,7 +158,7 @@ template <typename T, bool COL, int R, int NT> struct HeadRegs {
           for (int p = 0; p < 3; ++p) h[p][e] = w[p];
         }
 #pragma unroll
-        for (int p = 0; p < 3; ++p) *(UN_LDS u32x4*)(at + p * (R * 64)) = h[p];
+        for (int p = 0; p < 3; ++p) *(UN_LDS u32x4*)(at + p * (R * KB * 2)) = h[p];
       }
     }
   }
@@ -156,20 +166,20 @@ template <typename T, bool COL, int R, int NT> struct HeadRegs {
 
 // The operand values of a wave's F blocks of 32 rows from row0 on: 8 consecutive k of
 // row lane % 32 from k-step s and lane / 32 on.
-template <bool COL, int R, int F> struct HeadFrags {
-  uint32_t at[COL ? F : 2];
+template <bool COL, int R, int F, int KB> struct HeadFrags {
+  uint32_t at[COL ? F : KB / 16];
   __device__ void setup(int row0) {
     const int lane = threadIdx.x & 63;
     if constexpr (!COL) {
       const uint32_t row = row0 + (lane & 31);
-      at[0] = row * 64 + (((lane >> 5) ^ ((lane >> 2) & 3)) << 4);
-      at[1] = row * 64 + (((2 + (lane >> 5)) ^ ((lane >> 2) & 3)) << 4);
+#pragma unroll
+      for (int s = 0; s < KB / 16; ++s) at[s] = row * (KB * 2) + (head_chunk<KB>(row, 2 * s + (lane >> 5)) << 4);
     } else {
       const int h = lane >> 4, a = lane & 15, k = 8 * (h >> 1) + (a >> 2);
 #pragma unroll
       for (int i = 0; i < F; ++i) {
         const uint32_t r = row0 + 32 * i + 16 * (h & 1) + 4 * (a & 3);
-        at[i] = k * R * 2 + (((r >> 3) ^ HeadTile<COL, R, 1>::swizzle(k)) << 4) + (r & 7) * 2;
+        at[i] = k * R * 2 + (((r >> 3) ^ HeadTile<COL, R, 1, KB>::swizzle(k)) << 4) + (r & 7) * 2;
       }
     }
   }
@@ -177,7 +187,7 @@ template <bool COL, int R, int F> struct HeadFrags {
 #pragma unroll
     for (int i = 0; i < F; ++i) {
       if constexpr (!COL) {
-        f[i] = __builtin_bit_cast(bf16x8, *(UN_LDS const u32x4*)(lds + at[s] + i * 2048));
+        f[i] = __builtin_bit_cast(bf16x8, *(UN_LDS const u32x4*)(lds + at[s] + i * (64 * KB)));
       } else {
         const uint32_t p = lds + at[i] + s * (16 * R * 2);
         const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((UN_LDS s16x4*)p));
@@ -193,11 +203,19 @@ template <HeadKind KIND> struct HeadShape {
 };
 
 // P: terms of an operand
-template <int BM, int BN, int WGM, int WGN, int ST, int P> struct HeadCfg {
-  static constexpr int bm = BM, bn = BN, wgm = WGM, wgn = WGN, st = ST, planes = P, waves = WGM * WGN;
+template <int BM, int BN, int WGM, int WGN, int ST, int KB, int P> struct HeadCfg {
+  static constexpr int bm = BM, bn = BN, wgm = WGM, wgn = WGN, st = ST, kb = KB, planes = P, waves = WGM * WGN;
   static constexpr int fm = BM / WGM / 32, fn = BN / WGN / 32;
-  static constexpr int stage = (BM + BN) * 64 * P;
+  static constexpr int stage = (BM + BN) * KB * 2 * P;
 };
+
+// f(Int<0>) .. f(Int<N - 1>)
+template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F&& f) {
+  if constexpr (I < N) {
+    f(Int<I>{});
+    each<N, I + 1>(f);
+  }
+}
 
 // acc <- the tile's products over k-blocks [kb0, kb1); leaves no load in flight and LDS
 // free. REG: A passes through registers, as values of T.
@@ -205,19 +223,20 @@ template <HeadKind KIND, class C, typename T, bool REG>
 __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int64_t n0, int kb0, int kb1, char* sm, f32x16 (&acc)[C::fm][C::fn]) {
   constexpr bool CA = HeadShape<KIND>::COL_A, CB = HeadShape<KIND>::COL_B;
   constexpr int W = C::waves, ST = C::st, FM = C::fm, FN = C::fn, P = C::planes;
-  typedef HeadTile<CA, C::bm, W> TA;
-  typedef HeadTile<CB, C::bn, W> TB;
+  constexpr int KB = C::kb, STEPS = KB / 16;
+  typedef HeadTile<CA, C::bm, W, KB> TA;
+  typedef HeadTile<CB, C::bn, W, KB> TB;
   constexpr int PER = P * ((REG ? 0 : TA::LOADS) + TB::LOADS);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = max(kb1 - kb0, 0);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(UN_LDS char*)sm;
   TA ta;
   TB tb;
-  HeadRegs<T, CA, C::bm, W * 64> ra;
+  HeadRegs<T, CA, C::bm, W * 64, KB> ra;
   if constexpr (!REG) ta.setup(p.a, m0, wave);
   tb.setup(p.b, n0, wave);
-  HeadFrags<CA, C::bm, FM> fa;
-  HeadFrags<CB, C::bn, FN> fb;
+  HeadFrags<CA, C::bm, FM, KB> fa;
+  HeadFrags<CB, C::bn, FN, KB> fb;
   fa.setup(wave / C::wgn * (C::bm / C::wgm));
   fb.setup(wave % C::wgn * (C::bn / C::wgn));
 #pragma unroll
@@ -230,61 +249,87 @@ __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int6
   // (behind the last block zeros are loaded: the counts of loads in flight stay the same)
   int next = 0;  // the block whose loads are issued next, of A one before where it passes through registers
   if constexpr (REG) ra.load(p.a, m0, kb0, true);
-  auto issue = [&](uint32_t slot) {
+  // part g of G of the next block's loads
+  auto issue = [&](uint32_t slot, auto part, auto parts) {
+    constexpr int g = decltype(part)::value, G = decltype(parts)::value;
     const uint32_t lds = lds0 + slot * C::stage;
-    if constexpr (REG) {
+    if constexpr (REG && g == 0) {
       ra.store(lds);  // (the compiler waits for these loads, and so for all before them)
       ra.load(p.a, m0, kb0 + next + 1, next + 1 < n);
     }
+    constexpr int LA = REG ? 0 : TA::LOADS, L = LA + TB::LOADS;
 #pragma unroll
     for (int k = 0; k < P; ++k) {
-      if constexpr (!REG) ta.load(p.a, m0, k, kb0 + next, next < n, lds + k * TA::BYTES, wave);
-      tb.load(p.b, n0, k, kb0 + next, next < n, lds + P * TA::BYTES + k * TB::BYTES, wave);
+      constexpr int t0 = g * PER / G, t1 = (g + 1) * PER / G;
+      if (k * L >= t1 || (k + 1) * L <= t0) continue;
+      const auto ba = TA::block(p.a, m0, k, kb0 + next, next < n);
+      const auto bb = TB::block(p.b, n0, k, kb0 + next, next < n);
+#pragma unroll
+      for (int t = 0; t < L; ++t) {
+        if (k * L + t < t0 || k * L + t >= t1) continue;
+        if (t < LA) ta.load(ba, t, lds + k * TA::BYTES, wave);
+        else tb.load(bb, t - LA, lds + P * TA::BYTES + k * TB::BYTES, wave);
+      }
     }
-    ++next;
+    if constexpr (g == G - 1) ++next;
   };
   bf16x8 a[2][P][FM], b[2][P][FN];
-  auto read = [&](uint32_t slot, int s) {
+  // (the step is a constant: registers have no run-time index)
+  auto read = [&](uint32_t slot, auto step) {
+    constexpr int s = decltype(step)::value;
     const uint32_t lds = lds0 + slot * C::stage;
 #pragma unroll
     for (int k = 0; k < P; ++k) {
-      fa.read(lds + k * TA::BYTES, s, a[s][k]);
-      fb.read(lds + P * TA::BYTES + k * TB::BYTES, s, b[s][k]);
+      fa.read(lds + k * TA::BYTES, s, a[s & 1][k]);
+      fb.read(lds + P * TA::BYTES + k * TB::BYTES, s, b[s & 1][k]);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto multiply = [&](int s) {
+  // between(part, parts): what is done between the products, a part of it behind each row of blocks
+  auto multiply = [&](auto step, auto between) {
+    constexpr int s = decltype(step)::value;
     // products of terms, the smallest first: (0, 2), (2, 0), (1, 1), (0, 1), (1, 0), (0, 0)
     constexpr int PA[6] = {0, 2, 1, 0, 1, 0}, PB[6] = {2, 0, 1, 1, 0, 0};
+    constexpr int T0 = P == 1 ? 5 : 0, G = (6 - T0) * FM;
+    auto row = [&](auto part) {
+      constexpr int g = decltype(part)::value, t = T0 + g / FM, x = g % FM;
 #pragma unroll
-    for (int t = P == 1 ? 5 : 0; t < 6; ++t)
-#pragma unroll
-      for (int x = 0; x < FM; ++x)
-#pragma unroll
-        for (int y = 0; y < FN; ++y)
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s][PA[t]][x], b[s][PB[t]][y], acc[x][y], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
+      for (int y = 0; y < FN; ++y)
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][PA[t]][x], b[s & 1][PB[t]][y], acc[x][y], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      between(part, Int<G>{});
+    };
+    each<G>(row);
   };
+  auto nothing = [](auto, auto) {};
 #pragma unroll
-  for (int s = 0; s < ST; ++s) issue(s);
+  for (int s = 0; s < ST; ++s) issue(s, Int<0>{}, Int<1>{});
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   wait_loads<REG ? 0 : (ST - 1) * PER>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  read(0, 0);
+  read(0, Int<0>{});
   uint32_t slot = 0;
   for (int i = 0; i < n; ++i) {
     const uint32_t slot1 = slot + 1 == ST ? 0 : slot + 1;
-    read(slot, 1);
-    multiply(0);
+    read(slot, Int<1>{});
+    multiply(Int<0>{}, nothing);
+    if constexpr (STEPS == 4) {
+      read(slot, Int<2>{});
+      multiply(Int<1>{}, nothing);
+      read(slot, Int<3>{});
+      multiply(Int<2>{}, nothing);
+    }
     // this stage is read, by every wave; the next one is there
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     wait_loads<REG ? 0 : (ST - 2) * PER>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    issue(slot);
-    read(slot1, 0);
-    multiply(1);
+    read(slot1, Int<0>{});
+    multiply(Int<STEPS - 1>{}, [&](auto part, auto parts) {
+      issue(slot, part, parts);
+      __builtin_amdgcn_sched_barrier(0);
+    });
     slot = slot1;
   }
   wait_loads<0>();
@@ -306,114 +351,155 @@ template <class C, class F> __device__ __forceinline__ void head_each(const f32x
       }
 }
 
-constexpr float LOG2E = 1.44269504088896f;
-
-// (m, s) and (n, t): maxima and sums of exp(z - maximum), joined. A part without values is (-inf, 0).
+// A part of a row's sum of exponentials: sum = s 2^m, m a whole number (so that what is
+// added to an exponent is exact), or -inf for a part without values.
 __device__ __forceinline__ float2 join_stat(float2 a, float2 b) {
   const float m = fmaxf(a.x, b.x);
   // (a NaN stays in s: it is where the maximum skips it)
-  const float ea = a.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((a.x - m) * LOG2E);
-  const float eb = b.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((b.x - m) * LOG2E);
-  return float2{m, (a.x == -INFINITY ? a.y : a.y * ea) + (b.x == -INFINITY ? b.y : b.y * eb)};
+  const float s = a.x == -INFINITY ? a.y : a.y * __builtin_amdgcn_exp2f(a.x - m);
+  const float t = b.x == -INFINITY ? b.y : b.y * __builtin_amdgcn_exp2f(b.x - m);
+  return float2{m, s + t};
+}
+
+// A tile's columns n as rows of LDS, so that they leave in whole lines: a row is `pitch`
+// bytes of T (16 more than its values, which moves the rows' banks apart).
+template <class C, typename T> constexpr int head_pitch() { return C::bm * (int)sizeof(T) + 16; }
+template <HeadKind KIND, class C, typename T> constexpr int head_lds() {
+  constexpr int out = KIND == HEAD_GRAD ? C::bn * head_pitch<C, bf16_t>() * C::planes : KIND == HEAD_DW ? C::bn * head_pitch<C, T>() : 0;
+  return out > C::stage * C::st ? out : C::stage * C::st;
 }
 
 template <HeadKind KIND, class C, typename T, bool REG>
 __global__ __launch_bounds__(C::waves * 64, 2) void head_kernel(HeadProb p) {
-  __shared__ __attribute__((aligned(1024))) char sm[C::stage * C::st];
+  __shared__ __attribute__((aligned(1024))) char sm[head_lds<KIND, C, T>()];
+  constexpr int NT = C::waves * 64;
   const int live = *p.live;
   const int tn = KIND == HEAD_DW ? p.tiles_n : min(p.tiles_n, (live + C::bn - 1) / C::bn);
   // A workgroup's tile: those of one XCD (workgroup number % 8) are neighbours, runs of
-  // them 4 tiles wide in n, so that its L2 holds what they share.
+  // them 1024 columns wide in n, so that its L2 holds what they share.
   const int total = p.tiles_m * tn, all = total * p.splits, share = (all + 7) / 8;
   const int j = blockIdx.x >> 3;
   int id = (blockIdx.x & 7) * share + j;
   if (j >= share || id >= all) return;
   const int split = id / total;
   id -= split * total;
-  constexpr int GN = 4;
+  constexpr int GN = 1024 / C::bn;
   const int group = id / (GN * p.tiles_m), wide = min(GN, tn - group * GN), in = id - group * GN * p.tiles_m;
   const int64_t m0 = (int64_t)(in / wide) * C::bm, n0 = (int64_t)(group * GN + in % wide) * C::bn;
-  int kb0 = 0, kb1 = p.kb;
-  if constexpr (KIND == HEAD_DX) kb0 = split * p.per, kb1 = min(p.kb, kb0 + p.per);
-  if constexpr (KIND == HEAD_DW) kb1 = (live + HEAD_BK - 1) / HEAD_BK;
+  const int k = KIND == HEAD_DW ? live : p.k;
+  const int k0 = KIND == HEAD_DX ? split * p.per : 0, k1 = KIND == HEAD_DX ? min(k, k0 + p.per) : k;
   f32x16 acc[C::fm][C::fn];
-  head_product<KIND, C, T, REG>(p, m0, n0, kb0, kb1, sm, acc);
+  head_product<KIND, C, T, REG>(p, m0, n0, k0 / C::kb, (k1 + C::kb - 1) / C::kb, sm, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / C::wgn * (C::bm / C::wgm), wn = wave % C::wgn * (C::bn / C::wgn);
 
   if constexpr (KIND == HEAD_STATS) {
-    // per column of the tile: over the lane's values, its other half's, the waves'
+    // Per column of the tile and 128 of its rows: over a lane's 32 of 64 values, the other
+    // half's, then the two 64's, of one wave or two. All tiles join in this order, so a
+    // row's sums do not depend on the kind that a call takes.
     float2* red = (float2*)sm;  // [wgm][bn]
-    const int wm = wave / C::wgn * (C::bm / C::wgm), wn = wave % C::wgn * (C::bn / C::wgn);
+    constexpr int UNITS = C::fm / 2;
+    static_assert(UNITS == 2 || C::wgm == 2, "128 rows are a wave's, or two waves'");
+    if (m0 + C::bm > p.vocab) {
+#pragma unroll
+      for (int y = 0; y < C::fn; ++y)
+#pragma unroll
+        for (int x = 0; x < C::fm; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (m0 + wm + 32 * x + 8 * (e / 4) + 4 * (lane >> 5) + e % 4 >= p.vocab) acc[x][y][e] = -INFINITY;
+    }
 #pragma unroll
     for (int y = 0; y < C::fn; ++y) {
       const int64_t n = n0 + wn + 32 * y + (lane & 31);
-      const int target = p.target && n < live ? p.target[n] - (int)m0 : -1;
-      float m = -INFINITY, s = 0.f;
-#pragma unroll
-      for (int x = 0; x < C::fm; ++x)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int v = wm + 32 * x + 8 * (e / 4) + 4 * (lane >> 5) + e % 4;
-          acc[x][y][e] = m0 + v < p.vocab ? acc[x][y][e] * p.inv_t : -INFINITY;
-          if (v == target) p.picked[n] = acc[x][y][e];
-          m = fmaxf(m, acc[x][y][e]);
-        }
-      if (m > -INFINITY || m != m) {
+      const int target = p.target && n < live ? p.target[n] - (int)m0 - wm : -1;
+      if (__any(target >= 0 && target < C::bm / C::wgm)) {
 #pragma unroll
         for (int x = 0; x < C::fm; ++x)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((acc[x][y][e] - m) * LOG2E);
-      } else {
-        // nothing but -inf and NaN: a NaN has to stay
-#pragma unroll
-        for (int x = 0; x < C::fm; ++x)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s += acc[x][y][e] != acc[x][y][e] ? acc[x][y][e] : 0.f;
+          for (int e = 0; e < 16; ++e)
+            if (32 * x + 8 * (e / 4) + 4 * (lane >> 5) + e % 4 == target) p.picked[n] = acc[x][y][e] * p.inv_t;
       }
-      float2 mine{m, s};
-      mine = join_stat(mine, float2{__shfl_xor(m, 32), __shfl_xor(s, 32)});
-      if (lane < 32) red[wave / C::wgn * C::bn + wn + 32 * y + lane] = mine;
-    }
-    __syncthreads();
-    for (int k = threadIdx.x; k < C::bn; k += C::waves * 64) {
-      float2 r = red[k];
+      float2 unit[UNITS];
 #pragma unroll
-      for (int w = 1; w < C::wgm; ++w) r = join_stat(r, red[w * C::bn + k]);
-      p.stat[(m0 / C::bm) * p.ldn + n0 + k] = r;
+      for (int u = 0; u < UNITS; ++u) {
+        float m = -INFINITY, s = 0.f;
+#pragma unroll
+        for (int x = 2 * u; x < 2 * u + 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[x][y][e]);
+        m = ceilf(m * p.scale);
+        const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int x = 2 * u; x < 2 * u + 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(fmaf(acc[x][y][e], p.scale, -from));
+        const float2 other{__shfl_xor(m, 32), __shfl_xor(s, 32)};
+        unit[u] = join_stat(float2{m, s}, other);
+      }
+      if constexpr (UNITS == 2) {
+        if (lane < 32) p.stat[((m0 + wm) / 128) * p.ldn + n] = join_stat(unit[0], unit[1]);
+      } else {
+        if (lane < 32) red[wave / C::wgn * C::bn + wn + 32 * y + lane] = unit[0];
+      }
+    }
+    if constexpr (UNITS == 1) {
+      __syncthreads();
+      for (int c = threadIdx.x; c < C::bn; c += NT) p.stat[(m0 / 128) * p.ldn + n0 + c] = join_stat(red[c], red[C::bn + c]);
     }
   } else if constexpr (KIND == HEAD_GRAD) {
-    const int wn = wave % C::wgn * (C::bn / C::wgn);
-    float lse[C::fn], coef[C::fn];
-    int target[C::fn];
+    constexpr int PITCH = head_pitch<C, bf16_t>(), PLANE = C::bn * PITCH;
 #pragma unroll
     for (int y = 0; y < C::fn; ++y) {
       const int64_t n = n0 + wn + 32 * y + (lane & 31);
       const bool on = n < live;
-      lse[y] = on ? p.lse[n] : 0.f;
-      coef[y] = on ? p.coef[n] : 0.f;
-      target[y] = on && p.target ? p.target[n] - p.first - (int)m0 : -1;
+      // softmax = 2^(z' - l) 2^(l - lse'), primes: times log2(e); l whole, so that the first difference rounds once. (Rows
+      // behind the live ones get zeros, the next products' padding.)
+      const float lse = on ? p.lse[n] : 0.f, l = rintf(lse * LOG2E);
+      const float rest = fmaf(lse, LOG2E_LOW, fmaf(lse, LOG2E, -l));
+      const float coef = on ? p.coef[n] : 0.f, f = coef * __builtin_amdgcn_exp2f(-rest);
+#pragma unroll
+      for (int x = 0; x < C::fm; ++x)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[x][y][e] = f * __builtin_amdgcn_exp2f(fmaf(acc[x][y][e], p.scale, -l));
+      const int target = on && p.target ? p.target[n] - p.first - (int)m0 - wm : -1;
+      if (__any(target >= 0 && target < C::bm / C::wgm)) {
+#pragma unroll
+        for (int x = 0; x < C::fm; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (32 * x + 8 * (e / 4) + 4 * (lane >> 5) + e % 4 == target) acc[x][y][e] -= coef;
+      }
+    }
+    if (m0 + C::bm > p.vocab) {  // columns behind the vocabulary are padding, too
+#pragma unroll
+      for (int y = 0; y < C::fn; ++y)
+#pragma unroll
+        for (int x = 0; x < C::fm; ++x)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (m0 + wm + 32 * x + 8 * (e / 4) + 4 * (lane >> 5) + e % 4 >= p.vocab) acc[x][y][e] = 0.f;
     }
     head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {
-      const int y = (n - wn) >> 5;
-      float g[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float q = __builtin_amdgcn_exp2f(fmaf(v[e], p.inv_t, -lse[y]) * LOG2E);
-        g[e] = coef[y] * (m + e == target[y] ? q - 1.f : q);
-        // rows behind the live ones and columns behind the vocabulary are the next products' padding
-        g[e] = n0 + n < live && m0 + m + e < p.vocab ? g[e] : 0.f;
-      }
-      uint16_t* o = p.g + (n0 + n) * p.ldg + m0 + m;
+      char* o = sm + n * PITCH + m * 2;
       if constexpr (C::planes == 1) {
-        *(u32x2*)o = u32x2{f2bf2(g[0], g[1]), f2bf2(g[2], g[3])};
+        *(u32x2*)o = u32x2{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
       } else {
         uint32_t h[2][3];
-        three_terms2(g[0], g[1], h[0]);
-        three_terms2(g[2], g[3], h[1]);
+        three_terms2(v[0], v[1], h[0]);
+        three_terms2(v[2], v[3], h[1]);
 #pragma unroll
-        for (int k = 0; k < 3; ++k) *(u32x2*)(o + k * p.gplane) = u32x2{h[0][k], h[1][k]};
+        for (int q = 0; q < 3; ++q) *(u32x2*)(o + q * PLANE) = u32x2{h[0][q], h[1][q]};
       }
     });
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < C::planes; ++q)
+#pragma unroll 4
+      for (int c = threadIdx.x; c < C::bn * C::bm / 8; c += NT) {
+        const int n = c / (C::bm / 8), m = c % (C::bm / 8) * 8;
+        *(u32x4*)(p.g + q * p.gplane + (n0 + n) * p.ldg + m0 + m) = *(const u32x4*)(sm + q * PLANE + n * PITCH + m * 2);
+      }
   } else if constexpr (KIND == HEAD_DX) {
     head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {
       if (n0 + n >= live) return;
@@ -421,32 +507,48 @@ __global__ __launch_bounds__(C::waves * 64, 2) void head_kernel(HeadProb p) {
       const f32x4 r = {v[0], v[1], v[2], v[3]};
       *o = p.add ? *o + r : r;
     });
-  } else {
+  } else if (p.add) {
     head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {
       const int64_t row = n0 + n, col = m0 + m;
-      if (row >= p.vocab || col >= p.out_cols) return;
+      const int have = row < p.vocab ? (int)min(max(p.out_cols - col, (int64_t)0), (int64_t)4) : 0;
       T* o = (T*)p.out + row * p.ldo + col;
-      if (p.vec) {
+      if (have == 4) {
         if constexpr (sizeof(T) == 4) {
-          const f32x4 r = {v[0], v[1], v[2], v[3]};
-          *(f32x4*)o = p.add ? *(const f32x4*)o + r : r;
+          *(f32x4_a4*)o = *(const f32x4_a4*)o + f32x4{v[0], v[1], v[2], v[3]};
         } else {
-          float f[4] = {v[0], v[1], v[2], v[3]};
-          if (p.add) {
-            const u32x2 w = *(const u32x2*)o;
-            f[0] += __uint_as_float(w[0] << 16);
-            f[1] += __uint_as_float(w[0] & 0xffff0000u);
-            f[2] += __uint_as_float(w[1] << 16);
-            f[3] += __uint_as_float(w[1] & 0xffff0000u);
-          }
-          *(u32x2*)o = u32x2{f2bf2(f[0], f[1]), f2bf2(f[2], f[3])};
+          const u32x2 w = *(const u32x2_a2*)o;
+          *(u32x2_a2*)o = u32x2{f2bf2(__uint_as_float(w[0] << 16) + v[0], __uint_as_float(w[0] & 0xffff0000u) + v[1]),
+                                f2bf2(__uint_as_float(w[1] << 16) + v[2], __uint_as_float(w[1] & 0xffff0000u) + v[3])};
         }
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (col + e < p.out_cols) V16<T>::store1(o + e, p.add ? V16<T>::load1(o + e) + v[e] : v[e]);
+          if (e < have) V16<T>::store1(o + e, V16<T>::load1(o + e) + v[e]);
       }
     });
+  } else {
+    constexpr int PITCH = head_pitch<C, T>(), N = V16<T>::N;
+    head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {
+      char* o = sm + n * PITCH + m * (int)sizeof(T);
+      if constexpr (sizeof(T) == 4) *(f32x4*)o = f32x4{v[0], v[1], v[2], v[3]};
+      else *(u32x2*)o = u32x2{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+    });
+    __syncthreads();
+#pragma unroll 4
+    for (int c = threadIdx.x; c < C::bn * C::bm / N; c += NT) {
+      const int n = c / (C::bm / N), m = c % (C::bm / N) * N;
+      const int64_t row = n0 + n, col = m0 + m;
+      const int have = row < p.vocab ? (int)min(max(p.out_cols - col, (int64_t)0), (int64_t)N) : 0;
+      const T* from = (const T*)(sm + n * PITCH) + m;
+      T* o = (T*)p.out + row * p.ldo + col;
+      if (have == N) {
+        *(u32x4_a2*)o = *(const u32x4*)from;
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (e < have) o[e] = from[e];
+      }
+    }
   }
 }
 

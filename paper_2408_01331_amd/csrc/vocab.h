@@ -59,7 +59,7 @@ hipError_t launch_embed_bwd(bool bf16, const EmbedPlan& plan, EmbedProb p, void*
 // instructions; fp32 operands enter as three bf16 terms whose sum they are, and six of
 // the nine products of terms (the others are below 2^-24 of the result's terms).
 // ---------------------------------------------------------------------------
-constexpr int HEAD_BK = 32;         // k of a block
+constexpr int HEAD_BK = 64;         // k of a block at most: what is laid out is padded to this
 constexpr int HEAD_BM = 256;        // the vocabulary's pieces and the partial sums' columns are padded to this
 constexpr int HEAD_PAD = 256;       // live rows are padded to this with zeros
 struct HeadOperand {
@@ -76,14 +76,14 @@ enum HeadKind {
 };
 struct HeadProb {
   HeadOperand a, b;
-  int32_t kb;                       // k-blocks (HEAD_DW: counted from `live`)
+  int32_t k;                        // (HEAD_DW: `live`)
   int32_t tiles_m, tiles_n;
-  int32_t splits, per;              // HEAD_DX: parts of k, and k-blocks of each
+  int32_t splits, per;              // HEAD_DX: parts of k, and k of each (a multiple of HEAD_BK)
   const int32_t* live;              // rows that count
   int32_t vocab;                    // HEAD_STATS, HEAD_GRAD: rows of A (the piece's)
-  float inv_t;
+  float inv_t, scale;               // 1 / T, and that times log2(e)
   const int32_t* target;            // [c], counted from the piece's first row; none: negative
-  float2* stat;                     // HEAD_STATS: [tiles_m][ldn]
+  float2* stat;                     // HEAD_STATS: [vocab / 128][ldn], as join_stat has them
   float* picked;                    // HEAD_STATS: z at the target
   const float *lse, *coef;          // HEAD_GRAD: [c]
   int32_t first;                    // HEAD_GRAD: the piece's first row of the table
@@ -94,7 +94,7 @@ struct HeadProb {
   void* out;                        // HEAD_DW: [rows of the piece][ldo]
   int64_t ldo;
   int32_t out_cols;
-  int32_t add, vec;                 // HEAD_DX, HEAD_DW: onto what is there; HEAD_DW: 4 values at a time are aligned
+  int32_t add;                      // HEAD_DX, HEAD_DW: onto what is there
 };
 
 
@@ -133,7 +133,7 @@ inline bool head_direct(bool bf16, const void* w, int32_t width, int64_t ldw) {
 struct HeadPlan {
   int planes;
   int64_t dp, npad;                 // columns and rows of the laid-out hidden states
-  bool small[4];                    // by HeadKind: small tiles (fp32: always)
+  int tile[4];                      // by HeadKind: 0 large, 1 medium, 2 small (bf16)
   int64_t piece;                    // vocabulary of a piece
   int splits;                       // HEAD_DX
   int64_t ldn, ldd;                 // rows and columns of its partial sums
