@@ -16,6 +16,12 @@ __device__ __forceinline__ int64_t index_at(const void* p, int wide, int64_t i) 
   return wide ? ((const int64_t*)p)[i] : (int64_t)((const int32_t*)p)[i];
 }
 
+// a row's target, -1 where it has none
+__device__ __forceinline__ int32_t head_target(const HeadCall& c, int64_t row) {
+  const int64_t t = index_at(c.targets, c.wide, row);
+  return t >= 0 && t < c.vocab && t != c.ignore ? (int32_t)t : -1;
+}
+
 struct HeadRows {
   HeadCall c;
   int32_t *map, *inv, *target, *live;   // [live] -> row; [row] -> number or -1; [live]
@@ -71,58 +77,50 @@ __global__ __launch_bounds__(256) void head_flag_kernel(HeadRows r) {
   if ((threadIdx.x & 63) == 0) r.flag[row] = any;
 }
 
-// Numbers the rows that count, in order (one workgroup; 8 rows a thread at a time),
-// with what the products read of each. A row that does not count gets its zeros here.
+// Numbers the rows that count, in order (one workgroup; 8 runs of 1024 rows at a time).
+// A row that does not count gets its zeros here.
 __global__ __launch_bounds__(1024) void head_rows_kernel(HeadRows r, int backward) {
   constexpr int PER = 8;
-  __shared__ int32_t sums[16];
+  __shared__ int32_t sums[PER][16];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const HeadCall& c = r.c;
   int32_t base = 0;
   for (int64_t r0 = 0; r0 < c.rows; r0 += 1024 * PER) {
-    int32_t target[PER], count = 0;
+    bool on[PER];
+    int32_t before[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-      const int64_t row = r0 + threadIdx.x * PER + k;
-      target[k] = -1;
-      if (row < c.rows) {
-        if (c.targets) {
-          const int64_t t = index_at(c.targets, c.wide, row);
-          if (t >= 0 && t < c.vocab && t != c.ignore) target[k] = (int32_t)t;
-        } else if (r.flag[row]) {
-          target[k] = 0;
-        }
-      }
-      count += target[k] >= 0;
+      const int64_t row = r0 + k * 1024 + threadIdx.x;
+      on[k] = false;
+      if (row < c.rows) on[k] = c.targets ? head_target(c, row) >= 0 : r.flag[row] != 0;
     }
-    int32_t run = count;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const uint64_t all = __ballot(on[k]);
+      before[k] = __popcll(all & (((uint64_t)1 << lane) - 1));
+      if (lane == 0) sums[k][w] = __popcll(all);
+    }
+    __syncthreads();
+    // the 128 counts' prefix sums, two a lane, in every wave
+    const int32_t a = sums[lane >> 3][lane * 2 & 15], both = a + sums[lane >> 3][(lane * 2 & 15) + 1];
+    int32_t run = both;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int32_t v = __shfl_up(run, o);
       if (lane >= o) run += v;
     }
-    if (lane == 63) sums[w] = run;
-    __syncthreads();
-    int32_t at = base + run - count;
-    for (int v = 0; v < 16; ++v) {
-      if (v < w) at += sums[v];
-      base += sums[v];
-    }
+    const int32_t ahead = base + run - both;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) before[k] += __shfl(w & 1 ? ahead + a : ahead, k * 8 + (w >> 1));
+    base += __shfl(run, 63);
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-      const int64_t row = r0 + threadIdx.x * PER + k;
-      if (row >= c.rows) break;
-      const bool on = target[k] >= 0;
-      r.inv[row] = on ? at : -1;
-      if (on) {
-        r.map[at] = (int32_t)row;
-        r.target[at] = target[k];
-        if (backward) {
-          r.lse[at] = c.lse[row];
-          r.coef[at] = c.dloss[row * c.dloss_step] * c.temperature;
-        }
-        ++at;
+      const int64_t row = r0 + k * 1024 + threadIdx.x;
+      if (row >= c.rows) continue;
+      r.inv[row] = on[k] ? before[k] : -1;
+      if (on[k]) {
+        r.map[before[k]] = (int32_t)row;
       } else if (!backward) {
         c.loss[row] = 0.f;
         c.lse[row] = 0.f;
@@ -133,16 +131,24 @@ __global__ __launch_bounds__(1024) void head_rows_kernel(HeadRows r, int backwar
 }
 
 // The rows that count, in chunks of 8 values, as bf16 or three bf16 terms of fp32, padded
-// with zeros to `dp` columns and to the next HEAD_PAD rows.
-template <typename T> __global__ __launch_bounds__(256) void head_layout_kernel(const T* x, int64_t ld, int d, int64_t rows, const int32_t* map,
-                                                                               const int32_t* live, uint16_t* o, int64_t dp, int64_t plane) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = dp / 8;
+// with zeros to `dp` columns and to the next HEAD_PAD rows; and what the products read of
+// each, by its number.
+template <typename T> __global__ __launch_bounds__(256) void head_layout_kernel(HeadRows r, uint16_t* o, int64_t rows, int64_t dp, int backward) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = dp / 8, plane = rows * dp, ld = r.c.ldx;
   const int64_t row = i / per;
-  const int c = (int)(i - row * per) * 8;
+  const int c = (int)(i - row * per) * 8, d = r.c.width;
   if (row >= rows) return;
-  const int64_t n = *live;
+  const T* x = (const T*)r.c.x;
+  const int64_t n = *r.live;
   if (row >= (n + HEAD_PAD - 1) / HEAD_PAD * HEAD_PAD) return;
-  const int64_t from = row < n ? map[row] : 0;
+  const int64_t from = row < n ? r.map[row] : 0;
+  if (c == 0 && row < n) {
+    if (r.c.targets) r.target[row] = head_target(r.c, from);
+    if (backward) {
+      r.lse[row] = r.c.lse[from];
+      r.coef[row] = r.c.dloss[from * r.c.dloss_step] * r.c.temperature;
+    }
+  }
   const int have = row < n ? min(max(d - c, 0), 8) : 0;
   if constexpr (sizeof(T) == 2) {
     u32x4 v = {0, 0, 0, 0};
@@ -327,7 +333,8 @@ template <typename T> __global__ __launch_bounds__(256) void head_dx_kernel(Head
 typedef HeadCfg<256, 256, 2, 4, 2, 64, 1> Large;
 typedef HeadCfg<128, 128, 2, 2, 2, 64, 1> Medium;
 typedef HeadCfg<128, 64, 2, 2, 3, 64, 1> Small;
-typedef HeadCfg<128, 64, 2, 2, 2, 32, 3> Terms;   // fp32
+typedef HeadCfg<128, 64, 2, 2, 2, 64, 1> SmallRegs;   // (through registers a stage less does)
+typedef HeadCfg<128, 64, 2, 2, 2, 32, 3> Terms;       // fp32
 
 constexpr int64_t HEAD_G_BYTES = (int64_t)512 << 20;   // of g's piece
 
@@ -337,17 +344,13 @@ template <HeadKind KIND, class C, typename T, bool REG> void head_go(HeadProb& p
   const int64_t all = (int64_t)p.tiles_m * p.tiles_n * p.splits;
   hipLaunchKernelGGL((head_kernel<KIND, C, T, REG>), dim3((unsigned)((all + 7) / 8 * 8)), dim3(C::waves * 64), 0, s, p);
 }
-// a product of m x n; direct: the weights' rows can be loaded directly
+// a product of m x n; direct: the weights' rows can be loaded directly (others pass through registers, of which large tiles have none left)
 template <HeadKind KIND> void head_launch(const HeadPlan& plan, bool direct, HeadProb& p, int64_t m, int64_t n, hipStream_t s) {
   constexpr bool W = KIND != HEAD_DW;  // A is the weights
-  auto go = [&](auto cfg) {
-    using C = decltype(cfg);
-    W && !direct ? head_go<KIND, C, bf16_t, W>(p, m, n, s) : head_go<KIND, C, bf16_t, false>(p, m, n, s);
-  };
   if (plan.planes == 3) head_go<KIND, Terms, float, W>(p, m, n, s);
-  else if (plan.tile[KIND] == 0) go(Large{});
-  else if (plan.tile[KIND] == 1) go(Medium{});
-  else go(Small{});
+  else if (plan.tile[KIND] == 0) head_go<KIND, Large, bf16_t, false>(p, m, n, s);
+  else if (plan.tile[KIND] == 1) W && !direct ? head_go<KIND, Medium, bf16_t, W>(p, m, n, s) : head_go<KIND, Medium, bf16_t, false>(p, m, n, s);
+  else W && !direct ? head_go<KIND, SmallRegs, bf16_t, W>(p, m, n, s) : head_go<KIND, Small, bf16_t, false>(p, m, n, s);
 }
 
 // A product's time on tiles of a kind, in us: rounds of the workgroups that run at once,
@@ -362,10 +365,10 @@ double head_time(const HeadTime& t, int64_t m, int64_t n, int64_t k, int64_t spl
   return (double)((tiles + t.slots - 1) / t.slots) * (kb * t.block + t.rest);
 }
 // the kind of tiles, and for HEAD_DX the parts of k, that take the least; partial sums are written and read at some 4 TB/s
-int head_tiles(bool bf16, int64_t m, int64_t n, int64_t k, int* splits = nullptr) {
+int head_tiles(bool bf16, bool direct, int64_t m, int64_t n, int64_t k, int* splits = nullptr) {
   int best = 0;
   double least = 1e300;
-  for (int t = bf16 ? 0 : 3; t < (bf16 ? 3 : 4); ++t)
+  for (int t = !bf16 ? 3 : direct ? 0 : 1; t < (bf16 ? 3 : 4); ++t)
     for (int64_t s = 1; s <= (splits ? std::min<int64_t>(128, k / 128 + 1) : 1); ++s) {
       const double us = head_time(HEAD_TIMES[t], m, n, k, s) + (splits ? (double)s * m * n * 8 / 4e6 : 0);
       if (us >= least) continue;
@@ -378,7 +381,7 @@ int head_tiles(bool bf16, int64_t m, int64_t n, int64_t k, int* splits = nullptr
 
 }  // namespace
 
-HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool backward) {
+HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool direct, bool backward) {
   HeadPlan p{};
   p.planes = bf16 ? 1 : 3;
   auto up = [](int64_t x, int64_t m) { return (x + m - 1) / m * m; };
@@ -390,10 +393,10 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool b
   p.piece = mv;
   if (backward && rows > 0) p.piece = std::min(mv, std::max<int64_t>(4096, HEAD_G_BYTES / (p.npad * 2 * p.planes) / HEAD_BM * HEAD_BM));
   p.splits = 1;
-  p.tile[HEAD_STATS] = head_tiles(bf16, vocab, rows, width);
-  p.tile[HEAD_GRAD] = head_tiles(bf16, p.piece, rows, width);
-  p.tile[HEAD_DX] = head_tiles(bf16, width, rows, p.piece, &p.splits);
-  p.tile[HEAD_DW] = head_tiles(bf16, width, p.piece, rows);
+  p.tile[HEAD_STATS] = head_tiles(bf16, direct, vocab, rows, width);
+  p.tile[HEAD_GRAD] = head_tiles(bf16, direct, p.piece, rows, width);
+  p.tile[HEAD_DX] = head_tiles(bf16, direct, width, rows, p.piece, &p.splits);
+  p.tile[HEAD_DW] = head_tiles(bf16, true, width, p.piece, rows);
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t a = at;
@@ -437,12 +440,8 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
   uint16_t* xs = (uint16_t*)(ws + plan.at_x);
   if (c.rows > 0) {
     const dim3 g = grid((plan.npad * (plan.dp / 8) + 255) / 256);
-    if (c.bf16)
-      hipLaunchKernelGGL((head_layout_kernel<bf16_t>), g, dim3(256), 0, s, (const bf16_t*)c.x, c.ldx, c.width, plan.npad, r.map, r.live, xs,
-                         plan.dp, plan.npad * plan.dp);
-    else
-      hipLaunchKernelGGL((head_layout_kernel<float>), g, dim3(256), 0, s, (const float*)c.x, c.ldx, c.width, plan.npad, r.map, r.live, xs,
-                         plan.dp, plan.npad * plan.dp);
+    if (c.bf16) hipLaunchKernelGGL((head_layout_kernel<bf16_t>), g, dim3(256), 0, s, r, xs, plan.npad, plan.dp, backward);
+    else hipLaunchKernelGGL((head_layout_kernel<float>), g, dim3(256), 0, s, r, xs, plan.npad, plan.dp, backward);
   }
   const bool direct = head_direct(c.bf16, c.w, c.width, c.ldw);
   const HeadOperand x{xs, plan.dp, plan.npad * plan.dp, plan.npad, (int32_t)plan.dp};

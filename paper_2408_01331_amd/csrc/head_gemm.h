@@ -107,53 +107,87 @@ __device__ __forceinline__ void three_terms2(float a, float b, uint32_t (&h)[3])
   h[2] = f2bf2(a, b);
 }
 
-// One operand's tile of R rows (or columns) x KB k of T, of any row stride, through
-// registers: chunks of 8 values, zeros where the operand ends.
+// One operand's tile of R rows (or columns) x KB k of T, of any alignment of its
+// elements, through registers: two blocks in flight, each in a set of its own, in chunks
+// of 8 values. Every block is the same number of loads (what lies past the operand reads
+// as zeros), which the waits count on.
 template <typename T, bool COL, int R, int NT, int KB> struct HeadRegs {
   static constexpr int CH = R * (KB / 8) / NT, V = sizeof(T) / 2, C = COL ? R / 8 : KB / 8;  // C: chunks of a row
-  u32x4 raw[CH][V];
+  static constexpr int LOADS = CH * V;
+  u32x4 raw[2][CH][V];
+  uint32_t voff[CH];
+  int have[2];               // columns of the block
+  const uint16_t* last[2];   // the operand's last value, where a 16-bit one stands alone behind the last whole word of its chunk
+  int last_at[2];            // the chunk's number and, of 8, the value's
+  __device__ void setup(const HeadOperand& op) {
+#pragma unroll
+    for (int t = 0; t < CH; ++t) {
+      const uint32_t i = threadIdx.x + t * NT;
+      voff[t] = (i / C * (uint32_t)op.ld + i % C * 8) * (uint32_t)sizeof(T);
+    }
+  }
   __device__ static uint32_t lds_at(int t) {
     const uint32_t i = threadIdx.x + t * NT;
     if constexpr (!COL) return i / C * (KB * 2) + (head_chunk<KB>(i / C, i % C) << 4);
     else return i / C * (R * 2) + (((i % C) ^ HeadTile<COL, R, 1, KB>::swizzle(i / C)) << 4);
   }
-  __device__ void load(const HeadOperand& op, int64_t r0, int kb, bool real) {
+  template <int SET> __device__ __forceinline__ void load(const HeadOperand& op, int64_t r0, int kb, bool real) {
     const int64_t k0 = (int64_t)kb * KB;
+    constexpr int ROWS = COL ? KB : R;
+    const int64_t rows = op.rows - (COL ? k0 : r0), left = op.cols - (COL ? r0 : k0);
+    const int64_t seen = min(rows, (int64_t)ROWS + 1);  // (one more than the block's, so that its last row's end is no end)
+    const bool any = real && rows > 0 && left > 0;
+    const T* base = (const T*)op.p + (COL ? k0 * op.ld + r0 : r0 * op.ld + k0);
+    have[SET] = (int)min(left, (int64_t)(C * 8));
+    if constexpr (V == 1) {
+      last[SET] = any && rows <= ROWS && left <= C * 8 && left % 2 == 1 ? base + (rows - 1) * op.ld + left - 1 : nullptr;
+      last_at[SET] = (int)((rows - 1) * (C * 8) + left - 1);
+    }
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, any ? (int)(((seen - 1) * op.ld + left) * (int64_t)sizeof(T)) : 0, 0x00020000);
 #pragma unroll
-    for (int t = 0; t < CH; ++t) {
-      const int i = threadIdx.x + t * NT;
-      const int64_t row = (COL ? k0 : r0) + i / C, col = (COL ? r0 : k0) + i % C * 8;
-      const int have = real && row < op.rows ? (int)min(max(op.cols - col, (int64_t)0), (int64_t)8) : 0;
-      const T* q = (const T*)op.p + row * op.ld + col;
-      if (have == 8) {
+    for (int t = 0; t < CH; ++t)
 #pragma unroll
-        for (int v = 0; v < V; ++v) raw[t][v] = ((const u32x4_a2*)q)[v];
-      } else {
+      for (int v = 0; v < V; ++v) raw[SET][t][v] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff[t] + 16 * v, 0, 0);
+  }
+  template <int SET> __device__ __forceinline__ void store(uint32_t lds) {
+    if constexpr (V == 1) {
+      if (last[SET]) {  // (a word that ends behind the operand has been read as 0)
+        const int at = last_at[SET], word = at % 8 / 2;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          raw[t][v] = u32x4{0, 0, 0, 0};
+        for (int t = 0; t < CH; ++t)
+          if ((int)threadIdx.x + t * NT == at / 8) {
+            const uint32_t v = *last[SET];
 #pragma unroll
-          for (int e = 0; e < 8 / V; ++e)
-            if (v * (8 / V) + e < have) {
-              if constexpr (V == 1) raw[t][v][e / 2] |= (uint32_t)q[e] << (16 * (e & 1));
-              else raw[t][v][e] = __float_as_uint(q[v * 4 + e]);
-            }
-        }
+            for (int e = 0; e < 4; ++e)
+              if (e == word) raw[SET][t][0][e] = v;
+          }
       }
     }
-  }
-  __device__ void store(uint32_t lds) const {
+    if (have[SET] < C * 8) {  // the operand's last columns: what follows in memory is the next row's
+#pragma unroll
+      for (int t = 0; t < CH; ++t) {
+        const int n = have[SET] - (int)((threadIdx.x + t * NT) % C) * 8;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int at = v * (8 / V) + e * (2 / V);  // first value of the word
+            if (at >= n) raw[SET][t][v][e] = 0;
+            if (V == 1 && at + 1 == n) raw[SET][t][v][e] &= 0xffffu;
+          }
+      }
+    }
 #pragma unroll
     for (int t = 0; t < CH; ++t) {
       const uint32_t at = lds + lds_at(t);
       if constexpr (V == 1) {
-        *(UN_LDS u32x4*)at = raw[t][0];
+        *(UN_LDS u32x4*)at = raw[SET][t][0];
       } else {
         u32x4 h[3];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           uint32_t w[3];
-          three_terms2(__uint_as_float(raw[t][e / 2][e % 2 * 2]), __uint_as_float(raw[t][e / 2][e % 2 * 2 + 1]), w);
+          three_terms2(__uint_as_float(raw[SET][t][e / 2][e % 2 * 2]), __uint_as_float(raw[SET][t][e / 2][e % 2 * 2 + 1]), w);
 #pragma unroll
           for (int p = 0; p < 3; ++p) h[p][e] = w[p];
         }
@@ -247,15 +281,23 @@ __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int6
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
   if (n == 0) return;
   // (behind the last block zeros are loaded: the counts of loads in flight stay the same)
-  int next = 0;  // the block whose loads are issued next, of A one before where it passes through registers
-  if constexpr (REG) ra.load(p.a, m0, kb0, true);
-  // part g of G of the next block's loads
-  auto issue = [&](uint32_t slot, auto part, auto parts) {
-    constexpr int g = decltype(part)::value, G = decltype(parts)::value;
+  int next = 0;  // the block whose loads are issued next
+  if constexpr (REG) {
+    ra.setup(p.a);
+    ra.template load<0>(p.a, m0, kb0, true);
+    ra.template load<1>(p.a, m0, kb0 + 1, 1 < n);
+  }
+  // Part g of G of the next block's loads. Where A passes through registers: first the
+  // block that waits there (in set SET, an even or odd one's) to LDS, last the loads of the
+  // one after the next. The compiler's wait in front of the first counts the loads that it
+  // knows, those of the other set: they are the latest, so it waits for what lies before
+  // them, direct loads that are a whole block old.
+  auto issue = [&](uint32_t slot, auto part, auto parts, auto set) {
+    constexpr int g = decltype(part)::value, G = decltype(parts)::value, SET = decltype(set)::value;
     const uint32_t lds = lds0 + slot * C::stage;
     if constexpr (REG && g == 0) {
-      ra.store(lds);  // (the compiler waits for these loads, and so for all before them)
-      ra.load(p.a, m0, kb0 + next + 1, next + 1 < n);
+      ra.template store<SET>(lds);
+      __builtin_amdgcn_sched_barrier(0);
     }
     constexpr int LA = REG ? 0 : TA::LOADS, L = LA + TB::LOADS;
 #pragma unroll
@@ -271,7 +313,10 @@ __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int6
         else tb.load(bb, t - LA, lds + P * TA::BYTES + k * TB::BYTES, wave);
       }
     }
-    if constexpr (g == G - 1) ++next;
+    if constexpr (g == G - 1) {
+      if constexpr (REG) ra.template load<SET>(p.a, m0, kb0 + next + 2, next + 2 < n);
+      ++next;
+    }
   };
   bf16x8 a[2][P][FM], b[2][P][FN];
   // (the step is a constant: registers have no run-time index)
@@ -302,15 +347,16 @@ __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int6
     each<G>(row);
   };
   auto nothing = [](auto, auto) {};
-#pragma unroll
-  for (int s = 0; s < ST; ++s) issue(s, Int<0>{}, Int<1>{});
+  each<ST>([&](auto st) { issue(st(), Int<0>{}, Int<1>{}, Int<(decltype(st)::value & 1)>{}); });
+  // loads that may be in flight when the oldest of ST (ST - 1) stages has to be there
+  constexpr int ALL = PER + (REG ? HeadRegs<T, CA, C::bm, W * 64, KB>::LOADS : 0), LAST = ALL - PER;
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  wait_loads<REG ? 0 : (ST - 1) * PER>();
+  wait_loads<(ST - 1) * ALL + LAST>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   read(0, Int<0>{});
   uint32_t slot = 0;
-  for (int i = 0; i < n; ++i) {
+  auto body = [&](auto set) {
     const uint32_t slot1 = slot + 1 == ST ? 0 : slot + 1;
     read(slot, Int<1>{});
     multiply(Int<0>{}, nothing);
@@ -322,15 +368,24 @@ __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int6
     }
     // this stage is read, by every wave; the next one is there
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    wait_loads<REG ? 0 : (ST - 2) * PER>();
+    wait_loads<(ST - 2) * ALL + LAST>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     read(slot1, Int<0>{});
     multiply(Int<STEPS - 1>{}, [&](auto part, auto parts) {
-      issue(slot, part, parts);
+      issue(slot, part, parts, set);
       __builtin_amdgcn_sched_barrier(0);
     });
     slot = slot1;
+  };
+  if constexpr (!REG) {
+    for (int i = 0; i < n; ++i) body(Int<0>{});
+  } else {
+    for (int i = 0; i < n; i += 2) {  // (a register set is a constant)
+      body(Int<(ST & 1)>{});
+      if (i + 1 == n) break;
+      body(Int<((ST + 1) & 1)>{});
+    }
   }
   wait_loads<0>();
   __syncthreads();

@@ -3,6 +3,7 @@
 // before every check has passed.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -433,6 +434,7 @@ template <typename A> un_status head_common(const char* F, const A* a, bool back
   if (a->index_bits != 32 && a->index_bits != 64) return bad(F, "index_bits must be 32 or 64");
   if (a->rows > 0 && (!a->x || !a->weight || !a->lse)) return bad(F, "x, weight or lse is NULL");
   if ((a->rows > 1 && a->ldx < a->width) || (a->vocab > 1 && a->ldw < a->width)) return bad(F, "a row stride is smaller than the width");
+  if (a->vocab > 1 && a->ldw > HEAD_MAX_LD) return bad(F, "a row stride of the weight above 2^21 is not supported", UN_ERR_UNSUPPORTED);
   c->bf16 = a->type == UN_TYPE_BF16;
   c->rows = a->rows;
   c->width = a->width;
@@ -440,11 +442,11 @@ template <typename A> un_status head_common(const char* F, const A* a, bool back
   c->x = a->x;
   c->w = a->weight;
   c->ldx = a->ldx;
-  c->ldw = a->ldw;
+  c->ldw = a->vocab > 1 ? a->ldw : a->width;
   c->wide = a->index_bits == 64;
   c->lse = const_cast<float*>(a->lse);
   c->temperature = 1.f;
-  *plan = head_plan(c->bf16, a->rows, a->width, a->vocab, backward);
+  *plan = head_plan(c->bf16, a->rows, a->width, a->vocab, head_direct(c->bf16, a->weight, a->width, c->ldw), backward);
   if (a->rows == 0 && !backward) return UN_OK;
   if (!a->workspace || a->workspace_bytes < plan->bytes) return bad(F, "workspace too small (un_vocab_workspace)", UN_ERR_BUFSIZE);
   if ((uintptr_t)a->workspace % 16) return bad(F, "workspace is not 16-byte aligned");
@@ -486,7 +488,8 @@ un_status un_vocab_workspace(int32_t type, int64_t rows, int32_t width, int32_t 
   if (!bytes) return bad(F, "bytes is NULL");
   const un_status st = head_sizes_ok(F, type, rows, width, vocab);
   if (st != UN_OK) return st;
-  *bytes = head_plan(type == UN_TYPE_BF16, rows, width, vocab, backward != 0).bytes;
+  const bool bf16 = type == UN_TYPE_BF16;
+  *bytes = std::max(head_plan(bf16, rows, width, vocab, bf16, backward != 0).bytes, head_plan(bf16, rows, width, vocab, false, backward != 0).bytes);
   return UN_OK;
 }
 

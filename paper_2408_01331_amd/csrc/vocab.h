@@ -125,10 +125,10 @@ struct HeadCall {
   bool add;                         // dW onto what is there
 };
 constexpr int HEAD_MAX_WIDTH = 1 << 16, HEAD_MAX_TOP = 128;
-constexpr int64_t HEAD_MAX_ROWS = (int64_t)1 << 24, HEAD_MAX_LD = (int64_t)1 << 20;
+constexpr int64_t HEAD_MAX_ROWS = (int64_t)1 << 24, HEAD_MAX_LD = (int64_t)1 << 21;   // (a tile's rows and one more within 2^31 bytes)
 // weights whose rows the direct loads take; others pass through registers
 inline bool head_direct(bool bf16, const void* w, int32_t width, int64_t ldw) {
-  return bf16 && (uintptr_t)w % 16 == 0 && width % 8 == 0 && ldw % 8 == 0 && ldw <= HEAD_MAX_LD;
+  return bf16 && (uintptr_t)w % 16 == 0 && width % 8 == 0 && ldw % 8 == 0;
 }
 struct HeadPlan {
   int planes;
@@ -140,7 +140,7 @@ struct HeadPlan {
   // offsets in the workspace
   size_t at_map, at_inv, at_target, at_lse, at_coef, at_flag, at_live, at_x, at_stat, at_picked, at_g, at_part, bytes;
 };
-HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool backward);
+HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool direct, bool backward);
 hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, void* workspace, hipStream_t s);
 
 }  // namespace un
