@@ -316,8 +316,15 @@ template <typename T> __global__ __launch_bounds__(256) void head_dx_kernel(Head
   f32x4 a = {0.f, 0.f, 0.f, 0.f};
   if (n >= 0) {
     const float* p = part + n * ldd + col;
+    const int64_t step = ldn * ldd;
     a = *(const f32x4*)p;
-    for (int s = 1; s < splits; ++s) a += *(const f32x4*)(p + s * ldn * ldd);
+    for (int s = 1; s < splits; s += 8) {
+      f32x4 b[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) b[u] = s + u < splits ? *(const f32x4*)(p + (s + u) * step) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < 8; ++u) a += b[u];
+    }
   }
   T* o = (T*)r.c.dx + row * r.c.lddx + col;
   if (col + 4 <= r.c.width) {

@@ -330,12 +330,6 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__
 // squares are those of the centred values, from the registers: a mean that is large
 // against the spread costs no digits.
 // ---------------------------------------------------------------------------
-// n of a vector's values less m, the others 0
-template <int N> __device__ __forceinline__ void centre(float (&f)[N], int n, float m) {
-#pragma unroll
-  for (int e = 0; e < N; ++e) f[e] = e < n ? f[e] - m : 0.f;
-}
-
 template <typename T, int TPR, int NV, bool ONCE>
 __global__ __launch_bounds__(norm_threads(TPR)) void layer_fwd_kernel(LayerProb p) {
   constexpr int N = V16<T>::N;
@@ -348,6 +342,15 @@ __global__ __launch_bounds__(norm_threads(TPR)) void layer_fwd_kernel(LayerProb 
   RowVec<T, NV> x, r;
   x.template load<ONCE>((const T*)p.x + at * p.ldx, live, TPR, t);
   if (p.r) r.template load<ONCE>((const T*)p.r + at * p.ldr, live, TPR, t);
+  constexpr bool HELD = TPR < 1024;  // (1024 threads have 128 registers each)
+  float w[NV][N], b[NV][N];
+  auto weights = [&](int j) {
+    load_f32<N>(p.w + (j * TPR + t) * N, live[j], w[j]);
+    if (p.b) load_f32<N>(p.b + (j * TPR + t) * N, live[j], b[j]);
+  };
+  if constexpr (HELD)
+#pragma unroll
+    for (int j = 0; j < NV; ++j) weights(j);
   float sum[1] = {0.f};
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -373,7 +376,12 @@ __global__ __launch_bounds__(norm_threads(TPR)) void layer_fwd_kernel(LayerProb 
   for (int j = 0; j < NV; ++j) {
     float f[N];
     x.get(j, f);
-    centre(f, live[j], mean);
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] -= mean;
+    if (live[j] < N) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[e] = e < live[j] ? f[e] : 0.f;
+    }
 #pragma unroll
     for (int e = 0; e < N; ++e) sq[0] = fmaf(f[e], f[e], sq[0]);
   }
@@ -387,33 +395,42 @@ __global__ __launch_bounds__(norm_threads(TPR)) void layer_fwd_kernel(LayerProb 
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = (j * TPR + t) * N;
-    float f[N], w[N], b[N];
-    load_f32<N>(p.w + c, live[j], w);
-    if (p.b) load_f32<N>(p.b + c, live[j], b);
+    float f[N];
+    if constexpr (!HELD) weights(j);
     x.get(j, f);
 #pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = fmaf((f[e] - mean) * q, w[e], p.b ? b[e] : 0.f);
+    for (int e = 0; e < N; ++e) f[e] = fmaf((f[e] - mean) * q, w[j][e], p.b ? b[j][e] : 0.f);
     store_vec<T>((T*)p.y + row * p.ldy + c, live[j], f);
   }
 }
 
+template <int TPR, int NV> constexpr int layer_rows() { return std::max(1, norm_rows<TPR, NV>() / 2); }
 // Backward, as the RMS norm's: shares of dw and db per workgroup, joined in order by
 // a second launch.
 template <typename T, int TPR, int NV, int R, bool ONCE>
 __global__ __launch_bounds__(norm_threads(TPR)) void layer_bwd_kernel(LayerProb p) {
   constexpr int N = V16<T>::N, NT = norm_threads(TPR), G = NT / TPR;
   __shared__ float sm[norm_sm<TPR, 2 * R>()];
-  __shared__ float acc[norm_acc<T, TPR, NV>()];
+  // Rows above 8192 values: the shares do not fit the registers, and each thread keeps its own in LDS (4096 x 16384 in bf16
+  // 243 us with the spilled ones).
+  constexpr bool IN_LDS = TPR == 1024 && NV * N > 8;
+  constexpr int ROW = TPR * NV * N;
+  __shared__ __attribute__((aligned(16))) float acc[IN_LDS ? 2 * ROW : norm_acc<T, TPR, NV>()];
   const int t = threadIdx.x & (TPR - 1), g = threadIdx.x / TPR, d = p.d;
-  float w[NV][N], dw[NV][N], db[NV][N];
+  constexpr bool HELD = TPR < 1024;  // 1024 threads have 128 registers each: the weights are read again (from the L1)
+  float w[NV][N], dw[IN_LDS ? 1 : NV][N], db[IN_LDS ? 1 : NV][N];
   int cnt[NV], flip = 0;
+  auto weights = [&](int j) { load_f32<N>(p.w + (j * TPR + t) * N, cnt[j], w[j]); };
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = (j * TPR + t) * N;
     cnt[j] = min(max(d - c, 0), N);
-    load_f32<N>(p.w + c, cnt[j], w[j]);
+    if constexpr (HELD) weights(j);
 #pragma unroll
-    for (int e = 0; e < N; ++e) dw[j][e] = db[j][e] = 0.f;
+    for (int e = 0; e < N; ++e) {
+      if constexpr (IN_LDS) acc[c + e] = acc[ROW + c + e] = 0.f;
+      else dw[j][e] = db[j][e] = 0.f;
+    }
   }
   const float invd = 1.f / (float)d;
   for (int64_t r0 = (int64_t)blockIdx.x * (G * R); r0 < p.rows; r0 += (int64_t)p.blocks * (G * R)) {
@@ -437,14 +454,20 @@ __global__ __launch_bounds__(norm_threads(TPR)) void layer_bwd_kernel(LayerProb 
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         float a[N], b[N];
+        if constexpr (!HELD) weights(j);
         s[k].get(j, a);
         dy[k].get(j, b);
-        centre(a, live[k][j], mean[k]);
+        // (behind the row's end dy is 0, and so is every term)
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          const float gx = b[e] * (a[e] * q[k]);
-          dw[j][e] += gx;
-          db[j][e] += b[e];
+          const float gx = b[e] * ((a[e] - mean[k]) * q[k]);
+          if constexpr (IN_LDS) {
+            acc[(j * TPR + t) * N + e] += gx;
+            acc[ROW + (j * TPR + t) * N + e] += b[e];
+          } else {
+            dw[j][e] += gx;
+            db[j][e] += b[e];
+          }
           sum[k] = fmaf(b[e], w[j][e], sum[k]);
           sum[R + k] = fmaf(gx, w[j][e], sum[R + k]);
         }
@@ -461,6 +484,7 @@ __global__ __launch_bounds__(norm_threads(TPR)) void layer_bwd_kernel(LayerProb 
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           float a[N], b[N], o[N];
+          if constexpr (!HELD) weights(j);
           s[k].get(j, a);
           dy[k].get(j, b);
           if (p.r) ds[k].get(j, o);
@@ -478,11 +502,16 @@ __global__ __launch_bounds__(norm_threads(TPR)) void layer_bwd_kernel(LayerProb 
 #pragma unroll
       for (int e = 0; e < N; ++e)
         if (e < cnt[j]) {
-          part[(j * TPR + t) * N + e] = dw[j][e];
-          part[d + (j * TPR + t) * N + e] = db[j][e];
+          const int c = (j * TPR + t) * N + e;
+          if constexpr (IN_LDS) {
+            part[c] = acc[c];
+            part[d + c] = acc[ROW + c];
+          } else {
+            part[c] = dw[j][e];
+            part[d + c] = db[j][e];
+          }
         }
   } else {
-    constexpr int ROW = TPR * NV * N;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       if (half) __syncthreads();
@@ -1246,7 +1275,7 @@ hipError_t launch_layer_bwd(bool bf16, const NormPlan& plan, const LayerProb& p,
   const bool once = p.rows * p.d * (bf16 ? 2 : 4) * (p.r ? 4 : 3) >= LAST_LEVEL;
   const hipError_t e = norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
     using T = decltype(t);
-    constexpr int MANY = norm_rows<tpr(), nv()>();
+    constexpr int MANY = layer_rows<tpr(), nv()>();
     const dim3 g(p.blocks), blk(norm_threads(tpr()));
     if (once) hipLaunchKernelGGL((layer_bwd_kernel<T, tpr(), nv(), MANY, true>), g, blk, 0, s, p);
     else hipLaunchKernelGGL((layer_bwd_kernel<T, tpr(), nv(), MANY, false>), g, blk, 0, s, p);
