@@ -307,12 +307,16 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadRows r, uint16_t*
   }
 }
 
-// dx of every row: the parts of its number's sum in order, or zeros
-template <typename T> __global__ __launch_bounds__(256) void head_dx_kernel(HeadRows r, const float* part, int splits, int64_t ldn, int64_t ldd) {
-  const int per = (r.c.width + 3) / 4;
+// Rows of a result from the parts of their sums, added in order: dx of every row that has
+// a number (others: zeros), or, without `inv`, dW.
+template <typename T>
+__global__ __launch_bounds__(256) void head_join_kernel(const int32_t* inv, int64_t rows, int width, const float* part, int splits, int64_t ldn,
+                                                        int64_t ldd, T* out, int64_t ldo, int add) {
+  const int per = (width + 3) / 4;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
-  if (row >= r.c.rows) return;
-  const int col = (int)(i - row * per) * 4, n = r.inv[row];
+  if (row >= rows) return;
+  const int col = (int)(i - row * per) * 4;
+  const int64_t n = inv ? inv[row] : row;
   f32x4 a = {0.f, 0.f, 0.f, 0.f};
   if (n >= 0) {
     const float* p = part + n * ldd + col;
@@ -326,14 +330,19 @@ template <typename T> __global__ __launch_bounds__(256) void head_dx_kernel(Head
       for (int u = 0; u < 8; ++u) a += b[u];
     }
   }
-  T* o = (T*)r.c.dx + row * r.c.lddx + col;
-  if (col + 4 <= r.c.width) {
+  T* o = out + row * ldo + col;
+  if (add) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < width) a[e] += V16<T>::load1(o + e);
+  }
+  if (col + 4 <= width) {
     if constexpr (sizeof(T) == 4) *(f32x4_a4*)o = a;
     else *(u32x2_a2*)o = u32x2{f2bf2(a[0], a[1]), f2bf2(a[2], a[3])};
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (col + e < r.c.width) V16<T>::store1(o + e, a[e]);
+      if (col + e < width) V16<T>::store1(o + e, a[e]);
   }
 }
 
@@ -371,17 +380,20 @@ double head_time(const HeadTime& t, int64_t m, int64_t n, int64_t k, int64_t spl
   const int64_t tiles = (m + t.bm - 1) / t.bm * ((n + t.bn - 1) / t.bn) * splits, kb = ((k + splits - 1) / splits + t.kb - 1) / t.kb;
   return (double)((tiles + t.slots - 1) / t.slots) * (kb * t.block + t.rest);
 }
-// the kind of tiles, and for HEAD_DX the parts of k, that take the least; partial sums are written and read at some 4 TB/s
-int head_tiles(bool bf16, bool direct, int64_t m, int64_t n, int64_t k, int* splits = nullptr) {
+// the kind of tiles, and of a long k the parts, that take the least; partial sums are written and read at some 4 TB/s, by a
+// launch more where one part needs none (`alone`)
+int head_tiles(bool bf16, bool direct, int64_t m, int64_t n, int64_t k, int* splits = nullptr, bool alone = false) {
+  constexpr int PARTS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
   int best = 0;
   double least = 1e300;
   for (int t = !bf16 ? 3 : direct ? 0 : 1; t < (bf16 ? 3 : 4); ++t)
-    for (int64_t s = 1; s <= (splits ? std::min<int64_t>(128, k / 128 + 1) : 1); ++s) {
-      const double us = head_time(HEAD_TIMES[t], m, n, k, s) + (splits ? (double)s * m * n * 8 / 4e6 : 0);
+    for (const int s : PARTS) {
+      if (s > 1 && (!splits || s > k / 128 + 1)) break;
+      const double us = head_time(HEAD_TIMES[t], m, n, k, s) + (splits && !(alone && s == 1) ? (double)s * m * n * 8 / 4e6 + (alone ? 4 : 0) : 0);
       if (us >= least) continue;
       least = us;
       best = t;
-      if (splits) *splits = (int)s;
+      if (splits) *splits = s;
     }
   return best;
 }
@@ -399,11 +411,12 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool d
   const int64_t mv = up(vocab, HEAD_BM);
   p.piece = mv;
   if (backward && rows > 0) p.piece = std::min(mv, std::max<int64_t>(4096, HEAD_G_BYTES / (p.npad * 2 * p.planes) / HEAD_BM * HEAD_BM));
-  p.splits = 1;
+  p.splits = p.splits_w = 1;
   p.tile[HEAD_STATS] = head_tiles(bf16, direct, vocab, rows, width);
   p.tile[HEAD_GRAD] = head_tiles(bf16, direct, p.piece, rows, width);
   p.tile[HEAD_DX] = head_tiles(bf16, direct, width, rows, p.piece, &p.splits);
-  p.tile[HEAD_DW] = head_tiles(bf16, true, width, p.piece, rows);
+  p.tile[HEAD_DW] = head_tiles(bf16, true, width, p.piece, rows, &p.splits_w, true);
+  p.ldnw = p.piece;
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t a = at;
@@ -421,6 +434,7 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool d
     p.at_coef = take(rows * 4);
     p.at_g = take(p.npad * p.piece * 2 * p.planes);
     p.at_part = take(p.splits * p.ldn * p.ldd * 4);
+    p.at_partw = take(p.splits_w > 1 ? p.splits_w * p.ldnw * p.ldd * 4 : 0);
   } else {
     p.at_picked = take(rows * 4);
     p.at_stat = take(mv / 128 * p.npad * 8);
@@ -479,6 +493,11 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
   uint16_t* g = (uint16_t*)(ws + plan.at_g);
   float* part = (float*)(ws + plan.at_part);
   const int64_t gplane = plan.npad * plan.piece;
+  auto join = [&](const int32_t* inv, int64_t rows, const float* sums, int splits, int64_t ldn, void* out, int64_t ldo, bool add) {
+    const dim3 blocks = grid((rows * ((c.width + 3) / 4) + 255) / 256);
+    if (c.bf16) hipLaunchKernelGGL((head_join_kernel<bf16_t>), blocks, dim3(256), 0, s, inv, rows, c.width, sums, splits, ldn, plan.ldd, (bf16_t*)out, ldo, add);
+    else hipLaunchKernelGGL((head_join_kernel<float>), blocks, dim3(256), 0, s, inv, rows, c.width, sums, splits, ldn, plan.ldd, (float*)out, ldo, add);
+  };
   for (int64_t v0 = 0; v0 < c.vocab; v0 += plan.piece) {
     const int64_t n = std::min<int64_t>(plan.piece, c.vocab - v0), padded = (n + HEAD_BM - 1) / HEAD_BM * HEAD_BM;
     const HeadOperand gop{g, plan.piece, gplane, plan.npad, (int32_t)padded};
@@ -502,7 +521,6 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
       q.b = gop;
       q.k = (int)n;
       q.splits = plan.splits;
-      q.per = (int)((n + (int64_t)plan.splits * HEAD_BK - 1) / ((int64_t)plan.splits * HEAD_BK)) * HEAD_BK;
       q.part = part;
       q.ldn = plan.ldn;
       q.ldd = plan.ldd;
@@ -517,13 +535,14 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
     q.ldo = c.lddw;
     q.out_cols = c.width;
     q.add = c.add;
+    q.splits = plan.splits_w;
+    q.part = (float*)(ws + plan.at_partw);
+    q.ldn = plan.ldnw;
+    q.ldd = plan.ldd;
     head_launch<HEAD_DW>(plan, direct, q, c.width, n, s);
+    if (plan.splits_w > 1) join(nullptr, n, q.part, plan.splits_w, plan.ldnw, q.out, c.lddw, c.add);
   }
-  if (c.rows > 0) {
-    const int64_t n = c.rows * ((c.width + 3) / 4);
-    if (c.bf16) hipLaunchKernelGGL((head_dx_kernel<bf16_t>), grid((n + 255) / 256), dim3(256), 0, s, r, part, plan.splits, plan.ldn, plan.ldd);
-    else hipLaunchKernelGGL((head_dx_kernel<float>), grid((n + 255) / 256), dim3(256), 0, s, r, part, plan.splits, plan.ldn, plan.ldd);
-  }
+  if (c.rows > 0) join(r.inv, c.rows, part, plan.splits, plan.ldn, c.dx, c.lddx, false);
   return hipGetLastError();
 }
 

@@ -442,7 +442,12 @@ __global__ __launch_bounds__(C::waves * 64, 2) void head_kernel(HeadProb p) {
   const int group = id / (GN * p.tiles_m), wide = min(GN, tn - group * GN), in = id - group * GN * p.tiles_m;
   const int64_t m0 = (int64_t)(in / wide) * C::bm, n0 = (int64_t)(group * GN + in % wide) * C::bn;
   const int k = KIND == HEAD_DW ? live : p.k;
-  const int k0 = KIND == HEAD_DX ? split * p.per : 0, k1 = KIND == HEAD_DX ? min(k, k0 + p.per) : k;
+  int k0 = 0, k1 = k;
+  if constexpr (KIND == HEAD_DX || KIND == HEAD_DW) {
+    const int per = ((k + p.splits - 1) / p.splits + HEAD_BK - 1) / HEAD_BK * HEAD_BK;
+    k0 = split * per;  // (behind the end: no blocks, zeros)
+    k1 = max(k0, min(k, k0 + per));
+  }
   f32x16 acc[C::fm][C::fn];
   head_product<KIND, C, T, REG>(p, m0, n0, k0 / C::kb, (k1 + C::kb - 1) / C::kb, sm, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -555,12 +560,13 @@ __global__ __launch_bounds__(C::waves * 64, 2) void head_kernel(HeadProb p) {
         const int n = c / (C::bm / 8), m = c % (C::bm / 8) * 8;
         *(u32x4*)(p.g + q * p.gplane + (n0 + n) * p.ldg + m0 + m) = *(const u32x4*)(sm + q * PLANE + n * PITCH + m * 2);
       }
-  } else if constexpr (KIND == HEAD_DX) {
+  } else if (KIND == HEAD_DX || p.splits > 1) {
+    const int64_t rows = KIND == HEAD_DX ? live : p.vocab;
     head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {
-      if (n0 + n >= live) return;
+      if (n0 + n >= rows) return;
       f32x4* o = (f32x4*)(p.part + ((int64_t)split * p.ldn + n0 + n) * p.ldd + m0 + m);
       const f32x4 r = {v[0], v[1], v[2], v[3]};
-      *o = p.add ? *o + r : r;
+      *o = KIND == HEAD_DX && p.add ? *o + r : r;
     });
   } else if (p.add) {
     head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {

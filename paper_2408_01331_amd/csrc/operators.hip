@@ -330,80 +330,95 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* __restrict__
 // squares are those of the centred values, from the registers: a mean that is large
 // against the spread costs no digits.
 // ---------------------------------------------------------------------------
-template <typename T, int TPR, int NV, bool ONCE>
+template <typename T, int TPR, int NV, int R, bool ONCE>
 __global__ __launch_bounds__(norm_threads(TPR)) void layer_fwd_kernel(LayerProb p) {
-  constexpr int N = V16<T>::N;
-  __shared__ float sm[norm_sm<TPR, 1>()];
+  constexpr int N = V16<T>::N, G = norm_threads(TPR) / TPR;
+  __shared__ float sm[norm_sm<TPR, R>()];
   const int t = threadIdx.x & (TPR - 1), d = p.d;
-  const int64_t row = (int64_t)blockIdx.x * (norm_threads(TPR) / TPR) + threadIdx.x / TPR, at = row < p.rows ? row : 0;
-  int live[NV], flip = 0;
+  const int64_t r0 = (int64_t)blockIdx.x * (G * R) + threadIdx.x / TPR;
+  int cnt[NV], live[R][NV], flip = 0;
+  RowVec<T, NV> x[R], r[R];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) live[j] = row < p.rows ? min(max(d - (j * TPR + t) * N, 0), N) : 0;
-  RowVec<T, NV> x, r;
-  x.template load<ONCE>((const T*)p.x + at * p.ldx, live, TPR, t);
-  if (p.r) r.template load<ONCE>((const T*)p.r + at * p.ldr, live, TPR, t);
-  constexpr bool HELD = TPR < 1024;  // (1024 threads have 128 registers each)
-  float w[NV][N], b[NV][N];
-  auto weights = [&](int j) {
-    load_f32<N>(p.w + (j * TPR + t) * N, live[j], w[j]);
-    if (p.b) load_f32<N>(p.b + (j * TPR + t) * N, live[j], b[j]);
-  };
-  if constexpr (HELD)
+  for (int j = 0; j < NV; ++j) cnt[j] = min(max(d - (j * TPR + t) * N, 0), N);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) weights(j);
-  float sum[1] = {0.f};
+  for (int k = 0; k < R; ++k) {
+    const int64_t row = r0 + k * G, at = row < p.rows ? row : 0;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    float f[N];
-    x.get(j, f);
-    if (p.r) {
-      float g[N];
-      r.get(j, g);
-#pragma unroll
-      for (int e = 0; e < N; ++e) f[e] += g[e];
-      x.raw[j] = V16<T>::pack(f);
-      x.get(j, f);  // the norm is that of the stored sum
-    }
-    if (p.s) store_vec<T>((T*)p.s + row * p.lds + (j * TPR + t) * N, live[j], f);
-#pragma unroll
-    for (int e = 0; e < N; ++e) sum[0] += f[e];
+    for (int j = 0; j < NV; ++j) live[k][j] = row < p.rows ? cnt[j] : 0;
+    x[k].template load<ONCE>((const T*)p.x + at * p.ldx, live[k], TPR, t);
+    if (p.r) r[k].template load<ONCE>((const T*)p.r + at * p.ldr, live[k], TPR, t);
   }
-  row_reduce<TPR, 1>(sum, Add{}, sm, flip);
-  x.forget();
-  const float mean = sum[0] / (float)d;
-  float sq[1] = {0.f};
+  float sum[R], sq[R], mean[R], q[R];
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    float f[N];
-    x.get(j, f);
+  for (int k = 0; k < R; ++k) {
+    sum[k] = 0.f;
 #pragma unroll
-    for (int e = 0; e < N; ++e) f[e] -= mean;
-    if (live[j] < N) {
+    for (int j = 0; j < NV; ++j) {
+      float f[N];
+      x[k].get(j, f);
+      if (p.r) {
+        float g[N];
+        r[k].get(j, g);
 #pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = e < live[j] ? f[e] : 0.f;
+        for (int e = 0; e < N; ++e) f[e] += g[e];
+        x[k].raw[j] = V16<T>::pack(f);
+        x[k].get(j, f);  // the norm is that of the stored sum
+      }
+      if (p.s) store_vec<T>((T*)p.s + (r0 + k * G) * p.lds + (j * TPR + t) * N, live[k][j], f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[k] += f[e];
     }
-#pragma unroll
-    for (int e = 0; e < N; ++e) sq[0] = fmaf(f[e], f[e], sq[0]);
   }
-  row_reduce<TPR, 1>(sq, Add{}, sm, flip);
-  x.forget();
-  const float q = 1.f / sqrtf(sq[0] / (float)d + p.eps);
-  if (p.stats && t == 0 && row < p.rows) {
-    p.stats[2 * row] = mean;
-    p.stats[2 * row + 1] = q;
+  row_reduce<TPR, R>(sum, Add{}, sm, flip);
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    x[k].forget();
+    mean[k] = sum[k] / (float)d;
+    sq[k] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float f[N];
+      x[k].get(j, f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[e] -= mean[k];
+      if (live[k][j] < N) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = e < live[k][j] ? f[e] : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) sq[k] = fmaf(f[e], f[e], sq[k]);
+    }
+  }
+  row_reduce<TPR, R>(sq, Add{}, sm, flip);
+#pragma unroll
+  for (int k = 0; k < R; ++k) {
+    const int64_t row = r0 + k * G;
+    x[k].forget();
+    q[k] = 1.f / sqrtf(sq[k] / (float)d + p.eps);
+    if (p.stats && t == 0 && row < p.rows) {
+      p.stats[2 * row] = mean[k];
+      p.stats[2 * row + 1] = q[k];
+    }
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = (j * TPR + t) * N;
-    float f[N];
-    if constexpr (!HELD) weights(j);
-    x.get(j, f);
+    float w[N], b[N];
+    load_f32<N>(p.w + c, cnt[j], w);
+    if (p.b) load_f32<N>(p.b + c, cnt[j], b);
 #pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = fmaf((f[e] - mean) * q, w[j][e], p.b ? b[j][e] : 0.f);
-    store_vec<T>((T*)p.y + row * p.ldy + c, live[j], f);
+    for (int k = 0; k < R; ++k) {
+      float f[N];
+      x[k].get(j, f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[e] = fmaf((f[e] - mean[k]) * q[k], w[e], p.b ? b[e] : 0.f);
+      store_vec<T>((T*)p.y + (r0 + k * G) * p.ldy + c, live[k][j], f);
+    }
   }
 }
 
+// (half the RMS norm's rows: two sums and two shares more. Its number / half, bf16, us: 32768 x 2048 111 / 104; 262144 x 64 79
+// / 44.)
 template <int TPR, int NV> constexpr int layer_rows() { return std::max(1, norm_rows<TPR, NV>() / 2); }
 // Backward, as the RMS norm's: shares of dw and db per workgroup, joined in order by
 // a second launch.
@@ -1266,9 +1281,17 @@ hipError_t launch_layer(bool bf16, const NormPlan& plan, const LayerProb& p, hip
   const bool once = p.rows * p.d * (bf16 ? 2 : 4) * ((p.r ? 2 : 1) + (p.s ? 2 : 1)) >= LAST_LEVEL;  // as the RMS norm's
   return norm_pick(bf16, plan, [&](auto t, auto tpr, auto nv) {
     using T = decltype(t);
-    const dim3 g((unsigned)((p.rows + plan.group - 1) / plan.group)), blk(norm_threads(tpr()));
-    if (once) hipLaunchKernelGGL((layer_fwd_kernel<T, tpr(), nv(), true>), g, blk, 0, s, p);
-    else hipLaunchKernelGGL((layer_fwd_kernel<T, tpr(), nv(), false>), g, blk, 0, s, p);
+    auto go = [&](auto r) {
+      const int64_t rows = plan.group * r();
+      const dim3 g((unsigned)((p.rows + rows - 1) / rows)), blk(norm_threads(tpr()));
+      if (once) hipLaunchKernelGGL((layer_fwd_kernel<T, tpr(), nv(), r(), true>), g, blk, 0, s, p);
+      else hipLaunchKernelGGL((layer_fwd_kernel<T, tpr(), nv(), r(), false>), g, blk, 0, s, p);
+    };
+    // Two rows a thread where there are rows enough for every CU: the second reduction keeps a workgroup longer than the RMS
+    // norm's, and two rows share it (one / two rows, bf16 with a residual, us: 32768 x 2048 98 / 88; 8192 x 8192 96 / 88; 262144 x
+    // 64 34 / 33; but 4096 x 16384, two vectors in each of 1024 threads, 93 / 96).
+    if (p.rows >= (int64_t)4096 * plan.group && !(plan.tpr == 1024 && plan.nv > 1)) go(Int<2>{});
+    else go(Int<1>{});
   });
 }
 hipError_t launch_layer_bwd(bool bf16, const NormPlan& plan, const LayerProb& p, float* dw, float* db, hipStream_t s) {

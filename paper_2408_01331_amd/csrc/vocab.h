@@ -78,7 +78,7 @@ struct HeadProb {
   HeadOperand a, b;
   int32_t k;                        // (HEAD_DW: `live`)
   int32_t tiles_m, tiles_n;
-  int32_t splits, per;              // HEAD_DX: parts of k, and k of each (a multiple of HEAD_BK)
+  int32_t splits;                   // HEAD_DX, HEAD_DW: parts of k
   const int32_t* live;              // rows that count
   int32_t vocab;                    // HEAD_STATS, HEAD_GRAD: rows of A (the piece's)
   float inv_t, scale;               // 1 / T, and that times log2(e)
@@ -89,7 +89,7 @@ struct HeadProb {
   int32_t first;                    // HEAD_GRAD: the piece's first row of the table
   uint16_t* g;                      // HEAD_GRAD
   int64_t ldg, gplane;
-  float* part;                      // HEAD_DX: [splits][ldn][ldd]
+  float* part;                      // HEAD_DX, HEAD_DW of several parts: [splits][ldn][ldd]
   int64_t ldn, ldd;
   void* out;                        // HEAD_DW: [rows of the piece][ldo]
   int64_t ldo;
@@ -135,10 +135,10 @@ struct HeadPlan {
   int64_t dp, npad;                 // columns and rows of the laid-out hidden states
   int tile[4];                      // by HeadKind: 0 large, 1 medium, 2 small (bf16)
   int64_t piece;                    // vocabulary of a piece
-  int splits;                       // HEAD_DX
-  int64_t ldn, ldd;                 // rows and columns of its partial sums
+  int splits, splits_w;             // parts of k of HEAD_DX and HEAD_DW
+  int64_t ldn, ldnw, ldd;           // rows of their partial sums, and columns
   // offsets in the workspace
-  size_t at_map, at_inv, at_target, at_lse, at_coef, at_flag, at_live, at_x, at_stat, at_picked, at_g, at_part, bytes;
+  size_t at_map, at_inv, at_target, at_lse, at_coef, at_flag, at_live, at_x, at_stat, at_picked, at_g, at_part, at_partw, bytes;
 };
 HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool direct, bool backward);
 hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, void* workspace, hipStream_t s);
