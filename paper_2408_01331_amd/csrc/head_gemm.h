@@ -73,25 +73,35 @@ template <bool COL, int R, int W, int KB> struct HeadTile {
       }
     }
   }
-  // The descriptor of k-block kb of a plane (!real: of nothing, so that zeros are loaded), and the wave's t-th load.
-  struct Block {
-    u32x4 rsrc;
-    int64_t left;
-  };
-  __device__ static Block block(const HeadOperand& op, int64_t r0, int plane, int kb, bool real) {
-    const int64_t k0 = (int64_t)kb * KB;
-    const int64_t at = plane * op.plane + (COL ? k0 * op.ld + r0 : r0 * op.ld + k0);
-    const int64_t rows = COL ? min(op.rows - k0, (int64_t)KB) : min(op.rows - r0, (int64_t)R);
-    const int64_t left = op.cols - (COL ? r0 : k0);
-    const uint64_t base = (uint64_t)((const uint16_t*)op.p + at);
-    const uint32_t bytes = real && rows > 0 && left > 0 ? (uint32_t)(((rows - 1) * op.ld + left) * 2) : 0;
-    return Block{{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xffff),
-                  (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u},
-                 left};
+  // The next block: where it begins and what is left of the operand from there on.
+  uint64_t base, step, plane;
+  uint32_t row_bytes, ld2;   // k innermost: from the first to the last row of the tile
+  int32_t left, wide;        // k left; k outermost: columns
+  __device__ void begin(const HeadOperand& op, int64_t r0, int kb) {
+    const int64_t k0 = (int64_t)kb * KB, rows = min(op.rows - r0, (int64_t)R), most = 1 << 30;
+    base = (uint64_t)((const uint16_t*)op.p + (COL ? k0 * op.ld + r0 : r0 * op.ld + k0));
+    step = COL ? (uint64_t)op.ld * (KB * 2) : KB * 2;
+    plane = (uint64_t)op.plane * 2;
+    ld2 = (uint32_t)op.ld * 2;
+    row_bytes = (uint32_t)(max(rows, (int64_t)1) - 1) * ld2;
+    wide = (int32_t)min(op.cols - r0, most);
+    left = (int32_t)min((COL ? op.rows : (int64_t)op.cols) - k0, most);
+    if (COL ? wide <= 0 : rows <= 0) left = 0;
   }
-  __device__ void load(const Block& b, int t, uint32_t lds, int wave) const {
-    const uint32_t v = COL ? voff[t] : (int64_t)k8[COL ? 0 : t] < b.left ? voff[t] : HEAD_OUT;
-    lds_load(__builtin_amdgcn_readfirstlane(lds + (wave + t * W) * 1024), v, b.rsrc);
+  __device__ void advance() {
+    base += step;
+    left -= KB;
+  }
+  // its descriptor (!real: of nothing, so that zeros are loaded), and the wave's t-th load
+  __device__ u32x4 block(int k, bool real) const {
+    const uint64_t at = base + k * plane;
+    const uint32_t bytes = COL ? (uint32_t)(min(left, KB) - 1) * ld2 + (uint32_t)wide * 2 : row_bytes + (uint32_t)left * 2;
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32) & 0xffff),
+                 (uint32_t)__builtin_amdgcn_readfirstlane(real && left > 0 ? bytes : 0), 0x00020000u};
+  }
+  __device__ void load(u32x4 rsrc, int t, uint32_t lds, int wave) const {
+    const uint32_t v = COL ? voff[t] : (int32_t)k8[COL ? 0 : t] < left ? voff[t] : HEAD_OUT;
+    lds_load(__builtin_amdgcn_readfirstlane(lds + (wave + t * W) * 1024), v, rsrc);
   }
 };
 
@@ -114,7 +124,7 @@ __device__ __forceinline__ void three_terms2(float a, float b, uint32_t (&h)[3])
 template <typename T, bool COL, int R, int NT, int KB> struct HeadRegs {
   static constexpr int CH = R * (KB / 8) / NT, V = sizeof(T) / 2, C = COL ? R / 8 : KB / 8;  // C: chunks of a row
   static constexpr int LOADS = CH * V;
-  u32x4 raw[2][CH][V];
+  u32x4 raw[2][CH][V], term[3];
   uint32_t voff[CH];
   int have[2];               // columns of the block
   const uint16_t* last[2];   // the operand's last value, where a 16-bit one stands alone behind the last whole word of its chunk
@@ -149,50 +159,57 @@ template <typename T, bool COL, int R, int NT, int KB> struct HeadRegs {
 #pragma unroll
       for (int v = 0; v < V; ++v) raw[SET][t][v] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, voff[t] + 16 * v, 0, 0);
   }
-  template <int SET> __device__ __forceinline__ void store(uint32_t lds) {
-    if constexpr (V == 1) {
-      if (last[SET]) {  // (a word that ends behind the operand has been read as 0)
-        const int at = last_at[SET], word = at % 8 / 2;
+  // Part g of G of a block's way to LDS. The first one waits for all of it.
+  template <int SET, int g, int G> __device__ __forceinline__ void store(uint32_t lds) {
+    if constexpr (g == 0) {
 #pragma unroll
-        for (int t = 0; t < CH; ++t)
-          if ((int)threadIdx.x + t * NT == at / 8) {
-            const uint32_t v = *last[SET];
+      for (int t = 0; t < CH; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (e == word) raw[SET][t][0][e] = v;
-          }
+        for (int v = 0; v < V; ++v) asm volatile("" : "+v"(raw[SET][t][v]));
+      if constexpr (V == 1) {
+        if (last[SET]) {  // (a word that ends behind the operand has been read as 0)
+          const int at = last_at[SET], word = at % 8 / 2;
+#pragma unroll
+          for (int t = 0; t < CH; ++t)
+            if ((int)threadIdx.x + t * NT == at / 8) {
+              const uint32_t v = *last[SET];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (e == word) raw[SET][t][0][e] = v;
+            }
+        }
+      }
+      if (have[SET] < C * 8) {  // the operand's last columns: what follows in memory is the next row's
+#pragma unroll
+        for (int t = 0; t < CH; ++t) {
+          const int n = have[SET] - (int)((threadIdx.x + t * NT) % C) * 8;
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int at = v * (8 / V) + e * (2 / V);  // first value of the word
+              if (at >= n) raw[SET][t][v][e] = 0;
+              if (V == 1 && at + 1 == n) raw[SET][t][v][e] &= 0xffffu;
+            }
+        }
       }
     }
-    if (have[SET] < C * 8) {  // the operand's last columns: what follows in memory is the next row's
+    // units of a pair of values (fp32), or of a chunk
+    constexpr int PER = V == 1 ? 1 : 4, U = CH * PER;
 #pragma unroll
-      for (int t = 0; t < CH; ++t) {
-        const int n = have[SET] - (int)((threadIdx.x + t * NT) % C) * 8;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int at = v * (8 / V) + e * (2 / V);  // first value of the word
-            if (at >= n) raw[SET][t][v][e] = 0;
-            if (V == 1 && at + 1 == n) raw[SET][t][v][e] &= 0xffffu;
-          }
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < CH; ++t) {
+    for (int u = g * U / G; u < (g + 1) * U / G; ++u) {
+      const int t = u / PER, e = u % PER;
       const uint32_t at = lds + lds_at(t);
       if constexpr (V == 1) {
         *(UN_LDS u32x4*)at = raw[SET][t][0];
       } else {
-        u32x4 h[3];
+        uint32_t w[3];
+        three_terms2(__uint_as_float(raw[SET][t][e / 2][e % 2 * 2]), __uint_as_float(raw[SET][t][e / 2][e % 2 * 2 + 1]), w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          uint32_t w[3];
-          three_terms2(__uint_as_float(raw[SET][t][e / 2][e % 2 * 2]), __uint_as_float(raw[SET][t][e / 2][e % 2 * 2 + 1]), w);
+        for (int p = 0; p < 3; ++p) term[p][e] = w[p];
+        if (e == 3)
 #pragma unroll
-          for (int p = 0; p < 3; ++p) h[p][e] = w[p];
-        }
-#pragma unroll
-        for (int p = 0; p < 3; ++p) *(UN_LDS u32x4*)(at + p * (R * KB * 2)) = h[p];
+          for (int p = 0; p < 3; ++p) *(UN_LDS u32x4*)(at + p * (R * KB * 2)) = term[p];
       }
     }
   }
@@ -267,8 +284,12 @@ __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int6
   TA ta;
   TB tb;
   HeadRegs<T, CA, C::bm, W * 64, KB> ra;
-  if constexpr (!REG) ta.setup(p.a, m0, wave);
+  if constexpr (!REG) {
+    ta.setup(p.a, m0, wave);
+    ta.begin(p.a, m0, kb0);
+  }
   tb.setup(p.b, n0, wave);
+  tb.begin(p.b, n0, kb0);
   HeadFrags<CA, C::bm, FM, KB> fa;
   HeadFrags<CB, C::bn, FN, KB> fb;
   fa.setup(wave / C::wgn * (C::bm / C::wgm));
@@ -295,17 +316,14 @@ __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int6
   auto issue = [&](uint32_t slot, auto part, auto parts, auto set) {
     constexpr int g = decltype(part)::value, G = decltype(parts)::value, SET = decltype(set)::value;
     const uint32_t lds = lds0 + slot * C::stage;
-    if constexpr (REG && g == 0) {
-      ra.template store<SET>(lds);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    if constexpr (REG) ra.template store<SET, g, G>(lds);
     constexpr int LA = REG ? 0 : TA::LOADS, L = LA + TB::LOADS;
 #pragma unroll
     for (int k = 0; k < P; ++k) {
       constexpr int t0 = g * PER / G, t1 = (g + 1) * PER / G;
       if (k * L >= t1 || (k + 1) * L <= t0) continue;
-      const auto ba = TA::block(p.a, m0, k, kb0 + next, next < n);
-      const auto bb = TB::block(p.b, n0, k, kb0 + next, next < n);
+      u32x4 ba = {}, bb = tb.block(k, next < n);
+      if constexpr (!REG) ba = ta.block(k, next < n);
 #pragma unroll
       for (int t = 0; t < L; ++t) {
         if (k * L + t < t0 || k * L + t >= t1) continue;
@@ -315,6 +333,8 @@ __device__ __forceinline__ void head_product(const HeadProb& p, int64_t m0, int6
     }
     if constexpr (g == G - 1) {
       if constexpr (REG) ra.template load<SET>(p.a, m0, kb0 + next + 2, next + 2 < n);
+      else ta.advance();
+      tb.advance();
       ++next;
     }
   };
