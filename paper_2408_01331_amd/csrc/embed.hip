@@ -68,13 +68,30 @@ __device__ __forceinline__ uint32_t key_in(const EmbedProb& p, int pass, int64_t
   return pass == 0 ? key_of(p, i) : p.keys[(pass + 1) & 1][i];
 }
 
+constexpr int SORT_BATCH = 8;   // places that a lane has in flight
+
+// A wave's part [a, b) of the block [i0, i1).
+template <int W> __device__ __forceinline__ void sort_part(int64_t i0, int64_t i1, int64_t& a, int64_t& b) {
+  const int64_t part = ((i1 - i0 + W * 64 - 1) / (W * 64)) * 64;
+  a = min(i1, i0 + (threadIdx.x >> 6) * part);
+  b = min(i1, a + part);
+}
+
 // Counts of the block's digits, a row of LDS per wave: cnt[w][digit].
 template <int W> __device__ __forceinline__ void sort_count(const EmbedProb& p, int pass, int bits, int64_t i0, int64_t i1, uint32_t* cnt) {
   const int D = 1 << bits, w = threadIdx.x >> 6, lane = threadIdx.x & 63, shift = pass * bits;
-  const int64_t part = ((i1 - i0 + W * 64 - 1) / (W * 64)) * 64, a = i0 + w * part, b = min(i1, a + part);
+  int64_t a, b;
+  sort_part<W>(i0, i1, a, b);
   for (int k = threadIdx.x; k < W * D; k += W * 64) cnt[k] = 0;
   __syncthreads();
-  for (int64_t i = a + lane; i < b; i += 64) atomicAdd(&cnt[w * D + ((key_in(p, pass, i) >> shift) & (D - 1))], 1u);
+  for (int64_t i = a + lane; i < b; i += 64 * SORT_BATCH) {
+    uint32_t key[SORT_BATCH];
+#pragma unroll
+    for (int u = 0; u < SORT_BATCH; ++u) key[u] = i + u * 64 < b ? key_in(p, pass, i + u * 64) : 0;
+#pragma unroll
+    for (int u = 0; u < SORT_BATCH; ++u)
+      if (i + u * 64 < b) atomicAdd(&cnt[w * D + ((key[u] >> shift) & (D - 1))], 1u);
+  }
   __syncthreads();
 }
 
@@ -83,7 +100,8 @@ template <int W> __device__ __forceinline__ void sort_count(const EmbedProb& p, 
 template <int W>
 __device__ __forceinline__ void sort_move(const EmbedProb& p, int pass, int bits, int64_t i0, int64_t i1, uint32_t* cnt, uint32_t* base) {
   const int D = 1 << bits, w = threadIdx.x >> 6, lane = threadIdx.x & 63, shift = pass * bits;
-  const int64_t part = ((i1 - i0 + W * 64 - 1) / (W * 64)) * 64, a = i0 + w * part, b = min(i1, a + part);
+  int64_t a, b;
+  sort_part<W>(i0, i1, a, b);
   for (int k = threadIdx.x; k < D; k += W * 64) {
     uint32_t at = base[k];
 #pragma unroll
@@ -95,29 +113,38 @@ __device__ __forceinline__ void sort_move(const EmbedProb& p, int pass, int bits
   }
   __syncthreads();
   uint32_t* mine = cnt + w * D;
-  for (int64_t i = a; i < b; i += 64) {
-    const bool on = i + lane < b;
-    const uint32_t key = on ? key_in(p, pass, i + lane) : 0;
-    const uint32_t place = !on ? 0 : pass == 0 ? (uint32_t)(i + lane) : p.place[(pass + 1) & 1][i + lane];
-    const uint32_t digit = (key >> shift) & (D - 1);
-    uint64_t same = __ballot(on);
-    for (int k = 0; k < bits; ++k) {
-      const uint64_t one = __ballot((digit >> k) & 1);
-      same &= (digit >> k) & 1 ? one : ~one;
+  for (int64_t i = a; i < b; i += 64 * SORT_BATCH) {
+    uint32_t key[SORT_BATCH], place[SORT_BATCH];
+#pragma unroll
+    for (int u = 0; u < SORT_BATCH; ++u) {
+      const int64_t at = i + u * 64 + lane;
+      key[u] = at < b ? key_in(p, pass, at) : 0;
+      place[u] = at >= b ? 0 : pass == 0 ? (uint32_t)at : p.place[(pass + 1) & 1][at];
     }
-    const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
-    if (on) {
-      const uint32_t first = mine[digit];
-      p.keys[pass & 1][first + rank] = key;
-      p.place[pass & 1][first + rank] = place;
-      // (a wave's LDS accesses happen in order: the read above is before this write)
-      if ((same >> lane) == 1) mine[digit] = first + rank + 1;
+#pragma unroll
+    for (int u = 0; u < SORT_BATCH; ++u) {
+      if (i + u * 64 >= b) break;
+      const bool on = i + u * 64 + lane < b;
+      const uint32_t digit = (key[u] >> shift) & (D - 1);
+      uint64_t same = __ballot(on);
+      for (int k = 0; k < bits; ++k) {
+        const uint64_t one = __ballot((digit >> k) & 1);
+        same &= (digit >> k) & 1 ? one : ~one;
+      }
+      const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+      if (on) {
+        const uint32_t first = mine[digit];
+        p.keys[pass & 1][first + rank] = key[u];
+        p.place[pass & 1][first + rank] = place[u];
+        // (a wave's LDS accesses happen in order: the read above is before this write)
+        if ((same >> lane) == 1) mine[digit] = first + rank + 1;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
-// base[0 .. D) <- its exclusive prefix sum (D up to 8 values a thread of 256)
+// base[0 .. D) <- its exclusive prefix sum
 template <int NT> __device__ __forceinline__ void sort_prefix(uint32_t* base, int D, uint32_t* sm) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, per = (D + NT - 1) / NT;
   uint32_t sum = 0;
@@ -164,25 +191,32 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedProb p, int passes,
 }
 
 // One pass over many workgroups: their counts, then their moves.
-__global__ __launch_bounds__(256) void sort_count_kernel(EmbedProb p, int pass, int bits, int64_t per) {
-  __shared__ uint32_t cnt[4 << SORT_BITS];
+template <int BITS> __global__ __launch_bounds__(1024) void sort_count_kernel(EmbedProb p, int pass, int bits, int64_t per) {
+  constexpr int W = 16;
+  __shared__ uint32_t cnt[W << BITS];
   const int64_t i0 = blockIdx.x * per, i1 = min(p.n, i0 + per);
   const int D = 1 << bits;
-  sort_count<4>(p, pass, bits, i0, i1, cnt);
-  for (int k = threadIdx.x; k < D; k += 256) p.table[(int64_t)blockIdx.x * D + k] = cnt[k] + cnt[D + k] + cnt[2 * D + k] + cnt[3 * D + k];
+  sort_count<W>(p, pass, bits, i0, i1, cnt);
+  for (int k = threadIdx.x; k < D; k += W * 64) {
+    uint32_t c = 0;
+#pragma unroll
+    for (int v = 0; v < W; ++v) c += cnt[v * D + k];
+    p.table[(int64_t)blockIdx.x * D + k] = c;
+  }
 }
-__global__ __launch_bounds__(256) void sort_move_kernel(EmbedProb p, int pass, int bits, int64_t per) {
-  __shared__ uint32_t cnt[4 << SORT_BITS], base[1 << SORT_BITS], before[1 << SORT_BITS], sm[4];
+template <int BITS> __global__ __launch_bounds__(1024) void sort_move_kernel(EmbedProb p, int pass, int bits, int64_t per) {
+  constexpr int W = 16;
+  __shared__ uint32_t cnt[W << BITS], base[1 << BITS], before[1 << BITS], sm[W];
   const int64_t i0 = blockIdx.x * per, i1 = min(p.n, i0 + per);
   const int D = 1 << bits;
-  for (int k = threadIdx.x; k < D; k += 256) {
+  for (int k = threadIdx.x; k < D; k += W * 64) {
     uint32_t all = 0, less = 0;
-    for (int b = 0; b < (int)gridDim.x; b += 8) {
-      uint32_t c[8];
+    for (int b = 0; b < (int)gridDim.x; b += 16) {
+      uint32_t c[16];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) c[u] = b + u < (int)gridDim.x ? p.table[(int64_t)(b + u) * D + k] : 0;
+      for (int u = 0; u < 16; ++u) c[u] = b + u < (int)gridDim.x ? p.table[(int64_t)(b + u) * D + k] : 0;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < 16; ++u) {
         all += c[u];
         less += b + u < (int)blockIdx.x ? c[u] : 0;
       }
@@ -191,10 +225,10 @@ __global__ __launch_bounds__(256) void sort_move_kernel(EmbedProb p, int pass, i
     before[k] = less;
   }
   __syncthreads();
-  sort_prefix<256>(base, D, sm);
-  for (int k = threadIdx.x; k < D; k += 256) base[k] += before[k];
-  sort_count<4>(p, pass, bits, i0, i1, cnt);
-  sort_move<4>(p, pass, bits, i0, i1, cnt, base);
+  sort_prefix<W * 64>(base, D, sm);
+  for (int k = threadIdx.x; k < D; k += W * 64) base[k] += before[k];
+  sort_count<W>(p, pass, bits, i0, i1, cnt);
+  sort_move<W>(p, pass, bits, i0, i1, cnt, base);
 }
 
 // ---------------------------------------------------------------------------
@@ -315,9 +349,9 @@ template <typename T> __global__ __launch_bounds__(64) void embed_join_kernel(Em
   const int lane = threadIdx.x & 63;
   const int64_t chunk = blockIdx.x / tiles, start = chunk * len, end = start + len;
   if (end >= p.n) return;
-  const uint32_t key = __builtin_amdgcn_readfirstlane(keys[end - 1]);
+  const uint32_t before = start > 0 ? keys[start - 1] : (uint32_t)p.vocab, key = __builtin_amdgcn_readfirstlane(keys[end - 1]);
   if (key == (uint32_t)p.vocab || __builtin_amdgcn_readfirstlane(keys[end]) != key) return;
-  if (start > 0 && __builtin_amdgcn_readfirstlane(keys[start - 1]) == key) return;  // began earlier
+  if (__builtin_amdgcn_readfirstlane(before) == key) return;  // began earlier
   const int c = ((int)(blockIdx.x % tiles) * 64 + lane) * 4, live = min(max(p.d - c, 0), 4);
   const int64_t step = (int64_t)2 * p.d;
   const float* part = p.part + chunk * step + c;
@@ -331,14 +365,25 @@ template <typename T> __global__ __launch_bounds__(64) void embed_join_kernel(Em
     const int m = ~on ? __builtin_ctzll(~on) + 1 : 64;
     more = !~on;
     part = p.part + k * step + c;
-    for (int i = 0; i < m; i += 8) {
-      float f[8][4];
+    for (int i = 0; i < m; i += 16) {
+      // (those behind the run's end read its last one, and are not added)
+      f32x4 f[16];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) load_f32<4>(part + (i + u) * step, i + u < m ? live : 0, f[u]);
+      for (int u = 0; u < 16; ++u) {
+        const float* q = part + min(i + u, m - 1) * step;
+        f[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (live == 4) {
+          f[u] = *(const f32x4_a4*)q;
+        } else {
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+          for (int e = 0; e < 3; ++e)
+            if (e < live) f[u][e] = q[e];
+        }
+      }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += f[u][e];
+      for (int u = 0; u < 16; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += i + u < m ? f[u][e] : 0.f;
     }
   }
   put_row<T, 4>(p, key, c, live, acc);
@@ -349,6 +394,8 @@ template <typename T> __global__ __launch_bounds__(64) void embed_join_kernel(Em
 // ---------------------------------------------------------------------------
 // Plans and launches
 // ---------------------------------------------------------------------------
+constexpr int64_t EMBED_FEW = 16384;
+
 EmbedPlan embed_plan(int64_t n, int32_t vocab, int32_t d) {
   EmbedPlan p{};
   int bits = 1;
@@ -359,7 +406,7 @@ EmbedPlan embed_plan(int64_t n, int32_t vocab, int32_t d) {
   p.bits = (bits + p.passes - 1) / p.passes;
   p.per = std::max<int64_t>(2048, (n + SORT_BLOCKS - 1) / SORT_BLOCKS);
   p.blocks = (int)((n + p.per - 1) / p.per);
-  p.chunk = 32;
+  p.chunk = n < EMBED_FEW ? 16 : 32;
   while (n / p.chunk > 4096) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -396,8 +443,13 @@ hipError_t launch_embed_bwd(bool bf16, const EmbedPlan& plan, EmbedProb p, void*
       hipLaunchKernelGGL(sort_one_kernel, dim3(1), dim3(1024), 0, s, p, plan.passes, plan.bits);
     } else {
       for (int k = 0; k < plan.passes; ++k) {
-        hipLaunchKernelGGL(sort_count_kernel, dim3(plan.blocks), dim3(256), 0, s, p, k, plan.bits, plan.per);
-        hipLaunchKernelGGL(sort_move_kernel, dim3(plan.blocks), dim3(256), 0, s, p, k, plan.bits, plan.per);
+        if (plan.bits <= 9) {
+          hipLaunchKernelGGL((sort_count_kernel<9>), dim3(plan.blocks), dim3(1024), 0, s, p, k, plan.bits, plan.per);
+          hipLaunchKernelGGL((sort_move_kernel<9>), dim3(plan.blocks), dim3(1024), 0, s, p, k, plan.bits, plan.per);
+        } else {
+          hipLaunchKernelGGL((sort_count_kernel<SORT_BITS>), dim3(plan.blocks), dim3(1024), 0, s, p, k, plan.bits, plan.per);
+          hipLaunchKernelGGL((sort_move_kernel<SORT_BITS>), dim3(plan.blocks), dim3(1024), 0, s, p, k, plan.bits, plan.per);
+        }
       }
     }
   }
