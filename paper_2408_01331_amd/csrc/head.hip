@@ -77,71 +77,90 @@ __global__ __launch_bounds__(256) void head_flag_kernel(HeadRows r) {
   if ((threadIdx.x & 63) == 0) r.flag[row] = any;
 }
 
-// Numbers the rows that count, in order (one workgroup; 8 runs of 1024 rows at a time).
-// A row that does not count gets its zeros here.
-__global__ __launch_bounds__(1024) void head_rows_kernel(HeadRows r, int backward) {
-  constexpr int PER = 8;
-  __shared__ int32_t sums[PER][16];
+// Numbers the rows [r0, r0 + 8 * NT) that count, in order from `base` on: emit(row, number
+// or -1) for each. Returns the next number. (All NT threads of the workgroup.)
+template <int NT, typename F> __device__ __forceinline__ int32_t head_number(const HeadRows& r, int64_t r0, int32_t base, int32_t* sums, F&& emit) {
+  constexpr int PER = 8, W = NT / 64;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const HeadCall& c = r.c;
-  int32_t base = 0;
-  for (int64_t r0 = 0; r0 < c.rows; r0 += 1024 * PER) {
-    bool on[PER];
-    int32_t before[PER];
+  bool on[PER];
+  int32_t before[PER];
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int64_t row = r0 + k * 1024 + threadIdx.x;
-      on[k] = false;
-      if (row < c.rows) on[k] = c.targets ? head_target(c, row) >= 0 : r.flag[row] != 0;
-    }
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const uint64_t all = __ballot(on[k]);
-      before[k] = __popcll(all & (((uint64_t)1 << lane) - 1));
-      if (lane == 0) sums[k][w] = __popcll(all);
-    }
-    __syncthreads();
-    // the 128 counts' prefix sums, two a lane, in every wave
-    const int32_t a = sums[lane >> 3][lane * 2 & 15], both = a + sums[lane >> 3][(lane * 2 & 15) + 1];
-    int32_t run = both;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int32_t v = __shfl_up(run, o);
-      if (lane >= o) run += v;
-    }
-    const int32_t ahead = base + run - both;
-#pragma unroll
-    for (int k = 0; k < PER; ++k) before[k] += __shfl(w & 1 ? ahead + a : ahead, k * 8 + (w >> 1));
-    base += __shfl(run, 63);
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < PER; ++k) {
-      const int64_t row = r0 + k * 1024 + threadIdx.x;
-      if (row >= c.rows) continue;
-      r.inv[row] = on[k] ? before[k] : -1;
-      if (on[k]) {
-        r.map[before[k]] = (int32_t)row;
-      } else if (!backward) {
-        c.loss[row] = 0.f;
-        c.lse[row] = 0.f;
-      }
-    }
+  for (int k = 0; k < PER; ++k) {
+    const int64_t row = r0 + k * NT + threadIdx.x;
+    on[k] = row < r.c.rows && (r.c.targets ? head_target(r.c, row) >= 0 : r.flag[row] != 0);
   }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const uint64_t all = __ballot(on[k]);
+    before[k] = __popcll(all & (((uint64_t)1 << lane) - 1));
+    if (lane == 0) sums[k * W + w] = __popcll(all);
+  }
+  __syncthreads();
+  // the counts' prefix sums, two a lane, in every wave
+  const int32_t a = lane * 2 < PER * W ? sums[lane * 2] : 0, both = a + (lane * 2 < PER * W ? sums[lane * 2 + 1] : 0);
+  int32_t run = both;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int32_t v = __shfl_up(run, o);
+    if (lane >= o) run += v;
+  }
+  const int32_t ahead = base + run - both;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int at = k * W + w, number = before[k] + __shfl(at & 1 ? ahead + a : ahead, at >> 1);
+    const int64_t row = r0 + k * NT + threadIdx.x;
+    if (row < r.c.rows) emit(row, on[k] ? number : -1);
+  }
+  base += __shfl(run, 63);
+  __syncthreads();
+  return base;
+}
+// what is kept of a row's number; a row without one gets its zeros here
+__device__ __forceinline__ void head_keep(const HeadRows& r, int64_t row, int32_t number, int backward) {
+  r.inv[row] = number;
+  if (number >= 0) {
+    r.map[number] = (int32_t)row;
+  } else if (!backward) {
+    r.c.loss[row] = 0.f;
+    r.c.lse[row] = 0.f;
+  }
+}
+__global__ __launch_bounds__(1024) void head_rows_kernel(HeadRows r, int backward) {
+  __shared__ int32_t sums[128];
+  int32_t base = 0;
+  for (int64_t r0 = 0; r0 < r.c.rows; r0 += 1024 * 8)
+    base = head_number<1024>(r, r0, base, sums, [&](int64_t row, int32_t n) { head_keep(r, row, n, backward); });
   if (threadIdx.x == 0) *r.live = base;
 }
 
+constexpr int HEAD_FEW = 256 * 8;   // rows that every workgroup of the next kernel numbers by itself
+
 // The rows that count, in chunks of 8 values, as bf16 or three bf16 terms of fp32, padded
 // with zeros to `dp` columns and to the next HEAD_PAD rows; and what the products read of
-// each, by its number.
-template <typename T> __global__ __launch_bounds__(256) void head_layout_kernel(HeadRows r, uint16_t* o, int64_t rows, int64_t dp, int backward) {
+// each, by its number. FEW: the rows are numbered here, too (a launch less: 32 rows 24.4 us,
+// so 21).
+template <typename T, bool FEW>
+__global__ __launch_bounds__(256) void head_layout_kernel(HeadRows r, uint16_t* o, int64_t rows, int64_t dp, int backward) {
+  __shared__ int32_t sums[32], map[FEW ? HEAD_FEW : 1];
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = dp / 8, plane = rows * dp, ld = r.c.ldx;
   const int64_t row = i / per;
   const int c = (int)(i - row * per) * 8, d = r.c.width;
-  if (row >= rows) return;
-  const T* x = (const T*)r.c.x;
-  const int64_t n = *r.live;
+  int64_t n, from;
+  if constexpr (FEW) {
+    n = head_number<256>(r, 0, 0, sums, [&](int64_t at, int32_t number) {
+      if (number >= 0) map[number] = (int32_t)at;
+      if (blockIdx.x == 0) head_keep(r, at, number, backward);
+    });
+    if (i == 0) *r.live = (int32_t)n;
+    if (row >= rows) return;
+    from = row < n ? map[row] : 0;
+  } else {
+    if (row >= rows) return;
+    n = *r.live;
+    from = row < n ? r.map[row] : 0;
+  }
   if (row >= (n + HEAD_PAD - 1) / HEAD_PAD * HEAD_PAD) return;
-  const int64_t from = row < n ? r.map[row] : 0;
+  const T* x = (const T*)r.c.x;
   if (c == 0 && row < n) {
     if (r.c.targets) r.target[row] = head_target(r.c, from);
     if (backward) {
@@ -457,12 +476,17 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
   const bool distill = !c.targets;
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
   if (distill && c.rows > 0) hipLaunchKernelGGL(head_flag_kernel, grid((c.rows + 3) / 4), dim3(256), 0, s, r);
-  hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(1024), 0, s, r, backward);
+  const bool few = c.rows > 0 && c.rows <= HEAD_FEW;
+  if (!few) hipLaunchKernelGGL(head_rows_kernel, dim3(1), dim3(1024), 0, s, r, backward);
   uint16_t* xs = (uint16_t*)(ws + plan.at_x);
   if (c.rows > 0) {
     const dim3 g = grid((plan.npad * (plan.dp / 8) + 255) / 256);
-    if (c.bf16) hipLaunchKernelGGL((head_layout_kernel<bf16_t>), g, dim3(256), 0, s, r, xs, plan.npad, plan.dp, backward);
-    else hipLaunchKernelGGL((head_layout_kernel<float>), g, dim3(256), 0, s, r, xs, plan.npad, plan.dp, backward);
+    auto go = [&](auto t) {
+      using T = decltype(t);
+      if (few) hipLaunchKernelGGL((head_layout_kernel<T, true>), g, dim3(256), 0, s, r, xs, plan.npad, plan.dp, backward);
+      else hipLaunchKernelGGL((head_layout_kernel<T, false>), g, dim3(256), 0, s, r, xs, plan.npad, plan.dp, backward);
+    };
+    c.bf16 ? go(bf16_t{}) : go(float{});
   }
   const bool direct = head_direct(c.bf16, c.w, c.width, c.ldw);
   const HeadOperand x{xs, plan.dp, plan.npad * plan.dp, plan.npad, (int32_t)plan.dp};
