@@ -436,6 +436,15 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool d
   p.tile[HEAD_DX] = head_tiles(bf16, direct, width, rows, p.piece, &p.splits);
   p.tile[HEAD_DW] = head_tiles(bf16, true, width, p.piece, rows, &p.splits_w, true);
   p.ldnw = p.piece;
+  auto threads = [&](int kind, int64_t m, int64_t n, int splits) {
+    const HeadTime& t = HEAD_TIMES[p.tile[kind]];
+    p.threads = std::max(p.threads, ((m + t.bm - 1) / t.bm * ((n + t.bn - 1) / t.bn) * splits + 8) * (p.tile[kind] == 0 ? 512 : 256));
+  };
+  threads(HEAD_STATS, vocab, rows, 1);
+  threads(HEAD_GRAD, p.piece, rows, 1);
+  threads(HEAD_DX, width, rows, p.splits);
+  threads(HEAD_DW, width, p.piece, p.splits_w);
+  p.threads = std::max({p.threads, p.npad * (p.dp / 8) + 256, std::max(rows, p.splits_w > 1 ? p.piece : 0) * ((width + 3) / 4) + 256, rows * 64 + 1024});
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t a = at;

@@ -420,11 +420,10 @@ un_status head_sizes_ok(const char* F, int32_t type, int64_t rows, int32_t width
   if (width > HEAD_MAX_WIDTH) return bad(F, "a width above 65536 is not supported", UN_ERR_UNSUPPORTED);
   if (rows > HEAD_MAX_ROWS) return bad(F, "more than 2^24 rows are not supported", UN_ERR_UNSUPPORTED);
   if (vocab > (1 << 30)) return bad(F, "a vocabulary above 2^30 is not supported", UN_ERR_UNSUPPORTED);
-  // tiles of 128 x 64, up to 128 parts of a sum, and 4 values a thread of the rows' kernels
-  const int64_t v = ((int64_t)vocab + 127) / 128 + 2, n = (rows + 63) / 64 + 4, d = ((int64_t)width + 127) / 128 + 1;
-  if (too_many(v * n + 8, 256) || too_many(d * n * 128 + 8, 256) || too_many(d * 2 * v + 8, 256) || too_many((rows + 256) * d * 32 / 256 + 8, 256))
-    return bad(F, "too many rows, columns or vocabulary", UN_ERR_UNSUPPORTED);
   return UN_OK;
+}
+un_status head_plan_ok(const char* F, const HeadPlan& plan) {
+  return too_many(plan.threads, 1) ? bad(F, "too many rows, columns or vocabulary", UN_ERR_UNSUPPORTED) : UN_OK;
 }
 
 // what all four calls check and take over (A: their arguments)
@@ -447,6 +446,7 @@ template <typename A> un_status head_common(const char* F, const A* a, bool back
   c->lse = const_cast<float*>(a->lse);
   c->temperature = 1.f;
   *plan = head_plan(c->bf16, a->rows, a->width, a->vocab, head_direct(c->bf16, a->weight, a->width, c->ldw), backward);
+  if (const un_status too = head_plan_ok(F, *plan); too != UN_OK) return too;
   if (a->rows == 0 && !backward) return UN_OK;
   if (!a->workspace || a->workspace_bytes < plan->bytes) return bad(F, "workspace too small (un_vocab_workspace)", UN_ERR_BUFSIZE);
   if ((uintptr_t)a->workspace % 16) return bad(F, "workspace is not 16-byte aligned");
@@ -489,7 +489,10 @@ un_status un_vocab_workspace(int32_t type, int64_t rows, int32_t width, int32_t 
   const un_status st = head_sizes_ok(F, type, rows, width, vocab);
   if (st != UN_OK) return st;
   const bool bf16 = type == UN_TYPE_BF16;
-  *bytes = std::max(head_plan(bf16, rows, width, vocab, bf16, backward != 0).bytes, head_plan(bf16, rows, width, vocab, false, backward != 0).bytes);
+  // (weights that the products read directly, and others)
+  const HeadPlan direct = head_plan(bf16, rows, width, vocab, bf16, backward != 0), other = head_plan(bf16, rows, width, vocab, false, backward != 0);
+  if (const un_status too = head_plan_ok(F, direct); too != UN_OK) return too;
+  *bytes = std::max(direct.bytes, other.bytes);
   return UN_OK;
 }
 

@@ -137,6 +137,7 @@ struct HeadPlan {
   int64_t piece;                    // vocabulary of a piece
   int splits, splits_w;             // parts of k of HEAD_DX and HEAD_DW
   int64_t ldn, ldnw, ldd;           // rows of their partial sums, and columns
+  int64_t threads;                  // of the largest launch
   // offsets in the workspace
   size_t at_map, at_inv, at_target, at_lse, at_coef, at_flag, at_live, at_x, at_stat, at_picked, at_g, at_part, at_partw, bytes;
 };

@@ -143,3 +143,67 @@ def test_embedding_python(monkeypatch):
         ops.embedding_backward(torch.zeros(3, 8), t, 5, out=torch.zeros(4, 8))
     with pytest.raises(ValueError, match="out's rows must not overlap"):
         ops.embedding_backward(torch.zeros(3, 8), t, 5, out=torch.zeros(8).expand(5, 8))
+
+
+# ---------------------------------------------------------------------------
+# Losses over a vocabulary
+# ---------------------------------------------------------------------------
+HEAD = dict(type=0, width=64, vocab=10, index_bits=64, rows=4, x=P, ldx=64, weight=P, ldw=64, lse=P, workspace=P, workspace_bytes=1 << 30)
+GRADS = dict(dloss=P, dloss_stride=1, dx=P, lddx=64, dweight=P, lddw=64)
+TEACHER = dict(top=3, logits_type=1, ids=P, logits=P, temperature=1.0, picked=P)
+CALLS = {"un_vocab_loss": ("un_vocab_loss_args", {**HEAD, "targets": P, "loss": P}),
+         "un_vocab_loss_backward": ("un_vocab_loss_grad_args", {**HEAD, **GRADS, "targets": P}),
+         "un_distill_loss": ("un_distill_loss_args", {**HEAD, **TEACHER, "loss": P}),
+         "un_distill_loss_backward": ("un_distill_loss_grad_args", {**HEAD, **GRADS, **TEACHER})}
+
+
+@pytest.mark.parametrize("fn", CALLS)
+@pytest.mark.parametrize("change,want,text", [
+    (dict(type=2), 1, "type"), (dict(rows=-1), 1, "rows"), (dict(width=0), 1, "width"), (dict(vocab=0), 1, "vocab"),
+    (dict(width=65537, ldx=70000, ldw=70000, lddx=70000, lddw=70000), 7, "65536"), (dict(rows=(1 << 24) + 1), 7, "2^24"),
+    (dict(vocab=(1 << 30) + 1), 7, "2^30"), (dict(rows=1 << 24, vocab=1 << 24), 7, "too many"), (dict(index_bits=8), 1, "index_bits"),
+    (dict(x=None), 1, "NULL"), (dict(weight=None), 1, "NULL"), (dict(lse=None), 1, "NULL"), (dict(ldx=63), 1, "stride"),
+    (dict(ldw=63), 1, "stride"), (dict(ldw=(1 << 21) + 1), 7, "2^21"), (dict(workspace=None), 6, "workspace"),
+    (dict(workspace_bytes=100), 6, "workspace"), (dict(workspace=P + 8), 1, "aligned")])
+def test_head_refused(fn, change, want, text):
+    struct, base = CALLS[fn]
+    known = {k for k, _ in getattr(U, struct)._fields_}
+    refused(fn, struct, base, {k: v for k, v in change.items() if k in known}, want, text)
+
+
+@pytest.mark.parametrize("fn,change,want,text", [
+    ("un_vocab_loss", dict(targets=None), 1, "NULL"), ("un_vocab_loss", dict(loss=None), 1, "NULL"),
+    ("un_vocab_loss_backward", dict(targets=None), 1, "NULL"), ("un_distill_loss", dict(loss=None), 1, "NULL"),
+    *[(fn, change, 1, text) for fn in ("un_vocab_loss_backward", "un_distill_loss_backward") for change, text in (
+        (dict(dloss=None), "NULL"), (dict(dx=None), "NULL"), (dict(dweight=None), "NULL"), (dict(lddx=63), "stride"), (dict(lddw=63), "stride"),
+        (dict(dloss_stride=-1), "stride"))],
+    *[(fn, change, want, text) for fn in ("un_distill_loss", "un_distill_loss_backward") for change, want, text in (
+        (dict(top=0), 1, "top"), (dict(top=129), 7, "128"), (dict(logits_type=3), 1, "logits"), (dict(temperature=0.0), 1, "temperature"),
+        (dict(temperature=-1.0), 1, "temperature"), (dict(temperature=float("inf")), 1, "temperature"), (dict(ids=None), 1, "NULL"),
+        (dict(logits=None), 1, "NULL"), (dict(picked=None), 1, "NULL"))]])
+def test_head_refused_more(fn, change, want, text):
+    struct, base = CALLS[fn]
+    refused(fn, struct, base, change, want, text)
+
+
+def test_head_without_rows_or_arguments():
+    L = U.lib()
+    for fn, (struct, base) in CALLS.items():
+        assert getattr(L, fn)(None, None) == U.UN_ERR_INVALID and fn in L.un_last_error(None).decode()
+        if "backward" not in fn:
+            a = getattr(U, struct)(**{**base, "rows": 0, "x": None, "workspace": None})
+            assert getattr(L, fn)(ctypes.byref(a), None) == U.UN_OK
+
+
+@pytest.mark.parametrize("kind", [0, 1])
+@pytest.mark.parametrize("backward", [0, 1])
+@pytest.mark.parametrize("rows,width,vocab", [(0, 8, 8), (1, 1, 1), (777, 500, 10007), (8192, 2048, 131072), (1 << 18, 4096, 200000), (7, 65536, 1 << 20)])
+def test_head_workspace(kind, backward, rows, width, vocab):
+    """Grows with the problem and stays far below the logits of a large one; a call with other strides needs no more."""
+    b = ctypes.c_size_t()
+    assert U.lib().un_vocab_workspace(kind, rows, width, vocab, backward, ctypes.byref(b)) == U.UN_OK
+    assert b.value > 0 or rows == 0
+    if rows * vocab > 1 << 29:
+        assert b.value < rows * vocab * 4
+    assert U.lib().un_vocab_workspace(kind, rows, 0, vocab, backward, ctypes.byref(b)) == U.UN_ERR_INVALID
+    assert U.lib().un_vocab_workspace(kind, rows, width, vocab, backward, None) == U.UN_ERR_INVALID
