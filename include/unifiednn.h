@@ -646,9 +646,9 @@ un_status un_embedding_workspace(int64_t tokens, int32_t vocab, int32_t width, s
  *   lse_n = log(sum over v of exp(z_nv)),  loss_n = lse_n - z_n[target_n]  (>= 0).
  * A row whose target is `ignore` or outside [0, vocab) is left out: loss and lse are 0,
  * its x is not used, and it costs next to nothing. fp32 operands are multiplied as three
- * bf16 terms each (products to 2^-24 of the terms' size); a value that is not finite
- * makes the sums that it enters NaN. workspace: as many bytes as
- * un_vocab_workspace says. */
+ * bf16 terms each (products to 2^-24 of the terms' size); a value that is not finite,
+ * or so near the largest that it rounds to infinity in bf16, makes the sums that it
+ * enters NaN. workspace: as many bytes as un_vocab_workspace says. */
 typedef struct {
   int32_t type;              /* un_type of x, weight */
   int32_t width, vocab;      /* width in [1, 65536], vocab >= 1 */

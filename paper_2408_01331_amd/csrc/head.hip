@@ -35,7 +35,7 @@ struct HeadRows {
 // ---------------------------------------------------------------------------
 struct Teacher {
   int32_t id[2];      // -1: no entry
-  float u[2];         // logit / T
+  float u[2];         // logit (-inf: no entry)
   __device__ void load(const HeadCall& c, int64_t row) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
@@ -48,21 +48,26 @@ struct Teacher {
         const float v = c.logits16 ? bf2f(((const bf16_t*)c.logits)[at]) : ((const float*)c.logits)[at];
         if (i >= 0 && i < c.vocab && !(v == -INFINITY)) {
           id[h] = (int32_t)i;
-          u[h] = v / c.temperature;
+          u[h] = v;
         }
       }
     }
   }
   __device__ bool any() const { return __ballot(id[0] >= 0 || id[1] >= 0) != 0; }
-  // p and log p of the entries (0 and 0 elsewhere)
-  __device__ void softmax(float (&p)[2], float (&logp)[2]) const {
+  // p and log p of the entries (0 and 0 elsewhere). (Divided by T behind the subtraction: a row of the type's lowest
+  // values, divided before, would be one of -inf.)
+  __device__ void softmax(float temperature, float (&p)[2], float (&logp)[2]) const {
     const float m = wave_max(fmaxf(u[0], u[1]));
+    float t[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) p[h] = id[h] >= 0 ? expf(u[h] - m) : 0.f;
+    for (int h = 0; h < 2; ++h) {
+      t[h] = (u[h] - m) / temperature;
+      p[h] = id[h] >= 0 ? expf(t[h]) : 0.f;
+    }
     const float sum = wave64(p[0] + p[1], Add{}), log_sum = logf(sum);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      logp[h] = id[h] >= 0 ? u[h] - m - log_sum : 0.f;
+      logp[h] = id[h] >= 0 ? t[h] - log_sum : 0.f;
       p[h] /= sum;
     }
   }
@@ -238,7 +243,7 @@ template <typename T> __global__ __launch_bounds__(256) void head_distill_kernel
   Teacher t;
   t.load(c, row);
   float p[2], logp[2], z[2] = {0.f, 0.f};
-  t.softmax(p, logp);
+  t.softmax(c.temperature, p, logp);
   const T* x = (const T*)c.x + row * c.ldx;
   const T* w = (const T*)c.w;
   for (int k0 = 0; k0 < c.top; k0 += U) {
@@ -302,7 +307,7 @@ __global__ __launch_bounds__(256) void head_entries_kernel(HeadRows r, uint16_t*
   Teacher t;
   t.load(c, row);
   float p[2], logp[2], share[2] = {0.f, 0.f};
-  t.softmax(p, logp);
+  t.softmax(c.temperature, p, logp);
   for (int k = 0; k < c.top; ++k) {
     const int32_t id = __builtin_amdgcn_readlane(k < 64 ? t.id[0] : t.id[1], k & 63);
     const float q = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k < 64 ? p[0] : p[1]), k & 63));

@@ -82,7 +82,7 @@ struct HeadProb {
   const int32_t* live;              // rows that count
   int32_t vocab;                    // HEAD_STATS, HEAD_GRAD: rows of A (the piece's)
   float inv_t, scale;               // 1 / T, and that times log2(e)
-  const int32_t* target;            // [c], counted from the piece's first row; none: negative
+  const int32_t* target;            // [c]; null: none
   float2* stat;                     // HEAD_STATS: [vocab / 128][ldn], as join_stat has them
   float* picked;                    // HEAD_STATS: z at the target
   const float *lse, *coef;          // HEAD_GRAD: [c]
@@ -96,7 +96,6 @@ struct HeadProb {
   int32_t out_cols;
   int32_t add;                      // HEAD_DX, HEAD_DW: onto what is there
 };
-
 
 // A loss's call. Rows count by their target (CE), or by their teacher's entries.
 struct HeadCall {

@@ -321,6 +321,30 @@ def test_distill_entries(ops, dtype):
     R.close(one, ce, e + 1e-5, "loss of one entry")
 
 
+@pytest.mark.parametrize("logits_type", DTYPES, ids=["f32", "bf16"])
+def test_distill_lowest_logits(ops, logits_type):
+    """Entries masked with the type's lowest value, at a temperature below 1: none of their probability is left; a row of
+    nothing else is one of equal logits."""
+    low = torch.finfo(logits_type).min
+    x, w, _ = problem(12, 72, 200, F32)
+    ids, logits = ints(1, (12, 70), 200), rand(2, (12, 70), logits_type, std=2.0)
+    same = logits.clone()
+    logits[:4], same[:4] = low, 0.0
+    logits[4:8, ::3], same[4:8, ::3] = low, -float("inf")
+    logits[8, 1:], same[8, 1:] = low, -float("inf")
+    dloss = rand(3, (12,))
+    got, want = [], []
+    for u, out in ((logits, got), (same, want)):
+        loss, lse, picked = ops.distill_loss(x, w, ids, u, temperature=0.5)
+        out += [loss, lse, *ops.distill_loss_backward(x, w, ids, u, lse, picked, dloss, temperature=0.5)]
+    assert all(t.isfinite().all() for t in got)
+    # (an entry without probability is a term of 0 where it counts; its g is the softmax either way, from z by its own
+    # products or by the others': off by the logits' product, twice norm_tol's share of it as T is 1/2, and the exponential)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for g, v in zip(got[2:], want[2:]):
+        R.near(g, v.double(), R.U32 * (2 * 5 * (6 * 72) ** 0.5 + 24), "gradient")
+
+
 def test_distill_learned(ops):
     """A student that has the teacher's probabilities: the loss is near 0 and the gradient at the entries cancels to what is
     left over, exactly."""
