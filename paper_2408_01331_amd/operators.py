@@ -411,8 +411,9 @@ def _embed_workspace(tokens, vocab, width):
 def embedding_backward(dy, tokens, vocab, scale=1.0, padding=None, out=None):
     """The gradient at embedding's weight, [vocab, width] in dy's type, from the
     gradient dy at its output. Rows that no token names are zeros. out: a tensor of
-    that shape and type (its rows may be apart) onto which the gradient is added
-    instead, and which is returned. Tokens equal to `padding` have no gradient."""
+    that shape and type (its rows may be apart) that overlaps no input, onto which the
+    gradient is added instead, and which is returned. Tokens equal to `padding` have no
+    gradient."""
     t, dev = _check_type(dy, "dy")
     bits, ids = _indices(tokens, "tokens", dev)
     _require(dy.dim() == ids.dim() + 1 and dy.shape[:-1] == ids.shape, f"dy must have shape {(*ids.shape, 'width')}, not {tuple(dy.shape)}")
@@ -506,8 +507,8 @@ def vocab_loss(x, weight, targets, ignore=-100):
 def vocab_loss_backward(x, weight, targets, lse, dloss, ignore=-100, out=None):
     """(dx, dweight) of vocab_loss from the gradient dloss at the losses (float32, of
     their shape, or one number's tensor for all rows). lse: as vocab_loss returned it.
-    out: a tensor of weight's shape and type (its rows may be apart) onto which
-    dweight is added instead, and which is returned."""
+    out: a tensor of weight's shape and type (its rows may be apart) that overlaps no
+    input, onto which dweight is added instead, and which is returned."""
     t, dev, lead, (rows, xp, ldx, wp, ldw), (vocab, width), xv = _head(x, weight)
     bits, targets = _indices(targets, "targets", dev, lead)
     _flat(lse, "lse", lead, _F32, dev)

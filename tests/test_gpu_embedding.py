@@ -148,6 +148,24 @@ def test_far_rows(ops):
     assert not dw.any()
 
 
+def test_far_tokens(ops):
+    """Rows beyond 2^31 elements of the output and of its gradient."""
+    n, vocab, width = 600_000, 700, 4096
+    w, t = rand(1, (vocab, width), BF16), tokens_of(3, n, vocab, "even")
+    y = ops.embedding(t, w)
+    for a in range(0, n, 100_000):
+        assert torch.equal(y[a:a + 100_000], w[t[a:a + 100_000]])
+    y.zero_()
+    far = torch.tensor([0, 524_288, 524_289, n - 1], device="cuda")
+    t[far] = torch.tensor([5, 6, 7, 6], device="cuda")
+    y[far] = rand(2, (4, width), BF16)
+    dw = ops.embedding_backward(y, t, vocab)
+    assert torch.equal(dw[5], y[far[0]]) and torch.equal(dw[7], y[far[2]])
+    assert torch.equal(dw[6], (y[far[1]].float() + y[far[3]].float()).to(BF16))
+    dw[5:8] = 0
+    assert not dw.any()
+
+
 def test_against_autograd(ops):
     """Lookup and gradient against torch's autograd of the definition in 64 bits."""
     w, t, dy = rand(1, (50, 33)), tokens_of(1, 200, 50, "text").view(4, 50), rand(3, (4, 50, 33))

@@ -238,6 +238,28 @@ def test_pieces_of_the_vocabulary(ops, dtype):
     R.near(dw, total, h.norm_tol(rows), "dw")
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+def test_far_weights(ops, dtype):
+    """Rows of the weights and of their gradient beyond 2^31 elements, at the largest stride that is taken."""
+    vocab, width, ld = 1100, 72, 1 << 21
+    x, dense, targets = problem(40, width, vocab, dtype)
+    w = torch.empty((vocab - 1) * ld + width, dtype=dtype, device="cuda").as_strided((vocab, width), (ld, 1))
+    w.copy_(dense)
+    dloss = rand(3, (40,))
+    loss, lse = ops.vocab_loss(x, dense, targets)
+    dx, dw = ops.vocab_loss_backward(x, dense, targets, lse, dloss, out=dense.clone())
+    got = ops.vocab_loss(x, w, targets)
+    assert torch.equal(got[0], loss) and torch.equal(got[1], lse)
+    # (the gradient in place of a copy of the weights that is as far apart)
+    out = torch.empty((vocab - 1) * ld + width, dtype=dtype, device="cuda").as_strided((vocab, width), (ld, 1))
+    out.copy_(dense)
+    dx2, back = ops.vocab_loss_backward(x, w, targets, lse, dloss, out=out)
+    assert back is out and torch.equal(dx2, dx) and torch.equal(out, dw)
+    wider = torch.empty((vocab - 1) * (ld + 8) + width, dtype=dtype, device="cuda").as_strided((vocab, width), (ld + 8, 1))
+    with pytest.raises(ops.UnError, match="stride of the weight"):
+        ops.vocab_loss(x, wider, targets)
+
+
 def test_against_differences(ops):
     """The gradients against central differences of the definition in 64 bits, in random directions."""
     x, w, targets = problem(40, 24, 90, F32, left_out=0.2)
