@@ -194,6 +194,20 @@ __global__ __launch_bounds__(256) void head_layout_kernel(HeadRows r, uint16_t* 
   }
 }
 
+// fp32 weights as three bf16 terms, rows of `dp` columns (zeros behind the width).
+__global__ __launch_bounds__(256) void head_terms_kernel(const float* w, int64_t ldw, int64_t rows, int width, uint16_t* o, int64_t dp, int64_t plane) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per = dp / 8, row = i / per;
+  if (row >= rows) return;
+  const int c = (int)(i - row * per) * 8;
+  float f[8];
+  load_f32<8>(w + row * ldw + c, min(max(width - c, 0), 8), f);
+  uint32_t h[4][3];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) three_terms2(f[2 * e], f[2 * e + 1], h[e]);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) *(u32x4*)(o + k * plane + row * dp + c) = u32x4{h[0][k], h[1][k], h[2][k], h[3][k]};
+}
+
 // The statistics of 16 rows, joined by 64 groups of their threads and then in
 // order: the rows' lse, and the cross entropy's loss.
 __global__ __launch_bounds__(1024) void head_finish_kernel(HeadRows r, const float2* stat, int tiles, int64_t ldn, const float* picked) {
@@ -375,8 +389,10 @@ typedef HeadCfg<128, 128, 2, 2, 2, 64, 1> Medium;
 typedef HeadCfg<128, 64, 2, 2, 3, 64, 1> Small;
 typedef HeadCfg<128, 64, 2, 2, 2, 64, 1> SmallRegs;   // (through registers a stage less does)
 typedef HeadCfg<128, 64, 2, 2, 2, 32, 3> Terms;       // fp32
+typedef HeadCfg<128, 64, 2, 2, 4, 32, 3> TermsDeep;   // fp32 from terms that lie ready
+typedef HeadCfg<256, 128, 4, 2, 2, 32, 3> TermsLarge;
 
-constexpr int64_t HEAD_G_BYTES = (int64_t)512 << 20;   // of g's piece
+constexpr int64_t HEAD_G_BYTES = (int64_t)512 << 20;   // of g's piece, and of the weights' terms
 
 template <HeadKind KIND, class C, typename T, bool REG> void head_go(HeadProb& p, int64_t m, int64_t n, hipStream_t s) {
   p.tiles_m = (int)((m + C::bm - 1) / C::bm);
@@ -387,30 +403,34 @@ template <HeadKind KIND, class C, typename T, bool REG> void head_go(HeadProb& p
 // a product of m x n; direct: the weights' rows can be loaded directly (others pass through registers, of which large tiles have none left)
 template <HeadKind KIND> void head_launch(const HeadPlan& plan, bool direct, HeadProb& p, int64_t m, int64_t n, hipStream_t s) {
   constexpr bool W = KIND != HEAD_DW;  // A is the weights
-  if (plan.planes == 3) head_go<KIND, Terms, float, W>(p, m, n, s);
+  if (plan.tile[KIND] == 3) head_go<KIND, Terms, float, W>(p, m, n, s);
+  else if (plan.tile[KIND] == 4) head_go<KIND, TermsDeep, float, false>(p, m, n, s);
+  else if (plan.tile[KIND] == 5) head_go<KIND, TermsLarge, float, false>(p, m, n, s);
   else if (plan.tile[KIND] == 0) head_go<KIND, Large, bf16_t, false>(p, m, n, s);
   else if (plan.tile[KIND] == 1) W && !direct ? head_go<KIND, Medium, bf16_t, W>(p, m, n, s) : head_go<KIND, Medium, bf16_t, false>(p, m, n, s);
   else W && !direct ? head_go<KIND, SmallRegs, bf16_t, W>(p, m, n, s) : head_go<KIND, Small, bf16_t, false>(p, m, n, s);
 }
 
-// A product's time on tiles of a kind, in us: rounds of the workgroups that run at once,
-// each with its blocks and what it takes beside them (the first loads, the epilogue).
+// A product's time on tiles of a kind, in us: rounds of the workgroups that run at once, each with its blocks and what it
+// takes beside them (the first loads, the epilogue). A last round of at most one workgroup a CU takes less than one of two.
+// (Measured, all columns in cache: a block of 256 CUs of one, and of two.)
 struct HeadTime {
   int bm, bn, slots, kb;
-  double block, rest;
+  double lone, block, rest;
 };
-constexpr HeadTime HEAD_TIMES[4] = {{256, 256, 256, 64, 1.63, 6.0}, {128, 128, 512, 64, 0.97, 3.0}, {128, 64, 512, 64, 0.6, 2.5}, {128, 64, 512, 32, 0.8, 2.5}};
+constexpr HeadTime HEAD_TIMES[6] = {{256, 256, 256, 64, 1.4, 1.63, 6.0}, {128, 128, 512, 64, 0.62, 1.0, 3.0}, {128, 64, 512, 64, 0.38, 0.64, 2.5},
+                                    {128, 64, 512, 32, 0.95, 1.68, 2.5},  {128, 64, 256, 32, 0.62, 1.03, 3.0}, {256, 128, 256, 32, 2.3, 2.8, 6.0}};
 double head_time(const HeadTime& t, int64_t m, int64_t n, int64_t k, int64_t splits = 1) {
-  const int64_t tiles = (m + t.bm - 1) / t.bm * ((n + t.bn - 1) / t.bn) * splits, kb = ((k + splits - 1) / splits + t.kb - 1) / t.kb;
-  return (double)((tiles + t.slots - 1) / t.slots) * (kb * t.block + t.rest);
+  const int64_t tiles = (m + t.bm - 1) / t.bm * ((n + t.bn - 1) / t.bn) * splits, kb = ((k + splits - 1) / splits + t.kb - 1) / t.kb, rem = tiles % t.slots;
+  return (double)(tiles / t.slots) * (kb * t.block + t.rest) + (rem ? kb * (rem <= t.slots / 2 ? t.lone : t.block) + t.rest : 0.0);
 }
 // the kind of tiles, and of a long k the parts, that take the least; partial sums are written and read at some 4 TB/s, by a
 // launch more where one part needs none (`alone`)
-int head_tiles(bool bf16, bool direct, int64_t m, int64_t n, int64_t k, int* splits = nullptr, bool alone = false) {
+int head_tiles(int first, int end, int64_t m, int64_t n, int64_t k, int* splits = nullptr, bool alone = false, double* time = nullptr) {
   constexpr int PARTS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
   int best = 0;
   double least = 1e300;
-  for (int t = !bf16 ? 3 : direct ? 0 : 1; t < (bf16 ? 3 : 4); ++t)
+  for (int t = first; t < end; ++t)
     for (const int s : PARTS) {
       if (s > 1 && (!splits || s > k / 128 + 1)) break;
       const double us = head_time(HEAD_TIMES[t], m, n, k, s) + (splits && !(alone && s == 1) ? (double)s * m * n * 8 / 4e6 + (alone ? 4 : 0) : 0);
@@ -419,6 +439,7 @@ int head_tiles(bool bf16, bool direct, int64_t m, int64_t n, int64_t k, int* spl
       best = t;
       if (splits) *splits = s;
     }
+  if (time) *time += least;
   return best;
 }
 
@@ -433,23 +454,38 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool d
   p.ldn = up(rows, Large::bn);
   p.ldd = up(width, HEAD_BM);
   const int64_t mv = up(vocab, HEAD_BM);
-  p.piece = mv;
-  if (backward && rows > 0) p.piece = std::min(mv, std::max<int64_t>(4096, HEAD_G_BYTES / (p.npad * 2 * p.planes) / HEAD_BM * HEAD_BM));
-  p.splits = p.splits_w = 1;
-  p.tile[HEAD_STATS] = head_tiles(bf16, direct, vocab, rows, width);
-  p.tile[HEAD_GRAD] = head_tiles(bf16, direct, p.piece, rows, width);
-  p.tile[HEAD_DX] = head_tiles(bf16, direct, width, rows, p.piece, &p.splits);
-  p.tile[HEAD_DW] = head_tiles(bf16, true, width, p.piece, rows, &p.splits_w, true);
+  // the products with the weights on kinds [first, end) of tiles; their time
+  auto with = [&](HeadPlan& q, int first, int end) {
+    double us = 0;
+    q.piece = mv;
+    if (backward && rows > 0) q.piece = std::min(mv, std::max<int64_t>(4096, HEAD_G_BYTES / (q.npad * 2 * q.planes) / HEAD_BM * HEAD_BM));
+    if (q.terms) q.piece = std::min(q.piece, std::max<int64_t>(4096, HEAD_G_BYTES / (q.dp * 6) / HEAD_BM * HEAD_BM));
+    q.splits = 1;
+    q.tile[HEAD_STATS] = head_tiles(first, end, q.terms ? q.piece : vocab, rows, width, nullptr, false, backward ? nullptr : &us);
+    q.tile[HEAD_GRAD] = head_tiles(first, end, q.piece, rows, width, nullptr, false, backward ? &us : nullptr);
+    q.tile[HEAD_DX] = head_tiles(first, end, width, rows, q.piece, &q.splits, false, backward ? &us : nullptr);
+    return us * vocab / q.piece;
+  };
+  if (bf16) {
+    with(p, direct ? 0 : 1, 3);
+  } else {
+    HeadPlan q = p;
+    q.terms = true;
+    const double us = with(q, 4, 6) + (double)vocab * p.dp * 10 / 4.5e6 + 5;
+    if (with(p, 3, 4) > us) p = q;
+  }
+  p.splits_w = 1;
+  p.tile[HEAD_DW] = head_tiles(bf16 ? 0 : 3, bf16 ? 3 : 6, width, p.piece, rows, &p.splits_w, true);
   p.ldnw = p.piece;
   auto threads = [&](int kind, int64_t m, int64_t n, int splits) {
     const HeadTime& t = HEAD_TIMES[p.tile[kind]];
-    p.threads = std::max(p.threads, ((m + t.bm - 1) / t.bm * ((n + t.bn - 1) / t.bn) * splits + 8) * (p.tile[kind] == 0 ? 512 : 256));
+    p.threads = std::max(p.threads, ((m + t.bm - 1) / t.bm * ((n + t.bn - 1) / t.bn) * splits + 8) * (p.tile[kind] == 0 || p.tile[kind] == 5 ? 512 : 256));
   };
   threads(HEAD_STATS, vocab, rows, 1);
   threads(HEAD_GRAD, p.piece, rows, 1);
   threads(HEAD_DX, width, rows, p.splits);
   threads(HEAD_DW, width, p.piece, p.splits_w);
-  p.threads = std::max({p.threads, p.npad * (p.dp / 8) + 256, std::max(rows, p.splits_w > 1 ? p.piece : 0) * ((width + 3) / 4) + 256, rows * 64 + 1024});
+  p.threads = std::max({p.threads, p.npad * (p.dp / 8) + 256, std::max(rows, p.splits_w > 1 ? p.piece : 0) * ((width + 3) / 4) + 256, rows * 64 + 1024, p.terms ? p.piece * (p.dp / 8) + 256 : 0});
   size_t at = 0;
   auto take = [&](int64_t bytes) {
     const size_t a = at;
@@ -462,6 +498,7 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool d
   p.at_target = take(rows * 4);
   p.at_flag = take(rows);
   p.at_x = take(p.npad * p.dp * 2 * p.planes);
+  p.at_w = take(p.terms ? p.piece * p.dp * 6 : 0);
   if (backward) {
     p.at_lse = take(rows * 4);
     p.at_coef = take(rows * 4);
@@ -504,7 +541,14 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
   }
   const bool direct = head_direct(c.bf16, c.w, c.width, c.ldw);
   const HeadOperand x{xs, plan.dp, plan.npad * plan.dp, plan.npad, (int32_t)plan.dp};
-  auto weights = [&](int64_t v0, int64_t n) { return HeadOperand{(const char*)c.w + v0 * c.ldw * (c.bf16 ? 2 : 4), c.ldw, 0, n, c.width}; };
+  // rows v0 .. v0 + n of the weights
+  auto weights = [&](int64_t v0, int64_t n) {
+    if (!plan.terms) return HeadOperand{(const char*)c.w + v0 * c.ldw * (c.bf16 ? 2 : 4), c.ldw, 0, n, c.width};
+    uint16_t* o = (uint16_t*)(ws + plan.at_w);
+    const int64_t plane = plan.piece * plan.dp;
+    hipLaunchKernelGGL(head_terms_kernel, grid((n * (plan.dp / 8) + 255) / 256), dim3(256), 0, s, (const float*)c.w + v0 * c.ldw, c.ldw, n, c.width, o, plan.dp, plane);
+    return HeadOperand{o, plan.dp, plane, n, (int32_t)plan.dp};
+  };
   HeadProb base{};
   base.live = r.live;
   base.inv_t = 1.f / c.temperature;
@@ -513,15 +557,20 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
   base.target = distill ? nullptr : r.target;
   if (!backward) {
     HeadProb p = base;
-    p.a = weights(0, c.vocab);
     p.b = x;
     p.k = c.width;
-    p.vocab = c.vocab;
-    p.stat = (float2*)(ws + plan.at_stat);
     p.ldn = plan.npad;
     p.picked = (float*)(ws + plan.at_picked);
-    head_launch<HEAD_STATS>(plan, direct, p, c.vocab, c.rows, s);
-    hipLaunchKernelGGL(head_finish_kernel, grid((c.rows + 15) / 16), dim3(1024), 0, s, r, p.stat, (c.vocab + 127) / 128, p.ldn, p.picked);
+    float2* stat = (float2*)(ws + plan.at_stat);
+    for (int64_t v0 = 0; v0 < c.vocab; v0 += plan.piece) {
+      const int64_t n = std::min<int64_t>(plan.piece, c.vocab - v0);
+      p.a = weights(v0, n);
+      p.vocab = (int32_t)n;
+      p.first = (int32_t)v0;
+      p.stat = stat + v0 / 128 * p.ldn;
+      head_launch<HEAD_STATS>(plan, direct, p, n, c.rows, s);
+    }
+    hipLaunchKernelGGL(head_finish_kernel, grid((c.rows + 15) / 16), dim3(1024), 0, s, r, stat, (c.vocab + 127) / 128, p.ldn, p.picked);
     if (distill) {
       if (c.bf16) hipLaunchKernelGGL((head_distill_kernel<bf16_t>), grid((c.rows + 3) / 4), dim3(256), 0, s, r);
       else hipLaunchKernelGGL((head_distill_kernel<float>), grid((c.rows + 3) / 4), dim3(256), 0, s, r);
@@ -540,8 +589,9 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
     const int64_t n = std::min<int64_t>(plan.piece, c.vocab - v0), padded = (n + HEAD_BM - 1) / HEAD_BM * HEAD_BM;
     const HeadOperand gop{g, plan.piece, gplane, plan.npad, (int32_t)padded};
     if (c.rows > 0) {
+      const HeadOperand w = weights(v0, n);
       HeadProb p = base;
-      p.a = weights(v0, n);
+      p.a = w;
       p.b = x;
       p.k = c.width;
       p.vocab = (int32_t)n;
@@ -555,7 +605,7 @@ hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, v
       if (distill)
         hipLaunchKernelGGL(head_entries_kernel, grid((c.rows + 3) / 4), dim3(256), 0, s, r, g, plan.piece, gplane, plan.planes, (int)v0, (int)n);
       HeadProb q = base;
-      q.a = weights(v0, n);
+      q.a = w;
       q.b = gop;
       q.k = (int)n;
       q.splits = plan.splits;

@@ -440,7 +440,7 @@ __device__ __forceinline__ float2 join_stat(float2 a, float2 b) {
 // bytes of T (16 more than its values, which moves the rows' banks apart).
 template <class C, typename T> constexpr int head_pitch() { return C::bm * (int)sizeof(T) + 16; }
 template <HeadKind KIND, class C, typename T> constexpr int head_lds() {
-  constexpr int out = KIND == HEAD_GRAD ? C::bn * head_pitch<C, bf16_t>() * C::planes : KIND == HEAD_DW ? C::bn * head_pitch<C, T>() : 0;
+  constexpr int out = KIND == HEAD_GRAD ? C::bn * head_pitch<C, bf16_t>() : KIND == HEAD_DW ? C::bn * head_pitch<C, T>() : 0;
   return out > C::stage * C::st ? out : C::stage * C::st;
 }
 
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(C::waves * 64, 2) void head_kernel(HeadProb p) {
     // row's sums do not depend on the kind that a call takes.
     float2* red = (float2*)sm;  // [wgm][bn]
     constexpr int UNITS = C::fm / 2;
-    static_assert(UNITS == 2 || C::wgm == 2, "128 rows are a wave's, or two waves'");
+    static_assert(UNITS == 2 || (UNITS == 1 && C::wgm % 2 == 0), "128 rows are a wave's, or two waves'");
     if (m0 + C::bm > p.vocab) {
 #pragma unroll
       for (int y = 0; y < C::fn; ++y)
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(C::waves * 64, 2) void head_kernel(HeadProb p) {
 #pragma unroll
     for (int y = 0; y < C::fn; ++y) {
       const int64_t n = n0 + wn + 32 * y + (lane & 31);
-      const int target = p.target && n < live ? p.target[n] - (int)m0 - wm : -1;
+      const int target = p.target && n < live ? p.target[n] - p.first - (int)m0 - wm : -1;
       if (__any(target >= 0 && target < C::bm / C::wgm)) {
 #pragma unroll
         for (int x = 0; x < C::fm; ++x)
@@ -525,7 +525,10 @@ __global__ __launch_bounds__(C::waves * 64, 2) void head_kernel(HeadProb p) {
     }
     if constexpr (UNITS == 1) {
       __syncthreads();
-      for (int c = threadIdx.x; c < C::bn; c += NT) p.stat[(m0 / 128) * p.ldn + n0 + c] = join_stat(red[c], red[C::bn + c]);
+      for (int c = threadIdx.x; c < C::bn * C::wgm / 2; c += NT) {
+        const int u = c / C::bn, n = c % C::bn;
+        p.stat[(m0 / 128 + u) * p.ldn + n0 + n] = join_stat(red[2 * u * C::bn + n], red[(2 * u + 1) * C::bn + n]);
+      }
     }
   } else if constexpr (KIND == HEAD_GRAD) {
     constexpr int PITCH = head_pitch<C, bf16_t>(), PLANE = C::bn * PITCH;
@@ -560,26 +563,32 @@ __global__ __launch_bounds__(C::waves * 64, 2) void head_kernel(HeadProb p) {
           for (int e = 0; e < 16; ++e)
             if (m0 + wm + 32 * x + 8 * (e / 4) + 4 * (lane >> 5) + e % 4 >= p.vocab) acc[x][y][e] = 0.f;
     }
-    head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {
-      char* o = sm + n * PITCH + m * 2;
-      if constexpr (C::planes == 1) {
-        *(u32x2*)o = u32x2{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
-      } else {
-        uint32_t h[2][3];
-        three_terms2(v[0], v[1], h[0]);
-        three_terms2(v[2], v[3], h[1]);
+    // (of three terms as many at a time as LDS holds)
+    constexpr int AT_ONCE = C::planes * PLANE <= C::stage * C::st ? C::planes : 1;
+    each<C::planes / AT_ONCE>([&](auto turn) {
+      constexpr int Q0 = decltype(turn)::value * AT_ONCE;
+      if (Q0) __syncthreads();
+      head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {
+        char* o = sm + n * PITCH + m * 2;
+        if constexpr (C::planes == 1) {
+          *(u32x2*)o = u32x2{f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+        } else {
+          uint32_t h[2][3];
+          three_terms2(v[0], v[1], h[0]);
+          three_terms2(v[2], v[3], h[1]);
 #pragma unroll
-        for (int q = 0; q < 3; ++q) *(u32x2*)(o + q * PLANE) = u32x2{h[0][q], h[1][q]};
-      }
-    });
-    __syncthreads();
+          for (int q = 0; q < AT_ONCE; ++q) *(u32x2*)(o + q * PLANE) = u32x2{h[0][Q0 + q], h[1][Q0 + q]};
+        }
+      });
+      __syncthreads();
 #pragma unroll
-    for (int q = 0; q < C::planes; ++q)
+      for (int q = 0; q < AT_ONCE; ++q)
 #pragma unroll 4
-      for (int c = threadIdx.x; c < C::bn * C::bm / 8; c += NT) {
-        const int n = c / (C::bm / 8), m = c % (C::bm / 8) * 8;
-        *(u32x4*)(p.g + q * p.gplane + (n0 + n) * p.ldg + m0 + m) = *(const u32x4*)(sm + q * PLANE + n * PITCH + m * 2);
-      }
+        for (int c = threadIdx.x; c < C::bn * C::bm / 8; c += NT) {
+          const int n = c / (C::bm / 8), m = c % (C::bm / 8) * 8;
+          *(u32x4*)(p.g + (Q0 + q) * p.gplane + (n0 + n) * p.ldg + m0 + m) = *(const u32x4*)(sm + q * PLANE + n * PITCH + m * 2);
+        }
+    });
   } else if (KIND == HEAD_DX || p.splits > 1) {
     const int64_t rows = KIND == HEAD_DX ? live : p.vocab;
     head_each<C>(acc, [&](int m, int n, const float (&v)[4]) {

@@ -80,13 +80,13 @@ struct HeadProb {
   int32_t tiles_m, tiles_n;
   int32_t splits;                   // HEAD_DX, HEAD_DW: parts of k
   const int32_t* live;              // rows that count
-  int32_t vocab;                    // HEAD_STATS, HEAD_GRAD: rows of A (the piece's)
+  int32_t vocab;                    // HEAD_STATS, HEAD_GRAD: rows of A (the piece's); HEAD_DW: of the result
   float inv_t, scale;               // 1 / T, and that times log2(e)
   const int32_t* target;            // [c]; null: none
   float2* stat;                     // HEAD_STATS: [vocab / 128][ldn], as join_stat has them
   float* picked;                    // HEAD_STATS: z at the target
   const float *lse, *coef;          // HEAD_GRAD: [c]
-  int32_t first;                    // HEAD_GRAD: the piece's first row of the table
+  int32_t first;                    // HEAD_STATS, HEAD_GRAD: the piece's first row of the table
   uint16_t* g;                      // HEAD_GRAD
   int64_t ldg, gplane;
   float* part;                      // HEAD_DX, HEAD_DW of several parts: [splits][ldn][ldd]
@@ -132,13 +132,14 @@ inline bool head_direct(bool bf16, const void* w, int32_t width, int64_t ldw) {
 struct HeadPlan {
   int planes;
   int64_t dp, npad;                 // columns and rows of the laid-out hidden states
-  int tile[4];                      // by HeadKind: 0 large, 1 medium, 2 small (bf16)
+  int tile[4];                      // by HeadKind, a kind of tiles: 0 large, 1 medium, 2 small (bf16), 3 .. 5 (fp32)
+  bool terms;                       // fp32: the weights' terms are laid out, a piece at a time
   int64_t piece;                    // vocabulary of a piece
   int splits, splits_w;             // parts of k of HEAD_DX and HEAD_DW
   int64_t ldn, ldnw, ldd;           // rows of their partial sums, and columns
   int64_t threads;                  // of the largest launch
   // offsets in the workspace
-  size_t at_map, at_inv, at_target, at_lse, at_coef, at_flag, at_live, at_x, at_stat, at_picked, at_g, at_part, at_partw, bytes;
+  size_t at_map, at_inv, at_target, at_lse, at_coef, at_flag, at_live, at_x, at_w, at_stat, at_picked, at_g, at_part, at_partw, bytes;
 };
 HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool direct, bool backward);
 hipError_t launch_head(const HeadPlan& plan, const HeadCall& c, bool backward, void* workspace, hipStream_t s);

@@ -238,6 +238,36 @@ def test_pieces_of_the_vocabulary(ops, dtype):
     R.near(dw, total, h.norm_tol(rows), "dw")
 
 
+def test_terms_laid_out(ops):
+    """fp32 weights whose terms are laid out first, in several pieces, from rows that are apart: the losses' bits are those of
+    calls on few rows, which split the weights on their way; targets in both pieces and at their borders."""
+    rows, width, vocab, piece = 2100, 4100, 24000, (512 << 20) // (4160 * 6) // 256 * 256
+    x, w, targets = problem(rows, width, vocab, F32, left_out=0.1)
+    w = torch.cat([w, torch.full((vocab, 3), float("nan"), device="cuda")], 1)[:, :width]
+    targets[:4] = torch.tensor([piece - 1, piece, vocab - 1, 0], device="cuda")
+    dloss = rand(4, (rows,), std=1.0 / rows)
+    # (the terms' piece is in the workspace of the one, and not of the other)
+    assert ops._head_workspace(0, rows, width, vocab, 0) > piece * 4160 * 6 > ops._head_workspace(0, 64, width, vocab, 0)
+    assert piece < vocab < 2 * piece
+    loss, lse = ops.vocab_loss(x, w, targets)
+    dx, dw = ops.vocab_loss_backward(x, w, targets, lse, dloss)
+    for s in (slice(0, 64), slice(rows - 64, rows)):
+        l2, s2 = ops.vocab_loss(x[s], w, targets[s])
+        assert torch.equal(l2, loss[s]) and torch.equal(s2, lse[s])
+    X, W = x.double(), w.double()
+    z = X @ W.t()
+    live = targets >= 0
+    want = torch.where(live, torch.logsumexp(z, 1) - z.gather(1, targets.clamp(min=0)[:, None])[:, 0], 0.0)
+    h = R.Head.__new__(R.Head)
+    h.t, h.x = F32, X
+    R.near(loss, want, h.norm_tol(1), "loss")
+    g = torch.softmax(z, 1)
+    g[torch.arange(rows, device="cuda"), targets.clamp(min=0)] -= 1
+    g *= torch.where(live, dloss.double(), 0.0)[:, None]
+    R.near(dx, g @ W, h.norm_tol(vocab), "dx")
+    R.near(dw, g.t() @ X, h.norm_tol(rows), "dw")
+
+
 @pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
 def test_far_weights(ops, dtype):
     """Rows of the weights and of their gradient beyond 2^31 elements, at the largest stride that is taken."""
