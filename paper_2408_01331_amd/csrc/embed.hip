@@ -1,6 +1,11 @@
 // gfx950 (CDNA4) kernels of the embedding lookup and of its gradient. Both are bound
 // by HBM: rows are read and written once, 16 bytes a lane. A wave's unit is 64
 // vectors of one row (512 values in bf16).
+//
+// 32768 tokens of a table of 131072 x 2048 in bf16: the lookup 50 us (87 MB
+// read, as rows repeat, and 134 MB written: 4.4 TB/s), the sort 2 x 14 us, sums and zeros 123 us
+// (135 MB read, 544 MB written: 5.5 TB/s), the join 12 us. Small calls are a chain of short launches: 5003 tokens of 10007 x 333 in fp32 take
+// 5, 20, 12 and 6 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -27,7 +32,9 @@ template <typename T> __device__ __forceinline__ u32x4 load_raw(const T* p, int 
 }
 
 // ---------------------------------------------------------------------------
-// Forward: a wave takes R rows' share of a column tile, all their loads in flight.
+// Forward: a wave takes R rows' share of a column tile, all their loads in flight. R = 4
+// where 16384 units leave waves enough: 32768 tokens x 2048 in bf16 49.8 us (R = 1 54.1),
+// 8192 x 1024 6.3 (6.8); 64 x 1024 take 4.4 (3.0).
 // ---------------------------------------------------------------------------
 template <typename T, int R> __global__ __launch_bounds__(256) void embed_kernel(EmbedProb p, int tiles) {
   constexpr int N = V16<T>::N;
@@ -58,7 +65,9 @@ template <typename T, int R> __global__ __launch_bounds__(256) void embed_kernel
 // belongs to a workgroup and a contiguous part of it to each wave; a place's rank
 // among the wave's 64 is the number of lower lanes with the same digit (a ballot per
 // bit), and the counts of the lower waves, blocks and digits come before it. Tokens
-// without a gradient get the key `vocab`, behind all others.
+// without a gradient get the key `vocab`, behind all others. A
+// chain of latencies (keys, LDS counts, ranks), so 16 waves, each with SORT_BATCH keys in
+// flight.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t key_of(const EmbedProb& p, int64_t i) {
   const int64_t t = token_at(p, i);
@@ -233,7 +242,10 @@ template <int BITS> __global__ __launch_bounds__(1024) void sort_move_kernel(Emb
 
 // ---------------------------------------------------------------------------
 // Sums of the runs. What a run's end does with the sum, by whether the run came in
-// from the chunk before and whether it goes on behind this one.
+// from the chunk before and whether it goes on behind this one. Chunks are short where
+// there are few of them, so that more waves share the reading (16 and 32 places: 5003 x 333
+// in fp32 11.6 us and 6.6 for the join against 19.1 and 4.4; 32768 x 2048 in bf16 123 and 18
+// against 123 and 12), and at most 4096, whose sums the join reads.
 // ---------------------------------------------------------------------------
 template <typename T, int N> __device__ __forceinline__ void put_row(const EmbedProb& p, uint32_t key, int c, int live, float* f) {
   T* o = (T*)p.y + (int64_t)key * p.ldy + c;

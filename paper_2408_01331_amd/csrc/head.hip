@@ -142,8 +142,8 @@ constexpr int HEAD_FEW = 256 * 8;   // rows that every workgroup of the next ker
 
 // The rows that count, in chunks of 8 values, as bf16 or three bf16 terms of fp32, padded
 // with zeros to `dp` columns and to the next HEAD_PAD rows; and what the products read of
-// each, by its number. FEW: the rows are numbered here, too (a launch less: 32 rows 24.4 us,
-// so 21).
+// each, by its number. FEW: the rows are numbered here, too, by every workgroup for itself
+// and a launch less (32 rows 4.6 us, against 3.2 and 3.6; 2048 rows 8.4, against 3.8 and 4.8).
 template <typename T, bool FEW>
 __global__ __launch_bounds__(256) void head_layout_kernel(HeadRows r, uint16_t* o, int64_t rows, int64_t dp, int backward) {
   __shared__ int32_t sums[32], map[FEW ? HEAD_FEW : 1];
@@ -384,6 +384,7 @@ __global__ __launch_bounds__(256) void head_join_kernel(const int32_t* inv, int6
   }
 }
 
+// Kinds of tiles, by number: 0 .. 2 bf16, 3 .. 5 fp32. (Large tiles through registers would spill: 203 VGPRs are taken.)
 typedef HeadCfg<256, 256, 2, 4, 2, 64, 1> Large;
 typedef HeadCfg<128, 128, 2, 2, 2, 64, 1> Medium;
 typedef HeadCfg<128, 64, 2, 2, 3, 64, 1> Small;
@@ -392,7 +393,9 @@ typedef HeadCfg<128, 64, 2, 2, 2, 32, 3> Terms;       // fp32
 typedef HeadCfg<128, 64, 2, 2, 4, 32, 3> TermsDeep;   // fp32 from terms that lie ready
 typedef HeadCfg<256, 128, 4, 2, 2, 32, 3> TermsLarge;
 
-constexpr int64_t HEAD_G_BYTES = (int64_t)512 << 20;   // of g's piece, and of the weights' terms
+// Of g's piece, and of the weights' terms: with 128 MiB 8192 x 2048 x 131072 trains in 14.8 ms, with 512 in 14.66, with 2 GiB
+// in 14.56.
+constexpr int64_t HEAD_G_BYTES = (int64_t)512 << 20;
 
 template <HeadKind KIND, class C, typename T, bool REG> void head_go(HeadProb& p, int64_t m, int64_t n, hipStream_t s) {
   p.tiles_m = (int)((m + C::bm - 1) / C::bm);
@@ -400,7 +403,7 @@ template <HeadKind KIND, class C, typename T, bool REG> void head_go(HeadProb& p
   const int64_t all = (int64_t)p.tiles_m * p.tiles_n * p.splits;
   hipLaunchKernelGGL((head_kernel<KIND, C, T, REG>), dim3((unsigned)((all + 7) / 8 * 8)), dim3(C::waves * 64), 0, s, p);
 }
-// a product of m x n; direct: the weights' rows can be loaded directly (others pass through registers, of which large tiles have none left)
+// a product of m x n; direct: the weights' rows can be loaded directly (others pass through registers)
 template <HeadKind KIND> void head_launch(const HeadPlan& plan, bool direct, HeadProb& p, int64_t m, int64_t n, hipStream_t s) {
   constexpr bool W = KIND != HEAD_DW;  // A is the weights
   if (plan.tile[KIND] == 3) head_go<KIND, Terms, float, W>(p, m, n, s);
@@ -424,7 +427,7 @@ double head_time(const HeadTime& t, int64_t m, int64_t n, int64_t k, int64_t spl
   const int64_t tiles = (m + t.bm - 1) / t.bm * ((n + t.bn - 1) / t.bn) * splits, kb = ((k + splits - 1) / splits + t.kb - 1) / t.kb, rem = tiles % t.slots;
   return (double)(tiles / t.slots) * (kb * t.block + t.rest) + (rem ? kb * (rem <= t.slots / 2 ? t.lone : t.block) + t.rest : 0.0);
 }
-// the kind of tiles, and of a long k the parts, that take the least; partial sums are written and read at some 4 TB/s, by a
+// the kind of tiles in [first, end), and of a long k the parts, that take the least; partial sums are written and read at some 4 TB/s, by a
 // launch more where one part needs none (`alone`)
 int head_tiles(int first, int end, int64_t m, int64_t n, int64_t k, int* splits = nullptr, bool alone = false, double* time = nullptr) {
   constexpr int PARTS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
@@ -454,7 +457,9 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool d
   p.ldn = up(rows, Large::bn);
   p.ldd = up(width, HEAD_BM);
   const int64_t mv = up(vocab, HEAD_BM);
-  // the products with the weights on kinds [first, end) of tiles; their time
+  // the products with the weights on kinds [first, end) of tiles; their time. (fp32 weights are split by every tile that
+  // reads them, or once: 4 bytes read and 6 written a value. 2048 x 1024 x 32768: 3.46 ms with all splitting, 2.83 so;
+  // 64 x 1024 x 131072: 170 us with all splitting, of which the layout alone would take 300.)
   auto with = [&](HeadPlan& q, int first, int end) {
     double us = 0;
     q.piece = mv;
