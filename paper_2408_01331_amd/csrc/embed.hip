@@ -5,7 +5,7 @@
 // 32768 tokens of a table of 131072 x 2048 in bf16: the lookup 50 us (87 MB
 // read, as rows repeat, and 134 MB written: 4.4 TB/s), the sort 2 x 14 us, sums and zeros 123 us
 // (135 MB read, 544 MB written: 5.5 TB/s), the join 12 us. Small calls are a chain of short launches: 5003 tokens of 10007 x 333 in fp32 take
-// 5, 20, 12 and 6 us.
+// 5, 17, 12 and 6 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -73,9 +73,36 @@ __device__ __forceinline__ uint32_t key_of(const EmbedProb& p, int64_t i) {
   const int64_t t = token_at(p, i);
   return t >= 0 && t < p.vocab && t != p.padding ? (uint32_t)t : (uint32_t)p.vocab;
 }
-__device__ __forceinline__ uint32_t key_in(const EmbedProb& p, int pass, int64_t i) {
-  return pass == 0 ? key_of(p, i) : p.keys[(pass + 1) & 1][i];
-}
+// A pass's input and output. In memory, by turns:
+struct SortMemory {
+  const EmbedProb& p;
+  int pass;
+  __device__ uint32_t key(int64_t i) const { return pass == 0 ? key_of(p, i) : p.keys[(pass + 1) & 1][i]; }
+  __device__ uint32_t place(int64_t i) const { return pass == 0 ? (uint32_t)i : p.place[(pass + 1) & 1][i]; }
+  __device__ void put(uint32_t at, uint32_t key, uint32_t place) const {
+    p.keys[pass & 1][at] = key;
+    p.place[pass & 1][at] = place;
+  }
+};
+// and in LDS, where only the last pass's output leaves it.
+struct SortLds {
+  const EmbedProb& p;
+  int pass;
+  bool last;
+  uint32_t (*keys)[SORT_ONE];
+  uint16_t (*places)[SORT_ONE];
+  __device__ uint32_t key(int64_t i) const { return keys[pass & 1][i]; }
+  __device__ uint32_t place(int64_t i) const { return pass == 0 ? (uint32_t)i : places[pass & 1][i]; }
+  __device__ void put(uint32_t at, uint32_t key, uint32_t place) const {
+    if (last) {
+      p.keys[pass & 1][at] = key;
+      p.place[pass & 1][at] = place;
+    } else {
+      keys[(pass + 1) & 1][at] = key;
+      places[(pass + 1) & 1][at] = (uint16_t)place;
+    }
+  }
+};
 
 constexpr int SORT_BATCH = 8;   // places that a lane has in flight
 
@@ -87,8 +114,8 @@ template <int W> __device__ __forceinline__ void sort_part(int64_t i0, int64_t i
 }
 
 // Counts of the block's digits, a row of LDS per wave: cnt[w][digit].
-template <int W> __device__ __forceinline__ void sort_count(const EmbedProb& p, int pass, int bits, int64_t i0, int64_t i1, uint32_t* cnt) {
-  const int D = 1 << bits, w = threadIdx.x >> 6, lane = threadIdx.x & 63, shift = pass * bits;
+template <int W, typename S> __device__ __forceinline__ void sort_count(const S& in, int bits, int64_t i0, int64_t i1, uint32_t* cnt) {
+  const int D = 1 << bits, w = threadIdx.x >> 6, lane = threadIdx.x & 63, shift = in.pass * bits;
   int64_t a, b;
   sort_part<W>(i0, i1, a, b);
   for (int k = threadIdx.x; k < W * D; k += W * 64) cnt[k] = 0;
@@ -96,7 +123,7 @@ template <int W> __device__ __forceinline__ void sort_count(const EmbedProb& p, 
   for (int64_t i = a + lane; i < b; i += 64 * SORT_BATCH) {
     uint32_t key[SORT_BATCH];
 #pragma unroll
-    for (int u = 0; u < SORT_BATCH; ++u) key[u] = i + u * 64 < b ? key_in(p, pass, i + u * 64) : 0;
+    for (int u = 0; u < SORT_BATCH; ++u) key[u] = i + u * 64 < b ? in.key(i + u * 64) : 0;
 #pragma unroll
     for (int u = 0; u < SORT_BATCH; ++u)
       if (i + u * 64 < b) atomicAdd(&cnt[w * D + ((key[u] >> shift) & (D - 1))], 1u);
@@ -106,9 +133,8 @@ template <int W> __device__ __forceinline__ void sort_count(const EmbedProb& p, 
 
 // The block's places to where they belong: base[digit] is the first of the block's
 // digit, cnt the waves' counts (both overwritten).
-template <int W>
-__device__ __forceinline__ void sort_move(const EmbedProb& p, int pass, int bits, int64_t i0, int64_t i1, uint32_t* cnt, uint32_t* base) {
-  const int D = 1 << bits, w = threadIdx.x >> 6, lane = threadIdx.x & 63, shift = pass * bits;
+template <int W, typename S> __device__ __forceinline__ void sort_move(const S& in, int bits, int64_t i0, int64_t i1, uint32_t* cnt, uint32_t* base) {
+  const int D = 1 << bits, w = threadIdx.x >> 6, lane = threadIdx.x & 63, shift = in.pass * bits;
   int64_t a, b;
   sort_part<W>(i0, i1, a, b);
   for (int k = threadIdx.x; k < D; k += W * 64) {
@@ -127,24 +153,29 @@ __device__ __forceinline__ void sort_move(const EmbedProb& p, int pass, int bits
 #pragma unroll
     for (int u = 0; u < SORT_BATCH; ++u) {
       const int64_t at = i + u * 64 + lane;
-      key[u] = at < b ? key_in(p, pass, at) : 0;
-      place[u] = at >= b ? 0 : pass == 0 ? (uint32_t)at : p.place[(pass + 1) & 1][at];
+      key[u] = at < b ? in.key(at) : 0;
+      place[u] = at < b ? in.place(at) : 0;
     }
 #pragma unroll
     for (int u = 0; u < SORT_BATCH; ++u) {
       if (i + u * 64 >= b) break;
       const bool on = i + u * 64 + lane < b;
       const uint32_t digit = (key[u] >> shift) & (D - 1);
-      uint64_t same = __ballot(on);
-      for (int k = 0; k < bits; ++k) {
+      const uint64_t there = __ballot(on);
+      uint32_t lo = (uint32_t)there, hi = (uint32_t)(there >> 32);
+#pragma unroll
+      for (int k = 0; k < SORT_BITS; ++k) {
+        if (k >= bits) break;
         const uint64_t one = __ballot((digit >> k) & 1);
-        same &= (digit >> k) & 1 ? one : ~one;
+        const uint32_t set = (uint32_t)((int32_t)(digit << (31 - k)) >> 31);  // all bits of it the lane's own
+        lo &= ~((uint32_t)one ^ set);
+        hi &= ~((uint32_t)(one >> 32) ^ set);
       }
+      const uint64_t same = (uint64_t)hi << 32 | lo;
       const int rank = __popcll(same & (((uint64_t)1 << lane) - 1));
       if (on) {
         const uint32_t first = mine[digit];
-        p.keys[pass & 1][first + rank] = key[u];
-        p.place[pass & 1][first + rank] = place[u];
+        in.put(first + rank, key[u], place[u]);
         // (a wave's LDS accesses happen in order: the read above is before this write)
         if ((same >> lane) == 1) mine[digit] = first + rank + 1;
       }
@@ -178,13 +209,17 @@ template <int NT> __device__ __forceinline__ void sort_prefix(uint32_t* base, in
   __syncthreads();
 }
 
-// All passes by one workgroup.
+// All passes by one workgroup, from LDS to LDS.
 __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedProb p, int passes, int bits) {
   constexpr int W = 16;
-  __shared__ uint32_t cnt[W << 9], base[1 << 9], sm[W];
+  __shared__ uint32_t cnt[W << 9], base[1 << 9], sm[W], keys[2][SORT_ONE];
+  __shared__ uint16_t places[2][SORT_ONE];
+  const int D = 1 << bits;
+  for (int i = threadIdx.x; i < p.n; i += W * 64) keys[0][i] = key_of(p, i);
+  __syncthreads();
   for (int pass = 0; pass < passes; ++pass) {
-    const int D = 1 << bits;
-    sort_count<W>(p, pass, bits, 0, p.n, cnt);
+    const SortLds in{p, pass, pass == passes - 1, keys, places};
+    sort_count<W>(in, bits, 0, p.n, cnt);
     for (int k = threadIdx.x; k < D; k += W * 64) {
       uint32_t c = 0;
 #pragma unroll
@@ -193,8 +228,7 @@ __global__ __launch_bounds__(1024) void sort_one_kernel(EmbedProb p, int passes,
     }
     __syncthreads();
     sort_prefix<W * 64>(base, D, sm);
-    sort_move<W>(p, pass, bits, 0, p.n, cnt, base);
-    __threadfence_block();
+    sort_move<W>(in, bits, 0, p.n, cnt, base);
     __syncthreads();
   }
 }
@@ -205,7 +239,7 @@ template <int BITS> __global__ __launch_bounds__(1024) void sort_count_kernel(Em
   __shared__ uint32_t cnt[W << BITS];
   const int64_t i0 = blockIdx.x * per, i1 = min(p.n, i0 + per);
   const int D = 1 << bits;
-  sort_count<W>(p, pass, bits, i0, i1, cnt);
+  sort_count<W>(SortMemory{p, pass}, bits, i0, i1, cnt);
   for (int k = threadIdx.x; k < D; k += W * 64) {
     uint32_t c = 0;
 #pragma unroll
@@ -236,8 +270,8 @@ template <int BITS> __global__ __launch_bounds__(1024) void sort_move_kernel(Emb
   __syncthreads();
   sort_prefix<W * 64>(base, D, sm);
   for (int k = threadIdx.x; k < D; k += W * 64) base[k] += before[k];
-  sort_count<W>(p, pass, bits, i0, i1, cnt);
-  sort_move<W>(p, pass, bits, i0, i1, cnt, base);
+  sort_count<W>(SortMemory{p, pass}, bits, i0, i1, cnt);
+  sort_move<W>(SortMemory{p, pass}, bits, i0, i1, cnt, base);
 }
 
 // ---------------------------------------------------------------------------

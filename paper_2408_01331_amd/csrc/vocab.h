@@ -31,8 +31,8 @@ struct EmbedProb {
   uint32_t* table;                // counts [sort blocks][digits]
   float* part;                    // [chunks][2][d]: of the run that comes in, of the one that goes on
 };
-// Up to SORT_ONE tokens one workgroup sorts in one launch, where many need two a digit: 1000 tokens into 50000 rows 10 us (17),
-// 5003 into 10007 19.6 (21.6), 8192 into 32768 28.9 (23).
+// Up to SORT_ONE tokens one workgroup sorts in one launch, from LDS to LDS, where many need two launches a digit: 1000 tokens into
+// 50000 rows 10 us (17), 5003 into 10007 16.5 (21.6), 6144 into 32768 19 (8192 by many 23).
 constexpr int SORT_ONE = 6144;
 constexpr int SORT_BLOCKS = 256;   // workgroups of the others at most
 constexpr int SORT_BITS = 11;      // bits of a digit at most (one workgroup: 9)
