@@ -13,8 +13,8 @@
 // fp32 (and are split there) where few tiles read them: they are read once, as they are.
 // Where many do, their terms are laid out first, and load directly.
 //
-// Bound by the matrix units and the power they draw: in bf16 the 256 x 256 tiles reach 1.20 to
-// 1.25 PFLOP/s over a piece of 8192 x 2048 x 32768 (64 to 68 % of the cycles multiply, at the clock that
+// Bound by the matrix units and the power they draw: in bf16 the 256 x 256 tiles reach 1.1 to
+// 1.25 PFLOP/s over a piece of 8192 x 2048 x 32768 (56 to 67 % of the cycles multiply, at the clock that
 // this leaves), 1.30 without an epilogue; a large library product 1.2 to 1.6 by its layout. Per
 // k of a tile BM + BN values are read for BM BN products, so a workgroup owns as large a tile
 // as LDS holds two stages of: with k-blocks of 64, 256 x 256 1.30 PFLOP/s, 128 x 128 by two a CU
