@@ -268,6 +268,19 @@ def test_terms_laid_out(ops):
     R.near(dw, g.t() @ X, h.norm_tol(rows), "dw")
 
 
+def test_few_tiles_of_a_long_width(ops):
+    """fp32 in few workgroups, from terms laid out (tiles of their own); the losses' bits are those of a larger call."""
+    rows, width, vocab = 1300, 3001, 700
+    x, w, targets = problem(rows, width, vocab, F32, left_out=0.2)
+    loss, lse = ops.vocab_loss(x, w, targets)
+    for s in (slice(0, 40), slice(1000, 1130)):
+        n = s.stop - s.start
+        for backward in (0, 1):
+            assert ops._head_workspace(0, n, width, vocab, backward) > 768 * 3008 * 6
+        a = check_loss(ops, x[s], w, targets[s], rand(5, (n,), std=1.0 / n))
+        assert torch.equal(a[0], loss[s]) and torch.equal(a[1], lse[s])
+
+
 @pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
 def test_far_weights(ops, dtype):
     """Rows of the weights and of their gradient beyond 2^31 elements, at the largest stride that is taken."""
