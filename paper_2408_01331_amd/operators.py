@@ -376,8 +376,12 @@ def _indices(x, name, dev, shape=None):
     return _INDEX[x.dtype], x if x.is_contiguous() else x.contiguous()
 
 
-def _table(x, name, shape=None):
+def _table(x, name):
     """(rows, width, row stride) of a tensor [rows, width] with a dense last axis."""
+    if x.dim() == 2 and x.is_contiguous():
+        rows, width = x.shape
+        if rows and width:
+            return rows, width, width
     _require(x.dim() == 2 and x.shape[0] >= 1 and x.shape[1] >= 1, f"{name} must have shape [vocab, width], not {tuple(x.shape)}")
     _dense(x, name)
     rows, width = x.shape
