@@ -268,6 +268,20 @@ def test_terms_laid_out(ops):
     R.near(dw, g.t() @ X, h.norm_tol(rows), "dw")
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+def test_a_row_alone_and_in_batches(ops, dtype):
+    """A row's loss has the same bits in calls of one row and of thousands, from weights at any alignment."""
+    rows, width, vocab = 3000, 520, 5000
+    x, w, targets = problem(rows, width, vocab, dtype, left_out=0.1)
+    targets[:1] = 77
+    loss, lse = ops.vocab_loss(x, w, targets)
+    apart = torch.cat([w, w[:, :3]], 1)[:, :width]
+    for weights in (w, apart):
+        for n in (1, 64, 130, 700, 3000):
+            l2, s2 = ops.vocab_loss(x[:n], weights, targets[:n])
+            assert torch.equal(l2, loss[:n]) and torch.equal(s2, lse[:n])
+
+
 def test_few_tiles_of_a_long_width(ops):
     """fp32 in few workgroups, from terms laid out (tiles of their own); the losses' bits are those of a larger call."""
     rows, width, vocab = 1300, 3001, 700
