@@ -416,7 +416,8 @@ template <HeadKind KIND> void head_launch(const HeadPlan& plan, bool direct, Hea
 
 // A product's time on tiles of a kind, in us: rounds of the workgroups that run at once, each with its blocks and what it
 // takes beside them (the first loads, the epilogue). A last round of at most one workgroup a CU takes less than one of two.
-// (Measured, all columns in cache: a block of 256 CUs of one, and of two.)
+// (A block's times: measured with one workgroup on each of up to 256 CUs, half of them where one fills a CU, and with all
+// slots taken; operands in the caches.)
 struct HeadTime {
   int bm, bn, slots, kb;
   double lone, block, rest;
@@ -458,7 +459,7 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool d
   p.ldd = up(width, HEAD_BM);
   const int64_t mv = up(vocab, HEAD_BM);
   // the products with the weights on kinds [first, end) of tiles; their time. (fp32 weights are split by every tile that
-  // reads them, or once: 4 bytes read and 6 written a value. 2048 x 1024 x 32768: 3.46 ms with all splitting, 2.83 so;
+  // reads them, or once: 4 bytes read and 6 written a value, at 4.5 TB/s. 2048 x 1024 x 32768: 3.46 ms with all splitting, 2.83 so;
   // 64 x 1024 x 131072: 170 us with all splitting, of which the layout alone would take 300.)
   auto with = [&](HeadPlan& q, int first, int end) {
     double us = 0;
