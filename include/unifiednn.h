@@ -632,7 +632,7 @@ typedef struct {
   int64_t lddy;
   float scale;
   int64_t padding;
-  void* dweight;             /* [vocab][width], overlaps nothing else */
+  void* dweight;             /* [vocab][width], overlaps nothing else (not checked) */
   int64_t lddw;
   int32_t accumulate;
   void* workspace;
@@ -671,7 +671,7 @@ un_status un_vocab_loss(const un_vocab_loss_args* a, void* stream);
  *   dx = g weight (zeros in the rows that are left out),  dweight = g^T x,
  * summed in fp32 in a fixed order and rounded once; g itself enters the products as the
  * operands do (in bf16: rounded to it). accumulate != 0: dweight is added onto what is
- * there. dx and dweight must not overlap anything else. */
+ * there. dx and dweight must not overlap anything else (not checked). */
 typedef struct {
   int32_t type;              /* of x, weight, dx, dweight */
   int32_t width, vocab;

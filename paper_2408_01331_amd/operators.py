@@ -80,6 +80,37 @@ def _ptr(x):
     return None if x is None else x.data_ptr()
 
 
+def _span(x, rows=1, ld=0):
+    """x's memory as (address, rows, bytes from one row to the next, bytes of a row): a dense tensor, or one of `rows` rows, `ld`
+    elements apart and as wide as its last axis."""
+    size = x.element_size()
+    if ld:
+        return x.data_ptr(), rows, ld * size, x.shape[-1] * size
+    n = x.numel() * size
+    return x.data_ptr(), 1, n, n
+
+
+def _meet(a, b):
+    """Whether two such pieces of memory share a byte. a's rows do not overlap one another; b's may (a stride of 0)."""
+    (pa, na, la, wa), (pb, nb, lb, wb) = a, b
+    if not (na and nb and wa and wb) or pa + (na - 1) * la + wa <= pb or pb + (nb - 1) * lb + wb <= pa:
+        return False
+    if la == lb and wa <= (pb - pa) % la <= la - wb:  # b's rows lie between a's
+        return False
+    # the last of a's rows that begins before one of b's ends is the one that reaches furthest
+    starts = torch.arange(nb, device="cpu") * lb + pb
+    k = ((starts + (wb - 1 - pa)) // la).clamp(max=na - 1)
+    return bool(((k >= 0) & (k * la + (pa + wa) > starts)).any())
+
+
+def _apart(out, ld, **inputs):
+    """`out` [rows, width], which is written while the inputs (their memory, as _span has it) are still read, overlaps none."""
+    a = _span(out, out.shape[0], ld)
+    for name, b in inputs.items():
+        if _meet(a, b):
+            raise ValueError(f"out overlaps {name}")
+
+
 def _call(fn, args, dev, plan=None):
     """fn on torch's current stream of GPU `dev`. (The default stream has no device of its own: it is the current one's.)"""
     if _current_device() != dev:
@@ -415,8 +446,8 @@ def _embed_workspace(tokens, vocab, width):
 def embedding_backward(dy, tokens, vocab, scale=1.0, padding=None, out=None):
     """The gradient at embedding's weight, [vocab, width] in dy's type, from the
     gradient dy at its output. Rows that no token names are zeros. out: a tensor of
-    that shape and type (its rows may be apart) that overlaps no input, onto which the
-    gradient is added instead, and which is returned. Tokens equal to `padding` have no
+    that shape and type (its rows may be apart) that overlaps no input (refused), onto which
+    the gradient is added instead, and which is returned. Tokens equal to `padding` have no
     gradient."""
     t, dev = _check_type(dy, "dy")
     bits, ids = _indices(tokens, "tokens", dev)
@@ -428,6 +459,7 @@ def embedding_backward(dy, tokens, vocab, scale=1.0, padding=None, out=None):
     if out is not None:
         _like(out, "out", torch.Size((vocab, width)), dy.dtype, dev)
         _, _, lddw = _table(out, "out")
+        _apart(out, lddw, dy=_span(dyv, ids.numel(), lddy), tokens=_span(ids))
     _unrecorded(dy, out)
     need = _embed_workspace(ids.numel(), vocab, width)
     given = out is not None
@@ -466,8 +498,9 @@ def _head(x, weight):
     return t, dev, x.shape[:-1], (rows, xv.data_ptr(), ldx, weight.data_ptr(), ldw), (vocab, width), xv
 
 
-def _head_out(weight, lead, dloss, out, dev):
-    """(dloss's address, its stride, dweight's row stride, what keeps dloss alive) of a backward call."""
+def _head_out(xv, weight, lead, dloss, out, dev, args, **others):
+    """(dloss's address, its stride, dweight's row stride, what keeps dloss alive) of a backward call. args: as _head returned
+    them; others: tensors that `out` must not overlap, either."""
     step = 1
     if isinstance(dloss, torch.Tensor) and dloss.dim() == 0:
         step = 0
@@ -487,6 +520,9 @@ def _head_out(weight, lead, dloss, out, dev):
     if out is not None:
         _like(out, "out", weight.shape, weight.dtype, dev)
         _, _, lddw = _table(out, "out")
+        rows, _, ldx, _, ldw = args
+        _apart(out, lddw, x=_span(xv, rows, ldx), weight=_span(weight, weight.shape[0], ldw),
+               dloss=(dloss.data_ptr(), rows, 4 * step, 4), **{k: _span(v) for k, v in others.items()})
     return dloss.data_ptr(), step, lddw, dloss
 
 
@@ -512,11 +548,12 @@ def vocab_loss_backward(x, weight, targets, lse, dloss, ignore=-100, out=None):
     """(dx, dweight) of vocab_loss from the gradient dloss at the losses (float32, of
     their shape, or one number's tensor for all rows). lse: as vocab_loss returned it.
     out: a tensor of weight's shape and type (its rows may be apart) that overlaps no
-    input, onto which dweight is added instead, and which is returned."""
-    t, dev, lead, (rows, xp, ldx, wp, ldw), (vocab, width), xv = _head(x, weight)
+    input (refused), onto which dweight is added instead, and which is returned."""
+    t, dev, lead, args, (vocab, width), xv = _head(x, weight)
+    rows, xp, ldx, wp, ldw = args
     bits, targets = _indices(targets, "targets", dev, lead)
     _flat(lse, "lse", lead, _F32, dev)
-    dlp, step, lddw, dloss = _head_out(weight, lead, dloss, out, dev)
+    dlp, step, lddw, dloss = _head_out(xv, weight, lead, dloss, out, dev, args, targets=targets, lse=lse)
     _unrecorded(x, weight, lse, dloss, out)
     given = out is not None
     dx = x.new_empty(x.shape)
@@ -565,11 +602,12 @@ def distill_loss(x, weight, ids, logits, temperature=1.0):
 def distill_loss_backward(x, weight, ids, logits, lse, picked, dloss, temperature=1.0, out=None):
     """(dx, dweight) of distill_loss (the teacher gets no gradient). lse, picked: as
     distill_loss returned them; dloss, out: as vocab_loss_backward's."""
-    t, dev, lead, (rows, xp, ldx, wp, ldw), (vocab, width), xv = _head(x, weight)
+    t, dev, lead, args, (vocab, width), xv = _head(x, weight)
+    rows, xp, ldx, wp, ldw = args
     bits, ids, lt, logits = _teacher(ids, logits, lead, dev)
     _flat(lse, "lse", lead, _F32, dev)
     _flat(picked, "picked", ids.shape, _F32, dev)
-    dlp, step, lddw, dloss = _head_out(weight, lead, dloss, out, dev)
+    dlp, step, lddw, dloss = _head_out(xv, weight, lead, dloss, out, dev, args, ids=ids, logits=logits, lse=lse, picked=picked)
     _unrecorded(x, weight, logits, lse, picked, dloss, out)
     given = out is not None
     dx = x.new_empty(x.shape)
