@@ -51,7 +51,7 @@ constexpr uint32_t HEAD_OUT = 0x80000000u;   // an offset past every descriptor'
 // out, so that the compiler's own waits do not serialise the stages: the kernel waits
 // by count. It has no output register that could be reused too early.)
 __device__ __forceinline__ void lds_load(uint32_t lds, uint32_t voff, u32x4 rsrc) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "m0", "memory");
 }
 template <int N> __device__ __forceinline__ void wait_loads() {
   static_assert(N < 64, "the counter has 6 bits");
