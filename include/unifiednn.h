@@ -617,8 +617,9 @@ typedef struct {
 un_status un_embedding(const un_embedding_args* a, void* stream);
 
 /* Its gradient: dweight[v] = scale * (the sum of dy_n over the n with token_n = v, in
- * fp32 in a fixed order, which depends on `tokens` alone), rounded once; rows that no
- * token names are zeros. accumulate != 0: added onto dweight instead, whose other rows
+ * fp32 in a fixed order: ascending n, grouped by where v's run lies among all sorted
+ * tokens, so the same tokens give the same bits, whatever the other rows of dy hold, and
+ * others may group v's terms otherwise), rounded once; rows that no token names are zeros. accumulate != 0: added onto dweight instead, whose other rows
  * stay as they are. Tokens equal to `padding` (negative: none) and tokens outside [0,
  * vocab) have no gradient, and their rows of dy are not used. workspace: as many
  * bytes as un_embedding_workspace says. */

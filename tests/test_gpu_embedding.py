@@ -133,6 +133,24 @@ def test_order_and_repeats(ops):
     assert not torch.equal(t, perm[t])
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [700, 30000])
+def test_other_tokens_rows(ops, dtype, n):
+    """With the same tokens a row of the table has the same bits, whatever the other tokens' rows of dy hold; with others its
+    terms are the same and may be grouped otherwise."""
+    t = tokens_of(1, n, 2000, "text")
+    dy = rand(2, (n, 64), dtype)
+    first = ops.embedding_backward(dy, t, 2000)
+    for watched in (t < 3, t % 2 == 1, t == t[n // 2]):
+        other = torch.where(watched[:, None], dy, rand(3, (n, 64), dtype) * 100)
+        other[torch.nonzero(~watched)[0, 0]] = float("nan")
+        rows = torch.unique(t[watched])
+        assert torch.equal(ops.embedding_backward(other, t, 2000)[rows], first[rows])
+    moved = torch.where(t == 0, 1999, t)  # every run lies elsewhere
+    want, bound = R.embedding_backward(dy, moved, 2000, 1.0, None, None)
+    R.close(ops.embedding_backward(dy, moved, 2000), want, bound + (R.half_step(dtype) * (want.abs() + bound) if dtype != F32 else 0), "dw")
+
+
 def test_far_rows(ops):
     """Rows beyond 2^31 elements of a table."""
     vocab, width = 600_000, 4096
