@@ -717,7 +717,7 @@ typedef struct {
   int32_t logits_type;       /* un_type */
   const void* ids;           /* [rows][top] */
   const void* logits;        /* [rows][top] */
-  float temperature;         /* finite, > 0 */
+  float temperature;         /* in [2^-60, 2^60] */
   float *loss, *lse;         /* [rows] */
   float* picked;             /* [rows][top] */
   void* workspace;

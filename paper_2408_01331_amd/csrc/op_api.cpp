@@ -470,6 +470,8 @@ template <typename A> un_status head_teacher(const char* F, const A* a, HeadCall
   if (a->top > HEAD_MAX_TOP) return bad(F, "more than 128 entries are not supported", UN_ERR_UNSUPPORTED);
   if (!type_ok(a->logits_type)) return bad(F, "unknown type of the logits");
   if (!std::isfinite(a->temperature) || !(a->temperature > 0.f)) return bad(F, "temperature must be finite and > 0");
+  // (its square is the loss's factor, and it divides z: neither may leave fp32's normal range)
+  if (a->temperature < 0x1p-60f || a->temperature > 0x1p60f) return bad(F, "a temperature outside [2^-60, 2^60] is not supported", UN_ERR_UNSUPPORTED);
   if (a->rows > 0 && (!a->ids || !a->logits || !a->picked)) return bad(F, "ids, logits or picked is NULL");
   c->top = a->top;
   c->ids = a->ids;

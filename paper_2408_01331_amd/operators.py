@@ -582,7 +582,8 @@ def distill_loss(x, weight, ids, logits, temperature=1.0):
     """(loss, lse, picked): temperature^2 KL(p, q) per row, of a teacher's p = softmax(
     logits / temperature) over its `top` entries and the student's q = softmax(x @
     weight.T / temperature) over the vocabulary. x, weight: as vocab_loss's; ids: int32
-    or int64 [..., top], logits: float32 or bfloat16 [..., top], top up to 128. Entries
+    or int64 [..., top], logits: float32 or bfloat16 [..., top], top up to 128;
+    temperature: a number in [2^-60, 2^60]. Entries
     with an id outside [0, vocab) or a logit of -inf do not count; a row without
     entries is left out: zeros. lse and picked (float32 [..., top]) are what
     distill_loss_backward needs."""

@@ -186,6 +186,16 @@ def test_head_refused_more(fn, change, want, text):
     refused(fn, struct, base, change, want, text)
 
 
+@pytest.mark.parametrize("fn", ["un_distill_loss", "un_distill_loss_backward"])
+def test_temperatures_whose_square_is_lost(fn):
+    """T^2 is 0 or infinite in 32 bits: the loss would be 0, infinite or NaN whatever the student has learned."""
+    struct, base = CALLS[fn]
+    for T in (1e-25, 2.0 ** -61, 2.0 ** 61, 1e20, 3e38, 1e-40):
+        refused(fn, struct, base, dict(temperature=T), U.UN_ERR_UNSUPPORTED, "temperature")
+    for T in (2.0 ** -60, 2.0 ** 60):  # the ends are taken: the next check's refusal
+        refused(fn, struct, base, dict(temperature=T, ids=None), 1, "NULL")
+
+
 def test_head_without_rows_or_arguments():
     L = U.lib()
     for fn, (struct, base) in CALLS.items():
