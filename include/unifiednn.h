@@ -601,12 +601,14 @@ un_status un_gated_scan_backward(const un_gated_scan_grad_args* a, void* stream)
 un_status un_gated_scan_sizes(int32_t batch, int32_t tokens, int32_t width, size_t* states, size_t* workspace_bytes);
 
 /* Embedding lookup: y_n = scale weight[token_n], rounded once, for `tokens` tokens and
- * a table of vocab rows. A token outside [0, vocab) gets a row of zeros. */
+ * a table of vocab rows. A token outside [0, vocab) gets a row of zeros. Of this and the
+ * gradient a launch holds tokens * ceil(width / 256) + vocab <= 2^26 - 8; more is refused
+ * (UN_ERR_UNSUPPORTED). */
 typedef struct {
   int32_t type;              /* un_type of weight, y */
   int32_t width, vocab;      /* >= 1; width up to 2^24 */
   int32_t index_bits;        /* of a token: 32 or 64 (signed) */
-  int64_t tokens;            /* up to 2^30 */
+  int64_t tokens;
   const void* ids;           /* [tokens] */
   const void* weight;        /* [vocab][width] */
   int64_t ldw;

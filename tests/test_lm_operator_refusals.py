@@ -117,6 +117,19 @@ def test_embedding_workspace():
     assert U.lib().un_embedding_workspace(100, 10, 64, None) == U.UN_ERR_INVALID
 
 
+@pytest.mark.parametrize("tokens,vocab,width", [((1 << 26) - 18, 10, 256), ((1 << 25) - 9, 10, 257), (1, (1 << 26) - 9, 1),
+                                               ((1 << 18) - 1, 262391, 65280)])
+def test_embedding_at_the_limit(tokens, vocab, width):
+    """tokens * ceil(width / 256) + vocab = 2^26 - 8 is the most that a launch holds."""
+    assert tokens * -(-width // 256) + vocab == (1 << 26) - 8
+    b = ctypes.c_size_t()
+    assert U.lib().un_embedding_workspace(tokens, vocab, width, ctypes.byref(b)) == U.UN_OK and b.value > 0
+    for fn, struct, base in (("un_embedding", "un_embedding_args", EMBED), ("un_embedding_backward", "un_embedding_grad_args", EMBEDG)):
+        size = dict(tokens=tokens, vocab=vocab, width=width)
+        refused(fn, struct, base, {**size, "ids": None}, 1, "NULL")
+        refused(fn, struct, base, {**size, "vocab": vocab + 1}, U.UN_ERR_UNSUPPORTED, "too many")
+
+
 def test_embedding_python(monkeypatch):
     from paper_2408_01331_amd import operators as ops
     w, t = torch.zeros(5, 8), torch.zeros(3, dtype=torch.int64)
