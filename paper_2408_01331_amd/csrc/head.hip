@@ -459,8 +459,11 @@ HeadPlan head_plan(bool bf16, int64_t rows, int32_t width, int32_t vocab, bool d
   p.ldd = up(width, HEAD_BM);
   const int64_t mv = up(vocab, HEAD_BM);
   // the products with the weights on kinds [first, end) of tiles; their time. (fp32 weights are split by every tile that
-  // reads them, or once: 4 bytes read and 6 written a value, at 4.5 TB/s. 2048 x 1024 x 32768: 3.46 ms with all splitting, 2.83 so;
-  // 64 x 1024 x 131072: 170 us with all splitting, of which the layout alone would take 300.)
+  // reads them, or once: 4 bytes read and 6 written a value, at 4.5 TB/s. Forward and backward of 2048 x 1024 x 32768: 3.15 ms with all
+  // splitting, 2.73 so; forward of 64 x 1024 x 131072: 150 us with all splitting, 451 with the terms laid out.)
+  // (k of HEAD_STATS and HEAD_GRAD is not cut, so few tiles of a long width are a chain of blocks: 1 x 4096 x 500 in fp32 107 us, where
+  // products of the library and elementary operations take 57. Parts of a length that follows from the width alone, summed apart
+  // and joined in order by every kind of tiles, would keep a row's bits; they are not built.)
   auto with = [&](HeadPlan& q, int first, int end) {
     double us = 0;
     q.piece = mv;

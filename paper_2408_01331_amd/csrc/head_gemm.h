@@ -20,8 +20,9 @@
 // as LDS holds two stages of: with k-blocks of 64, 256 x 256 1.30 PFLOP/s, 128 x 128 by two a CU
 // 1.11, 128 x 64 0.9 (and 256 x 128 with k-blocks of 32 by two a CU 1.09 to 1.2). Raised wave
 // priority around the products, a transposed grid of waves and loads spread wider changed
-// these by less than 2 %. In fp32 (six products) 256 x 128 tiles reach 195 TFLOP/s of fp32,
-// 1.17 P of bf16, against 154 of the library's.
+// these by less than 2 %. In fp32 (six products) the 256 x 128 tiles reach 217 to 223 TFLOP/s of
+// fp32 over 2048 x 1024 x 32768 (1.3 P of bf16; 58 to 70 % of the cycles multiply), 191 where g is
+// formed; the library's products of these sizes take 142 to 146.
 //
 // LDS images, in 16-byte chunks. An operand with k innermost: rows of KB / 8 chunks,
 // chunk c of row r at c ^ (r / 4 % 4) (KB = 32) or c ^ (r / 2 % 8) (64), so the 16 rows
