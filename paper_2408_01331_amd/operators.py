@@ -80,18 +80,9 @@ def _ptr(x):
     return None if x is None else x.data_ptr()
 
 
-def _span(x, rows=1, ld=0):
-    """x's memory as (address, rows, bytes from one row to the next, bytes of a row): a dense tensor, or one of `rows` rows, `ld`
-    elements apart and as wide as its last axis."""
-    size = x.element_size()
-    if ld:
-        return x.data_ptr(), rows, ld * size, x.shape[-1] * size
-    n = x.numel() * size
-    return x.data_ptr(), 1, n, n
-
-
 def _meet(a, b):
-    """Whether two such pieces of memory share a byte. a's rows do not overlap one another; b's may (a stride of 0)."""
+    """Whether two pieces of memory, (address, rows, bytes from one row to the next, bytes of a row) each, share a byte. a's rows do
+    not overlap one another; b's may (a stride of 0)."""
     (pa, na, la, wa), (pb, nb, lb, wb) = a, b
     if not (na and nb and wa and wb) or pa + (na - 1) * la + wa <= pb or pb + (nb - 1) * lb + wb <= pa:
         return False
@@ -103,11 +94,14 @@ def _meet(a, b):
     return bool(((k >= 0) & (k * la + (pa + wa) > starts)).any())
 
 
-def _apart(out, ld, **inputs):
-    """`out` [rows, width], which is written while the inputs (their memory, as _span has it) are still read, overlaps none."""
-    a = _span(out, out.shape[0], ld)
-    for name, b in inputs.items():
-        if _meet(a, b):
+def _apart(out, ld, size, *inputs):
+    """`out` [rows, width] of values of `size` bytes, which is written while the inputs are still read, overlaps none of them: name
+    and memory, as _meet has it, of each."""
+    rows, width = out.shape
+    lo = out.data_ptr()
+    hi = lo + ((rows - 1) * ld + width) * size
+    for name, *b in inputs:
+        if b[0] < hi and b[0] + (b[1] - 1) * b[2] + b[3] > lo and _meet((lo, rows, ld * size, width * size), b):
             raise ValueError(f"out overlaps {name}")
 
 
@@ -459,7 +453,8 @@ def embedding_backward(dy, tokens, vocab, scale=1.0, padding=None, out=None):
     if out is not None:
         _like(out, "out", torch.Size((vocab, width)), dy.dtype, dev)
         _, _, lddw = _table(out, "out")
-        _apart(out, lddw, dy=_span(dyv, ids.numel(), lddy), tokens=_span(ids))
+        n, size = ids.numel(), 2 if t else 4
+        _apart(out, lddw, size, ("dy", dyv.data_ptr(), n, lddy * size, width * size), ("tokens", ids.data_ptr(), 1, 0, n * bits // 8))
     _unrecorded(dy, out)
     need = _embed_workspace(ids.numel(), vocab, width)
     given = out is not None
@@ -498,9 +493,9 @@ def _head(x, weight):
     return t, dev, x.shape[:-1], (rows, xv.data_ptr(), ldx, weight.data_ptr(), ldw), (vocab, width), xv
 
 
-def _head_out(xv, weight, lead, dloss, out, dev, args, **others):
+def _head_out(weight, lead, dloss, out, t, dev, args, *others):
     """(dloss's address, its stride, dweight's row stride, what keeps dloss alive) of a backward call. args: as _head returned
-    them; others: tensors that `out` must not overlap, either."""
+    them; others: name, address and bytes of the dense tensors that `out` must not overlap, either."""
     step = 1
     if isinstance(dloss, torch.Tensor) and dloss.dim() == 0:
         step = 0
@@ -520,9 +515,10 @@ def _head_out(xv, weight, lead, dloss, out, dev, args, **others):
     if out is not None:
         _like(out, "out", weight.shape, weight.dtype, dev)
         _, _, lddw = _table(out, "out")
-        rows, _, ldx, _, ldw = args
-        _apart(out, lddw, x=_span(xv, rows, ldx), weight=_span(weight, weight.shape[0], ldw),
-               dloss=(dloss.data_ptr(), rows, 4 * step, 4), **{k: _span(v) for k, v in others.items()})
+        rows, xp, ldx, wp, ldw = args
+        size, width = 2 if t else 4, out.shape[1]
+        _apart(out, lddw, size, ("x", xp, rows, ldx * size, width * size), ("weight", wp, out.shape[0], ldw * size, width * size),
+               ("dloss", dloss.data_ptr(), rows, 4 * step, 4), *((name, p, 1, 0, n) for name, p, n in others))
     return dloss.data_ptr(), step, lddw, dloss
 
 
@@ -553,7 +549,8 @@ def vocab_loss_backward(x, weight, targets, lse, dloss, ignore=-100, out=None):
     rows, xp, ldx, wp, ldw = args
     bits, targets = _indices(targets, "targets", dev, lead)
     _flat(lse, "lse", lead, _F32, dev)
-    dlp, step, lddw, dloss = _head_out(xv, weight, lead, dloss, out, dev, args, targets=targets, lse=lse)
+    dlp, step, lddw, dloss = _head_out(weight, lead, dloss, out, t, dev, args, ("targets", targets.data_ptr(), rows * bits // 8),
+                                        ("lse", lse.data_ptr(), rows * 4))
     _unrecorded(x, weight, lse, dloss, out)
     given = out is not None
     dx = x.new_empty(x.shape)
@@ -608,7 +605,9 @@ def distill_loss_backward(x, weight, ids, logits, lse, picked, dloss, temperatur
     bits, ids, lt, logits = _teacher(ids, logits, lead, dev)
     _flat(lse, "lse", lead, _F32, dev)
     _flat(picked, "picked", ids.shape, _F32, dev)
-    dlp, step, lddw, dloss = _head_out(xv, weight, lead, dloss, out, dev, args, ids=ids, logits=logits, lse=lse, picked=picked)
+    dlp, step, lddw, dloss = _head_out(weight, lead, dloss, out, t, dev, args, ("ids", ids.data_ptr(), ids.numel() * bits // 8),
+                                        ("logits", logits.data_ptr(), ids.numel() * (2 if lt else 4)), ("lse", lse.data_ptr(), rows * 4),
+                                        ("picked", picked.data_ptr(), ids.numel() * 4))
     _unrecorded(x, weight, logits, lse, picked, dloss, out)
     given = out is not None
     dx = x.new_empty(x.shape)

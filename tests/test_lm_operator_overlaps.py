@@ -30,16 +30,15 @@ def test_pieces_of_memory(ops):
     assert 2000 < met < 18000
 
 
-def test_memory_of_tensors(ops):
-    x = torch.zeros(6, 10)
-    at = x.data_ptr()
-    assert ops._span(x) == (at, 1, 240, 240) and ops._span(x, 6, 10) == (at, 6, 40, 40)
-    assert ops._span(x[1:, 2:5], 5, 10) == (at + 48, 5, 40, 12)
-    assert ops._span(x.to(torch.bfloat16)[:0])[1:] == (1, 0, 0)
-    halves = torch.zeros(7, 16)
-    ops._apart(halves[:, :8], 16, weight=ops._span(halves[:, 8:], 7, 16))
-    with pytest.raises(ValueError, match="out overlaps weight"):
-        ops._apart(halves[:, :8], 16, x=ops._span(x), weight=ops._span(halves[:, 7:], 7, 16))
+def test_rows_of_a_tensor(ops):
+    halves = torch.zeros(7, 16, dtype=torch.bfloat16)
+    at = halves.data_ptr()
+    for size, scale in ((2, 1), (4, 2)):  # (of fp32 the same rows are half as many values)
+        out = halves[:, :8] if size == 2 else halves.view(torch.float32)[:, :4]
+        ops._apart(out, 16 // scale, size, ("tokens", at + 300, 1, 0, 9), ("weight", at + 16, 7, 32, 16), ("lse", at, 1, 0, 0), ("x", at, 0, 32, 16))
+        for b in ((at + 14, 7, 32, 16), (at + 16, 7, 32, 17), (at + 6 * 32 + 15, 1, 0, 4), (at - 3, 1, 0, 4)):
+            with pytest.raises(ValueError, match="out overlaps weight"):
+                ops._apart(out, 16 // scale, size, ("x", at + 16, 7, 32, 16), ("weight", *b))
 
 
 def test_refused(ops, monkeypatch):
